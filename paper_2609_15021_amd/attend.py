@@ -1,0 +1,270 @@
+"""Python binding of ``include/kvx_attend.h``: operators on a replica's paged KV cache (argument marshalling only).
+
+Every step runs in the HIP library that ``kvx`` binds (``libkvx.so``); caches are ``kvx.Cache`` handles, errors
+``kvx.KvError``, streams as for ``kvx.kv_store``.  The names are the C ABI's.
+
+A batch of sequences is ``tables`` (int32 [B][pages]: block tables), ``lens`` (int32 [B]: tokens in the cache, the new
+ones among them) and ``starts`` (int32 [B + 1]: where each sequence's new tokens start among all; None: one each).  All
+three are device tensors; ``max_q`` and ``max_len`` are the host's bounds of new tokens and tokens per sequence, by
+default (and at most) what the shapes allow.  Tight bounds size the launches better; numbers beyond them are refused on the device
+(``kv_attend_async_error``).
+"""
+from __future__ import annotations
+
+import ctypes
+
+import torch
+
+from .kvx import Cache, KvCache, _in_use_on, _lib, _raise
+
+KV_DTYPE_BF16 = 1
+KV_DTYPE_F16 = 2
+KV_DTYPE_E4M3 = 3
+KV_ASYNC_BAD_BATCH = 2
+
+_DTYPES = {torch.bfloat16: KV_DTYPE_BF16, torch.float16: KV_DTYPE_F16, torch.float8_e4m3fn: KV_DTYPE_E4M3}
+
+EXPORTS = ("kv_append", "kv_attend", "kv_attend_workspace", "kv_keep", "kv_compact", "kv_attend_async_error")
+
+
+class KvRows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+                ("heads", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class KvBatch(ctypes.Structure):
+    _fields_ = [("num_seqs", ctypes.c_int32), ("max_queries", ctypes.c_int32), ("num_queries", ctypes.c_int32),
+                ("max_len", ctypes.c_int32), ("table_len", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("table_stride", ctypes.c_int64), ("block_tables", ctypes.c_void_p), ("lens", ctypes.c_void_p),
+                ("starts", ctypes.c_void_p)]
+
+
+class KvAttendOptions(ctypes.Structure):
+    _fields_ = [("cache_dtype", ctypes.c_int32), ("window", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("softcap", ctypes.c_float), ("k_scale", ctypes.c_float), ("v_scale", ctypes.c_float),
+                ("slopes", ctypes.c_void_p), ("weights_in", ctypes.c_void_p), ("weights_out", ctypes.c_void_p),
+                ("weights_seq_stride", ctypes.c_int64), ("weights_head_stride", ctypes.c_int64)]
+
+
+def _declare(lib):
+    P, i32, i64, f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
+    cache, batch, rows = ctypes.POINTER(KvCache), ctypes.POINTER(KvBatch), ctypes.POINTER(KvRows)
+    options = ctypes.POINTER(KvAttendOptions)
+    for name, args, res in (
+            ("kv_append", [cache, i32, batch, rows, rows, i32, f32, f32, P], i32),
+            ("kv_attend", [cache, i32, batch, options, rows, rows, P, P, i64, P], i32),
+            ("kv_attend_workspace", [cache, batch, options, rows], i64),
+            ("kv_keep", [P, i64, i64, P, i32, i32, i32, i32, i32, i32, P, P, P, P], i32),
+            ("kv_compact", [cache, i32, i32, P, i64, i32, P, i32, i32, P, P, i64, i32, P], i32),
+            ("kv_attend_async_error", [ctypes.c_int], i32)):
+        fn = getattr(lib, name)
+        fn.argtypes, fn.restype = args, res
+
+
+_declare(_lib)
+
+
+def _ints(t, name: str, dims: int, rows=None):
+    """A device tensor of int32 whose last dimension is dense."""
+    if not isinstance(t, torch.Tensor) or t.dtype != torch.int32 or not t.is_cuda or t.dim() != dims or \
+            (t.numel() and t.stride(-1) != 1):
+        raise TypeError(f"{name} must be a {dims}-dimensional int32 device tensor with a dense last dimension")
+    if rows is not None and t.shape[0] != rows:
+        raise ValueError(f"{name} has {t.shape[0]} rows; {rows} are needed")
+    return t
+
+
+def _rows(t, name: str, head_dim: int) -> KvRows:
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dim() != 3 or t.dtype not in (torch.bfloat16, torch.float16):
+        raise TypeError(f"{name} must be a [tokens][heads][D] device tensor of bfloat16 or float16")
+    if t.shape[2] != head_dim or (t.numel() and t.stride(2) != 1):
+        raise ValueError(f"{name}: rows of {t.shape[2]} elements {t.stride(2)} apart; dense rows of {head_dim} are needed")
+    return KvRows(t.data_ptr(), t.stride(0), t.stride(1), t.shape[1], _DTYPES[t.dtype])
+
+
+def _batch(cache: Cache, tables, lens, starts, tokens: int, max_q, max_len) -> KvBatch:
+    tables = _ints(tables, "tables", 2)
+    B, pages = tables.shape
+    _ints(lens, "lens", 1, B)
+    if starts is None:
+        if tokens != B:
+            raise ValueError(f"{tokens} new tokens for {B} sequences of one each: starts is needed")
+        max_q = 1
+    else:
+        _ints(starts, "starts", 1, B + 1)
+        max_q = max(1, tokens if max_q is None else int(max_q))
+    most = min(pages * cache.layout.block_size, 2**31 - 1)
+    return KvBatch(B, max_q, tokens, most if max_len is None else min(most, int(max_len)), pages, 0, tables.stride(0),
+                   tables.data_ptr(), lens.data_ptr(), None if starts is None else starts.data_ptr())
+
+
+def _cache_dtype(cache: Cache, dtype, rows) -> int:
+    """KV_DTYPE of the cache: ``dtype``, or by its element size the rows' type or e4m3."""
+    if dtype is None:
+        dtype = torch.float8_e4m3fn if cache.layout.elem_bytes == 1 else rows.dtype
+    if dtype not in _DTYPES:
+        raise TypeError(f"caches are bfloat16, float16 or float8_e4m3fn, not {dtype}")
+    return _DTYPES[dtype]
+
+
+def _stream(stream):
+    return torch.cuda.current_stream(torch.cuda.current_device()) if stream is None else stream
+
+
+def _handle(stream) -> int:
+    return stream.cuda_stream if isinstance(stream, torch.cuda.Stream) else int(stream)
+
+
+def _used(stream, *tensors) -> None:
+    for t in tensors:
+        if t is not None:
+            _in_use_on(t, stream)
+
+
+class _allocating:
+    """New tensors belong to the call's stream, which may be another than the current one."""
+
+    def __init__(self, stream, given):
+        self.context = None
+        if given is not None:
+            if not isinstance(stream, torch.cuda.Stream):
+                stream = torch.cuda.ExternalStream(int(stream))
+            self.context = torch.cuda.stream(stream)
+
+    def __enter__(self):
+        if self.context is not None:
+            self.context.__enter__()
+
+    def __exit__(self, *exc):
+        if self.context is not None:
+            self.context.__exit__(*exc)
+
+
+def kv_append(cache: Cache, layer: int, k, v, tables, lens, starts=None, *, max_q=None, max_len=None, dtype=None,
+              k_scale: float = 1.0, v_scale: float = 1.0, stream=None) -> None:
+    """Write the new tokens' rows ``k`` and ``v`` ([tokens][H][D], any token and head strides) into layer ``layer``.
+
+    ``dtype``: the cache's; by default that of ``k``, or float8_e4m3fn in a cache of 1-byte elements, where x is stored
+    as e4m3(x / scale).
+    """
+    D = cache.layout.head_dim
+    kr, vr = _rows(k, "k", D), _rows(v, "v", D)
+    if k.shape != v.shape:
+        raise ValueError(f"k and v differ in shape: {tuple(k.shape)} and {tuple(v.shape)}")
+    batch = _batch(cache, tables, lens, starts, k.shape[0], max_q, max_len)
+    s = _stream(stream)
+    _raise(_lib.kv_append(ctypes.byref(cache.struct), int(layer), ctypes.byref(batch), ctypes.byref(kr), ctypes.byref(vr),
+                          _cache_dtype(cache, dtype, k), float(k_scale), float(v_scale), _handle(s)))
+    _used(s, k, v, tables, lens, starts)
+
+
+def kv_attend(cache: Cache, layer: int, q, tables, lens, starts=None, *, max_q=None, max_len=None, dtype=None,
+              scale=None, softcap: float = 0.0, window: int = 0, slopes=None, k_scale: float = 1.0, v_scale: float = 1.0,
+              weights=None, prior=None, out=None, lse=None, stream=None):
+    """Attention of the new tokens' queries ``q`` ([tokens][query heads][D], any token and head strides) over layer
+    ``layer``; returns (out, lse).
+
+    ``weights`` (float32 [B][H][>= max_len]): receives ``prior`` (same shape and strides; None: 0) plus what each cached
+    token got in this call; ``prior=weights`` accumulates in place.  ``out`` (like ``q``) and ``lse`` (float32 [tokens]
+    [query heads]) are made if not given; rows that belong to no sequence are left as they were.
+    """
+    qr = _rows(q, "q", cache.layout.head_dim)
+    batch = _batch(cache, tables, lens, starts, q.shape[0], max_q, max_len)
+    options = KvAttendOptions(_cache_dtype(cache, dtype, q), int(window), 0.0 if scale is None else float(scale),
+                              float(softcap), float(k_scale), float(v_scale))
+    if slopes is not None:
+        if slopes.dtype != torch.float32 or not slopes.is_cuda or slopes.shape != (q.shape[1],) or \
+                not slopes.is_contiguous():
+            raise TypeError(f"slopes must be a contiguous float32 device tensor of {q.shape[1]} elements")
+        options.slopes = slopes.data_ptr()
+    if weights is not None:
+        shape = (tables.shape[0], cache.layout.num_kv_heads)
+        if weights.dtype != torch.float32 or not weights.is_cuda or weights.dim() != 3 or weights.shape[:2] != shape or \
+                (weights.numel() and weights.stride(2) != 1):
+            raise TypeError(f"weights must be a float32 device tensor of {shape} dense rows")
+        if max_len is None:
+            batch.max_len = min(batch.max_len, weights.shape[2])
+        elif weights.shape[2] < batch.max_len:
+            raise ValueError(f"weights of {weights.shape[2]} tokens for sequences of up to {batch.max_len}")
+        options.weights_out = weights.data_ptr()
+        options.weights_seq_stride, options.weights_head_stride = weights.stride(0), weights.stride(1)
+        if prior is not None:
+            if prior.dtype != torch.float32 or not prior.is_cuda or prior.shape != weights.shape or \
+                    prior.stride() != weights.stride():
+                raise TypeError("prior must have the type, shape and strides of weights")
+            options.weights_in = prior.data_ptr()
+    elif prior is not None:
+        raise ValueError("prior without weights")
+    heads = (q.shape[0], q.shape[1])
+    if out is not None and (out.dtype != q.dtype or out.shape != q.shape):
+        raise TypeError("out must have the type and shape of q")
+    if lse is not None and (lse.dtype != torch.float32 or lse.shape != heads or not lse.is_cuda or
+                            not lse.is_contiguous()):
+        raise TypeError(f"lse must be a contiguous float32 device tensor of {heads}")
+    need = _lib.kv_attend_workspace(ctypes.byref(cache.struct), ctypes.byref(batch), ctypes.byref(options),
+                                    ctypes.byref(qr))
+    if need < 0:
+        _raise(need)
+    s = _stream(stream)
+    with _allocating(s, stream):
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        if lse is None:
+            lse = torch.empty(heads, dtype=torch.float32, device=q.device)
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+    outr = _rows(out, "out", cache.layout.head_dim)
+    _raise(_lib.kv_attend(ctypes.byref(cache.struct), int(layer), ctypes.byref(batch), ctypes.byref(options),
+                          ctypes.byref(qr), ctypes.byref(outr), lse.data_ptr(),
+                          workspace.data_ptr() if need else None, need, _handle(s)))
+    _used(s, q, tables, lens, starts, slopes, weights, prior, out, lse)
+    return out, lse
+
+
+def kv_keep(weights, lens, budget: int, *, sinks: int = 0, recent: int = 0, max_len=None, stream=None):
+    """The tokens that each sequence keeps under ``budget``: its first ``sinks``, its last ``recent`` and the heaviest
+    others by ``weights`` (float32 [B][H or 1][tokens], dense rows).  Returns (keep int32 [B][H][budget], ascending and
+    then -1; kept_lens int32 [B]; kept_weights float32 like keep, then 0)."""
+    if not isinstance(weights, torch.Tensor) or weights.dtype != torch.float32 or not weights.is_cuda or \
+            weights.dim() != 3 or (weights.numel() and weights.stride(2) != 1):
+        raise TypeError("weights must be a [sequences][heads][tokens] float32 device tensor with dense rows")
+    B, H, L = weights.shape
+    _ints(lens, "lens", 1, B)
+    if max_len is not None and int(max_len) > L:
+        raise ValueError(f"weights of {L} tokens for sequences of up to {max_len}")
+    if budget < 1:
+        raise ValueError(f"budget must be positive (got {budget})")
+    s = _stream(stream)
+    with _allocating(s, stream):
+        keep = torch.empty((B, H, int(budget)), dtype=torch.int32, device=weights.device)
+        kept_lens = torch.empty(B, dtype=torch.int32, device=weights.device)
+        kept_weights = torch.empty((B, H, int(budget)), dtype=torch.float32, device=weights.device)
+    _raise(_lib.kv_keep(weights.data_ptr(), weights.stride(0), weights.stride(1), lens.data_ptr(), B, H,
+                        L if max_len is None else int(max_len), int(budget), int(sinks), int(recent), keep.data_ptr(),
+                        kept_lens.data_ptr(), kept_weights.data_ptr(), _handle(s)))
+    _used(s, weights, lens)
+    return keep, kept_lens, kept_weights
+
+
+def kv_compact(cache: Cache, layer: int, tables, keep, kept_lens, dst_tables, *, stream=None) -> None:
+    """Copy the kept tokens' rows of layer ``layer`` into the pages of ``dst_tables``: token ``keep[b][h][j]`` becomes
+    token j (``keep`` int32 [B][H or 1][budget], contiguous; ``kept_lens`` int32 [B] of them count).  The destination's
+    pages are distinct and none of the sources'."""
+    tables = _ints(tables, "tables", 2)
+    B = tables.shape[0]
+    if not _ints(keep, "keep", 3, B).is_contiguous():
+        raise TypeError("keep must be contiguous")
+    _ints(kept_lens, "kept_lens", 1, B)
+    _ints(dst_tables, "dst_tables", 2, B)
+    s = _stream(stream)
+    _raise(_lib.kv_compact(ctypes.byref(cache.struct), int(layer), B, tables.data_ptr(), tables.stride(0), tables.shape[1],
+                           keep.data_ptr(), keep.shape[1], keep.shape[2], kept_lens.data_ptr(), dst_tables.data_ptr(),
+                           dst_tables.stride(0), dst_tables.shape[1], _handle(s)))
+    _used(s, tables, keep, kept_lens, dst_tables)
+
+
+def kv_attend_async_error(clear: bool = False) -> int:
+    """Device-side faults of these operators on the current device since the last clear (KV_ASYNC_* bits)."""
+    mask = int(_lib.kv_attend_async_error(1 if clear else 0))
+    if mask < 0:
+        _raise(mask)
+    return mask
