@@ -6,24 +6,11 @@
 #include <algorithm>
 #include <cmath>
 
-#include "kvx_paged.h"
+#include "kvx_attend_kernels.h"
 
 namespace kvx {
 
 namespace {
-
-struct AttendArgs {
-    Pages pages;
-    Batch batch;
-    Rows q, out;
-    float *lse;
-    const float *slopes, *weights_in;
-    float *weights_out;
-    int64_t weights_seq_stride, weights_head_stride;
-    float scale, softcap, v_scale;  // scale: with k_scale
-    int32_t window, heads, group, num_seqs;
-    int32_t q_type, cache_type;
-};
 
 __device__ __forceinline__ float load_2(const uint8_t *p, int type) {
     const uint16_t bits = *reinterpret_cast<const uint16_t *>(p);
@@ -72,7 +59,7 @@ __global__ __launch_bounds__(256) void attend_kernel(const AttendArgs a) {
     __shared__ float q[256], sums[4][256], most[4], total[4];
     const int b = blockIdx.z, head = blockIdx.y, i = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     Sequence s;
-    if (!sequence(a.batch, b, a.pages.err, s) || i >= s.nq)
+    if (!sequence(a.batch, b, a.pages.err, s) || i >= s.nq || s.nq * a.group <= kStepRows)
         return;
     const int row = s.q0 + i, h = head / a.group, D = a.pages.D, p = s.n - s.nq + i;
     if (static_cast<int>(threadIdx.x) < D)
@@ -171,8 +158,8 @@ kv_status check_attend(const kv_cache *cache, const kv_batch *batch, const kv_at
     const int H = cache->layout.num_kv_heads;
     if (q->heads % H != 0)
         return fail(KV_EINVAL, "%d query heads for %d KV heads", q->heads, H);
-    if (q->heads > 65535)
-        return fail(KV_EUNSUPPORTED, "%d query heads (at most 65,535)", q->heads);
+    if (q->heads > 16383)
+        return fail(KV_EUNSUPPORTED, "%d query heads (at most 16,383)", q->heads);
     const bool quantised = o->cache_dtype == KV_DTYPE_E4M3;
     if (!quantised && q->dtype != o->cache_dtype)
         return fail(KV_EINVAL, "rows of type %d for a cache of type %d", q->dtype, o->cache_dtype);
@@ -195,8 +182,47 @@ kv_status check_attend(const kv_cache *cache, const kv_batch *batch, const kv_at
     return KV_OK;
 }
 
-int64_t lse_bytes(const kv_batch *batch, const kv_rows *q) {
-    return (static_cast<int64_t>(batch->num_queries) * q->heads * 4 + 15) / 16 * 16;
+// How a call is cut, and what its workspace holds.  Only the host's numbers count.
+struct Plan {
+    int32_t max_queries, max_rows, row_cap, split_len, splits;
+    bool tail, scores;  // some sequence may have more than kStepRows rows; weights_out from the step kernel's scores
+    int64_t score_len, lse_at, stats_at, sums_at, scores_at, bytes;
+};
+
+int64_t round_up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
+
+Plan plan_of(const kv_cache *cache, const kv_batch *batch, const kv_attend_options *o, const kv_rows *q) {
+    const int64_t H = cache->layout.num_kv_heads, D = cache->layout.head_dim, group = q->heads / H;
+    const int64_t sequences = batch->num_seqs;
+    Plan p{};
+    p.max_queries = std::min(batch->max_queries, batch->num_queries);
+    if (sequences == 0 || p.max_queries == 0)
+        return p;
+    const int64_t all_rows = p.max_queries * group;
+    p.max_rows = static_cast<int32_t>(std::min<int64_t>(all_rows, kStepRows));
+    p.tail = all_rows > kStepRows;
+    // A sequence of more than one row per head has its weights recomputed (kept scores would outgrow K).
+    p.scores = o->weights_out && all_rows <= 16;
+    p.row_cap = p.max_rows;
+    // Parts: about 4 workgroups of the step kernel per CU, of 128 to 4,096 tokens each (a ragged batch's longest
+    // sequence must not be one workgroup's).
+    const int64_t tile = step_tile_rows(p.max_rows, static_cast<int>(D)), tiles = (p.max_rows + tile - 1) / tile;
+    int64_t longest = batch->max_len;
+    if (o->window > 0)
+        longest = std::min<int64_t>(longest, static_cast<int64_t>(o->window) + p.max_rows / group + 31);
+    longest = std::max<int64_t>(longest, 1);
+    const int64_t wanted = (1024 + sequences * H * tiles - 1) / (sequences * H * tiles);
+    p.split_len = static_cast<int32_t>(
+        std::min<int64_t>(4096, round_up((longest + wanted - 1) / wanted, 128)));
+    p.splits = static_cast<int32_t>((longest + p.split_len - 1) / p.split_len);
+    p.score_len = round_up(batch->max_len, 32);
+    const int64_t slots = sequences * H * p.row_cap;
+    p.lse_at = 0;
+    p.stats_at = round_up(static_cast<int64_t>(batch->num_queries) * q->heads * 4, 16);
+    p.sums_at = p.stats_at + (p.splits > 1 ? round_up(slots * p.splits * 8, 16) : 0);
+    p.scores_at = p.sums_at + (p.splits > 1 ? slots * p.splits * D * 4 : 0);
+    p.bytes = p.scores_at + (p.scores ? slots * p.score_len * 4 : 0);
+    return p;
 }
 
 kv_status attend(const kv_cache *cache, int32_t layer, const kv_batch *batch, const kv_attend_options *o,
@@ -212,7 +238,8 @@ kv_status attend(const kv_cache *cache, int32_t layer, const kv_batch *batch, co
     if (out->heads != q->heads || out->dtype != q->dtype)
         return fail(KV_EINVAL, "out has %d heads of type %d, q %d of type %d", out->heads, out->dtype, q->heads,
                     q->dtype);
-    const int64_t need = lse_bytes(batch, q);
+    const Plan plan = plan_of(cache, batch, o, q);
+    const int64_t need = plan.bytes;
     if (workspace_bytes < need || (need > 0 && !workspace))
         return fail(KV_EINVAL, "workspace of %lld bytes; %lld are needed", static_cast<long long>(workspace_bytes),
                     static_cast<long long>(need));
@@ -231,7 +258,15 @@ kv_status attend(const kv_cache *cache, int32_t layer, const kv_batch *batch, co
     a.batch = batch_of(batch);
     a.q = Rows{static_cast<uint8_t *>(q->data), q->token_stride * 2, q->head_stride * 2};
     a.out = Rows{static_cast<uint8_t *>(out->data), out->token_stride * 2, out->head_stride * 2};
-    a.lse = lse ? lse : static_cast<float *>(workspace);
+    uint8_t *space = static_cast<uint8_t *>(workspace);
+    a.lse = lse ? lse : reinterpret_cast<float *>(space + plan.lse_at);
+    a.split_len = plan.split_len;
+    a.splits = plan.splits;
+    a.row_cap = plan.row_cap;
+    a.part_stats = reinterpret_cast<float *>(space + plan.stats_at);
+    a.part_sums = reinterpret_cast<float *>(space + plan.sums_at);
+    a.scores = plan.scores ? reinterpret_cast<float *>(space + plan.scores_at) : nullptr;
+    a.score_len = plan.score_len;
     a.slopes = o->slopes;
     a.weights_in = o->weights_in;
     a.weights_out = o->weights_out;
@@ -247,13 +282,17 @@ kv_status attend(const kv_cache *cache, int32_t layer, const kv_batch *batch, co
     a.num_seqs = batch->num_seqs;
     a.q_type = q->dtype;
     a.cache_type = o->cache_dtype;
-    const uint32_t rows = static_cast<uint32_t>(std::min(batch->max_queries, batch->num_queries));
-    if (rows > 0) {
-        const dim3 grid(rows, static_cast<uint32_t>(q->heads), static_cast<uint32_t>(batch->num_seqs));
-        hipLaunchKernelGGL(attend_kernel, grid, dim3(256), 0, stream, a);
-        KVX_HIP(hipGetLastError());
+    a.by_group = divisor(a.group);
+    if (plan.max_queries > 0) {
+        KVX_HIP(launch_step(a, plan.max_queries, stream));
+        if (plan.tail) {
+            const dim3 grid(static_cast<uint32_t>(plan.max_queries), static_cast<uint32_t>(q->heads),
+                            static_cast<uint32_t>(batch->num_seqs));
+            hipLaunchKernelGGL(attend_kernel, grid, dim3(256), 0, stream, a);
+            KVX_HIP(hipGetLastError());
+        }
     }
-    if (a.weights_out && batch->max_len > 0) {
+    if (a.weights_out && !a.scores && batch->max_len > 0) {
         const dim3 grid(static_cast<uint32_t>((batch->max_len + 63) / 64), static_cast<uint32_t>(a.pages.H),
                         static_cast<uint32_t>(batch->num_seqs));
         hipLaunchKernelGGL(weigh_kernel, grid, dim3(64), 0, stream, a);
@@ -274,7 +313,7 @@ int64_t kv_attend_workspace(const kv_cache *cache, const kv_batch *batch, const 
     const kv_status st = kvx::guarded([&]() -> kv_status {
         const kv_status checked = kvx::check_attend(cache, batch, options, q);
         if (checked == KV_OK)
-            bytes = kvx::lse_bytes(batch, q);
+            bytes = kvx::plan_of(cache, batch, options, q).bytes;
         return checked;
     });
     return st == KV_OK ? bytes : st;

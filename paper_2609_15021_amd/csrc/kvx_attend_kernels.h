@@ -1,0 +1,115 @@
+// What the kernels of kv_attend share.
+#pragma once
+
+#include "kvx_paged.h"
+
+namespace kvx {
+
+// Sequences of at most this many (new token, query head) rows per KV head go to the step kernel, others to the tail one.
+constexpr int kStepRows = 64;
+
+struct AttendArgs {
+    Pages pages;
+    Batch batch;
+    Rows q, out;
+    float *lse;  // never NULL (the caller's or the workspace's)
+    const float *slopes, *weights_in;
+    float *weights_out;
+    int64_t weights_seq_stride, weights_head_stride;
+    float scale, softcap, v_scale;  // scale: with k_scale
+    int32_t window, heads, group, num_seqs;
+    Divisor by_group;
+    int32_t q_type, cache_type;
+    // The step kernel's split of a sequence's tokens and what its parts leave for the join (workspace).
+    int32_t split_len, splits;  // tokens of a part; most parts of a sequence
+    int32_t row_cap;            // most rows per KV head of a sequence that has parts or scores
+    float *part_sums;           // [sequence][KV head][row_cap][splits][D], unscaled
+    float *part_stats;          // [sequence][KV head][row_cap][splits][2]: largest score and sum, in powers of 2
+    float *scores;              // [sequence][KV head][row_cap][score_len] in powers of 2, for weights_out; or NULL
+    int64_t score_len;
+};
+
+// Tokens that rows [row0, row1) of a sequence see between them: [first, end); parts start at `start`.
+struct Span {
+    int first, start, end;
+};
+
+__host__ __device__ __forceinline__ Span span_of(int n, int nq, int i0, int i1, int window) {
+    const int p0 = n - nq + i0;
+    Span s;
+    s.first = window > 0 && p0 + 1 > window ? p0 + 1 - window : 0;
+    s.start = s.first & ~31;
+    s.end = n - nq + i1;
+    return s;
+}
+
+// Rows of a tile of the step kernel.
+inline int step_tile_rows(int max_rows, int head_dim) { return max_rows > 16 && head_dim <= 128 ? 32 : 16; }
+
+__device__ __forceinline__ int parts_of(const Span &s, int split_len) {
+    return s.end > s.start ? (s.end - s.start + split_len - 1) / split_len : 1;
+}
+
+// Two-byte element types on the matrix cores.  kShift: weights are exp2(s - m + kShift), and m is at least the largest
+// score less 8: a float16 weight is at most 2^15, and its smallest normal 2^-21 or less of the largest.
+struct Bf16 {
+    typedef __bf16 frag __attribute__((ext_vector_type(8)));
+    typedef __bf16 pair __attribute__((ext_vector_type(2)));
+    static constexpr float kShift = 0.f;
+    static __device__ __forceinline__ uint32_t from_e4m3(uint32_t x, bool high) {
+        return high ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.f, true))
+                    : __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.f, false));
+    }
+    static __device__ __forceinline__ uint32_t pack(float a, float b) {
+        pair p;
+        p[0] = static_cast<__bf16>(a);
+        p[1] = static_cast<__bf16>(b);
+        return __builtin_bit_cast(uint32_t, p);
+    }
+};
+
+struct F16 {
+    typedef _Float16 frag __attribute__((ext_vector_type(8)));
+    typedef _Float16 pair __attribute__((ext_vector_type(2)));
+    static constexpr float kShift = 7.f;
+    static __device__ __forceinline__ uint32_t from_e4m3(uint32_t x, bool high) {
+        return high ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x, 1.f, true))
+                    : __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x, 1.f, false));
+    }
+    static __device__ __forceinline__ uint32_t pack(float a, float b) {
+        pair p;
+        p[0] = static_cast<_Float16>(a);
+        p[1] = static_cast<_Float16>(b);
+        return __builtin_bit_cast(uint32_t, p);
+    }
+};
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ f32x4 mfma_16x16x32(const u32x4 &a, const u32x4 &b, const f32x4 &c, Bf16) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(Bf16::frag, a), __builtin_bit_cast(Bf16::frag, b),
+                                                   c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mfma_16x16x32(const u32x4 &a, const u32x4 &b, const f32x4 &c, F16) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(F16::frag, a), __builtin_bit_cast(F16::frag, b), c,
+                                                  0, 0, 0);
+}
+
+constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
+constexpr float kLowest = -3.402823466e+38f;  // the largest score of nothing (finite: its differences are numbers)
+
+// cap * tanh(x / cap) for x * inv = x / cap: tanh by its series below 1/4 (the first term left out is 2^-27 of it), else
+// from exp2; an error of 2^-23 or so of cap.
+__device__ __forceinline__ float capped(float x, float inv, float cap) {
+    const float y = x * inv, y2 = y * y, t = fabsf(y);
+    const float series =
+        y * (1.f + y2 * (-1.f / 3 + y2 * (2.f / 15 + y2 * (-17.f / 315 + y2 * (62.f / 2835)))));
+    const float far = 1.f - 2.f * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(2.f * kLog2e * t));
+    return cap * (t < 0.25f ? series : copysignf(far, y));
+}
+
+hipError_t launch_step(const AttendArgs &a, int max_queries, hipStream_t stream);
+
+}  // namespace kvx

@@ -1,0 +1,525 @@
+// kv_attend for few new tokens per sequence (a decoding step): bound by reading the cache.
+//
+// A KV head's rows (its query heads times the new tokens, up to 16 or 32 of them at a time) share one pass over K and V.
+// Per 32 tokens a wave takes the scores as K Q^T and the output as V^T P^T on the matrix cores (16x16x32): then a row is
+// a column of both results, and its largest score, sum and rescaling stay inside a lane.
+//
+//  * K's operand wants a token's consecutive elements per lane: 16-byte loads straight into registers.  Its 32 tokens
+//    are given to the two products' rows in the order in which the second product wants them: row m of product j is
+//    token (m / 4) * 8 + j * 4 + m % 4, so that a lane's 8 scores are those of 8 consecutive tokens, and their weights
+//    are the operand of the second product as they stand.  Nothing passes through LDS.
+//  * V's operand wants 8 consecutive tokens of one column per lane.  A lane loads 8 rows of VE columns, and byte
+//    permutations in registers turn them (one per pair of elements); e4m3 is turned while it is widened.
+//  * The pages of 32 tokens are looked up by 32 lanes, one token each, a round ahead, and handed out by lane shuffles.
+//
+// A sequence's tokens are split over workgroups (split_len each) until the chip is full, and inside a workgroup over its
+// 4 waves; the waves' sums are joined through LDS, the workgroups' by join_kernel.  K of the next 32 tokens is requested
+// as soon as the scores have used the last, V as soon as the second product has: a wave has 16 KiB in flight (bf16,
+// D 128) without a second set of registers.
+#include <algorithm>
+
+#include "kvx_attend_kernels.h"
+
+namespace kvx {
+
+namespace {
+
+constexpr int kWaves = 4;
+
+template <int BYTES>
+struct Vec;
+template <>
+struct Vec<4> {
+    uint32_t w[1];
+    __device__ __forceinline__ void load(const uint8_t *p) { w[0] = *reinterpret_cast<const uint32_t *>(p); }
+};
+template <>
+struct Vec<8> {
+    uint32_t w[2];
+    __device__ __forceinline__ void load(const uint8_t *p) {
+        const u32x2 x = *reinterpret_cast<const u32x2 *>(p);
+        w[0] = x[0];
+        w[1] = x[1];
+    }
+};
+template <>
+struct Vec<16> {
+    uint32_t w[4];
+    __device__ __forceinline__ void load(const uint8_t *p) {
+        const u32x4 x = *reinterpret_cast<const u32x4 *>(p);
+        w[0] = x[0];
+        w[1] = x[1];
+        w[2] = x[2];
+        w[3] = x[3];
+    }
+};
+
+// T: type of q, of the weights and of out; FP8: the cache holds e4m3; DP >= D columns; NT: tiles of 16 rows.
+template <class T, bool FP8, int DP, int NT>
+__global__ __launch_bounds__(64 * kWaves) void step_kernel(const AttendArgs a) {
+    constexpr int E = FP8 ? 1 : 2;                       // bytes of a cached element
+    constexpr int KC = DP * E / 64;                      // 16-byte pieces of a token's K in a lane
+    constexpr int VE = DP / 16 * E > 16 ? 16 / E : DP / 16;  // V columns of a lane in a piece
+    constexpr int NV = DP / (16 * VE);                   // such pieces
+    constexpr int TILES = NV * VE;                       // 16-column tiles of the output
+    const Pages &pg = a.pages;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
+    const int split = blockIdx.x, tile = blockIdx.y / pg.H, h = blockIdx.y - tile * pg.H, b = blockIdx.z;
+    Sequence seq;
+    if (!sequence(a.batch, b, pg.err, seq))
+        return;
+    const int rows = seq.nq * a.group, row0 = tile * 16 * NT;
+    if (row0 >= rows || rows > kStepRows)
+        return;
+    const int i0 = divide(row0, a.by_group), i1 = divide(min(row0 + 16 * NT, rows) - 1, a.by_group) + 1;
+    const Span span = span_of(seq.n, seq.nq, i0, i1, a.window);
+    const int begin = span.start + split * a.split_len;
+    if (split > 0 && begin >= span.end)
+        return;
+    const int stop = min(span.end, begin + a.split_len);
+    const bool whole = span.end - span.start <= a.split_len;  // no other part
+    const int p_first = seq.n - seq.nq + i0;
+    const int low_last = a.window > 0 ? span.end - a.window : 0;  // from here on every row's window is open
+
+    const int64_t slot0 = (static_cast<int64_t>(b) * pg.H + h) * a.row_cap + row0;
+
+    // Queries: a row's elements in the order in which K's pieces hold them.
+    u32x4 qf[NT][KC * 2 / E];
+    int p_of[NT];
+    float slope[NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        const int r = row0 + nt * 16 + c;
+        const bool row = r < rows;
+        const int i = divide(min(r, rows - 1), a.by_group), head = h * a.group + min(r, rows - 1) - i * a.group;
+        p_of[nt] = row ? seq.n - seq.nq + i : -1;
+        slope[nt] = a.slopes ? a.slopes[head] * kLog2e : 0.f;
+        const uint8_t *q = a.q.data + (seq.q0 + i) * a.q.token_stride + head * a.q.head_stride;
+#pragma unroll
+        for (int k = 0; k < KC * 2 / E; ++k) {
+            const int d = FP8 ? (k >> 1) * 64 + g * 16 + (k & 1) * 8 : k * 32 + g * 8;
+            qf[nt][k] = row && d < pg.D ? *reinterpret_cast<const u32x4 *>(q + 2 * d) : u32x4{0, 0, 0, 0};
+        }
+    }
+
+    // Where a lane's pieces start in a row (columns beyond D: the row's start, which Q's zeros or the output ignore).
+    int k_at[KC], v_at[NV];
+#pragma unroll
+    for (int k = 0; k < KC; ++k)
+        k_at[k] = k * 64 + g * 16 < pg.row_bytes ? k * 64 + g * 16 : 0;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        const int at = (v * 16 + c) * VE * E;
+        v_at[v] = static_cast<int>(pg.v_bytes) + (at < pg.row_bytes ? at : 0);
+    }
+    const bool by_8 = pg.BS % 8 == 0;
+    const int32_t *table = a.batch.tables + b * a.batch.table_stride;
+    const uint8_t *cache = pg.base + static_cast<uint32_t>(h) * pg.head_bytes;
+
+    // Page of token base + lane % 32, and where that token's row is (-1: none that a row sees).
+    auto page_at = [&](int base, int &page, bool &shown) {
+        const int t = base + (lane & 31);
+        page = divide(t, pg.by_bs);
+        shown = t < stop && (page + 1) * static_cast<int64_t>(pg.BS) > span.first;
+        return shown ? table[page] : 0;
+    };
+    auto offset_at = [&](int base, int page, bool shown, int block) -> int64_t {
+        if (!shown || !in_cache(pg, block))
+            return -1;
+        return block * pg.block_stride + static_cast<uint32_t>(base + (lane & 31) - page * pg.BS) * pg.token_bytes;
+    };
+    auto from_lane = [&](int64_t x, int src) -> int64_t {
+        const uint32_t lo = __shfl(static_cast<uint32_t>(x), src), hi = __shfl(static_cast<uint32_t>(x >> 32), src);
+        return static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo);
+    };
+
+    Vec<16> k_reg[2][KC];
+    Vec<VE * E> v_reg[8][NV];
+    auto load_k = [&](int64_t off) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int64_t at = max(from_lane(off, (c >> 2) * 8 + j * 4 + (c & 3)), int64_t{0});
+#pragma unroll
+            for (int k = 0; k < KC; ++k)
+                k_reg[j][k].load(cache + at + k_at[k]);
+        }
+    };
+    auto load_v = [&](int64_t off) {
+        if (by_8) {
+            int64_t at = max(from_lane(off, g * 8), int64_t{0});
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+#pragma unroll
+                for (int v = 0; v < NV; ++v)
+                    v_reg[e][v].load(cache + at + v_at[v]);
+                at += pg.token_bytes;
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int64_t at = max(from_lane(off, g * 8 + e), int64_t{0});
+#pragma unroll
+                for (int v = 0; v < NV; ++v)
+                    v_reg[e][v].load(cache + at + v_at[v]);
+            }
+        }
+    };
+
+    f32x4 acc[NT][TILES];
+    float m[NT], l[NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        m[nt] = kLowest;
+        l[nt] = 0.f;
+#pragma unroll
+        for (int t = 0; t < TILES; ++t)
+            acc[nt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+
+    constexpr int kStride = 32 * kWaves;
+    int base = begin + wave * 32;
+    if (base < stop) {
+        int page, next_page = 0, next_block = 0;
+        bool shown, next_shown = false;
+        int block = page_at(base, page, shown);
+        int64_t off = offset_at(base, page, shown, block);
+        if (stop - base > kStride)
+            next_block = page_at(base + kStride, next_page, next_shown);
+        load_k(off);
+        load_v(off);
+        while (true) {
+            const int t_lane = base + (lane & 31);
+            const bool use = off >= 0 && t_lane >= span.first && t_lane < stop;
+            const uint32_t usable = static_cast<uint32_t>(__ballot(use));
+            const bool edge = usable != 0xffffffffu || p_first - base < 31 || base < low_last;
+            const bool more = stop - base > kStride;
+
+            f32x4 s[NT][2];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    s[nt][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int k = 0; k < KC; ++k) {
+                        const Vec<16> &x = k_reg[j][k];
+                        if constexpr (FP8) {
+                            s[nt][j] = mfma_16x16x32(u32x4{T::from_e4m3(x.w[0], false), T::from_e4m3(x.w[0], true),
+                                                           T::from_e4m3(x.w[1], false), T::from_e4m3(x.w[1], true)},
+                                                     qf[nt][2 * k], s[nt][j], T{});
+                            s[nt][j] = mfma_16x16x32(u32x4{T::from_e4m3(x.w[2], false), T::from_e4m3(x.w[2], true),
+                                                           T::from_e4m3(x.w[3], false), T::from_e4m3(x.w[3], true)},
+                                                     qf[nt][2 * k + 1], s[nt][j], T{});
+                        } else {
+                            s[nt][j] = mfma_16x16x32(u32x4{x.w[0], x.w[1], x.w[2], x.w[3]}, qf[nt][k], s[nt][j], T{});
+                        }
+                    }
+                }
+            int64_t next_off = -1;
+            if (more) {
+                next_off = offset_at(base + kStride, next_page, next_shown, next_block);
+                load_k(next_off);
+                if (stop - base > 2 * kStride)
+                    next_block = page_at(base + 2 * kStride, next_page, next_shown);
+            }
+
+            // Weights.  Everything from here on is in powers of 2.
+            u32x4 p[NT];
+            const uint32_t bits = usable >> (g * 8);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                float x[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    x[e] = s[nt][e >> 2][e & 3];
+                    if (a.softcap > 0.f)
+                        x[e] = capped(x[e], a.scale / a.softcap, a.softcap * kLog2e);
+                    else
+                        x[e] *= a.scale * kLog2e;
+                    const int t = base + g * 8 + e;
+                    if (a.slopes)
+                        x[e] -= slope[nt] * static_cast<float>(p_of[nt] - t);
+                    if (edge && (!(bits >> e & 1) || t > p_of[nt] || (a.window > 0 && p_of[nt] - t >= a.window)))
+                        x[e] = -INFINITY;
+                }
+                if (a.scores && row0 + nt * 16 + c < rows) {
+                    float *to = a.scores + (slot0 + nt * 16 + c) * a.score_len + base + g * 8;
+                    *reinterpret_cast<f32x4 *>(to) = f32x4{x[0], x[1], x[2], x[3]};
+                    *reinterpret_cast<f32x4 *>(to + 4) = f32x4{x[4], x[5], x[6], x[7]};
+                }
+                float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+                // The sums are scaled down only when some score has outgrown them by 2^8.
+                if (__any(top > m[nt] + 8.f)) {
+                    top = fmaxf(top, __shfl_xor(top, 16));
+                    top = fmaxf(top, __shfl_xor(top, 32));
+                    const float next = fmaxf(m[nt], top), f = __builtin_amdgcn_exp2f(m[nt] - next);
+                    m[nt] = next;
+                    l[nt] *= f;
+#pragma unroll
+                    for (int t = 0; t < TILES; ++t)
+                        acc[nt][t] *= f;
+                }
+                const float zero = m[nt] - T::kShift;
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    x[e] = __builtin_amdgcn_exp2f(x[e] - zero);
+                l[nt] += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+                p[nt] = u32x4{T::pack(x[0], x[1]), T::pack(x[2], x[3]), T::pack(x[4], x[5]), T::pack(x[6], x[7])};
+            }
+
+            // A slot without a token may hold anything, and 0 times it need not be 0.
+            if (usable != 0xffffffffu) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (!(bits >> e & 1)) {
+#pragma unroll
+                        for (int v = 0; v < NV; ++v)
+#pragma unroll
+                            for (int w = 0; w < VE * E / 4; ++w)
+                                v_reg[e][v].w[w] = 0;
+                    }
+            }
+#pragma unroll
+            for (int v = 0; v < NV; ++v)
+#pragma unroll
+                for (int w = 0; w < VE * E / 4; ++w) {
+                    constexpr int kEach = 4 / E;  // columns in 4 bytes
+                    u32x4 turned[kEach];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const uint32_t x = v_reg[2 * e][v].w[w], y = v_reg[2 * e + 1][v].w[w];
+                        if constexpr (FP8) {
+                            const uint32_t lo = __builtin_amdgcn_perm(y, x, 0x05010400);
+                            const uint32_t hi = __builtin_amdgcn_perm(y, x, 0x07030602);
+                            turned[0][e] = T::from_e4m3(lo, false);
+                            turned[1][e] = T::from_e4m3(lo, true);
+                            turned[2][e] = T::from_e4m3(hi, false);
+                            turned[3][e] = T::from_e4m3(hi, true);
+                        } else {
+                            turned[0][e] = __builtin_amdgcn_perm(y, x, 0x05040100);
+                            turned[1][e] = __builtin_amdgcn_perm(y, x, 0x07060302);
+                        }
+                    }
+#pragma unroll
+                    for (int j = 0; j < kEach; ++j)
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) {
+                            f32x4 &x = acc[nt][v * VE + w * kEach + j];
+                            x = mfma_16x16x32(turned[j], p[nt], x, T{});
+                        }
+                }
+            if (!more)
+                break;
+            load_v(next_off);
+            off = next_off;
+            base += kStride;
+        }
+    }
+
+    // Join the waves: every wave's largest score and sum, then wave w collects component w of every tile, which are VE
+    // consecutive columns per lane.
+    __shared__ float stats[kWaves][NT * 16][2];
+    __shared__ float parts[kWaves][kWaves - 1][NT * TILES][64];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        l[nt] += __shfl_xor(l[nt], 16);
+        l[nt] += __shfl_xor(l[nt], 32);
+        if (g == 0) {
+            stats[wave][nt * 16 + c][0] = m[nt];
+            stats[wave][nt * 16 + c][1] = l[nt];
+        }
+    }
+    __syncthreads();
+    float most[NT], total[NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        const int col = nt * 16 + c;
+        most[nt] = fmaxf(fmaxf(stats[0][col][0], stats[1][col][0]), fmaxf(stats[2][col][0], stats[3][col][0]));
+        total[nt] = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w)
+            total[nt] += stats[w][col][1] * __builtin_amdgcn_exp2f(stats[w][col][0] - most[nt]);
+        const float f = __builtin_amdgcn_exp2f(m[nt] - most[nt]);
+#pragma unroll
+        for (int t = 0; t < TILES; ++t) {
+            acc[nt][t] *= f;
+#pragma unroll
+            for (int r = 0; r < kWaves; ++r)
+                if (r != wave)
+                    parts[r][wave - (wave > r)][nt * TILES + t][lane] = acc[nt][t][r];
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        const int r = row0 + nt * 16 + c;
+        if (r >= rows)
+            continue;
+        const int i = divide(r, a.by_group), head = h * a.group + r - i * a.group, row = seq.q0 + i;
+        const int64_t slot = (slot0 + nt * 16 + c) * a.splits + split;
+        const float inv = total[nt] == 0.f ? 0.f : a.v_scale / total[nt];
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int d = v * 16 * VE + (g * 4 + wave) * VE;
+            float x[VE];
+#pragma unroll
+            for (int j = 0; j < VE; ++j) {
+                const f32x4 &own = acc[nt][v * VE + j];
+                x[j] = wave == 0 ? own[0] : wave == 1 ? own[1] : wave == 2 ? own[2] : own[3];
+#pragma unroll
+                for (int k = 0; k < kWaves - 1; ++k)
+                    x[j] += parts[wave][k][nt * TILES + v * VE + j][lane];
+            }
+            if (d >= pg.D)
+                continue;
+            if (whole) {
+                uint8_t *to = a.out.data + row * a.out.token_stride + head * a.out.head_stride + 2 * d;
+#pragma unroll
+                for (int j = 0; j < VE; j += 4)
+                    *reinterpret_cast<u32x2 *>(to + 2 * j) = u32x2{T::pack(x[j] * inv, x[j + 1] * inv),
+                                                                    T::pack(x[j + 2] * inv, x[j + 3] * inv)};
+            } else {
+                float *to = a.part_sums + slot * pg.D + d;
+#pragma unroll
+                for (int j = 0; j < VE; j += 4)
+                    *reinterpret_cast<f32x4 *>(to + j) = f32x4{x[j], x[j + 1], x[j + 2], x[j + 3]};
+            }
+        }
+        if (wave == 0 && g == 0) {
+            if (whole) {
+                a.lse[static_cast<int64_t>(row) * a.heads + head] =
+                    total[nt] == 0.f ? -INFINITY : (most[nt] - T::kShift + __builtin_amdgcn_logf(total[nt])) * kLn2;
+            } else {
+                a.part_stats[slot * 2] = most[nt] - T::kShift;
+                a.part_stats[slot * 2 + 1] = total[nt];
+            }
+        }
+    }
+}
+
+// The parts of a row joined: sum_s 2^(m_s - m) x_s / sum_s 2^(m_s - m) l_s.  One row and head per workgroup; 4 columns
+// per lane, the parts spread over the lanes' groups.
+__global__ __launch_bounds__(256) void join_kernel(const AttendArgs a, const int tile_rows) {
+    __shared__ float sums[256][4];
+    __shared__ float shared_stats[2];
+    const int b = blockIdx.z, head = blockIdx.y, i = blockIdx.x, h = divide(head, a.by_group);
+    Sequence seq;
+    if (!sequence(a.batch, b, a.pages.err, seq) || i >= seq.nq || seq.nq * a.group > kStepRows)
+        return;
+    // The parts are those of the row's tile.
+    const int r = i * a.group + head - h * a.group, rows = seq.nq * a.group, row0 = r - r % tile_rows;
+    const Span span = span_of(seq.n, seq.nq, divide(row0, a.by_group),
+                              divide(min(row0 + tile_rows, rows) - 1, a.by_group) + 1, a.window);
+    const int parts = parts_of(span, a.split_len), D = a.pages.D, tid = threadIdx.x;
+    if (parts == 1)
+        return;
+    const int64_t slot = ((static_cast<int64_t>(b) * a.pages.H + h) * a.row_cap + r) * a.splits;
+    const float *stats = a.part_stats + slot * 2;
+    if (tid < 64) {
+        float most = kLowest;
+        for (int s = tid; s < parts; s += 64)
+            most = fmaxf(most, stats[2 * s]);
+        for (int o = 32; o; o >>= 1)
+            most = fmaxf(most, __shfl_xor(most, o));
+        float total = 0.f;
+        for (int s = tid; s < parts; s += 64)
+            total += stats[2 * s + 1] * __builtin_amdgcn_exp2f(stats[2 * s] - most);
+        for (int o = 32; o; o >>= 1)
+            total += __shfl_xor(total, o);
+        if (tid == 0) {
+            shared_stats[0] = most;
+            shared_stats[1] = total;
+        }
+    }
+    __syncthreads();
+    const float most = shared_stats[0], total = shared_stats[1];
+    const int lanes = D / 4, groups = 256 / lanes, part0 = tid / lanes, d = (tid - part0 * lanes) * 4;
+    f32x4 x{0.f, 0.f, 0.f, 0.f};
+    if (part0 < groups)
+        for (int s = part0; s < parts; s += groups)
+            x += *reinterpret_cast<const f32x4 *>(a.part_sums + (slot + s) * D + d) *
+                 __builtin_amdgcn_exp2f(stats[2 * s] - most);
+    for (int k = 0; k < 4; ++k)
+        sums[tid][k] = x[k];
+    __syncthreads();
+    if (part0 == 0) {
+        for (int s = 1; s < groups; ++s)
+            for (int k = 0; k < 4; ++k)
+                x[k] += sums[s * lanes + tid][k];
+        const float inv = total == 0.f ? 0.f : a.v_scale / total;
+        u32x2 y;
+        if (a.q_type == KV_DTYPE_BF16)
+            y = u32x2{Bf16::pack(x[0] * inv, x[1] * inv), Bf16::pack(x[2] * inv, x[3] * inv)};
+        else
+            y = u32x2{F16::pack(x[0] * inv, x[1] * inv), F16::pack(x[2] * inv, x[3] * inv)};
+        *reinterpret_cast<u32x2 *>(a.out.data + (seq.q0 + i) * a.out.token_stride + head * a.out.head_stride + 2 * d) = y;
+    }
+    if (tid == 0)
+        a.lse[static_cast<int64_t>(seq.q0 + i) * a.heads + head] =
+            total == 0.f ? -INFINITY : (most + __builtin_amdgcn_logf(total)) * kLn2;
+}
+
+// What each token received from the rows of a sequence, from the scores that the step kernel left.
+__global__ __launch_bounds__(256) void weigh_step_kernel(const AttendArgs a) {
+    const int b = blockIdx.z, h = blockIdx.y, t = blockIdx.x * 256 + threadIdx.x;
+    Sequence seq;
+    if (!sequence(a.batch, b, a.pages.err, seq) || seq.nq * a.group > kStepRows || t >= seq.n)
+        return;
+    float sum = 0.f;
+    for (int i = 0; i < seq.nq; ++i) {
+        const int p = seq.n - seq.nq + i;
+        if (t > p || (a.window > 0 && p - t >= a.window))
+            continue;
+        const int64_t at = static_cast<int64_t>(seq.q0 + i) * a.heads + h * a.group;
+        const int64_t slot = (static_cast<int64_t>(b) * a.pages.H + h) * a.row_cap + i * a.group;
+        for (int k = 0; k < a.group; ++k) {
+            const float lse = a.lse[at + k];
+            if (lse != -INFINITY)
+                sum += __builtin_amdgcn_exp2f(a.scores[(slot + k) * a.score_len + t] - lse * kLog2e);
+        }
+    }
+    const int64_t at = b * a.weights_seq_stride + h * a.weights_head_stride + t;
+    a.weights_out[at] = (a.weights_in ? a.weights_in[at] : 0.f) + sum;
+}
+
+template <class T, bool FP8, int DP, int NT>
+void launch(const AttendArgs &a, int max_rows, hipStream_t stream) {
+    const int tiles = (max_rows + 16 * NT - 1) / (16 * NT);
+    hipLaunchKernelGGL((step_kernel<T, FP8, DP, NT>), dim3(a.splits, tiles * a.pages.H, a.num_seqs), dim3(64 * kWaves), 0,
+                       stream, a);
+}
+
+template <class T, bool FP8>
+void launch(const AttendArgs &a, int max_rows, hipStream_t stream) {
+    const bool two = step_tile_rows(max_rows, a.pages.D) == 32;
+    if (a.pages.D > 128)
+        launch<T, FP8, 256, 1>(a, max_rows, stream);
+    else if (a.pages.D > 64)
+        two ? launch<T, FP8, 128, 2>(a, max_rows, stream) : launch<T, FP8, 128, 1>(a, max_rows, stream);
+    else
+        two ? launch<T, FP8, 64, 2>(a, max_rows, stream) : launch<T, FP8, 64, 1>(a, max_rows, stream);
+}
+
+}  // namespace
+
+hipError_t launch_step(const AttendArgs &a, int max_queries, hipStream_t stream) {
+    const int max_rows = static_cast<int>(std::min<int64_t>(kStepRows, static_cast<int64_t>(max_queries) * a.group));
+    const bool fp8 = a.cache_type == KV_DTYPE_E4M3;
+    if (a.q_type == KV_DTYPE_BF16)
+        fp8 ? launch<Bf16, true>(a, max_rows, stream) : launch<Bf16, false>(a, max_rows, stream);
+    else
+        fp8 ? launch<F16, true>(a, max_rows, stream) : launch<F16, false>(a, max_rows, stream);
+    const uint32_t queries = static_cast<uint32_t>(std::min(max_queries, kStepRows));
+    if (a.splits > 1) {
+        const int tile_rows = step_tile_rows(max_rows, a.pages.D);
+        hipLaunchKernelGGL(join_kernel, dim3(queries, static_cast<uint32_t>(a.heads), static_cast<uint32_t>(a.num_seqs)),
+                           dim3(256), 0, stream, a, tile_rows);
+    }
+    if (a.scores)
+        hipLaunchKernelGGL(weigh_step_kernel, dim3(static_cast<uint32_t>((a.batch.max_len + 255) / 256),
+                                                   static_cast<uint32_t>(a.pages.H), static_cast<uint32_t>(a.num_seqs)),
+                           dim3(256), 0, stream, a);
+    return hipGetLastError();
+}
+
+}  // namespace kvx

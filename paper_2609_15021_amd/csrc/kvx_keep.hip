@@ -106,7 +106,7 @@ __global__ __launch_bounds__(kKeepThreads) void keep_kernel(const KeepArgs a) {
             equal += c;
         }
         const uint64_t below = (uint64_t{1} << lane) - 1;
-        const bool chosen = t < n && (!middle || (any && (key > threshold || (tie && seen + __popcll(ties & below) < left))));
+        const bool chosen = t < n && (!middle || (any && (key > threshold || (tie && seen + static_cast<int>(__popcll(ties & below)) < left))));
         const uint64_t all = __ballot(chosen);
         if (lane == 0)
             wave_sums[1][wave] = __popcll(all);
