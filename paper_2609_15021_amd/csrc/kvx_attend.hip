@@ -1,8 +1,9 @@
-// kv_attend: attention of the new tokens over a paged cache.
+// kv_attend: attention of the new tokens over a paged cache (host side).
 //
 // For a row (a new token and a query head) with scores s_t over the tokens it sees, out = sum exp(s_t - m) v_t / sum
-// exp(s_t - m) in one pass over the tokens: m is the largest score so far, and what was summed under a smaller one is
-// scaled down when it grows.
+// exp(s_t - m) in one pass over the tokens: m is the largest score so far (up to a factor of 2^8), and what was summed
+// under a smaller one is scaled down when it grows.  Sequences of few rows per KV head go to the step kernel, others to
+// the tail kernel; both split a long sequence over workgroups where the batch alone does not fill the chip.
 #include <algorithm>
 #include <cmath>
 
@@ -11,133 +12,6 @@
 namespace kvx {
 
 namespace {
-
-__device__ __forceinline__ float load_2(const uint8_t *p, int type) {
-    const uint16_t bits = *reinterpret_cast<const uint16_t *>(p);
-    return type == KV_DTYPE_BF16 ? __builtin_bit_cast(float, static_cast<uint32_t>(bits) << 16)
-                                 : static_cast<float>(__builtin_bit_cast(_Float16, bits));
-}
-
-__device__ __forceinline__ float load_cached(const uint8_t *row, int d, int type) {
-    if (type == KV_DTYPE_E4M3)
-        return __builtin_amdgcn_cvt_f32_fp8(row[d], 0);
-    return load_2(row + 2 * d, type);
-}
-
-__device__ __forceinline__ void store_2(uint8_t *p, float x, int type) {
-    if (type == KV_DTYPE_BF16)
-        *reinterpret_cast<__bf16 *>(p) = static_cast<__bf16>(x);
-    else
-        *reinterpret_cast<_Float16 *>(p) = static_cast<_Float16>(x);
-}
-
-__device__ __forceinline__ const uint8_t *cached_row(const AttendArgs &a, int b, int t, int kv, int h) {
-    const int page = divide(t, a.pages.by_bs);
-    const int block = a.batch.tables[b * a.batch.table_stride + page];
-    if (!in_cache(a.pages, block))
-        return nullptr;
-    return a.pages.base + page_offset(a.pages, block, kv, h) +
-           static_cast<uint32_t>(t - page * a.pages.BS) * a.pages.token_bytes;
-}
-
-// The score of a row at token p with query `q` for token t.
-__device__ __forceinline__ float score(const AttendArgs &a, const float *q, const uint8_t *k, int p, int t, int head) {
-    float x = 0.f;
-    for (int d = 0; d < a.pages.D; ++d)
-        x = fmaf(q[d], load_cached(k, d, a.cache_type), x);
-    x *= a.scale;
-    if (a.softcap > 0.f)
-        x = a.softcap * tanhf(x / a.softcap);
-    if (a.slopes)
-        x -= a.slopes[head] * static_cast<float>(p - t);
-    return x;
-}
-
-// One row and query head per workgroup: each wave takes 64 tokens at a time, one per lane for the scores and D / 64
-// columns per lane for the sums; the waves' sums are joined at the end.
-__global__ __launch_bounds__(256) void attend_kernel(const AttendArgs a) {
-    __shared__ float q[256], sums[4][256], most[4], total[4];
-    const int b = blockIdx.z, head = blockIdx.y, i = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    Sequence s;
-    if (!sequence(a.batch, b, a.pages.err, s) || i >= s.nq || s.nq * a.group <= kStepRows)
-        return;
-    const int row = s.q0 + i, h = head / a.group, D = a.pages.D, p = s.n - s.nq + i;
-    if (static_cast<int>(threadIdx.x) < D)
-        q[threadIdx.x] = load_2(a.q.data + row * a.q.token_stride + head * a.q.head_stride + 2 * threadIdx.x, a.q_type);
-    __syncthreads();
-    float m = -INFINITY, l = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
-    const int begin = a.window > 0 ? max(0, p + 1 - a.window) : 0;
-    for (int t0 = begin + wave * 64; t0 <= p; t0 += 256) {
-        const int t = t0 + lane;
-        const uint8_t *k = t <= p ? cached_row(a, b, t, 0, h) : nullptr;
-        const float x = k ? score(a, q, k, p, t, head) : -INFINITY;
-        float top = x;
-        for (int o = 32; o; o >>= 1)
-            top = fmaxf(top, __shfl_xor(top, o));
-        const float next = fmaxf(m, top);
-        if (next == -INFINITY && !__any(x != x))
-            continue;
-        const float keep = m == -INFINITY ? 0.f : expf(m - next), e = k ? expf(x - next) : 0.f;
-        m = next;
-        l = l * keep + e;
-        for (int c = 0; c < 4; ++c)
-            acc[c] *= keep;
-        for (int j = 0; j < 64; ++j) {
-            const float w = __shfl(e, j);
-            const uint8_t *v = t0 + j <= p ? cached_row(a, b, t0 + j, 1, h) : nullptr;
-            if (v)
-                for (int c = 0; c < 4; ++c)
-                    if (c * 64 + lane < D)
-                        acc[c] = fmaf(w, load_cached(v, c * 64 + lane, a.cache_type), acc[c]);
-        }
-    }
-    for (int o = 32; o; o >>= 1)
-        l += __shfl_xor(l, o);
-    for (int c = 0; c < 4; ++c)
-        sums[wave][c * 64 + lane] = acc[c];
-    if (lane == 0) {
-        most[wave] = m;
-        total[wave] = l;
-    }
-    __syncthreads();
-    const float top = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
-    float x = 0.f, all = 0.f;
-    for (int w = 0; w < 4; ++w) {
-        const float f = most[w] == -INFINITY ? 0.f : expf(most[w] - top);
-        x += f * sums[w][threadIdx.x];
-        all += f * total[w];
-    }
-    if (static_cast<int>(threadIdx.x) < D)
-        store_2(a.out.data + row * a.out.token_stride + head * a.out.head_stride + 2 * threadIdx.x,
-                all == 0.f ? 0.f : x / all * a.v_scale, a.q_type);
-    if (threadIdx.x == 0)
-        a.lse[static_cast<int64_t>(row) * a.heads + head] = all == 0.f ? -INFINITY : top + logf(all);
-}
-
-// What each token received: one token per lane, over all rows that see it.
-__global__ __launch_bounds__(64) void weigh_kernel(const AttendArgs a) {
-    __shared__ float q[256];
-    const int b = blockIdx.z, h = blockIdx.y, t = blockIdx.x * 64 + threadIdx.x;
-    Sequence s;
-    if (!sequence(a.batch, b, a.pages.err, s))
-        return;
-    const int begin = a.window > 0 ? s.n - s.nq + 1 - a.window : 0;  // the first token that a row sees
-    const uint8_t *k = t < s.n && t >= begin && s.nq > 0 ? cached_row(a, b, t, 0, h) : nullptr;
-    float sum = 0.f;
-    for (int r = 0; r < s.nq * a.group; ++r) {
-        const int i = r / a.group, head = h * a.group + r - i * a.group, row = s.q0 + i, p = s.n - s.nq + i;
-        __syncthreads();
-        for (int d = threadIdx.x; d < a.pages.D; d += 64)
-            q[d] = load_2(a.q.data + row * a.q.token_stride + head * a.q.head_stride + 2 * d, a.q_type);
-        __syncthreads();
-        const float lse = a.lse[static_cast<int64_t>(row) * a.heads + head];
-        if (k && t <= p && (a.window == 0 || p - t < a.window) && lse != -INFINITY)
-            sum += expf(score(a, q, k, p, t, head) - lse);
-    }
-    const int64_t at = b * a.weights_seq_stride + h * a.weights_head_stride + t;
-    if (t < s.n)
-        a.weights_out[at] = (a.weights_in ? a.weights_in[at] : 0.f) + sum;
-}
 
 // The checks of kv_attend that need no stream.
 kv_status check_attend(const kv_cache *cache, const kv_batch *batch, const kv_attend_options *o, const kv_rows *q) {
@@ -184,44 +58,66 @@ kv_status check_attend(const kv_cache *cache, const kv_batch *batch, const kv_at
 
 // How a call is cut, and what its workspace holds.  Only the host's numbers count.
 struct Plan {
-    int32_t max_queries, max_rows, row_cap, split_len, splits;
-    bool tail, scores;  // some sequence may have more than kStepRows rows; weights_out from the step kernel's scores
-    int64_t score_len, lse_at, stats_at, sums_at, scores_at, bytes;
+    int32_t max_queries, max_rows;  // of a sequence; rows per KV head in the step kernel
+    bool tail;                      // some sequence may have more than kStepRows rows
+    bool scores;                    // weights_out from the step kernel's scores
+    int64_t score_len, step_stats, step_sums, tail_stats, tail_sums, scores_at, bytes;
+    Parts step_parts, tail_parts;
 };
 
 int64_t round_up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 
+// Parts of a multiple of `unit` tokens (at most `most`) so that there are `wanted` workgroups where there are `have`
+// without a split.
+Parts parts_for(int64_t longest, int64_t have, int64_t wanted, int64_t unit, int64_t most, int64_t row_cap) {
+    Parts p{};
+    const int64_t splits = (wanted + have - 1) / have;
+    longest = std::max<int64_t>(longest, 1);
+    p.len = static_cast<int32_t>(std::min(most, round_up((longest + splits - 1) / splits, unit)));
+    p.splits = static_cast<int32_t>((longest + p.len - 1) / p.len);
+    p.row_cap = static_cast<int32_t>(row_cap);
+    return p;
+}
+
 Plan plan_of(const kv_cache *cache, const kv_batch *batch, const kv_attend_options *o, const kv_rows *q) {
     const int64_t H = cache->layout.num_kv_heads, D = cache->layout.head_dim, group = q->heads / H;
-    const int64_t sequences = batch->num_seqs;
+    const int64_t heads = batch->num_seqs * H;
     Plan p{};
     p.max_queries = std::min(batch->max_queries, batch->num_queries);
-    if (sequences == 0 || p.max_queries == 0)
+    if (heads == 0 || p.max_queries == 0)
         return p;
     const int64_t all_rows = p.max_queries * group;
     p.max_rows = static_cast<int32_t>(std::min<int64_t>(all_rows, kStepRows));
     p.tail = all_rows > kStepRows;
-    // A sequence of more than one row per head has its weights recomputed (kept scores would outgrow K).
+    // With more rows than a tile has the scores would outgrow K itself: they are taken again instead.
     p.scores = o->weights_out && all_rows <= 16;
-    p.row_cap = p.max_rows;
-    // Parts: about 4 workgroups of the step kernel per CU, of 128 to 4,096 tokens each (a ragged batch's longest
-    // sequence must not be one workgroup's).
-    const int64_t tile = step_tile_rows(p.max_rows, static_cast<int>(D)), tiles = (p.max_rows + tile - 1) / tile;
-    int64_t longest = batch->max_len;
-    if (o->window > 0)
-        longest = std::min<int64_t>(longest, static_cast<int64_t>(o->window) + p.max_rows / group + 31);
-    longest = std::max<int64_t>(longest, 1);
-    const int64_t wanted = (1024 + sequences * H * tiles - 1) / (sequences * H * tiles);
-    p.split_len = static_cast<int32_t>(
-        std::min<int64_t>(4096, round_up((longest + wanted - 1) / wanted, 128)));
-    p.splits = static_cast<int32_t>((longest + p.split_len - 1) / p.split_len);
+    const auto longest = [&](int64_t queries) {  // tokens that a tile of rows sees
+        const int64_t window = o->window > 0 ? o->window + queries + 31 : batch->max_len;
+        return std::min<int64_t>(window, batch->max_len);
+    };
+    // The step kernel: about 4 workgroups per CU, of 128 to 4,096 tokens (a ragged batch's longest sequence must not
+    // be one workgroup's).
+    const int64_t tile = step_tile_rows(p.max_rows, static_cast<int>(D));
+    p.step_parts = parts_for(longest(kStepRows), heads * ((p.max_rows + tile - 1) / tile), 1024, 128, 4096, p.max_rows);
+    if (p.tail) {
+        // The tail kernel: 2 workgroups per CU, of no fewer than 512 tokens.
+        const int64_t tiles = (all_rows + kTailRows - 1) / kTailRows;
+        p.tail_parts = parts_for(longest(kTailRows), heads * tiles, 512, 512, INT32_MAX - 511, all_rows);
+    }
+    int64_t at = round_up(static_cast<int64_t>(batch->num_queries) * q->heads * 4, 16);
+    const auto take = [&](int64_t bytes) {
+        const int64_t here = at;
+        at += round_up(bytes, 16);
+        return here;
+    };
+    const auto slots = [&](const Parts &x) { return x.splits > 1 ? heads * x.row_cap * x.splits : 0; };
+    p.step_stats = take(slots(p.step_parts) * 8);
+    p.step_sums = take(slots(p.step_parts) * D * 4);
+    p.tail_stats = take(slots(p.tail_parts) * 8);
+    p.tail_sums = take(slots(p.tail_parts) * D * 4);
     p.score_len = round_up(batch->max_len, 32);
-    const int64_t slots = sequences * H * p.row_cap;
-    p.lse_at = 0;
-    p.stats_at = round_up(static_cast<int64_t>(batch->num_queries) * q->heads * 4, 16);
-    p.sums_at = p.stats_at + (p.splits > 1 ? round_up(slots * p.splits * 8, 16) : 0);
-    p.scores_at = p.sums_at + (p.splits > 1 ? slots * p.splits * D * 4 : 0);
-    p.bytes = p.scores_at + (p.scores ? slots * p.score_len * 4 : 0);
+    p.scores_at = take(p.scores ? heads * all_rows * p.score_len * 4 : 0);
+    p.bytes = at;
     return p;
 }
 
@@ -259,14 +155,16 @@ kv_status attend(const kv_cache *cache, int32_t layer, const kv_batch *batch, co
     a.q = Rows{static_cast<uint8_t *>(q->data), q->token_stride * 2, q->head_stride * 2};
     a.out = Rows{static_cast<uint8_t *>(out->data), out->token_stride * 2, out->head_stride * 2};
     uint8_t *space = static_cast<uint8_t *>(workspace);
-    a.lse = lse ? lse : reinterpret_cast<float *>(space + plan.lse_at);
-    a.split_len = plan.split_len;
-    a.splits = plan.splits;
-    a.row_cap = plan.row_cap;
-    a.part_stats = reinterpret_cast<float *>(space + plan.stats_at);
-    a.part_sums = reinterpret_cast<float *>(space + plan.sums_at);
-    a.scores = plan.scores ? reinterpret_cast<float *>(space + plan.scores_at) : nullptr;
+    a.lse = lse ? lse : reinterpret_cast<float *>(space);
+    const auto at = [&](int64_t offset) { return reinterpret_cast<float *>(space + offset); };
+    Parts step = plan.step_parts, tail = plan.tail_parts;
+    step.stats = at(plan.step_stats);
+    step.sums = at(plan.step_sums);
+    tail.stats = at(plan.tail_stats);
+    tail.sums = at(plan.tail_sums);
+    a.scores = plan.scores ? at(plan.scores_at) : nullptr;
     a.score_len = plan.score_len;
+    a.score_cap = plan.max_rows;
     a.slopes = o->slopes;
     a.weights_in = o->weights_in;
     a.weights_out = o->weights_out;
@@ -284,20 +182,18 @@ kv_status attend(const kv_cache *cache, int32_t layer, const kv_batch *batch, co
     a.cache_type = o->cache_dtype;
     a.by_group = divisor(a.group);
     if (plan.max_queries > 0) {
-        KVX_HIP(launch_step(a, plan.max_queries, stream));
+        KVX_HIP(launch_step(a, step, plan.max_queries, stream));
+        if (step.splits > 1)
+            KVX_HIP(launch_join(a, step, std::min(plan.max_queries, kStepRows), 1, kStepRows,
+                                step_tile_rows(plan.max_rows, cache->layout.head_dim), stream));
         if (plan.tail) {
-            const dim3 grid(static_cast<uint32_t>(plan.max_queries), static_cast<uint32_t>(q->heads),
-                            static_cast<uint32_t>(batch->num_seqs));
-            hipLaunchKernelGGL(attend_kernel, grid, dim3(256), 0, stream, a);
-            KVX_HIP(hipGetLastError());
+            KVX_HIP(launch_tail(a, tail, plan.max_queries, stream));
+            if (tail.splits > 1)
+                KVX_HIP(launch_join(a, tail, plan.max_queries, kStepRows + 1, INT32_MAX, kTailRows, stream));
         }
     }
-    if (a.weights_out && !a.scores && batch->max_len > 0) {
-        const dim3 grid(static_cast<uint32_t>((batch->max_len + 63) / 64), static_cast<uint32_t>(a.pages.H),
-                        static_cast<uint32_t>(batch->num_seqs));
-        hipLaunchKernelGGL(weigh_kernel, grid, dim3(64), 0, stream, a);
-        KVX_HIP(hipGetLastError());
-    }
+    if (a.weights_out && batch->max_len > 0)
+        KVX_HIP(a.scores ? launch_weigh_step(a, stream) : launch_weigh(a, stream));
     return KV_OK;
 }
 

@@ -5,6 +5,9 @@
 
 namespace kvx {
 
+// Rows of a workgroup of the tail kernel.
+constexpr int kTailRows = 128;
+
 // Sequences of at most this many (new token, query head) rows per KV head go to the step kernel, others to the tail one.
 constexpr int kStepRows = 64;
 
@@ -20,16 +23,20 @@ struct AttendArgs {
     int32_t window, heads, group, num_seqs;
     Divisor by_group;
     int32_t q_type, cache_type;
-    // The step kernel's split of a sequence's tokens and what its parts leave for the join (workspace).
-    int32_t split_len, splits;  // tokens of a part; most parts of a sequence
-    int32_t row_cap;            // most rows per KV head of a sequence that has parts or scores
-    float *part_sums;           // [sequence][KV head][row_cap][splits][D], unscaled
-    float *part_stats;          // [sequence][KV head][row_cap][splits][2]: largest score and sum, in powers of 2
-    float *scores;              // [sequence][KV head][row_cap][score_len] in powers of 2, for weights_out; or NULL
+    float *scores;  // [sequence][KV head][score_cap][score_len] in powers of 2, for weights_out; or NULL
     int64_t score_len;
+    int32_t score_cap;
 };
 
-// Tokens that rows [row0, row1) of a sequence see between them: [first, end); parts start at `start`.
+// How a kernel splits a sequence's tokens over workgroups, and what the parts of a row leave for the join.
+struct Parts {
+    int32_t len, splits;  // tokens of a part; most parts of a row
+    int32_t row_cap;      // most rows per KV head of a sequence
+    float *sums;          // [sequence][KV head][row_cap][splits][D], unscaled
+    float *stats;         // [sequence][KV head][row_cap][splits][2]: largest score and sum, in powers of 2
+};
+
+// Tokens that the new tokens [i0, i1) of a sequence see between them: [first, end); parts start at `start`.
 struct Span {
     int first, start, end;
 };
@@ -46,8 +53,8 @@ __host__ __device__ __forceinline__ Span span_of(int n, int nq, int i0, int i1, 
 // Rows of a tile of the step kernel.
 inline int step_tile_rows(int max_rows, int head_dim) { return max_rows > 16 && head_dim <= 128 ? 32 : 16; }
 
-__device__ __forceinline__ int parts_of(const Span &s, int split_len) {
-    return s.end > s.start ? (s.end - s.start + split_len - 1) / split_len : 1;
+__device__ __forceinline__ int parts_of(const Span &s, int len) {
+    return s.end > s.start ? (s.end - s.start + len - 1) / len : 1;
 }
 
 // Two-byte element types on the matrix cores.  kShift: weights are exp2(s - m + kShift), and m is at least the largest
@@ -110,6 +117,14 @@ __device__ __forceinline__ float capped(float x, float inv, float cap) {
     return cap * (t < 0.25f ? series : copysignf(far, y));
 }
 
-hipError_t launch_step(const AttendArgs &a, int max_queries, hipStream_t stream);
+// Each covers the sequences of its kind only, whatever else is in the batch.
+hipError_t launch_step(const AttendArgs &a, const Parts &parts, int max_queries, hipStream_t stream);
+hipError_t launch_tail(const AttendArgs &a, const Parts &parts, int max_queries, hipStream_t stream);
+// Joins the parts of rows in sequences of min_rows to max_rows rows per KV head, cut in tiles of tile_rows.
+hipError_t launch_join(const AttendArgs &a, const Parts &parts, int max_queries, int min_rows, int max_rows,
+                       int tile_rows, hipStream_t stream);
+// weights_out, from the scores that the step kernel left, or with the scores taken again.
+hipError_t launch_weigh_step(const AttendArgs &a, hipStream_t stream);
+hipError_t launch_weigh(const AttendArgs &a, hipStream_t stream);
 
 }  // namespace kvx

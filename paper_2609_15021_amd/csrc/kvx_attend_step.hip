@@ -56,7 +56,7 @@ struct Vec<16> {
 
 // T: type of q, of the weights and of out; FP8: the cache holds e4m3; DP >= D columns; NT: tiles of 16 rows.
 template <class T, bool FP8, int DP, int NT>
-__global__ __launch_bounds__(64 * kWaves) void step_kernel(const AttendArgs a) {
+__global__ __launch_bounds__(64 * kWaves) void step_kernel(const AttendArgs a, const Parts parts_to) {
     constexpr int E = FP8 ? 1 : 2;                       // bytes of a cached element
     constexpr int KC = DP * E / 64;                      // 16-byte pieces of a token's K in a lane
     constexpr int VE = DP / 16 * E > 16 ? 16 / E : DP / 16;  // V columns of a lane in a piece
@@ -73,15 +73,16 @@ __global__ __launch_bounds__(64 * kWaves) void step_kernel(const AttendArgs a) {
         return;
     const int i0 = divide(row0, a.by_group), i1 = divide(min(row0 + 16 * NT, rows) - 1, a.by_group) + 1;
     const Span span = span_of(seq.n, seq.nq, i0, i1, a.window);
-    const int begin = span.start + split * a.split_len;
+    const int begin = span.start + split * parts_to.len;
     if (split > 0 && begin >= span.end)
         return;
-    const int stop = min(span.end, begin + a.split_len);
-    const bool whole = span.end - span.start <= a.split_len;  // no other part
+    const int stop = min(span.end, begin + parts_to.len);
+    const bool whole = span.end - span.start <= parts_to.len;  // no other part
     const int p_first = seq.n - seq.nq + i0;
     const int low_last = a.window > 0 ? span.end - a.window : 0;  // from here on every row's window is open
 
-    const int64_t slot0 = (static_cast<int64_t>(b) * pg.H + h) * a.row_cap + row0;
+    const int64_t slot0 = (static_cast<int64_t>(b) * pg.H + h) * parts_to.row_cap + row0;
+    const int64_t score0 = (static_cast<int64_t>(b) * pg.H + h) * a.score_cap + row0;
 
     // Queries: a row's elements in the order in which K's pieces hold them.
     u32x4 qf[NT][KC * 2 / E];
@@ -243,7 +244,7 @@ __global__ __launch_bounds__(64 * kWaves) void step_kernel(const AttendArgs a) {
                         x[e] = -INFINITY;
                 }
                 if (a.scores && row0 + nt * 16 + c < rows) {
-                    float *to = a.scores + (slot0 + nt * 16 + c) * a.score_len + base + g * 8;
+                    float *to = a.scores + (score0 + nt * 16 + c) * a.score_len + base + g * 8;
                     *reinterpret_cast<f32x4 *>(to) = f32x4{x[0], x[1], x[2], x[3]};
                     *reinterpret_cast<f32x4 *>(to + 4) = f32x4{x[4], x[5], x[6], x[7]};
                 }
@@ -356,7 +357,7 @@ __global__ __launch_bounds__(64 * kWaves) void step_kernel(const AttendArgs a) {
         if (r >= rows)
             continue;
         const int i = divide(r, a.by_group), head = h * a.group + r - i * a.group, row = seq.q0 + i;
-        const int64_t slot = (slot0 + nt * 16 + c) * a.splits + split;
+        const int64_t slot = (slot0 + nt * 16 + c) * parts_to.splits + split;
         const float inv = total[nt] == 0.f ? 0.f : a.v_scale / total[nt];
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
@@ -379,7 +380,7 @@ __global__ __launch_bounds__(64 * kWaves) void step_kernel(const AttendArgs a) {
                     *reinterpret_cast<u32x2 *>(to + 2 * j) = u32x2{T::pack(x[j] * inv, x[j + 1] * inv),
                                                                     T::pack(x[j + 2] * inv, x[j + 3] * inv)};
             } else {
-                float *to = a.part_sums + slot * pg.D + d;
+                float *to = parts_to.sums + slot * pg.D + d;
 #pragma unroll
                 for (int j = 0; j < VE; j += 4)
                     *reinterpret_cast<f32x4 *>(to + j) = f32x4{x[j], x[j + 1], x[j + 2], x[j + 3]};
@@ -390,8 +391,8 @@ __global__ __launch_bounds__(64 * kWaves) void step_kernel(const AttendArgs a) {
                 a.lse[static_cast<int64_t>(row) * a.heads + head] =
                     total[nt] == 0.f ? -INFINITY : (most[nt] - T::kShift + __builtin_amdgcn_logf(total[nt])) * kLn2;
             } else {
-                a.part_stats[slot * 2] = most[nt] - T::kShift;
-                a.part_stats[slot * 2 + 1] = total[nt];
+                parts_to.stats[slot * 2] = most[nt] - T::kShift;
+                parts_to.stats[slot * 2 + 1] = total[nt];
             }
         }
     }
@@ -399,22 +400,24 @@ __global__ __launch_bounds__(64 * kWaves) void step_kernel(const AttendArgs a) {
 
 // The parts of a row joined: sum_s 2^(m_s - m) x_s / sum_s 2^(m_s - m) l_s.  One row and head per workgroup; 4 columns
 // per lane, the parts spread over the lanes' groups.
-__global__ __launch_bounds__(256) void join_kernel(const AttendArgs a, const int tile_rows) {
+__global__ __launch_bounds__(256) void join_kernel(const AttendArgs a, const Parts from, const int min_rows, const int max_rows,
+                                                    const int tile_rows) {
     __shared__ float sums[256][4];
     __shared__ float shared_stats[2];
     const int b = blockIdx.z, head = blockIdx.y, i = blockIdx.x, h = divide(head, a.by_group);
     Sequence seq;
-    if (!sequence(a.batch, b, a.pages.err, seq) || i >= seq.nq || seq.nq * a.group > kStepRows)
+    if (!sequence(a.batch, b, a.pages.err, seq) || i >= seq.nq || seq.nq * a.group < min_rows ||
+        seq.nq * a.group > max_rows)
         return;
     // The parts are those of the row's tile.
     const int r = i * a.group + head - h * a.group, rows = seq.nq * a.group, row0 = r - r % tile_rows;
     const Span span = span_of(seq.n, seq.nq, divide(row0, a.by_group),
                               divide(min(row0 + tile_rows, rows) - 1, a.by_group) + 1, a.window);
-    const int parts = parts_of(span, a.split_len), D = a.pages.D, tid = threadIdx.x;
+    const int parts = parts_of(span, from.len), D = a.pages.D, tid = threadIdx.x;
     if (parts == 1)
         return;
-    const int64_t slot = ((static_cast<int64_t>(b) * a.pages.H + h) * a.row_cap + r) * a.splits;
-    const float *stats = a.part_stats + slot * 2;
+    const int64_t slot = ((static_cast<int64_t>(b) * a.pages.H + h) * from.row_cap + r) * from.splits;
+    const float *stats = from.stats + slot * 2;
     if (tid < 64) {
         float most = kLowest;
         for (int s = tid; s < parts; s += 64)
@@ -437,7 +440,7 @@ __global__ __launch_bounds__(256) void join_kernel(const AttendArgs a, const int
     f32x4 x{0.f, 0.f, 0.f, 0.f};
     if (part0 < groups)
         for (int s = part0; s < parts; s += groups)
-            x += *reinterpret_cast<const f32x4 *>(a.part_sums + (slot + s) * D + d) *
+            x += *reinterpret_cast<const f32x4 *>(from.sums + (slot + s) * D + d) *
                  __builtin_amdgcn_exp2f(stats[2 * s] - most);
     for (int k = 0; k < 4; ++k)
         sums[tid][k] = x[k];
@@ -463,7 +466,7 @@ __global__ __launch_bounds__(256) void join_kernel(const AttendArgs a, const int
 __global__ __launch_bounds__(256) void weigh_step_kernel(const AttendArgs a) {
     const int b = blockIdx.z, h = blockIdx.y, t = blockIdx.x * 256 + threadIdx.x;
     Sequence seq;
-    if (!sequence(a.batch, b, a.pages.err, seq) || seq.nq * a.group > kStepRows || t >= seq.n)
+    if (!sequence(a.batch, b, a.pages.err, seq) || t >= seq.n)
         return;
     float sum = 0.f;
     for (int i = 0; i < seq.nq; ++i) {
@@ -471,7 +474,7 @@ __global__ __launch_bounds__(256) void weigh_step_kernel(const AttendArgs a) {
         if (t > p || (a.window > 0 && p - t >= a.window))
             continue;
         const int64_t at = static_cast<int64_t>(seq.q0 + i) * a.heads + h * a.group;
-        const int64_t slot = (static_cast<int64_t>(b) * a.pages.H + h) * a.row_cap + i * a.group;
+        const int64_t slot = (static_cast<int64_t>(b) * a.pages.H + h) * a.score_cap + i * a.group;
         for (int k = 0; k < a.group; ++k) {
             const float lse = a.lse[at + k];
             if (lse != -INFINITY)
@@ -483,42 +486,46 @@ __global__ __launch_bounds__(256) void weigh_step_kernel(const AttendArgs a) {
 }
 
 template <class T, bool FP8, int DP, int NT>
-void launch(const AttendArgs &a, int max_rows, hipStream_t stream) {
+void launch(const AttendArgs &a, const Parts &parts, int max_rows, hipStream_t stream) {
     const int tiles = (max_rows + 16 * NT - 1) / (16 * NT);
-    hipLaunchKernelGGL((step_kernel<T, FP8, DP, NT>), dim3(a.splits, tiles * a.pages.H, a.num_seqs), dim3(64 * kWaves), 0,
-                       stream, a);
+    hipLaunchKernelGGL((step_kernel<T, FP8, DP, NT>), dim3(parts.splits, tiles * a.pages.H, a.num_seqs),
+                       dim3(64 * kWaves), 0, stream, a, parts);
 }
 
 template <class T, bool FP8>
-void launch(const AttendArgs &a, int max_rows, hipStream_t stream) {
+void launch(const AttendArgs &a, const Parts &parts, int max_rows, hipStream_t stream) {
     const bool two = step_tile_rows(max_rows, a.pages.D) == 32;
     if (a.pages.D > 128)
-        launch<T, FP8, 256, 1>(a, max_rows, stream);
+        launch<T, FP8, 256, 1>(a, parts, max_rows, stream);
     else if (a.pages.D > 64)
-        two ? launch<T, FP8, 128, 2>(a, max_rows, stream) : launch<T, FP8, 128, 1>(a, max_rows, stream);
+        two ? launch<T, FP8, 128, 2>(a, parts, max_rows, stream) : launch<T, FP8, 128, 1>(a, parts, max_rows, stream);
     else
-        two ? launch<T, FP8, 64, 2>(a, max_rows, stream) : launch<T, FP8, 64, 1>(a, max_rows, stream);
+        two ? launch<T, FP8, 64, 2>(a, parts, max_rows, stream) : launch<T, FP8, 64, 1>(a, parts, max_rows, stream);
 }
 
 }  // namespace
 
-hipError_t launch_step(const AttendArgs &a, int max_queries, hipStream_t stream) {
+hipError_t launch_step(const AttendArgs &a, const Parts &parts, int max_queries, hipStream_t stream) {
     const int max_rows = static_cast<int>(std::min<int64_t>(kStepRows, static_cast<int64_t>(max_queries) * a.group));
     const bool fp8 = a.cache_type == KV_DTYPE_E4M3;
     if (a.q_type == KV_DTYPE_BF16)
-        fp8 ? launch<Bf16, true>(a, max_rows, stream) : launch<Bf16, false>(a, max_rows, stream);
+        fp8 ? launch<Bf16, true>(a, parts, max_rows, stream) : launch<Bf16, false>(a, parts, max_rows, stream);
     else
-        fp8 ? launch<F16, true>(a, max_rows, stream) : launch<F16, false>(a, max_rows, stream);
-    const uint32_t queries = static_cast<uint32_t>(std::min(max_queries, kStepRows));
-    if (a.splits > 1) {
-        const int tile_rows = step_tile_rows(max_rows, a.pages.D);
-        hipLaunchKernelGGL(join_kernel, dim3(queries, static_cast<uint32_t>(a.heads), static_cast<uint32_t>(a.num_seqs)),
-                           dim3(256), 0, stream, a, tile_rows);
-    }
-    if (a.scores)
-        hipLaunchKernelGGL(weigh_step_kernel, dim3(static_cast<uint32_t>((a.batch.max_len + 255) / 256),
-                                                   static_cast<uint32_t>(a.pages.H), static_cast<uint32_t>(a.num_seqs)),
-                           dim3(256), 0, stream, a);
+        fp8 ? launch<F16, true>(a, parts, max_rows, stream) : launch<F16, false>(a, parts, max_rows, stream);
+    return hipGetLastError();
+}
+
+hipError_t launch_join(const AttendArgs &a, const Parts &parts, int max_queries, int min_rows, int max_rows,
+                       int tile_rows, hipStream_t stream) {
+    const dim3 grid(static_cast<uint32_t>(max_queries), static_cast<uint32_t>(a.heads), static_cast<uint32_t>(a.num_seqs));
+    hipLaunchKernelGGL(join_kernel, grid, dim3(256), 0, stream, a, parts, min_rows, max_rows, tile_rows);
+    return hipGetLastError();
+}
+
+hipError_t launch_weigh_step(const AttendArgs &a, hipStream_t stream) {
+    const dim3 grid(static_cast<uint32_t>((a.batch.max_len + 255) / 256), static_cast<uint32_t>(a.pages.H),
+                    static_cast<uint32_t>(a.num_seqs));
+    hipLaunchKernelGGL(weigh_step_kernel, grid, dim3(256), 0, stream, a);
     return hipGetLastError();
 }
 

@@ -1,0 +1,458 @@
+// kv_attend for many new tokens of a sequence (a prompt's tail behind a restored prefix, or a whole prompt): bound by
+// the matrix cores and the exponentials between their products.
+//
+// A workgroup takes 128 rows (new token, query head) of one KV head, 32 a wave, so that all query heads of a KV head
+// share what is read of it, and goes over the tokens TK at a time.  K and V of TK tokens lie in LDS, twice: while one is
+// used, the next is on its way through registers, and one barrier a round separates them.  A wave takes S^T = K Q^T and
+// O^T = V^T P^T in 32x32x16 products: a row is a column of both, so its largest score, sum and rescaling stay in a lane
+// (and its neighbour 32 lanes on), and the weights are the second product's operand in the order in which the first
+// leaves them: k-index e of half h of products of 16 tokens is token h * 4 + e for e < 4, and 8 + h * 4 + e - 4 beyond.
+// V's operand in that order is two transposing LDS reads (ds_read_b64_tr_b16: 16 lanes read 4 rows of 16 columns, a lane
+// gets a column).  Rows in LDS are permuted in 16-byte pieces (by token for K, by pairs for V), so that neither kind of
+// read meets a bank twice.
+//
+// e4m3 is widened on its way into LDS, once per workgroup.  Workgroups that share a KV head run on one XCD where the
+// number of heads allows (consecutive workgroups go to consecutive XCDs), and use its L2 together.
+#include <algorithm>
+
+#include "kvx_attend_kernels.h"
+
+namespace kvx {
+
+namespace {
+
+constexpr int kWaves = 4;
+constexpr int kRows = 32 * kWaves;
+static_assert(kRows == kTailRows, "a wave takes 32 rows");
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ f32x16 mfma_32x32x16(const u32x4 &a, const u32x4 &b, const f32x16 &c, Bf16) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(Bf16::frag, a), __builtin_bit_cast(Bf16::frag, b),
+                                                   c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 mfma_32x32x16(const u32x4 &a, const u32x4 &b, const f32x16 &c, F16) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(F16::frag, a), __builtin_bit_cast(F16::frag, b), c,
+                                                  0, 0, 0);
+}
+
+typedef __attribute__((address_space(3))) uint8_t lds_byte;
+
+__device__ __forceinline__ u32x2 read_turned(lds_byte *p) {
+    return __builtin_bit_cast(u32x2,
+                              __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<__attribute__((address_space(3))) s16x4 *>(p)));
+}
+
+// The largest and the sum over a lane and the one 32 lanes on.
+__device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
+
+template <class T, bool FP8, int DP, int TK>
+__global__ __launch_bounds__(64 * kWaves, 2) void tail_kernel(const AttendArgs a, const Parts parts, const int tiles) {
+    constexpr int E = FP8 ? 1 : 2;
+    constexpr int ROW = 2 * DP;                     // bytes of a row in LDS
+    constexpr int GC = DP * E / 16;                 // 16-byte pieces of a cached row
+    constexpr int RP = 64 * kWaves / GC;            // rows that the workgroup loads at once
+    constexpr int NP = TK / RP;                     // times
+    constexpr int KM = DP / 8 < 16 ? DP / 8 - 1 : 15, VM = DP / 16 < 8 ? DP / 16 - 1 : 7;  // permutations' masks
+    constexpr int TB = TK / 32, KS = DP / 16, DB = DP / 32;
+    static_assert(TK % RP == 0, "whole rounds of loads");
+    __shared__ __align__(16) uint8_t lds[2][2][TK * ROW];  // [round][K, V]
+
+    const Pages &pg = a.pages;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane & 31, half = lane >> 5;
+    const int groups = a.num_seqs * pg.H, group = blockIdx.x % groups, item = blockIdx.x / groups;
+    const int b = group / pg.H, h = group - b * pg.H;
+    const int split = item % parts.splits, tile = tiles - 1 - item / parts.splits;  // the longest first
+    Sequence seq;
+    if (!sequence(a.batch, b, pg.err, seq))
+        return;
+    const int rows = seq.nq * a.group, row0 = tile * kRows;
+    if (row0 >= rows || rows <= kStepRows)
+        return;
+    const int i0 = divide(row0, a.by_group), i1 = divide(min(row0 + kRows, rows) - 1, a.by_group) + 1;
+    const Span span = span_of(seq.n, seq.nq, i0, i1, a.window);
+    const int begin = span.start + split * parts.len;
+    if (split > 0 && begin >= span.end)
+        return;
+    const int stop = min(span.end, begin + parts.len);
+    const bool whole = span.end - span.start <= parts.len;
+
+    // This lane's row: its query as the first product's operand, and what it sees.
+    const int r = row0 + wave * 32 + c;
+    const bool row_ok = r < rows;
+    const int row_i = divide(min(r, rows - 1), a.by_group), head = h * a.group + min(r, rows - 1) - row_i * a.group;
+    const int p_row = row_ok ? seq.n - seq.nq + row_i : -1;
+    const int wave_r0 = min(row0 + wave * 32, rows - 1), wave_r1 = min(row0 + wave * 32 + 31, rows - 1);
+    const int p_first = seq.n - seq.nq + divide(wave_r0, a.by_group), p_last = seq.n - seq.nq + divide(wave_r1, a.by_group);
+    const int low_last = a.window > 0 ? p_last + 1 - a.window : 0;
+    const int low_first = a.window > 0 ? p_first + 1 - a.window : 0;
+    const bool idle = row0 + wave * 32 >= rows;
+    const float slope = a.slopes ? a.slopes[head] * kLog2e : 0.f;
+    const float scale = a.scale * kLog2e;
+    const bool plain = a.softcap == 0.f && !a.slopes;
+    u32x4 qf[KS];
+    {
+        const uint8_t *q = a.q.data + (seq.q0 + row_i) * a.q.token_stride + head * a.q.head_stride;
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+            const int d = k * 16 + half * 8;
+            qf[k] = row_ok && d < pg.D ? *reinterpret_cast<const u32x4 *>(q + 2 * d) : u32x4{0, 0, 0, 0};
+        }
+    }
+
+    const int32_t *table = a.batch.tables + b * a.batch.table_stride;
+    const uint8_t *cache = pg.base + static_cast<uint32_t>(h) * pg.head_bytes;
+    const int piece = tid % GC, first_row = tid / GC;
+    const bool piece_ok = piece * 16 < pg.row_bytes;
+    const int piece_at = piece_ok ? piece * 16 : 0;
+
+    // Lanes look up a round's tokens (lane % TK each): the page's block, then where the token's row is; -1 for a token
+    // that takes part in nothing.
+    auto block_at = [&](int base, int &page, bool &shown) {
+        const int t = base + (lane & (TK - 1));
+        page = divide(t, pg.by_bs);
+        shown = t < stop && t >= span.first;
+        return shown ? table[page] : 0;
+    };
+    auto offset_at = [&](int base, int page, bool shown, int block) -> int64_t {
+        if (!shown || !in_cache(pg, block))
+            return -1;
+        return block * pg.block_stride + static_cast<uint32_t>(base + (lane & (TK - 1)) - page * pg.BS) * pg.token_bytes;
+    };
+    u32x4 k_next[NP], v_next[NP];
+    auto request = [&](int64_t off) {
+#pragma unroll
+        for (int n = 0; n < NP; ++n) {
+            const int src = first_row + n * RP;
+            const uint32_t lo = __shfl(static_cast<uint32_t>(off), src), hi = __shfl(static_cast<uint32_t>(off >> 32), src);
+            const int64_t at = static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo);
+            const uint8_t *x = cache + max(at, int64_t{0}) + piece_at;
+            k_next[n] = *reinterpret_cast<const u32x4 *>(x);
+            v_next[n] = *reinterpret_cast<const u32x4 *>(x + pg.v_bytes);
+            // Slots without a token and columns beyond D may hold anything: 0 times it need not be 0.
+            if (at < 0 || !piece_ok) {
+                k_next[n] = u32x4{0, 0, 0, 0};
+                v_next[n] = u32x4{0, 0, 0, 0};
+            }
+        }
+    };
+    auto deposit = [&](int buffer) {
+#pragma unroll
+        for (int n = 0; n < NP; ++n) {
+            const int t = first_row + n * RP;
+            uint8_t *k = lds[buffer][0] + t * ROW, *v = lds[buffer][1] + t * ROW;
+            const int ks = t & KM, vs = 2 * (t & VM);
+            if constexpr (FP8) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const uint32_t x0 = k_next[n][2 * j], x1 = k_next[n][2 * j + 1];
+                    const uint32_t y0 = v_next[n][2 * j], y1 = v_next[n][2 * j + 1];
+                    *reinterpret_cast<u32x4 *>(k + ((2 * piece + j) ^ ks) * 16) =
+                        u32x4{T::from_e4m3(x0, false), T::from_e4m3(x0, true), T::from_e4m3(x1, false), T::from_e4m3(x1, true)};
+                    *reinterpret_cast<u32x4 *>(v + ((2 * piece + j) ^ vs) * 16) =
+                        u32x4{T::from_e4m3(y0, false), T::from_e4m3(y0, true), T::from_e4m3(y1, false), T::from_e4m3(y1, true)};
+                }
+            } else {
+                *reinterpret_cast<u32x4 *>(k + (piece ^ ks) * 16) = k_next[n];
+                *reinterpret_cast<u32x4 *>(v + (piece ^ vs) * 16) = v_next[n];
+            }
+        }
+    };
+
+    f32x16 acc[DB];
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int x = 0; x < 16; ++x)
+            acc[d][x] = 0.f;
+    float m = kLowest, l = 0.f;
+
+    // Where this lane reads: K's row c of 32 (its piece of product k is (2 * k + half) ^ swizzle), and V's 8 bytes of
+    // row half * 4 + lane / 4 % 4 of 8, columns lane / 16 % 2 * 16 + lane % 4 * 4 of 32.
+    const int k_at = c * ROW, k_swizzle = c & KM;
+    const int v_row = half * 4 + (lane >> 2 & 3), v_piece = (lane >> 4 & 1) * 2 + (lane >> 1 & 1);
+    const int v_swizzle = 2 * (v_row & VM);
+    int v_at[DB];
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+        v_at[d] = v_row * ROW + ((d * 4 + v_piece) ^ v_swizzle) * 16 + (lane & 1) * 8;
+
+    if (begin < stop) {
+        int page, next_page = 0, next_block = 0, buffer = 0;
+        bool shown, next_shown = false;
+        const int block = block_at(begin, page, shown);
+        int64_t off = offset_at(begin, page, shown, block);
+        if (stop - begin > TK)
+            next_block = block_at(begin + TK, next_page, next_shown);
+        request(off);
+        deposit(0);
+        __syncthreads();
+        for (int base = begin;; base += TK, buffer ^= 1) {
+            const uint64_t usable = __ballot(off >= 0);
+            const bool more = stop - base > TK;
+            if (more) {
+                off = offset_at(base + TK, next_page, next_shown, next_block);
+                request(off);
+                if (stop - base > 2 * TK)
+                    next_block = block_at(base + 2 * TK, next_page, next_shown);
+            }
+            // A wave whose rows see nothing of these tokens has only helped to load them.
+            if (!idle && base <= p_last && base + (TK - 1) >= low_first) {
+                const uint8_t *k_lds = lds[buffer][0];
+                f32x16 s[TB];
+#pragma unroll
+                for (int t = 0; t < TB; ++t) {
+#pragma unroll
+                    for (int x = 0; x < 16; ++x)
+                        s[t][x] = 0.f;
+#pragma unroll
+                    for (int k = 0; k < KS; ++k) {
+                        const u32x4 x = *reinterpret_cast<const u32x4 *>(k_lds + t * 32 * ROW + k_at +
+                                                                         ((2 * k + half) ^ k_swizzle) * 16);
+                        s[t] = mfma_32x32x16(x, qf[k], s[t], T{});
+                    }
+                }
+                const bool edge = usable != ~uint64_t{0} || p_first - base < TK - 1 || base < low_last;
+                // Scores in powers of 2; in the plain case the factor is left to the exponent's argument.
+                const float factor = plain ? scale : 1.f;
+                if (!plain) {
+                    const float inv = a.scale / a.softcap, cap = a.softcap * kLog2e;
+#pragma unroll
+                    for (int t = 0; t < TB; ++t)
+#pragma unroll
+                        for (int x = 0; x < 16; ++x) {
+                            float y = a.softcap > 0.f ? capped(s[t][x], inv, cap) : s[t][x] * scale;
+                            if (a.slopes)
+                                y -= slope * static_cast<float>(p_row - (base + t * 32 + 8 * (x >> 2) + half * 4 + (x & 3)));
+                            s[t][x] = y;
+                        }
+                }
+                if (edge) {
+#pragma unroll
+                    for (int t = 0; t < TB; ++t)
+#pragma unroll
+                        for (int x = 0; x < 16; ++x) {
+                            const int at = t * 32 + 8 * (x >> 2) + half * 4 + (x & 3), token = base + at;
+                            if (!(usable >> at & 1) || token > p_row || (a.window > 0 && p_row - token >= a.window))
+                                s[t][x] = -INFINITY;
+                        }
+                }
+                float top = -INFINITY;
+#pragma unroll
+                for (int t = 0; t < TB; ++t)
+#pragma unroll
+                    for (int x = 0; x < 16; x += 2)
+                        top = fmaxf(fmaxf(top, s[t][x]), s[t][x + 1]);
+                top *= factor;
+                if (__any(top > m + 8.f)) {
+                    const float next = fmaxf(m, fmaxf(top, other_half(top))), f = __builtin_amdgcn_exp2f(m - next);
+                    m = next;
+                    l *= f;
+#pragma unroll
+                    for (int d = 0; d < DB; ++d)
+#pragma unroll
+                        for (int x = 0; x < 16; ++x)
+                            acc[d][x] *= f;
+                }
+                const float zero = m - T::kShift;
+                u32x4 p[TB][2];
+                float sums[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int t = 0; t < TB; ++t)
+#pragma unroll
+                    for (int x = 0; x < 16; x += 2) {
+                        const float e0 = __builtin_amdgcn_exp2f(fmaf(s[t][x], factor, -zero));
+                        const float e1 = __builtin_amdgcn_exp2f(fmaf(s[t][x + 1], factor, -zero));
+                        sums[x & 2] += e0;
+                        sums[(x & 2) + 1] += e1;
+                        p[t][x >> 3][x >> 1 & 3] = T::pack(e0, e1);
+                    }
+                l += (sums[0] + sums[1]) + (sums[2] + sums[3]);
+                lds_byte *v_lds = (lds_byte *)(lds[buffer][1]);  // (a cast between address spaces)
+#pragma unroll
+                for (int d = 0; d < DB; ++d)
+#pragma unroll
+                    for (int t = 0; t < TB; ++t)
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            const int at = (t * 32 + j * 16) * ROW;
+                            const u32x2 x = read_turned(v_lds + v_at[d] + at), y = read_turned(v_lds + v_at[d] + at + 8 * ROW);
+                            acc[d] = mfma_32x32x16(u32x4{x[0], x[1], y[0], y[1]}, p[t][j], acc[d], T{});
+                        }
+            }
+            if (!more)
+                break;
+            deposit(buffer ^ 1);
+            __syncthreads();
+        }
+    }
+
+    l += other_half(l);
+    if (!row_ok)
+        return;
+    const float inv = l == 0.f ? 0.f : a.v_scale / l;
+    const int64_t slot = ((static_cast<int64_t>(b) * pg.H + h) * parts.row_cap + r) * parts.splits + split;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int x = 0; x < 16; x += 4) {
+            const int col = d * 32 + 2 * x + half * 4;
+            if (col >= pg.D)
+                continue;
+            if (whole) {
+                uint8_t *to = a.out.data + (seq.q0 + row_i) * a.out.token_stride + head * a.out.head_stride + 2 * col;
+                *reinterpret_cast<u32x2 *>(to) = u32x2{T::pack(acc[d][x] * inv, acc[d][x + 1] * inv),
+                                                        T::pack(acc[d][x + 2] * inv, acc[d][x + 3] * inv)};
+            } else {
+                *reinterpret_cast<f32x4 *>(parts.sums + slot * pg.D + col) =
+                    f32x4{acc[d][x], acc[d][x + 1], acc[d][x + 2], acc[d][x + 3]};
+            }
+        }
+    if (half == 0) {
+        if (whole) {
+            a.lse[static_cast<int64_t>(seq.q0 + row_i) * a.heads + head] =
+                l == 0.f ? -INFINITY : (m - T::kShift + __builtin_amdgcn_logf(l)) * kLn2;
+        } else {
+            parts.stats[slot * 2] = m - T::kShift;
+            parts.stats[slot * 2 + 1] = l;
+        }
+    }
+}
+
+// What each token received: a wave holds K of 32 tokens, goes over the rows that see them, 32 at a time, with their
+// scores taken again, and adds up exp2(s - lse) for each token; a token's 32 partial sums are joined at the end.
+template <class T, bool FP8, int DP>
+__global__ __launch_bounds__(64 * kWaves) void weigh_kernel(const AttendArgs a) {
+    constexpr int KC = DP * (FP8 ? 1 : 2) / 32;  // 16-byte pieces of a token's K in a lane
+    const Pages &pg = a.pages;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 31, half = lane >> 5;
+    const int b = blockIdx.z, h = blockIdx.y, base = (blockIdx.x * kWaves + wave) * 32;
+    Sequence seq;
+    if (!sequence(a.batch, b, pg.err, seq) || base >= seq.n)
+        return;
+    // Rows that see any of the 32 tokens: new tokens from base on, and before the window has closed on the last.
+    const int past = seq.n - seq.nq;
+    const int i0 = max(0, base - past), i1 = a.window > 0 ? min<int64_t>(seq.nq, int64_t{base} + 31 + a.window - past) : seq.nq;
+    const int first_seen = a.window > 0 ? max(0, past + 1 - a.window) : 0;
+    const int t_lane = base + c;
+    float sums[16];
+#pragma unroll
+    for (int x = 0; x < 16; ++x)
+        sums[x] = 0.f;
+    if (i0 < i1) {
+        const bool seen = t_lane < seq.n && t_lane >= first_seen;
+        const int page = divide(t_lane, pg.by_bs);
+        const int block = seen ? a.batch.tables[b * a.batch.table_stride + page] : 0;
+        const bool use = seen && in_cache(pg, block);
+        const uint32_t usable = static_cast<uint32_t>(__ballot(use));
+        const uint8_t *k_row = pg.base + static_cast<uint32_t>(h) * pg.head_bytes +
+                               (use ? block * pg.block_stride + static_cast<uint32_t>(t_lane - page * pg.BS) * pg.token_bytes
+                                    : int64_t{0});
+        u32x4 k_reg[KC];
+#pragma unroll
+        for (int k = 0; k < KC; ++k)
+            k_reg[k] = *reinterpret_cast<const u32x4 *>(k_row + (k * 32 + half * 16 < pg.row_bytes ? k * 32 + half * 16 : 0));
+        const float scale = a.scale * kLog2e;
+        for (int r0 = i0 * a.group; r0 < i1 * a.group; r0 += 32) {
+            const int r = min(r0 + c, i1 * a.group - 1), i = divide(r, a.by_group), head = h * a.group + r - i * a.group;
+            const int p = r0 + c < i1 * a.group ? past + i : -1;
+            const uint8_t *q = a.q.data + (seq.q0 + i) * a.q.token_stride + head * a.q.head_stride;
+            const float lse = a.lse[static_cast<int64_t>(seq.q0 + i) * a.heads + head] * kLog2e;
+            f32x16 s;
+#pragma unroll
+            for (int x = 0; x < 16; ++x)
+                s[x] = 0.f;
+#pragma unroll
+            for (int k = 0; k < KC; ++k) {
+                if constexpr (FP8) {
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const int d = k * 32 + half * 16 + j * 8;
+                        const u32x4 x = d < pg.D ? *reinterpret_cast<const u32x4 *>(q + 2 * d) : u32x4{0, 0, 0, 0};
+                        const uint32_t y0 = k_reg[k][2 * j], y1 = k_reg[k][2 * j + 1];
+                        s = mfma_32x32x16(u32x4{T::from_e4m3(y0, false), T::from_e4m3(y0, true), T::from_e4m3(y1, false),
+                                                T::from_e4m3(y1, true)}, x, s, T{});
+                    }
+                } else {
+                    const int d = k * 16 + half * 8;
+                    s = mfma_32x32x16(k_reg[k], d < pg.D ? *reinterpret_cast<const u32x4 *>(q + 2 * d) : u32x4{0, 0, 0, 0}, s,
+                                      T{});
+                }
+            }
+            const float slope = a.slopes ? a.slopes[head] * kLog2e : 0.f;
+#pragma unroll
+            for (int x = 0; x < 16; ++x) {
+                const int at = 8 * (x >> 2) + half * 4 + (x & 3), t = base + at;
+                float y = a.softcap > 0.f ? capped(s[x], a.scale / a.softcap, a.softcap * kLog2e) : s[x] * scale;
+                if (a.slopes)
+                    y -= slope * static_cast<float>(p - t);
+                const bool sees = (usable >> at & 1) && t <= p && (a.window == 0 || p - t < a.window) && lse != -INFINITY;
+                sums[x] += sees ? __builtin_amdgcn_exp2f(y - lse) : 0.f;
+            }
+        }
+    }
+    // Joined over the 32 columns: lane c ends with the sum of token base + c (of its half's 16).
+#pragma unroll
+    for (int x = 0; x < 16; ++x) {
+#pragma unroll
+        for (int o = 16; o; o >>= 1)
+            sums[x] += __shfl_xor(sums[x], o);
+        const int t = base + 8 * (x >> 2) + half * 4 + (x & 3);
+        if (c == x && t < seq.n) {
+            const int64_t at = b * a.weights_seq_stride + h * a.weights_head_stride + t;
+            a.weights_out[at] = (a.weights_in ? a.weights_in[at] : 0.f) + sums[x];
+        }
+    }
+}
+
+template <class T, bool FP8, int DP, int TK>
+void launch(const AttendArgs &a, const Parts &parts, int max_queries, hipStream_t stream) {
+    const int tiles = static_cast<int>((static_cast<int64_t>(max_queries) * a.group + kRows - 1) / kRows);
+    const uint32_t grid = static_cast<uint32_t>(tiles) * parts.splits * a.pages.H * a.num_seqs;
+    hipLaunchKernelGGL((tail_kernel<T, FP8, DP, TK>), dim3(grid), dim3(64 * kWaves), 0, stream, a, parts, tiles);
+}
+
+template <class T, bool FP8>
+void launch(const AttendArgs &a, const Parts &parts, int max_queries, hipStream_t stream) {
+    if (a.pages.D > 128)
+        launch<T, FP8, 256, 32>(a, parts, max_queries, stream);
+    else if (a.pages.D > 64)
+        launch<T, FP8, 128, 64>(a, parts, max_queries, stream);
+    else
+        launch<T, FP8, 64, 64>(a, parts, max_queries, stream);
+}
+
+template <class T, bool FP8>
+void launch_weigh(const AttendArgs &a, hipStream_t stream) {
+    const dim3 grid(static_cast<uint32_t>((a.batch.max_len + 32 * kWaves - 1) / (32 * kWaves)),
+                    static_cast<uint32_t>(a.pages.H), static_cast<uint32_t>(a.num_seqs));
+    if (a.pages.D > 128)
+        hipLaunchKernelGGL((weigh_kernel<T, FP8, 256>), grid, dim3(64 * kWaves), 0, stream, a);
+    else if (a.pages.D > 64)
+        hipLaunchKernelGGL((weigh_kernel<T, FP8, 128>), grid, dim3(64 * kWaves), 0, stream, a);
+    else
+        hipLaunchKernelGGL((weigh_kernel<T, FP8, 64>), grid, dim3(64 * kWaves), 0, stream, a);
+}
+
+}  // namespace
+
+hipError_t launch_tail(const AttendArgs &a, const Parts &parts, int max_queries, hipStream_t stream) {
+    const bool fp8 = a.cache_type == KV_DTYPE_E4M3;
+    if (a.q_type == KV_DTYPE_BF16)
+        fp8 ? launch<Bf16, true>(a, parts, max_queries, stream) : launch<Bf16, false>(a, parts, max_queries, stream);
+    else
+        fp8 ? launch<F16, true>(a, parts, max_queries, stream) : launch<F16, false>(a, parts, max_queries, stream);
+    return hipGetLastError();
+}
+
+hipError_t launch_weigh(const AttendArgs &a, hipStream_t stream) {
+    const bool fp8 = a.cache_type == KV_DTYPE_E4M3;
+    if (a.q_type == KV_DTYPE_BF16)
+        fp8 ? launch_weigh<Bf16, true>(a, stream) : launch_weigh<Bf16, false>(a, stream);
+    else
+        fp8 ? launch_weigh<F16, true>(a, stream) : launch_weigh<F16, false>(a, stream);
+    return hipGetLastError();
+}
+
+}  // namespace kvx
