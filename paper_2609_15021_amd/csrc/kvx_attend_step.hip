@@ -63,7 +63,8 @@ __global__ __launch_bounds__(64 * kWaves) void step_kernel(const AttendArgs a, c
     constexpr int NV = DP / (16 * VE);                   // such pieces
     constexpr int TILES = NV * VE;                       // 16-column tiles of the output
     const Pages &pg = a.pages;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
+    const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int split = blockIdx.x, tile = blockIdx.y / pg.H, h = blockIdx.y - tile * pg.H, b = blockIdx.z;
     Sequence seq;
     if (!sequence(a.batch, b, pg.err, seq))
@@ -231,17 +232,28 @@ __global__ __launch_bounds__(64 * kWaves) void step_kernel(const AttendArgs a, c
             for (int nt = 0; nt < NT; ++nt) {
                 float x[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
+                for (int e = 0; e < 8; ++e)
                     x[e] = s[nt][e >> 2][e & 3];
-                    if (a.softcap > 0.f)
-                        x[e] = capped(x[e], a.scale / a.softcap, a.softcap * kLog2e);
-                    else
+                if (a.softcap > 0.f) {
+                    const float inv = a.scale / a.softcap, cap = a.softcap * kLog2e;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        x[e] = capped(x[e], inv, cap);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
                         x[e] *= a.scale * kLog2e;
-                    const int t = base + g * 8 + e;
-                    if (a.slopes)
-                        x[e] -= slope[nt] * static_cast<float>(p_of[nt] - t);
-                    if (edge && (!(bits >> e & 1) || t > p_of[nt] || (a.window > 0 && p_of[nt] - t >= a.window)))
-                        x[e] = -INFINITY;
+                }
+                if (a.slopes) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        x[e] -= slope[nt] * static_cast<float>(p_of[nt] - (base + g * 8 + e));
+                }
+                if (edge) {
+                    const int to = p_of[nt] - (base + g * 8) + 1, from = a.window > 0 ? to - a.window : INT32_MIN;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        x[e] = (bits >> e & 1) && e < to && e >= from ? x[e] : -INFINITY;
                 }
                 if (a.scores && row0 + nt * 16 + c < rows) {
                     float *to = a.scores + (score0 + nt * 16 + c) * a.score_len + base + g * 8;

@@ -38,16 +38,35 @@ __device__ __forceinline__ f32x16 mfma_32x32x16(const u32x4 &a, const u32x4 &b, 
 }
 
 typedef __attribute__((address_space(3))) uint8_t lds_byte;
+typedef __attribute__((address_space(1))) const uint8_t global_byte;
+
+// What takes the place of pieces that hold no element.
+__device__ const __align__(16) uint8_t zeros[16] = {};
 
 __device__ __forceinline__ u32x2 read_turned(lds_byte *p) {
     return __builtin_bit_cast(u32x2,
                               __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<__attribute__((address_space(3))) s16x4 *>(p)));
 }
 
+// Asks the compiler to keep `ahead` LDS reads (each `reads` instructions) in flight before the first of `products`
+// products, and to issue one more after each.
+template <int PRODUCTS, int READS, int AHEAD>
+__device__ __forceinline__ void interleave() {
+    constexpr int kProduct = 0x8, kRead = 0x100;
+    __builtin_amdgcn_sched_group_barrier(kRead, AHEAD * READS, 0);
+#pragma unroll
+    for (int i = 0; i < PRODUCTS - AHEAD; ++i) {
+        __builtin_amdgcn_sched_group_barrier(kProduct, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(kRead, READS, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(kProduct, AHEAD, 0);
+}
+
 // The largest and the sum over a lane and the one 32 lanes on.
 __device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
 
-template <class T, bool FP8, int DP, int TK>
+// PLAIN: neither a cap nor slopes.
+template <class T, bool FP8, int DP, int TK, bool PLAIN>
 __global__ __launch_bounds__(64 * kWaves, 2) void tail_kernel(const AttendArgs a, const Parts parts, const int tiles) {
     constexpr int E = FP8 ? 1 : 2;
     constexpr int ROW = 2 * DP;                     // bytes of a row in LDS
@@ -60,7 +79,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void tail_kernel(const AttendArgs a
     __shared__ __align__(16) uint8_t lds[2][2][TK * ROW];  // [round][K, V]
 
     const Pages &pg = a.pages;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = lane & 31, half = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, c = lane & 31, half = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int groups = a.num_seqs * pg.H, group = blockIdx.x % groups, item = blockIdx.x / groups;
     const int b = group / pg.H, h = group - b * pg.H;
     const int split = item % parts.splits, tile = tiles - 1 - item / parts.splits;  // the longest first
@@ -90,7 +110,6 @@ __global__ __launch_bounds__(64 * kWaves, 2) void tail_kernel(const AttendArgs a
     const bool idle = row0 + wave * 32 >= rows;
     const float slope = a.slopes ? a.slopes[head] * kLog2e : 0.f;
     const float scale = a.scale * kLog2e;
-    const bool plain = a.softcap == 0.f && !a.slopes;
     u32x4 qf[KS];
     {
         const uint8_t *q = a.q.data + (seq.q0 + row_i) * a.q.token_stride + head * a.q.head_stride;
@@ -109,24 +128,35 @@ __global__ __launch_bounds__(64 * kWaves, 2) void tail_kernel(const AttendArgs a
 
     // Lanes look up a round's tokens (lane % TK each): the page's block, then where the token's row is; -1 for a token
     // that takes part in nothing.
-    auto block_at = [&](int base, int &page, bool &shown) {
+    // (No branch: beyond the part the last token's entry is read again, and waits are counted, not emptied.)
+    auto block_at = [&](int base) {
         const int t = base + (lane & (TK - 1));
-        page = divide(t, pg.by_bs);
-        shown = t < stop && t >= span.first;
-        return shown ? table[page] : 0;
+        return table[divide(max(min(t, stop - 1), span.first), pg.by_bs)];
     };
-    auto offset_at = [&](int base, int page, bool shown, int block) -> int64_t {
-        if (!shown || !in_cache(pg, block))
+    auto offset_at = [&](int base, int block) -> int64_t {
+        const int t = base + (lane & (TK - 1));
+        if (t >= stop || t < span.first || !in_cache(pg, block))
             return -1;
-        return block * pg.block_stride + static_cast<uint32_t>(base + (lane & (TK - 1)) - page * pg.BS) * pg.token_bytes;
+        return block * pg.block_stride + static_cast<uint32_t>(t - divide(t, pg.by_bs) * pg.BS) * pg.token_bytes;
     };
-    u32x4 k_next[NP], v_next[NP];
-    auto request = [&](int64_t off) {
+    u32x4 k_next[FP8 ? NP : 1], v_next[FP8 ? NP : 1];
+    // Requests the rows of a round: two-byte rows straight into LDS (a wave's 64 pieces of 16 bytes lie there as its lanes
+    // do, so a lane fetches the piece that the permutation wants in its place), e4m3 into registers.
+    auto request = [&](int64_t off, int buffer) {
 #pragma unroll
         for (int n = 0; n < NP; ++n) {
             const int src = first_row + n * RP;
             const uint32_t lo = __shfl(static_cast<uint32_t>(off), src), hi = __shfl(static_cast<uint32_t>(off >> 32), src);
             const int64_t at = static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo);
+            if constexpr (!FP8) {
+                const int k_piece = piece ^ (src & KM), v_piece = piece ^ 2 * (src & VM);
+                const uint8_t *k = at < 0 || k_piece * 16 >= pg.row_bytes ? zeros : cache + at + k_piece * 16;
+                const uint8_t *v = at < 0 || v_piece * 16 >= pg.row_bytes ? zeros : cache + at + pg.v_bytes + v_piece * 16;
+                const int to = (n * RP + wave * (64 / GC)) * ROW;  // the wave's first row
+                __builtin_amdgcn_global_load_lds((global_byte *)k, (lds_byte *)(lds[buffer][0] + to), 16, 0, 0);
+                __builtin_amdgcn_global_load_lds((global_byte *)v, (lds_byte *)(lds[buffer][1] + to), 16, 0, 0);
+                continue;
+            }
             const uint8_t *x = cache + max(at, int64_t{0}) + piece_at;
             k_next[n] = *reinterpret_cast<const u32x4 *>(x);
             v_next[n] = *reinterpret_cast<const u32x4 *>(x + pg.v_bytes);
@@ -137,13 +167,18 @@ __global__ __launch_bounds__(64 * kWaves, 2) void tail_kernel(const AttendArgs a
             }
         }
     };
+    // What request() fetched is in LDS when every wave has done this and met at a barrier.
     auto deposit = [&](int buffer) {
+        if constexpr (!FP8) {
+            __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
+            return;
+        }
 #pragma unroll
-        for (int n = 0; n < NP; ++n) {
+        for (int n = 0; n < (FP8 ? NP : 0); ++n) {
             const int t = first_row + n * RP;
             uint8_t *k = lds[buffer][0] + t * ROW, *v = lds[buffer][1] + t * ROW;
             const int ks = t & KM, vs = 2 * (t & VM);
-            if constexpr (FP8) {
+            {
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     const uint32_t x0 = k_next[n][2 * j], x1 = k_next[n][2 * j + 1];
@@ -153,9 +188,6 @@ __global__ __launch_bounds__(64 * kWaves, 2) void tail_kernel(const AttendArgs a
                     *reinterpret_cast<u32x4 *>(v + ((2 * piece + j) ^ vs) * 16) =
                         u32x4{T::from_e4m3(y0, false), T::from_e4m3(y0, true), T::from_e4m3(y1, false), T::from_e4m3(y1, true)};
                 }
-            } else {
-                *reinterpret_cast<u32x4 *>(k + (piece ^ ks) * 16) = k_next[n];
-                *reinterpret_cast<u32x4 *>(v + (piece ^ vs) * 16) = v_next[n];
             }
         }
     };
@@ -179,23 +211,19 @@ __global__ __launch_bounds__(64 * kWaves, 2) void tail_kernel(const AttendArgs a
         v_at[d] = v_row * ROW + ((d * 4 + v_piece) ^ v_swizzle) * 16 + (lane & 1) * 8;
 
     if (begin < stop) {
-        int page, next_page = 0, next_block = 0, buffer = 0;
-        bool shown, next_shown = false;
-        const int block = block_at(begin, page, shown);
-        int64_t off = offset_at(begin, page, shown, block);
-        if (stop - begin > TK)
-            next_block = block_at(begin + TK, next_page, next_shown);
-        request(off);
+        int buffer = 0;
+        int64_t off = offset_at(begin, block_at(begin));
+        int next_block = block_at(min(begin + TK, stop));
+        request(off, 0);
         deposit(0);
         __syncthreads();
         for (int base = begin;; base += TK, buffer ^= 1) {
             const uint64_t usable = __ballot(off >= 0);
             const bool more = stop - base > TK;
             if (more) {
-                off = offset_at(base + TK, next_page, next_shown, next_block);
-                request(off);
-                if (stop - base > 2 * TK)
-                    next_block = block_at(base + 2 * TK, next_page, next_shown);
+                off = offset_at(base + TK, next_block);
+                next_block = block_at(stop - base > 2 * TK ? base + 2 * TK : stop);
+                request(off, buffer ^ 1);
             }
             // A wave whose rows see nothing of these tokens has only helped to load them.
             if (!idle && base <= p_last && base + (TK - 1) >= low_first) {
@@ -213,29 +241,38 @@ __global__ __launch_bounds__(64 * kWaves, 2) void tail_kernel(const AttendArgs a
                         s[t] = mfma_32x32x16(x, qf[k], s[t], T{});
                     }
                 }
+                interleave<TB * KS, 1, 6>();
                 const bool edge = usable != ~uint64_t{0} || p_first - base < TK - 1 || base < low_last;
                 // Scores in powers of 2; in the plain case the factor is left to the exponent's argument.
-                const float factor = plain ? scale : 1.f;
-                if (!plain) {
-                    const float inv = a.scale / a.softcap, cap = a.softcap * kLog2e;
+                const float factor = PLAIN ? scale : 1.f;
+                if constexpr (!PLAIN) {
+                    const auto each = [&](auto &&f) {
 #pragma unroll
-                    for (int t = 0; t < TB; ++t)
+                        for (int t = 0; t < TB; ++t)
 #pragma unroll
-                        for (int x = 0; x < 16; ++x) {
-                            float y = a.softcap > 0.f ? capped(s[t][x], inv, cap) : s[t][x] * scale;
-                            if (a.slopes)
-                                y -= slope * static_cast<float>(p_row - (base + t * 32 + 8 * (x >> 2) + half * 4 + (x & 3)));
-                            s[t][x] = y;
-                        }
+                            for (int x = 0; x < 16; ++x)
+                                s[t][x] = f(s[t][x], t * 32 + 8 * (x >> 2) + half * 4 + (x & 3));
+                    };
+                    if (a.softcap > 0.f) {
+                        const float inv = a.scale / a.softcap, cap = a.softcap * kLog2e;
+                        each([&](float y, int) { return capped(y, inv, cap); });
+                    } else {
+                        each([&](float y, int) { return y * scale; });
+                    }
+                    if (a.slopes)
+                        each([&](float y, int at) { return y - slope * static_cast<float>(p_row - (base + at)); });
                 }
                 if (edge) {
+                    // Tokens of this round that the row sees, counted from `base`: [from, to), and usable ones.
+                    const int to = p_row - base + 1, from = a.window > 0 ? to - a.window : INT32_MIN;
+                    const uint64_t mine = usable >> (half * 4);
 #pragma unroll
                     for (int t = 0; t < TB; ++t)
 #pragma unroll
                         for (int x = 0; x < 16; ++x) {
-                            const int at = t * 32 + 8 * (x >> 2) + half * 4 + (x & 3), token = base + at;
-                            if (!(usable >> at & 1) || token > p_row || (a.window > 0 && p_row - token >= a.window))
-                                s[t][x] = -INFINITY;
+                            const int bit = t * 32 + 8 * (x >> 2) + (x & 3), at = bit + half * 4;
+                            const bool sees = (mine >> bit & 1) && at < to && at >= from;
+                            s[t][x] = sees ? s[t][x] : -INFINITY;
                         }
                 }
                 float top = -INFINITY;
@@ -271,11 +308,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void tail_kernel(const AttendArgs a
                 l += (sums[0] + sums[1]) + (sums[2] + sums[3]);
                 lds_byte *v_lds = (lds_byte *)(lds[buffer][1]);  // (a cast between address spaces)
 #pragma unroll
-                for (int d = 0; d < DB; ++d)
+                for (int t = 0; t < TB; ++t)
 #pragma unroll
-                    for (int t = 0; t < TB; ++t)
+                    for (int j = 0; j < 2; ++j)
 #pragma unroll
-                        for (int j = 0; j < 2; ++j) {
+                        for (int d = 0; d < DB; ++d) {
                             const int at = (t * 32 + j * 16) * ROW;
                             const u32x2 x = read_turned(v_lds + v_at[d] + at), y = read_turned(v_lds + v_at[d] + at + 8 * ROW);
                             acc[d] = mfma_32x32x16(u32x4{x[0], x[1], y[0], y[1]}, p[t][j], acc[d], T{});
@@ -326,7 +363,8 @@ template <class T, bool FP8, int DP>
 __global__ __launch_bounds__(64 * kWaves) void weigh_kernel(const AttendArgs a) {
     constexpr int KC = DP * (FP8 ? 1 : 2) / 32;  // 16-byte pieces of a token's K in a lane
     const Pages &pg = a.pages;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 31, half = lane >> 5;
+    const int lane = threadIdx.x & 63, c = lane & 31, half = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int b = blockIdx.z, h = blockIdx.y, base = (blockIdx.x * kWaves + wave) * 32;
     Sequence seq;
     if (!sequence(a.batch, b, pg.err, seq) || base >= seq.n)
@@ -380,15 +418,29 @@ __global__ __launch_bounds__(64 * kWaves) void weigh_kernel(const AttendArgs a) 
                                       T{});
                 }
             }
-            const float slope = a.slopes ? a.slopes[head] * kLog2e : 0.f;
+            if (a.softcap > 0.f) {
+                const float inv = a.scale / a.softcap, cap = a.softcap * kLog2e;
+#pragma unroll
+                for (int x = 0; x < 16; ++x)
+                    s[x] = capped(s[x], inv, cap);
+            } else {
+#pragma unroll
+                for (int x = 0; x < 16; ++x)
+                    s[x] *= scale;
+            }
+            if (a.slopes) {
+                const float slope = a.slopes[head] * kLog2e;
+#pragma unroll
+                for (int x = 0; x < 16; ++x)
+                    s[x] -= slope * static_cast<float>(p - (base + 8 * (x >> 2) + half * 4 + (x & 3)));
+            }
+            const int to = lse == -INFINITY ? INT32_MIN : p - base + 1, from = a.window > 0 ? p - base + 1 - a.window : INT32_MIN;
+            const uint32_t mine = usable >> (half * 4);
 #pragma unroll
             for (int x = 0; x < 16; ++x) {
-                const int at = 8 * (x >> 2) + half * 4 + (x & 3), t = base + at;
-                float y = a.softcap > 0.f ? capped(s[x], a.scale / a.softcap, a.softcap * kLog2e) : s[x] * scale;
-                if (a.slopes)
-                    y -= slope * static_cast<float>(p - t);
-                const bool sees = (usable >> at & 1) && t <= p && (a.window == 0 || p - t < a.window) && lse != -INFINITY;
-                sums[x] += sees ? __builtin_amdgcn_exp2f(y - lse) : 0.f;
+                const int bit = 8 * (x >> 2) + (x & 3), at = bit + half * 4;
+                const bool sees = (mine >> bit & 1) && at < to && at >= from;
+                sums[x] += sees ? __builtin_amdgcn_exp2f(s[x] - lse) : 0.f;
             }
         }
     }
@@ -406,21 +458,29 @@ __global__ __launch_bounds__(64 * kWaves) void weigh_kernel(const AttendArgs a) 
     }
 }
 
-template <class T, bool FP8, int DP, int TK>
+template <class T, bool FP8, int DP, int TK, bool PLAIN>
 void launch(const AttendArgs &a, const Parts &parts, int max_queries, hipStream_t stream) {
     const int tiles = static_cast<int>((static_cast<int64_t>(max_queries) * a.group + kRows - 1) / kRows);
     const uint32_t grid = static_cast<uint32_t>(tiles) * parts.splits * a.pages.H * a.num_seqs;
-    hipLaunchKernelGGL((tail_kernel<T, FP8, DP, TK>), dim3(grid), dim3(64 * kWaves), 0, stream, a, parts, tiles);
+    hipLaunchKernelGGL((tail_kernel<T, FP8, DP, TK, PLAIN>), dim3(grid), dim3(64 * kWaves), 0, stream, a, parts, tiles);
+}
+
+template <class T, bool FP8, bool PLAIN>
+void launch(const AttendArgs &a, const Parts &parts, int max_queries, hipStream_t stream) {
+    if (a.pages.D > 128)
+        launch<T, FP8, 256, 32, PLAIN>(a, parts, max_queries, stream);
+    else if (a.pages.D > 64)
+        launch<T, FP8, 128, 64, PLAIN>(a, parts, max_queries, stream);
+    else
+        launch<T, FP8, 64, 64, PLAIN>(a, parts, max_queries, stream);
 }
 
 template <class T, bool FP8>
 void launch(const AttendArgs &a, const Parts &parts, int max_queries, hipStream_t stream) {
-    if (a.pages.D > 128)
-        launch<T, FP8, 256, 32>(a, parts, max_queries, stream);
-    else if (a.pages.D > 64)
-        launch<T, FP8, 128, 64>(a, parts, max_queries, stream);
+    if (a.softcap == 0.f && !a.slopes)
+        launch<T, FP8, true>(a, parts, max_queries, stream);
     else
-        launch<T, FP8, 64, 64>(a, parts, max_queries, stream);
+        launch<T, FP8, false>(a, parts, max_queries, stream);
 }
 
 template <class T, bool FP8>
