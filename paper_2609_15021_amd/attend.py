@@ -93,7 +93,7 @@ def _batch(cache: Cache, tables, lens, starts, tokens: int, max_q, max_len) -> K
     else:
         _ints(starts, "starts", 1, B + 1)
         max_q = max(1, tokens if max_q is None else int(max_q))
-    most = min(pages * cache.layout.block_size, 2**31 - 128)
+    most = min(pages * cache.layout.block_size, 2**31 - 1024)
     return KvBatch(B, max_q, tokens, most if max_len is None else min(most, int(max_len)), pages, 0, tables.stride(0),
                    tables.data_ptr(), lens.data_ptr(), None if starts is None else starts.data_ptr())
 

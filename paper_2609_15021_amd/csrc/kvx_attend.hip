@@ -79,6 +79,31 @@ Parts parts_for(int64_t longest, int64_t have, int64_t wanted, int64_t unit, int
     return p;
 }
 
+// The tail kernel's parts.  512 of its workgroups run at once (2 per CU; 256 where D > 128), so `have` of them may leave
+// the last round nearly empty, and fewer leave CUs idle: the number of parts is the one whose rounds and joining take
+// least, at the 0.2 ns per token and column that such a round takes and the 5 TB/s at which parts are written and read
+// again.  Parts have no fewer than 256 tokens and no more than 256 MB between them.
+Parts tail_parts_for(int64_t longest, int64_t have, int64_t rows, int64_t head_dim) {
+    longest = std::max<int64_t>(longest, 1);
+    const int64_t at_once = head_dim > 128 ? 256 : 512;
+    const double tokens_us = 0.2e-3 * static_cast<double>(head_dim) * static_cast<double>(longest);
+    const double parts_bytes = static_cast<double>(have) * kTailRows * static_cast<double>(head_dim) * 4;
+    int64_t best = 1;
+    double best_us = 0.;
+    for (int64_t splits = 1; splits <= 64; ++splits) {
+        if (splits > 1 && (longest < 256 * splits || parts_bytes * static_cast<double>(splits) > 256e6))
+            break;
+        const double us =
+            static_cast<double>((have * splits + at_once - 1) / at_once) * tokens_us / static_cast<double>(splits) +
+            (splits > 1 ? 5. + static_cast<double>(splits) * parts_bytes * 2 / 5e6 : 0.);
+        if (splits == 1 || us < 0.95 * best_us) {
+            best = splits;
+            best_us = us;
+        }
+    }
+    return parts_for(longest, 1, best, 64, INT32_MAX - 63, rows);
+}
+
 Plan plan_of(const kv_cache *cache, const kv_batch *batch, const kv_attend_options *o, const kv_rows *q) {
     const int64_t H = cache->layout.num_kv_heads, D = cache->layout.head_dim, group = q->heads / H;
     const int64_t heads = batch->num_seqs * H;
@@ -100,9 +125,7 @@ Plan plan_of(const kv_cache *cache, const kv_batch *batch, const kv_attend_optio
     const int64_t tile = step_tile_rows(p.max_rows, static_cast<int>(D));
     p.step_parts = parts_for(longest(kStepRows), heads * ((p.max_rows + tile - 1) / tile), 1024, 128, 4096, p.max_rows);
     if (p.tail) {
-        // The tail kernel: 2 workgroups per CU, of no fewer than 512 tokens.
-        const int64_t tiles = (all_rows + kTailRows - 1) / kTailRows;
-        p.tail_parts = parts_for(longest(kTailRows), heads * tiles, 512, 512, INT32_MAX - 511, all_rows);
+        p.tail_parts = tail_parts_for(longest(kTailRows), heads * ((all_rows + kTailRows - 1) / kTailRows), all_rows, D);
     }
     int64_t at = round_up(static_cast<int64_t>(batch->num_queries) * q->heads * 4, 16);
     const auto take = [&](int64_t bytes) {

@@ -117,6 +117,13 @@ __device__ __forceinline__ float capped(float x, float inv, float cap) {
     return cap * (t < 0.25f ? series : copysignf(far, y));
 }
 
+// The same for caps up to kSmallCap, from exp2 alone (twice = 2 log2(e) inv): its error of 2^-22 or so of cap, whatever x,
+// is then at most that of a score of 16.
+constexpr float kSmallCap = 64.f;
+__device__ __forceinline__ float small_capped(float x, float twice, float cap) {
+    return fmaf(-2.f * cap, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * twice)), cap);
+}
+
 // Each covers the sequences of its kind only, whatever else is in the batch.
 hipError_t launch_step(const AttendArgs &a, const Parts &parts, int max_queries, hipStream_t stream);
 hipError_t launch_tail(const AttendArgs &a, const Parts &parts, int max_queries, hipStream_t stream);

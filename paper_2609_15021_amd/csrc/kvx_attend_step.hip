@@ -410,66 +410,68 @@ __global__ __launch_bounds__(64 * kWaves) void step_kernel(const AttendArgs a, c
     }
 }
 
-// The parts of a row joined: sum_s 2^(m_s - m) x_s / sum_s 2^(m_s - m) l_s.  One row and head per workgroup; 4 columns
-// per lane, the parts spread over the lanes' groups.
+// The parts of a row joined: sum_s 2^(m_s - m) x_s / sum_s 2^(m_s - m) l_s.  4 columns per lane; a workgroup takes one
+// row and spreads its parts over its lanes' groups (SPREAD: many parts, few rows), or a row per group of lanes.
+template <bool SPREAD>
 __global__ __launch_bounds__(256) void join_kernel(const AttendArgs a, const Parts from, const int min_rows, const int max_rows,
                                                     const int tile_rows) {
-    __shared__ float sums[256][4];
-    __shared__ float shared_stats[2];
-    const int b = blockIdx.z, head = blockIdx.y, i = blockIdx.x, h = divide(head, a.by_group);
+    __shared__ f32x4 sums[SPREAD ? 256 : 1];
+    const int b = blockIdx.z, head = blockIdx.y, h = divide(head, a.by_group), D = a.pages.D, tid = threadIdx.x;
+    const int lanes = D / 4, groups = 256 / lanes, mine = tid / lanes, d = (tid - mine * lanes) * 4;
+    const int i = SPREAD ? blockIdx.x : blockIdx.x * groups + mine;
     Sequence seq;
-    if (!sequence(a.batch, b, a.pages.err, seq) || i >= seq.nq || seq.nq * a.group < min_rows ||
-        seq.nq * a.group > max_rows)
+    if (!sequence(a.batch, b, a.pages.err, seq) || seq.nq * a.group < min_rows || seq.nq * a.group > max_rows)
+        return;
+    const bool row = i < seq.nq && mine < groups;
+    if (SPREAD ? i >= seq.nq : !row)
         return;
     // The parts are those of the row's tile.
     const int r = i * a.group + head - h * a.group, rows = seq.nq * a.group, row0 = r - r % tile_rows;
     const Span span = span_of(seq.n, seq.nq, divide(row0, a.by_group),
                               divide(min(row0 + tile_rows, rows) - 1, a.by_group) + 1, a.window);
-    const int parts = parts_of(span, from.len), D = a.pages.D, tid = threadIdx.x;
+    const int parts = parts_of(span, from.len);
     if (parts == 1)
         return;
     const int64_t slot = ((static_cast<int64_t>(b) * a.pages.H + h) * from.row_cap + r) * from.splits;
     const float *stats = from.stats + slot * 2;
-    if (tid < 64) {
-        float most = kLowest;
-        for (int s = tid; s < parts; s += 64)
+    float most = kLowest, total = 0.f;
+    if constexpr (SPREAD) {  // every wave for itself
+        const int lane = tid & 63;
+        for (int s = lane; s < parts; s += 64)
             most = fmaxf(most, stats[2 * s]);
         for (int o = 32; o; o >>= 1)
             most = fmaxf(most, __shfl_xor(most, o));
-        float total = 0.f;
-        for (int s = tid; s < parts; s += 64)
+        for (int s = lane; s < parts; s += 64)
             total += stats[2 * s + 1] * __builtin_amdgcn_exp2f(stats[2 * s] - most);
         for (int o = 32; o; o >>= 1)
             total += __shfl_xor(total, o);
-        if (tid == 0) {
-            shared_stats[0] = most;
-            shared_stats[1] = total;
-        }
+    } else {
+        for (int s = 0; s < parts; ++s)
+            most = fmaxf(most, stats[2 * s]);
+        for (int s = 0; s < parts; ++s)
+            total += stats[2 * s + 1] * __builtin_amdgcn_exp2f(stats[2 * s] - most);
     }
-    __syncthreads();
-    const float most = shared_stats[0], total = shared_stats[1];
-    const int lanes = D / 4, groups = 256 / lanes, part0 = tid / lanes, d = (tid - part0 * lanes) * 4;
     f32x4 x{0.f, 0.f, 0.f, 0.f};
-    if (part0 < groups)
-        for (int s = part0; s < parts; s += groups)
+    if (row)
+        for (int s = SPREAD ? mine : 0; s < parts; s += SPREAD ? groups : 1)
             x += *reinterpret_cast<const f32x4 *>(from.sums + (slot + s) * D + d) *
                  __builtin_amdgcn_exp2f(stats[2 * s] - most);
-    for (int k = 0; k < 4; ++k)
-        sums[tid][k] = x[k];
-    __syncthreads();
-    if (part0 == 0) {
+    if constexpr (SPREAD) {
+        sums[tid] = x;
+        __syncthreads();
+        if (mine > 0)
+            return;
         for (int s = 1; s < groups; ++s)
-            for (int k = 0; k < 4; ++k)
-                x[k] += sums[s * lanes + tid][k];
-        const float inv = total == 0.f ? 0.f : a.v_scale / total;
-        u32x2 y;
-        if (a.q_type == KV_DTYPE_BF16)
-            y = u32x2{Bf16::pack(x[0] * inv, x[1] * inv), Bf16::pack(x[2] * inv, x[3] * inv)};
-        else
-            y = u32x2{F16::pack(x[0] * inv, x[1] * inv), F16::pack(x[2] * inv, x[3] * inv)};
-        *reinterpret_cast<u32x2 *>(a.out.data + (seq.q0 + i) * a.out.token_stride + head * a.out.head_stride + 2 * d) = y;
+            x += sums[s * lanes + tid];
     }
-    if (tid == 0)
+    const float inv = total == 0.f ? 0.f : a.v_scale / total;
+    u32x2 y;
+    if (a.q_type == KV_DTYPE_BF16)
+        y = u32x2{Bf16::pack(x[0] * inv, x[1] * inv), Bf16::pack(x[2] * inv, x[3] * inv)};
+    else
+        y = u32x2{F16::pack(x[0] * inv, x[1] * inv), F16::pack(x[2] * inv, x[3] * inv)};
+    *reinterpret_cast<u32x2 *>(a.out.data + (seq.q0 + i) * a.out.token_stride + head * a.out.head_stride + 2 * d) = y;
+    if (d == 0)
         a.lse[static_cast<int64_t>(seq.q0 + i) * a.heads + head] =
             total == 0.f ? -INFINITY : (most + __builtin_amdgcn_logf(total)) * kLn2;
 }
@@ -529,8 +531,14 @@ hipError_t launch_step(const AttendArgs &a, const Parts &parts, int max_queries,
 
 hipError_t launch_join(const AttendArgs &a, const Parts &parts, int max_queries, int min_rows, int max_rows,
                        int tile_rows, hipStream_t stream) {
-    const dim3 grid(static_cast<uint32_t>(max_queries), static_cast<uint32_t>(a.heads), static_cast<uint32_t>(a.num_seqs));
-    hipLaunchKernelGGL(join_kernel, grid, dim3(256), 0, stream, a, parts, min_rows, max_rows, tile_rows);
+    const int groups = 256 / (a.pages.D / 4);
+    const bool spread = parts.splits > 8;  // (8 parts one after the other take about as long as one row's launch)
+    const dim3 grid(static_cast<uint32_t>(spread ? max_queries : (max_queries + groups - 1) / groups),
+                    static_cast<uint32_t>(a.heads), static_cast<uint32_t>(a.num_seqs));
+    if (spread)
+        hipLaunchKernelGGL(join_kernel<true>, grid, dim3(256), 0, stream, a, parts, min_rows, max_rows, tile_rows);
+    else
+        hipLaunchKernelGGL(join_kernel<false>, grid, dim3(256), 0, stream, a, parts, min_rows, max_rows, tile_rows);
     return hipGetLastError();
 }
 

@@ -14,6 +14,7 @@
 // e4m3 is widened on its way into LDS, once per workgroup.  Workgroups that share a KV head run on one XCD where the
 // number of heads allows (consecutive workgroups go to consecutive XCDs), and use its L2 together.
 #include <algorithm>
+#include <type_traits>
 
 #include "kvx_attend_kernels.h"
 
@@ -21,9 +22,8 @@ namespace kvx {
 
 namespace {
 
-constexpr int kWaves = 4;
-constexpr int kRows = 32 * kWaves;
-static_assert(kRows == kTailRows, "a wave takes 32 rows");
+constexpr int kRows = kTailRows;
+constexpr int kWeighWaves = 4;
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -37,6 +37,26 @@ __device__ __forceinline__ f32x16 mfma_32x32x16(const u32x4 &a, const u32x4 &b, 
                                                   0, 0, 0);
 }
 
+// A tile of RW x RW sums, and the product that adds to it.
+template <int RW>
+struct Tile;
+template <>
+struct Tile<32> {
+    typedef f32x16 type;
+};
+template <>
+struct Tile<16> {
+    typedef f32x4 type;
+};
+template <class T>
+__device__ __forceinline__ f32x16 product(const u32x4 &a, const u32x4 &b, const f32x16 &c, T) {
+    return mfma_32x32x16(a, b, c, T{});
+}
+template <class T>
+__device__ __forceinline__ f32x4 product(const u32x4 &a, const u32x4 &b, const f32x4 &c, T) {
+    return mfma_16x16x32(a, b, c, T{});
+}
+
 typedef __attribute__((address_space(3))) uint8_t lds_byte;
 typedef __attribute__((address_space(1))) const uint8_t global_byte;
 
@@ -48,38 +68,49 @@ __device__ __forceinline__ u32x2 read_turned(lds_byte *p) {
                               __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<__attribute__((address_space(3))) s16x4 *>(p)));
 }
 
-// Asks the compiler to keep `ahead` LDS reads (each `reads` instructions) in flight before the first of `products`
-// products, and to issue one more after each.
-template <int PRODUCTS, int READS, int AHEAD>
+// Asks the compiler to keep `ahead` LDS reads (of `reads` instructions) in flight before the first of `products`
+// products, and to issue one more, and `others` vector instructions, after each.
+template <int PRODUCTS, int READS, int AHEAD, int OTHERS>
 __device__ __forceinline__ void interleave() {
-    constexpr int kProduct = 0x8, kRead = 0x100;
+    constexpr int kVector = 0x2, kProduct = 0x8, kRead = 0x100;
     __builtin_amdgcn_sched_group_barrier(kRead, AHEAD * READS, 0);
 #pragma unroll
-    for (int i = 0; i < PRODUCTS - AHEAD; ++i) {
+    for (int i = 0; i < PRODUCTS; ++i) {
         __builtin_amdgcn_sched_group_barrier(kProduct, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(kRead, READS, 0);
+        if (i < PRODUCTS - AHEAD)
+            __builtin_amdgcn_sched_group_barrier(kRead, READS, 0);
+        if (OTHERS > 0)
+            __builtin_amdgcn_sched_group_barrier(kVector, OTHERS, 0);
     }
-    __builtin_amdgcn_sched_group_barrier(kProduct, AHEAD, 0);
 }
 
-// The largest and the sum over a lane and the one 32 lanes on.
-__device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
-
-// PLAIN: neither a cap nor slopes.
-template <class T, bool FP8, int DP, int TK, bool PLAIN>
-__global__ __launch_bounds__(64 * kWaves, 2) void tail_kernel(const AttendArgs a, const Parts parts, const int tiles) {
+// RW: rows of a wave, 32 (products of 32x32x16) or 16 (16x16x32).  PLAIN: neither a cap nor slopes.
+template <class T, bool FP8, int DP, int TK, int RW, bool PLAIN>
+__global__ __launch_bounds__(64 * kRows / RW, 2) void tail_kernel(const AttendArgs a, const Parts parts, const int tiles) {
     constexpr int E = FP8 ? 1 : 2;
     constexpr int ROW = 2 * DP;                     // bytes of a row in LDS
     constexpr int GC = DP * E / 16;                 // 16-byte pieces of a cached row
-    constexpr int RP = 64 * kWaves / GC;            // rows that the workgroup loads at once
+    constexpr int WAVES = kRows / RW, RP = 64 * WAVES / GC;  // rows that the workgroup loads at once
     constexpr int NP = TK / RP;                     // times
-    constexpr int KM = DP / 8 < 16 ? DP / 8 - 1 : 15, VM = DP / 16 < 8 ? DP / 16 - 1 : 7;  // permutations' masks
-    constexpr int TB = TK / 32, KS = DP / 16, DB = DP / 32;
+    constexpr bool WIDE = RW == 32;
+    constexpr int TB = TK / 32, NS = RW / 2;        // rounds of 32 tokens; scores of a lane in one
+    constexpr int KD = WIDE ? 16 : 32;              // columns of a product of scores
+    constexpr int KS = DP / KD, DB = DP / RW;       // products of 32 tokens' scores, tiles of the output
+    constexpr int SETS = WIDE ? 2 : 1;              // products of a tile of the output in 32 tokens
+    typedef typename Tile<RW>::type Sums;
+    // Permutations of a row's 16-byte pieces in LDS, so that the lanes that read together meet 256 different bytes of
+    // the banks: 16 rows of one piece (K), 4 rows of 4 or 8 of 2 pieces (V).
+    const auto k_permute = [](int t) { return (WIDE ? t : (t & 3) | (t >> 1 & 12)) & (DP / 8 < 16 ? DP / 8 - 1 : 15); };
+    const auto v_permute = [](int t) {
+        return !WIDE ? 2 * ((t & 3) | (t >> 1 & 4)) : DP == 64 ? 4 * (t >> 1 & 1) : 4 * (t & 3);
+    };
+    // Token (of 32) of a lane's x-th score.
+    const auto token_of = [](int x, int part) { return WIDE ? 8 * (x >> 2) + part * 4 + (x & 3) : part * 8 + x; };
     static_assert(TK % RP == 0, "whole rounds of loads");
-    __shared__ __align__(16) uint8_t lds[2][2][TK * ROW];  // [round][K, V]
+    __shared__ __align__(16) uint8_t lds[2][2][TK * ROW];  // [K, V][round]
 
     const Pages &pg = a.pages;
-    const int tid = threadIdx.x, lane = tid & 63, c = lane & 31, half = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, c = lane & (RW - 1), part = lane / RW;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int groups = a.num_seqs * pg.H, group = blockIdx.x % groups, item = blockIdx.x / groups;
     const int b = group / pg.H, h = group - b * pg.H;
@@ -99,15 +130,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void tail_kernel(const AttendArgs a
     const bool whole = span.end - span.start <= parts.len;
 
     // This lane's row: its query as the first product's operand, and what it sees.
-    const int r = row0 + wave * 32 + c;
+    const int r = row0 + wave * RW + c;
     const bool row_ok = r < rows;
     const int row_i = divide(min(r, rows - 1), a.by_group), head = h * a.group + min(r, rows - 1) - row_i * a.group;
     const int p_row = row_ok ? seq.n - seq.nq + row_i : -1;
-    const int wave_r0 = min(row0 + wave * 32, rows - 1), wave_r1 = min(row0 + wave * 32 + 31, rows - 1);
+    const int wave_r0 = min(row0 + wave * RW, rows - 1), wave_r1 = min(row0 + wave * RW + RW - 1, rows - 1);
     const int p_first = seq.n - seq.nq + divide(wave_r0, a.by_group), p_last = seq.n - seq.nq + divide(wave_r1, a.by_group);
     const int low_last = a.window > 0 ? p_last + 1 - a.window : 0;
-    const int low_first = a.window > 0 ? p_first + 1 - a.window : 0;
-    const bool idle = row0 + wave * 32 >= rows;
     const float slope = a.slopes ? a.slopes[head] * kLog2e : 0.f;
     const float scale = a.scale * kLog2e;
     u32x4 qf[KS];
@@ -115,7 +144,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void tail_kernel(const AttendArgs a
         const uint8_t *q = a.q.data + (seq.q0 + row_i) * a.q.token_stride + head * a.q.head_stride;
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
-            const int d = k * 16 + half * 8;
+            const int d = k * KD + part * 8;
             qf[k] = row_ok && d < pg.D ? *reinterpret_cast<const u32x4 *>(q + 2 * d) : u32x4{0, 0, 0, 0};
         }
     }
@@ -124,7 +153,6 @@ __global__ __launch_bounds__(64 * kWaves, 2) void tail_kernel(const AttendArgs a
     const uint8_t *cache = pg.base + static_cast<uint32_t>(h) * pg.head_bytes;
     const int piece = tid % GC, first_row = tid / GC;
     const bool piece_ok = piece * 16 < pg.row_bytes;
-    const int piece_at = piece_ok ? piece * 16 : 0;
 
     // Lanes look up a round's tokens (lane % TK each): the page's block, then where the token's row is; -1 for a token
     // that takes part in nothing.
@@ -139,193 +167,225 @@ __global__ __launch_bounds__(64 * kWaves, 2) void tail_kernel(const AttendArgs a
             return -1;
         return block * pg.block_stride + static_cast<uint32_t>(t - divide(t, pg.by_bs) * pg.BS) * pg.token_bytes;
     };
-    u32x4 k_next[FP8 ? NP : 1], v_next[FP8 ? NP : 1];
-    // Requests the rows of a round: two-byte rows straight into LDS (a wave's 64 pieces of 16 bytes lie there as its lanes
-    // do, so a lane fetches the piece that the permutation wants in its place), e4m3 into registers.
+    // Requests K and V rows of a round: two-byte rows straight into LDS (a wave's 64 pieces of 16 bytes lie there as its
+    // lanes do, so a lane fetches the piece that the permutation wants in its place), e4m3 into registers.  Slots without
+    // a token and columns beyond D may hold anything, and 0 times it need not be 0: they become zeros.
+    u32x4 next[2][FP8 ? NP : 1];
     auto request = [&](int64_t off, int buffer) {
+        int64_t at[NP];
 #pragma unroll
         for (int n = 0; n < NP; ++n) {
             const int src = first_row + n * RP;
             const uint32_t lo = __shfl(static_cast<uint32_t>(off), src), hi = __shfl(static_cast<uint32_t>(off >> 32), src);
-            const int64_t at = static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo);
-            if constexpr (!FP8) {
-                const int k_piece = piece ^ (src & KM), v_piece = piece ^ 2 * (src & VM);
-                const uint8_t *k = at < 0 || k_piece * 16 >= pg.row_bytes ? zeros : cache + at + k_piece * 16;
-                const uint8_t *v = at < 0 || v_piece * 16 >= pg.row_bytes ? zeros : cache + at + pg.v_bytes + v_piece * 16;
-                const int to = (n * RP + wave * (64 / GC)) * ROW;  // the wave's first row
-                __builtin_amdgcn_global_load_lds((global_byte *)k, (lds_byte *)(lds[buffer][0] + to), 16, 0, 0);
-                __builtin_amdgcn_global_load_lds((global_byte *)v, (lds_byte *)(lds[buffer][1] + to), 16, 0, 0);
-                continue;
-            }
-            const uint8_t *x = cache + max(at, int64_t{0}) + piece_at;
-            k_next[n] = *reinterpret_cast<const u32x4 *>(x);
-            v_next[n] = *reinterpret_cast<const u32x4 *>(x + pg.v_bytes);
-            // Slots without a token and columns beyond D may hold anything: 0 times it need not be 0.
-            if (at < 0 || !piece_ok) {
-                k_next[n] = u32x4{0, 0, 0, 0};
-                v_next[n] = u32x4{0, 0, 0, 0};
-            }
+            at[n] = static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo);
+        }
+        if constexpr (FP8) {
+#pragma unroll
+            for (int n = 0; n < NP; ++n)
+#pragma unroll
+                for (int kv = 0; kv < 2; ++kv) {
+                    const u32x4 x = *reinterpret_cast<const u32x4 *>((kv ? cache + pg.v_bytes : cache) +
+                                                                     max(at[n], int64_t{0}) + (piece_ok ? piece * 16 : 0));
+                    next[kv][n] = at[n] < 0 || !piece_ok ? u32x4{0, 0, 0, 0} : x;
+                }
+        } else {
+            const auto fetch = [&](auto every) {
+#pragma unroll
+                for (int n = 0; n < NP; ++n) {
+                    const int src = first_row + n * RP;
+                    const int to = (n * RP + wave * (64 / GC)) * ROW;  // the wave's first row
+#pragma unroll
+                    for (int kv = 0; kv < 2; ++kv) {
+                        const int from = piece ^ (kv ? v_permute(src) : k_permute(src));
+                        const uint8_t *x = (kv ? cache + pg.v_bytes : cache) + from * 16 + at[n];
+                        if (!every && (at[n] < 0 || from * 16 >= pg.row_bytes))
+                            x = zeros;
+                        __builtin_amdgcn_global_load_lds((global_byte *)x, (lds_byte *)(lds[kv][buffer] + to), 16, 0, 0);
+                    }
+                }
+            };
+            if (pg.D == DP && __all(off >= 0))
+                fetch(std::true_type{});
+            else
+                fetch(std::false_type{});
         }
     };
     // What request() fetched is in LDS when every wave has done this and met at a barrier.
-    auto deposit = [&](int buffer) {
-        if constexpr (!FP8) {
-            __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
-            return;
-        }
+    auto deposit = [&](int kv, int buffer) {
+        if constexpr (FP8) {
 #pragma unroll
-        for (int n = 0; n < (FP8 ? NP : 0); ++n) {
-            const int t = first_row + n * RP;
-            uint8_t *k = lds[buffer][0] + t * ROW, *v = lds[buffer][1] + t * ROW;
-            const int ks = t & KM, vs = 2 * (t & VM);
-            {
+            for (int n = 0; n < NP; ++n) {
+                const int t = first_row + n * RP, permute = kv ? v_permute(t) : k_permute(t);
+                uint8_t *to = lds[kv][buffer] + t * ROW;
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    const uint32_t x0 = k_next[n][2 * j], x1 = k_next[n][2 * j + 1];
-                    const uint32_t y0 = v_next[n][2 * j], y1 = v_next[n][2 * j + 1];
-                    *reinterpret_cast<u32x4 *>(k + ((2 * piece + j) ^ ks) * 16) =
+                    const uint32_t x0 = next[kv][n][2 * j], x1 = next[kv][n][2 * j + 1];
+                    *reinterpret_cast<u32x4 *>(to + ((2 * piece + j) ^ permute) * 16) =
                         u32x4{T::from_e4m3(x0, false), T::from_e4m3(x0, true), T::from_e4m3(x1, false), T::from_e4m3(x1, true)};
-                    *reinterpret_cast<u32x4 *>(v + ((2 * piece + j) ^ vs) * 16) =
-                        u32x4{T::from_e4m3(y0, false), T::from_e4m3(y0, true), T::from_e4m3(y1, false), T::from_e4m3(y1, true)};
                 }
             }
+        } else {
+            __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
         }
     };
 
-    f32x16 acc[DB];
+    constexpr int AN = RW * RW / 64;  // elements of a tile of the output in a lane
+    Sums acc[DB];
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
-        for (int x = 0; x < 16; ++x)
+        for (int x = 0; x < AN; ++x)
             acc[d][x] = 0.f;
     float m = kLowest, l = 0.f;
 
-    // Where this lane reads: K's row c of 32 (its piece of product k is (2 * k + half) ^ swizzle), and V's 8 bytes of
-    // row half * 4 + lane / 4 % 4 of 8, columns lane / 16 % 2 * 16 + lane % 4 * 4 of 32.
-    const int k_at = c * ROW, k_swizzle = c & KM;
-    const int v_row = half * 4 + (lane >> 2 & 3), v_piece = (lane >> 4 & 1) * 2 + (lane >> 1 & 1);
-    const int v_swizzle = 2 * (v_row & VM);
-    int v_at[DB];
+    // Where this lane reads.  K: 16 bytes of a token's row per product, the token c of 32, or for the two products of 16
+    // tokens (c / 4) * 8 + c % 4 and that + 4.  V: 8 bytes, of one of 4 tokens' rows for the 16 lanes that turn them, and
+    // of the one 8 (or 4) on.  Rows start at multiples of their length, so a permuted piece's address is the first one's
+    // with bits of the product's (or the tile's) number turned over.
+    const int k_row = WIDE ? c : (c >> 2) * 8 + (c & 3), v_row = part * (WIDE ? 4 : 8) + (lane >> 2 & 3);
+    const int v_piece = (WIDE ? (lane >> 4 & 1) * 2 : 0) + (lane >> 1 & 1);
+    int k_at = k_row * ROW + (part ^ k_permute(k_row)) * 16;
+    int v_at = v_row * ROW + (v_piece ^ v_permute(v_row)) * 16 + (lane & 1) * 8;
+
+    float s[TB][NS];
+    auto take_scores = [&](int buffer) {
+        const uint8_t *k_lds = lds[0][buffer];
+        constexpr int SETS_K = WIDE ? 1 : 2;  // products side by side of 32 tokens
 #pragma unroll
-    for (int d = 0; d < DB; ++d)
-        v_at[d] = v_row * ROW + ((d * 4 + v_piece) ^ v_swizzle) * 16 + (lane & 1) * 8;
+        for (int t = 0; t < TB; ++t) {
+            Sums sum[SETS_K];
+#pragma unroll
+            for (int j = 0; j < SETS_K; ++j) {
+#pragma unroll
+                for (int x = 0; x < AN; ++x)
+                    sum[j][x] = 0.f;
+                // (The permutation does not see the 4 tokens between the two products' rows.)
+#pragma unroll
+                for (int k = 0; k < KS; ++k)
+                    sum[j] = product(*reinterpret_cast<const u32x4 *>(k_lds + (t * 32 + j * 4) * ROW + (k_at ^ k * 2 * KD)),
+                                     qf[k], sum[j], T{});
+            }
+#pragma unroll
+            for (int x = 0; x < NS; ++x)
+                s[t][x] = sum[x / AN][x % AN];
+        }
+        interleave<TB * SETS_K * KS, 1, 6, 0>();
+    };
+    // The largest over the lanes that share a row.
+    const auto over_parts = [](float x) {
+        x = fmaxf(x, __shfl_xor(x, 32));
+        return WIDE ? x : fmaxf(x, __shfl_xor(x, 16));
+    };
 
     if (begin < stop) {
         int buffer = 0;
         int64_t off = offset_at(begin, block_at(begin));
-        int next_block = block_at(min(begin + TK, stop));
+        int next_block = block_at(begin + TK);
         request(off, 0);
-        deposit(0);
+        deposit(0, 0);
+        deposit(1, 0);
         __syncthreads();
         for (int base = begin;; base += TK, buffer ^= 1) {
-            const uint64_t usable = __ballot(off >= 0);
             const bool more = stop - base > TK;
+            const uint64_t usable = __ballot(off >= 0);
             if (more) {
                 off = offset_at(base + TK, next_block);
-                next_block = block_at(stop - base > 2 * TK ? base + 2 * TK : stop);
+                next_block = block_at(base + 2 * TK);
                 request(off, buffer ^ 1);
             }
-            // A wave whose rows see nothing of these tokens has only helped to load them.
-            if (!idle && base <= p_last && base + (TK - 1) >= low_first) {
-                const uint8_t *k_lds = lds[buffer][0];
-                f32x16 s[TB];
-#pragma unroll
-                for (int t = 0; t < TB; ++t) {
-#pragma unroll
-                    for (int x = 0; x < 16; ++x)
-                        s[t][x] = 0.f;
-#pragma unroll
-                    for (int k = 0; k < KS; ++k) {
-                        const u32x4 x = *reinterpret_cast<const u32x4 *>(k_lds + t * 32 * ROW + k_at +
-                                                                         ((2 * k + half) ^ k_swizzle) * 16);
-                        s[t] = mfma_32x32x16(x, qf[k], s[t], T{});
-                    }
-                }
-                interleave<TB * KS, 1, 6>();
-                const bool edge = usable != ~uint64_t{0} || p_first - base < TK - 1 || base < low_last;
-                // Scores in powers of 2; in the plain case the factor is left to the exponent's argument.
-                const float factor = PLAIN ? scale : 1.f;
-                if constexpr (!PLAIN) {
-                    const auto each = [&](auto &&f) {
-#pragma unroll
-                        for (int t = 0; t < TB; ++t)
-#pragma unroll
-                            for (int x = 0; x < 16; ++x)
-                                s[t][x] = f(s[t][x], t * 32 + 8 * (x >> 2) + half * 4 + (x & 3));
-                    };
-                    if (a.softcap > 0.f) {
-                        const float inv = a.scale / a.softcap, cap = a.softcap * kLog2e;
-                        each([&](float y, int) { return capped(y, inv, cap); });
-                    } else {
-                        each([&](float y, int) { return y * scale; });
-                    }
-                    if (a.slopes)
-                        each([&](float y, int at) { return y - slope * static_cast<float>(p_row - (base + at)); });
-                }
-                if (edge) {
-                    // Tokens of this round that the row sees, counted from `base`: [from, to), and usable ones.
-                    const int to = p_row - base + 1, from = a.window > 0 ? to - a.window : INT32_MIN;
-                    const uint64_t mine = usable >> (half * 4);
+            // (Addresses are worked out where they are used: kept, they would cost registers.)
+            asm volatile("" : "+v"(k_at), "+v"(v_at));
+            take_scores(buffer);
+            const bool edge = usable != ~uint64_t{0} || p_first - base < TK - 1 || base < low_last;
+            // Scores in powers of 2; in the plain case the factor is left to the exponent's argument.
+            const float factor = PLAIN ? scale : 1.f;
+            if constexpr (!PLAIN) {
+                const auto each = [&](auto &&f) {
 #pragma unroll
                     for (int t = 0; t < TB; ++t)
 #pragma unroll
-                        for (int x = 0; x < 16; ++x) {
-                            const int bit = t * 32 + 8 * (x >> 2) + (x & 3), at = bit + half * 4;
-                            const bool sees = (mine >> bit & 1) && at < to && at >= from;
-                            s[t][x] = sees ? s[t][x] : -INFINITY;
-                        }
+                        for (int x = 0; x < NS; ++x)
+                            s[t][x] = f(s[t][x], t * 32 + token_of(x, part));
+                };
+                if (a.softcap > kSmallCap) {
+                    const float inv = a.scale / a.softcap, cap = a.softcap * kLog2e;
+                    each([&](float y, int) { return capped(y, inv, cap); });
+                } else if (a.softcap > 0.f) {
+                    const float twice = 2.f * kLog2e * a.scale / a.softcap, cap = a.softcap * kLog2e;
+                    each([&](float y, int) { return small_capped(y, twice, cap); });
+                } else {
+                    each([&](float y, int) { return y * scale; });
                 }
-                float top = -INFINITY;
-#pragma unroll
-                for (int t = 0; t < TB; ++t)
-#pragma unroll
-                    for (int x = 0; x < 16; x += 2)
-                        top = fmaxf(fmaxf(top, s[t][x]), s[t][x + 1]);
-                top *= factor;
-                if (__any(top > m + 8.f)) {
-                    const float next = fmaxf(m, fmaxf(top, other_half(top))), f = __builtin_amdgcn_exp2f(m - next);
-                    m = next;
-                    l *= f;
-#pragma unroll
-                    for (int d = 0; d < DB; ++d)
-#pragma unroll
-                        for (int x = 0; x < 16; ++x)
-                            acc[d][x] *= f;
-                }
-                const float zero = m - T::kShift;
-                u32x4 p[TB][2];
-                float sums[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int t = 0; t < TB; ++t)
-#pragma unroll
-                    for (int x = 0; x < 16; x += 2) {
-                        const float e0 = __builtin_amdgcn_exp2f(fmaf(s[t][x], factor, -zero));
-                        const float e1 = __builtin_amdgcn_exp2f(fmaf(s[t][x + 1], factor, -zero));
-                        sums[x & 2] += e0;
-                        sums[(x & 2) + 1] += e1;
-                        p[t][x >> 3][x >> 1 & 3] = T::pack(e0, e1);
-                    }
-                l += (sums[0] + sums[1]) + (sums[2] + sums[3]);
-                lds_byte *v_lds = (lds_byte *)(lds[buffer][1]);  // (a cast between address spaces)
-#pragma unroll
-                for (int t = 0; t < TB; ++t)
-#pragma unroll
-                    for (int j = 0; j < 2; ++j)
-#pragma unroll
-                        for (int d = 0; d < DB; ++d) {
-                            const int at = (t * 32 + j * 16) * ROW;
-                            const u32x2 x = read_turned(v_lds + v_at[d] + at), y = read_turned(v_lds + v_at[d] + at + 8 * ROW);
-                            acc[d] = mfma_32x32x16(u32x4{x[0], x[1], y[0], y[1]}, p[t][j], acc[d], T{});
-                        }
+                if (a.slopes)
+                    each([&](float y, int at) { return y - slope * static_cast<float>(p_row - (base + at)); });
             }
+            if (edge) {
+                // Tokens of this round that the row sees, counted from `base`: [from, to), and usable ones.
+                const int to = p_row - base + 1, from = a.window > 0 ? to - a.window : INT32_MIN;
+                const uint64_t mine = usable >> token_of(0, part);
+#pragma unroll
+                for (int t = 0; t < TB; ++t)
+#pragma unroll
+                    for (int x = 0; x < NS; ++x) {
+                        const int bit = t * 32 + token_of(x, 0), at = t * 32 + token_of(x, part);
+                        const bool sees = (mine >> bit & 1) && at < to && at >= from;
+                        s[t][x] = sees ? s[t][x] : -INFINITY;
+                    }
+            }
+            float top = -INFINITY;
+#pragma unroll
+            for (int t = 0; t < TB; ++t)
+#pragma unroll
+                for (int x = 0; x < NS; x += 2)
+                    top = fmaxf(fmaxf(top, s[t][x]), s[t][x + 1]);
+            top *= factor;
+            if (__any(top > m + 8.f)) {
+                const float higher = fmaxf(m, over_parts(top)), f = __builtin_amdgcn_exp2f(m - higher);
+                m = higher;
+                l *= f;
+#pragma unroll
+                for (int d = 0; d < DB; ++d)
+#pragma unroll
+                    for (int x = 0; x < AN; ++x)
+                        acc[d][x] *= f;
+            }
+            const float zero = m - T::kShift;
+            u32x4 p[TB][SETS];
+            float sums[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int t = 0; t < TB; ++t)
+#pragma unroll
+                for (int x = 0; x < NS; x += 2) {
+                    const float e0 = __builtin_amdgcn_exp2f(fmaf(s[t][x], factor, -zero));
+                    const float e1 = __builtin_amdgcn_exp2f(fmaf(s[t][x + 1], factor, -zero));
+                    sums[x & 2] += e0;
+                    sums[(x & 2) + 1] += e1;
+                    p[t][x >> 3][x >> 1 & 3] = T::pack(e0, e1);
+                }
+            l += (sums[0] + sums[1]) + (sums[2] + sums[3]);
+            lds_byte *v_lds = (lds_byte *)(lds[1][buffer]);  // (a cast between address spaces)
+#pragma unroll
+            for (int t = 0; t < TB; ++t)
+#pragma unroll
+                for (int j = 0; j < SETS; ++j)
+#pragma unroll
+                    for (int d = 0; d < DB; ++d) {
+                        lds_byte *at = v_lds + (v_at ^ d * 2 * RW) + (t * 32 + j * 16) * ROW;
+                        const u32x2 x = read_turned(at), y = read_turned(at + (WIDE ? 8 : 4) * ROW);
+                        acc[d] = product(u32x4{x[0], x[1], y[0], y[1]}, p[t][j], acc[d], T{});
+                    }
+            interleave<TB * SETS * DB, 2, 3, 0>();
             if (!more)
                 break;
-            deposit(buffer ^ 1);
+            deposit(0, buffer ^ 1);
+            deposit(1, buffer ^ 1);
             __syncthreads();
         }
     }
 
-    l += other_half(l);
+    l += __shfl_xor(l, 32);
+    if constexpr (!WIDE)
+        l += __shfl_xor(l, 16);
     if (!row_ok)
         return;
     const float inv = l == 0.f ? 0.f : a.v_scale / l;
@@ -333,8 +393,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void tail_kernel(const AttendArgs a
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
-        for (int x = 0; x < 16; x += 4) {
-            const int col = d * 32 + 2 * x + half * 4;
+        for (int x = 0; x < AN; x += 4) {
+            const int col = d * RW + 2 * x + part * 4;
             if (col >= pg.D)
                 continue;
             if (whole) {
@@ -346,7 +406,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void tail_kernel(const AttendArgs a
                     f32x4{acc[d][x], acc[d][x + 1], acc[d][x + 2], acc[d][x + 3]};
             }
         }
-    if (half == 0) {
+    if (part == 0) {
         if (whole) {
             a.lse[static_cast<int64_t>(seq.q0 + row_i) * a.heads + head] =
                 l == 0.f ? -INFINITY : (m - T::kShift + __builtin_amdgcn_logf(l)) * kLn2;
@@ -360,12 +420,12 @@ __global__ __launch_bounds__(64 * kWaves, 2) void tail_kernel(const AttendArgs a
 // What each token received: a wave holds K of 32 tokens, goes over the rows that see them, 32 at a time, with their
 // scores taken again, and adds up exp2(s - lse) for each token; a token's 32 partial sums are joined at the end.
 template <class T, bool FP8, int DP>
-__global__ __launch_bounds__(64 * kWaves) void weigh_kernel(const AttendArgs a) {
+__global__ __launch_bounds__(64 * kWeighWaves) void weigh_kernel(const AttendArgs a) {
     constexpr int KC = DP * (FP8 ? 1 : 2) / 32;  // 16-byte pieces of a token's K in a lane
     const Pages &pg = a.pages;
     const int lane = threadIdx.x & 63, c = lane & 31, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int b = blockIdx.z, h = blockIdx.y, base = (blockIdx.x * kWaves + wave) * 32;
+    const int b = blockIdx.z, h = blockIdx.y, base = (blockIdx.x * kWeighWaves + wave) * 32;
     Sequence seq;
     if (!sequence(a.batch, b, pg.err, seq) || base >= seq.n)
         return;
@@ -458,21 +518,21 @@ __global__ __launch_bounds__(64 * kWaves) void weigh_kernel(const AttendArgs a) 
     }
 }
 
-template <class T, bool FP8, int DP, int TK, bool PLAIN>
+template <class T, bool FP8, int DP, int TK, int RW, bool PLAIN>
 void launch(const AttendArgs &a, const Parts &parts, int max_queries, hipStream_t stream) {
     const int tiles = static_cast<int>((static_cast<int64_t>(max_queries) * a.group + kRows - 1) / kRows);
     const uint32_t grid = static_cast<uint32_t>(tiles) * parts.splits * a.pages.H * a.num_seqs;
-    hipLaunchKernelGGL((tail_kernel<T, FP8, DP, TK, PLAIN>), dim3(grid), dim3(64 * kWaves), 0, stream, a, parts, tiles);
+    hipLaunchKernelGGL((tail_kernel<T, FP8, DP, TK, RW, PLAIN>), dim3(grid), dim3(64 * kRows / RW), 0, stream, a, parts, tiles);
 }
 
 template <class T, bool FP8, bool PLAIN>
 void launch(const AttendArgs &a, const Parts &parts, int max_queries, hipStream_t stream) {
     if (a.pages.D > 128)
-        launch<T, FP8, 256, 32, PLAIN>(a, parts, max_queries, stream);
+        launch<T, FP8, 256, 64, 16, PLAIN>(a, parts, max_queries, stream);
     else if (a.pages.D > 64)
-        launch<T, FP8, 128, 64, PLAIN>(a, parts, max_queries, stream);
+        launch<T, FP8, 128, 64, 32, PLAIN>(a, parts, max_queries, stream);
     else
-        launch<T, FP8, 64, 64, PLAIN>(a, parts, max_queries, stream);
+        launch<T, FP8, 64, 64, 32, PLAIN>(a, parts, max_queries, stream);
 }
 
 template <class T, bool FP8>
@@ -485,14 +545,14 @@ void launch(const AttendArgs &a, const Parts &parts, int max_queries, hipStream_
 
 template <class T, bool FP8>
 void launch_weigh(const AttendArgs &a, hipStream_t stream) {
-    const dim3 grid(static_cast<uint32_t>((a.batch.max_len + 32 * kWaves - 1) / (32 * kWaves)),
+    const dim3 grid(static_cast<uint32_t>((a.batch.max_len + 32 * kWeighWaves - 1) / (32 * kWeighWaves)),
                     static_cast<uint32_t>(a.pages.H), static_cast<uint32_t>(a.num_seqs));
     if (a.pages.D > 128)
-        hipLaunchKernelGGL((weigh_kernel<T, FP8, 256>), grid, dim3(64 * kWaves), 0, stream, a);
+        hipLaunchKernelGGL((weigh_kernel<T, FP8, 256>), grid, dim3(64 * kWeighWaves), 0, stream, a);
     else if (a.pages.D > 64)
-        hipLaunchKernelGGL((weigh_kernel<T, FP8, 128>), grid, dim3(64 * kWaves), 0, stream, a);
+        hipLaunchKernelGGL((weigh_kernel<T, FP8, 128>), grid, dim3(64 * kWeighWaves), 0, stream, a);
     else
-        hipLaunchKernelGGL((weigh_kernel<T, FP8, 64>), grid, dim3(64 * kWaves), 0, stream, a);
+        hipLaunchKernelGGL((weigh_kernel<T, FP8, 64>), grid, dim3(64 * kWeighWaves), 0, stream, a);
 }
 
 }  // namespace

@@ -74,8 +74,8 @@ kv_status check_batch(const kv_cache *cache, const kv_batch *batch) {
         return KV_OK;
     if (batch->num_seqs > 65535)
         return fail(KV_EUNSUPPORTED, "%d sequences in one call (at most 65,535)", batch->num_seqs);
-    if (batch->max_len > INT32_MAX - 127)
-        return fail(KV_EUNSUPPORTED, "sequences of up to %d tokens (at most 2^31 - 128)", batch->max_len);
+    if (batch->max_len > INT32_MAX - 1023)
+        return fail(KV_EUNSUPPORTED, "sequences of up to %d tokens (at most 2^31 - 1024)", batch->max_len);
     if (batch->max_len > static_cast<int64_t>(batch->table_len) * cache->layout.block_size)
         return fail(KV_EINVAL, "max_len %d exceeds %d pages of %d tokens", batch->max_len, batch->table_len,
                     cache->layout.block_size);

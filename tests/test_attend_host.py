@@ -158,7 +158,7 @@ def test_attend_workspace_follows_the_batch():
     cache = _cache(kvx, kvx.make_layout(1, 8, 128, 2, 16, 16), num_blocks=1 << 20)
     o = attend.KvAttendOptions(cache_dtype=attend.KV_DTYPE_BF16)
     for seqs, queries, length in ((1, 1, 1), (1, 1, 131077), (64, 1, 8192), (1, 2085, 34853), (7, 37, 131072),
-                                  (65535, 1, 16), (1, 1, 2**31 - 128), (3, 100000, 200000)):
+                                  (65535, 1, 16), (1, 1, 2**31 - 1024), (3, 100000, 200000)):
         tokens = seqs * queries
         b = _batch(attend, num_seqs=seqs, max_queries=queries, num_queries=tokens, max_len=length,
                    table_len=-(-length // 16), table_stride=-(-length // 16), starts=SOME)
