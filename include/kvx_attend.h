@@ -131,12 +131,18 @@ KV_API int64_t kv_attend_workspace(const kv_cache *cache, const kv_batch *batch,
  *   keep:         DEVICE int32[num_seqs][heads][budget]: the kept tokens, ascending, then -1;
  *   kept_lens:    DEVICE int32[num_seqs]: min(lens[b], budget);
  *   kept_weights: DEVICE float[num_seqs][heads][budget]: their weights, then 0; or NULL.
+ *   workspace:    DEVICE, kv_keep_workspace's bytes (4-byte aligned; may be NULL for 0 bytes), as kv_attend's.
  * heads: one row per KV head, or 1 for a choice that all heads share.  Errors: KV_EINVAL (NULL, sizes; sinks + recent
- * > budget), KV_EUNSUPPORTED (more than 65,535 sequences), KV_EHIP.
+ * > budget; a workspace that is too small), KV_EUNSUPPORTED (more than 65,535 sequences, more than 2^31 - 2^20
+ * tokens), KV_EHIP.
  */
 KV_API kv_status kv_keep(const float *weights, int64_t seq_stride, int64_t head_stride, const int32_t *lens,
                          int32_t num_seqs, int32_t heads, int32_t max_len, int32_t budget, int32_t sinks,
-                         int32_t recent, int32_t *keep, int32_t *kept_lens, float *kept_weights, void *stream);
+                         int32_t recent, int32_t *keep, int32_t *kept_lens, float *kept_weights, void *workspace,
+                         int64_t workspace_bytes, void *stream);
+
+/* Bytes of workspace that kv_keep needs (host only; 0 unless a few long rows are cut).  Negative: a kv_status. */
+KV_API int64_t kv_keep_workspace(int32_t num_seqs, int32_t heads, int32_t max_len, int32_t budget);
 
 /*
  * kv_compact -- copy the kept tokens' K and V rows of layer `layer` into the pages of dst_tables: for j < kept_lens[b],

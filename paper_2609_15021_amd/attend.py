@@ -24,7 +24,8 @@ KV_ASYNC_BAD_BATCH = 2
 
 _DTYPES = {torch.bfloat16: KV_DTYPE_BF16, torch.float16: KV_DTYPE_F16, torch.float8_e4m3fn: KV_DTYPE_E4M3}
 
-EXPORTS = ("kv_append", "kv_attend", "kv_attend_workspace", "kv_keep", "kv_compact", "kv_attend_async_error")
+EXPORTS = ("kv_append", "kv_attend", "kv_attend_workspace", "kv_keep", "kv_keep_workspace", "kv_compact",
+           "kv_attend_async_error")
 
 
 class KvRows(ctypes.Structure):
@@ -54,7 +55,8 @@ def _declare(lib):
             ("kv_append", [cache, i32, batch, rows, rows, i32, f32, f32, P], i32),
             ("kv_attend", [cache, i32, batch, options, rows, rows, P, P, i64, P], i32),
             ("kv_attend_workspace", [cache, batch, options, rows], i64),
-            ("kv_keep", [P, i64, i64, P, i32, i32, i32, i32, i32, i32, P, P, P, P], i32),
+            ("kv_keep", [P, i64, i64, P, i32, i32, i32, i32, i32, i32, P, P, P, P, i64, P], i32),
+            ("kv_keep_workspace", [i32, i32, i32, i32], i64),
             ("kv_compact", [cache, i32, i32, P, i64, i32, P, i32, i32, P, P, i64, i32, P], i32),
             ("kv_attend_async_error", [ctypes.c_int], i32)):
         fn = getattr(lib, name)
@@ -233,14 +235,19 @@ def kv_keep(weights, lens, budget: int, *, sinks: int = 0, recent: int = 0, max_
         raise ValueError(f"weights of {L} tokens for sequences of up to {max_len}")
     if budget < 1:
         raise ValueError(f"budget must be positive (got {budget})")
+    most = L if max_len is None else int(max_len)
+    need = _lib.kv_keep_workspace(B, H, most, int(budget))
+    if need < 0:
+        _raise(need)
     s = _stream(stream)
     with _allocating(s, stream):
+        workspace = torch.empty(need, dtype=torch.uint8, device=weights.device) if need else None
         keep = torch.empty((B, H, int(budget)), dtype=torch.int32, device=weights.device)
         kept_lens = torch.empty(B, dtype=torch.int32, device=weights.device)
         kept_weights = torch.empty((B, H, int(budget)), dtype=torch.float32, device=weights.device)
     _raise(_lib.kv_keep(weights.data_ptr(), weights.stride(0), weights.stride(1), lens.data_ptr(), B, H,
-                        L if max_len is None else int(max_len), int(budget), int(sinks), int(recent), keep.data_ptr(),
-                        kept_lens.data_ptr(), kept_weights.data_ptr(), _handle(s)))
+                        most, int(budget), int(sinks), int(recent), keep.data_ptr(), kept_lens.data_ptr(),
+                        kept_weights.data_ptr(), workspace.data_ptr() if need else None, need, _handle(s)))
     _used(s, weights, lens)
     return keep, kept_lens, kept_weights
 

@@ -27,7 +27,7 @@ def test_exports():
     exported = {ln.split()[-1] for ln in out.splitlines() if " T " in ln}
     assert set(attend.EXPORTS) <= exported
     for name in attend.EXPORTS:
-        assert callable(getattr(attend, name, None)) or name == "kv_attend_workspace"
+        assert callable(getattr(attend, name, None)) or name.endswith("_workspace")
 
 
 def test_header_compiles_as_plain_c(tmp_path):
@@ -170,14 +170,21 @@ def test_attend_workspace_follows_the_batch():
 def test_keep_and_compact_refusals():
     from paper_2609_15021_amd import attend, kvx
 
-    def keep(weights=SOME, lens=SOME, seqs=2, heads=2, max_len=64, budget=16, sinks=2, recent=4, out=SOME, kept=SOME):
+    def keep(weights=SOME, lens=SOME, seqs=2, heads=2, max_len=64, budget=16, sinks=2, recent=4, out=SOME, kept=SOME,
+             space=SOME, size=1 << 30):
         return kvx._lib.kv_keep(weights, 128, 64, lens, seqs, heads, max_len, budget, sinks, recent, out, kept, SOME,
-                                None)
+                                space, size, None)
 
     for changes in (dict(weights=None), dict(lens=None), dict(out=None), dict(kept=None), dict(seqs=-1), dict(heads=0),
                     dict(max_len=-1), dict(budget=0), dict(sinks=-1), dict(recent=-1), dict(sinks=13)):
         assert keep(**changes) == kvx.KV_EINVAL, changes
     assert keep(seqs=65536) == kvx.KV_EUNSUPPORTED
+    assert keep(max_len=2**31 - 1) == kvx.KV_EUNSUPPORTED
+    need = kvx._lib.kv_keep_workspace(2, 2, 100000, 16)
+    assert need > 0 and kvx._lib.kv_keep_workspace(2, 2, 100000, 100000) == 0
+    assert keep(max_len=100000, size=need - 1) == keep(max_len=100000, space=None) == kvx.KV_EINVAL
+    assert keep(max_len=100000, space=SOME + 2) == kvx.KV_EUNSUPPORTED
+    assert kvx._lib.kv_keep_workspace(2, 2, 64, 0) == kvx.KV_EINVAL
     assert keep(seqs=0, lens=None) == kvx.KV_OK
 
     def compact(cache, layer=0, seqs=2, src=SOME, stride=4, length=4, idx=SOME, heads=2, budget=16, kept=SOME, dst=SOME,

@@ -387,6 +387,19 @@ def test_keep_long(budget):
     assert kept.cpu().tolist() == [budget, budget]
 
 
+@pytest.mark.parametrize("seqs,heads,longest", [(65, 2, 9001), (1, 2, 17000), (128, 1, 8193)])
+def test_keep_many_rows_and_pieces(seqs, heads, longest):
+    """Rows that no longer fit one workgroup's registers: many of them, and few, with lengths around the pieces' edges."""
+    gen = torch.Generator().manual_seed(longest)
+    w = (torch.rand(seqs, heads, longest, generator=gen) * 50).round() / 50  # every value many times
+    edges = [longest, 8192, 8193, 4096, 4097, 1, 0, 3, 700, 699]
+    lens = [edges[i % len(edges)] for i in range(seqs)]
+    got = attend.kv_keep(w.to(DEV), torch.tensor(lens, dtype=torch.int32, device=DEV), 700, sinks=3, recent=200)
+    want = ref.keep(w.numpy(), lens, 700, 3, 200)
+    assert torch.equal(got[0].cpu(), torch.from_numpy(want[0])) and got[1].cpu().tolist() == want[1].tolist()
+    assert np.array_equal(got[2].cpu().numpy(), want[2])
+
+
 def test_keep_refuses_lengths_on_the_device():
     w = torch.rand(3, 1, 50, device=DEV)
     keep, kept, _ = attend.kv_keep(w, torch.tensor([51, 20, -1], dtype=torch.int32, device=DEV), 8)
