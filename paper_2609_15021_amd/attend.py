@@ -1,7 +1,7 @@
 """Python binding of ``include/kvx_attend.h``: operators on a replica's paged KV cache (argument marshalling only).
 
 Every step runs in the HIP library that ``kvx`` binds (``libkvx.so``); caches are ``kvx.Cache`` handles, errors
-``kvx.KvError``, streams as for ``kvx.kv_store``.  The names are the C ABI's.
+``kvx.KvError``, ``stream`` a torch stream, a raw handle, or None for the current one.  The names are the C ABI's.
 
 A batch of sequences is ``tables`` (int32 [B][pages]: block tables), ``lens`` (int32 [B]: tokens in the cache, the new
 ones among them) and ``starts`` (int32 [B + 1]: where each sequence's new tokens start among all; None: one each).  All
@@ -11,6 +11,7 @@ default (and at most) what the shapes allow.  Tight bounds size the launches bet
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 
 import torch
@@ -66,10 +67,14 @@ def _declare(lib):
 _declare(_lib)
 
 
+# A decoding step makes a call per layer, and short calls are bound by this module: checks read each property once, and
+# what only the numbers decide is remembered by them.
+
+
 def _ints(t, name: str, dims: int, rows=None):
     """A device tensor of int32 whose last dimension is dense."""
-    if not isinstance(t, torch.Tensor) or t.dtype != torch.int32 or not t.is_cuda or t.dim() != dims or \
-            (t.numel() and t.stride(-1) != 1):
+    if not isinstance(t, torch.Tensor) or t.dtype is not torch.int32 or not t.is_cuda or t.dim() != dims or \
+            (t.stride(-1) != 1 and t.numel()):
         raise TypeError(f"{name} must be a {dims}-dimensional int32 device tensor with a dense last dimension")
     if rows is not None and t.shape[0] != rows:
         raise ValueError(f"{name} has {t.shape[0]} rows; {rows} are needed")
@@ -77,27 +82,29 @@ def _ints(t, name: str, dims: int, rows=None):
 
 
 def _rows(t, name: str, head_dim: int) -> KvRows:
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dim() != 3 or t.dtype not in (torch.bfloat16, torch.float16):
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dim() != 3 or \
+            t.dtype not in (torch.bfloat16, torch.float16):
         raise TypeError(f"{name} must be a [tokens][heads][D] device tensor of bfloat16 or float16")
-    if t.shape[2] != head_dim or (t.numel() and t.stride(2) != 1):
-        raise ValueError(f"{name}: rows of {t.shape[2]} elements {t.stride(2)} apart; dense rows of {head_dim} are needed")
-    return KvRows(t.data_ptr(), t.stride(0), t.stride(1), t.shape[1], _DTYPES[t.dtype])
+    _, heads, width = t.shape
+    token, head, column = t.stride()
+    if width != head_dim or (column != 1 and t.numel()):
+        raise ValueError(f"{name}: rows of {width} elements {column} apart; dense rows of {head_dim} are needed")
+    return KvRows(t.data_ptr(), token, head, heads, _DTYPES[t.dtype])
 
 
 def _batch(cache: Cache, tables, lens, starts, tokens: int, max_q, max_len) -> KvBatch:
-    tables = _ints(tables, "tables", 2)
-    B, pages = tables.shape
+    B, pages = _ints(tables, "tables", 2).shape
     _ints(lens, "lens", 1, B)
     if starts is None:
         if tokens != B:
             raise ValueError(f"{tokens} new tokens for {B} sequences of one each: starts is needed")
-        max_q = 1
+        max_q, starts_at = 1, None
     else:
-        _ints(starts, "starts", 1, B + 1)
+        starts_at = _ints(starts, "starts", 1, B + 1).data_ptr()
         max_q = max(1, tokens if max_q is None else int(max_q))
     most = min(pages * cache.layout.block_size, 2**31 - 1024)
     return KvBatch(B, max_q, tokens, most if max_len is None else min(most, int(max_len)), pages, 0, tables.stride(0),
-                   tables.data_ptr(), lens.data_ptr(), None if starts is None else starts.data_ptr())
+                   tables.data_ptr(), lens.data_ptr(), starts_at)
 
 
 def _cache_dtype(cache: Cache, dtype, rows) -> int:
@@ -109,37 +116,26 @@ def _cache_dtype(cache: Cache, dtype, rows) -> int:
     return _DTYPES[dtype]
 
 
-def _stream(stream):
-    return torch.cuda.current_stream(torch.cuda.current_device()) if stream is None else stream
+def _call_stream(stream):
+    """(the stream's handle, the context in which the call's own tensors are made): they belong to the call's stream, which
+    may be another than the current one."""
+    if stream is None:
+        return torch.cuda.current_stream(torch.cuda.current_device()).cuda_stream, _HERE
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(stream))
+    return stream.cuda_stream, torch.cuda.stream(stream)
 
 
-def _handle(stream) -> int:
-    return stream.cuda_stream if isinstance(stream, torch.cuda.Stream) else int(stream)
+_HERE = contextlib.nullcontext()
 
 
 def _used(stream, *tensors) -> None:
-    for t in tensors:
-        if t is not None:
-            _in_use_on(t, stream)
-
-
-class _allocating:
-    """New tensors belong to the call's stream, which may be another than the current one."""
-
-    def __init__(self, stream, given):
-        self.context = None
-        if given is not None:
-            if not isinstance(stream, torch.cuda.Stream):
-                stream = torch.cuda.ExternalStream(int(stream))
-            self.context = torch.cuda.stream(stream)
-
-    def __enter__(self):
-        if self.context is not None:
-            self.context.__enter__()
-
-    def __exit__(self, *exc):
-        if self.context is not None:
-            self.context.__exit__(*exc)
+    """Tensors used on a stream that was named: as with a store's block table, torch must not hand their memory out again
+    before the call's work is done there.  (With no stream named the call is like torch's own on the current stream.)"""
+    if stream is not None:
+        for t in tensors:
+            if t is not None:
+                _in_use_on(t, stream)
 
 
 def kv_append(cache: Cache, layer: int, k, v, tables, lens, starts=None, *, max_q=None, max_len=None, dtype=None,
@@ -154,10 +150,10 @@ def kv_append(cache: Cache, layer: int, k, v, tables, lens, starts=None, *, max_
     if k.shape != v.shape:
         raise ValueError(f"k and v differ in shape: {tuple(k.shape)} and {tuple(v.shape)}")
     batch = _batch(cache, tables, lens, starts, k.shape[0], max_q, max_len)
-    s = _stream(stream)
+    handle, _ = _call_stream(stream)
     _raise(_lib.kv_append(ctypes.byref(cache.struct), int(layer), ctypes.byref(batch), ctypes.byref(kr), ctypes.byref(vr),
-                          _cache_dtype(cache, dtype, k), float(k_scale), float(v_scale), _handle(s)))
-    _used(s, k, v, tables, lens, starts)
+                          _cache_dtype(cache, dtype, k), float(k_scale), float(v_scale), handle))
+    _used(stream, k, v, tables, lens, starts)
 
 
 def kv_attend(cache: Cache, layer: int, q, tables, lens, starts=None, *, max_q=None, max_len=None, dtype=None,
@@ -203,23 +199,34 @@ def kv_attend(cache: Cache, layer: int, q, tables, lens, starts=None, *, max_q=N
     if lse is not None and (lse.dtype != torch.float32 or lse.shape != heads or not lse.is_cuda or
                             not lse.is_contiguous()):
         raise TypeError(f"lse must be a contiguous float32 device tensor of {heads}")
-    need = _lib.kv_attend_workspace(ctypes.byref(cache.struct), ctypes.byref(batch), ctypes.byref(options),
-                                    ctypes.byref(qr))
-    if need < 0:
-        _raise(need)
-    s = _stream(stream)
-    with _allocating(s, stream):
+    layout = cache.layout
+    key = (layout.num_kv_heads, layout.head_dim, layout.elem_bytes, layout.block_size, batch.num_seqs, batch.max_queries,
+           batch.num_queries, batch.max_len, options.window, weights is None, q.shape[1])
+    need = _attend_bytes.get(key)
+    if need is None:
+        need = _lib.kv_attend_workspace(ctypes.byref(cache.struct), ctypes.byref(batch), ctypes.byref(options),
+                                        ctypes.byref(qr))
+        if need < 0:
+            _raise(need)
+        if len(_attend_bytes) >= 4096:
+            _attend_bytes.clear()
+        _attend_bytes[key] = need
+    handle, here = _call_stream(stream)
+    with here:
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            out = q.new_empty(q.shape)
         if lse is None:
             lse = torch.empty(heads, dtype=torch.float32, device=q.device)
         workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
-    outr = _rows(out, "out", cache.layout.head_dim)
+    outr = _rows(out, "out", layout.head_dim)
     _raise(_lib.kv_attend(ctypes.byref(cache.struct), int(layer), ctypes.byref(batch), ctypes.byref(options),
                           ctypes.byref(qr), ctypes.byref(outr), lse.data_ptr(),
-                          workspace.data_ptr() if need else None, need, _handle(s)))
-    _used(s, q, tables, lens, starts, slopes, weights, prior, out, lse)
+                          workspace.data_ptr() if need else None, need, handle))
+    _used(stream, q, tables, lens, starts, slopes, weights, prior, out, lse)
     return out, lse
+
+
+_attend_bytes = {}  # kv_attend_workspace by the numbers that it depends on
 
 
 def kv_keep(weights, lens, budget: int, *, sinks: int = 0, recent: int = 0, max_len=None, stream=None):
@@ -239,16 +246,16 @@ def kv_keep(weights, lens, budget: int, *, sinks: int = 0, recent: int = 0, max_
     need = _lib.kv_keep_workspace(B, H, most, int(budget))
     if need < 0:
         _raise(need)
-    s = _stream(stream)
-    with _allocating(s, stream):
+    handle, here = _call_stream(stream)
+    with here:
         workspace = torch.empty(need, dtype=torch.uint8, device=weights.device) if need else None
         keep = torch.empty((B, H, int(budget)), dtype=torch.int32, device=weights.device)
         kept_lens = torch.empty(B, dtype=torch.int32, device=weights.device)
         kept_weights = torch.empty((B, H, int(budget)), dtype=torch.float32, device=weights.device)
     _raise(_lib.kv_keep(weights.data_ptr(), weights.stride(0), weights.stride(1), lens.data_ptr(), B, H,
                         most, int(budget), int(sinks), int(recent), keep.data_ptr(), kept_lens.data_ptr(),
-                        kept_weights.data_ptr(), workspace.data_ptr() if need else None, need, _handle(s)))
-    _used(s, weights, lens)
+                        kept_weights.data_ptr(), workspace.data_ptr() if need else None, need, handle))
+    _used(stream, weights, lens)
     return keep, kept_lens, kept_weights
 
 
@@ -262,11 +269,11 @@ def kv_compact(cache: Cache, layer: int, tables, keep, kept_lens, dst_tables, *,
         raise TypeError("keep must be contiguous")
     _ints(kept_lens, "kept_lens", 1, B)
     _ints(dst_tables, "dst_tables", 2, B)
-    s = _stream(stream)
+    handle, _ = _call_stream(stream)
     _raise(_lib.kv_compact(ctypes.byref(cache.struct), int(layer), B, tables.data_ptr(), tables.stride(0), tables.shape[1],
                            keep.data_ptr(), keep.shape[1], keep.shape[2], kept_lens.data_ptr(), dst_tables.data_ptr(),
-                           dst_tables.stride(0), dst_tables.shape[1], _handle(s)))
-    _used(s, tables, keep, kept_lens, dst_tables)
+                           dst_tables.stride(0), dst_tables.shape[1], handle))
+    _used(stream, tables, keep, kept_lens, dst_tables)
 
 
 def kv_attend_async_error(clear: bool = False) -> int:

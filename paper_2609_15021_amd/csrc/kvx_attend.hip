@@ -61,23 +61,13 @@ struct Plan {
     int32_t max_queries, max_rows;  // of a sequence; rows per KV head in the step kernel
     bool tail;                      // some sequence may have more than kStepRows rows
     bool scores;                    // weights_out from the step kernel's scores
+    bool parts;                     // the step kernel's sequences may have several parts
     int64_t score_len, step_stats, step_sums, tail_stats, tail_sums, scores_at, bytes;
-    Parts step_parts, tail_parts;
+    Shares shares;
+    Parts tail_parts;
 };
 
 int64_t round_up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
-
-// Parts of a multiple of `unit` tokens (at most `most`) so that there are `wanted` workgroups where there are `have`
-// without a split.
-Parts parts_for(int64_t longest, int64_t have, int64_t wanted, int64_t unit, int64_t most, int64_t row_cap) {
-    Parts p{};
-    const int64_t splits = (wanted + have - 1) / have;
-    longest = std::max<int64_t>(longest, 1);
-    p.len = static_cast<int32_t>(std::min(most, round_up((longest + splits - 1) / splits, unit)));
-    p.splits = static_cast<int32_t>((longest + p.len - 1) / p.len);
-    p.row_cap = static_cast<int32_t>(row_cap);
-    return p;
-}
 
 // The tail kernel's parts.  512 of its workgroups run at once (2 per CU; 256 where D > 128), so `have` of them may leave
 // the last round nearly empty, and fewer leave CUs idle: the number of parts is the one whose rounds and joining take
@@ -101,7 +91,11 @@ Parts tail_parts_for(int64_t longest, int64_t have, int64_t rows, int64_t head_d
             best_us = us;
         }
     }
-    return parts_for(longest, 1, best, 64, INT32_MAX - 63, rows);
+    Parts p{};
+    p.len = static_cast<int32_t>(round_up((longest + best - 1) / best, 64));
+    p.splits = static_cast<int32_t>((longest + p.len - 1) / p.len);
+    p.row_cap = static_cast<int32_t>(rows);
+    return p;
 }
 
 Plan plan_of(const kv_cache *cache, const kv_batch *batch, const kv_attend_options *o, const kv_rows *q) {
@@ -116,16 +110,24 @@ Plan plan_of(const kv_cache *cache, const kv_batch *batch, const kv_attend_optio
     p.tail = all_rows > kStepRows;
     // With more rows than a tile has the scores would outgrow K itself: they are taken again instead.
     p.scores = o->weights_out && all_rows <= 16;
-    const auto longest = [&](int64_t queries) {  // tokens that a tile of rows sees
-        const int64_t window = o->window > 0 ? o->window + queries + 31 : batch->max_len;
-        return std::min<int64_t>(window, batch->max_len);
-    };
-    // The step kernel: about 4 workgroups per CU, of 128 to 4,096 tokens (a ragged batch's longest sequence must not
-    // be one workgroup's).
-    const int64_t tile = step_tile_rows(p.max_rows, static_cast<int>(D));
-    p.step_parts = parts_for(longest(kStepRows), heads * ((p.max_rows + tile - 1) / tile), 1024, 128, 4096, p.max_rows);
+    // The step kernel: as many workgroups as run at once (by its registers 2 per CU, 3 up to 64 columns, 1 with wide
+    // 2-byte rows), one each for more sequences than that.
+    const int64_t tile = step_tile_rows(p.max_rows, static_cast<int>(D)), tiles = (p.max_rows + tile - 1) / tile;
+    const int64_t at_once = D <= 64 ? 768 : D > 128 && cache->layout.elem_bytes == 2 ? 256 : 512;
+    const int64_t window = o->window > 0 ? o->window + kStepRows + 31 : batch->max_len;
+    const int64_t longest = std::max<int64_t>(std::min<int64_t>(window, batch->max_len), 1);
+    const int64_t most = (longest + kShareLen - 1) / kShareLen * batch->num_seqs;  // parts that can be
+    p.shares.target = static_cast<int32_t>(std::min(std::max<int64_t>(at_once / (H * tiles), 1), most));
+    p.shares.items = std::max(p.shares.target, batch->num_seqs) + (batch->num_seqs > 1 ? batch->num_seqs : 0);
+    if (batch->num_seqs > kShareSeqs || p.shares.target == 1)
+        p.shares.items = batch->num_seqs;
+    p.shares.num_seqs = batch->num_seqs;
+    p.shares.row_cap = p.max_rows;
+    p.parts = batch->num_seqs <= kShareSeqs && p.shares.target > 1;
     if (p.tail) {
-        p.tail_parts = tail_parts_for(longest(kTailRows), heads * ((all_rows + kTailRows - 1) / kTailRows), all_rows, D);
+        const int64_t longest_tail =
+            std::min<int64_t>(batch->max_len, o->window > 0 ? o->window + int64_t{kTailRows} + 31 : batch->max_len);
+        p.tail_parts = tail_parts_for(longest_tail, heads * ((all_rows + kTailRows - 1) / kTailRows), all_rows, D);
     }
     int64_t at = round_up(static_cast<int64_t>(batch->num_queries) * q->heads * 4, 16);
     const auto take = [&](int64_t bytes) {
@@ -134,8 +136,9 @@ Plan plan_of(const kv_cache *cache, const kv_batch *batch, const kv_attend_optio
         return here;
     };
     const auto slots = [&](const Parts &x) { return x.splits > 1 ? heads * x.row_cap * x.splits : 0; };
-    p.step_stats = take(slots(p.step_parts) * 8);
-    p.step_sums = take(slots(p.step_parts) * D * 4);
+    const int64_t shared = p.parts ? H * p.shares.items * p.shares.row_cap : 0;
+    p.step_stats = take(shared * 8);
+    p.step_sums = take(shared * D * 4);
     p.tail_stats = take(slots(p.tail_parts) * 8);
     p.tail_sums = take(slots(p.tail_parts) * D * 4);
     p.score_len = round_up(batch->max_len, 32);
@@ -180,7 +183,8 @@ kv_status attend(const kv_cache *cache, int32_t layer, const kv_batch *batch, co
     uint8_t *space = static_cast<uint8_t *>(workspace);
     a.lse = lse ? lse : reinterpret_cast<float *>(space);
     const auto at = [&](int64_t offset) { return reinterpret_cast<float *>(space + offset); };
-    Parts step = plan.step_parts, tail = plan.tail_parts;
+    Shares step = plan.shares;
+    Parts tail = plan.tail_parts;
     step.stats = at(plan.step_stats);
     step.sums = at(plan.step_sums);
     tail.stats = at(plan.tail_stats);
@@ -206,13 +210,12 @@ kv_status attend(const kv_cache *cache, int32_t layer, const kv_batch *batch, co
     a.by_group = divisor(a.group);
     if (plan.max_queries > 0) {
         KVX_HIP(launch_step(a, step, plan.max_queries, stream));
-        if (step.splits > 1)
-            KVX_HIP(launch_join(a, step, std::min(plan.max_queries, kStepRows), 1, kStepRows,
-                                step_tile_rows(plan.max_rows, cache->layout.head_dim), stream));
+        if (plan.parts)
+            KVX_HIP(launch_join_step(a, step, plan.max_queries, stream));
         if (plan.tail) {
             KVX_HIP(launch_tail(a, tail, plan.max_queries, stream));
             if (tail.splits > 1)
-                KVX_HIP(launch_join(a, tail, plan.max_queries, kStepRows + 1, INT32_MAX, kTailRows, stream));
+                KVX_HIP(launch_join_tail(a, tail, plan.max_queries, stream));
         }
     }
     if (a.weights_out && batch->max_len > 0)

@@ -53,6 +53,105 @@ __host__ __device__ __forceinline__ Span span_of(int n, int nq, int i0, int i1, 
 // Rows of a tile of the step kernel.
 inline int step_tile_rows(int max_rows, int head_dim) { return max_rows > 16 && head_dim <= 128 ? 32 : 16; }
 
+// How the step kernel shares its sequences' tokens out: in parts of one length for all, on the device, where the lengths
+// are.  A long sequence among short ones is then no workgroup's alone, and the parts number at most `target`, which fill
+// the chip once.  items >= the parts of any batch: target, or one each of more sequences than that.
+struct Shares {
+    int32_t target, items, num_seqs;
+    int32_t row_cap;  // most rows per KV head of a sequence
+    float *sums;      // [KV head][item][row_cap][D], unscaled
+    float *stats;     // [KV head][item][row_cap][2]: largest score and sum, in powers of 2
+};
+
+// A sequence's part: `split` of `parts`, `len` tokens each; its first part is item `item0`.
+struct Share {
+    int b, split, parts, len, item0;
+};
+
+constexpr int kShareSeqs = 1024;  // more sequences than this are one part each
+constexpr int kShareLen = 128;    // shortest part: 32 tokens a wave
+
+// Tokens of sequence b that the step kernel takes, from span.start on; 0 and no rows if none.
+__device__ __forceinline__ int share_tokens(const AttendArgs &a, int b, bool tell, bool &rows) {
+    const int n = a.batch.lens[b], q0 = a.batch.starts ? a.batch.starts[b] : b;
+    const int q1 = a.batch.starts ? a.batch.starts[b + 1] : b + 1, nq = q1 - q0;
+    const bool good = n >= 0 && n <= a.batch.max_len && q0 >= 0 && q1 >= q0 && q1 <= a.batch.num_queries &&
+                      nq <= a.batch.max_queries;
+    if (!good && tell)
+        report(a.pages.err, KV_ASYNC_BAD_BATCH);
+    rows = good && nq > 0 && nq <= kStepRows && nq * a.group <= kStepRows;
+    if (!rows)
+        return 0;
+    const Span span = span_of(n, nq, 0, nq, a.window);
+    return max(span.end - span.start, 0);
+}
+
+__device__ __forceinline__ int64_t sum_of_wave(int64_t x) {
+#pragma unroll
+    for (int o = 32; o; o >>= 1)
+        x += __shfl_xor(x, o);
+    return x;
+}
+
+// The part that is item `item`, or (by_seq) sequence `item`'s parts; false if there is none.  Every wave for itself.
+__device__ __forceinline__ bool share_of(const AttendArgs &a, const Shares &shares, int item, bool by_seq, Share &s) {
+    const int lane = threadIdx.x & 63, seqs = shares.num_seqs;
+    const bool tell = !by_seq && item == 0 && blockIdx.y == 0 && threadIdx.x < 64;
+    if (seqs > kShareSeqs) {
+        s = Share{item, 0, 1, INT32_MAX, item};
+        bool rows;
+        share_tokens(a, item, tell || (!by_seq && blockIdx.y == 0 && threadIdx.x == 0), rows);
+        return rows;
+    }
+    int64_t total = 0;
+    for (int b = lane; b < seqs; b += 64) {
+        bool rows;
+        total += share_tokens(a, b, tell, rows);
+    }
+    total = sum_of_wave(total);
+    // The shortest length, up to a few percent, that makes no more parts than the target.
+    const auto parts_of_seq = [&](int b, int64_t len) -> int {
+        bool rows;
+        const int tokens = share_tokens(a, b, false, rows);
+        return rows ? static_cast<int>(max((tokens + len - 1) / len, int64_t{1})) : 0;
+    };
+    const auto round_len = [](int64_t len) { return max((len + 31) / 32 * 32, int64_t{kShareLen}); };
+    int64_t len = round_len((total + shares.target - 1) / shares.target);
+    for (int tries = 0; tries < 4 && seqs > 1; ++tries) {
+        int64_t parts = 0;
+        for (int b = lane; b < seqs; b += 64)
+            parts += parts_of_seq(b, len);
+        parts = sum_of_wave(parts);
+        if (parts <= max(shares.target, seqs))
+            break;
+        len = round_len(len * parts / shares.target);
+    }
+    int item0 = 0;
+    for (int b0 = 0; b0 < seqs; b0 += 64) {
+        const int mine = b0 + lane < seqs ? parts_of_seq(b0 + lane, len) : 0;
+        int upto = mine;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int y = __shfl_up(upto, o);
+            upto += lane >= o ? y : 0;
+        }
+        const int from = item0 + upto - mine;
+        const bool here = by_seq ? b0 + lane == item : item >= from && item < from + mine;
+        const uint64_t found = __ballot(here);
+        if (found) {
+            const int at = __builtin_ctzll(found);
+            s.b = b0 + at;
+            s.parts = __builtin_amdgcn_readlane(mine, at);
+            s.item0 = __builtin_amdgcn_readlane(from, at);
+            s.split = by_seq ? 0 : item - s.item0;
+            s.len = static_cast<int>(min(len, int64_t{INT32_MAX}));
+            return s.parts > 0;
+        }
+        item0 += __builtin_amdgcn_readlane(upto, 63);
+    }
+    return false;
+}
+
 __device__ __forceinline__ int parts_of(const Span &s, int len) {
     return s.end > s.start ? (s.end - s.start + len - 1) / len : 1;
 }
@@ -125,11 +224,11 @@ __device__ __forceinline__ float small_capped(float x, float twice, float cap) {
 }
 
 // Each covers the sequences of its kind only, whatever else is in the batch.
-hipError_t launch_step(const AttendArgs &a, const Parts &parts, int max_queries, hipStream_t stream);
+hipError_t launch_step(const AttendArgs &a, const Shares &shares, int max_queries, hipStream_t stream);
 hipError_t launch_tail(const AttendArgs &a, const Parts &parts, int max_queries, hipStream_t stream);
-// Joins the parts of rows in sequences of min_rows to max_rows rows per KV head, cut in tiles of tile_rows.
-hipError_t launch_join(const AttendArgs &a, const Parts &parts, int max_queries, int min_rows, int max_rows,
-                       int tile_rows, hipStream_t stream);
+// Join what these left of rows in parts.
+hipError_t launch_join_step(const AttendArgs &a, const Shares &shares, int max_queries, hipStream_t stream);
+hipError_t launch_join_tail(const AttendArgs &a, const Parts &parts, int max_queries, hipStream_t stream);
 // weights_out, from the scores that the step kernel left, or with the scores taken again.
 hipError_t launch_weigh_step(const AttendArgs &a, hipStream_t stream);
 hipError_t launch_weigh(const AttendArgs &a, hipStream_t stream);

@@ -12,7 +12,7 @@
 //    permutations in registers turn them (one per pair of elements); e4m3 is turned while it is widened.
 //  * The pages of 32 tokens are looked up by 32 lanes, one token each, a round ahead, and handed out by lane shuffles.
 //
-// A sequence's tokens are split over workgroups (split_len each) until the chip is full, and inside a workgroup over its
+// The sequences' tokens are shared out to workgroups (Shares) so that they fill the chip once, and inside a workgroup over its
 // 4 waves; the waves' sums are joined through LDS, the workgroups' by join_kernel.  K of the next 32 tokens is requested
 // as soon as the scores have used the last, V as soon as the second product has: a wave has 16 KiB in flight (bf16,
 // D 128) without a second set of registers.
@@ -56,7 +56,7 @@ struct Vec<16> {
 
 // T: type of q, of the weights and of out; FP8: the cache holds e4m3; DP >= D columns; NT: tiles of 16 rows.
 template <class T, bool FP8, int DP, int NT>
-__global__ __launch_bounds__(64 * kWaves) void step_kernel(const AttendArgs a, const Parts parts_to) {
+__global__ __launch_bounds__(64 * kWaves, !FP8 && DP > 128 ? 1 : 2) void step_kernel(const AttendArgs a, const Shares shares) {
     constexpr int E = FP8 ? 1 : 2;                       // bytes of a cached element
     constexpr int KC = DP * E / 64;                      // 16-byte pieces of a token's K in a lane
     constexpr int VE = DP / 16 * E > 16 ? 16 / E : DP / 16;  // V columns of a lane in a piece
@@ -65,24 +65,27 @@ __global__ __launch_bounds__(64 * kWaves) void step_kernel(const AttendArgs a, c
     const Pages &pg = a.pages;
     const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int split = blockIdx.x, tile = blockIdx.y / pg.H, h = blockIdx.y - tile * pg.H, b = blockIdx.z;
+    const int tile = blockIdx.y / pg.H, h = blockIdx.y - tile * pg.H;
+    Share share;
+    if (!share_of(a, shares, blockIdx.x, false, share))
+        return;
+    const int b = share.b;
     Sequence seq;
     if (!sequence(a.batch, b, pg.err, seq))
         return;
     const int rows = seq.nq * a.group, row0 = tile * 16 * NT;
-    if (row0 >= rows || rows > kStepRows)
+    if (row0 >= rows)
         return;
     const int i0 = divide(row0, a.by_group), i1 = divide(min(row0 + 16 * NT, rows) - 1, a.by_group) + 1;
     const Span span = span_of(seq.n, seq.nq, i0, i1, a.window);
-    const int begin = span.start + split * parts_to.len;
-    if (split > 0 && begin >= span.end)
-        return;
-    const int stop = min(span.end, begin + parts_to.len);
-    const bool whole = span.end - span.start <= parts_to.len;  // no other part
+    const int64_t part_at = span_of(seq.n, seq.nq, 0, seq.nq, a.window).start + static_cast<int64_t>(share.split) * share.len;
+    const int begin = static_cast<int>(min(part_at, int64_t{INT32_MAX} - 1023));
+    const int stop = static_cast<int>(min(part_at + share.len, static_cast<int64_t>(span.end)));
+    const bool whole = share.parts == 1;
     const int p_first = seq.n - seq.nq + i0;
     const int low_last = a.window > 0 ? span.end - a.window : 0;  // from here on every row's window is open
 
-    const int64_t slot0 = (static_cast<int64_t>(b) * pg.H + h) * parts_to.row_cap + row0;
+    const int64_t slot0 = (static_cast<int64_t>(h) * shares.items + blockIdx.x) * shares.row_cap + row0;
     const int64_t score0 = (static_cast<int64_t>(b) * pg.H + h) * a.score_cap + row0;
 
     // Queries: a row's elements in the order in which K's pieces hold them.
@@ -369,7 +372,7 @@ __global__ __launch_bounds__(64 * kWaves) void step_kernel(const AttendArgs a, c
         if (r >= rows)
             continue;
         const int i = divide(r, a.by_group), head = h * a.group + r - i * a.group, row = seq.q0 + i;
-        const int64_t slot = (slot0 + nt * 16 + c) * parts_to.splits + split;
+        const int64_t slot = slot0 + nt * 16 + c;
         const float inv = total[nt] == 0.f ? 0.f : a.v_scale / total[nt];
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
@@ -392,7 +395,7 @@ __global__ __launch_bounds__(64 * kWaves) void step_kernel(const AttendArgs a, c
                     *reinterpret_cast<u32x2 *>(to + 2 * j) = u32x2{T::pack(x[j] * inv, x[j + 1] * inv),
                                                                     T::pack(x[j + 2] * inv, x[j + 3] * inv)};
             } else {
-                float *to = parts_to.sums + slot * pg.D + d;
+                float *to = shares.sums + slot * pg.D + d;
 #pragma unroll
                 for (int j = 0; j < VE; j += 4)
                     *reinterpret_cast<f32x4 *>(to + j) = f32x4{x[j], x[j + 1], x[j + 2], x[j + 3]};
@@ -403,59 +406,76 @@ __global__ __launch_bounds__(64 * kWaves) void step_kernel(const AttendArgs a, c
                 a.lse[static_cast<int64_t>(row) * a.heads + head] =
                     total[nt] == 0.f ? -INFINITY : (most[nt] - T::kShift + __builtin_amdgcn_logf(total[nt])) * kLn2;
             } else {
-                parts_to.stats[slot * 2] = most[nt] - T::kShift;
-                parts_to.stats[slot * 2 + 1] = total[nt];
+                shares.stats[slot * 2] = most[nt] - T::kShift;
+                shares.stats[slot * 2 + 1] = total[nt];
             }
         }
     }
 }
 
+// Where the parts of a row lie.
+struct Row {
+    int64_t slot, stride;  // of its first part, and between parts
+    int parts;
+};
+
+// Row i of head h's sequence b, or no parts.
+__device__ __forceinline__ Row parts_at(const AttendArgs &a, const Shares &from, int b, int h, int r, const Sequence &) {
+    Share share;
+    if (!share_of(a, from, b, true, share))
+        return Row{0, 0, 0};
+    return Row{(static_cast<int64_t>(h) * from.items + share.item0) * from.row_cap + r, from.row_cap, share.parts};
+}
+__device__ __forceinline__ Row parts_at(const AttendArgs &a, const Parts &from, int b, int h, int r, const Sequence &seq) {
+    const int rows = seq.nq * a.group, row0 = r - r % kTailRows;
+    if (rows <= kStepRows)
+        return Row{0, 0, 0};
+    const Span span = span_of(seq.n, seq.nq, divide(row0, a.by_group),
+                              divide(min(row0 + kTailRows, rows) - 1, a.by_group) + 1, a.window);
+    return Row{((static_cast<int64_t>(b) * a.pages.H + h) * from.row_cap + r) * from.splits, 1, parts_of(span, from.len)};
+}
+
 // The parts of a row joined: sum_s 2^(m_s - m) x_s / sum_s 2^(m_s - m) l_s.  4 columns per lane; a workgroup takes one
 // row and spreads its parts over its lanes' groups (SPREAD: many parts, few rows), or a row per group of lanes.
-template <bool SPREAD>
-__global__ __launch_bounds__(256) void join_kernel(const AttendArgs a, const Parts from, const int min_rows, const int max_rows,
-                                                    const int tile_rows) {
+template <bool SPREAD, class From>
+__global__ __launch_bounds__(256) void join_kernel(const AttendArgs a, const From from) {
     __shared__ f32x4 sums[SPREAD ? 256 : 1];
     const int b = blockIdx.z, head = blockIdx.y, h = divide(head, a.by_group), D = a.pages.D, tid = threadIdx.x;
     const int lanes = D / 4, groups = 256 / lanes, mine = tid / lanes, d = (tid - mine * lanes) * 4;
     const int i = SPREAD ? blockIdx.x : blockIdx.x * groups + mine;
     Sequence seq;
-    if (!sequence(a.batch, b, a.pages.err, seq) || seq.nq * a.group < min_rows || seq.nq * a.group > max_rows)
+    if (!sequence(a.batch, b, a.pages.err, seq))
         return;
+    // (All lanes look the parts up together; the lanes of a row that is none then leave.)
+    const Row row_at = parts_at(a, from, b, h, min(i, max(seq.nq - 1, 0)) * a.group + head - h * a.group, seq);
+    const int parts = row_at.parts;
     const bool row = i < seq.nq && mine < groups;
-    if (SPREAD ? i >= seq.nq : !row)
+    if (parts <= 1 || (SPREAD ? i >= seq.nq : !row))
         return;
-    // The parts are those of the row's tile.
-    const int r = i * a.group + head - h * a.group, rows = seq.nq * a.group, row0 = r - r % tile_rows;
-    const Span span = span_of(seq.n, seq.nq, divide(row0, a.by_group),
-                              divide(min(row0 + tile_rows, rows) - 1, a.by_group) + 1, a.window);
-    const int parts = parts_of(span, from.len);
-    if (parts == 1)
-        return;
-    const int64_t slot = ((static_cast<int64_t>(b) * a.pages.H + h) * from.row_cap + r) * from.splits;
-    const float *stats = from.stats + slot * 2;
+    const float *stats = from.stats + row_at.slot * 2;
+    const int64_t step = row_at.stride;
     float most = kLowest, total = 0.f;
     if constexpr (SPREAD) {  // every wave for itself
         const int lane = tid & 63;
         for (int s = lane; s < parts; s += 64)
-            most = fmaxf(most, stats[2 * s]);
+            most = fmaxf(most, stats[2 * s * step]);
         for (int o = 32; o; o >>= 1)
             most = fmaxf(most, __shfl_xor(most, o));
         for (int s = lane; s < parts; s += 64)
-            total += stats[2 * s + 1] * __builtin_amdgcn_exp2f(stats[2 * s] - most);
+            total += stats[2 * s * step + 1] * __builtin_amdgcn_exp2f(stats[2 * s * step] - most);
         for (int o = 32; o; o >>= 1)
             total += __shfl_xor(total, o);
     } else {
         for (int s = 0; s < parts; ++s)
-            most = fmaxf(most, stats[2 * s]);
+            most = fmaxf(most, stats[2 * s * step]);
         for (int s = 0; s < parts; ++s)
-            total += stats[2 * s + 1] * __builtin_amdgcn_exp2f(stats[2 * s] - most);
+            total += stats[2 * s * step + 1] * __builtin_amdgcn_exp2f(stats[2 * s * step] - most);
     }
     f32x4 x{0.f, 0.f, 0.f, 0.f};
     if (row)
         for (int s = SPREAD ? mine : 0; s < parts; s += SPREAD ? groups : 1)
-            x += *reinterpret_cast<const f32x4 *>(from.sums + (slot + s) * D + d) *
-                 __builtin_amdgcn_exp2f(stats[2 * s] - most);
+            x += *reinterpret_cast<const f32x4 *>(from.sums + (row_at.slot + s * step) * D + d) *
+                 __builtin_amdgcn_exp2f(stats[2 * s * step] - most);
     if constexpr (SPREAD) {
         sums[tid] = x;
         __syncthreads();
@@ -500,46 +520,56 @@ __global__ __launch_bounds__(256) void weigh_step_kernel(const AttendArgs a) {
 }
 
 template <class T, bool FP8, int DP, int NT>
-void launch(const AttendArgs &a, const Parts &parts, int max_rows, hipStream_t stream) {
+void launch(const AttendArgs &a, const Shares &shares, int max_rows, hipStream_t stream) {
     const int tiles = (max_rows + 16 * NT - 1) / (16 * NT);
-    hipLaunchKernelGGL((step_kernel<T, FP8, DP, NT>), dim3(parts.splits, tiles * a.pages.H, a.num_seqs),
-                       dim3(64 * kWaves), 0, stream, a, parts);
+    hipLaunchKernelGGL((step_kernel<T, FP8, DP, NT>), dim3(shares.items, tiles * a.pages.H),
+                       dim3(64 * kWaves), 0, stream, a, shares);
 }
 
 template <class T, bool FP8>
-void launch(const AttendArgs &a, const Parts &parts, int max_rows, hipStream_t stream) {
+void launch(const AttendArgs &a, const Shares &shares, int max_rows, hipStream_t stream) {
     const bool two = step_tile_rows(max_rows, a.pages.D) == 32;
     if (a.pages.D > 128)
-        launch<T, FP8, 256, 1>(a, parts, max_rows, stream);
+        launch<T, FP8, 256, 1>(a, shares, max_rows, stream);
     else if (a.pages.D > 64)
-        two ? launch<T, FP8, 128, 2>(a, parts, max_rows, stream) : launch<T, FP8, 128, 1>(a, parts, max_rows, stream);
+        two ? launch<T, FP8, 128, 2>(a, shares, max_rows, stream) : launch<T, FP8, 128, 1>(a, shares, max_rows, stream);
     else
-        two ? launch<T, FP8, 64, 2>(a, parts, max_rows, stream) : launch<T, FP8, 64, 1>(a, parts, max_rows, stream);
+        two ? launch<T, FP8, 64, 2>(a, shares, max_rows, stream) : launch<T, FP8, 64, 1>(a, shares, max_rows, stream);
 }
 
 }  // namespace
 
-hipError_t launch_step(const AttendArgs &a, const Parts &parts, int max_queries, hipStream_t stream) {
+hipError_t launch_step(const AttendArgs &a, const Shares &shares, int max_queries, hipStream_t stream) {
     const int max_rows = static_cast<int>(std::min<int64_t>(kStepRows, static_cast<int64_t>(max_queries) * a.group));
     const bool fp8 = a.cache_type == KV_DTYPE_E4M3;
     if (a.q_type == KV_DTYPE_BF16)
-        fp8 ? launch<Bf16, true>(a, parts, max_rows, stream) : launch<Bf16, false>(a, parts, max_rows, stream);
+        fp8 ? launch<Bf16, true>(a, shares, max_rows, stream) : launch<Bf16, false>(a, shares, max_rows, stream);
     else
-        fp8 ? launch<F16, true>(a, parts, max_rows, stream) : launch<F16, false>(a, parts, max_rows, stream);
+        fp8 ? launch<F16, true>(a, shares, max_rows, stream) : launch<F16, false>(a, shares, max_rows, stream);
     return hipGetLastError();
 }
 
-hipError_t launch_join(const AttendArgs &a, const Parts &parts, int max_queries, int min_rows, int max_rows,
-                       int tile_rows, hipStream_t stream) {
-    const int groups = 256 / (a.pages.D / 4);
-    const bool spread = parts.splits > 8;  // (8 parts one after the other take about as long as one row's launch)
-    const dim3 grid(static_cast<uint32_t>(spread ? max_queries : (max_queries + groups - 1) / groups),
-                    static_cast<uint32_t>(a.heads), static_cast<uint32_t>(a.num_seqs));
-    if (spread)
-        hipLaunchKernelGGL(join_kernel<true>, grid, dim3(256), 0, stream, a, parts, min_rows, max_rows, tile_rows);
-    else
-        hipLaunchKernelGGL(join_kernel<false>, grid, dim3(256), 0, stream, a, parts, min_rows, max_rows, tile_rows);
+namespace {
+
+template <bool SPREAD, class From>
+hipError_t launch_join(const AttendArgs &a, const From &from, int max_queries, hipStream_t stream) {
+    const int groups = SPREAD ? 1 : 256 / (a.pages.D / 4);
+    const dim3 grid(static_cast<uint32_t>((max_queries + groups - 1) / groups), static_cast<uint32_t>(a.heads),
+                    static_cast<uint32_t>(a.num_seqs));
+    hipLaunchKernelGGL((join_kernel<SPREAD, From>), grid, dim3(256), 0, stream, a, from);
     return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_join_step(const AttendArgs &a, const Shares &shares, int max_queries, hipStream_t stream) {
+    return launch_join<true>(a, shares, std::min(max_queries, kStepRows), stream);
+}
+
+hipError_t launch_join_tail(const AttendArgs &a, const Parts &parts, int max_queries, hipStream_t stream) {
+    // (8 parts one after the other take about as long as one row's launch.)
+    return parts.splits > 8 ? launch_join<true>(a, parts, max_queries, stream)
+                            : launch_join<false>(a, parts, max_queries, stream);
 }
 
 hipError_t launch_weigh_step(const AttendArgs &a, hipStream_t stream) {

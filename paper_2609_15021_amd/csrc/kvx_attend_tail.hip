@@ -295,7 +295,10 @@ __global__ __launch_bounds__(64 * kRows / RW, 2) void tail_kernel(const AttendAr
             }
             // (Addresses are worked out where they are used: kept, they would cost registers.)
             asm volatile("" : "+v"(k_at), "+v"(v_at));
+            // (The products go first: the other wave of the SIMD has its exponentials for the time between them.)
+            __builtin_amdgcn_s_setprio(1);
             take_scores(buffer);
+            __builtin_amdgcn_s_setprio(0);
             const bool edge = usable != ~uint64_t{0} || p_first - base < TK - 1 || base < low_last;
             // Scores in powers of 2; in the plain case the factor is left to the exponent's argument.
             const float factor = PLAIN ? scale : 1.f;
@@ -363,6 +366,7 @@ __global__ __launch_bounds__(64 * kRows / RW, 2) void tail_kernel(const AttendAr
                     p[t][x >> 3][x >> 1 & 3] = T::pack(e0, e1);
                 }
             l += (sums[0] + sums[1]) + (sums[2] + sums[3]);
+            __builtin_amdgcn_s_setprio(1);
             lds_byte *v_lds = (lds_byte *)(lds[1][buffer]);  // (a cast between address spaces)
 #pragma unroll
             for (int t = 0; t < TB; ++t)
@@ -375,6 +379,7 @@ __global__ __launch_bounds__(64 * kRows / RW, 2) void tail_kernel(const AttendAr
                         acc[d] = product(u32x4{x[0], x[1], y[0], y[1]}, p[t][j], acc[d], T{});
                     }
             interleave<TB * SETS * DB, 2, 3, 0>();
+            __builtin_amdgcn_s_setprio(0);
             if (!more)
                 break;
             deposit(0, buffer ^ 1);
