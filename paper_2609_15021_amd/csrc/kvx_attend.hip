@@ -69,24 +69,25 @@ struct Plan {
 
 int64_t round_up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 
-// The tail kernel's parts.  512 of its workgroups run at once (2 per CU; 256 where D > 128), so `have` of them may leave
-// the last round nearly empty, and fewer leave CUs idle: the number of parts is the one whose rounds and joining take
-// least, at the 0.2 ns per token and column that such a round takes and the 5 TB/s at which parts are written and read
-// again.  Parts have no fewer than 256 tokens and no more than 256 MB between them.
-Parts tail_parts_for(int64_t longest, int64_t have, int64_t rows, int64_t head_dim) {
-    longest = std::max<int64_t>(longest, 1);
+// The tail kernel's parts, for `have` tiles of rows.  512 of its workgroups run at once (2 per CU; 256 where D > 128), so
+// they may leave the last round nearly empty, and tiles that see less than others end it early: the number of parts is the
+// one whose rounds (between those of equal parts, and those without an edge and half a part idle at the end) and joining
+// take least, at the 0.2 ns per token and column that such a round takes and the 5 TB/s at which parts are written and
+// read again.  Parts have no fewer than 256 tokens and no more than 256 MB between them.
+Parts tail_parts_for(int64_t longest, int64_t have, int64_t head_dim) {
     const int64_t at_once = head_dim > 128 ? 256 : 512;
     const double tokens_us = 0.2e-3 * static_cast<double>(head_dim) * static_cast<double>(longest);
     const double parts_bytes = static_cast<double>(have) * kTailRows * static_cast<double>(head_dim) * 4;
     int64_t best = 1;
     double best_us = 0.;
     for (int64_t splits = 1; splits <= 64; ++splits) {
-        if (splits > 1 && (longest < 256 * splits || parts_bytes * static_cast<double>(splits) > 256e6))
+        const double n = static_cast<double>(splits);
+        if (splits > 1 && (longest < 256 * splits || parts_bytes * n > 256e6))
             break;
-        const double us =
-            static_cast<double>((have * splits + at_once - 1) / at_once) * tokens_us / static_cast<double>(splits) +
-            (splits > 1 ? 5. + static_cast<double>(splits) * parts_bytes * 2 / 5e6 : 0.);
-        if (splits == 1 || us < 0.95 * best_us) {
+        const double rounds = 0.5 * (static_cast<double>((have * splits + at_once - 1) / at_once) +
+                                     static_cast<double>(have * splits) / static_cast<double>(at_once) + 0.5);
+        const double us = rounds / n * tokens_us + (splits > 1 ? 5. + n * parts_bytes * 2 / 5e6 : 0.);
+        if (splits == 1 || us < 0.97 * best_us) {
             best = splits;
             best_us = us;
         }
@@ -94,7 +95,6 @@ Parts tail_parts_for(int64_t longest, int64_t have, int64_t rows, int64_t head_d
     Parts p{};
     p.len = static_cast<int32_t>(round_up((longest + best - 1) / best, 64));
     p.splits = static_cast<int32_t>((longest + p.len - 1) / p.len);
-    p.row_cap = static_cast<int32_t>(rows);
     return p;
 }
 
@@ -125,9 +125,11 @@ Plan plan_of(const kv_cache *cache, const kv_batch *batch, const kv_attend_optio
     p.shares.row_cap = p.max_rows;
     p.parts = batch->num_seqs <= kShareSeqs && p.shares.target > 1;
     if (p.tail) {
-        const int64_t longest_tail =
-            std::min<int64_t>(batch->max_len, o->window > 0 ? o->window + int64_t{kTailRows} + 31 : batch->max_len);
-        p.tail_parts = tail_parts_for(longest_tail, heads * ((all_rows + kTailRows - 1) / kTailRows), all_rows, D);
+        const int64_t seen = o->window > 0 ? o->window + int64_t{kTailRows} + 31 : batch->max_len;
+        const int64_t tiles_each = (all_rows + kTailRows - 1) / kTailRows;
+        const int64_t tiles_all = (batch->num_queries * group + kTailRows - 1) / kTailRows + batch->num_seqs;
+        p.tail_parts = tail_parts_for(std::max<int64_t>(std::min<int64_t>(seen, batch->max_len), 1),
+                                      H * std::min(batch->num_seqs * tiles_each, tiles_all), D);
     }
     int64_t at = round_up(static_cast<int64_t>(batch->num_queries) * q->heads * 4, 16);
     const auto take = [&](int64_t bytes) {
@@ -135,12 +137,13 @@ Plan plan_of(const kv_cache *cache, const kv_batch *batch, const kv_attend_optio
         at += round_up(bytes, 16);
         return here;
     };
-    const auto slots = [&](const Parts &x) { return x.splits > 1 ? heads * x.row_cap * x.splits : 0; };
     const int64_t shared = p.parts ? H * p.shares.items * p.shares.row_cap : 0;
     p.step_stats = take(shared * 8);
     p.step_sums = take(shared * D * 4);
-    p.tail_stats = take(slots(p.tail_parts) * 8);
-    p.tail_sums = take(slots(p.tail_parts) * D * 4);
+    const int64_t split =
+        p.tail_parts.splits > 1 ? static_cast<int64_t>(batch->num_queries) * q->heads * p.tail_parts.splits : 0;
+    p.tail_stats = take(split * 8);
+    p.tail_sums = take(split * D * 4);
     p.score_len = round_up(batch->max_len, 32);
     p.scores_at = take(p.scores ? heads * all_rows * p.score_len * 4 : 0);
     p.bytes = at;

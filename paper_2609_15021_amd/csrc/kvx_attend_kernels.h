@@ -28,12 +28,11 @@ struct AttendArgs {
     int32_t score_cap;
 };
 
-// How a kernel splits a sequence's tokens over workgroups, and what the parts of a row leave for the join.
+// How the tail kernel splits the tokens of a tile of rows over workgroups, and what the parts of a row leave for the join.
 struct Parts {
     int32_t len, splits;  // tokens of a part; most parts of a row
-    int32_t row_cap;      // most rows per KV head of a sequence
-    float *sums;          // [sequence][KV head][row_cap][splits][D], unscaled
-    float *stats;         // [sequence][KV head][row_cap][splits][2]: largest score and sum, in powers of 2
+    float *sums;          // [row][query head][splits][D], unscaled
+    float *stats;         // [row][query head][splits][2]: largest score and sum, in powers of 2
 };
 
 // Tokens that the new tokens [i0, i1) of a sequence see between them: [first, end); parts start at `start`.

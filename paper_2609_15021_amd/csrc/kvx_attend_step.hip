@@ -426,13 +426,14 @@ __device__ __forceinline__ Row parts_at(const AttendArgs &a, const Shares &from,
         return Row{0, 0, 0};
     return Row{(static_cast<int64_t>(h) * from.items + share.item0) * from.row_cap + r, from.row_cap, share.parts};
 }
-__device__ __forceinline__ Row parts_at(const AttendArgs &a, const Parts &from, int b, int h, int r, const Sequence &seq) {
+__device__ __forceinline__ Row parts_at(const AttendArgs &a, const Parts &from, int, int h, int r, const Sequence &seq) {
     const int rows = seq.nq * a.group, row0 = r - r % kTailRows;
     if (rows <= kStepRows)
         return Row{0, 0, 0};
     const Span span = span_of(seq.n, seq.nq, divide(row0, a.by_group),
                               divide(min(row0 + kTailRows, rows) - 1, a.by_group) + 1, a.window);
-    return Row{((static_cast<int64_t>(b) * a.pages.H + h) * from.row_cap + r) * from.splits, 1, parts_of(span, from.len)};
+    const int i = divide(r, a.by_group), head = h * a.group + r - i * a.group;
+    return Row{(static_cast<int64_t>(seq.q0 + i) * a.heads + head) * from.splits, 1, parts_of(span, from.len)};
 }
 
 // The parts of a row joined: sum_s 2^(m_s - m) x_s / sum_s 2^(m_s - m) l_s.  4 columns per lane; a workgroup takes one

@@ -394,7 +394,7 @@ __global__ __launch_bounds__(64 * kRows / RW, 2) void tail_kernel(const AttendAr
     if (!row_ok)
         return;
     const float inv = l == 0.f ? 0.f : a.v_scale / l;
-    const int64_t slot = ((static_cast<int64_t>(b) * pg.H + h) * parts.row_cap + r) * parts.splits + split;
+    const int64_t slot = (static_cast<int64_t>(seq.q0 + row_i) * a.heads + head) * parts.splits + split;
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
