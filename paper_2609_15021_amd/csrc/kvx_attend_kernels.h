@@ -171,6 +171,8 @@ struct Bf16 {
         p[1] = static_cast<__bf16>(b);
         return __builtin_bit_cast(uint32_t, p);
     }
+    static __device__ __forceinline__ float low(uint32_t x) { return __builtin_bit_cast(float, x << 16); }
+    static __device__ __forceinline__ float high(uint32_t x) { return __builtin_bit_cast(float, x & 0xffff0000u); }
 };
 
 struct F16 {
@@ -187,6 +189,8 @@ struct F16 {
         p[1] = static_cast<_Float16>(b);
         return __builtin_bit_cast(uint32_t, p);
     }
+    static __device__ __forceinline__ float low(uint32_t x) { return static_cast<float>(__builtin_bit_cast(pair, x)[0]); }
+    static __device__ __forceinline__ float high(uint32_t x) { return static_cast<float>(__builtin_bit_cast(pair, x)[1]); }
 };
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));

@@ -229,7 +229,7 @@ __global__ __launch_bounds__(64 * kWaves, !FP8 && DP > 128 ? 1 : 2) void step_ke
             }
 
             // Weights.  Everything from here on is in powers of 2.
-            u32x4 p[NT];
+            u32x4 p[NT], p_rest[NT];
             const uint32_t bits = usable >> (g * 8);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
@@ -280,7 +280,14 @@ __global__ __launch_bounds__(64 * kWaves, !FP8 && DP > 128 ? 1 : 2) void step_ke
                 for (int e = 0; e < 8; ++e)
                     x[e] = __builtin_amdgcn_exp2f(x[e] - zero);
                 l[nt] += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
-                p[nt] = u32x4{T::pack(x[0], x[1]), T::pack(x[2], x[3]), T::pack(x[4], x[5]), T::pack(x[6], x[7])};
+                // A weight is two numbers of the rows' type, so that its rounding does not add to the output's: the
+                // products wait for memory anyway.
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) {
+                    const uint32_t w = T::pack(x[e], x[e + 1]);
+                    p[nt][e / 2] = w;
+                    p_rest[nt][e / 2] = T::pack(x[e] - T::low(w), x[e + 1] - T::high(w));
+                }
             }
 
             // A slot without a token may hold anything, and 0 times it need not be 0.
@@ -322,6 +329,7 @@ __global__ __launch_bounds__(64 * kWaves, !FP8 && DP > 128 ? 1 : 2) void step_ke
                         for (int nt = 0; nt < NT; ++nt) {
                             f32x4 &x = acc[nt][v * VE + w * kEach + j];
                             x = mfma_16x16x32(turned[j], p[nt], x, T{});
+                            x = mfma_16x16x32(turned[j], p_rest[nt], x, T{});
                         }
                 }
             if (!more)
@@ -497,27 +505,48 @@ __global__ __launch_bounds__(256) void join_kernel(const AttendArgs a, const Fro
             total == 0.f ? -INFINITY : (most + __builtin_amdgcn_logf(total)) * kLn2;
 }
 
-// What each token received from the rows of a sequence, from the scores that the step kernel left.
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));  // weights' rows start anywhere
+
+// What each token received from the rows of a sequence, from the scores that the step kernel left; 4 tokens a lane.
 __global__ __launch_bounds__(256) void weigh_step_kernel(const AttendArgs a) {
-    const int b = blockIdx.z, h = blockIdx.y, t = blockIdx.x * 256 + threadIdx.x;
+    const int b = blockIdx.z, h = blockIdx.y, t = (blockIdx.x * 256 + threadIdx.x) * 4;
     Sequence seq;
     if (!sequence(a.batch, b, a.pages.err, seq) || t >= seq.n)
         return;
-    float sum = 0.f;
-    for (int i = 0; i < seq.nq; ++i) {
-        const int p = seq.n - seq.nq + i;
-        if (t > p || (a.window > 0 && p - t >= a.window))
-            continue;
-        const int64_t at = static_cast<int64_t>(seq.q0 + i) * a.heads + h * a.group;
-        const int64_t slot = (static_cast<int64_t>(b) * a.pages.H + h) * a.score_cap + i * a.group;
-        for (int k = 0; k < a.group; ++k) {
-            const float lse = a.lse[at + k];
-            if (lse != -INFINITY)
-                sum += __builtin_amdgcn_exp2f(a.scores[(slot + k) * a.score_len + t] - lse * kLog2e);
+    const int64_t at = b * a.weights_seq_stride + h * a.weights_head_stride + t;
+    const bool all = seq.n - t >= 4;
+    f32x4 sum{0.f, 0.f, 0.f, 0.f};
+    if (a.weights_in) {
+        if (all) {
+            sum = *reinterpret_cast<const f32x4_any *>(a.weights_in + at);
+        } else {
+            for (int j = 0; j < seq.n - t; ++j)
+                sum[j] = a.weights_in[at + j];
         }
     }
-    const int64_t at = b * a.weights_seq_stride + h * a.weights_head_stride + t;
-    a.weights_out[at] = (a.weights_in ? a.weights_in[at] : 0.f) + sum;
+    f32x4 got{0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < seq.nq; ++i) {
+        // Of these tokens the row sees [from, to); others' scores may not be there.
+        const int p = seq.n - seq.nq + i, to = p - t + 1, from = a.window > 0 ? to - a.window : INT32_MIN;
+        if (to <= 0 || from >= 4)
+            continue;
+        const float *lse = a.lse + static_cast<int64_t>(seq.q0 + i) * a.heads + h * a.group;
+        const float *scores = a.scores + ((static_cast<int64_t>(b) * a.pages.H + h) * a.score_cap + i * a.group) * a.score_len + t;
+        for (int k = 0; k < a.group; ++k) {
+            const float zero = lse[k] * kLog2e;
+            const f32x4 x = *reinterpret_cast<const f32x4 *>(scores + k * a.score_len);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                got[j] += j < to && j >= from && lse[k] != -INFINITY ? __builtin_amdgcn_exp2f(x[j] - zero) : 0.f;
+        }
+    }
+    sum += got;
+    if (all) {
+        *reinterpret_cast<f32x4_any *>(a.weights_out + at) = sum;
+    } else {
+        for (int j = 0; j < seq.n - t; ++j)
+            a.weights_out[at + j] = sum[j];
+    }
 }
 
 template <class T, bool FP8, int DP, int NT>
@@ -574,7 +603,7 @@ hipError_t launch_join_tail(const AttendArgs &a, const Parts &parts, int max_que
 }
 
 hipError_t launch_weigh_step(const AttendArgs &a, hipStream_t stream) {
-    const dim3 grid(static_cast<uint32_t>((a.batch.max_len + 255) / 256), static_cast<uint32_t>(a.pages.H),
+    const dim3 grid(static_cast<uint32_t>((a.batch.max_len + 1023) / 1024), static_cast<uint32_t>(a.pages.H),
                     static_cast<uint32_t>(a.num_seqs));
     hipLaunchKernelGGL(weigh_step_kernel, grid, dim3(256), 0, stream, a);
     return hipGetLastError();
