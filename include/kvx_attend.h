@@ -15,7 +15,8 @@
  * allocates nothing, never blocks the host, keeps nothing between calls and may be captured into a graph.  All reads
  * and writes of a call follow earlier work on `stream` and precede later work there; calls on different streams are
  * ordered by the caller where they share a written buffer (a cache, an output or a workspace).  DEVICE arrays are read
- * and written until the call's work has completed there.  Results do not depend on the order in which workgroups run.
+ * and written until the call's work has completed there.  Outputs overlap neither inputs nor the workspace, unless said.
+ * Results do not depend on the order in which workgroups run: the same call gives the same bits.
  *
  * ---------------------------------------------------------------------------
  * A batch of sequences.  Sequence b has lens[b] tokens, its new ones among them: token t lies in block
@@ -106,12 +107,17 @@ KV_API kv_status kv_append(const kv_cache *cache, int32_t layer, const kv_batch 
 /*
  * kv_attend -- out[row] = v_scale * sum over its tokens of softmax(s) * v, rounded once to q's type, and lse[row] = log
  * of the sum of exp(s), for every new row; query head h reads KV head h / (q->heads / H).  A row that sees no token
- * gets 0 and -infinity.
+ * gets 0 and -infinity.  Sums, largest scores and lse are held in 32 bits; the weights exp(s) meet V as two numbers of q's
+ * type for sequences of up to 64 rows (new tokens times query heads) per KV head, and as one, rounded to nearest, for
+ * longer ones (off by up to half a step of that type each).  What slots behind a sequence's last token hold does not
+ * matter, but its own tokens' V are taken to be finite: 0 times an infinity of a token that a row does not see reaches
+ * that row.
  *   q, out:    [num_queries][query heads][D], same type; the cache's, or either 2-byte type for E4M3;
  *   lse:       DEVICE float[num_queries][query heads], or NULL;
  *   workspace: DEVICE, kv_attend_workspace's bytes (16-byte aligned; may be NULL for 0 bytes), the call's own until its
  *              work has completed: calls that may overlap, and graphs whose replays may, need one each.
- * Errors as kv_append; KV_EINVAL for a workspace that is too small.
+ * Errors as kv_append; KV_EINVAL for a workspace that is too small; KV_EUNSUPPORTED also for more than 16,383 query heads,
+ * scales whose product (or its quotient by softcap) leaves 1e-36 .. 1e36, and bounds of more rows than one launch takes.
  */
 KV_API kv_status kv_attend(const kv_cache *cache, int32_t layer, const kv_batch *batch, const kv_attend_options *options,
                            const kv_rows *q, const kv_rows *out, float *lse, void *workspace, int64_t workspace_bytes,

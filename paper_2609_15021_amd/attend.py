@@ -71,20 +71,40 @@ _declare(_lib)
 # what only the numbers decide is remembered by them.
 
 
-def _ints(t, name: str, dims: int, rows=None):
-    """A device tensor of int32 whose last dimension is dense."""
-    if not isinstance(t, torch.Tensor) or t.dtype is not torch.int32 or not t.is_cuda or t.dim() != dims or \
+def _ints(t, name: str, dims: int, device: int, rows=None):
+    """A tensor of int32 on the call's device whose last dimension is dense."""
+    if not isinstance(t, torch.Tensor) or t.dtype is not torch.int32 or t.dim() != dims or \
             (t.stride(-1) != 1 and t.numel()):
         raise TypeError(f"{name} must be a {dims}-dimensional int32 device tensor with a dense last dimension")
+    _on(t, name, device)
     if rows is not None and t.shape[0] != rows:
         raise ValueError(f"{name} has {t.shape[0]} rows; {rows} are needed")
     return t
 
 
-def _rows(t, name: str, head_dim: int) -> KvRows:
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dim() != 3 or \
-            t.dtype not in (torch.bfloat16, torch.float16):
+def _on(t, name: str, device: int) -> None:
+    if t.get_device() != device:  # -1 for a host tensor
+        raise TypeError(f"{name} must be a device tensor on device {device}, where the call works (it is on {t.device})")
+
+
+def _floats(t, name: str, device: int, shape) -> None:
+    if not isinstance(t, torch.Tensor) or t.dtype is not torch.float32 or t.shape != shape or not t.is_contiguous():
+        raise TypeError(f"{name} must be a contiguous float32 device tensor of {tuple(shape)}")
+    _on(t, name, device)
+
+
+def _weights(t, name: str, device: int, rows=None) -> None:
+    if not isinstance(t, torch.Tensor) or t.dtype is not torch.float32 or t.dim() != 3 or \
+            (t.stride(2) != 1 and t.numel()) or (rows is not None and t.shape[:2] != rows):
+        raise TypeError(f"{name} must be a [sequences][heads][tokens] float32 device tensor with dense rows"
+                        f"{'' if rows is None else f' ({rows} of them)'}")
+    _on(t, name, device)
+
+
+def _rows(t, name: str, head_dim: int, device: int) -> KvRows:
+    if not isinstance(t, torch.Tensor) or t.dim() != 3 or t.dtype not in (torch.bfloat16, torch.float16):
         raise TypeError(f"{name} must be a [tokens][heads][D] device tensor of bfloat16 or float16")
+    _on(t, name, device)
     _, heads, width = t.shape
     token, head, column = t.stride()
     if width != head_dim or (column != 1 and t.numel()):
@@ -93,15 +113,16 @@ def _rows(t, name: str, head_dim: int) -> KvRows:
 
 
 def _batch(cache: Cache, tables, lens, starts, tokens: int, max_q, max_len) -> KvBatch:
-    B, pages = _ints(tables, "tables", 2).shape
-    _ints(lens, "lens", 1, B)
+    device = cache.struct.device
+    B, pages = _ints(tables, "tables", 2, device).shape
+    _ints(lens, "lens", 1, device, B)
     if starts is None:
         if tokens != B:
             raise ValueError(f"{tokens} new tokens for {B} sequences of one each: starts is needed")
         max_q, starts_at = 1, None
     else:
-        starts_at = _ints(starts, "starts", 1, B + 1).data_ptr()
-        max_q = max(1, tokens if max_q is None else int(max_q))
+        starts_at = _ints(starts, "starts", 1, device, B + 1).data_ptr()
+        max_q = max(1, tokens if max_q is None else min(tokens, int(max_q)))
     most = min(pages * cache.layout.block_size, 2**31 - 1024)
     return KvBatch(B, max_q, tokens, most if max_len is None else min(most, int(max_len)), pages, 0, tables.stride(0),
                    tables.data_ptr(), lens.data_ptr(), starts_at)
@@ -146,7 +167,8 @@ def kv_append(cache: Cache, layer: int, k, v, tables, lens, starts=None, *, max_
     as e4m3(x / scale).
     """
     D = cache.layout.head_dim
-    kr, vr = _rows(k, "k", D), _rows(v, "v", D)
+    device = cache.struct.device
+    kr, vr = _rows(k, "k", D, device), _rows(v, "v", D, device)
     if k.shape != v.shape:
         raise ValueError(f"k and v differ in shape: {tuple(k.shape)} and {tuple(v.shape)}")
     batch = _batch(cache, tables, lens, starts, k.shape[0], max_q, max_len)
@@ -166,20 +188,16 @@ def kv_attend(cache: Cache, layer: int, q, tables, lens, starts=None, *, max_q=N
     token got in this call; ``prior=weights`` accumulates in place.  ``out`` (like ``q``) and ``lse`` (float32 [tokens]
     [query heads]) are made if not given; rows that belong to no sequence are left as they were.
     """
-    qr = _rows(q, "q", cache.layout.head_dim)
+    device = cache.struct.device
+    qr = _rows(q, "q", cache.layout.head_dim, device)
     batch = _batch(cache, tables, lens, starts, q.shape[0], max_q, max_len)
     options = KvAttendOptions(_cache_dtype(cache, dtype, q), int(window), 0.0 if scale is None else float(scale),
                               float(softcap), float(k_scale), float(v_scale))
     if slopes is not None:
-        if slopes.dtype != torch.float32 or not slopes.is_cuda or slopes.shape != (q.shape[1],) or \
-                not slopes.is_contiguous():
-            raise TypeError(f"slopes must be a contiguous float32 device tensor of {q.shape[1]} elements")
+        _floats(slopes, "slopes", device, (q.shape[1],))
         options.slopes = slopes.data_ptr()
     if weights is not None:
-        shape = (tables.shape[0], cache.layout.num_kv_heads)
-        if weights.dtype != torch.float32 or not weights.is_cuda or weights.dim() != 3 or weights.shape[:2] != shape or \
-                (weights.numel() and weights.stride(2) != 1):
-            raise TypeError(f"weights must be a float32 device tensor of {shape} dense rows")
+        _weights(weights, "weights", device, (tables.shape[0], cache.layout.num_kv_heads))
         if max_len is None:
             batch.max_len = min(batch.max_len, weights.shape[2])
         elif weights.shape[2] < batch.max_len:
@@ -187,18 +205,17 @@ def kv_attend(cache: Cache, layer: int, q, tables, lens, starts=None, *, max_q=N
         options.weights_out = weights.data_ptr()
         options.weights_seq_stride, options.weights_head_stride = weights.stride(0), weights.stride(1)
         if prior is not None:
-            if prior.dtype != torch.float32 or not prior.is_cuda or prior.shape != weights.shape or \
-                    prior.stride() != weights.stride():
-                raise TypeError("prior must have the type, shape and strides of weights")
+            _weights(prior, "prior", device)
+            if prior.shape != weights.shape or prior.stride() != weights.stride():
+                raise TypeError("prior must have the shape and strides of weights")
             options.weights_in = prior.data_ptr()
     elif prior is not None:
         raise ValueError("prior without weights")
     heads = (q.shape[0], q.shape[1])
-    if out is not None and (out.dtype != q.dtype or out.shape != q.shape):
-        raise TypeError("out must have the type and shape of q")
-    if lse is not None and (lse.dtype != torch.float32 or lse.shape != heads or not lse.is_cuda or
-                            not lse.is_contiguous()):
-        raise TypeError(f"lse must be a contiguous float32 device tensor of {heads}")
+    if out is not None and (out is q or out.dtype != q.dtype or out.shape != q.shape):
+        raise TypeError("out must have the type and shape of q, and be another tensor")
+    if lse is not None:
+        _floats(lse, "lse", device, heads)
     layout = cache.layout
     key = (layout.num_kv_heads, layout.head_dim, layout.elem_bytes, layout.block_size, batch.num_seqs, batch.max_queries,
            batch.num_queries, batch.max_len, options.window, weights is None, q.shape[1])
@@ -218,7 +235,7 @@ def kv_attend(cache: Cache, layer: int, q, tables, lens, starts=None, *, max_q=N
         if lse is None:
             lse = torch.empty(heads, dtype=torch.float32, device=q.device)
         workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
-    outr = _rows(out, "out", layout.head_dim)
+    outr = _rows(out, "out", layout.head_dim, device)
     _raise(_lib.kv_attend(ctypes.byref(cache.struct), int(layer), ctypes.byref(batch), ctypes.byref(options),
                           ctypes.byref(qr), ctypes.byref(outr), lse.data_ptr(),
                           workspace.data_ptr() if need else None, need, handle))
@@ -233,11 +250,10 @@ def kv_keep(weights, lens, budget: int, *, sinks: int = 0, recent: int = 0, max_
     """The tokens that each sequence keeps under ``budget``: its first ``sinks``, its last ``recent`` and the heaviest
     others by ``weights`` (float32 [B][H or 1][tokens], dense rows).  Returns (keep int32 [B][H][budget], ascending and
     then -1; kept_lens int32 [B]; kept_weights float32 like keep, then 0)."""
-    if not isinstance(weights, torch.Tensor) or weights.dtype != torch.float32 or not weights.is_cuda or \
-            weights.dim() != 3 or (weights.numel() and weights.stride(2) != 1):
-        raise TypeError("weights must be a [sequences][heads][tokens] float32 device tensor with dense rows")
+    device = torch.cuda.current_device() if torch.cuda.is_available() else -2
+    _weights(weights, "weights", device)
     B, H, L = weights.shape
-    _ints(lens, "lens", 1, B)
+    _ints(lens, "lens", 1, device, B)
     if max_len is not None and int(max_len) > L:
         raise ValueError(f"weights of {L} tokens for sequences of up to {max_len}")
     if budget < 1:
@@ -263,12 +279,12 @@ def kv_compact(cache: Cache, layer: int, tables, keep, kept_lens, dst_tables, *,
     """Copy the kept tokens' rows of layer ``layer`` into the pages of ``dst_tables``: token ``keep[b][h][j]`` becomes
     token j (``keep`` int32 [B][H or 1][budget], contiguous; ``kept_lens`` int32 [B] of them count).  The destination's
     pages are distinct and none of the sources'."""
-    tables = _ints(tables, "tables", 2)
-    B = tables.shape[0]
-    if not _ints(keep, "keep", 3, B).is_contiguous():
+    device = cache.struct.device
+    B = _ints(tables, "tables", 2, device).shape[0]
+    if not _ints(keep, "keep", 3, device, B).is_contiguous():
         raise TypeError("keep must be contiguous")
-    _ints(kept_lens, "kept_lens", 1, B)
-    _ints(dst_tables, "dst_tables", 2, B)
+    _ints(kept_lens, "kept_lens", 1, device, B)
+    _ints(dst_tables, "dst_tables", 2, device, B)
     handle, _ = _call_stream(stream)
     _raise(_lib.kv_compact(ctypes.byref(cache.struct), int(layer), B, tables.data_ptr(), tables.stride(0), tables.shape[1],
                            keep.data_ptr(), keep.shape[1], keep.shape[2], kept_lens.data_ptr(), dst_tables.data_ptr(),

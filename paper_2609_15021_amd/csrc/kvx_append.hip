@@ -136,13 +136,10 @@ kv_status append(const kv_cache *cache, int32_t layer, const kv_batch *batch, co
                     static_cast<long long>(most));
     const int64_t groups = (2 * most * a.token_vecs + kThreads - 1) / kThreads;
     const dim3 grid(static_cast<uint32_t>(std::min<int64_t>(groups, 32768)), static_cast<uint32_t>(batch->num_seqs));
-    if (!quantised)
-        hipLaunchKernelGGL(append_kernel<0>, grid, dim3(kThreads), 0, stream, a);
-    else if (k->dtype == KV_DTYPE_BF16)
-        hipLaunchKernelGGL(append_kernel<KV_DTYPE_BF16>, grid, dim3(kThreads), 0, stream, a);
-    else
-        hipLaunchKernelGGL(append_kernel<KV_DTYPE_F16>, grid, dim3(kThreads), 0, stream, a);
-    KVX_HIP(hipGetLastError());
+    const auto kernel = !quantised                  ? append_kernel<0>
+                        : k->dtype == KV_DTYPE_BF16 ? append_kernel<KV_DTYPE_BF16>
+                                                    : append_kernel<KV_DTYPE_F16>;
+    KVX_HIP(launch_kernel(kernel, grid, kThreads, stream, a));
     return KV_OK;
 }
 

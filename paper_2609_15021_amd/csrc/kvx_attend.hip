@@ -13,6 +13,14 @@ namespace kvx {
 
 namespace {
 
+constexpr int64_t kMaxWorkgroups = int64_t{1} << 22;  // of the tail kernel: 2^31 lanes
+
+// The factor of q . k.
+float scale_of(const kv_cache *cache, const kv_attend_options *o) {
+    return (o->scale == 0.f ? 1.f / std::sqrt(static_cast<float>(cache->layout.head_dim)) : o->scale) *
+           (o->k_scale == 0.f ? 1.f : o->k_scale);
+}
+
 // The checks of kv_attend that need no stream.
 kv_status check_attend(const kv_cache *cache, const kv_batch *batch, const kv_attend_options *o, const kv_rows *q) {
     if (!cache)
@@ -45,8 +53,19 @@ kv_status check_attend(const kv_cache *cache, const kv_batch *batch, const kv_at
     if (!(ks > 0.f && std::isfinite(ks)) || !(vs > 0.f && std::isfinite(vs)) ||
         (!quantised && (ks != 1.f || vs != 1.f)))
         return fail(KV_EINVAL, "scales must be positive, and 1 for a cache of 2-byte elements (got %g and %g)", ks, vs);
+    // What the kernels multiply scores by has to be a normal number.
+    const float product = scale_of(cache, o), inv = o->softcap > 0.f ? product / o->softcap : 1.f;
+    if (!(product >= 1e-36f && product <= 1e36f) || !(inv >= 1e-36f && inv <= 1e36f))
+        return fail(KV_EUNSUPPORTED, "scale %g with k_scale %g and softcap %g is beyond 32-bit scores", o->scale, o->k_scale,
+                    o->softcap);
     if (o->weights_in && !o->weights_out)
         return fail(KV_EINVAL, "weights_in without weights_out");
+    // Rows are counted in 32 bits, and the tail kernel's workgroups by what one launch takes.
+    const int64_t queries = std::min(batch->max_queries, batch->num_queries), group = q->heads / H;
+    if (queries * group > INT32_MAX / 2 || (queries * group > kStepRows &&
+                                            tail_tiles(queries, group) * H * batch->num_seqs > kMaxWorkgroups))
+        return fail(KV_EUNSUPPORTED, "up to %lld new tokens in each of %d sequences of %d query heads are too many for one "
+                    "call", static_cast<long long>(queries), batch->num_seqs, q->heads);
     if (o->weights_out && (o->weights_seq_stride < 0 || o->weights_head_stride < 0 ||
                            (batch->num_seqs > 0 && H > 1 && o->weights_head_stride < batch->max_len) ||
                            (batch->num_seqs > 1 && o->weights_seq_stride < batch->max_len)))
@@ -69,12 +88,12 @@ struct Plan {
 
 int64_t round_up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 
-// The tail kernel's parts, for `have` tiles of rows.  512 of its workgroups run at once (2 per CU; 256 where D > 128), so
+// The tail kernel's parts, for `have` tiles of rows (of the `launched`, others are empty).  512 of its workgroups run at once (2 per CU; 256 where D > 128), so
 // they may leave the last round nearly empty, and tiles that see less than others end it early: the number of parts is the
 // one whose rounds (between those of equal parts, and those without an edge and half a part idle at the end) and joining
 // take least, at the 0.2 ns per token and column that such a round takes and the 5 TB/s at which parts are written and
 // read again.  Parts have no fewer than 256 tokens and no more than 256 MB between them.
-Parts tail_parts_for(int64_t longest, int64_t have, int64_t head_dim) {
+Parts tail_parts_for(int64_t longest, int64_t have, int64_t launched, int64_t head_dim) {
     const int64_t at_once = head_dim > 128 ? 256 : 512;
     const double tokens_us = 0.2e-3 * static_cast<double>(head_dim) * static_cast<double>(longest);
     const double parts_bytes = static_cast<double>(have) * kTailRows * static_cast<double>(head_dim) * 4;
@@ -82,7 +101,7 @@ Parts tail_parts_for(int64_t longest, int64_t have, int64_t head_dim) {
     double best_us = 0.;
     for (int64_t splits = 1; splits <= 64; ++splits) {
         const double n = static_cast<double>(splits);
-        if (splits > 1 && (longest < 256 * splits || parts_bytes * n > 256e6))
+        if (splits > 1 && (longest < 256 * splits || parts_bytes * n > 256e6 || launched * splits > kMaxWorkgroups))
             break;
         const double rounds = 0.5 * (static_cast<double>((have * splits + at_once - 1) / at_once) +
                                      static_cast<double>(have * splits) / static_cast<double>(at_once) + 0.5);
@@ -126,10 +145,10 @@ Plan plan_of(const kv_cache *cache, const kv_batch *batch, const kv_attend_optio
     p.parts = batch->num_seqs <= kShareSeqs && p.shares.target > 1;
     if (p.tail) {
         const int64_t seen = o->window > 0 ? o->window + int64_t{kTailRows} + 31 : batch->max_len;
-        const int64_t tiles_each = (all_rows + kTailRows - 1) / kTailRows;
+        const int64_t tiles_each = tail_tiles(p.max_queries, group);
         const int64_t tiles_all = (batch->num_queries * group + kTailRows - 1) / kTailRows + batch->num_seqs;
         p.tail_parts = tail_parts_for(std::max<int64_t>(std::min<int64_t>(seen, batch->max_len), 1),
-                                      H * std::min(batch->num_seqs * tiles_each, tiles_all), D);
+                                      H * std::min(batch->num_seqs * tiles_each, tiles_all), heads * tiles_each, D);
     }
     int64_t at = round_up(static_cast<int64_t>(batch->num_queries) * q->heads * 4, 16);
     const auto take = [&](int64_t bytes) {
@@ -200,8 +219,7 @@ kv_status attend(const kv_cache *cache, int32_t layer, const kv_batch *batch, co
     a.weights_out = o->weights_out;
     a.weights_seq_stride = o->weights_seq_stride;
     a.weights_head_stride = o->weights_head_stride;
-    a.scale = (o->scale == 0.f ? 1.f / std::sqrt(static_cast<float>(cache->layout.head_dim)) : o->scale) *
-              (o->k_scale == 0.f ? 1.f : o->k_scale);
+    a.scale = scale_of(cache, o);
     a.softcap = o->softcap;
     a.v_scale = o->v_scale == 0.f ? 1.f : o->v_scale;
     a.window = o->window;

@@ -7,6 +7,7 @@ namespace kvx {
 
 // Rows of a workgroup of the tail kernel.
 constexpr int kTailRows = 128;
+inline int64_t tail_tiles(int64_t max_queries, int64_t group) { return (max_queries * group + kTailRows - 1) / kTailRows; }
 
 // Sequences of at most this many (new token, query head) rows per KV head go to the step kernel, others to the tail one.
 constexpr int kStepRows = 64;

@@ -550,21 +550,27 @@ __global__ __launch_bounds__(256) void weigh_step_kernel(const AttendArgs a) {
 }
 
 template <class T, bool FP8, int DP, int NT>
-void launch(const AttendArgs &a, const Shares &shares, int max_rows, hipStream_t stream) {
+hipError_t launch(const AttendArgs &a, const Shares &shares, int max_rows, hipStream_t stream) {
     const int tiles = (max_rows + 16 * NT - 1) / (16 * NT);
-    hipLaunchKernelGGL((step_kernel<T, FP8, DP, NT>), dim3(shares.items, tiles * a.pages.H),
-                       dim3(64 * kWaves), 0, stream, a, shares);
+    return launch_kernel(step_kernel<T, FP8, DP, NT>, dim3(shares.items, tiles * a.pages.H), 64 * kWaves, stream, a, shares);
 }
 
 template <class T, bool FP8>
-void launch(const AttendArgs &a, const Shares &shares, int max_rows, hipStream_t stream) {
+hipError_t launch(const AttendArgs &a, const Shares &shares, int max_rows, hipStream_t stream) {
     const bool two = step_tile_rows(max_rows, a.pages.D) == 32;
     if (a.pages.D > 128)
-        launch<T, FP8, 256, 1>(a, shares, max_rows, stream);
-    else if (a.pages.D > 64)
-        two ? launch<T, FP8, 128, 2>(a, shares, max_rows, stream) : launch<T, FP8, 128, 1>(a, shares, max_rows, stream);
-    else
-        two ? launch<T, FP8, 64, 2>(a, shares, max_rows, stream) : launch<T, FP8, 64, 1>(a, shares, max_rows, stream);
+        return launch<T, FP8, 256, 1>(a, shares, max_rows, stream);
+    if (a.pages.D > 64)
+        return two ? launch<T, FP8, 128, 2>(a, shares, max_rows, stream) : launch<T, FP8, 128, 1>(a, shares, max_rows, stream);
+    return two ? launch<T, FP8, 64, 2>(a, shares, max_rows, stream) : launch<T, FP8, 64, 1>(a, shares, max_rows, stream);
+}
+
+template <bool SPREAD, class From>
+hipError_t launch_join(const AttendArgs &a, const From &from, int max_queries, hipStream_t stream) {
+    const int groups = SPREAD ? 1 : 256 / (a.pages.D / 4);
+    const dim3 grid(static_cast<uint32_t>((max_queries + groups - 1) / groups), static_cast<uint32_t>(a.heads),
+                    static_cast<uint32_t>(a.num_seqs));
+    return launch_kernel(join_kernel<SPREAD, From>, grid, 256, stream, a, from);
 }
 
 }  // namespace
@@ -573,24 +579,9 @@ hipError_t launch_step(const AttendArgs &a, const Shares &shares, int max_querie
     const int max_rows = static_cast<int>(std::min<int64_t>(kStepRows, static_cast<int64_t>(max_queries) * a.group));
     const bool fp8 = a.cache_type == KV_DTYPE_E4M3;
     if (a.q_type == KV_DTYPE_BF16)
-        fp8 ? launch<Bf16, true>(a, shares, max_rows, stream) : launch<Bf16, false>(a, shares, max_rows, stream);
-    else
-        fp8 ? launch<F16, true>(a, shares, max_rows, stream) : launch<F16, false>(a, shares, max_rows, stream);
-    return hipGetLastError();
+        return fp8 ? launch<Bf16, true>(a, shares, max_rows, stream) : launch<Bf16, false>(a, shares, max_rows, stream);
+    return fp8 ? launch<F16, true>(a, shares, max_rows, stream) : launch<F16, false>(a, shares, max_rows, stream);
 }
-
-namespace {
-
-template <bool SPREAD, class From>
-hipError_t launch_join(const AttendArgs &a, const From &from, int max_queries, hipStream_t stream) {
-    const int groups = SPREAD ? 1 : 256 / (a.pages.D / 4);
-    const dim3 grid(static_cast<uint32_t>((max_queries + groups - 1) / groups), static_cast<uint32_t>(a.heads),
-                    static_cast<uint32_t>(a.num_seqs));
-    hipLaunchKernelGGL((join_kernel<SPREAD, From>), grid, dim3(256), 0, stream, a, from);
-    return hipGetLastError();
-}
-
-}  // namespace
 
 hipError_t launch_join_step(const AttendArgs &a, const Shares &shares, int max_queries, hipStream_t stream) {
     return launch_join<true>(a, shares, std::min(max_queries, kStepRows), stream);
@@ -605,8 +596,7 @@ hipError_t launch_join_tail(const AttendArgs &a, const Parts &parts, int max_que
 hipError_t launch_weigh_step(const AttendArgs &a, hipStream_t stream) {
     const dim3 grid(static_cast<uint32_t>((a.batch.max_len + 1023) / 1024), static_cast<uint32_t>(a.pages.H),
                     static_cast<uint32_t>(a.num_seqs));
-    hipLaunchKernelGGL(weigh_step_kernel, grid, dim3(256), 0, stream, a);
-    return hipGetLastError();
+    return launch_kernel(weigh_step_kernel, grid, 256, stream, a);
 }
 
 }  // namespace kvx

@@ -524,40 +524,37 @@ __global__ __launch_bounds__(64 * kWeighWaves) void weigh_kernel(const AttendArg
 }
 
 template <class T, bool FP8, int DP, int TK, int RW, bool PLAIN>
-void launch(const AttendArgs &a, const Parts &parts, int max_queries, hipStream_t stream) {
-    const int tiles = static_cast<int>((static_cast<int64_t>(max_queries) * a.group + kRows - 1) / kRows);
+hipError_t launch(const AttendArgs &a, const Parts &parts, int max_queries, hipStream_t stream) {
+    const int tiles = static_cast<int>(tail_tiles(max_queries, a.group));
     const uint32_t grid = static_cast<uint32_t>(tiles) * parts.splits * a.pages.H * a.num_seqs;
-    hipLaunchKernelGGL((tail_kernel<T, FP8, DP, TK, RW, PLAIN>), dim3(grid), dim3(64 * kRows / RW), 0, stream, a, parts, tiles);
+    return launch_kernel(tail_kernel<T, FP8, DP, TK, RW, PLAIN>, dim3(grid), 64 * kRows / RW, stream, a, parts, tiles);
 }
 
 template <class T, bool FP8, bool PLAIN>
-void launch(const AttendArgs &a, const Parts &parts, int max_queries, hipStream_t stream) {
+hipError_t launch(const AttendArgs &a, const Parts &parts, int max_queries, hipStream_t stream) {
+    // (Wide rows: 32 of them would need more registers than two waves of a SIMD have, and one wave alone took 1.7 times
+    // as long.)
     if (a.pages.D > 128)
-        launch<T, FP8, 256, 64, 16, PLAIN>(a, parts, max_queries, stream);
-    else if (a.pages.D > 64)
-        launch<T, FP8, 128, 64, 32, PLAIN>(a, parts, max_queries, stream);
-    else
-        launch<T, FP8, 64, 64, 32, PLAIN>(a, parts, max_queries, stream);
+        return launch<T, FP8, 256, 64, 16, PLAIN>(a, parts, max_queries, stream);
+    if (a.pages.D > 64)
+        return launch<T, FP8, 128, 64, 32, PLAIN>(a, parts, max_queries, stream);
+    return launch<T, FP8, 64, 64, 32, PLAIN>(a, parts, max_queries, stream);
 }
 
 template <class T, bool FP8>
-void launch(const AttendArgs &a, const Parts &parts, int max_queries, hipStream_t stream) {
-    if (a.softcap == 0.f && !a.slopes)
-        launch<T, FP8, true>(a, parts, max_queries, stream);
-    else
-        launch<T, FP8, false>(a, parts, max_queries, stream);
+hipError_t launch(const AttendArgs &a, const Parts &parts, int max_queries, hipStream_t stream) {
+    return a.softcap == 0.f && !a.slopes ? launch<T, FP8, true>(a, parts, max_queries, stream)
+                                         : launch<T, FP8, false>(a, parts, max_queries, stream);
 }
 
 template <class T, bool FP8>
-void launch_weigh(const AttendArgs &a, hipStream_t stream) {
+hipError_t launch_weigh(const AttendArgs &a, hipStream_t stream) {
     const dim3 grid(static_cast<uint32_t>((a.batch.max_len + 32 * kWeighWaves - 1) / (32 * kWeighWaves)),
                     static_cast<uint32_t>(a.pages.H), static_cast<uint32_t>(a.num_seqs));
-    if (a.pages.D > 128)
-        hipLaunchKernelGGL((weigh_kernel<T, FP8, 256>), grid, dim3(64 * kWeighWaves), 0, stream, a);
-    else if (a.pages.D > 64)
-        hipLaunchKernelGGL((weigh_kernel<T, FP8, 128>), grid, dim3(64 * kWeighWaves), 0, stream, a);
-    else
-        hipLaunchKernelGGL((weigh_kernel<T, FP8, 64>), grid, dim3(64 * kWeighWaves), 0, stream, a);
+    const auto kernel = a.pages.D > 128  ? weigh_kernel<T, FP8, 256>
+                        : a.pages.D > 64 ? weigh_kernel<T, FP8, 128>
+                                         : weigh_kernel<T, FP8, 64>;
+    return launch_kernel(kernel, grid, 64 * kWeighWaves, stream, a);
 }
 
 }  // namespace
@@ -565,19 +562,15 @@ void launch_weigh(const AttendArgs &a, hipStream_t stream) {
 hipError_t launch_tail(const AttendArgs &a, const Parts &parts, int max_queries, hipStream_t stream) {
     const bool fp8 = a.cache_type == KV_DTYPE_E4M3;
     if (a.q_type == KV_DTYPE_BF16)
-        fp8 ? launch<Bf16, true>(a, parts, max_queries, stream) : launch<Bf16, false>(a, parts, max_queries, stream);
-    else
-        fp8 ? launch<F16, true>(a, parts, max_queries, stream) : launch<F16, false>(a, parts, max_queries, stream);
-    return hipGetLastError();
+        return fp8 ? launch<Bf16, true>(a, parts, max_queries, stream) : launch<Bf16, false>(a, parts, max_queries, stream);
+    return fp8 ? launch<F16, true>(a, parts, max_queries, stream) : launch<F16, false>(a, parts, max_queries, stream);
 }
 
 hipError_t launch_weigh(const AttendArgs &a, hipStream_t stream) {
     const bool fp8 = a.cache_type == KV_DTYPE_E4M3;
     if (a.q_type == KV_DTYPE_BF16)
-        fp8 ? launch_weigh<Bf16, true>(a, stream) : launch_weigh<Bf16, false>(a, stream);
-    else
-        fp8 ? launch_weigh<F16, true>(a, stream) : launch_weigh<F16, false>(a, stream);
-    return hipGetLastError();
+        return fp8 ? launch_weigh<Bf16, true>(a, stream) : launch_weigh<Bf16, false>(a, stream);
+    return fp8 ? launch_weigh<F16, true>(a, stream) : launch_weigh<F16, false>(a, stream);
 }
 
 }  // namespace kvx

@@ -126,8 +126,7 @@ kv_status compact(const kv_cache *cache, int32_t layer, int32_t num_seqs, const 
     const int64_t groups = (budget * vecs + kEach * kThreads - 1) / (kEach * kThreads);
     const dim3 grid(static_cast<uint32_t>(std::min<int64_t>(groups, 32768)), static_cast<uint32_t>(num_seqs),
                     static_cast<uint32_t>(2 * lay.num_kv_heads));
-    hipLaunchKernelGGL(compact_kernel, grid, dim3(kThreads), 0, stream, a);
-    KVX_HIP(hipGetLastError());
+    KVX_HIP(launch_kernel(compact_kernel, grid, kThreads, stream, a));
     return KV_OK;
 }
 

@@ -361,9 +361,10 @@ __global__ __launch_bounds__(kThreads) void clear_kernel(int32_t *x, int64_t n) 
 // Pieces of a row: where a few long rows would leave most CUs idle (whole rows of 16,384 tokens and 128 of them or more
 // take less than the launches that pieces need).
 int pieces_of(int32_t num_seqs, int32_t heads, int32_t max_len, int32_t budget) {
-    if (max_len <= 2 * kPiece || max_len <= budget || static_cast<int64_t>(num_seqs) * heads >= 128)
+    const int pieces = max_len > 0 ? (max_len - 1) / kPiece + 1 : 1;
+    if (max_len <= 2 * kPiece || max_len <= budget || static_cast<int64_t>(num_seqs) * heads >= 128 || pieces > 65535)
         return 1;
-    return (max_len - 1) / kPiece + 1;
+    return pieces;
 }
 
 int64_t workspace_bytes_of(int32_t num_seqs, int32_t heads, int32_t pieces) {
@@ -412,21 +413,18 @@ kv_status keep(const float *weights, int64_t seq_stride, int64_t head_stride, co
     const KeepArgs a{weights, seq_stride, head_stride, lens, heads, max_len, budget, sinks, recent, keep, kept_lens,
                      kept_weights, err, pieces, digits, need > 0 ? digits + digit_words : nullptr};
     const dim3 grid(static_cast<uint32_t>(heads), static_cast<uint32_t>(num_seqs), static_cast<uint32_t>(pieces));
-    const auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kKeepThreads), 0, stream, a); };
+    const auto launch = [&](void (*kernel)(KeepArgs)) { return launch_kernel(kernel, grid, kKeepThreads, stream, a); };
     if (pieces > 1) {
         const uint32_t clear = static_cast<uint32_t>(std::min<int64_t>((digit_words + kThreads - 1) / kThreads, 1024));
-        hipLaunchKernelGGL(clear_kernel, dim3(clear), dim3(kThreads), 0, stream, digits, digit_words);
-        launch(keep_kernel<2, 0>);
-        launch(keep_kernel<2, 1>);
-        launch(keep_kernel<2, 2>);
-        launch(keep_kernel<2, kCount>);
-        launch(keep_kernel<2, kWrite>);
-    } else if (max_len <= 2 * kRound) {
-        launch(keep_kernel<2, kWhole>);
+        KVX_HIP(launch_kernel(clear_kernel, dim3(clear), kThreads, stream, digits, digit_words));
+        KVX_HIP(launch(keep_kernel<2, 0>));
+        KVX_HIP(launch(keep_kernel<2, 1>));
+        KVX_HIP(launch(keep_kernel<2, 2>));
+        KVX_HIP(launch(keep_kernel<2, kCount>));
+        KVX_HIP(launch(keep_kernel<2, kWrite>));
     } else {
-        launch(keep_kernel<0, kWhole>);
+        KVX_HIP(launch(max_len <= 2 * kRound ? keep_kernel<2, kWhole> : keep_kernel<0, kWhole>));
     }
-    KVX_HIP(hipGetLastError());
     return KV_OK;
 }
 

@@ -1,6 +1,8 @@
 // Internal declarations of the operators on a paged cache (include/kvx_attend.h).
 #pragma once
 
+#include <tuple>
+
 #include "kvx_internal.h"
 
 #include "kvx_attend.h"
@@ -66,6 +68,19 @@ __device__ __forceinline__ bool in_cache(const Pages &p, int block) {
         return true;
     report(p.err, KV_ASYNC_BAD_BLOCK);
     return false;
+}
+
+// Launches kernel(args...), whose own error it returns.
+template <class... Args, class... Given>
+hipError_t launch_kernel(void (*kernel)(Args...), dim3 grid, int threads, hipStream_t stream, const Given &...given) {
+    std::tuple<Args...> args(given...);
+    return std::apply(
+        [&](auto &...arg) {
+            void *kernel_args[] = {&arg...};
+            return hipLaunchKernel(reinterpret_cast<const void *>(kernel), grid, dim3(static_cast<uint32_t>(threads)),
+                                   kernel_args, 0, stream);
+        },
+        args);
 }
 
 // Host side.

@@ -141,6 +141,11 @@ def test_attend_refusals():
                     dict(weights_out=SOME, weights_seq_stride=-128, weights_head_stride=64)):
         assert call(good, 0, batch, **options) == kvx.KV_EINVAL, options
         assert call(good, 0, batch, workspace_only=True, **options) == kvx.KV_EINVAL, options
+    for options in (dict(scale=1e-38), dict(scale=1e37), dict(scale=1e-30, softcap=1e10)):
+        assert call(good, 0, batch, **options) == kvx.KV_EUNSUPPORTED, options
+    for changes in (dict(max_queries=2**30, num_queries=2**30), dict(max_queries=1 << 20, num_queries=1 << 20, num_seqs=500)):
+        many = _batch(attend, starts=SOME, **changes)
+        assert call(good, 0, many) == kvx.KV_EUNSUPPORTED, changes
     need = call(good, 0, batch, workspace_only=True)
     assert need >= 0
     if need:
@@ -217,6 +222,7 @@ def test_binding_refuses_before_any_library_call(monkeypatch):
 
     cache = object.__new__(kvx.Cache)
     cache.layout = kvx.make_layout(*LAYOUT)
+    cache.struct = _cache(kvx, cache.layout)
     monkeypatch.setattr(attend, "_lib", NoLibrary())
     rows = torch.zeros(2, 2, 64, dtype=torch.bfloat16)
     ints = torch.zeros(2, 4, dtype=torch.int32)

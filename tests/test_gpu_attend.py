@@ -104,6 +104,53 @@ def test_several_new_tokens(H, G, D, BS, nhd, fp8, dtype, lens, new):
     run(c, weights="fresh")
 
 
+@pytest.mark.parametrize("lens,new,window", [([3000], [70], 0), ([1300, 4100], [66, 90], 0), ([4100, 700], [129, 65], 300),
+                                             ([2500, 100, 900], [3, 100, 1], 0)])
+@pytest.mark.parametrize("H,G,D,fp8,dtype", [(1, 1, 128, False, BF16), (2, 2, 64, False, F16), (1, 3, 256, True, BF16),
+                                              (1, 2, 200, False, BF16)])
+def test_long_sequences_in_parts(H, G, D, fp8, dtype, lens, new, window):
+    """Few rows over many tokens: they are split, and joined."""
+    c = ref.Case(H, G, D, 16, lens, new, fp8=fp8, dtype=dtype, seed=D + G)
+    run(c, dict(window=window), weights="fresh")
+
+
+@pytest.mark.parametrize("softcap", [0.5, 64.0, 65.0, 3000.0])
+def test_caps(softcap):
+    """Small and large caps, where scores are far below and far above them."""
+    for new in ([1, 1], [90, 70]):
+        c = ref.Case(2, 2, 64, 16, [200, 100], new, seed=21, spread=6.0)
+        run(c, dict(softcap=softcap, scale=1.0), weights="fresh")
+
+
+def test_many_sequences():
+    """Hundreds of sequences, long ones among short ones, and more than are shared out in parts."""
+    gen = np.random.default_rng(3)
+    lens = [int(n) for n in gen.integers(0, 60, 150)]
+    lens[7], lens[70], lens[149] = 3000, 1500, 700
+    c = ref.Case(2, 2, 64, 16, lens, [1 if n % 5 else 0 for n in lens], seed=22)
+    run(c, weights="fresh")
+    lens = [int(n) for n in gen.integers(0, 12, 1100)]
+    lens[1000] = 400
+    run(ref.Case(1, 2, 16, 4, lens, [1 + n % 2 for n in lens], seed=23))
+
+
+def test_weights_at_any_element():
+    """Rows of weights that start at odd elements, of odd lengths."""
+    for new in ([1, 1, 1], [30, 70, 1]):
+        c = ref.Case(2, 3, 64, 16, [37, 90, 258], new, seed=24)
+        cache, _, q, _, _, tables, lens, starts = c.device()
+        wide = torch.rand(3, 2, 2, 263, device=DEV)
+        before = wide.clone()
+        view = wide[:, 1, :, 1:260]
+        attend.kv_attend(cache, 0, q, tables, lens, starts, weights=view, prior=view, max_len=258)
+        want = ref.attend(c)
+        for b, n in enumerate(c.lens):
+            expected = before[b, 1, :, 1:1 + n].double().cpu().numpy() + want[2][b, :, :n]
+            ref.check(view[b, :, :n], expected, want[5][b, :, :n] + np.abs(expected) * 2.0**-24, "weights")
+            assert torch.equal(wide[b, 1, :, 1 + n:], before[b, 1, :, 1 + n:])
+        assert torch.equal(wide[:, 0], before[:, 0]) and torch.equal(wide[..., 0], before[..., 0])
+
+
 def test_rows_without_tokens():
     """Empty sequences, sequences without new tokens, and rows that would lie before token 0: 0 and -infinity."""
     for lens, new in (([0, 5, 0, 3], [1, 1, 0, 6]), ([0], [4]), ([2, 100], [130, 0]), ([0, 0], [0, 0]), ([3], [0])):
@@ -276,16 +323,17 @@ def test_cache_beyond_32_bits(nhd):
     assert torch.equal(got[0, 2], c.new_k[0]) and torch.equal(got[1, 2], c.new_v[0])
 
 
-def test_repeatable_and_independent_of_the_batch():
+def test_repeatable():
     """The same bits on every run."""
-    c = ref.Case(2, 5, 128, 16, [3000, 17, 900], [1, 1, 1], seed=14)
-    cache, _, q, _, _, tables, lens, _ = c.device()
-    weights = torch.zeros(3, 2, 3000, device=DEV)
-    first = [t.clone() for t in attend.kv_attend(cache, 0, q, tables, lens, weights=weights)] + [weights.clone()]
-    for _ in range(20):
-        got = (*attend.kv_attend(cache, 0, q, tables, lens, weights=weights), weights)
-        for x, y in zip(first, got):
-            assert torch.equal(x, y)
+    for new in ([1, 1, 1], [100, 17, 3]):
+        c = ref.Case(2, 5, 128, 16, [3000, 17, 900], new, seed=14)
+        cache, _, q, _, _, tables, lens, starts = c.device()
+        weights = torch.zeros(3, 2, 3000, device=DEV)
+        first = [t.clone() for t in attend.kv_attend(cache, 0, q, tables, lens, starts, weights=weights)] + [weights.clone()]
+        for _ in range(20):
+            got = (*attend.kv_attend(cache, 0, q, tables, lens, starts, weights=weights), weights)
+            for x, y in zip(first, got):
+                assert torch.equal(x, y)
 
 
 # ---- kv_append ----------------------------------------------------------------------------
