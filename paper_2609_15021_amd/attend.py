@@ -76,15 +76,20 @@ def _ints(t, name: str, dims: int, device: int, rows=None):
     if not isinstance(t, torch.Tensor) or t.dtype is not torch.int32 or t.dim() != dims or \
             (t.stride(-1) != 1 and t.numel()):
         raise TypeError(f"{name} must be a {dims}-dimensional int32 device tensor with a dense last dimension")
-    _on(t, name, device)
+    if t.get_device() != device:
+        _elsewhere(t, name, device)
     if rows is not None and t.shape[0] != rows:
         raise ValueError(f"{name} has {t.shape[0]} rows; {rows} are needed")
     return t
 
 
+def _elsewhere(t, name: str, device: int) -> None:
+    raise TypeError(f"{name} must be a device tensor on device {device}, where the call works (it is on {t.device})")
+
+
 def _on(t, name: str, device: int) -> None:
-    if t.get_device() != device:  # -1 for a host tensor
-        raise TypeError(f"{name} must be a device tensor on device {device}, where the call works (it is on {t.device})")
+    if t.get_device() != device:
+        _elsewhere(t, name, device)
 
 
 def _floats(t, name: str, device: int, shape) -> None:
@@ -104,7 +109,8 @@ def _weights(t, name: str, device: int, rows=None) -> None:
 def _rows(t, name: str, head_dim: int, device: int) -> KvRows:
     if not isinstance(t, torch.Tensor) or t.dim() != 3 or t.dtype not in (torch.bfloat16, torch.float16):
         raise TypeError(f"{name} must be a [tokens][heads][D] device tensor of bfloat16 or float16")
-    _on(t, name, device)
+    if t.get_device() != device:
+        _elsewhere(t, name, device)
     _, heads, width = t.shape
     token, head, column = t.stride()
     if width != head_dim or (column != 1 and t.numel()):

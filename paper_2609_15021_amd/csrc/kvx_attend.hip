@@ -80,8 +80,8 @@ struct Plan {
     int32_t max_queries, max_rows;  // of a sequence; rows per KV head in the step kernel
     bool tail;                      // some sequence may have more than kStepRows rows
     bool scores;                    // weights_out from the step kernel's scores
-    bool parts;                     // the step kernel's sequences may have several parts
-    int64_t score_len, step_stats, step_sums, tail_stats, tail_sums, scores_at, bytes;
+    bool listed;                    // the step kernel's parts are listed by a kernel
+    int64_t score_len, lists, step_stats, step_sums, tail_stats, tail_sums, scores_at, bytes;
     Shares shares;
     Parts tail_parts;
 };
@@ -130,19 +130,21 @@ Plan plan_of(const kv_cache *cache, const kv_batch *batch, const kv_attend_optio
     // With more rows than a tile has the scores would outgrow K itself: they are taken again instead.
     p.scores = o->weights_out && all_rows <= 16;
     // The step kernel: as many workgroups as run at once (by its registers 2 per CU, 3 up to 64 columns, 1 with wide
-    // 2-byte rows), one each for more sequences than that.
+    // 2-byte rows), or one for each sequence where that is more.
     const int64_t tile = step_tile_rows(p.max_rows, static_cast<int>(D)), tiles = (p.max_rows + tile - 1) / tile;
     const int64_t at_once = D <= 64 ? 768 : D > 128 && cache->layout.elem_bytes == 2 ? 256 : 512;
-    const int64_t window = o->window > 0 ? o->window + kStepRows + 31 : batch->max_len;
+    const int64_t window = o->window > 0 ? o->window + int64_t{kStepRows} + 31 : batch->max_len;
     const int64_t longest = std::max<int64_t>(std::min<int64_t>(window, batch->max_len), 1);
-    const int64_t most = (longest + kShareLen - 1) / kShareLen * batch->num_seqs;  // parts that can be
-    p.shares.target = static_cast<int32_t>(std::min(std::max<int64_t>(at_once / (H * tiles), 1), most));
-    p.shares.items = std::max(p.shares.target, batch->num_seqs) + (batch->num_seqs > 1 ? batch->num_seqs : 0);
-    if (batch->num_seqs > kShareSeqs || p.shares.target == 1)
-        p.shares.items = batch->num_seqs;
-    p.shares.num_seqs = batch->num_seqs;
-    p.shares.row_cap = p.max_rows;
-    p.parts = batch->num_seqs <= kShareSeqs && p.shares.target > 1;
+    // A part has 32 tokens a wave at least; where the sequences alone fill the chip, enough that splitting and joining
+    // take less than the wait for a long one does (2,000 sequences of up to 300 tokens: 82 us whole, 129 in parts).
+    Shares &s = p.shares;
+    s.shortest = heads * tiles >= at_once ? 512 : 128;
+    const int64_t most = (longest + s.shortest - 1) / s.shortest * batch->num_seqs;  // parts that can be
+    s.num_seqs = batch->num_seqs;
+    s.target = static_cast<int32_t>(std::min(std::max<int64_t>(at_once / (H * tiles), s.num_seqs), most));
+    s.alone = longest <= s.shortest || s.target == 1;
+    s.items = s.alone || s.num_seqs == 1 ? std::max(s.num_seqs, s.alone ? 1 : s.target) : s.target + s.num_seqs;
+    s.row_cap = p.max_rows;
     if (p.tail) {
         const int64_t seen = o->window > 0 ? o->window + int64_t{kTailRows} + 31 : batch->max_len;
         const int64_t tiles_each = tail_tiles(p.max_queries, group);
@@ -156,7 +158,9 @@ Plan plan_of(const kv_cache *cache, const kv_batch *batch, const kv_attend_optio
         at += round_up(bytes, 16);
         return here;
     };
-    const int64_t shared = p.parts ? H * p.shares.items * p.shares.row_cap : 0;
+    const int64_t shared = s.alone ? 0 : H * s.items * s.row_cap;
+    p.listed = !s.alone && s.num_seqs > kShareSeqs;
+    p.lists = take(p.listed ? (2 + 2 * (int64_t{s.num_seqs} + s.items)) * 4 : 0);
     p.step_stats = take(shared * 8);
     p.step_sums = take(shared * D * 4);
     const int64_t split =
@@ -209,6 +213,7 @@ kv_status attend(const kv_cache *cache, int32_t layer, const kv_batch *batch, co
     Parts tail = plan.tail_parts;
     step.stats = at(plan.step_stats);
     step.sums = at(plan.step_sums);
+    step.items_of = plan.listed ? reinterpret_cast<int32_t *>(space + plan.lists) : nullptr;
     tail.stats = at(plan.tail_stats);
     tail.sums = at(plan.tail_sums);
     a.scores = plan.scores ? at(plan.scores_at) : nullptr;
@@ -230,8 +235,10 @@ kv_status attend(const kv_cache *cache, int32_t layer, const kv_batch *batch, co
     a.cache_type = o->cache_dtype;
     a.by_group = divisor(a.group);
     if (plan.max_queries > 0) {
+        if (plan.listed)
+            KVX_HIP(launch_share(a, step, stream));
         KVX_HIP(launch_step(a, step, plan.max_queries, stream));
-        if (plan.parts)
+        if (!step.alone)
             KVX_HIP(launch_join_step(a, step, plan.max_queries, stream));
         if (plan.tail) {
             KVX_HIP(launch_tail(a, tail, plan.max_queries, stream));

@@ -55,12 +55,16 @@ inline int step_tile_rows(int max_rows, int head_dim) { return max_rows > 16 && 
 
 // How the step kernel shares its sequences' tokens out: in parts of one length for all, on the device, where the lengths
 // are.  A long sequence among short ones is then no workgroup's alone, and the parts number at most `target`, which fill
-// the chip once.  items >= the parts of any batch: target, or one each of more sequences than that.
+// the chip once (or twice the sequences, where those are more).  Up to kShareSeqs sequences every wave works out the
+// sharing for itself; more of them are shared out by a kernel of its own, which leaves the lists below.
 struct Shares {
-    int32_t target, items, num_seqs;
-    int32_t row_cap;  // most rows per KV head of a sequence
-    float *sums;      // [KV head][item][row_cap][D], unscaled
-    float *stats;     // [KV head][item][row_cap][2]: largest score and sum, in powers of 2
+    int32_t target, items, num_seqs;  // items >= the parts of any batch
+    int32_t shortest;                 // tokens of a part at least
+    int32_t alone;                    // every sequence is one part
+    int32_t row_cap;                  // most rows per KV head of a sequence
+    float *sums;                      // [KV head][item][row_cap][D], unscaled
+    float *stats;                     // [KV head][item][row_cap][2]: largest score and sum, in powers of 2
+    int32_t *items_of;                // NULL, or: length of a part; [sequence]: first item, parts; [item]: sequence, split
 };
 
 // A sequence's part: `split` of `parts`, `len` tokens each; its first part is item `item0`.
@@ -68,8 +72,7 @@ struct Share {
     int b, split, parts, len, item0;
 };
 
-constexpr int kShareSeqs = 1024;  // more sequences than this are one part each
-constexpr int kShareLen = 128;    // shortest part: 32 tokens a wave
+constexpr int kShareSeqs = 64;
 
 // Tokens of sequence b that the step kernel takes, from span.start on; 0 and no rows if none.
 __device__ __forceinline__ int share_tokens(const AttendArgs &a, int b, bool tell, bool &rows) {
@@ -93,63 +96,80 @@ __device__ __forceinline__ int64_t sum_of_wave(int64_t x) {
     return x;
 }
 
-// The part that is item `item`, or (by_seq) sequence `item`'s parts; false if there is none.  Every wave for itself.
-__device__ __forceinline__ bool share_of(const AttendArgs &a, const Shares &shares, int item, bool by_seq, Share &s) {
-    const int lane = threadIdx.x & 63, seqs = shares.num_seqs;
-    const bool tell = !by_seq && item == 0 && blockIdx.y == 0 && threadIdx.x < 64;
-    if (seqs > kShareSeqs) {
-        s = Share{item, 0, 1, INT32_MAX, item};
-        bool rows;
-        share_tokens(a, item, tell || (!by_seq && blockIdx.y == 0 && threadIdx.x == 0), rows);
-        return rows;
+__device__ __forceinline__ int sum_up_to_lane(int x) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int y = __shfl_up(x, o);
+        x += lane >= o ? y : 0;
     }
+    return x;
+}
+
+// Parts of sequence b at a length.
+__device__ __forceinline__ int share_parts(const AttendArgs &a, int b, int64_t len) {
+    bool rows;
+    const int tokens = share_tokens(a, b, false, rows);
+    return rows ? static_cast<int>(max((tokens + len - 1) / len, int64_t{1})) : 0;
+}
+
+// The shortest length of a part, up to a few percent, that makes no more parts than wanted.  `first` and `step`: this
+// lane's sequences; sum(x): x over all lanes.
+template <class Sum>
+__device__ __forceinline__ int64_t share_len(const AttendArgs &a, const Shares &shares, int first, int step, bool tell,
+                                             Sum &&sum) {
+    const auto round_len = [&](int64_t len) { return max((len + 31) / 32 * 32, int64_t{shares.shortest}); };
     int64_t total = 0;
-    for (int b = lane; b < seqs; b += 64) {
+    for (int b = first; b < shares.num_seqs; b += step) {
         bool rows;
         total += share_tokens(a, b, tell, rows);
     }
-    total = sum_of_wave(total);
-    // The shortest length, up to a few percent, that makes no more parts than the target.
-    const auto parts_of_seq = [&](int b, int64_t len) -> int {
-        bool rows;
-        const int tokens = share_tokens(a, b, false, rows);
-        return rows ? static_cast<int>(max((tokens + len - 1) / len, int64_t{1})) : 0;
-    };
-    const auto round_len = [](int64_t len) { return max((len + 31) / 32 * 32, int64_t{kShareLen}); };
-    int64_t len = round_len((total + shares.target - 1) / shares.target);
-    for (int tries = 0; tries < 4 && seqs > 1; ++tries) {
+    int64_t len = round_len((sum(total) + shares.target - 1) / shares.target);
+    for (int tries = 0; tries < 4 && shares.num_seqs > 1; ++tries) {
         int64_t parts = 0;
-        for (int b = lane; b < seqs; b += 64)
-            parts += parts_of_seq(b, len);
-        parts = sum_of_wave(parts);
-        if (parts <= max(shares.target, seqs))
+        for (int b = first; b < shares.num_seqs; b += step)
+            parts += share_parts(a, b, len);
+        parts = sum(parts);
+        if (parts <= max(int64_t{shares.target}, 2 * int64_t{shares.num_seqs}))
             break;
         len = round_len(len * parts / shares.target);
     }
-    int item0 = 0;
-    for (int b0 = 0; b0 < seqs; b0 += 64) {
-        const int mine = b0 + lane < seqs ? parts_of_seq(b0 + lane, len) : 0;
-        int upto = mine;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int y = __shfl_up(upto, o);
-            upto += lane >= o ? y : 0;
-        }
-        const int from = item0 + upto - mine;
-        const bool here = by_seq ? b0 + lane == item : item >= from && item < from + mine;
-        const uint64_t found = __ballot(here);
-        if (found) {
-            const int at = __builtin_ctzll(found);
-            s.b = b0 + at;
-            s.parts = __builtin_amdgcn_readlane(mine, at);
-            s.item0 = __builtin_amdgcn_readlane(from, at);
-            s.split = by_seq ? 0 : item - s.item0;
-            s.len = static_cast<int>(min(len, int64_t{INT32_MAX}));
-            return s.parts > 0;
-        }
-        item0 += __builtin_amdgcn_readlane(upto, 63);
+    return min(len, int64_t{INT32_MAX});
+}
+
+// The part that is item `item`, or (by_seq) sequence `item`'s parts; false if there is none.  Every wave for itself.
+__device__ __forceinline__ bool share_of(const AttendArgs &a, const Shares &shares, int item, bool by_seq, Share &s) {
+    if (shares.alone) {
+        s = Share{item, 0, 1, INT32_MAX, item};
+        bool rows;
+        share_tokens(a, item, !by_seq && blockIdx.y == 0 && threadIdx.x == 0, rows);
+        return rows;
     }
-    return false;
+    if (shares.items_of) {
+        const int32_t *seqs = shares.items_of + 2, *items = seqs + 2 * static_cast<int64_t>(shares.num_seqs);
+        s.b = by_seq ? item : items[2 * item];
+        if (s.b < 0)
+            return false;
+        s.split = by_seq ? 0 : items[2 * item + 1];
+        s.item0 = seqs[2 * s.b];
+        s.parts = seqs[2 * s.b + 1];
+        s.len = shares.items_of[0];
+        return s.parts > 0;
+    }
+    const int lane = threadIdx.x & 63;
+    const bool tell = !by_seq && item == 0 && blockIdx.y == 0 && threadIdx.x < 64;
+    const int64_t len = share_len(a, shares, lane, 64, tell, sum_of_wave);
+    const int mine = lane < shares.num_seqs ? share_parts(a, lane, len) : 0;
+    const int from = sum_up_to_lane(mine) - mine;
+    const uint64_t found = __ballot(by_seq ? lane == item : item >= from && item < from + mine);
+    if (!found)
+        return false;
+    s.b = __builtin_ctzll(found);
+    s.parts = __builtin_amdgcn_readlane(mine, s.b);
+    s.item0 = __builtin_amdgcn_readlane(from, s.b);
+    s.split = by_seq ? 0 : item - s.item0;
+    s.len = static_cast<int>(len);
+    return s.parts > 0;
 }
 
 __device__ __forceinline__ int parts_of(const Span &s, int len) {
@@ -228,6 +248,7 @@ __device__ __forceinline__ float small_capped(float x, float twice, float cap) {
 }
 
 // Each covers the sequences of its kind only, whatever else is in the batch.
+hipError_t launch_share(const AttendArgs &a, const Shares &shares, hipStream_t stream);
 hipError_t launch_step(const AttendArgs &a, const Shares &shares, int max_queries, hipStream_t stream);
 hipError_t launch_tail(const AttendArgs &a, const Parts &parts, int max_queries, hipStream_t stream);
 // Join what these left of rows in parts.

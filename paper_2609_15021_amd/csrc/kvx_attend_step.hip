@@ -421,6 +421,50 @@ __global__ __launch_bounds__(64 * kWaves, !FP8 && DP > 128 ? 1 : 2) void step_ke
     }
 }
 
+// The lists of Shares, by one workgroup.
+__global__ __launch_bounds__(1024) void share_kernel(const AttendArgs a, const Shares shares) {
+    __shared__ int64_t wave_sums[16];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const auto sum = [&](int64_t x) {
+        x = sum_of_wave(x);
+        __syncthreads();
+        if (lane == 0)
+            wave_sums[wave] = x;
+        __syncthreads();
+        x = 0;
+        for (int i = 0; i < 16; ++i)
+            x += wave_sums[i];
+        return x;
+    };
+    const int64_t len = share_len(a, shares, tid, 1024, true, sum);
+    int32_t *seqs = shares.items_of + 2, *items = seqs + 2 * static_cast<int64_t>(shares.num_seqs);
+    int base = 0;
+    for (int b0 = 0; b0 < shares.num_seqs; b0 += 1024) {
+        const int b = b0 + tid, mine = b < shares.num_seqs ? share_parts(a, b, len) : 0, upto = sum_up_to_lane(mine);
+        __syncthreads();
+        if (lane == 63)
+            wave_sums[wave] = upto;
+        __syncthreads();
+        int from = base + upto - mine;
+        for (int i = 0; i < 16; ++i) {
+            from += i < wave ? static_cast<int>(wave_sums[i]) : 0;
+            base += static_cast<int>(wave_sums[i]);
+        }
+        if (b < shares.num_seqs) {
+            seqs[2 * b] = from;
+            seqs[2 * b + 1] = mine;
+        }
+        for (int k = 0; k < mine; ++k) {
+            items[2 * (from + k)] = b;
+            items[2 * (from + k) + 1] = k;
+        }
+    }
+    for (int i = base + tid; i < shares.items; i += 1024)
+        items[2 * i] = -1;
+    if (tid == 0)
+        shares.items_of[0] = static_cast<int>(len);
+}
+
 // Where the parts of a row lie.
 struct Row {
     int64_t slot, stride;  // of its first part, and between parts
@@ -574,6 +618,10 @@ hipError_t launch_join(const AttendArgs &a, const From &from, int max_queries, h
 }
 
 }  // namespace
+
+hipError_t launch_share(const AttendArgs &a, const Shares &shares, hipStream_t stream) {
+    return launch_kernel(share_kernel, dim3(1), 1024, stream, a, shares);
+}
 
 hipError_t launch_step(const AttendArgs &a, const Shares &shares, int max_queries, hipStream_t stream) {
     const int max_rows = static_cast<int>(std::min<int64_t>(kStepRows, static_cast<int64_t>(max_queries) * a.group));
