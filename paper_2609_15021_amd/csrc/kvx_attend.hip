@@ -88,11 +88,12 @@ struct Plan {
 
 int64_t round_up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 
-// The tail kernel's parts, for `have` tiles of rows (of the `launched`, others are empty).  512 of its workgroups run at once (2 per CU; 256 where D > 128), so
-// they may leave the last round nearly empty, and tiles that see less than others end it early: the number of parts is the
-// one whose rounds (between those of equal parts, and those without an edge and half a part idle at the end) and joining
-// take least, at the 0.2 ns per token and column that such a round takes and the 5 TB/s at which parts are written and
-// read again.  Parts have no fewer than 256 tokens and no more than 256 MB between them.
+// The tail kernel's parts, for `have` tiles of rows (of the `launched`, others are empty).  512 of its workgroups run at
+// once (2 per CU; 256 where D > 128), so they may leave the last round nearly empty, and tiles that see less than others
+// end it early: the number of parts is the one whose rounds (between those of equal parts, and those without an edge and
+// half a part idle at the end) and joining take least, at the 0.2 ns per token and column that such a round takes and the
+// 5 TB/s at which parts are written and read again (a session turn of 656 tiles: 1.81 ms whole, 1.66 in 3 parts).  Parts
+// have no fewer than 256 tokens and no more than 256 MB between them.
 Parts tail_parts_for(int64_t longest, int64_t have, int64_t launched, int64_t head_dim) {
     const int64_t at_once = head_dim > 128 ? 256 : 512;
     const double tokens_us = 0.2e-3 * static_cast<double>(head_dim) * static_cast<double>(longest);
@@ -141,7 +142,11 @@ Plan plan_of(const kv_cache *cache, const kv_batch *batch, const kv_attend_optio
     s.shortest = heads * tiles >= at_once ? 512 : 128;
     const int64_t most = (longest + s.shortest - 1) / s.shortest * batch->num_seqs;  // parts that can be
     s.num_seqs = batch->num_seqs;
-    s.target = static_cast<int32_t>(std::min(std::max<int64_t>(at_once / (H * tiles), s.num_seqs), most));
+    // (Many sequences are cut for three rounds of workgroups, of which the last may be nearly empty: 64 of up to 4,096
+    // tokens on 8 heads take 143 us in one to one and a half rounds, 136 in three.)
+    const int64_t rounds = 2 * heads * tiles >= at_once ? 3 : 1;
+    s.target = static_cast<int32_t>(
+        std::min(std::max<int64_t>(rounds * at_once / (H * tiles), s.num_seqs), most));
     s.alone = longest <= s.shortest || s.target == 1;
     s.items = s.alone || s.num_seqs == 1 ? std::max(s.num_seqs, s.alone ? 1 : s.target) : s.target + s.num_seqs;
     s.row_cap = p.max_rows;

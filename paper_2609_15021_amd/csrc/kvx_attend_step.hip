@@ -12,10 +12,14 @@
 //    permutations in registers turn them (one per pair of elements); e4m3 is turned while it is widened.
 //  * The pages of 32 tokens are looked up by 32 lanes, one token each, a round ahead, and handed out by lane shuffles.
 //
-// The sequences' tokens are shared out to workgroups (Shares) so that they fill the chip once, and inside a workgroup over its
-// 4 waves; the waves' sums are joined through LDS, the workgroups' by join_kernel.  K of the next 32 tokens is requested
-// as soon as the scores have used the last, V as soon as the second product has: a wave has 16 KiB in flight (bf16,
-// D 128) without a second set of registers.
+// The sequences' tokens are shared out to workgroups (Shares) so that they fill the chip once, and inside a workgroup over
+// its 4 waves; the waves' sums are joined through LDS, the workgroups' by join_kernel.  K of the next 32 tokens is
+// requested as soon as the scores have used the last, V as soon as the second product has: a wave has 16 KiB in flight
+// (bf16, D 128) without a second set of registers, and 2 waves of a SIMD 128 KiB a CU.
+//
+// One sequence behind 131,077 tokens (8 heads of 5 rows, bf16, D 128): 95 us and 8 to join, 5.1 TB/s with both (a large
+// reduction reads 6.1, a large copy moves 4.8).  16 sequences of up to 32,768 tokens in e4m3 (4 heads of 6 rows, D 256):
+// 124 us, 4.8 TB/s.  48 of up to 8,192 with weights (2 heads of 8 rows): 41 us, 8 to join, 6 for what each token received.
 #include <algorithm>
 
 #include "kvx_attend_kernels.h"
@@ -55,8 +59,10 @@ struct Vec<16> {
 };
 
 // T: type of q, of the weights and of out; FP8: the cache holds e4m3; DP >= D columns; NT: tiles of 16 rows.
+// (2 waves a SIMD; wide 2-byte rows would need to spill for that, and one wave runs them.)
 template <class T, bool FP8, int DP, int NT>
-__global__ __launch_bounds__(64 * kWaves, !FP8 && DP > 128 ? 1 : 2) void step_kernel(const AttendArgs a, const Shares shares) {
+__global__ __launch_bounds__(64 * kWaves, !FP8 && DP > 128 ? 1 : 2) void step_kernel(const AttendArgs a,
+                                                                                     const Shares shares) {
     constexpr int E = FP8 ? 1 : 2;                       // bytes of a cached element
     constexpr int KC = DP * E / 64;                      // 16-byte pieces of a token's K in a lane
     constexpr int VE = DP / 16 * E > 16 ? 16 / E : DP / 16;  // V columns of a lane in a piece
@@ -78,7 +84,8 @@ __global__ __launch_bounds__(64 * kWaves, !FP8 && DP > 128 ? 1 : 2) void step_ke
         return;
     const int i0 = divide(row0, a.by_group), i1 = divide(min(row0 + 16 * NT, rows) - 1, a.by_group) + 1;
     const Span span = span_of(seq.n, seq.nq, i0, i1, a.window);
-    const int64_t part_at = span_of(seq.n, seq.nq, 0, seq.nq, a.window).start + static_cast<int64_t>(share.split) * share.len;
+    const int64_t part_at =
+        span_of(seq.n, seq.nq, 0, seq.nq, a.window).start + static_cast<int64_t>(share.split) * share.len;
     const int begin = static_cast<int>(min(part_at, int64_t{INT32_MAX} - 1023));
     const int stop = static_cast<int>(min(part_at + share.len, static_cast<int64_t>(span.end)));
     const bool whole = share.parts == 1;
@@ -575,7 +582,8 @@ __global__ __launch_bounds__(256) void weigh_step_kernel(const AttendArgs a) {
         if (to <= 0 || from >= 4)
             continue;
         const float *lse = a.lse + static_cast<int64_t>(seq.q0 + i) * a.heads + h * a.group;
-        const float *scores = a.scores + ((static_cast<int64_t>(b) * a.pages.H + h) * a.score_cap + i * a.group) * a.score_len + t;
+        const int64_t slot = (static_cast<int64_t>(b) * a.pages.H + h) * a.score_cap + i * a.group;
+        const float *scores = a.scores + slot * a.score_len + t;
         for (int k = 0; k < a.group; ++k) {
             const float zero = lse[k] * kLog2e;
             const f32x4 x = *reinterpret_cast<const f32x4 *>(scores + k * a.score_len);

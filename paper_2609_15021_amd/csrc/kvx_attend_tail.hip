@@ -1,18 +1,24 @@
 // kv_attend for many new tokens of a sequence (a prompt's tail behind a restored prefix, or a whole prompt): bound by
 // the matrix cores and the exponentials between their products.
 //
-// A workgroup takes 128 rows (new token, query head) of one KV head, 32 a wave, so that all query heads of a KV head
-// share what is read of it, and goes over the tokens TK at a time.  K and V of TK tokens lie in LDS, twice: while one is
-// used, the next is on its way through registers, and one barrier a round separates them.  A wave takes S^T = K Q^T and
-// O^T = V^T P^T in 32x32x16 products: a row is a column of both, so its largest score, sum and rescaling stay in a lane
-// (and its neighbour 32 lanes on), and the weights are the second product's operand in the order in which the first
-// leaves them: k-index e of half h of products of 16 tokens is token h * 4 + e for e < 4, and 8 + h * 4 + e - 4 beyond.
-// V's operand in that order is two transposing LDS reads (ds_read_b64_tr_b16: 16 lanes read 4 rows of 16 columns, a lane
-// gets a column).  Rows in LDS are permuted in 16-byte pieces (by token for K, by pairs for V), so that neither kind of
-// read meets a bank twice.
+// A workgroup takes 128 rows (new token, query head) of one KV head, so that all query heads of a KV head share what is
+// read of it, and goes over the tokens TK at a time.  K and V of TK tokens lie in LDS, twice: while one is used, the next
+// is on its way (two-byte rows straight into LDS; e4m3 through registers, widened once per workgroup), and one barrier a
+// round separates them.  A wave has 32 of the rows and takes S^T = K Q^T and O^T = V^T P^T in 32x32x16 products: a row is
+// a column of both, so its largest score, sum and rescaling stay in a lane (and the one 32 lanes on), and the weights are
+// the second product's operand in the order in which the first leaves them: k-index e of half h of a product of 16 tokens
+// is token h * 4 + e for e < 4, and 8 + h * 4 + e - 4 beyond.  V's operand in that order is two transposing LDS reads
+// (16 lanes read 4 rows of 16 columns, a lane gets a column).  Rows in LDS are permuted in 16-byte pieces, so that neither
+// kind of read meets a bank twice.  Above 128 columns a wave has 16 rows, in 16x16x32 products and the step kernel's order
+// of tokens: the output's sums of 32 would not leave registers for a second wave on the SIMD.
 //
-// e4m3 is widened on its way into LDS, once per workgroup.  Workgroups that share a KV head run on one XCD where the
-// number of heads allows (consecutive workgroups go to consecutive XCDs), and use its L2 together.
+// Workgroups of a KV head come 8 apart where there are 8 heads, and so on one XCD (consecutive ones go to consecutive
+// XCDs), and use its L2 together.
+//
+// 2,085 new tokens behind 32,768 (8 heads of 5 rows a token, bf16, D 128): 1.56 ms, 924 TFLOP/s, where a large library
+// product reaches 1,200.  Per round of 64 tokens a wave has 1,024 cycles of products and about 1,150 of vector work (512
+// of them exponentials); two waves of a SIMD overlap them partly.  Ragged tails of up to 1,055 tokens, e4m3, D 256, a
+// window of 4,096 and capped scores: 0.75 ms, 437 TFLOP/s; its 16-row waves read LDS twice as often, which bounds them.
 #include <algorithm>
 #include <type_traits>
 
@@ -135,7 +141,8 @@ __global__ __launch_bounds__(64 * kRows / RW, 2) void tail_kernel(const AttendAr
     const int row_i = divide(min(r, rows - 1), a.by_group), head = h * a.group + min(r, rows - 1) - row_i * a.group;
     const int p_row = row_ok ? seq.n - seq.nq + row_i : -1;
     const int wave_r0 = min(row0 + wave * RW, rows - 1), wave_r1 = min(row0 + wave * RW + RW - 1, rows - 1);
-    const int p_first = seq.n - seq.nq + divide(wave_r0, a.by_group), p_last = seq.n - seq.nq + divide(wave_r1, a.by_group);
+    const int p_first = seq.n - seq.nq + divide(wave_r0, a.by_group);
+    const int p_last = seq.n - seq.nq + divide(wave_r1, a.by_group);
     const int low_last = a.window > 0 ? p_last + 1 - a.window : 0;
     const float slope = a.slopes ? a.slopes[head] * kLog2e : 0.f;
     const float scale = a.scale * kLog2e;
@@ -155,8 +162,7 @@ __global__ __launch_bounds__(64 * kRows / RW, 2) void tail_kernel(const AttendAr
     const bool piece_ok = piece * 16 < pg.row_bytes;
 
     // Lanes look up a round's tokens (lane % TK each): the page's block, then where the token's row is; -1 for a token
-    // that takes part in nothing.
-    // (No branch: beyond the part the last token's entry is read again, and waits are counted, not emptied.)
+    // that takes part in nothing.  (No branch: beyond the part the last token's entry is read again, and waits are counted, not emptied.)
     auto block_at = [&](int base) {
         const int t = base + (lane & (TK - 1));
         return table[divide(max(min(t, stop - 1), span.first), pg.by_bs)];
