@@ -18,7 +18,7 @@
 // 2,085 new tokens behind 32,768 (8 heads of 5 rows a token, bf16, D 128): 1.56 ms, 924 TFLOP/s, where a large library
 // product reaches 1,200.  Per round of 64 tokens a wave has 1,024 cycles of products and about 1,150 of vector work (512
 // of them exponentials); two waves of a SIMD overlap them partly.  Ragged tails of up to 1,055 tokens, e4m3, D 256, a
-// window of 4,096 and capped scores: 0.75 ms, 437 TFLOP/s; its 16-row waves read LDS twice as often, which bounds them.
+// window of 4,096 and capped scores: 0.69 ms, 472 TFLOP/s; its 16-row waves read LDS twice as often, which bounds them.
 #include <algorithm>
 #include <type_traits>
 
@@ -177,7 +177,31 @@ __global__ __launch_bounds__(64 * kRows / RW, 2) void tail_kernel(const AttendAr
     // lanes do, so a lane fetches the piece that the permutation wants in its place), e4m3 into registers.  Slots without
     // a token and columns beyond D may hold anything, and 0 times it need not be 0: they become zeros.
     u32x4 next[2][FP8 ? NP : 1];
+    // Of e4m3 rows a wave's WR rows of one load lie in one page where pages hold multiples of them (rounds begin at
+    // multiples of 32).  If all of the round's tokens take part, the first row's address is the wave's, and the lanes'
+    // distances from it are the same every round: 0.69 ms instead of 0.74 for the ragged tails above.  2-byte rows do not
+    // gain (1.57 to 1.60 ms instead of 1.56): their pieces are permuted as well.
+    constexpr int WR = 64 / GC;  // rows of a wave in one load
+    const bool together = FP8 && pg.BS % WR == 0 && pg.D == DP;
+    const uint32_t lane_row = static_cast<uint32_t>(lane / GC) * pg.token_bytes;
     auto request = [&](int64_t off, int buffer) {
+        const bool all = __all(off >= 0);
+        if constexpr (FP8) {
+            if (together && all) {
+#pragma unroll
+                for (int n = 0; n < NP; ++n) {
+                    const int first = n * RP + wave * WR;
+                    const uint32_t lo = __builtin_amdgcn_readlane(static_cast<int>(off), first);
+                    const uint32_t hi = __builtin_amdgcn_readlane(static_cast<int>(off >> 32), first);
+                    const uint8_t *row = cache + static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo);
+#pragma unroll
+                    for (int kv = 0; kv < 2; ++kv)
+                        next[kv][n] = *reinterpret_cast<const u32x4 *>((kv ? row + pg.v_bytes : row) +
+                                                                         (lane_row + piece * 16));
+                }
+                return;
+            }
+        }
         int64_t at[NP];
 #pragma unroll
         for (int n = 0; n < NP; ++n) {
@@ -210,7 +234,7 @@ __global__ __launch_bounds__(64 * kRows / RW, 2) void tail_kernel(const AttendAr
                     }
                 }
             };
-            if (pg.D == DP && __all(off >= 0))
+            if (pg.D == DP && all)
                 fetch(std::true_type{});
             else
                 fetch(std::false_type{});
