@@ -504,17 +504,28 @@ __global__ __launch_bounds__(256) void join_kernel(const AttendArgs a, const Fro
     const int lanes = D / 4, groups = 256 / lanes, mine = tid / lanes, d = (tid - mine * lanes) * 4;
     const int i = SPREAD ? blockIdx.x : blockIdx.x * groups + mine;
     Sequence seq;
-    if (!sequence(a.batch, b, a.pages.err, seq))
+    if (!sequence(a.batch, b, a.pages.err, seq) || (SPREAD && i >= seq.nq))
         return;
     // (All lanes look the parts up together; the lanes of a row that is none then leave.)
     const Row row_at = parts_at(a, from, b, h, min(i, max(seq.nq - 1, 0)) * a.group + head - h * a.group, seq);
     const int parts = row_at.parts;
     const bool row = i < seq.nq && mine < groups;
-    if (parts <= 1 || (SPREAD ? i >= seq.nq : !row))
+    if (parts <= 1 || (!SPREAD && !row))
         return;
     const float *stats = from.stats + row_at.slot * 2;
     const int64_t step = row_at.stride;
     float most = kLowest, total = 0.f;
+    // (SPREAD: the first parts' sums are on their way while the row's largest score is looked for.)
+    constexpr int EARLY = SPREAD ? 8 : 0;
+    f32x4 early[SPREAD ? EARLY : 1];
+    float early_most[SPREAD ? EARLY : 1];
+#pragma unroll
+    for (int k = 0; k < EARLY; ++k) {
+        const int s = mine + k * groups;
+        const bool is = row && s < parts;
+        early[k] = is ? *reinterpret_cast<const f32x4 *>(from.sums + (row_at.slot + s * step) * D + d) : f32x4{0.f, 0.f, 0.f, 0.f};
+        early_most[k] = is ? stats[2 * s * step] : kLowest;
+    }
     if constexpr (SPREAD) {  // every wave for itself
         const int lane = tid & 63;
         for (int s = lane; s < parts; s += 64)
@@ -532,8 +543,11 @@ __global__ __launch_bounds__(256) void join_kernel(const AttendArgs a, const Fro
             total += stats[2 * s * step + 1] * __builtin_amdgcn_exp2f(stats[2 * s * step] - most);
     }
     f32x4 x{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < EARLY; ++k)
+        x += early[k] * __builtin_amdgcn_exp2f(early_most[k] - most);
     if (row)
-        for (int s = SPREAD ? mine : 0; s < parts; s += SPREAD ? groups : 1)
+        for (int s = SPREAD ? mine + EARLY * groups : 0; s < parts; s += SPREAD ? groups : 1)
             x += *reinterpret_cast<const f32x4 *>(from.sums + (row_at.slot + s * step) * D + d) *
                  __builtin_amdgcn_exp2f(stats[2 * s * step] - most);
     if constexpr (SPREAD) {
@@ -640,7 +654,7 @@ hipError_t launch_step(const AttendArgs &a, const Shares &shares, int max_querie
 }
 
 hipError_t launch_join_step(const AttendArgs &a, const Shares &shares, int max_queries, hipStream_t stream) {
-    return launch_join<true>(a, shares, std::min(max_queries, kStepRows), stream);
+    return launch_join<true>(a, shares, std::min(max_queries, std::max(kStepRows / a.group, 1)), stream);
 }
 
 hipError_t launch_join_tail(const AttendArgs &a, const Parts &parts, int max_queries, hipStream_t stream) {
