@@ -515,13 +515,14 @@ __global__ __launch_bounds__(256) void join_kernel(const AttendArgs a, const Fro
     const float *stats = from.stats + row_at.slot * 2;
     const int64_t step = row_at.stride;
     float most = kLowest, total = 0.f;
-    // (SPREAD: the first parts' sums are on their way while the row's largest score is looked for.)
-    constexpr int EARLY = SPREAD ? 8 : 0;
-    f32x4 early[SPREAD ? EARLY : 1];
-    float early_most[SPREAD ? EARLY : 1];
+    // (The first parts' sums are on their way while the row's largest score is looked for.)
+    constexpr int EARLY = SPREAD ? 8 : 4;
+    const int s0 = SPREAD ? mine : 0, ds = SPREAD ? groups : 1;
+    f32x4 early[EARLY];
+    float early_most[EARLY];
 #pragma unroll
     for (int k = 0; k < EARLY; ++k) {
-        const int s = mine + k * groups;
+        const int s = s0 + k * ds;
         const bool is = row && s < parts;
         early[k] = is ? *reinterpret_cast<const f32x4 *>(from.sums + (row_at.slot + s * step) * D + d) : f32x4{0.f, 0.f, 0.f, 0.f};
         early_most[k] = is ? stats[2 * s * step] : kLowest;
@@ -547,7 +548,7 @@ __global__ __launch_bounds__(256) void join_kernel(const AttendArgs a, const Fro
     for (int k = 0; k < EARLY; ++k)
         x += early[k] * __builtin_amdgcn_exp2f(early_most[k] - most);
     if (row)
-        for (int s = SPREAD ? mine + EARLY * groups : 0; s < parts; s += SPREAD ? groups : 1)
+        for (int s = s0 + EARLY * ds; s < parts; s += ds)
             x += *reinterpret_cast<const f32x4 *>(from.sums + (row_at.slot + s * step) * D + d) *
                  __builtin_amdgcn_exp2f(stats[2 * s * step] - most);
     if constexpr (SPREAD) {
