@@ -8,8 +8,9 @@
 //
 // One workgroup does all of that for a row whose 8,192 tokens fit its registers, and for longer rows where there are
 // enough of them to fill the chip; it is bound by its own instructions (15 us for 8,192 tokens, 148 for 131,077).  A few
-// long rows are cut into pieces of 8,192 tokens instead, a workgroup each, in six launches: clear the counters, a digit
-// each, count, write.
+// long rows are cut into pieces of 8,192 tokens instead, a workgroup each, in five launches: clear the counters, a digit
+// each, write (29 us for 131,077 tokens).  (For every value that the last digit may have a piece leaves how many of its tokens are above it, so
+// that the pieces behind it know where they begin to write without counting again.)
 #include <algorithm>
 
 #include "kvx_paged.h"
@@ -30,7 +31,8 @@ struct KeepArgs {
     int32_t *err;
     int32_t pieces;                   // of a row; 1: rows are not cut
     int32_t *digit_counts;            // [row][3][kBins]
-    int32_t *piece_counts;            // [row][pieces][2]: chosen outright, and ties
+    int32_t *states;                  // [row][2][2]: the threshold's first digits, and the tokens still to find
+    int32_t *piece_counts;            // [row][pieces][kPieceCounts]: tokens with keys above each of the last digit's values
 };
 
 // Orders as the weights do; both zeros alike, every NaN 0 (below -infinity).
@@ -86,8 +88,12 @@ __device__ __forceinline__ void find_digit(Count &&count, int left, int (&wave_s
     __syncthreads();
 }
 
-constexpr int kWhole = -1, kCount = 3, kWrite = 4;  // steps; 0 to 2: digits
+constexpr int kWhole = -1, kWrite = 3;  // steps; 0 to 2: digits
 constexpr int kPiece = 2 * kRound;
+constexpr int kLastBins = 1024, kPieceCounts = kLastBins + 1;
+
+constexpr int shift_of(int digit) { return digit == 0 ? 21 : digit == 1 ? 10 : 0; }
+constexpr uint32_t mask_of(int digit) { return digit < 2 ? kBins - 1 : kLastBins - 1; }
 
 // ROUNDS: keys of so many rounds stay in registers; 0: none.  STEP: everything of a row, or one step of a piece of it.
 template <int ROUNDS, int STEP>
@@ -189,34 +195,23 @@ __global__ __launch_bounds__(kKeepThreads) void keep_kernel(const KeepArgs a) {
     };
 
     const int middle = last - first;
+    const auto inside = [&](int t) { return static_cast<uint32_t>(t - first) < static_cast<uint32_t>(middle); };
     int *mine = counts[wave & (kCopies - 1)];
     uint32_t threshold = 0, known = 0;  // the digits found so far, and their mask
     const bool any = left > 0;
-    int32_t *digit_counts = a.digit_counts + row * 3 * kBins;
-    for (int digit = 0; any && digit < 3; ++digit) {
-        const int shift = digit == 0 ? 21 : digit == 1 ? 10 : 0;
-        const uint32_t mask = digit < 2 ? kBins - 1 : 1023;
-        if (STEP != kWhole && digit < STEP) {
-            find_digit([&](int value) { return digit_counts[digit * kBins + value]; }, left, wave_sums, found);
-            threshold |= static_cast<uint32_t>(found[0]) << shift;
-            known |= mask << shift;
-            left -= found[1];
-            __syncthreads();
-            continue;
-        }
-        if (STEP != kWhole && digit > STEP)
-            return;
+    // Counts the values of a digit among the tokens whose digits before it are the threshold's.
+    const auto count_digit = [&](int digit) {
         for (int j = tid; j < kCopies * kBins; j += kKeepThreads)
             counts[0][j] = 0;
         __syncthreads();
         each([&](int, int t, const Keys &x) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                if (static_cast<uint32_t>(t + j - first) >= static_cast<uint32_t>(middle) ||
-                    ((x.k[j] ^ threshold) & known) != 0)
+                if (!inside(t + j) || ((x.k[j] ^ threshold) & known) != 0)
                     continue;
                 // (One counter for a whole wave, as among equal weights, is raised once.)
-                const int bin = static_cast<int>(x.k[j] >> shift & mask), one = __builtin_amdgcn_readfirstlane(bin);
+                const int bin = static_cast<int>(x.k[j] >> shift_of(digit) & mask_of(digit));
+                const int one = __builtin_amdgcn_readfirstlane(bin);
                 const uint64_t lanes = __ballot(true);
                 if (__ballot(bin == one) != lanes)
                     atomicAdd(&mine[bin], 1);
@@ -225,48 +220,95 @@ __global__ __launch_bounds__(kKeepThreads) void keep_kernel(const KeepArgs a) {
             }
         });
         __syncthreads();
-        const auto sum = [&](int value) {
-            int c = 0;
+    };
+    const auto counted = [&](int value) {
+        int c = 0;
 #pragma unroll
-            for (int j = 0; j < kCopies; ++j)
-                c += counts[j][value];
-            return c;
-        };
-        if (STEP != kWhole) {
-            for (int value = tid; value < kBins; value += kKeepThreads) {
-                const int c = sum(value);
-                if (c > 0)
-                    atomicAdd(&digit_counts[digit * kBins + value], c);
-            }
-            return;
-        }
-        find_digit(sum, left, wave_sums, found);
-        threshold |= static_cast<uint32_t>(found[0]) << shift;
-        known |= mask << shift;
+        for (int j = 0; j < kCopies; ++j)
+            c += counts[j][value];
+        return c;
+    };
+    // Adds a digit to the threshold.
+    const auto find = [&](int digit, auto &&count) {
+        find_digit(count, left, wave_sums, found);
+        threshold |= static_cast<uint32_t>(found[0]) << shift_of(digit);
+        known |= mask_of(digit) << shift_of(digit);
         left -= found[1];
+    };
+    int32_t *digit_counts = a.digit_counts + row * 3 * kBins, *states = a.states + row * 4;
+    int32_t *piece_counts = a.piece_counts + (row * a.pieces + piece) * kPieceCounts;
+    if constexpr (STEP == kWhole) {
+        for (int digit = 0; any && digit < 3; ++digit) {
+            count_digit(digit);
+            find(digit, counted);
+        }
+    } else if (any && STEP > 0) {
+        if constexpr (STEP > 1) {
+            threshold = static_cast<uint32_t>(states[2 * (STEP - 2)]);
+            left = states[2 * (STEP - 2) + 1];
+            known = ~0u << shift_of(STEP - 2);
+        }
+        find(STEP - 1, [&](int value) { return digit_counts[(STEP - 1) * kBins + value]; });
+        if (STEP < kWrite && piece == 0 && tid == 0) {
+            states[2 * (STEP - 1)] = static_cast<int32_t>(threshold);
+            states[2 * (STEP - 1) + 1] = left;
+        }
     }
-    if constexpr (STEP != kWhole && STEP < kCount)
+    if constexpr (STEP >= 0 && STEP < kWrite) {
+        if (!any)
+            return;
+        count_digit(STEP);
+        for (int value = tid; value <= static_cast<int>(mask_of(STEP)); value += kKeepThreads) {
+            const int c = counted(value);
+            if (c > 0)
+                atomicAdd(&digit_counts[STEP * kBins + value], c);
+        }
+        if constexpr (STEP == 2) {
+            // What the pieces behind this one will want to know of it, whatever the last digit turns out to be: the
+            // tokens with keys above (the threshold's first digits, value - 1), for each value and one more.
+            int above = 0, all;
+            each([&](int, int t, const Keys &x) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    above += inside(t + j) && (x.k[j] & known) > threshold;
+            });
+            for (int o = 32; o; o >>= 1)
+                above += __shfl_xor(above, o);
+            const int value = kLastBins - 1 - tid, c = counted(value), higher = before_in_wave(c, lane, all);
+            if (lane == 0)
+                wave_sums[wave] = all + (above << 16);
+            __syncthreads();
+            int sum = higher + c, above_all = 0;
+            for (int i = 0; i < kKeepWaves; ++i) {
+                sum += i < wave ? wave_sums[i] & 0xffff : 0;
+                above_all += wave_sums[i] >> 16;
+            }
+            piece_counts[value] = above_all + sum;
+            if (tid == 0)
+                piece_counts[kLastBins] = above_all;
+        }
         return;
+    }
 
     // Chosen: every token outside [first, last), keys above the threshold, and the first `left` ties.
     const auto state_of = [&](int t, uint32_t key, bool &sure, bool &tie) {
-        const bool inside = static_cast<uint32_t>(t - first) < static_cast<uint32_t>(middle);
-        sure = t < n && (!inside || (any && key > threshold));
-        tie = any && inside && key == threshold;
+        const bool is_inside = inside(t);
+        sure = t < n && (!is_inside || (any && key > threshold));
+        tie = any && is_inside && key == threshold;
     };
     int sure_done = 0, ties_done = 0;  // in the rounds before this set of kMaxRounds
-    int32_t *piece_counts = a.piece_counts + row * a.pieces * 2;
-    if constexpr (STEP == kWrite) {
+    if constexpr (STEP == kWrite) {  // in the pieces before this one
         int s = 0, q = 0;
-        for (int i = lane; i < piece; i += 64) {
-            s += piece_counts[2 * i];
-            q += piece_counts[2 * i + 1];
+        for (int i = lane; any && i < piece; i += 64) {
+            const int32_t *of = piece_counts + (i - piece) * kPieceCounts + (threshold & mask_of(2));
+            s += of[1];
+            q += of[0] - of[1];
         }
         for (int o = 32; o; o >>= 1) {
             s += __shfl_xor(s, o);
             q += __shfl_xor(q, o);
         }
-        sure_done = s;
+        sure_done = s + min(origin, first) + max(origin - last, 0);
         ties_done = q;
     }
     for (int set = 0; set < rounds; set += kMaxRounds) {
@@ -310,13 +352,6 @@ __global__ __launch_bounds__(kKeepThreads) void keep_kernel(const KeepArgs a) {
         if (tid < entries) {
             of_wave[tid][0] = s_before + sure_done;
             of_wave[tid][1] = q_before + ties_done;
-        }
-        if constexpr (STEP == kCount) {
-            if (tid == 0) {
-                piece_counts[2 * piece] = s_set;
-                piece_counts[2 * piece + 1] = q_set;
-            }
-            return;
         }
         sure_done += s_set;
         ties_done += q_set;
@@ -368,7 +403,7 @@ int pieces_of(int32_t num_seqs, int32_t heads, int32_t max_len, int32_t budget) 
 }
 
 int64_t workspace_bytes_of(int32_t num_seqs, int32_t heads, int32_t pieces) {
-    return pieces == 1 ? 0 : static_cast<int64_t>(num_seqs) * heads * (3 * kBins + 2 * int64_t{pieces}) * 4;
+    return pieces == 1 ? 0 : static_cast<int64_t>(num_seqs) * heads * (3 * kBins + 4 + int64_t{kPieceCounts} * pieces) * 4;
 }
 
 kv_status check_keep(int32_t num_seqs, int32_t heads, int32_t max_len, int32_t budget, int32_t sinks, int32_t recent) {
@@ -409,9 +444,10 @@ kv_status keep(const float *weights, int64_t seq_stride, int64_t head_stride, co
     if (st != KV_OK)
         return st;
     int32_t *digits = static_cast<int32_t *>(workspace);
-    const int64_t digit_words = static_cast<int64_t>(num_seqs) * heads * 3 * kBins;
+    const int64_t rows = static_cast<int64_t>(num_seqs) * heads, digit_words = rows * 3 * kBins;
+    int32_t *states = need > 0 ? digits + digit_words : nullptr;
     const KeepArgs a{weights, seq_stride, head_stride, lens, heads, max_len, budget, sinks, recent, keep, kept_lens,
-                     kept_weights, err, pieces, digits, need > 0 ? digits + digit_words : nullptr};
+                     kept_weights, err, pieces, digits, states, states ? states + rows * 4 : nullptr};
     const dim3 grid(static_cast<uint32_t>(heads), static_cast<uint32_t>(num_seqs), static_cast<uint32_t>(pieces));
     const auto launch = [&](void (*kernel)(KeepArgs)) { return launch_kernel(kernel, grid, kKeepThreads, stream, a); };
     if (pieces > 1) {
@@ -420,7 +456,6 @@ kv_status keep(const float *weights, int64_t seq_stride, int64_t head_stride, co
         KVX_HIP(launch(keep_kernel<2, 0>));
         KVX_HIP(launch(keep_kernel<2, 1>));
         KVX_HIP(launch(keep_kernel<2, 2>));
-        KVX_HIP(launch(keep_kernel<2, kCount>));
         KVX_HIP(launch(keep_kernel<2, kWrite>));
     } else {
         KVX_HIP(launch(max_len <= 2 * kRound ? keep_kernel<2, kWhole> : keep_kernel<0, kWhole>));
