@@ -448,6 +448,24 @@ def test_keep_many_rows_and_pieces(seqs, heads, longest):
     assert np.array_equal(got[2].cpu().numpy(), want[2])
 
 
+@pytest.mark.parametrize("budget,sinks,recent", [(9000, 9000, 0), (9000, 0, 9000), (9000, 100, 8900), (9000, 8999, 0),
+                                                 (9000, 8192, 100), (16384, 1, 8192)])
+def test_keep_pieces(budget, sinks, recent):
+    """Rows cut into pieces: nothing left to choose, first and last tokens that end at or inside a piece, NaN, infinities
+    and ties in all of them, and lengths that leave pieces without a token."""
+    L, H = 40000, 2
+    lens = [40000, 32768, 16385, 9001, 9000, 0]
+    w = torch.randn(len(lens), H, L, generator=torch.Generator().manual_seed(sinks))
+    w[:, 1] = w[:, 1].round()
+    w[1::2, :, ::7] = float("nan")
+    w[:, :, 3::5001] = float("inf")
+    w[:, :, 5::4001] = float("-inf")
+    got = attend.kv_keep(w.to(DEV), torch.tensor(lens, dtype=torch.int32, device=DEV), budget, sinks=sinks, recent=recent)
+    want = ref.keep(w.numpy(), lens, budget, sinks, recent)
+    assert torch.equal(got[0].cpu(), torch.from_numpy(want[0])) and got[1].cpu().tolist() == want[1].tolist()
+    assert np.array_equal(got[2].cpu().numpy(), want[2], equal_nan=True)
+
+
 def test_keep_refuses_lengths_on_the_device():
     w = torch.rand(3, 1, 50, device=DEV)
     keep, kept, _ = attend.kv_keep(w, torch.tensor([51, 20, -1], dtype=torch.int32, device=DEV), 8)
