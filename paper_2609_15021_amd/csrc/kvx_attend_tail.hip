@@ -15,10 +15,10 @@
 // Workgroups of a KV head come 8 apart where there are 8 heads, and so on one XCD (consecutive ones go to consecutive
 // XCDs), and use its L2 together.
 //
-// 2,085 new tokens behind 32,768 (8 heads of 5 rows a token, bf16, D 128): 1.56 ms, 924 TFLOP/s, where a large library
-// product reaches 1,200.  Per round of 64 tokens a wave has 1,024 cycles of products and about 1,150 of vector work (512
+// 2,085 new tokens behind 32,768 (8 heads of 5 rows a token, bf16, D 128): 1.51 to 1.61 ms by machine, 900 to 955 TFLOP/s,
+// where a large library product reaches 1,200.  Per round of 64 tokens a wave has 1,024 cycles of products and about 1,150 of vector work (512
 // of them exponentials); two waves of a SIMD overlap them partly.  Ragged tails of up to 1,055 tokens, e4m3, D 256, a
-// window of 4,096 and capped scores: 0.69 ms, 472 TFLOP/s; its 16-row waves read LDS twice as often, which bounds them.
+// window of 4,096 and capped scores: 0.68 ms, 483 TFLOP/s; its 16-row waves read LDS twice as often, which bounds them.
 #include <algorithm>
 #include <type_traits>
 
@@ -162,7 +162,8 @@ __global__ __launch_bounds__(64 * kRows / RW, 2) void tail_kernel(const AttendAr
     const bool piece_ok = piece * 16 < pg.row_bytes;
 
     // Lanes look up a round's tokens (lane % TK each): the page's block, then where the token's row is; -1 for a token
-    // that takes part in nothing.  (No branch: beyond the part the last token's entry is read again, and waits are counted, not emptied.)
+    // that takes part in nothing.  (No branch: beyond the part the last token's entry is read again, and waits are
+    // counted, not emptied.)
     auto block_at = [&](int base) {
         const int t = base + (lane & (TK - 1));
         return table[divide(max(min(t, stop - 1), span.first), pg.by_bs)];
