@@ -18,7 +18,7 @@
 // 2,085 new tokens behind 32,768 (8 heads of 5 rows a token, bf16, D 128): 1.51 to 1.61 ms by machine, 900 to 955 TFLOP/s,
 // where a large library product reaches 1,200.  Per round of 64 tokens a wave has 1,024 cycles of products and about 1,150 of vector work (512
 // of them exponentials); two waves of a SIMD overlap them partly.  Ragged tails of up to 1,055 tokens, e4m3, D 256, a
-// window of 4,096 and capped scores: 0.68 ms, 483 TFLOP/s; its 16-row waves read LDS twice as often, which bounds them.
+// window of 4,096 and capped scores: 0.665 ms, 490 TFLOP/s; its 16-row waves read LDS twice as often, which bounds them.
 #include <algorithm>
 #include <type_traits>
 
@@ -278,8 +278,7 @@ __global__ __launch_bounds__(64 * kRows / RW, 2) void tail_kernel(const AttendAr
     int k_at = k_row * ROW + (part ^ k_permute(k_row)) * 16;
     int v_at = v_row * ROW + (v_piece ^ v_permute(v_row)) * 16 + (lane & 1) * 8;
 
-    float s[TB][NS];
-    auto take_scores = [&](int buffer) {
+    auto take_scores = [&](int buffer, float (&s)[TB][NS]) {
         const uint8_t *k_lds = lds[0][buffer];
         constexpr int SETS_K = WIDE ? 1 : 2;  // products side by side of 32 tokens
 #pragma unroll
@@ -328,7 +327,8 @@ __global__ __launch_bounds__(64 * kRows / RW, 2) void tail_kernel(const AttendAr
             asm volatile("" : "+v"(k_at), "+v"(v_at));
             // (The products go first: the other wave of the SIMD has its exponentials for the time between them.)
             __builtin_amdgcn_s_setprio(1);
-            take_scores(buffer);
+            float s[TB][NS];
+            take_scores(buffer, s);
             __builtin_amdgcn_s_setprio(0);
             const bool edge = usable != ~uint64_t{0} || p_first - base < TK - 1 || base < low_last;
             // Scores in powers of 2; in the plain case the factor is left to the exponent's argument.
@@ -397,6 +397,11 @@ __global__ __launch_bounds__(64 * kRows / RW, 2) void tail_kernel(const AttendAr
                     p[t][x >> 3][x >> 1 & 3] = T::pack(e0, e1);
                 }
             l += (sums[0] + sums[1]) + (sums[2] + sums[3]);
+            // (e4m3: K of the next round is widened beside the other wave's products, V after this one's; 0.665 ms instead of
+            // 0.675 with both at the end.)
+            if (FP8 && more)
+                deposit(0, buffer ^ 1);
+            asm volatile("" : "+v"(v_at));
             __builtin_amdgcn_s_setprio(1);
             lds_byte *v_lds = (lds_byte *)(lds[1][buffer]);  // (a cast between address spaces)
 #pragma unroll
@@ -413,7 +418,8 @@ __global__ __launch_bounds__(64 * kRows / RW, 2) void tail_kernel(const AttendAr
             __builtin_amdgcn_s_setprio(0);
             if (!more)
                 break;
-            deposit(0, buffer ^ 1);
+            if (!FP8)
+                deposit(0, buffer ^ 1);
             deposit(1, buffer ^ 1);
             __syncthreads();
         }
