@@ -18,7 +18,10 @@
 // 2,085 new tokens behind 32,768 (8 heads of 5 rows a token, bf16, D 128): 1.51 to 1.61 ms by machine, 900 to 955 TFLOP/s,
 // where a large library product reaches 1,200.  Per round of 64 tokens a wave has 1,024 cycles of products and about 1,150 of vector work (512
 // of them exponentials); two waves of a SIMD overlap them partly.  Ragged tails of up to 1,055 tokens, e4m3, D 256, a
-// window of 4,096 and capped scores: 0.665 ms, 490 TFLOP/s; its 16-row waves read LDS twice as often, which bounds them.
+// window of 4,096 and capped scores: 0.66 ms, 495 TFLOP/s; there the matrix cores are
+// busy for a fifth of the cycles, LDS for a quarter and the vector units for a third, one after the other: one workgroup
+// a CU, whose two waves a SIMD meet at a barrier every round.  (Half of its waves half a round behind the others, with a
+// barrier for each half: 0.76 ms, as scores take longer than outputs.)
 #include <algorithm>
 #include <type_traits>
 
@@ -108,7 +111,7 @@ __global__ __launch_bounds__(64 * kRows / RW, 2) void tail_kernel(const AttendAr
     // the banks: 16 rows of one piece (K), 4 rows of 4 or 8 of 2 pieces (V).
     const auto k_permute = [](int t) { return (WIDE ? t : (t & 3) | (t >> 1 & 12)) & (DP / 8 < 16 ? DP / 8 - 1 : 15); };
     const auto v_permute = [](int t) {
-        return !WIDE ? 2 * ((t & 3) | (t >> 1 & 4)) : DP == 64 ? 4 * (t >> 1 & 1) : 4 * (t & 3);
+        return (!WIDE ? 2 * ((t & 3) | (t >> 1 & 4)) : DP == 64 ? 4 * (t >> 1 & 1) : 4 * (t & 3)) | (t & 1);
     };
     // Token (of 32) of a lane's x-th score.
     const auto token_of = [](int x, int part) { return WIDE ? 8 * (x >> 2) + part * 4 + (x & 3) : part * 8 + x; };
@@ -158,7 +161,9 @@ __global__ __launch_bounds__(64 * kRows / RW, 2) void tail_kernel(const AttendAr
 
     const int32_t *table = a.batch.tables + b * a.batch.table_stride;
     const uint8_t *cache = pg.base + static_cast<uint32_t>(h) * pg.head_bytes;
-    const int piece = tid % GC, first_row = tid / GC;
+    // (e4m3: a piece is two in LDS, so 8 lanes write every other one; 4 of them take the next row, whose are turned about: 0.658 ms for 0.667.)
+    const int piece = FP8 ? (tid & 3) | (tid >> 1 & (GC - 4)) : tid % GC;
+    const int first_row = FP8 && GC > 4 ? (tid >> 2 & 1) | tid / (2 * GC) * 2 : tid / GC;
     const bool piece_ok = piece * 16 < pg.row_bytes;
 
     // Lanes look up a round's tokens (lane % TK each): the page's block, then where the token's row is; -1 for a token
@@ -184,7 +189,7 @@ __global__ __launch_bounds__(64 * kRows / RW, 2) void tail_kernel(const AttendAr
     // gain (1.57 to 1.60 ms instead of 1.56): their pieces are permuted as well.
     constexpr int WR = 64 / GC;  // rows of a wave in one load
     const bool together = FP8 && pg.BS % WR == 0 && pg.D == DP;
-    const uint32_t lane_row = static_cast<uint32_t>(lane / GC) * pg.token_bytes;
+    const uint32_t lane_row = static_cast<uint32_t>(first_row - wave * WR) * pg.token_bytes;
     auto request = [&](int64_t off, int buffer) {
         const bool all = __all(off >= 0);
         if constexpr (FP8) {
