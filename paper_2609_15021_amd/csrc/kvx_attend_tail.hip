@@ -15,13 +15,13 @@
 // Workgroups of a KV head come 8 apart where there are 8 heads, and so on one XCD (consecutive ones go to consecutive
 // XCDs), and use its L2 together.
 //
-// 2,085 new tokens behind 32,768 (8 heads of 5 rows a token, bf16, D 128): 1.51 to 1.61 ms by machine, 900 to 955 TFLOP/s,
-// where a large library product reaches 1,200.  Per round of 64 tokens a wave has 1,024 cycles of products and about 1,150 of vector work (512
-// of them exponentials); two waves of a SIMD overlap them partly.  Ragged tails of up to 1,055 tokens, e4m3, D 256, a
-// window of 4,096 and capped scores: 0.66 ms, 495 TFLOP/s; there the matrix cores are
-// busy for a fifth of the cycles, LDS for a quarter and the vector units for a third, one after the other: one workgroup
-// a CU, whose two waves a SIMD meet at a barrier every round.  (Half of its waves half a round behind the others, with a
-// barrier for each half: 0.76 ms, as scores take longer than outputs.)
+// 2,085 new tokens behind 32,768 (8 heads of 5 rows a token, bf16, D 128): 1.51 to 1.61 ms by machine, 900 to 955
+// TFLOP/s, where a large library product reaches 1,200.  Per round of 64 tokens a wave has 1,024 cycles of products and
+// about 1,150 of vector work (512 of them exponentials); two waves of a SIMD overlap them partly.  Ragged tails of up to
+// 1,055 tokens, e4m3, D 256, a window of 4,096 and capped scores: 0.66 ms, 495 TFLOP/s; there the matrix cores are busy
+// for a fifth of the cycles, LDS for a quarter and the vector units for a third, mostly one after the other: one
+// workgroup a CU, whose two waves a SIMD meet at a barrier every round.  (Half of its waves half a round behind the
+// others, with a barrier for each half: 0.76 ms, as scores take longer than outputs.)
 #include <algorithm>
 #include <type_traits>
 
@@ -161,7 +161,8 @@ __global__ __launch_bounds__(64 * kRows / RW, 2) void tail_kernel(const AttendAr
 
     const int32_t *table = a.batch.tables + b * a.batch.table_stride;
     const uint8_t *cache = pg.base + static_cast<uint32_t>(h) * pg.head_bytes;
-    // (e4m3: a piece is two in LDS, so 8 lanes write every other one; 4 of them take the next row, whose are turned about: 0.658 ms for 0.667.)
+    // (e4m3: a piece is two in LDS, so 8 lanes of a row would write every other one, and meet banks twice; 4 of the 8 take
+    // the next row, whose pairs are turned about: 0.658 ms instead of 0.667 for the ragged tails.)
     const int piece = FP8 ? (tid & 3) | (tid >> 1 & (GC - 4)) : tid % GC;
     const int first_row = FP8 && GC > 4 ? (tid >> 2 & 1) | tid / (2 * GC) * 2 : tid / GC;
     const bool piece_ok = piece * 16 < pg.row_bytes;
