@@ -466,14 +466,16 @@ __global__ __launch_bounds__(64 * kRows / RW, 2) void tail_kernel(const AttendAr
 }
 
 // What each token received: a wave holds K of 32 tokens, goes over the rows that see them, 32 at a time, with their
-// scores taken again, and adds up exp2(s - lse) for each token; a token's 32 partial sums are joined at the end.
-template <class T, bool FP8, int DP>
+// scores taken again, and adds up exp2(s - lse) for each token; a token's 32 partial sums are joined at the end.  SHARED:
+// a workgroup's waves have the same tokens and take turns with the rows; their sums are joined in order.
+template <class T, bool FP8, int DP, bool SHARED>
 __global__ __launch_bounds__(64 * kWeighWaves) void weigh_kernel(const AttendArgs a) {
     constexpr int KC = DP * (FP8 ? 1 : 2) / 32;  // 16-byte pieces of a token's K in a lane
     const Pages &pg = a.pages;
     const int lane = threadIdx.x & 63, c = lane & 31, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int b = blockIdx.z, h = blockIdx.y, base = (blockIdx.x * kWeighWaves + wave) * 32;
+    const int b = blockIdx.z, h = blockIdx.y, base = (SHARED ? blockIdx.x : blockIdx.x * kWeighWaves + wave) * 32;
+    __shared__ float wave_sums[SHARED ? kWeighWaves : 1][32];
     Sequence seq;
     if (!sequence(a.batch, b, pg.err, seq) || base >= seq.n)
         return;
@@ -500,7 +502,7 @@ __global__ __launch_bounds__(64 * kWeighWaves) void weigh_kernel(const AttendArg
         for (int k = 0; k < KC; ++k)
             k_reg[k] = *reinterpret_cast<const u32x4 *>(k_row + (k * 32 + half * 16 < pg.row_bytes ? k * 32 + half * 16 : 0));
         const float scale = a.scale * kLog2e;
-        for (int r0 = i0 * a.group; r0 < i1 * a.group; r0 += 32) {
+        for (int r0 = i0 * a.group + (SHARED ? wave * 32 : 0); r0 < i1 * a.group; r0 += 32 * (SHARED ? kWeighWaves : 1)) {
             const int r = min(r0 + c, i1 * a.group - 1), i = divide(r, a.by_group), head = h * a.group + r - i * a.group;
             const int p = r0 + c < i1 * a.group ? past + i : -1;
             const uint8_t *q = a.q.data + (seq.q0 + i) * a.q.token_stride + head * a.q.head_stride;
@@ -526,7 +528,12 @@ __global__ __launch_bounds__(64 * kWeighWaves) void weigh_kernel(const AttendArg
                                       T{});
                 }
             }
-            if (a.softcap > 0.f) {
+            if (a.softcap > 0.f && a.softcap <= kSmallCap) {
+                const float twice = 2.f * kLog2e * a.scale / a.softcap, cap = a.softcap * kLog2e;
+#pragma unroll
+                for (int x = 0; x < 16; ++x)
+                    s[x] = small_capped(s[x], twice, cap);
+            } else if (a.softcap > 0.f) {
                 const float inv = a.scale / a.softcap, cap = a.softcap * kLog2e;
 #pragma unroll
                 for (int x = 0; x < 16; ++x)
@@ -552,16 +559,30 @@ __global__ __launch_bounds__(64 * kWeighWaves) void weigh_kernel(const AttendArg
             }
         }
     }
-    // Joined over the 32 columns: lane c ends with the sum of token base + c (of its half's 16).
+    // Joined over the 32 columns: lane x of a half has the sum of its x-th token.
+    const auto receives = [&](int t, float sum) {
+        const int64_t at = b * a.weights_seq_stride + h * a.weights_head_stride + t;
+        a.weights_out[at] = (a.weights_in ? a.weights_in[at] : 0.f) + sum;
+    };
 #pragma unroll
     for (int x = 0; x < 16; ++x) {
 #pragma unroll
         for (int o = 16; o; o >>= 1)
             sums[x] += __shfl_xor(sums[x], o);
-        const int t = base + 8 * (x >> 2) + half * 4 + (x & 3);
-        if (c == x && t < seq.n) {
-            const int64_t at = b * a.weights_seq_stride + h * a.weights_head_stride + t;
-            a.weights_out[at] = (a.weights_in ? a.weights_in[at] : 0.f) + sums[x];
+        const int t = 8 * (x >> 2) + half * 4 + (x & 3);
+        if (SHARED && c == x)
+            wave_sums[wave][t] = sums[x];
+        else if (c == x && base + t < seq.n)
+            receives(base + t, sums[x]);
+    }
+    if constexpr (SHARED) {
+        __syncthreads();
+        const int t = threadIdx.x;
+        if (t < 32 && base + t < seq.n) {
+            float sum = 0.f;
+            for (int i = 0; i < kWeighWaves; ++i)
+                sum += wave_sums[i][t];
+            receives(base + t, sum);
         }
     }
 }
@@ -590,14 +611,23 @@ hipError_t launch(const AttendArgs &a, const Parts &parts, int max_queries, hipS
                                          : launch<T, FP8, false>(a, parts, max_queries, stream);
 }
 
+template <class T, bool FP8, bool SHARED>
+hipError_t launch_weigh(const AttendArgs &a, hipStream_t stream) {
+    const dim3 grid(static_cast<uint32_t>((a.batch.max_len - 1) / (SHARED ? 32 : 32 * kWeighWaves) + 1),
+                    static_cast<uint32_t>(a.pages.H), static_cast<uint32_t>(a.num_seqs));
+    const auto kernel = a.pages.D > 128  ? weigh_kernel<T, FP8, 256, SHARED>
+                        : a.pages.D > 64 ? weigh_kernel<T, FP8, 128, SHARED>
+                                         : weigh_kernel<T, FP8, 64, SHARED>;
+    return launch_kernel(kernel, grid, 64 * kWeighWaves, stream, a);
+}
+
 template <class T, bool FP8>
 hipError_t launch_weigh(const AttendArgs &a, hipStream_t stream) {
-    const dim3 grid(static_cast<uint32_t>((a.batch.max_len + 32 * kWeighWaves - 1) / (32 * kWeighWaves)),
-                    static_cast<uint32_t>(a.pages.H), static_cast<uint32_t>(a.num_seqs));
-    const auto kernel = a.pages.D > 128  ? weigh_kernel<T, FP8, 256>
-                        : a.pages.D > 64 ? weigh_kernel<T, FP8, 128>
-                                         : weigh_kernel<T, FP8, 64>;
-    return launch_kernel(kernel, grid, 64 * kWeighWaves, stream, a);
+    // A wave waits for each 32 rows' queries in turn, so where the tiles are fewer than 2 waves a SIMD, 4 take turns (7
+    // sequences of 308 new tokens in 2,196, 2 heads of 8 rows: the whole call 194 us instead of 284; 3 of 342, 64 instead
+    // of 125).  With more tiles K would only be read by more waves (31,000 tiles: 8 waves each take 1.46 ms, one 0.95).
+    const int64_t tiles = (int64_t{a.batch.max_len} + 31) / 32 * a.pages.H * a.num_seqs;
+    return tiles < 2048 ? launch_weigh<T, FP8, true>(a, stream) : launch_weigh<T, FP8, false>(a, stream);
 }
 
 }  // namespace

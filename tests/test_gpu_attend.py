@@ -134,6 +134,17 @@ def test_many_sequences():
     run(ref.Case(1, 2, 16, 4, lens, [1 + n % 2 for n in lens], seed=23))
 
 
+@pytest.mark.parametrize("options", [{}, dict(softcap=5.0, window=90), dict(softcap=100.0)])
+@pytest.mark.parametrize("fp8", [False, True])
+def test_weights_of_many_tiles(fp8, options):
+    """Received weights where the tokens alone fill the chip (2,280 tiles of 32), and of few tiles with many rows."""
+    lens = [600] + [1 + 37 * i % 400 for i in range(29)]
+    c = ref.Case(4, 5, 64, 16, lens, [min(n, 4 + i % 3) for i, n in enumerate(lens)], fp8=fp8, seed=61)
+    run(c, options, weights="fresh")
+    c = ref.Case(1, 5, 96, 16, [333, 40], [300, 7], fp8=fp8, seed=62)
+    run(c, options, weights="in_place")
+
+
 def test_weights_at_any_element():
     """Rows of weights that start at odd elements, of odd lengths."""
     for new in ([1, 1, 1], [30, 70, 1]):
