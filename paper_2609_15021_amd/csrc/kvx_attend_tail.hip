@@ -624,8 +624,8 @@ hipError_t launch_weigh(const AttendArgs &a, hipStream_t stream) {
 template <class T, bool FP8>
 hipError_t launch_weigh(const AttendArgs &a, hipStream_t stream) {
     // A wave waits for each 32 rows' queries in turn, so where the tiles are fewer than 2 waves a SIMD, 4 take turns (7
-    // sequences of 308 new tokens in 2,196, 2 heads of 8 rows: the whole call 194 us instead of 284; 3 of 342, 64 instead
-    // of 125).  With more tiles K would only be read by more waves (31,000 tiles: 8 waves each take 1.46 ms, one 0.95).
+    // sequences of 308 new tokens in 2,196, 2 heads of 8 rows: the whole call 194 us instead of 284; 3 of up
+    // to 208 in 342, 64 instead of 125).  With more tiles K would only be read by more waves (31,000 tiles: 8 waves each take 1.46 ms, one 0.95).
     const int64_t tiles = (int64_t{a.batch.max_len} + 31) / 32 * a.pages.H * a.num_seqs;
     return tiles < 2048 ? launch_weigh<T, FP8, true>(a, stream) : launch_weigh<T, FP8, false>(a, stream);
 }
