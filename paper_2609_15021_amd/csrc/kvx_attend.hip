@@ -232,7 +232,7 @@ kv_status attend(const kv_cache *cache, int32_t layer, const kv_batch *batch, co
     a.scale = scale_of(cache, o);
     a.softcap = o->softcap;
     a.v_scale = o->v_scale == 0.f ? 1.f : o->v_scale;
-    a.window = o->window;
+    a.window = o->window < batch->max_len ? o->window : 0;  // a window of every token hides none
     a.heads = q->heads;
     a.group = q->heads / cache->layout.num_kv_heads;
     a.num_seqs = batch->num_seqs;

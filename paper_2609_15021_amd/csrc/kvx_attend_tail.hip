@@ -482,7 +482,9 @@ __global__ __launch_bounds__(64 * kWeighWaves) void weigh_kernel(const AttendArg
     // Rows that see any of the 32 tokens: new tokens from base on, and before the window has closed on the last.
     const int past = seq.n - seq.nq;
     const int i0 = max(0, base - past), i1 = a.window > 0 ? min<int64_t>(seq.nq, int64_t{base} + 31 + a.window - past) : seq.nq;
-    const int first_seen = a.window > 0 ? max(0, past + 1 - a.window) : 0;
+    // (In 64 bits: rows before token 0 and a wide window are together beyond 32.)
+    const int first_seen =
+        a.window > 0 ? static_cast<int>(max(int64_t{0}, int64_t{past} + 1 - a.window)) : 0;
     const int t_lane = base + c;
     float sums[16];
 #pragma unroll
