@@ -173,7 +173,7 @@ __device__ __forceinline__ bool share_of(const AttendArgs &a, const Shares &shar
 }
 
 __device__ __forceinline__ int parts_of(const Span &s, int len) {
-    return s.end > s.start ? (s.end - s.start + len - 1) / len : 1;
+    return s.end > s.start ? (s.end - s.start - 1) / len + 1 : 1;
 }
 
 // Two-byte element types on the matrix cores.  kShift: weights are exp2(s - m + kShift), and m is at least the largest

@@ -36,3 +36,39 @@ def test_windows_that_hide_nothing(window, new):
     ref.check(lse, want[1], want[4], "lse")
     for b, n in enumerate(c.lens):
         ref.check(weights[b, :, :n], want[2][b, :, :n], want[5][b, :, :n], "weights")
+
+
+@pytest.mark.parametrize("new", [100, 1])
+def test_longest_sequence(new):
+    """A sequence of 2^31 - 1024 tokens, all pages but the last being one and the same: its last tokens, whose scores are
+    90 above the others' (which weigh 2^31 exp(-90) or 2e-30 together), are all that counts."""
+    BS, D = 4096, 8
+    n = 2**31 - 1024
+    pages = n // BS + 1
+    gen = torch.Generator().manual_seed(32)
+    t = torch.zeros(2, 2, 1, BS, D)
+    t[0, 1] = 7.0
+    t[1, 0, 0, :, 0] = 8.0
+    t[1, 0, 0, :, 1] = torch.randn(BS, generator=gen)
+    t[1, 1] = torch.randn(1, BS, D, generator=gen)
+    t = t.to(BF16)
+    q = torch.zeros(new, 1, D, dtype=BF16)
+    q[:, 0, 0] = 32.0
+    q[:, 0, 1] = torch.randn(new, generator=gen).to(BF16)
+    cache = kvx.Cache([t.to(DEV)], kvx.make_layout(1, 1, D, 2, BS, BS), 2)
+    tables = torch.zeros(1, pages, **INTS)
+    tables[0, -1] = 1
+    out, lse = attend.kv_attend(cache, 0, q.to(DEV), tables, torch.tensor([n], **INTS), torch.tensor([0, new], **INTS))
+    k, v = (t[1, i, 0].double().numpy() for i in (0, 1))
+    for i in range(new):
+        seen = n - new + i - (pages - 1) * BS + 1
+        s = k[:seen] @ q[i, 0].double().numpy() / np.sqrt(D)
+        w = np.exp(s - s.max())
+        total = w.sum()
+        w /= total
+        # A score is off by 8 additions and its roundings, a weight by that and half a step, the sums by 16 tokens at a time.
+        off = 2.0**-23 * (8 * np.abs(s).max() + 64 + seen / 16) * 4
+        magnitude = w @ np.abs(v[:seen])
+        want = w @ v[:seen]
+        ref.check(out[i, 0], want, 2.0**-8 * (np.abs(want) + magnitude) + off * magnitude, "out")
+        assert abs(float(lse[i, 0]) - (s.max() + np.log(total))) <= off + 2.0**-22 * 100
