@@ -166,20 +166,20 @@ __global__ __launch_bounds__(kKeepThreads) void keep_kernel(const KeepArgs a) {
 #pragma unroll
     for (int i = 0; i < ROUNDS; ++i)
         keys[i] = keys_of(load(origin + i * kRound + tid * 4), origin + i * kRound + tid * 4);
-    // f(round, first token, its 4 keys) for every round of the row.
-    const auto each = [&](auto &&f) {
+    // f(round, first token, its 4 keys) for the rounds [from, to) of the row.
+    const auto each = [&](int from, int to, auto &&f) {
         if constexpr (ROUNDS > 0) {
 #pragma unroll
             for (int i = 0; i < ROUNDS; ++i)
-                if (i < rounds)
+                if (i >= from && i < to)
                     f(i, origin + i * kRound + tid * 4, keys[i]);
         } else {
             // kAtOnce rounds are on their way (64 KiB) while as many are used.
             f32x4 next[kAtOnce];
 #pragma unroll
             for (int j = 0; j < kAtOnce; ++j)
-                next[j] = load(j * kRound + tid * 4);
-            for (int i = 0; i < rounds; i += kAtOnce) {
+                next[j] = load((from + j) * kRound + tid * 4);
+            for (int i = from; i < to; i += kAtOnce) {
                 f32x4 x[kAtOnce];
 #pragma unroll
                 for (int j = 0; j < kAtOnce; ++j) {
@@ -188,7 +188,7 @@ __global__ __launch_bounds__(kKeepThreads) void keep_kernel(const KeepArgs a) {
                 }
 #pragma unroll
                 for (int j = 0; j < kAtOnce; ++j)
-                    if (i + j < rounds)
+                    if (i + j < to)
                         f(i + j, (i + j) * kRound + tid * 4, keys_of(x[j], (i + j) * kRound + tid * 4));
             }
         }
@@ -204,7 +204,7 @@ __global__ __launch_bounds__(kKeepThreads) void keep_kernel(const KeepArgs a) {
         for (int j = tid; j < kCopies * kBins; j += kKeepThreads)
             counts[0][j] = 0;
         __syncthreads();
-        each([&](int, int t, const Keys &x) {
+        each(0, rounds, [&](int, int t, const Keys &x) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 if (!inside(t + j) || ((x.k[j] ^ threshold) & known) != 0)
@@ -267,7 +267,7 @@ __global__ __launch_bounds__(kKeepThreads) void keep_kernel(const KeepArgs a) {
             // What the pieces behind this one will want to know of it, whatever the last digit turns out to be: the
             // tokens with keys above (the threshold's first digits, value - 1), for each value and one more.
             int above = 0, all;
-            each([&](int, int t, const Keys &x) {
+            each(0, rounds, [&](int, int t, const Keys &x) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
                     above += inside(t + j) && (x.k[j] & known) > threshold;
@@ -312,9 +312,8 @@ __global__ __launch_bounds__(kKeepThreads) void keep_kernel(const KeepArgs a) {
         ties_done = q;
     }
     for (int set = 0; set < rounds; set += kMaxRounds) {
-        each([&](int i, int t, const Keys &x) {
-            if (i < set || i >= set + kMaxRounds)
-                return;
+        const int set_end = min(rounds, set + kMaxRounds);
+        each(set, set_end, [&](int i, int t, const Keys &x) {
             int sure_count = 0, tie_count = 0;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -330,7 +329,7 @@ __global__ __launch_bounds__(kKeepThreads) void keep_kernel(const KeepArgs a) {
         });
         __syncthreads();
         // Sums before each wave of each round: one entry a lane, carried from wave to wave.
-        const int entries = min(rounds - set, kMaxRounds) * kKeepWaves;
+        const int entries = (set_end - set) * kKeepWaves;
         int s = 0, q = 0, s_all, q_all;
         if (tid < entries) {
             s = of_wave[tid][0];
@@ -356,9 +355,7 @@ __global__ __launch_bounds__(kKeepThreads) void keep_kernel(const KeepArgs a) {
         sure_done += s_set;
         ties_done += q_set;
         __syncthreads();
-        each([&](int i, int t, const Keys &x) {
-            if (i < set || i >= set + kMaxRounds)
-                return;
+        each(set, set_end, [&](int i, int t, const Keys &x) {
             bool sure[4], tie[4];
             int sure_before = of_wave[(i - set) * kKeepWaves + wave][0], ties_before = of_wave[(i - set) * kKeepWaves + wave][1];
             uint64_t lanes = 0;

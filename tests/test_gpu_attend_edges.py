@@ -72,3 +72,43 @@ def test_longest_sequence(new):
         want = w @ v[:seen]
         ref.check(out[i, 0], want, 2.0**-8 * (np.abs(want) + magnitude) + off * magnitude, "out")
         assert abs(float(lse[i, 0]) - (s.max() + np.log(total))) <= off + 2.0**-22 * 100
+
+
+def test_keep_rows_of_several_sets():
+    """128 rows, some of more than 262,144 tokens, with ties on both sides of that and of twice that."""
+    L, B = 2 * 262144 + 5000, 128
+    lens = [min(L, 50 + 7 * b) for b in range(B)]
+    lens[5], lens[64], lens[127] = L, 262145, 262144
+    gen = torch.Generator().manual_seed(37)
+    w = torch.zeros(B, 1, L)
+    for b in (5, 64, 127):
+        w[b, 0] = (torch.rand(L, generator=gen) * 8).floor()  # an eighth of the tokens for each value
+    w[:, 0, :1000] = torch.rand(B, 1000, generator=gen)
+    w[5, 0, 262100:262200] = 9.0
+    device = w.to(DEV)
+    for budget in (40000, 300000):
+        got = attend.kv_keep(device, torch.tensor(lens, **INTS), budget, sinks=4, recent=1000)
+        for b in (0, 5, 64, 127):
+            want = ref.keep(w[b:b + 1].numpy(), lens[b:b + 1], budget, 4, 1000)
+            assert torch.equal(got[0][b:b + 1].cpu(), torch.from_numpy(want[0])) and int(got[1][b]) == want[1][0]
+            assert np.array_equal(got[2][b:b + 1].cpu().numpy(), want[2])
+
+
+def test_keep_very_long_rows():
+    """128 rows, one of 20 million tokens (77 sets of rounds, each of which is read once per step and no more): few
+    values, so that ties are everywhere, and a choice that ends in the first, in a middle and in the last set."""
+    L, B = 20_000_003, 128
+    w = (torch.rand(L, generator=torch.Generator().manual_seed(43)) * 50).floor()
+    w[-3000:] += 100.0
+    rows = w.to(DEV).expand(B, 1, L)  # one row in memory
+    lens = [100 + b for b in range(B)]
+    lens[77] = L
+    far = w.numpy()
+    for budget, sinks, recent in ((100_000, 7, 5), (3_000_000, 0, 100), (19_900_000, 4, 1000)):
+        keep, kept, kw = attend.kv_keep(rows, torch.tensor(lens, **INTS), budget, sinks=sinks, recent=recent)
+        middle = far[sinks:L - recent]
+        heavy = np.sort(np.argsort(-middle, kind="stable")[:budget - sinks - recent]) + sinks
+        want = np.concatenate([np.arange(sinks), heavy, np.arange(L - recent, L)])
+        assert np.array_equal(keep[77, 0].cpu().numpy(), want) and np.array_equal(kw[77, 0].cpu().numpy(), far[want])
+        assert kept.cpu().tolist() == [min(n, budget) for n in lens]
+        assert torch.equal(keep[3, 0, :103].cpu(), torch.arange(103, dtype=torch.int32)) and (keep[3, 0, 103:] == -1).all()
