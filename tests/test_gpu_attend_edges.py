@@ -58,7 +58,10 @@ def test_longest_sequence(new):
     cache = kvx.Cache([t.to(DEV)], kvx.make_layout(1, 1, D, 2, BS, BS), 2)
     tables = torch.zeros(1, pages, **INTS)
     tables[0, -1] = 1
-    out, lse = attend.kv_attend(cache, 0, q.to(DEV), tables, torch.tensor([n], **INTS), torch.tensor([0, new], **INTS))
+    weights = torch.full((1, 1, n), 5.0, device=DEV)
+    out, lse = attend.kv_attend(cache, 0, q.to(DEV), tables, torch.tensor([n], **INTS), torch.tensor([0, new], **INTS),
+                                weights=weights)
+    got = np.zeros(BS)
     k, v = (t[1, i, 0].double().numpy() for i in (0, 1))
     for i in range(new):
         seen = n - new + i - (pages - 1) * BS + 1
@@ -72,6 +75,30 @@ def test_longest_sequence(new):
         want = w @ v[:seen]
         ref.check(out[i, 0], want, 2.0**-8 * (np.abs(want) + magnitude) + off * magnitude, "out")
         assert abs(float(lse[i, 0]) - (s.max() + np.log(total))) <= off + 2.0**-22 * 100
+        got[:seen] += w
+    # (A weight is off by its score's error and lse's, and by a rounding for each of the rows.)
+    last = weights[0, 0, n - seen:].double().cpu().numpy()
+    assert (np.abs(last - got[:seen]) <= got[:seen] * (2 * off + 2.0**-22 * 100 + new * 2.0**-23) + 1e-30).all()
+    assert float(weights[0, 0, :n - seen].max()) < 1e-30
+
+
+def test_weights_of_wide_bounds():
+    """Bounds so wide that scores for all of them would take more than a GiB: weights are taken without them."""
+    c = ref.Case(2, 16, 64, 16, [300, 77, 1], [1, 1, 1], seed=33)
+    cache, _, q, _, _, tables, lens, _ = c.device()
+    most = 3_000_000
+    tables = torch.nn.functional.pad(tables, (0, most // 16 - tables.shape[1]), value=-1)
+    want = ref.attend(c)
+    weights = torch.zeros(3, 2, most, device=DEV)
+    torch.cuda.reset_peak_memory_stats()
+    before = torch.cuda.memory_allocated()
+    out, lse = attend.kv_attend(cache, 0, q, tables, lens, weights=weights, max_len=most)
+    assert torch.cuda.max_memory_allocated() - before <= 1 << 30
+    ref.check(out, want[0], want[3], "out")
+    ref.check(lse, want[1], want[4], "lse")
+    for b, n in enumerate(c.lens):
+        ref.check(weights[b, :, :n], want[2][b, :, :n], want[5][b, :, :n], "weights")
+        assert not weights[b, :, n:].any()
 
 
 def test_keep_rows_of_several_sets():
