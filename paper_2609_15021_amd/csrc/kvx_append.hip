@@ -4,6 +4,7 @@
 // lies.  Bound by HBM for long tails (every byte read once and written once; 3,880 tokens of 4 heads of 256 to e4m3, 24
 // MB, in 6.7 us), by the launch for a decoding step (2.4 us on the GPU, 10 with the host).
 #include <algorithm>
+#include <cmath>
 
 #include "kvx_paged.h"
 
@@ -109,9 +110,10 @@ kv_status append(const kv_cache *cache, int32_t layer, const kv_batch *batch, co
         return fail(KV_EINVAL, "rows of type %d for a cache of type %d", k->dtype, cache_dtype);
     k_scale = k_scale == 0.f ? 1.f : k_scale;
     v_scale = v_scale == 0.f ? 1.f : v_scale;
-    if (!(k_scale > 0.f) || !(v_scale > 0.f) || (!quantised && (k_scale != 1.f || v_scale != 1.f)))
-        return fail(KV_EINVAL, "scales must be positive, and 1 for a cache of 2-byte elements (got %g and %g)", k_scale,
-                    v_scale);
+    if (!(k_scale > 0.f && std::isfinite(k_scale)) || !(v_scale > 0.f && std::isfinite(v_scale)) ||
+        (!quantised && (k_scale != 1.f || v_scale != 1.f)))
+        return fail(KV_EINVAL, "scales must be positive and finite, and 1 for a cache of 2-byte elements (got %g and "
+                    "%g)", k_scale, v_scale);
     if (batch->num_seqs == 0 || batch->num_queries == 0)
         return KV_OK;
     st = check_on_current_device(cache);

@@ -1,5 +1,6 @@
 """Edges of the operators on the paged cache on the CPU: workspaces, and what is refused before any HIP call."""
 import ctypes
+import math
 
 import pytest
 import torch
@@ -25,3 +26,13 @@ def test_workspace_of_scores_is_bounded():
         without, score_bytes = need(seqs, length, False), seqs * 8 * 8 * -(-length // 32) * 32 * 4
         extra = need(seqs, length, True) - without
         assert without >= 0 and extra == (score_bytes if score_bytes <= 1 << 30 else 0), (seqs, length, extra)
+
+
+@pytest.mark.parametrize("which", ["ks", "vs"])
+def test_append_refuses_infinite_scales(which):
+    from paper_2609_15021_amd import attend, kvx
+    cache, batch, rows = _cache(kvx, kvx.make_layout(1, 2, 64, 1, 16, 16)), _batch(attend), _rows(attend, 2)
+    for scale in (math.inf, -math.inf):
+        scales = dict(dict(ks=1.0, vs=1.0), **{which: scale})
+        assert kvx._lib.kv_append(ctypes.byref(cache), 0, ctypes.byref(batch), ctypes.byref(rows), ctypes.byref(rows),
+                                  attend.KV_DTYPE_E4M3, scales["ks"], scales["vs"], None) == kvx.KV_EINVAL
