@@ -55,7 +55,7 @@ extern "C" {
  * (strides in elements; a view of a wider projection's output needs no copy). */
 typedef struct kv_rows {
     void *data;           /* DEVICE, 16-byte aligned */
-    int64_t token_stride; /* both strides >= 0 and multiples of 16 bytes */
+    int64_t token_stride; /* both strides >= 0 and, over more than one token or head, multiples of 16 bytes */
     int64_t head_stride;
     int32_t heads;
     int32_t dtype;        /* KV_DTYPE_BF16 or KV_DTYPE_F16 */

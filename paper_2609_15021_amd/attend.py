@@ -74,7 +74,7 @@ _declare(_lib)
 def _ints(t, name: str, dims: int, device: int, rows=None):
     """A tensor of int32 on the call's device whose last dimension is dense."""
     if not isinstance(t, torch.Tensor) or t.dtype is not torch.int32 or t.dim() != dims or \
-            (t.stride(-1) != 1 and t.numel()):
+            (t.stride(-1) != 1 and t.shape[-1] > 1 and t.numel()):
         raise TypeError(f"{name} must be a {dims}-dimensional int32 device tensor with a dense last dimension")
     if t.get_device() != device:
         _elsewhere(t, name, device)
@@ -100,7 +100,7 @@ def _floats(t, name: str, device: int, shape) -> None:
 
 def _weights(t, name: str, device: int, rows=None) -> None:
     if not isinstance(t, torch.Tensor) or t.dtype is not torch.float32 or t.dim() != 3 or \
-            (t.stride(2) != 1 and t.numel()) or (rows is not None and t.shape[:2] != rows):
+            (t.stride(2) != 1 and t.shape[2] > 1 and t.numel()) or (rows is not None and t.shape[:2] != rows):
         raise TypeError(f"{name} must be a [sequences][heads][tokens] float32 device tensor with dense rows"
                         f"{'' if rows is None else f' ({rows} of them)'}")
     _on(t, name, device)

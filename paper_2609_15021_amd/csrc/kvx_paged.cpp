@@ -115,7 +115,9 @@ kv_status check_rows(const kv_cache *cache, const kv_batch *batch, const kv_rows
         return KV_OK;
     if (!rows->data)
         return fail(KV_EINVAL, "%s: data must not be NULL", name);
-    if (reinterpret_cast<uintptr_t>(rows->data) % 16 != 0 || rows->token_stride % 8 != 0 || rows->head_stride % 8 != 0)
+    // (A stride over one token or head leads nowhere, and tensors have any there.)
+    if (reinterpret_cast<uintptr_t>(rows->data) % 16 != 0 || (batch->num_queries > 1 && rows->token_stride % 8 != 0) ||
+        (rows->heads > 1 && rows->head_stride % 8 != 0))
         return fail(KV_EUNSUPPORTED, "%s: rows must start at multiples of 16 bytes", name);
     return KV_OK;
 }

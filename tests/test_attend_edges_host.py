@@ -36,3 +36,65 @@ def test_append_refuses_infinite_scales(which):
         scales = dict(dict(ks=1.0, vs=1.0), **{which: scale})
         assert kvx._lib.kv_append(ctypes.byref(cache), 0, ctypes.byref(batch), ctypes.byref(rows), ctypes.byref(rows),
                                   attend.KV_DTYPE_E4M3, scales["ks"], scales["vs"], None) == kvx.KV_EINVAL
+
+
+def test_strides_that_lead_nowhere():
+    """A single token's or head's stride may be anything; over two it has to be a multiple of 16 bytes."""
+    from paper_2609_15021_amd import attend, kvx
+    cache = _cache(kvx, kvx.make_layout(1, 1, 64, 2, 16, 16))
+    o = attend.KvAttendOptions(cache_dtype=attend.KV_DTYPE_BF16)
+    for tokens, heads, changes, fine in ((1, 1, dict(token_stride=129, head_stride=3), True),
+                                         (1, 2, dict(token_stride=129), True), (2, 1, dict(head_stride=1), True),
+                                         (1, 2, dict(head_stride=129), False), (2, 1, dict(token_stride=129), False)):
+        b, q = _batch(attend, num_seqs=tokens, num_queries=tokens), _rows(attend, heads, **changes)
+        need = kvx._lib.kv_attend_workspace(ctypes.byref(cache), ctypes.byref(b), ctypes.byref(o), ctypes.byref(q))
+        assert need >= 0 if fine else need == kvx.KV_EUNSUPPORTED, (tokens, heads, changes)
+
+
+class _Answers:
+    """Stands in for the library: every call succeeds, and the last one's arguments are kept."""
+
+    def __getattr__(self, name):
+        def call(*args):
+            self.name, self.args = name, args
+            return 0
+        return call
+
+
+@pytest.fixture
+def host_cache(monkeypatch):
+    """(cache handle, library) for the binding's own work on host tensors."""
+    from paper_2609_15021_amd import attend, kvx
+    cache = object.__new__(kvx.Cache)
+    cache.layout = kvx.make_layout(2, 2, 64, 1, 16, 16)
+    cache.struct = _cache(kvx, cache.layout)
+    cache.struct.device = -1  # where host tensors are
+    lib = _Answers()
+    monkeypatch.setattr(attend, "_lib", lib)
+    monkeypatch.setattr(attend, "_call_stream", lambda stream: (None, attend._HERE))
+    monkeypatch.setattr(attend, "_attend_bytes", {})
+    monkeypatch.setattr(torch.cuda, "is_available", lambda: True)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: -1)
+    return cache, lib
+
+
+def test_binding_takes_single_entries_with_any_stride(host_cache):
+    """A batch of one cut from wider tensors: lengths, a table of one page, rows of one token, weights of one."""
+    from paper_2609_15021_amd import attend
+    cache, lib = host_cache
+    meta = torch.zeros(1, 7, dtype=torch.int32)
+    wide = torch.zeros(1, 3, 129, dtype=torch.bfloat16)
+    q, k = wide[:, :2, :64], wide[:, 1:, :64]
+    lens, table = meta[:, 3], meta[:, 1:2]
+    assert lens.stride() == (7,)
+    attend.kv_append(cache, 0, k, k, table.T.T, lens)
+    assert lib.name == "kv_append"
+    attend.kv_attend(cache, 0, q, torch.zeros(9, 1, dtype=torch.int32).T[:, :1], lens)
+    assert lib.name == "kv_attend"
+    attend.kv_keep(torch.zeros(1, 2, 5)[:, :, ::5], lens, 4)
+    assert lib.name == "kv_keep"
+    attend.kv_compact(cache, 0, table, torch.zeros(1, 1, 1, dtype=torch.int32), lens, table)
+    assert lib.name == "kv_compact"
+    two = torch.zeros(2, 7, dtype=torch.int32)
+    with pytest.raises(TypeError, match="dense last dimension"):
+        attend.kv_keep(torch.zeros(2, 2, 5), two[:, 3], 4)

@@ -139,3 +139,25 @@ def test_keep_very_long_rows():
         assert np.array_equal(keep[77, 0].cpu().numpy(), want) and np.array_equal(kw[77, 0].cpu().numpy(), far[want])
         assert kept.cpu().tolist() == [min(n, budget) for n in lens]
         assert torch.equal(keep[3, 0, :103].cpu(), torch.arange(103, dtype=torch.int32)) and (keep[3, 0, 103:] == -1).all()
+
+
+@pytest.mark.parametrize("n", [1, 77])
+def test_one_token_with_any_stride(n):
+    """A batch of one new token cut from wider tensors, whose strides between tokens (and of single entries) are odd."""
+    c = ref.Case(1, 3, 64, 16, [n], [1], seed=44)
+    cache, t, q, k, v, tables, lens, _ = c.device()
+    wide = torch.zeros(2, 5 * 64 + 1, dtype=BF16, device=DEV)
+    parts = wide[:, :320].view(2, 5, 64)[:1]
+    parts[:, :3], parts[:, 3:4], parts[:, 4:] = q, k, v
+    meta = torch.zeros(1, 7, **INTS)
+    meta[0, 3] = n
+    assert parts.stride(0) == 321 and meta[:, 3].stride() == (7,)
+    attend.kv_append(cache, 0, parts[:, 3:4], parts[:, 4:], tables, meta[:, 3])
+    out, lse = attend.kv_attend(cache, 0, parts[:, :3], tables, meta[:, 3])
+    for rows, stored in ((c.k, c.new_k), (c.v, c.new_v)):
+        rows[0][n - 1] = stored[0].double().numpy()
+    want = ref.attend(c)
+    ref.check(out, want[0], want[3], "out")
+    ref.check(lse, want[1], want[4], "lse")
+    keep, kept, _ = attend.kv_keep(torch.ones(1, 1, 3 * n, device=DEV)[:, :, ::3][:, :, :1], meta[:, 0], 2)
+    assert keep.tolist() == [[[-1, -1]]] and kept.tolist() == [0]
