@@ -112,7 +112,8 @@ KV_API kv_status kv_append(const kv_cache *cache, int32_t layer, const kv_batch 
  * longer ones (off by up to half a step of that type each).  What slots behind a sequence's last token hold does not
  * matter, but its own tokens' V are taken to be finite: 0 times an infinity of a token that a row does not see reaches
  * that row.
- *   q, out:    [num_queries][query heads][D], same type; the cache's, or either 2-byte type for E4M3;
+ *   q, out:    [num_queries][query heads][D], same type; the cache's, or either 2-byte type for E4M3; rows of out do not
+ *              overlap;
  *   lse:       DEVICE float[num_queries][query heads], or NULL;
  *   workspace: DEVICE, kv_attend_workspace's bytes (16-byte aligned; may be NULL for 0 bytes), the call's own until its
  *              work has completed: calls that may overlap, and graphs whose replays may, need one each.

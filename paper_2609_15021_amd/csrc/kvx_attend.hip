@@ -194,6 +194,11 @@ kv_status attend(const kv_cache *cache, int32_t layer, const kv_batch *batch, co
     if (out->heads != q->heads || out->dtype != q->dtype)
         return fail(KV_EINVAL, "out has %d heads of type %d, q %d of type %d", out->heads, out->dtype, q->heads,
                     q->dtype);
+    const int D = cache->layout.head_dim;
+    if (batch->num_seqs > 0 && ((batch->num_queries > 1 && out->token_stride < D) ||
+                                (batch->num_queries > 0 && out->heads > 1 && out->head_stride < D)))
+        return fail(KV_EINVAL, "rows of out (strides %lld and %lld) are shorter than %d elements",
+                    static_cast<long long>(out->token_stride), static_cast<long long>(out->head_stride), D);
     const Plan plan = plan_of(cache, batch, o, q);
     const int64_t need = plan.bytes;
     if (workspace_bytes < need || (need > 0 && !workspace))

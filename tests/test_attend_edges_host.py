@@ -98,3 +98,20 @@ def test_binding_takes_single_entries_with_any_stride(host_cache):
     two = torch.zeros(2, 7, dtype=torch.int32)
     with pytest.raises(TypeError, match="dense last dimension"):
         attend.kv_keep(torch.zeros(2, 2, 5), two[:, 3], 4)
+
+
+def test_attend_refuses_rows_of_out_that_overlap():
+    """Rows of q may be one and the same (a stride of 0), rows of out not."""
+    from paper_2609_15021_amd import attend, kvx
+    cache, batch = _cache(kvx, kvx.make_layout(1, 2, 64, 2, 16, 16)), _batch(attend)
+    o = attend.KvAttendOptions(cache_dtype=attend.KV_DTYPE_BF16)
+    for changes in (dict(token_stride=0), dict(head_stride=0), dict(token_stride=56), dict(head_stride=32)):
+        q, out = _rows(attend, 4, **changes), _rows(attend, 4)
+        assert kvx._lib.kv_attend_workspace(ctypes.byref(cache), ctypes.byref(batch), ctypes.byref(o),
+                                            ctypes.byref(q)) >= 0
+        assert kvx._lib.kv_attend(ctypes.byref(cache), 0, ctypes.byref(batch), ctypes.byref(o), ctypes.byref(out),
+                                  ctypes.byref(q), SOME, SOME, 1 << 40, None) == kvx.KV_EINVAL, changes
+        assert b"rows of out" in kvx._lib.kv_last_error()
+    nothing, rows = _batch(attend, num_seqs=0), _rows(attend, 4, token_stride=0, head_stride=0)
+    assert kvx._lib.kv_attend(ctypes.byref(cache), 0, ctypes.byref(nothing), ctypes.byref(o), ctypes.byref(rows),
+                              ctypes.byref(rows), None, SOME, 1 << 40, None) == kvx.KV_OK
