@@ -118,6 +118,14 @@ def _rows(t, name: str, head_dim: int, device: int) -> KvRows:
     return KvRows(t.data_ptr(), token, head, heads, _DTYPES[t.dtype])
 
 
+def _factor(x, name: str) -> float:
+    """A factor that the caller named; the ABI takes 0 in 32 bits for its default, which is not what 0 means here."""
+    x = float(x)
+    if x != 1.0 and ctypes.c_float(x).value == 0.0:
+        raise ValueError(f"{name} must be above 0 in 32 bits (got {x:g})")
+    return x
+
+
 def _batch(cache: Cache, tables, lens, starts, tokens: int, max_q, max_len) -> KvBatch:
     device = cache.struct.device
     B, pages = _ints(tables, "tables", 2, device).shape
@@ -180,7 +188,7 @@ def kv_append(cache: Cache, layer: int, k, v, tables, lens, starts=None, *, max_
     batch = _batch(cache, tables, lens, starts, k.shape[0], max_q, max_len)
     handle, _ = _call_stream(stream)
     _raise(_lib.kv_append(ctypes.byref(cache.struct), int(layer), ctypes.byref(batch), ctypes.byref(kr), ctypes.byref(vr),
-                          _cache_dtype(cache, dtype, k), float(k_scale), float(v_scale), handle))
+                          _cache_dtype(cache, dtype, k), _factor(k_scale, "k_scale"), _factor(v_scale, "v_scale"), handle))
     _used(stream, k, v, tables, lens, starts)
 
 
@@ -197,8 +205,9 @@ def kv_attend(cache: Cache, layer: int, q, tables, lens, starts=None, *, max_q=N
     device = cache.struct.device
     qr = _rows(q, "q", cache.layout.head_dim, device)
     batch = _batch(cache, tables, lens, starts, q.shape[0], max_q, max_len)
-    options = KvAttendOptions(_cache_dtype(cache, dtype, q), int(window), 0.0 if scale is None else float(scale),
-                              float(softcap), float(k_scale), float(v_scale))
+    options = KvAttendOptions(_cache_dtype(cache, dtype, q), int(window), 0.0 if scale is None else _factor(scale, "scale"),
+                              _factor(softcap, "softcap") if softcap else 0.0, _factor(k_scale, "k_scale"),
+                              _factor(v_scale, "v_scale"))
     if slopes is not None:
         _floats(slopes, "slopes", device, (q.shape[1],))
         options.slopes = slopes.data_ptr()

@@ -54,6 +54,8 @@ def test_strides_that_lead_nowhere():
 class _Answers:
     """Stands in for the library: every call succeeds, and the last one's arguments are kept."""
 
+    name = args = None
+
     def __getattr__(self, name):
         def call(*args):
             self.name, self.args = name, args
@@ -115,3 +117,23 @@ def test_attend_refuses_rows_of_out_that_overlap():
     nothing, rows = _batch(attend, num_seqs=0), _rows(attend, 4, token_stride=0, head_stride=0)
     assert kvx._lib.kv_attend(ctypes.byref(cache), 0, ctypes.byref(nothing), ctypes.byref(o), ctypes.byref(rows),
                               ctypes.byref(rows), None, SOME, 1 << 40, None) == kvx.KV_OK
+
+
+def test_binding_refuses_factors_that_the_library_takes_for_defaults(host_cache):
+    """0, and what is 0 in 32 bits, would be the default of the C ABI: 1 / sqrt(D), no cap, a scale of 1."""
+    from paper_2609_15021_amd import attend
+    cache, lib = host_cache
+    rows, kv = torch.zeros(2, 4, 64, dtype=torch.bfloat16), torch.zeros(2, 2, 64, dtype=torch.bfloat16)
+    tables, lens = torch.zeros(2, 4, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+    for options in (dict(scale=0.0), dict(scale=1e-50), dict(scale=-0.0), dict(softcap=1e-50), dict(softcap=-1e-60),
+                    dict(k_scale=0.0), dict(v_scale=0), dict(k_scale=1e-46), dict(v_scale=-1e-46)):
+        (name, value), = options.items()
+        with pytest.raises(ValueError, match=name):
+            attend.kv_attend(cache, 0, rows, tables, lens, **options)
+        if name[1:] == "_scale":
+            with pytest.raises(ValueError, match=name):
+                attend.kv_append(cache, 0, kv, kv, tables, lens, **options)
+    assert lib.name is None
+    attend.kv_attend(cache, 0, rows, tables, lens, scale=0.25, softcap=0, k_scale=2, v_scale=1e-30)
+    options = lib.args[3]._obj
+    assert (options.scale, options.softcap, options.k_scale) == (0.25, 0.0, 2.0) and 0 < options.v_scale < 2e-30
