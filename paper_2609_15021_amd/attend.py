@@ -126,9 +126,18 @@ def _factor(x, name: str) -> float:
     return x
 
 
+def _int32(x, name: str) -> int:
+    """ctypes would cut a longer number to its low 32 bits."""
+    x = int(x)
+    if not -2**31 <= x < 2**31:
+        raise ValueError(f"{name} must fit 32 bits (got {x})")
+    return x
+
+
 def _batch(cache: Cache, tables, lens, starts, tokens: int, max_q, max_len) -> KvBatch:
     device = cache.struct.device
     B, pages = _ints(tables, "tables", 2, device).shape
+    _int32(tokens, "the number of new tokens")
     _ints(lens, "lens", 1, device, B)
     if starts is None:
         if tokens != B:
@@ -138,7 +147,7 @@ def _batch(cache: Cache, tables, lens, starts, tokens: int, max_q, max_len) -> K
         starts_at = _ints(starts, "starts", 1, device, B + 1).data_ptr()
         max_q = max(1, tokens if max_q is None else min(tokens, int(max_q)))
     most = min(pages * cache.layout.block_size, 2**31 - 1024)
-    return KvBatch(B, max_q, tokens, most if max_len is None else min(most, int(max_len)), pages, 0, tables.stride(0),
+    return KvBatch(B, max_q, tokens, most if max_len is None else min(most, max(int(max_len), -1)), pages, 0, tables.stride(0),
                    tables.data_ptr(), lens.data_ptr(), starts_at)
 
 
@@ -187,7 +196,7 @@ def kv_append(cache: Cache, layer: int, k, v, tables, lens, starts=None, *, max_
         raise ValueError(f"k and v differ in shape: {tuple(k.shape)} and {tuple(v.shape)}")
     batch = _batch(cache, tables, lens, starts, k.shape[0], max_q, max_len)
     handle, _ = _call_stream(stream)
-    _raise(_lib.kv_append(ctypes.byref(cache.struct), int(layer), ctypes.byref(batch), ctypes.byref(kr), ctypes.byref(vr),
+    _raise(_lib.kv_append(ctypes.byref(cache.struct), _int32(layer, "layer"), ctypes.byref(batch), ctypes.byref(kr), ctypes.byref(vr),
                           _cache_dtype(cache, dtype, k), _factor(k_scale, "k_scale"), _factor(v_scale, "v_scale"), handle))
     _used(stream, k, v, tables, lens, starts)
 
@@ -205,7 +214,8 @@ def kv_attend(cache: Cache, layer: int, q, tables, lens, starts=None, *, max_q=N
     device = cache.struct.device
     qr = _rows(q, "q", cache.layout.head_dim, device)
     batch = _batch(cache, tables, lens, starts, q.shape[0], max_q, max_len)
-    options = KvAttendOptions(_cache_dtype(cache, dtype, q), int(window), 0.0 if scale is None else _factor(scale, "scale"),
+    options = KvAttendOptions(_cache_dtype(cache, dtype, q), _int32(window, "window"),
+                              0.0 if scale is None else _factor(scale, "scale"),
                               _factor(softcap, "softcap") if softcap else 0.0, _factor(k_scale, "k_scale"),
                               _factor(v_scale, "v_scale"))
     if slopes is not None:
@@ -251,7 +261,7 @@ def kv_attend(cache: Cache, layer: int, q, tables, lens, starts=None, *, max_q=N
             lse = torch.empty(heads, dtype=torch.float32, device=q.device)
         workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
     outr = _rows(out, "out", layout.head_dim, device)
-    _raise(_lib.kv_attend(ctypes.byref(cache.struct), int(layer), ctypes.byref(batch), ctypes.byref(options),
+    _raise(_lib.kv_attend(ctypes.byref(cache.struct), _int32(layer, "layer"), ctypes.byref(batch), ctypes.byref(options),
                           ctypes.byref(qr), ctypes.byref(outr), lse.data_ptr(),
                           workspace.data_ptr() if need else None, need, handle))
     _used(stream, q, tables, lens, starts, slopes, weights, prior, out, lse)
@@ -271,20 +281,21 @@ def kv_keep(weights, lens, budget: int, *, sinks: int = 0, recent: int = 0, max_
     _ints(lens, "lens", 1, device, B)
     if max_len is not None and int(max_len) > L:
         raise ValueError(f"weights of {L} tokens for sequences of up to {max_len}")
+    budget, sinks, recent = _int32(budget, "budget"), _int32(sinks, "sinks"), _int32(recent, "recent")
     if budget < 1:
         raise ValueError(f"budget must be positive (got {budget})")
-    most = L if max_len is None else int(max_len)
-    need = _lib.kv_keep_workspace(B, H, most, int(budget))
+    most = _int32(L if max_len is None else max_len, "max_len")
+    need = _lib.kv_keep_workspace(B, H, most, budget)
     if need < 0:
         _raise(need)
     handle, here = _call_stream(stream)
     with here:
         workspace = torch.empty(need, dtype=torch.uint8, device=weights.device) if need else None
-        keep = torch.empty((B, H, int(budget)), dtype=torch.int32, device=weights.device)
+        keep = torch.empty((B, H, budget), dtype=torch.int32, device=weights.device)
         kept_lens = torch.empty(B, dtype=torch.int32, device=weights.device)
-        kept_weights = torch.empty((B, H, int(budget)), dtype=torch.float32, device=weights.device)
+        kept_weights = torch.empty((B, H, budget), dtype=torch.float32, device=weights.device)
     _raise(_lib.kv_keep(weights.data_ptr(), weights.stride(0), weights.stride(1), lens.data_ptr(), B, H,
-                        most, int(budget), int(sinks), int(recent), keep.data_ptr(), kept_lens.data_ptr(),
+                        most, budget, sinks, recent, keep.data_ptr(), kept_lens.data_ptr(),
                         kept_weights.data_ptr(), workspace.data_ptr() if need else None, need, handle))
     _used(stream, weights, lens)
     return keep, kept_lens, kept_weights
@@ -301,7 +312,7 @@ def kv_compact(cache: Cache, layer: int, tables, keep, kept_lens, dst_tables, *,
     _ints(kept_lens, "kept_lens", 1, device, B)
     _ints(dst_tables, "dst_tables", 2, device, B)
     handle, _ = _call_stream(stream)
-    _raise(_lib.kv_compact(ctypes.byref(cache.struct), int(layer), B, tables.data_ptr(), tables.stride(0), tables.shape[1],
+    _raise(_lib.kv_compact(ctypes.byref(cache.struct), _int32(layer, "layer"), B, tables.data_ptr(), tables.stride(0), tables.shape[1],
                            keep.data_ptr(), keep.shape[1], keep.shape[2], kept_lens.data_ptr(), dst_tables.data_ptr(),
                            dst_tables.stride(0), dst_tables.shape[1], handle))
     _used(stream, tables, keep, kept_lens, dst_tables)

@@ -137,3 +137,28 @@ def test_binding_refuses_factors_that_the_library_takes_for_defaults(host_cache)
     attend.kv_attend(cache, 0, rows, tables, lens, scale=0.25, softcap=0, k_scale=2, v_scale=1e-30)
     options = lib.args[3]._obj
     assert (options.scale, options.softcap, options.k_scale) == (0.25, 0.0, 2.0) and 0 < options.v_scale < 2e-30
+
+
+def test_binding_refuses_numbers_beyond_32_bits(host_cache):
+    """A window of 2^32 + 5 is none of 5 tokens, and layer 2^32 is not layer 0."""
+    from paper_2609_15021_amd import attend
+    cache, lib = host_cache
+    rows, kv = torch.zeros(2, 4, 64, dtype=torch.bfloat16), torch.zeros(2, 2, 64, dtype=torch.bfloat16)
+    tables, lens = torch.zeros(2, 4, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+    weights, keep = torch.zeros(2, 2, 64), torch.zeros(2, 2, 4, dtype=torch.int32)
+    calls = [lambda: attend.kv_append(cache, 2**32, kv, kv, tables, lens),
+             lambda: attend.kv_attend(cache, 2**32 + 1, rows, tables, lens),
+             lambda: attend.kv_attend(cache, 0, rows, tables, lens, window=2**32 + 5),
+             lambda: attend.kv_attend(cache, 0, rows[:1].expand(2**32 + 2, 4, 64), tables, lens,
+                                      torch.zeros(3, dtype=torch.int32)),
+             lambda: attend.kv_keep(weights, lens, 2**32 + 4), lambda: attend.kv_keep(weights, lens, 4, sinks=2**32),
+             lambda: attend.kv_keep(weights, lens, 4, recent=-2**33),
+             lambda: attend.kv_compact(cache, -2**32, tables, keep, lens, tables)]
+    for call in calls:
+        with pytest.raises(ValueError, match="32 bits"):
+            call()
+    assert lib.name in (None, "kv_attend_workspace")  # which enqueues nothing
+    attend.kv_attend(cache, 0, rows, tables, lens, max_len=2**40)
+    assert lib.args[2]._obj.max_len == 64
+    attend.kv_attend(cache, 0, rows, tables, lens, max_len=-2**32)
+    assert lib.args[2]._obj.max_len == -1
