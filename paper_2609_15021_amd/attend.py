@@ -95,6 +95,8 @@ def _on(t, name: str, device: int) -> None:
 def _floats(t, name: str, device: int, shape) -> None:
     if not isinstance(t, torch.Tensor) or t.dtype is not torch.float32 or t.shape != shape or not t.is_contiguous():
         raise TypeError(f"{name} must be a contiguous float32 device tensor of {tuple(shape)}")
+    if t.requires_grad and torch.is_grad_enabled():
+        _no_gradient(name)
     _on(t, name, device)
 
 
@@ -103,12 +105,21 @@ def _weights(t, name: str, device: int, rows=None) -> None:
             (t.stride(2) != 1 and t.shape[2] > 1 and t.numel()) or (rows is not None and t.shape[:2] != rows):
         raise TypeError(f"{name} must be a [sequences][heads][tokens] float32 device tensor with dense rows"
                         f"{'' if rows is None else f' ({rows} of them)'}")
+    if t.requires_grad and torch.is_grad_enabled():
+        _no_gradient(name)
     _on(t, name, device)
+
+
+def _no_gradient(name: str):
+    raise RuntimeError(f"{name} requires a gradient, and these operators have none: detach it, or call under "
+                       "torch.no_grad()")
 
 
 def _rows(t, name: str, head_dim: int, device: int) -> KvRows:
     if not isinstance(t, torch.Tensor) or t.dim() != 3 or t.dtype not in (torch.bfloat16, torch.float16):
         raise TypeError(f"{name} must be a [tokens][heads][D] device tensor of bfloat16 or float16")
+    if t.requires_grad and torch.is_grad_enabled():
+        _no_gradient(name)
     if t.get_device() != device:
         _elsewhere(t, name, device)
     _, heads, width = t.shape

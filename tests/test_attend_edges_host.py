@@ -162,3 +162,27 @@ def test_binding_refuses_numbers_beyond_32_bits(host_cache):
     assert lib.args[2]._obj.max_len == 64
     attend.kv_attend(cache, 0, rows, tables, lens, max_len=-2**32)
     assert lib.args[2]._obj.max_len == -1
+
+
+def test_binding_refuses_what_requires_a_gradient(host_cache):
+    """The operators have no backward pass: an output without one must not stand for it silently."""
+    from paper_2609_15021_amd import attend
+    cache, lib = host_cache
+    q, kv = torch.zeros(2, 4, 64, dtype=torch.bfloat16), torch.zeros(2, 2, 64, dtype=torch.bfloat16)
+    leaf_q, leaf_kv = q.clone().requires_grad_(), kv.clone().requires_grad_()
+    tables, lens = torch.zeros(2, 4, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+    weights, slopes = torch.zeros(2, 2, 64), torch.zeros(4)
+    leaf_w, leaf_s = weights.clone().requires_grad_(), slopes.clone().requires_grad_()
+    calls = [lambda: attend.kv_append(cache, 0, leaf_kv, kv, tables, lens),
+             lambda: attend.kv_append(cache, 0, kv, leaf_kv * 2, tables, lens),
+             lambda: attend.kv_attend(cache, 0, leaf_q, tables, lens),
+             lambda: attend.kv_attend(cache, 0, q, tables, lens, out=leaf_q.clone()),
+             lambda: attend.kv_attend(cache, 0, q, tables, lens, slopes=leaf_s),
+             lambda: attend.kv_attend(cache, 0, q, tables, lens, weights=weights, prior=leaf_w + 1),
+             lambda: attend.kv_keep(leaf_w, lens, 4)]
+    for call in calls:
+        with pytest.raises(RuntimeError, match="gradient"):
+            call()
+        with torch.no_grad():
+            call()
+    attend.kv_attend(cache, 0, leaf_q.detach(), tables, lens, slopes=leaf_s.detach())
