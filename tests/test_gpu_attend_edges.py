@@ -1,6 +1,10 @@
 """Edges of the operators on the paged cache: bounds at the ends of 32 bits, plans that only large batches reach, and
 streams that are not the current one.
 """
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -101,6 +105,63 @@ def test_weights_of_wide_bounds():
         assert not weights[b, :, n:].any()
 
 
+def fine(c, **options):
+    """(reference, bound of out) where the weights exp(s - m) meet V as two numbers of the rows' type: in place of half a
+    step of each weight, a half step of a half step (its square), and for float16 half of its smallest number, 2^-25, at
+    weights of which the largest is at least 2^7."""
+    want = ref.attend(c, **options)
+    c.v, v = [np.abs(x) for x in c.v], c.v
+    magnitude = ref.attend(c, **options)[0]
+    c.v = v
+    half = ref.HALF_STEP[c.dtype]
+    largest = max((np.abs(x).max() for x in c.v if x.size), default=0.0) * c.v_scale
+    tiny = max(c.lens) * 2.0**-32 * largest if c.dtype == F16 else 0.0
+    return want, want[3] - half * magnitude + half * half * magnitude + tiny
+
+
+@pytest.mark.parametrize("lens,new", [([1, 33, 700, 3000], [1, 1, 1, 1]), ([40, 300, 900], [2, 3, 4])])
+@pytest.mark.parametrize("H,G,D,fp8,dtype", [(2, 5, 128, False, BF16), (1, 16, 64, False, F16), (1, 6, 256, True, BF16),
+                                              (2, 12, 80, True, F16), (1, 4, 200, False, BF16)])
+def test_few_rows_round_once(H, G, D, fp8, dtype, lens, new):
+    """Sequences of up to 64 rows per KV head: only the output's rounding shows."""
+    c = ref.Case(H, G, D, 16, lens, new, fp8=fp8, dtype=dtype, seed=34 + D)
+    cache, _, q, _, _, tables, ln, starts = c.device()
+    out, lse = attend.kv_attend(cache, 0, q, tables, ln, starts, k_scale=c.k_scale, v_scale=c.v_scale)
+    want, off = fine(c)
+    ref.check(out, want[0], off, "out")
+    ref.check(lse, want[1], want[4], "lse")
+
+
+@pytest.mark.parametrize("D,dtype", [(128, BF16), (64, F16), (256, BF16)])
+def test_hundreds_of_parts(D, dtype):
+    """One sequence on one KV head, cut into more parts than the join reads at first."""
+    c = ref.Case(1, 2, D, 16, [33003], [1], dtype=dtype, seed=35 + D)
+    cache, _, q, _, _, tables, lens, _ = c.device()
+    weights = torch.zeros(1, 1, 33003, device=DEV)
+    out, lse = attend.kv_attend(cache, 0, q, tables, lens, weights=weights)
+    want, off = fine(c)
+    ref.check(out, want[0], off, "out")
+    ref.check(lse, want[1], want[4], "lse")
+    ref.check(weights, want[2], want[5], "weights")
+
+
+def test_more_sequences_than_one_round_lists():
+    """Over 1,024 sequences, long ones on both sides of the 1,024th, shared out in parts of 512 tokens and more."""
+    gen = np.random.default_rng(36)
+    lens = [int(n) for n in gen.integers(0, 12, 1100)]
+    for b, n in ((3, 700), (1023, 1300), (1024, 513), (1090, 1025)):
+        lens[b] = n
+    c = ref.Case(1, 2, 16, 8, lens, [1 if n % 7 else 0 for n in lens], seed=36)
+    cache, _, q, _, _, tables, ln, starts = c.device()
+    weights = torch.zeros(1100, 1, 1300, device=DEV)
+    out, lse = attend.kv_attend(cache, 0, q, tables, ln, starts, max_q=1, weights=weights)
+    want = ref.attend(c)
+    ref.check(out, want[0], want[3], "out")
+    ref.check(lse, want[1], want[4], "lse")
+    for b, n in enumerate(c.lens):
+        ref.check(weights[b, :, :n], want[2][b, :, :n], want[5][b, :, :n], "weights")
+
+
 def test_keep_rows_of_several_sets():
     """128 rows, some of more than 262,144 tokens, with ties on both sides of that and of twice that."""
     L, B = 2 * 262144 + 5000, 128
@@ -161,3 +222,138 @@ def test_one_token_with_any_stride(n):
     ref.check(lse, want[1], want[4], "lse")
     keep, kept, _ = attend.kv_keep(torch.ones(1, 1, 3 * n, device=DEV)[:, :, ::3][:, :, :1], meta[:, 0], 2)
     assert keep.tolist() == [[[-1, -1]]] and kept.tolist() == [0]
+
+
+def test_group_beyond_a_step():
+    """One new token of more query heads per KV head than the kernel for few rows takes."""
+    for fp8 in (False, True):
+        c = ref.Case(1, 100, 64, 16, [1, 130, 0], [1, 1, 1], fp8=fp8, seed=38)
+        cache, _, q, _, _, tables, lens, _ = c.device()
+        weights = torch.zeros(3, 1, 130, device=DEV)
+        out, lse = attend.kv_attend(cache, 0, q, tables, lens, k_scale=c.k_scale, v_scale=c.v_scale, weights=weights)
+        want = ref.attend(c)
+        ref.check(out, want[0], want[3], "out")
+        ref.check(lse, want[1], want[4], "lse")
+        for b, n in enumerate(c.lens):
+            ref.check(weights[b, :, :n], want[2][b, :, :n], want[5][b, :, :n], "weights")
+
+
+def _overwrite(*shapes):
+    """Fills what the allocator has free for tensors of these shapes on the current stream."""
+    for shape, dtype in shapes:
+        for _ in range(4):
+            torch.empty(shape, dtype=dtype, device=DEV).fill_(-3)
+
+
+def test_named_stream_keeps_what_it_reads():
+    """Calls on a stream that is behind: their inputs are dropped at once, and the memory that the allocator then hands
+    out on the current stream is overwritten before the calls run."""
+    c = ref.Case(2, 4, 128, 16, [300, 40], [1, 1], seed=39)
+    cache, t, q0, k0, v0, tables0, lens0, starts0 = c.device()
+    s = torch.cuda.Stream()
+    results, scales = [], (1.0, 0.5, -1.0, 0.25)
+    for scale in scales:
+        q, slopes = q0 * scale, torch.full((8,), 0.01, device=DEV)
+        tables, lens, starts = tables0.clone(), lens0.clone(), starts0.clone()
+        weights, prior = torch.zeros(2, 2, 300, device=DEV), torch.zeros(2, 2, 300, device=DEV)
+        s.wait_stream(torch.cuda.current_stream())
+        gpu.spin(20.0, s)
+        out, lse = attend.kv_attend(cache, 0, q, tables, lens, starts, slopes=slopes, weights=weights, prior=prior,
+                                    stream=s)
+        shapes = [(x.shape, x.dtype) for x in (q, slopes, tables, lens, starts, prior)]
+        del q, slopes, tables, lens, starts, prior
+        _overwrite(*shapes)
+        results.append((out, lse, weights))
+    torch.cuda.synchronize()
+    for scale, (out, lse, weights) in zip(scales, results):
+        d = ref.Case(2, 4, 128, 16, [300, 40], [1, 1], seed=39)
+        d.q = d.q * scale
+        want = ref.attend(d, slopes=np.full(8, float(np.float32(0.01))))
+        ref.check(out, want[0], want[3], "out")
+        ref.check(lse, want[1], want[4], "lse")
+        for b, n in enumerate(d.lens):
+            ref.check(weights[b, :, :n], want[2][b, :, :n], want[5][b, :, :n], "weights")
+
+    # The other calls, each behind a spin of its own.
+    w0 = torch.rand(2, 2, 300, device=DEV)
+    k, v, tables, lens = k0.clone(), v0.clone(), tables0.clone(), lens0.clone()
+    fresh0 = torch.tensor([c.free[:2]], **INTS)
+    w, keep0 = w0.clone(), torch.tensor([[[3, 9, 299]]], **INTS)
+    kept0 = torch.tensor([3], **INTS)
+    source, keep, kept, fresh = tables0[:1].clone(), keep0.clone(), kept0.clone(), fresh0.clone()
+    lens_again = lens0.clone()
+    s.wait_stream(torch.cuda.current_stream())
+    gpu.spin(20.0, s)
+    attend.kv_append(cache, 0, k, v, tables, lens, stream=s)
+    chosen = attend.kv_keep(w, lens_again, 50, sinks=1, recent=9, stream=s)
+    attend.kv_compact(cache, 0, source, keep, kept, fresh, stream=s)
+    shapes = [(x.shape, x.dtype) for x in (k, v, tables, lens, w, lens_again, source, keep, kept, fresh)]
+    del k, v, tables, lens, w, lens_again, source, keep, kept, fresh
+    _overwrite(*shapes)
+    torch.cuda.synchronize()
+    want = ref.keep(w0.cpu().numpy(), c.lens, 50, 1, 9)
+    assert torch.equal(chosen[0].cpu(), torch.from_numpy(want[0])) and np.array_equal(chosen[2].cpu().numpy(), want[2])
+    now = t.cpu().view(c.num_blocks, *c.shape)
+    for b, n in enumerate(c.lens):
+        page = now[int(c.tables[b, (n - 1) // 16])]
+        assert torch.equal(page[0, :, (n - 1) % 16], c.new_k[b]) and torch.equal(page[1, :, (n - 1) % 16], c.new_v[b])
+    moved = now[c.free[0]]
+    for j, token in enumerate((3, 9)):
+        np.testing.assert_array_equal(moved[0, :, j].double().numpy(), c.k[0][token])
+        np.testing.assert_array_equal(moved[1, :, j].double().numpy(), c.v[0][token])
+    assert torch.equal(moved[0, :, 2], c.new_k[0])
+
+
+def test_two_calls_at_once():
+    """Two streams, each with calls of its own in a row: no workspace is shared."""
+    cases = [ref.Case(2, 5, 128, 16, [5000, 17], [1, 1], seed=40), ref.Case(2, 5, 128, 16, [5000, 900], [40, 100], seed=41)]
+    state, want = [c.device() for c in cases], [ref.attend(c) for c in cases]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    results = [[], []]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for i, (s, (cache, _, q, _, _, tables, lens, starts)) in enumerate(zip(streams, state)):
+            weights = torch.zeros(2, 2, 5000, device=DEV)
+            s.wait_stream(torch.cuda.current_stream())
+            results[i].append((*attend.kv_attend(cache, 0, q, tables, lens, starts, weights=weights, stream=s), weights))
+    torch.cuda.synchronize()
+    for c, got, (out, lse, weights, out_off, lse_off, weights_off) in zip(cases, results, want):
+        ref.check(got[0][0], out, out_off, "out")
+        ref.check(got[0][1], lse, lse_off, "lse")
+        for b, n in enumerate(c.lens):
+            ref.check(got[0][2][b, :, :n], weights[b, :, :n], weights_off[b, :, :n], "weights")
+        for again in got[1:]:
+            for x, y in zip(got[0], again):
+                assert torch.equal(x, y)
+
+
+FIRST_CALL_CAPTURED = """
+import sys
+sys.path[:0] = sys.argv[1:]
+import torch
+import attend_reference as ref
+from paper_2609_15021_amd import attend
+c = ref.Case(2, 4, 64, 16, [300, 40], [1, 1], seed=42)
+cache, _, q, k, v, tables, lens, _ = c.device()
+weights = torch.zeros(2, 2, 300, device=ref.DEV)
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    out, lse = attend.kv_attend(cache, 0, q, tables, lens, weights=weights)
+want = ref.attend(c)
+for _ in range(3):
+    out.zero_()
+    torch.cuda.synchronize()
+    graph.replay()
+    torch.cuda.synchronize()
+    ref.check(out, want[0], want[3], "out")
+    ref.check(lse, want[1], want[4], "lse")
+print("replayed")
+"""
+
+
+def test_first_call_of_a_process_may_be_captured():
+    here = os.path.dirname(os.path.abspath(__file__))
+    got = subprocess.run([sys.executable, "-c", FIRST_CALL_CAPTURED, here, os.path.dirname(here)], capture_output=True,
+                         text=True, timeout=100)
+    assert got.returncode == 0 and "replayed" in got.stdout, got.stderr[-2000:]
