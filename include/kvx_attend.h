@@ -30,8 +30,8 @@
  *   KV_ASYNC_BAD_BLOCK  a block id outside [0, num_blocks): that page is neither read nor written, and its tokens
  *                       take part in nothing;
  *   KV_ASYNC_BAD_BATCH  a length outside [0, max_len], or rows outside [0, num_queries] or more than max_queries: the
- *                       sequence is left out, and nothing of its outputs is written; a kept token outside its
- *                       sequence's table, or more kept tokens than the budget, likewise.
+ *                       sequence is left out, and nothing of its outputs is written; more kept tokens than the budget,
+ *                       likewise.  A kept token outside its sequence's table: that row alone is not moved.
  * ---------------------------------------------------------------------------
  */
 #ifndef KVX_ATTEND_H
@@ -111,7 +111,7 @@ KV_API kv_status kv_append(const kv_cache *cache, int32_t layer, const kv_batch 
  * type for sequences of up to 64 rows (new tokens times query heads) per KV head, and as one, rounded to nearest, for
  * longer ones (off by up to half a step of that type each).  What slots behind a sequence's last token hold does not
  * matter, but its own tokens' V are taken to be finite: 0 times an infinity of a token that a row does not see reaches
- * that row.
+ * that row.  K of a token reaches the rows that see it and no others; where it is not finite, they may become NaN.
  *   q, out:    [num_queries][query heads][D], same type; the cache's, or either 2-byte type for E4M3; rows of out do not
  *              overlap;
  *   lse:       DEVICE float[num_queries][query heads], or NULL;
@@ -156,7 +156,10 @@ KV_API int64_t kv_keep_workspace(int32_t num_seqs, int32_t heads, int32_t max_le
  * token keep[b][h][j] of source becomes token j of the destination, for KV head h (heads == 1: keep[b][0][j] for every
  * head).  Destination pages are distinct, and none of them is a source page of the call (precondition; otherwise the
  * result depends on the order of reads and writes): pages of a shared prefix stay as they are for their other users.
- * Every other byte of the cache is untouched.
+ * Every other byte of the cache is untouched.  From then on a kept token's place is its new slot: later calls count
+ * causality, `window` and `slopes` in those, so distances to kept tokens shrink by what was left out between (for each
+ * head by what that head left out).  A caller whose bias goes by the old distances has to carry it elsewhere, for
+ * example in K, as rotated embeddings do.
  *   block_tables, dst_tables: DEVICE int32[num_seqs][stride], of which table_len and dst_len entries may be read.
  * Errors: KV_EINVAL (NULL, sizes; budget > dst_len * BS), KV_EUNSUPPORTED as kv_append, KV_EHIP.
  */

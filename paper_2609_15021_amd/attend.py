@@ -6,8 +6,8 @@ Every step runs in the HIP library that ``kvx`` binds (``libkvx.so``); caches ar
 A batch of sequences is ``tables`` (int32 [B][pages]: block tables), ``lens`` (int32 [B]: tokens in the cache, the new
 ones among them) and ``starts`` (int32 [B + 1]: where each sequence's new tokens start among all; None: one each).  All
 three are device tensors; ``max_q`` and ``max_len`` are the host's bounds of new tokens and tokens per sequence, by
-default (and at most) what the shapes allow.  Tight bounds size the launches better; numbers beyond them are refused on the device
-(``kv_attend_async_error``).
+default (and at most) what the shapes allow.  Tight bounds size the launches better; numbers beyond them are refused on
+the device (``kv_attend_async_error``), and such a sequence's rows of the outputs hold what they held before.
 """
 from __future__ import annotations
 
@@ -195,7 +195,8 @@ def _used(stream, *tensors) -> None:
 
 def kv_append(cache: Cache, layer: int, k, v, tables, lens, starts=None, *, max_q=None, max_len=None, dtype=None,
               k_scale: float = 1.0, v_scale: float = 1.0, stream=None) -> None:
-    """Write the new tokens' rows ``k`` and ``v`` ([tokens][H][D], any token and head strides) into layer ``layer``.
+    """Write the new tokens' rows ``k`` and ``v`` ([tokens][H][D], token and head strides of whole 16 bytes) into layer
+    ``layer``.
 
     ``dtype``: the cache's; by default that of ``k``, or float8_e4m3fn in a cache of 1-byte elements, where x is stored
     as e4m3(x / scale).
@@ -215,12 +216,12 @@ def kv_append(cache: Cache, layer: int, k, v, tables, lens, starts=None, *, max_
 def kv_attend(cache: Cache, layer: int, q, tables, lens, starts=None, *, max_q=None, max_len=None, dtype=None,
               scale=None, softcap: float = 0.0, window: int = 0, slopes=None, k_scale: float = 1.0, v_scale: float = 1.0,
               weights=None, prior=None, out=None, lse=None, stream=None):
-    """Attention of the new tokens' queries ``q`` ([tokens][query heads][D], any token and head strides) over layer
-    ``layer``; returns (out, lse).
+    """Attention of the new tokens' queries ``q`` ([tokens][query heads][D], token and head strides of whole 16 bytes)
+    over layer ``layer``; returns (out, lse).
 
     ``weights`` (float32 [B][H][>= max_len]): receives ``prior`` (same shape and strides; None: 0) plus what each cached
     token got in this call; ``prior=weights`` accumulates in place.  ``out`` (like ``q``) and ``lse`` (float32 [tokens]
-    [query heads]) are made if not given; rows that belong to no sequence are left as they were.
+    [query heads]) are made if not given, and overlap no input; rows that belong to no sequence are left as they were.
     """
     device = cache.struct.device
     qr = _rows(q, "q", cache.layout.head_dim, device)
@@ -315,7 +316,7 @@ def kv_keep(weights, lens, budget: int, *, sinks: int = 0, recent: int = 0, max_
 def kv_compact(cache: Cache, layer: int, tables, keep, kept_lens, dst_tables, *, stream=None) -> None:
     """Copy the kept tokens' rows of layer ``layer`` into the pages of ``dst_tables``: token ``keep[b][h][j]`` becomes
     token j (``keep`` int32 [B][H or 1][budget], contiguous; ``kept_lens`` int32 [B] of them count).  The destination's
-    pages are distinct and none of the sources'."""
+    pages are distinct and none of the sources'.  ``window`` and ``slopes`` of later calls count in the new places."""
     device = cache.struct.device
     B = _ints(tables, "tables", 2, device).shape[0]
     if not _ints(keep, "keep", 3, device, B).is_contiguous():
