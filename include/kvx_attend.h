@@ -91,6 +91,8 @@ typedef struct kv_attend_options {
     const float *weights_in;  /* DEVICE */
     float *weights_out;       /* DEVICE, or NULL */
     int64_t weights_seq_stride, weights_head_stride;  /* elements; rows of max_len elements do not overlap */
+    int32_t full_weights;     /* 1: exp(s) meets V as two numbers of q's type in every sequence (see kv_attend) */
+    int32_t reserved;         /* must be 0 */
 } kv_attend_options;
 
 /*
@@ -107,11 +109,13 @@ KV_API kv_status kv_append(const kv_cache *cache, int32_t layer, const kv_batch 
 /*
  * kv_attend -- out[row] = v_scale * sum over its tokens of softmax(s) * v, rounded once to q's type, and lse[row] = log
  * of the sum of exp(s), for every new row; query head h reads KV head h / (q->heads / H).  A row that sees no token
- * gets 0 and -infinity.  Sums, largest scores and lse are held in 32 bits; the weights exp(s) meet V as two numbers of q's
- * type for sequences of up to 64 rows (new tokens times query heads) per KV head, and as one, rounded to nearest, for
- * longer ones (off by up to half a step of that type each).  What slots behind a sequence's last token hold does not
- * matter, but its own tokens' V are taken to be finite: 0 times an infinity of a token that a row does not see reaches
- * that row.  K of a token reaches the rows that see it and no others; where it is not finite, they may become NaN.
+ * gets 0 and -infinity.  Sums, largest scores and lse are held in 32 bits.  The weights exp(s) meet V as two numbers of
+ * q's type (the rounded weight and what it leaves) for sequences of up to 64 rows (new tokens times query heads) per KV
+ * head, so that only the output's rounding shows.  For longer ones they are one number, rounded to nearest (off by up to
+ * half a step of that type each), unless full_weights asks for two there as well.  What slots behind a sequence's last
+ * token hold does not matter, but its own tokens' V are taken to be finite: 0 times an infinity of a token that a row
+ * does not see reaches that row.  K of a token reaches the rows that see it and no others; where it is not finite, they
+ * may become NaN.
  *   q, out:    [num_queries][query heads][D], same type; the cache's, or either 2-byte type for E4M3; rows of out do not
  *              overlap;
  *   lse:       DEVICE float[num_queries][query heads], or NULL;

@@ -45,7 +45,8 @@ class KvAttendOptions(ctypes.Structure):
     _fields_ = [("cache_dtype", ctypes.c_int32), ("window", ctypes.c_int32), ("scale", ctypes.c_float),
                 ("softcap", ctypes.c_float), ("k_scale", ctypes.c_float), ("v_scale", ctypes.c_float),
                 ("slopes", ctypes.c_void_p), ("weights_in", ctypes.c_void_p), ("weights_out", ctypes.c_void_p),
-                ("weights_seq_stride", ctypes.c_int64), ("weights_head_stride", ctypes.c_int64)]
+                ("weights_seq_stride", ctypes.c_int64), ("weights_head_stride", ctypes.c_int64),
+                ("full_weights", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
 def _declare(lib):
@@ -215,12 +216,14 @@ def kv_append(cache: Cache, layer: int, k, v, tables, lens, starts=None, *, max_
 
 def kv_attend(cache: Cache, layer: int, q, tables, lens, starts=None, *, max_q=None, max_len=None, dtype=None,
               scale=None, softcap: float = 0.0, window: int = 0, slopes=None, k_scale: float = 1.0, v_scale: float = 1.0,
-              weights=None, prior=None, out=None, lse=None, stream=None):
+              weights=None, prior=None, full_weights: bool = False, out=None, lse=None, stream=None):
     """Attention of the new tokens' queries ``q`` ([tokens][query heads][D], token and head strides of whole 16 bytes)
     over layer ``layer``; returns (out, lse).
 
     ``weights`` (float32 [B][H][>= max_len]): receives ``prior`` (same shape and strides; None: 0) plus what each cached
-    token got in this call; ``prior=weights`` accumulates in place.  ``out`` (like ``q``) and ``lse`` (float32 [tokens]
+    token got in this call; ``prior=weights`` accumulates in place.  ``full_weights``: sequences of more than 64 rows (new
+    tokens times query heads) per KV head take exp(s) to V as two numbers of q's type, as shorter ones always do, for up
+    to 1.3 times the time; then the output's rounding alone shows.  ``out`` (like ``q``) and ``lse`` (float32 [tokens]
     [query heads]) are made if not given, and overlap no input; rows that belong to no sequence are left as they were.
     """
     device = cache.struct.device
@@ -230,6 +233,8 @@ def kv_attend(cache: Cache, layer: int, q, tables, lens, starts=None, *, max_q=N
                               0.0 if scale is None else _factor(scale, "scale"),
                               _factor(softcap, "softcap") if softcap else 0.0, _factor(k_scale, "k_scale"),
                               _factor(v_scale, "v_scale"))
+    if full_weights:
+        options.full_weights = 1
     if slopes is not None:
         _floats(slopes, "slopes", device, (q.shape[1],))
         options.slopes = slopes.data_ptr()

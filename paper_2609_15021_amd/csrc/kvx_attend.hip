@@ -59,6 +59,9 @@ kv_status check_attend(const kv_cache *cache, const kv_batch *batch, const kv_at
     if (!(product >= 1e-36f && product <= 1e36f) || !(inv >= 1e-36f && inv <= 1e36f))
         return fail(KV_EUNSUPPORTED, "scale %g with k_scale %g and softcap %g is beyond 32-bit scores", o->scale, o->k_scale,
                     o->softcap);
+    if ((o->full_weights != 0 && o->full_weights != 1) || o->reserved != 0)
+        return fail(KV_EINVAL, "full_weights must be 0 or 1 and reserved 0 (got %d and %d)", o->full_weights,
+                    o->reserved);
     if (o->weights_in && !o->weights_out)
         return fail(KV_EINVAL, "weights_in without weights_out");
     // Rows are counted in 32 bits, and the tail kernel's workgroups by what one launch takes.
@@ -246,6 +249,7 @@ kv_status attend(const kv_cache *cache, int32_t layer, const kv_batch *batch, co
     a.num_seqs = batch->num_seqs;
     a.q_type = q->dtype;
     a.cache_type = o->cache_dtype;
+    a.full_weights = o->full_weights;
     a.by_group = divisor(a.group);
     if (plan.max_queries > 0) {
         if (plan.listed)

@@ -24,6 +24,7 @@ struct AttendArgs {
     int32_t window, heads, group, num_seqs;
     Divisor by_group;
     int32_t q_type, cache_type;
+    int32_t full_weights;
     float *scores;  // [sequence][KV head][score_cap][score_len] in powers of 2, for weights_out; or NULL
     int64_t score_len;
     int32_t score_cap;

@@ -77,24 +77,25 @@ __device__ __forceinline__ u32x2 read_turned(lds_byte *p) {
                               __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<__attribute__((address_space(3))) s16x4 *>(p)));
 }
 
-// Asks the compiler to keep `ahead` LDS reads (of `reads` instructions) in flight before the first of `products`
-// products, and to issue one more, and `others` vector instructions, after each.
-template <int PRODUCTS, int READS, int AHEAD, int OTHERS>
+// Asks the compiler to keep `AHEAD` sets of `READS` LDS reads in flight before the first of `SETS` sets of `PRODUCTS`
+// products that take one each, and to issue one more after each.
+template <int SETS, int PRODUCTS, int READS, int AHEAD>
 __device__ __forceinline__ void interleave() {
-    constexpr int kVector = 0x2, kProduct = 0x8, kRead = 0x100;
+    constexpr int kProduct = 0x8, kRead = 0x100;
     __builtin_amdgcn_sched_group_barrier(kRead, AHEAD * READS, 0);
 #pragma unroll
-    for (int i = 0; i < PRODUCTS; ++i) {
-        __builtin_amdgcn_sched_group_barrier(kProduct, 1, 0);
-        if (i < PRODUCTS - AHEAD)
+    for (int i = 0; i < SETS; ++i) {
+        __builtin_amdgcn_sched_group_barrier(kProduct, PRODUCTS, 0);
+        if (i < SETS - AHEAD)
             __builtin_amdgcn_sched_group_barrier(kRead, READS, 0);
-        if (OTHERS > 0)
-            __builtin_amdgcn_sched_group_barrier(kVector, OTHERS, 0);
     }
 }
 
-// RW: rows of a wave, 32 (products of 32x32x16) or 16 (16x16x32).  PLAIN: neither a cap nor slopes.
-template <class T, bool FP8, int DP, int TK, int RW, bool PLAIN>
+// RW: rows of a wave, 32 (products of 32x32x16) or 16 (16x16x32).  PLAIN: neither a cap nor slopes.  FULL: weights meet
+// V as two numbers of T, the second being what the first leaves, so that the output's rounding alone shows: off by 0.00166
+// of its norm (bf16).  Else one, rounded, since a second product and its operands cost 1.28 times the time for the turn
+// above (2.00 ms instead of 1.57) and 1.18 for the ragged tails (0.78 instead of 0.66): 0.00225 and 0.00233.
+template <class T, bool FP8, int DP, int TK, int RW, bool PLAIN, bool FULL>
 __global__ __launch_bounds__(64 * kRows / RW, 2) void tail_kernel(const AttendArgs a, const Parts parts, const int tiles) {
     constexpr int E = FP8 ? 1 : 2;
     constexpr int ROW = 2 * DP;                     // bytes of a row in LDS
@@ -307,7 +308,7 @@ __global__ __launch_bounds__(64 * kRows / RW, 2) void tail_kernel(const AttendAr
             for (int x = 0; x < NS; ++x)
                 s[t][x] = sum[x / AN][x % AN];
         }
-        interleave<TB * SETS_K * KS, 1, 6, 0>();
+        interleave<TB * SETS_K * KS, 1, 1, 6>();
     };
     // The largest over the lanes that share a row.
     const auto over_parts = [](float x) {
@@ -392,7 +393,7 @@ __global__ __launch_bounds__(64 * kRows / RW, 2) void tail_kernel(const AttendAr
                         acc[d][x] *= f;
             }
             const float zero = m - T::kShift;
-            u32x4 p[TB][SETS];
+            u32x4 p[TB][SETS], p_rest[TB][FULL ? SETS : 1];
             float sums[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int t = 0; t < TB; ++t)
@@ -402,7 +403,10 @@ __global__ __launch_bounds__(64 * kRows / RW, 2) void tail_kernel(const AttendAr
                     const float e1 = __builtin_amdgcn_exp2f(fmaf(s[t][x + 1], factor, -zero));
                     sums[x & 2] += e0;
                     sums[(x & 2) + 1] += e1;
-                    p[t][x >> 3][x >> 1 & 3] = T::pack(e0, e1);
+                    const uint32_t w = T::pack(e0, e1);
+                    p[t][x >> 3][x >> 1 & 3] = w;
+                    if constexpr (FULL)
+                        p_rest[t][x >> 3][x >> 1 & 3] = T::pack(e0 - T::low(w), e1 - T::high(w));
                 }
             l += (sums[0] + sums[1]) + (sums[2] + sums[3]);
             // (e4m3: K of the next round is widened beside the other wave's products, V after this one's; 0.665 ms instead of
@@ -421,8 +425,10 @@ __global__ __launch_bounds__(64 * kRows / RW, 2) void tail_kernel(const AttendAr
                         lds_byte *at = v_lds + (v_at ^ d * 2 * RW) + (t * 32 + j * 16) * ROW;
                         const u32x2 x = read_turned(at), y = read_turned(at + (WIDE ? 8 : 4) * ROW);
                         acc[d] = product(u32x4{x[0], x[1], y[0], y[1]}, p[t][j], acc[d], T{});
+                        if constexpr (FULL)
+                            acc[d] = product(u32x4{x[0], x[1], y[0], y[1]}, p_rest[t][j], acc[d], T{});
                     }
-            interleave<TB * SETS * DB, 2, 3, 0>();
+            interleave<TB * SETS * DB, FULL ? 2 : 1, 2, 3>();
             __builtin_amdgcn_s_setprio(0);
             if (!more)
                 break;
@@ -591,28 +597,32 @@ __global__ __launch_bounds__(64 * kWeighWaves) void weigh_kernel(const AttendArg
     }
 }
 
-template <class T, bool FP8, int DP, int TK, int RW, bool PLAIN>
+template <class T, bool FP8, int DP, int TK, int RW, bool PLAIN, bool FULL>
 hipError_t launch(const AttendArgs &a, const Parts &parts, int max_queries, hipStream_t stream) {
     const int tiles = static_cast<int>(tail_tiles(max_queries, a.group));
     const uint32_t grid = static_cast<uint32_t>(tiles) * parts.splits * a.pages.H * a.num_seqs;
-    return launch_kernel(tail_kernel<T, FP8, DP, TK, RW, PLAIN>, dim3(grid), 64 * kRows / RW, stream, a, parts, tiles);
+    return launch_kernel(tail_kernel<T, FP8, DP, TK, RW, PLAIN, FULL>, dim3(grid), 64 * kRows / RW, stream, a, parts,
+                         tiles);
 }
 
-template <class T, bool FP8, bool PLAIN>
+template <class T, bool FP8, bool PLAIN, bool FULL>
 hipError_t launch(const AttendArgs &a, const Parts &parts, int max_queries, hipStream_t stream) {
     // (Wide rows: 32 of them would need more registers than two waves of a SIMD have, and one wave alone took 1.7 times
     // as long.)
     if (a.pages.D > 128)
-        return launch<T, FP8, 256, 64, 16, PLAIN>(a, parts, max_queries, stream);
+        return launch<T, FP8, 256, 64, 16, PLAIN, FULL>(a, parts, max_queries, stream);
     if (a.pages.D > 64)
-        return launch<T, FP8, 128, 64, 32, PLAIN>(a, parts, max_queries, stream);
-    return launch<T, FP8, 64, 64, 32, PLAIN>(a, parts, max_queries, stream);
+        return launch<T, FP8, 128, 64, 32, PLAIN, FULL>(a, parts, max_queries, stream);
+    return launch<T, FP8, 64, 64, 32, PLAIN, FULL>(a, parts, max_queries, stream);
 }
 
 template <class T, bool FP8>
 hipError_t launch(const AttendArgs &a, const Parts &parts, int max_queries, hipStream_t stream) {
-    return a.softcap == 0.f && !a.slopes ? launch<T, FP8, true>(a, parts, max_queries, stream)
-                                         : launch<T, FP8, false>(a, parts, max_queries, stream);
+    if (a.softcap == 0.f && !a.slopes)
+        return a.full_weights ? launch<T, FP8, true, true>(a, parts, max_queries, stream)
+                              : launch<T, FP8, true, false>(a, parts, max_queries, stream);
+    return a.full_weights ? launch<T, FP8, false, true>(a, parts, max_queries, stream)
+                          : launch<T, FP8, false, false>(a, parts, max_queries, stream);
 }
 
 template <class T, bool FP8, bool SHARED>

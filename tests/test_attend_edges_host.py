@@ -186,3 +186,19 @@ def test_binding_refuses_what_requires_a_gradient(host_cache):
         with torch.no_grad():
             call()
     attend.kv_attend(cache, 0, leaf_q.detach(), tables, lens, slopes=leaf_s.detach())
+
+
+def test_full_weights_is_a_choice_of_two(host_cache):
+    from paper_2609_15021_amd import attend, kvx
+    cache, batch, rows = _cache(kvx, kvx.make_layout(1, 2, 64, 2, 16, 16)), _batch(attend), _rows(attend, 4)
+    for fields, fine in ((dict(full_weights=1), True), (dict(full_weights=2), False), (dict(full_weights=-1), False),
+                         (dict(reserved=1), False)):
+        o = attend.KvAttendOptions(cache_dtype=attend.KV_DTYPE_BF16, **fields)
+        need = kvx._lib.kv_attend_workspace(ctypes.byref(cache), ctypes.byref(batch), ctypes.byref(o), ctypes.byref(rows))
+        assert need >= 0 if fine else need == kvx.KV_EINVAL, fields
+    handle, lib = host_cache
+    q = torch.zeros(2, 4, 64, dtype=torch.bfloat16)
+    tables, lens = torch.zeros(2, 4, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+    for full in (False, True):
+        attend.kv_attend(handle, 0, q, tables, lens, full_weights=full)
+        assert lib.args[3]._obj.full_weights == full

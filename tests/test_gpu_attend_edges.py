@@ -132,6 +132,33 @@ def test_few_rows_round_once(H, G, D, fp8, dtype, lens, new):
     ref.check(lse, want[1], want[4], "lse")
 
 
+@pytest.mark.parametrize("options", [{}, dict(softcap=5.0, window=90), dict(slopes=True)])
+@pytest.mark.parametrize("lens,new", [([100, 33, 700], [100, 1, 70]), ([3000, 130], [70, 129])])
+@pytest.mark.parametrize("H,G,D,fp8,dtype", [(2, 2, 128, False, BF16), (1, 3, 64, False, F16), (1, 2, 256, True, BF16),
+                                              (1, 4, 80, True, F16), (1, 2, 200, False, F16), (1, 1, 64, True, BF16)])
+def test_full_weights_round_once(H, G, D, fp8, dtype, lens, new, options):
+    """Sequences of more than 64 rows too, whole and in parts, where the caller asks for it; lse and what tokens receive
+    are the same either way."""
+    c = ref.Case(H, G, D, 16, lens, new, fp8=fp8, dtype=dtype, seed=45 + D)
+    cache, _, q, _, _, tables, ln, starts = c.device()
+    plain = dict(options)
+    if options.get("slopes"):
+        plain["slopes"] = np.array([2.0**-(1 + i % 7) for i in range(H * G)])
+        options = dict(slopes=torch.tensor(plain["slopes"], dtype=torch.float32, device=DEV))
+    got = []
+    for full in (True, False):
+        weights = torch.zeros(len(lens), H, max(lens), device=DEV)
+        got.append((*attend.kv_attend(cache, 0, q, tables, ln, starts, k_scale=c.k_scale, v_scale=c.v_scale, **options,
+                                      weights=weights, full_weights=full), weights))
+    want, off = fine(c, **plain)
+    ref.check(got[0][0], want[0], off, "out")
+    ref.check(got[0][1], want[1], want[4], "lse")
+    ref.check(got[1][0], want[0], want[3], "out")
+    assert torch.equal(got[0][1], got[1][1]) and torch.equal(got[0][2], got[1][2])
+    few = slice(int(c.starts[1]), int(c.starts[2])) if new[1] * G <= 64 else slice(0, 0)
+    assert torch.equal(got[0][0][few], got[1][0][few])
+
+
 @pytest.mark.parametrize("D,dtype", [(128, BF16), (64, F16), (256, BF16)])
 def test_hundreds_of_parts(D, dtype):
     """One sequence on one KV head, cut into more parts than the join reads at first."""
