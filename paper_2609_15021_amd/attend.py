@@ -117,39 +117,39 @@ def _no_gradient(name: str):
 
 
 def _rows(t, name: str, head_dim: int, device: int) -> KvRows:
-    if not isinstance(t, torch.Tensor) or t.dim() != 3 or t.dtype not in (torch.bfloat16, torch.float16):
+    if not isinstance(t, torch.Tensor) or len(shape := t.shape) != 3 or \
+            (dtype := t.dtype) not in (torch.bfloat16, torch.float16):
         raise TypeError(f"{name} must be a [tokens][heads][D] device tensor of bfloat16 or float16")
     if t.requires_grad and torch.is_grad_enabled():
         _no_gradient(name)
     if t.get_device() != device:
         _elsewhere(t, name, device)
-    _, heads, width = t.shape
+    _, heads, width = shape
     token, head, column = t.stride()
     if width != head_dim or (column != 1 and t.numel()):
         raise ValueError(f"{name}: rows of {width} elements {column} apart; dense rows of {head_dim} are needed")
-    return KvRows(t.data_ptr(), token, head, heads, _DTYPES[t.dtype])
+    return KvRows(t.data_ptr(), token, head, heads, _DTYPES[dtype])
 
 
 def _factor(x, name: str) -> float:
     """A factor that the caller named; the ABI takes 0 in 32 bits for its default, which is not what 0 means here."""
-    x = float(x)
-    if x != 1.0 and ctypes.c_float(x).value == 0.0:
-        raise ValueError(f"{name} must be above 0 in 32 bits (got {x:g})")
-    return x
+    if -2.0**-150 <= x <= 2.0**-150:
+        raise ValueError(f"{name} must be above 0 in 32 bits (got {x})")
+    return float(x)
 
 
 def _int32(x, name: str) -> int:
     """ctypes would cut a longer number to its low 32 bits."""
-    x = int(x)
     if not -2**31 <= x < 2**31:
         raise ValueError(f"{name} must fit 32 bits (got {x})")
-    return x
+    return int(x)
 
 
 def _batch(cache: Cache, tables, lens, starts, tokens: int, max_q, max_len) -> KvBatch:
     device = cache.struct.device
     B, pages = _ints(tables, "tables", 2, device).shape
-    _int32(tokens, "the number of new tokens")
+    if tokens >= 2**31:
+        _int32(tokens, "the number of new tokens")
     _ints(lens, "lens", 1, device, B)
     if starts is None:
         if tokens != B:
@@ -159,8 +159,9 @@ def _batch(cache: Cache, tables, lens, starts, tokens: int, max_q, max_len) -> K
         starts_at = _ints(starts, "starts", 1, device, B + 1).data_ptr()
         max_q = max(1, tokens if max_q is None else min(tokens, int(max_q)))
     most = min(pages * cache.layout.block_size, 2**31 - 1024)
-    return KvBatch(B, max_q, tokens, most if max_len is None else min(most, max(int(max_len), -1)), pages, 0, tables.stride(0),
-                   tables.data_ptr(), lens.data_ptr(), starts_at)
+    if max_len is not None:
+        most = min(most, max(int(max_len), -1))
+    return KvBatch(B, max_q, tokens, most, pages, 0, tables.stride(0), tables.data_ptr(), lens.data_ptr(), starts_at)
 
 
 def _cache_dtype(cache: Cache, dtype, rows) -> int:
@@ -209,8 +210,12 @@ def kv_append(cache: Cache, layer: int, k, v, tables, lens, starts=None, *, max_
         raise ValueError(f"k and v differ in shape: {tuple(k.shape)} and {tuple(v.shape)}")
     batch = _batch(cache, tables, lens, starts, k.shape[0], max_q, max_len)
     handle, _ = _call_stream(stream)
-    _raise(_lib.kv_append(ctypes.byref(cache.struct), _int32(layer, "layer"), ctypes.byref(batch), ctypes.byref(kr), ctypes.byref(vr),
-                          _cache_dtype(cache, dtype, k), _factor(k_scale, "k_scale"), _factor(v_scale, "v_scale"), handle))
+    if k_scale != 1.0 or v_scale != 1.0:
+        k_scale, v_scale = _factor(k_scale, "k_scale"), _factor(v_scale, "v_scale")
+    else:
+        k_scale = v_scale = 1.0
+    _raise(_lib.kv_append(ctypes.byref(cache.struct), _int32(layer, "layer"), ctypes.byref(batch), ctypes.byref(kr),
+                          ctypes.byref(vr), _cache_dtype(cache, dtype, k), k_scale, v_scale, handle))
     _used(stream, k, v, tables, lens, starts)
 
 
@@ -229,10 +234,13 @@ def kv_attend(cache: Cache, layer: int, q, tables, lens, starts=None, *, max_q=N
     device = cache.struct.device
     qr = _rows(q, "q", cache.layout.head_dim, device)
     batch = _batch(cache, tables, lens, starts, q.shape[0], max_q, max_len)
-    options = KvAttendOptions(_cache_dtype(cache, dtype, q), _int32(window, "window"),
+    if k_scale != 1.0 or v_scale != 1.0:
+        k_scale, v_scale = _factor(k_scale, "k_scale"), _factor(v_scale, "v_scale")
+    else:
+        k_scale = v_scale = 1.0
+    options = KvAttendOptions(_cache_dtype(cache, dtype, q), _int32(window, "window") if window else 0,
                               0.0 if scale is None else _factor(scale, "scale"),
-                              _factor(softcap, "softcap") if softcap else 0.0, _factor(k_scale, "k_scale"),
-                              _factor(v_scale, "v_scale"))
+                              _factor(softcap, "softcap") if softcap else 0.0, k_scale, v_scale)
     if full_weights:
         options.full_weights = 1
     if slopes is not None:
@@ -329,9 +337,9 @@ def kv_compact(cache: Cache, layer: int, tables, keep, kept_lens, dst_tables, *,
     _ints(kept_lens, "kept_lens", 1, device, B)
     _ints(dst_tables, "dst_tables", 2, device, B)
     handle, _ = _call_stream(stream)
-    _raise(_lib.kv_compact(ctypes.byref(cache.struct), _int32(layer, "layer"), B, tables.data_ptr(), tables.stride(0), tables.shape[1],
-                           keep.data_ptr(), keep.shape[1], keep.shape[2], kept_lens.data_ptr(), dst_tables.data_ptr(),
-                           dst_tables.stride(0), dst_tables.shape[1], handle))
+    _raise(_lib.kv_compact(ctypes.byref(cache.struct), _int32(layer, "layer"), B, tables.data_ptr(), tables.stride(0),
+                           tables.shape[1], keep.data_ptr(), keep.shape[1], keep.shape[2], kept_lens.data_ptr(),
+                           dst_tables.data_ptr(), dst_tables.stride(0), dst_tables.shape[1], handle))
     _used(stream, tables, keep, kept_lens, dst_tables)
 
 

@@ -133,12 +133,12 @@ __global__ __launch_bounds__(64 * kRows / RW, 2) void tail_kernel(const AttendAr
         return;
     const int i0 = divide(row0, a.by_group), i1 = divide(min(row0 + kRows, rows) - 1, a.by_group) + 1;
     const Span span = span_of(seq.n, seq.nq, i0, i1, a.window);
-    // (In 64 bits: the last part of the longest sequence would end beyond 32.)
-    const int64_t part_at = span.start + int64_t{split} * parts.len;
-    if (split > 0 && part_at >= span.end)
+    // (A part starts below 2^31, as the parts before it are shorter than the longest span, but may end beyond.)
+    const int begin = span.start + split * parts.len;
+    if (split > 0 && begin >= span.end)
         return;
-    const int begin = static_cast<int>(part_at);
-    const int stop = static_cast<int>(min(part_at + parts.len, static_cast<int64_t>(span.end)));
+    const uint32_t part_end = static_cast<uint32_t>(begin) + static_cast<uint32_t>(parts.len);
+    const int stop = min(span.end, static_cast<int>(min(part_end, uint32_t{INT32_MAX})));
     const bool whole = span.end - span.start <= parts.len;
 
     // This lane's row: its query as the first product's operand, and what it sees.
