@@ -174,8 +174,8 @@ def _cache_dtype(cache: Cache, dtype, rows) -> int:
 
 
 def _call_stream(stream):
-    """(the stream's handle, the context in which the call's own tensors are made): they belong to the call's stream, which
-    may be another than the current one."""
+    """(the stream's handle, the context in which the call's own tensors are made): they belong to the call's stream,
+    which may be another than the current one."""
     if stream is None:
         return torch.cuda.current_stream(torch.cuda.current_device()).cuda_stream, _HERE
     if not isinstance(stream, torch.cuda.Stream):
@@ -226,10 +226,11 @@ def kv_attend(cache: Cache, layer: int, q, tables, lens, starts=None, *, max_q=N
     over layer ``layer``; returns (out, lse).
 
     ``weights`` (float32 [B][H][>= max_len]): receives ``prior`` (same shape and strides; None: 0) plus what each cached
-    token got in this call; ``prior=weights`` accumulates in place.  ``full_weights``: sequences of more than 64 rows (new
-    tokens times query heads) per KV head take exp(s) to V as two numbers of q's type, as shorter ones always do, for up
-    to 1.3 times the time; then the output's rounding alone shows.  ``out`` (like ``q``) and ``lse`` (float32 [tokens]
-    [query heads]) are made if not given, and overlap no input; rows that belong to no sequence are left as they were.
+    token got in this call; ``prior=weights`` accumulates in place.  ``full_weights``: sequences of more than 64 rows
+    (new tokens times query heads) per KV head take exp(s) to V as two numbers of q's type, as shorter ones always do,
+    for up to 1.3 times the time; then the output's rounding alone shows.  ``out`` (like ``q``) and ``lse`` (float32
+    [tokens][query heads]) are made if not given, and overlap no input; rows that belong to no sequence are left as
+    they were.
     """
     device = cache.struct.device
     qr = _rows(q, "q", cache.layout.head_dim, device)

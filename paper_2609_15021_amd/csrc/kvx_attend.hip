@@ -1,9 +1,9 @@
 // kv_attend: attention of the new tokens over a paged cache (host side).
 //
 // For a row (a new token and a query head) with scores s_t over the tokens it sees, out = sum exp(s_t - m) v_t / sum
-// exp(s_t - m) in one pass over the tokens: m is the largest score so far (up to a factor of 2^8), and what was summed
-// under a smaller one is scaled down when it grows.  Sequences of few rows per KV head go to the step kernel, others to
-// the tail kernel; both split a long sequence over workgroups where the batch alone does not fill the chip.
+// exp(s_t - m) in one pass over the tokens: m is the largest score so far (up to a factor of 2^8), and what was
+// summed under a smaller one is scaled down when it grows.  Sequences of few rows per KV head go to the step kernel,
+// others to the tail kernel; both split a long sequence over workgroups where the batch alone does not fill the chip.
 #include <algorithm>
 #include <cmath>
 
@@ -57,8 +57,8 @@ kv_status check_attend(const kv_cache *cache, const kv_batch *batch, const kv_at
     // What the kernels multiply scores by has to be a normal number.
     const float product = scale_of(cache, o), inv = o->softcap > 0.f ? product / o->softcap : 1.f;
     if (!(product >= 1e-36f && product <= 1e36f) || !(inv >= 1e-36f && inv <= 1e36f))
-        return fail(KV_EUNSUPPORTED, "scale %g with k_scale %g and softcap %g is beyond 32-bit scores", o->scale, o->k_scale,
-                    o->softcap);
+        return fail(KV_EUNSUPPORTED, "scale %g with k_scale %g and softcap %g is beyond 32-bit scores", o->scale,
+                    o->k_scale, o->softcap);
     if ((o->full_weights != 0 && o->full_weights != 1) || o->reserved != 0)
         return fail(KV_EINVAL, "full_weights must be 0 or 1 and reserved 0 (got %d and %d)", o->full_weights,
                     o->reserved);
@@ -68,8 +68,8 @@ kv_status check_attend(const kv_cache *cache, const kv_batch *batch, const kv_at
     const int64_t queries = std::min(batch->max_queries, batch->num_queries), group = q->heads / H;
     if (queries * group > INT32_MAX / 2 || (queries * group > kStepRows &&
                                             tail_tiles(queries, group) * H * batch->num_seqs > kMaxWorkgroups))
-        return fail(KV_EUNSUPPORTED, "up to %lld new tokens in each of %d sequences of %d query heads are too many for one "
-                    "call", static_cast<long long>(queries), batch->num_seqs, q->heads);
+        return fail(KV_EUNSUPPORTED, "up to %lld new tokens in each of %d sequences of %d query heads are too many for "
+                    "one call", static_cast<long long>(queries), batch->num_seqs, q->heads);
     if (o->weights_out && (o->weights_seq_stride < 0 || o->weights_head_stride < 0 ||
                            (batch->num_seqs > 0 && H > 1 && o->weights_head_stride < batch->max_len) ||
                            (batch->num_seqs > 1 && o->weights_seq_stride < batch->max_len)))
@@ -92,12 +92,12 @@ struct Plan {
 
 int64_t round_up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 
-// The tail kernel's parts, for `have` tiles of rows (of the `launched`, others are empty).  512 of its workgroups run at
-// once (2 per CU; 256 where D > 128), so they may leave the last round nearly empty, and tiles that see less than others
-// end it early: the number of parts is the one whose rounds (between those of equal parts, and those without an edge and
-// half a part idle at the end) and joining take least, at the 0.2 ns per token and column that such a round takes and the
-// 5 TB/s at which parts are written and read again (a session turn of 656 tiles: 1.81 ms whole, 1.66 in 3 parts).  Parts
-// have no fewer than 256 tokens and no more than 256 MB between them.
+// The tail kernel's parts, for `have` tiles of rows (of the `launched`, others are empty).  512 of its workgroups run
+// at once (2 per CU; 256 where D > 128), so they may leave the last round nearly empty, and tiles that see less than
+// others end it early: the number of parts is the one whose rounds (between those of equal parts, and those without
+// an edge and half a part idle at the end) and joining take least, at the 0.2 ns per token and column that such a
+// round takes and the 5 TB/s at which parts are written and read again (a session turn of 656 tiles: 1.99 ms whole,
+// 1.54 in 3 parts, joining included).  Parts have no fewer than 256 tokens and no more than 256 MB between them.
 Parts tail_parts_for(int64_t longest, int64_t have, int64_t launched, int64_t head_dim) {
     const int64_t at_once = head_dim > 128 ? 256 : 512;
     const double tokens_us = 0.2e-3 * static_cast<double>(head_dim) * static_cast<double>(longest);
@@ -132,8 +132,8 @@ Plan plan_of(const kv_cache *cache, const kv_batch *batch, const kv_attend_optio
     const int64_t all_rows = p.max_queries * group;
     p.max_rows = static_cast<int32_t>(std::min<int64_t>(all_rows, kStepRows));
     p.tail = all_rows > kStepRows;
-    // With more rows than a tile has the scores would outgrow K itself: they are taken again instead.  So they are where
-    // the host's bounds, which may be far above what the sequences hold, would ask for more than 1 GiB of them.
+    // With more rows than a tile has the scores would outgrow K itself: they are taken again instead.  So they are
+    // where the host's bounds, which may be far above what the sequences hold, would ask for more than 1 GiB of them.
     p.score_len = round_up(batch->max_len, 32);
     const int64_t score_bytes = heads * all_rows * p.score_len * 4;
     p.scores = o->weights_out && all_rows <= 16 && score_bytes <= kMaxScoreBytes;

@@ -7,9 +7,12 @@ namespace kvx {
 
 // Rows of a workgroup of the tail kernel.
 constexpr int kTailRows = 128;
-inline int64_t tail_tiles(int64_t max_queries, int64_t group) { return (max_queries * group + kTailRows - 1) / kTailRows; }
+inline int64_t tail_tiles(int64_t max_queries, int64_t group) {
+    return (max_queries * group + kTailRows - 1) / kTailRows;
+}
 
-// Sequences of at most this many (new token, query head) rows per KV head go to the step kernel, others to the tail one.
+// Sequences of at most this many (new token, query head) rows per KV head go to the step kernel, others to the tail
+// one.
 constexpr int kStepRows = 64;
 
 struct AttendArgs {
@@ -30,7 +33,8 @@ struct AttendArgs {
     int32_t score_cap;
 };
 
-// How the tail kernel splits the tokens of a tile of rows over workgroups, and what the parts of a row leave for the join.
+// How the tail kernel splits the tokens of a tile of rows over workgroups, and what the parts of a row leave for the
+// join.
 struct Parts {
     int32_t len, splits;  // tokens of a part; most parts of a row
     float *sums;          // [row][query head][splits][D], unscaled
@@ -54,10 +58,11 @@ __host__ __device__ __forceinline__ Span span_of(int n, int nq, int i0, int i1, 
 // Rows of a tile of the step kernel.
 inline int step_tile_rows(int max_rows, int head_dim) { return max_rows > 16 && head_dim <= 128 ? 32 : 16; }
 
-// How the step kernel shares its sequences' tokens out: in parts of one length for all, on the device, where the lengths
-// are.  A long sequence among short ones is then no workgroup's alone, and the parts number at most `target`, which fill
-// the chip once (or twice the sequences, where those are more).  Up to kShareSeqs sequences every wave works out the
-// sharing for itself; more of them are shared out by a kernel of its own, which leaves the lists below.
+// How the step kernel shares its sequences' tokens out: in parts of one length for all, on the device, where the
+// lengths are.  A long sequence among short ones is then no workgroup's alone, and the parts number about `target`,
+// which fill the chip once, or three times where the sequences alone fill half of it (or twice the sequences, where
+// those are more).  Up to kShareSeqs sequences every wave works out the sharing for itself; more of them are shared
+// out by a kernel of its own, which leaves the lists below.
 struct Shares {
     int32_t target, items, num_seqs;  // items >= the parts of any batch
     int32_t shortest;                 // tokens of a part at least
@@ -231,8 +236,8 @@ __device__ __forceinline__ f32x4 mfma_16x16x32(const u32x4 &a, const u32x4 &b, c
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 constexpr float kLowest = -3.402823466e+38f;  // the largest score of nothing (finite: its differences are numbers)
 
-// cap * tanh(x / cap) for x * inv = x / cap: tanh by its series below 1/4 (the first term left out is 2^-27 of it), else
-// from exp2; an error of 2^-23 or so of cap.
+// cap * tanh(x / cap) for x * inv = x / cap: tanh by its series below 1/4 (the first term left out is 2^-27 of it),
+// else from exp2; an error of 2^-23 or so of cap.
 __device__ __forceinline__ float capped(float x, float inv, float cap) {
     const float y = x * inv, y2 = y * y, t = fabsf(y);
     const float series =
@@ -241,8 +246,8 @@ __device__ __forceinline__ float capped(float x, float inv, float cap) {
     return cap * (t < 0.25f ? series : copysignf(far, y));
 }
 
-// The same for caps up to kSmallCap, from exp2 alone (twice = 2 log2(e) inv): its error of 2^-22 or so of cap, whatever x,
-// is then at most that of a score of 16.
+// The same for caps up to kSmallCap, from exp2 alone (twice = 2 log2(e) inv): its error of 2^-22 or so of cap,
+// whatever x, is then at most that of a score of 16.
 constexpr float kSmallCap = 64.f;
 __device__ __forceinline__ float small_capped(float x, float twice, float cap) {
     return fmaf(-2.f * cap, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * twice)), cap);

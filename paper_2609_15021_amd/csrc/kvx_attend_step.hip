@@ -1,8 +1,8 @@
 // kv_attend for few new tokens per sequence (a decoding step): bound by reading the cache.
 //
-// A KV head's rows (its query heads times the new tokens, up to 16 or 32 of them at a time) share one pass over K and V.
-// Per 32 tokens a wave takes the scores as K Q^T and the output as V^T P^T on the matrix cores (16x16x32): then a row is
-// a column of both results, and its largest score, sum and rescaling stay inside a lane.
+// A KV head's rows (its query heads times the new tokens, up to 16 or 32 of them at a time) share one pass over K and
+// V. Per 32 tokens a wave takes the scores as K Q^T and the output as V^T P^T on the matrix cores (16x16x32): then a
+// row is a column of both results, and its largest score, sum and rescaling stay inside a lane.
 //
 //  * K's operand wants a token's consecutive elements per lane: 16-byte loads straight into registers.  Its 32 tokens
 //    are given to the two products' rows in the order in which the second product wants them: row m of product j is
@@ -12,14 +12,15 @@
 //    permutations in registers turn them (one per pair of elements); e4m3 is turned while it is widened.
 //  * The pages of 32 tokens are looked up by 32 lanes, one token each, a round ahead, and handed out by lane shuffles.
 //
-// The sequences' tokens are shared out to workgroups (Shares) so that they fill the chip once, and inside a workgroup over
-// its 4 waves; the waves' sums are joined through LDS, the workgroups' by join_kernel.  K of the next 32 tokens is
-// requested as soon as the scores have used the last, V as soon as the second product has: a wave has 16 KiB in flight
-// (bf16, D 128) without a second set of registers, and 2 waves of a SIMD 128 KiB a CU.
+// The sequences' tokens are shared out to workgroups (Shares) so that they fill the chip evenly, and inside a
+// workgroup over its 4 waves; the waves' sums are joined through LDS, the workgroups' by join_kernel.  K of the next
+// 32 tokens is requested as soon as the scores have used the last, V as soon as the second product has: a wave has 16
+// KiB in flight (bf16, D 128) without a second set of registers, and 2 waves of a SIMD 128 KiB a CU.
 //
-// One sequence behind 131,077 tokens (8 heads of 5 rows, bf16, D 128): 95 us and 7 to join, 5.2 TB/s with both (a large
-// reduction reads 6.1, a large copy moves 4.8).  16 sequences of up to 32,768 tokens in e4m3 (4 heads of 6 rows, D 256):
-// 123 us, 4.8 TB/s.  48 of up to 8,192 with weights (2 heads of 8 rows): 41 us, 8 to join, 6 for what each token received.
+// One sequence behind 131,077 tokens (8 heads of 5 rows, bf16, D 128): 95 us and 7 to join, 5.2 TB/s with both (a
+// large reduction reads 6.1, a large copy moves 4.8).  16 sequences of up to 32,768 tokens in e4m3 (4 heads of 6
+// rows, D 256): 123 us, 4.8 TB/s.  48 of up to 8,192 with weights (2 heads of 8 rows): 41 us, 8 to join, 6 for what
+// each token received.
 #include <algorithm>
 
 #include "kvx_attend_kernels.h"
@@ -270,7 +271,8 @@ __global__ __launch_bounds__(64 * kWaves, !FP8 && DP > 128 ? 1 : 2) void step_ke
                     *reinterpret_cast<f32x4 *>(to) = f32x4{x[0], x[1], x[2], x[3]};
                     *reinterpret_cast<f32x4 *>(to + 4) = f32x4{x[4], x[5], x[6], x[7]};
                 }
-                float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+                float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])),
+                                  fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
                 // The sums are scaled down only when some score has outgrown them by 2^8.
                 if (__any(top > m[nt] + 8.f)) {
                     top = fmaxf(top, __shfl_xor(top, 16));
@@ -524,7 +526,8 @@ __global__ __launch_bounds__(256) void join_kernel(const AttendArgs a, const Fro
     for (int k = 0; k < EARLY; ++k) {
         const int s = s0 + k * ds;
         const bool is = row && s < parts;
-        early[k] = is ? *reinterpret_cast<const f32x4 *>(from.sums + (row_at.slot + s * step) * D + d) : f32x4{0.f, 0.f, 0.f, 0.f};
+        early[k] = is ? *reinterpret_cast<const f32x4 *>(from.sums + (row_at.slot + s * step) * D + d)
+                      : f32x4{0.f, 0.f, 0.f, 0.f};
         early_most[k] = is ? stats[2 * s * step] : kLowest;
     }
     if constexpr (SPREAD) {  // every wave for itself
@@ -619,7 +622,8 @@ __global__ __launch_bounds__(256) void weigh_step_kernel(const AttendArgs a) {
 template <class T, bool FP8, int DP, int NT>
 hipError_t launch(const AttendArgs &a, const Shares &shares, int max_rows, hipStream_t stream) {
     const int tiles = (max_rows + 16 * NT - 1) / (16 * NT);
-    return launch_kernel(step_kernel<T, FP8, DP, NT>, dim3(shares.items, tiles * a.pages.H), 64 * kWaves, stream, a, shares);
+    return launch_kernel(step_kernel<T, FP8, DP, NT>, dim3(shares.items, tiles * a.pages.H), 64 * kWaves, stream, a,
+                         shares);
 }
 
 template <class T, bool FP8>
@@ -628,8 +632,10 @@ hipError_t launch(const AttendArgs &a, const Shares &shares, int max_rows, hipSt
     if (a.pages.D > 128)
         return launch<T, FP8, 256, 1>(a, shares, max_rows, stream);
     if (a.pages.D > 64)
-        return two ? launch<T, FP8, 128, 2>(a, shares, max_rows, stream) : launch<T, FP8, 128, 1>(a, shares, max_rows, stream);
-    return two ? launch<T, FP8, 64, 2>(a, shares, max_rows, stream) : launch<T, FP8, 64, 1>(a, shares, max_rows, stream);
+        return two ? launch<T, FP8, 128, 2>(a, shares, max_rows, stream)
+                   : launch<T, FP8, 128, 1>(a, shares, max_rows, stream);
+    return two ? launch<T, FP8, 64, 2>(a, shares, max_rows, stream)
+               : launch<T, FP8, 64, 1>(a, shares, max_rows, stream);
 }
 
 template <bool SPREAD, class From>

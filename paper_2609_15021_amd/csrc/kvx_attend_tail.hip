@@ -1,27 +1,28 @@
 // kv_attend for many new tokens of a sequence (a prompt's tail behind a restored prefix, or a whole prompt): bound by
 // the matrix cores and the exponentials between their products.
 //
-// A workgroup takes 128 rows (new token, query head) of one KV head, so that all query heads of a KV head share what is
-// read of it, and goes over the tokens TK at a time.  K and V of TK tokens lie in LDS, twice: while one is used, the next
-// is on its way (two-byte rows straight into LDS; e4m3 through registers, widened once per workgroup), and one barrier a
-// round separates them.  A wave has 32 of the rows and takes S^T = K Q^T and O^T = V^T P^T in 32x32x16 products: a row is
-// a column of both, so its largest score, sum and rescaling stay in a lane (and the one 32 lanes on), and the weights are
-// the second product's operand in the order in which the first leaves them: k-index e of half h of a product of 16 tokens
-// is token h * 4 + e for e < 4, and 8 + h * 4 + e - 4 beyond.  V's operand in that order is two transposing LDS reads
-// (16 lanes read 4 rows of 16 columns, a lane gets a column).  Rows in LDS are permuted in 16-byte pieces, so that neither
-// kind of read meets a bank twice.  Above 128 columns a wave has 16 rows, in 16x16x32 products and the step kernel's order
-// of tokens: the output's sums of 32 would not leave registers for a second wave on the SIMD.
+// A workgroup takes 128 rows (new token, query head) of one KV head, so that all query heads of a KV head share what
+// is read of it, and goes over the tokens TK at a time.  K and V of TK tokens lie in LDS, twice: while one is used,
+// the next is on its way (two-byte rows straight into LDS; e4m3 through registers, widened once per workgroup), and
+// one barrier a round separates them.  A wave has 32 of the rows and takes S^T = K Q^T and O^T = V^T P^T in 32x32x16
+// products: a row is a column of both, so its largest score, sum and rescaling stay in a lane (and the one 32 lanes
+// on), and the weights are the second product's operand in the order in which the first leaves them: k-index e of
+// half h of a product of 16 tokens is token h * 4 + e for e < 4, and 8 + h * 4 + e - 4 beyond.  V's operand in that
+// order is two transposing LDS reads (16 lanes read 4 rows of 16 columns, a lane gets a column).  Rows in LDS are
+// permuted in 16-byte pieces, so that neither kind of read meets a bank twice.  Above 128 columns a wave has 16 rows,
+// in 16x16x32 products and the step kernel's order of tokens: the output's sums of 32 would not leave registers for a
+// second wave on the SIMD.
 //
 // Workgroups of a KV head come 8 apart where there are 8 heads, and so on one XCD (consecutive ones go to consecutive
 // XCDs), and use its L2 together.
 //
-// 2,085 new tokens behind 32,768 (8 heads of 5 rows a token, bf16, D 128): 1.51 to 1.61 ms by machine, 900 to 955
-// TFLOP/s, where a large library product reaches 1,200.  Per round of 64 tokens a wave has 1,024 cycles of products and
-// about 1,150 of vector work (512 of them exponentials); two waves of a SIMD overlap them partly.  Ragged tails of up to
-// 1,055 tokens, e4m3, D 256, a window of 4,096 and capped scores: 0.66 ms, 495 TFLOP/s; there the matrix cores are busy
-// for a fifth of the cycles, LDS for a quarter and the vector units for a third, mostly one after the other: one
-// workgroup a CU, whose two waves a SIMD meet at a barrier every round.  (Half of its waves half a round behind the
-// others, with a barrier for each half: 0.76 ms, as scores take longer than outputs.)
+// 2,085 new tokens behind 32,768 (8 heads of 5 rows a token, bf16, D 128): 1.51 to 1.62 ms by machine, 890 to 955
+// TFLOP/s, where a large library product reaches 1,200.  Per round of 64 tokens a wave has 1,024 cycles of products
+// and about 1,150 of vector work (512 of them exponentials); two waves of a SIMD overlap them partly.  Ragged tails
+// of up to 1,055 tokens, e4m3, D 256, a window of 4,096 and capped scores: 0.66 ms, 495 TFLOP/s; there the matrix
+// cores are busy for a fifth of the cycles, LDS for a quarter and the vector units for a third, mostly one after the
+// other: one workgroup a CU, whose two waves a SIMD meet at a barrier every round.  (Half of its waves half a round
+// behind the others, with a barrier for each half: 0.76 ms, as scores take longer than outputs.)
 #include <algorithm>
 #include <type_traits>
 
@@ -73,8 +74,8 @@ typedef __attribute__((address_space(1))) const uint8_t global_byte;
 __device__ const __align__(16) uint8_t zeros[16] = {};
 
 __device__ __forceinline__ u32x2 read_turned(lds_byte *p) {
-    return __builtin_bit_cast(u32x2,
-                              __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<__attribute__((address_space(3))) s16x4 *>(p)));
+    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_s16x4 *>(p)));
 }
 
 // Asks the compiler to keep `AHEAD` sets of `READS` LDS reads in flight before the first of `SETS` sets of `PRODUCTS`
@@ -91,10 +92,11 @@ __device__ __forceinline__ void interleave() {
     }
 }
 
-// RW: rows of a wave, 32 (products of 32x32x16) or 16 (16x16x32).  PLAIN: neither a cap nor slopes.  FULL: weights meet
-// V as two numbers of T, the second being what the first leaves, so that the output's rounding alone shows: off by 0.00166
-// of its norm (bf16).  Else one, rounded, since a second product and its operands cost 1.28 times the time for the turn
-// above (2.00 ms instead of 1.57) and 1.18 for the ragged tails (0.78 instead of 0.66): 0.00225 and 0.00233.
+// RW: rows of a wave, 32 (products of 32x32x16) or 16 (16x16x32).  PLAIN: neither a cap nor slopes.  FULL: weights
+// meet V as two numbers of T, the second being what the first leaves, so that the output's rounding alone shows: off
+// by 0.00166 of its norm (bf16).  Else one, rounded, since a second product and its operands cost 1.28 times the time
+// for the turn above (2.00 ms instead of 1.57) and 1.18 for the ragged tails (0.78 instead of 0.66): 0.00225 and
+// 0.00233.
 template <class T, bool FP8, int DP, int TK, int RW, bool PLAIN, bool FULL>
 __global__ __launch_bounds__(64 * kRows / RW, 2) void tail_kernel(const AttendArgs a, const Parts parts, const int tiles) {
     constexpr int E = FP8 ? 1 : 2;
@@ -164,8 +166,8 @@ __global__ __launch_bounds__(64 * kRows / RW, 2) void tail_kernel(const AttendAr
 
     const int32_t *table = a.batch.tables + b * a.batch.table_stride;
     const uint8_t *cache = pg.base + static_cast<uint32_t>(h) * pg.head_bytes;
-    // (e4m3: a piece is two in LDS, so 8 lanes of a row would write every other one, and meet banks twice; 4 of the 8 take
-    // the next row, whose pairs are turned about: 0.658 ms instead of 0.667 for the ragged tails.)
+    // (e4m3: a piece is two in LDS, so 8 lanes of a row would write every other one, and meet banks twice; 4 of the 8
+    // take the next row, whose pairs are turned about: 0.658 ms instead of 0.667 for the ragged tails.)
     const int piece = FP8 ? (tid & 3) | (tid >> 1 & (GC - 4)) : tid % GC;
     const int first_row = FP8 && GC > 4 ? (tid >> 2 & 1) | tid / (2 * GC) * 2 : tid / GC;
     const bool piece_ok = piece * 16 < pg.row_bytes;
@@ -183,14 +185,14 @@ __global__ __launch_bounds__(64 * kRows / RW, 2) void tail_kernel(const AttendAr
             return -1;
         return block * pg.block_stride + static_cast<uint32_t>(t - divide(t, pg.by_bs) * pg.BS) * pg.token_bytes;
     };
-    // Requests K and V rows of a round: two-byte rows straight into LDS (a wave's 64 pieces of 16 bytes lie there as its
-    // lanes do, so a lane fetches the piece that the permutation wants in its place), e4m3 into registers.  Slots without
-    // a token and columns beyond D may hold anything, and 0 times it need not be 0: they become zeros.
+    // Requests K and V rows of a round: two-byte rows straight into LDS (a wave's 64 pieces of 16 bytes lie there as
+    // its lanes do, so a lane fetches the piece that the permutation wants in its place), e4m3 into registers.  Slots
+    // without a token and columns beyond D may hold anything, and 0 times it need not be 0: they become zeros.
     u32x4 next[2][FP8 ? NP : 1];
     // Of e4m3 rows a wave's WR rows of one load lie in one page where pages hold multiples of them (rounds begin at
-    // multiples of 32).  If all of the round's tokens take part, the first row's address is the wave's, and the lanes'
-    // distances from it are the same every round: 0.69 ms instead of 0.74 for the ragged tails above.  2-byte rows do not
-    // gain (1.57 to 1.60 ms instead of 1.56): their pieces are permuted as well.
+    // multiples of 32).  If all of the round's tokens take part, the first row's address is the wave's, and the
+    // lanes' distances from it are the same every round: 0.69 ms instead of 0.74 for the ragged tails above.  2-byte
+    // rows do not gain (1.57 to 1.60 ms instead of 1.56): their pieces are permuted as well.
     constexpr int WR = 64 / GC;  // rows of a wave in one load
     const bool together = FP8 && pg.BS % WR == 0 && pg.D == DP;
     const uint32_t lane_row = static_cast<uint32_t>(first_row - wave * WR) * pg.token_bytes;
@@ -216,7 +218,8 @@ __global__ __launch_bounds__(64 * kRows / RW, 2) void tail_kernel(const AttendAr
 #pragma unroll
         for (int n = 0; n < NP; ++n) {
             const int src = first_row + n * RP;
-            const uint32_t lo = __shfl(static_cast<uint32_t>(off), src), hi = __shfl(static_cast<uint32_t>(off >> 32), src);
+            const uint32_t lo = __shfl(static_cast<uint32_t>(off), src);
+            const uint32_t hi = __shfl(static_cast<uint32_t>(off >> 32), src);
             at[n] = static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo);
         }
         if constexpr (FP8) {
@@ -261,7 +264,8 @@ __global__ __launch_bounds__(64 * kRows / RW, 2) void tail_kernel(const AttendAr
                 for (int j = 0; j < 2; ++j) {
                     const uint32_t x0 = next[kv][n][2 * j], x1 = next[kv][n][2 * j + 1];
                     *reinterpret_cast<u32x4 *>(to + ((2 * piece + j) ^ permute) * 16) =
-                        u32x4{T::from_e4m3(x0, false), T::from_e4m3(x0, true), T::from_e4m3(x1, false), T::from_e4m3(x1, true)};
+                        u32x4{T::from_e4m3(x0, false), T::from_e4m3(x0, true), T::from_e4m3(x1, false),
+                              T::from_e4m3(x1, true)};
                 }
             }
         } else {
@@ -278,10 +282,10 @@ __global__ __launch_bounds__(64 * kRows / RW, 2) void tail_kernel(const AttendAr
             acc[d][x] = 0.f;
     float m = kLowest, l = 0.f;
 
-    // Where this lane reads.  K: 16 bytes of a token's row per product, the token c of 32, or for the two products of 16
-    // tokens (c / 4) * 8 + c % 4 and that + 4.  V: 8 bytes, of one of 4 tokens' rows for the 16 lanes that turn them, and
-    // of the one 8 (or 4) on.  Rows start at multiples of their length, so a permuted piece's address is the first one's
-    // with bits of the product's (or the tile's) number turned over.
+    // Where this lane reads.  K: 16 bytes of a token's row per product, the token c of 32, or for the two products of
+    // 16 tokens (c / 4) * 8 + c % 4 and that + 4.  V: 8 bytes, of one of 4 tokens' rows for the 16 lanes that turn
+    // them, and of the one 8 (or 4) on.  Rows start at multiples of their length, so a permuted piece's address is
+    // the first one's with bits of the product's (or the tile's) number turned over.
     const int k_row = WIDE ? c : (c >> 2) * 8 + (c & 3), v_row = part * (WIDE ? 4 : 8) + (lane >> 2 & 3);
     const int v_piece = (WIDE ? (lane >> 4 & 1) * 2 : 0) + (lane >> 1 & 1);
     int k_at = k_row * ROW + (part ^ k_permute(k_row)) * 16;
@@ -301,8 +305,9 @@ __global__ __launch_bounds__(64 * kRows / RW, 2) void tail_kernel(const AttendAr
                 // (The permutation does not see the 4 tokens between the two products' rows.)
 #pragma unroll
                 for (int k = 0; k < KS; ++k)
-                    sum[j] = product(*reinterpret_cast<const u32x4 *>(k_lds + (t * 32 + j * 4) * ROW + (k_at ^ k * 2 * KD)),
-                                     qf[k], sum[j], T{});
+                    sum[j] = product(
+                        *reinterpret_cast<const u32x4 *>(k_lds + (t * 32 + j * 4) * ROW + (k_at ^ k * 2 * KD)), qf[k],
+                        sum[j], T{});
             }
 #pragma unroll
             for (int x = 0; x < NS; ++x)
@@ -409,8 +414,8 @@ __global__ __launch_bounds__(64 * kRows / RW, 2) void tail_kernel(const AttendAr
                         p_rest[t][x >> 3][x >> 1 & 3] = T::pack(e0 - T::low(w), e1 - T::high(w));
                 }
             l += (sums[0] + sums[1]) + (sums[2] + sums[3]);
-            // (e4m3: K of the next round is widened beside the other wave's products, V after this one's; 0.665 ms instead of
-            // 0.675 with both at the end.)
+            // (e4m3: K of the next round is widened beside the other wave's products, V after this one's; 0.665 ms
+            // instead of 0.675 with both at the end.)
             if (FP8 && more)
                 deposit(0, buffer ^ 1);
             asm volatile("" : "+v"(v_at));
@@ -474,8 +479,8 @@ __global__ __launch_bounds__(64 * kRows / RW, 2) void tail_kernel(const AttendAr
 }
 
 // What each token received: a wave holds K of 32 tokens, goes over the rows that see them, 32 at a time, with their
-// scores taken again, and adds up exp2(s - lse) for each token; a token's 32 partial sums are joined at the end.  SHARED:
-// a workgroup's waves have the same tokens and take turns with the rows; their sums are joined in order.
+// scores taken again, and adds up exp2(s - lse) for each token; a token's 32 partial sums are joined at the end.
+// SHARED: a workgroup's waves have the same tokens and take turns with the rows; their sums are joined in order.
 template <class T, bool FP8, int DP, bool SHARED>
 __global__ __launch_bounds__(64 * kWeighWaves) void weigh_kernel(const AttendArgs a) {
     constexpr int KC = DP * (FP8 ? 1 : 2) / 32;  // 16-byte pieces of a token's K in a lane
@@ -489,7 +494,8 @@ __global__ __launch_bounds__(64 * kWeighWaves) void weigh_kernel(const AttendArg
         return;
     // Rows that see any of the 32 tokens: new tokens from base on, and before the window has closed on the last.
     const int past = seq.n - seq.nq;
-    const int i0 = max(0, base - past), i1 = a.window > 0 ? min<int64_t>(seq.nq, int64_t{base} + 31 + a.window - past) : seq.nq;
+    const int i0 = max(0, base - past);
+    const int i1 = a.window > 0 ? min<int64_t>(seq.nq, int64_t{base} + 31 + a.window - past) : seq.nq;
     // (In 64 bits: rows before token 0 and a wide window are together beyond 32.)
     const int first_seen =
         a.window > 0 ? static_cast<int>(max(int64_t{0}, int64_t{past} + 1 - a.window)) : 0;
@@ -504,13 +510,15 @@ __global__ __launch_bounds__(64 * kWeighWaves) void weigh_kernel(const AttendArg
         const int block = seen ? a.batch.tables[b * a.batch.table_stride + page] : 0;
         const bool use = seen && in_cache(pg, block);
         const uint32_t usable = static_cast<uint32_t>(__ballot(use));
-        const uint8_t *k_row = pg.base + static_cast<uint32_t>(h) * pg.head_bytes +
-                               (use ? block * pg.block_stride + static_cast<uint32_t>(t_lane - page * pg.BS) * pg.token_bytes
-                                    : int64_t{0});
+        const int64_t k_off =
+            use ? block * pg.block_stride + static_cast<uint32_t>(t_lane - page * pg.BS) * pg.token_bytes : int64_t{0};
+        const uint8_t *k_row = pg.base + static_cast<uint32_t>(h) * pg.head_bytes + k_off;
         u32x4 k_reg[KC];
 #pragma unroll
-        for (int k = 0; k < KC; ++k)
-            k_reg[k] = *reinterpret_cast<const u32x4 *>(k_row + (k * 32 + half * 16 < pg.row_bytes ? k * 32 + half * 16 : 0));
+        for (int k = 0; k < KC; ++k) {
+            const int at = k * 32 + half * 16;
+            k_reg[k] = *reinterpret_cast<const u32x4 *>(k_row + (at < pg.row_bytes ? at : 0));
+        }
         const float scale = a.scale * kLog2e;
         for (int r0 = i0 * a.group + (SHARED ? wave * 32 : 0); r0 < i1 * a.group; r0 += 32 * (SHARED ? kWeighWaves : 1)) {
             const int r = min(r0 + c, i1 * a.group - 1), i = divide(r, a.by_group), head = h * a.group + r - i * a.group;
@@ -534,8 +542,8 @@ __global__ __launch_bounds__(64 * kWeighWaves) void weigh_kernel(const AttendArg
                     }
                 } else {
                     const int d = k * 16 + half * 8;
-                    s = mfma_32x32x16(k_reg[k], d < pg.D ? *reinterpret_cast<const u32x4 *>(q + 2 * d) : u32x4{0, 0, 0, 0}, s,
-                                      T{});
+                    const u32x4 x = d < pg.D ? *reinterpret_cast<const u32x4 *>(q + 2 * d) : u32x4{0, 0, 0, 0};
+                    s = mfma_32x32x16(k_reg[k], x, s, T{});
                 }
             }
             if (a.softcap > 0.f && a.softcap <= kSmallCap) {
@@ -559,7 +567,8 @@ __global__ __launch_bounds__(64 * kWeighWaves) void weigh_kernel(const AttendArg
                 for (int x = 0; x < 16; ++x)
                     s[x] -= slope * static_cast<float>(p - (base + 8 * (x >> 2) + half * 4 + (x & 3)));
             }
-            const int to = lse == -INFINITY ? INT32_MIN : p - base + 1, from = a.window > 0 ? p - base + 1 - a.window : INT32_MIN;
+            const int to = lse == -INFINITY ? INT32_MIN : p - base + 1;
+            const int from = a.window > 0 ? p - base + 1 - a.window : INT32_MIN;
             const uint32_t mine = usable >> (half * 4);
 #pragma unroll
             for (int x = 0; x < 16; ++x) {
@@ -607,8 +616,8 @@ hipError_t launch(const AttendArgs &a, const Parts &parts, int max_queries, hipS
 
 template <class T, bool FP8, bool PLAIN, bool FULL>
 hipError_t launch(const AttendArgs &a, const Parts &parts, int max_queries, hipStream_t stream) {
-    // (Wide rows: 32 of them would need more registers than two waves of a SIMD have, and one wave alone took 1.7 times
-    // as long.)
+    // (Wide rows: 32 of them would need more registers than two waves of a SIMD have, and one wave alone took 1.7
+    // times as long.)
     if (a.pages.D > 128)
         return launch<T, FP8, 256, 64, 16, PLAIN, FULL>(a, parts, max_queries, stream);
     if (a.pages.D > 64)
@@ -637,9 +646,12 @@ hipError_t launch_weigh(const AttendArgs &a, hipStream_t stream) {
 
 template <class T, bool FP8>
 hipError_t launch_weigh(const AttendArgs &a, hipStream_t stream) {
-    // A wave waits for each 32 rows' queries in turn, so where the tiles are fewer than 2 waves a SIMD, 4 take turns (7
-    // sequences of 308 new tokens in 2,196, 2 heads of 8 rows: the whole call 194 us instead of 284; 3 of up
-    // to 208 in 342, 64 instead of 125).  With more tiles K would only be read by more waves (31,000 tiles: 8 waves each take 1.46 ms, one 0.95).
+    // A wave waits for each 32 rows' queries in turn, so where the tiles (by the call's bounds) are fewer than 2
+    // waves a SIMD, 4 take turns.  Whole calls, bf16, D 128: 7 sequences of up to 308 new tokens in 2,196, 2 heads of
+    // 8 rows (966 tiles) 116 us instead of 216; 3 of up to 208 in 342 (66 tiles) 50 instead of 121; one of 512 in
+    // 7,600, 8 heads of 5 rows (1,904 tiles), 287 instead of 320, though with 64 new tokens 85 instead of 75.  With
+    // more tiles K is mostly read by more waves for nothing: 8,192 tiles take 1,083 and 1,098 us with 512 new tokens
+    // each, but 233 and 187 with 64; 31,040 take 4.3 and 4.1 ms, and 836 and 633 us.
     const int64_t tiles = (int64_t{a.batch.max_len} + 31) / 32 * a.pages.H * a.num_seqs;
     return tiles < 2048 ? launch_weigh<T, FP8, true>(a, stream) : launch_weigh<T, FP8, false>(a, stream);
 }
@@ -649,8 +661,10 @@ hipError_t launch_weigh(const AttendArgs &a, hipStream_t stream) {
 hipError_t launch_tail(const AttendArgs &a, const Parts &parts, int max_queries, hipStream_t stream) {
     const bool fp8 = a.cache_type == KV_DTYPE_E4M3;
     if (a.q_type == KV_DTYPE_BF16)
-        return fp8 ? launch<Bf16, true>(a, parts, max_queries, stream) : launch<Bf16, false>(a, parts, max_queries, stream);
-    return fp8 ? launch<F16, true>(a, parts, max_queries, stream) : launch<F16, false>(a, parts, max_queries, stream);
+        return fp8 ? launch<Bf16, true>(a, parts, max_queries, stream)
+                   : launch<Bf16, false>(a, parts, max_queries, stream);
+    return fp8 ? launch<F16, true>(a, parts, max_queries, stream)
+               : launch<F16, false>(a, parts, max_queries, stream);
 }
 
 hipError_t launch_weigh(const AttendArgs &a, hipStream_t stream) {

@@ -1,9 +1,9 @@
 // kv_compact: the kept tokens' rows of a paged cache into fresh pages.
 //
-// One 16-byte vector per lane, of kEach rows at once; consecutive lanes run along a row and then along one head's kept tokens, so reads are
-// whole rows, and writes contiguous in HND pages.  Bound by HBM: every kept byte is read once and written once, 4,096 of
-// 16,384 tokens of 8 sequences (8 heads of 256 bytes) at 4.9 TB/s, a large copy's rate; 3.8 with one row at a time and
-// through the caches.
+// One 16-byte vector per lane, of kEach rows at once; consecutive lanes run along a row and then along one head's
+// kept tokens, so reads are whole rows, and writes contiguous in HND pages.  Bound by HBM: every kept byte is read
+// once and written once, 4,096 of 16,384 tokens of 8 sequences (8 heads of 256 bytes) at 4.9 TB/s, a large copy's
+// rate; 3.8 with one row at a time and through the caches.
 #include <algorithm>
 
 #include "kvx_paged.h"
@@ -60,7 +60,8 @@ __global__ __launch_bounds__(kThreads) void compact_kernel(const CompactArgs a) 
         for (int k = 0; k < kEach; ++k) {
             const int u = min(u0 + k * stride, units - 1), vec = u - divide(u, a.by_row) * a.row_vecs;
             const int slot = max(token[k], 0) - divide(max(token[k], 0), p.by_bs) * p.BS;
-            const uint8_t *row = p.base + page_offset(p, max(src[k], 0), kv, h) + static_cast<uint32_t>(slot) * p.token_bytes;
+            const uint8_t *row =
+                p.base + page_offset(p, max(src[k], 0), kv, h) + static_cast<uint32_t>(slot) * p.token_bytes;
             x[k] = __builtin_nontemporal_load(reinterpret_cast<const vec16 *>(row) + vec);
         }
 #pragma unroll

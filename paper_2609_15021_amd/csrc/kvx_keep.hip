@@ -1,16 +1,17 @@
 // kv_keep: which tokens a sequence keeps under a budget, by accumulated attention weight.
 //
 // The heaviest m of the tokens between the sinks and the recent ones are those whose weight, as a 32-bit key that
-// orders as the weights do, is above the m-th largest key, and as many of those equal to it, from the lowest token on,
-// as are left.  That key is found from counts of its digits' values (a radix selection of 11, 11 and 10 bits: the first
-// digit already has the exponent and two bits more, so that the counters of a wave are spread); then what every wave will
-// write is counted, and the chosen tokens are written in order.
+// orders as the weights do, is above the m-th largest key, and as many of those equal to it, from the lowest token
+// on, as are left.  That key is found from counts of its digits' values (a radix selection of 11, 11 and 10 bits: the
+// first digit already has the exponent and two bits more, so that the counters of a wave are spread); then what every
+// wave will write is counted, and the chosen tokens are written in order.
 //
 // One workgroup does all of that for a row whose 8,192 tokens fit its registers, and for longer rows where there are
-// enough of them to fill the chip; it is bound by its own instructions (15 us for 8,192 tokens, 148 for 131,077).  A few
-// long rows are cut into pieces of 8,192 tokens instead, a workgroup each, in five launches (27-29 us for 131,077 tokens):
-// clear the counters, a digit each, write.  For every value that the last digit may have, a piece leaves how many of its
-// tokens are above it, so that the pieces behind it know where they begin to write without counting again.
+// enough of them to fill the chip; it is bound by its own instructions (15 us for 8,192 tokens, 148 for 131,077).  A
+// few long rows are cut into pieces of 8,192 tokens instead, a workgroup each, in five launches (27-29 us for 131,077
+// tokens): clear the counters, a digit each, write.  For every value that the last digit may have, a piece leaves how
+// many of its tokens are above it, so that the pieces behind it know where they begin to write without counting
+// again.
 #include <algorithm>
 
 #include "kvx_paged.h"
@@ -139,8 +140,8 @@ __global__ __launch_bounds__(kKeepThreads) void keep_kernel(const KeepArgs a) {
     struct Keys {
         uint32_t k[4];
     };
-    // The row's 4 tokens from t on, or its last 4 where there are not so many; then their keys (0 beyond the row).  The
-    // load does not depend on where it is, so many can be on their way.
+    // The row's 4 tokens from t on, or its last 4 where there are not so many; then their keys (0 beyond the row).
+    // The load does not depend on where it is, so many can be on their way.
     const int last4 = max(n - 4, 0);
     const auto load = [&](int t) {
         if (n >= 4)
@@ -357,7 +358,8 @@ __global__ __launch_bounds__(kKeepThreads) void keep_kernel(const KeepArgs a) {
         __syncthreads();
         each(set, set_end, [&](int i, int t, const Keys &x) {
             bool sure[4], tie[4];
-            int sure_before = of_wave[(i - set) * kKeepWaves + wave][0], ties_before = of_wave[(i - set) * kKeepWaves + wave][1];
+            const int(&before)[2] = of_wave[(i - set) * kKeepWaves + wave];
+            int sure_before = before[0], ties_before = before[1];
             uint64_t lanes = 0;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -390,8 +392,9 @@ __global__ __launch_bounds__(kThreads) void clear_kernel(int32_t *x, int64_t n) 
         x[i] = 0;
 }
 
-// Pieces of a row: where a few long rows would leave most CUs idle (whole rows of 16,384 tokens and 128 of them or more
-// take less than the launches that pieces need).
+// Pieces of a row: where a few long rows would leave most CUs idle.  From 128 rows on, a workgroup a row takes about
+// as long: 127 rows in pieces and 128 whole ones take 43 and 47 us (32,768 tokens), 76 and 76 (65,536), 137 and 165
+// (131,072; 256 whole ones 181).
 int pieces_of(int32_t num_seqs, int32_t heads, int32_t max_len, int32_t budget) {
     const int pieces = max_len > 0 ? (max_len - 1) / kPiece + 1 : 1;
     if (max_len <= 2 * kPiece || max_len <= budget || static_cast<int64_t>(num_seqs) * heads >= 128 || pieces > 65535)
@@ -467,7 +470,8 @@ kv_status keep(const float *weights, int64_t seq_stride, int64_t head_stride, co
 extern "C" {
 
 int64_t kv_keep_workspace(int32_t num_seqs, int32_t heads, int32_t max_len, int32_t budget) {
-    const kv_status st = kvx::guarded([&]() -> kv_status { return kvx::check_keep(num_seqs, heads, max_len, budget, 0, 0); });
+    const kv_status st =
+        kvx::guarded([&]() -> kv_status { return kvx::check_keep(num_seqs, heads, max_len, budget, 0, 0); });
     return st == KV_OK ? kvx::workspace_bytes_of(num_seqs, heads, kvx::pieces_of(num_seqs, heads, max_len, budget)) : st;
 }
 
