@@ -2,7 +2,7 @@
 //
 // One 16-byte vector of the cache per lane: consecutive lanes run along a row, then along a token's heads, as the
 // source lies.  2,608 new tokens of 4 heads of 256 to e4m3 (16 MB read and written once, 3.5 us at a large copy's
-// rate) take 6.5 to 6.8 us on the GPU: a lane waits for its page's number, then for its row, and has one of each on
+// rate) take 6.5 to 7.2 us on the GPU: a lane waits for its page's number, then for its row, and has one of each on
 // its way.  A decoding step is bound by the launch (2.4 to 2.8 us on the GPU, 10 with the host).
 #include <algorithm>
 #include <cmath>

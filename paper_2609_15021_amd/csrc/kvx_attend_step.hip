@@ -19,8 +19,8 @@
 //
 // One sequence behind 131,077 tokens (8 heads of 5 rows, bf16, D 128): 95 us and 7 to join, 5.2 TB/s with both (a
 // large reduction reads 6.1, a large copy moves 4.8).  16 sequences of up to 32,768 tokens in e4m3 (4 heads of 6
-// rows, D 256): 123 us, 4.8 TB/s.  48 of up to 8,192 with weights (2 heads of 8 rows): 41 us, 8 to join, 6 for what
-// each token received.
+// rows, D 256): 117 us and 8 to join, 4.8 TB/s.  48 of up to 8,192 with weights (2 heads of 8 rows): 53 us (209 MB of
+// K and V read, 13 MB of scores written), 8 to join, 7 for what each token received.
 #include <algorithm>
 
 #include "kvx_attend_kernels.h"
