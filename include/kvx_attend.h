@@ -69,7 +69,7 @@ typedef struct kv_batch {
     int32_t table_len;           /* entries of a sequence's block table that may be read */
     int32_t reserved;            /* must be 0 */
     int64_t table_stride;        /* entries between the tables of two sequences */
-    const int32_t *block_tables; /* DEVICE int32[num_seqs][table_stride] */
+    const int32_t *block_tables; /* DEVICE int32[num_seqs][table_stride]; may be NULL where table_len is 0 */
     const int32_t *lens;         /* DEVICE int32[num_seqs] */
     const int32_t *starts;       /* DEVICE int32[num_seqs + 1]; NULL: one new token each, row b of sequence b */
 } kv_batch;

@@ -82,7 +82,7 @@ kv_status check_batch(const kv_cache *cache, const kv_batch *batch) {
     if (batch->num_seqs > 1 && batch->table_stride < batch->table_len)
         return fail(KV_EINVAL, "table_stride %lld is smaller than table_len %d",
                     static_cast<long long>(batch->table_stride), batch->table_len);
-    if (!batch->block_tables || !batch->lens)
+    if ((!batch->block_tables && batch->table_len > 0) || !batch->lens)
         return fail(KV_EINVAL, "block_tables and lens must not be NULL");
     if (!batch->starts && (batch->num_queries < batch->num_seqs))
         return fail(KV_EINVAL, "%d rows of new tokens for %d sequences of one each", batch->num_queries,

@@ -202,3 +202,16 @@ def test_full_weights_is_a_choice_of_two(host_cache):
     for full in (False, True):
         attend.kv_attend(handle, 0, q, tables, lens, full_weights=full)
         assert lib.args[3]._obj.full_weights == full
+
+
+def test_tables_without_entries_need_no_address():
+    """Sequences of no tokens: a table of no entries has no address in torch."""
+    from paper_2609_15021_amd import attend, kvx
+    cache, rows = _cache(kvx, kvx.make_layout(1, 2, 64, 2, 16, 16)), _rows(attend, 4)
+    o = attend.KvAttendOptions(cache_dtype=attend.KV_DTYPE_BF16)
+    for fields, fine in ((dict(table_len=0, table_stride=0, max_len=0, block_tables=None), True),
+                         (dict(table_len=1, table_stride=1, max_len=0, block_tables=None), False),
+                         (dict(table_len=0, table_stride=0, max_len=0, block_tables=None, lens=None), False)):
+        batch = _batch(attend, **fields)
+        need = kvx._lib.kv_attend_workspace(ctypes.byref(cache), ctypes.byref(batch), ctypes.byref(o), ctypes.byref(rows))
+        assert need >= 0 if fine else need == kvx.KV_EINVAL, fields

@@ -251,6 +251,35 @@ def test_one_token_with_any_stride(n):
     assert keep.tolist() == [[[-1, -1]]] and kept.tolist() == [0]
 
 
+@pytest.mark.parametrize("new", [1, 3, 40])
+def test_sequences_of_no_tokens_and_no_pages(new):
+    """A batch in which nothing is cached yet, its tables without an entry: rows of 0 and -infinity, nothing written."""
+    c = ref.Case(2, 3, 64, 16, [5], [1], seed=46)
+    cache, t, _, _, _, _, _, _ = c.device()
+    before = t.clone()
+    tables, lens = torch.zeros(2, 0, **INTS), torch.zeros(2, **INTS)
+    starts = torch.tensor([0, new, 2 * new], **INTS)
+    q, k = torch.ones(2 * new, 6, 64, dtype=BF16, device=DEV), torch.ones(2 * new, 2, 64, dtype=BF16, device=DEV)
+    weights = torch.full((2, 2, 7), 3.0, device=DEV)
+    attend.kv_append(cache, 0, k, k, tables, lens, starts)
+    out, lse = attend.kv_attend(cache, 0, q, tables, lens, starts, weights=weights, prior=weights)
+    assert not out.any() and (lse == -torch.inf).all() and (weights == 3).all()
+    assert torch.equal(t.view(torch.int16), before.view(torch.int16))
+
+
+def test_streams_by_handle():
+    """The null stream and torch's default stream, named."""
+    c = ref.Case(2, 4, 128, 16, [3000, 40], [1, 1], seed=47)
+    cache, _, q, _, _, tables, lens, _ = c.device()
+    want = ref.attend(c)
+    torch.cuda.synchronize()
+    for stream in (0, torch.cuda.default_stream(), torch.cuda.current_stream().cuda_stream):
+        out, lse = attend.kv_attend(cache, 0, q, tables, lens, stream=stream)
+        torch.cuda.synchronize()
+        ref.check(out, want[0], want[3], "out")
+        ref.check(lse, want[1], want[4], "lse")
+
+
 def test_group_beyond_a_step():
     """One new token of more query heads per KV head than the kernel for few rows takes."""
     for fp8 in (False, True):
