@@ -135,8 +135,7 @@ Plan plan_of(const kv_cache *cache, const kv_batch *batch, const kv_attend_optio
     // With more rows than a tile has the scores would outgrow K itself: they are taken again instead.  So they are
     // where the host's bounds, which may be far above what the sequences hold, would ask for more than 1 GiB of them.
     p.score_len = round_up(batch->max_len, 32);
-    const int64_t score_bytes = heads * all_rows * p.score_len * 4;
-    p.scores = o->weights_out && all_rows <= 16 && score_bytes <= kMaxScoreBytes;
+    p.scores = o->weights_out && all_rows <= 16 && p.score_len <= kMaxScoreBytes / (4 * heads * all_rows);
     // The step kernel: as many workgroups as run at once (by its registers 2 per CU, 3 up to 64 columns, 1 with wide
     // 2-byte rows), or one for each sequence where that is more.
     const int64_t tile = step_tile_rows(p.max_rows, static_cast<int>(D)), tiles = (p.max_rows + tile - 1) / tile;
@@ -179,7 +178,7 @@ Plan plan_of(const kv_cache *cache, const kv_batch *batch, const kv_attend_optio
         p.tail_parts.splits > 1 ? static_cast<int64_t>(batch->num_queries) * q->heads * p.tail_parts.splits : 0;
     p.tail_stats = take(split * 8);
     p.tail_sums = take(split * D * 4);
-    p.scores_at = take(p.scores ? score_bytes : 0);
+    p.scores_at = take(p.scores ? heads * all_rows * p.score_len * 4 : 0);
     p.bytes = at;
     return p;
 }

@@ -215,3 +215,20 @@ def test_tables_without_entries_need_no_address():
         batch = _batch(attend, **fields)
         need = kvx._lib.kv_attend_workspace(ctypes.byref(cache), ctypes.byref(batch), ctypes.byref(o), ctypes.byref(rows))
         assert need >= 0 if fine else need == kvx.KV_EINVAL, fields
+
+
+def test_workspace_of_the_widest_bounds():
+    """Scores for everything that a call may name would take 2^67 bytes: more than a size holds, and none are kept."""
+    from paper_2609_15021_amd import attend, kvx
+    H, most = 16383, 2**31 - 1024
+    cache = _cache(kvx, kvx.make_layout(1, H, 8, 2, 1, 1))
+    q = _rows(attend, H, token_stride=H * 8, head_stride=8)
+    need = []
+    for weights_out in (None, SOME):
+        b = _batch(attend, num_seqs=65535, max_queries=16, num_queries=16 * 65535, max_len=most, table_len=most,
+                   table_stride=most, starts=SOME)
+        o = attend.KvAttendOptions(cache_dtype=attend.KV_DTYPE_BF16, weights_out=weights_out,
+                                   weights_seq_stride=most * H, weights_head_stride=most)
+        need.append(kvx._lib.kv_attend_workspace(ctypes.byref(cache), ctypes.byref(b), ctypes.byref(o),
+                                                 ctypes.byref(q)))
+    assert need[0] == need[1] > 0
