@@ -8,6 +8,8 @@ ones among them) and ``starts`` (int32 [B + 1]: where each sequence's new tokens
 three are device tensors; ``max_q`` and ``max_len`` are the host's bounds of new tokens and tokens per sequence, by
 default (and at most) what the shapes allow.  Tight bounds size the launches better; numbers beyond them are refused on
 the device (``kv_attend_async_error``), and such a sequence's rows of the outputs hold what they held before.
+
+There is no backward pass: tensors that require a gradient are refused while torch records one.
 """
 from __future__ import annotations
 
