@@ -2,11 +2,18 @@
  * kvx_attend -- operators on a replica's paged KV cache (kv_cache of kvx.h), on AMD Instinct MI355X
  * (gfx950): what a replica computes on a cache that kv_load restored and kv_store will publish.
  *
- *   kv_append   the new tokens' K/V rows into the cache's pages (as they are, or as e4m3 with a scale)
+ *   kv_append   the new tokens' K/V rows into the cache's pages (as they are, or as e4m3 with a scale);
+ *               kv_append_scaled: as e4m3 with a scale for each page, K or V, and head
+ *   kv_rotate   the new tokens' queries and keys normed for each head and rotated by their position; the keys, with
+ *               the values, into the cache's pages
  *   kv_attend   attention of the new tokens over their sequence's cached tokens, from one new token per
  *               sequence to the tail of a prompt behind a restored prefix, and the weight that every
  *               cached token received
- *   kv_keep     from accumulated weights: the tokens that a sequence keeps under a budget
+ *   kv_attend_pages  the same over pages with scales of their own, or over the pages alone that each new token chose
+ *   kv_bounds   of each page the lowest and the highest K in every column
+ *   kv_score    from these, what no token of a page can exceed with a new token's queries: a score to choose pages by
+ *   kv_keep     from accumulated weights: the tokens that a sequence keeps under a budget (and from the scores of
+ *               pages, the pages that a token attends over)
  *   kv_compact  the kept tokens' rows into fresh pages
  *
  * Conventions are kvx.h's: a plain C ABI, explicit HOST and DEVICE pointers, streams as void*, a kv_status from
@@ -47,6 +54,7 @@ extern "C" {
 #define KV_DTYPE_BF16 1
 #define KV_DTYPE_F16 2
 #define KV_DTYPE_E4M3 3  /* caches only: a value is the stored e4m3 (fn: no infinities) times k_scale or v_scale */
+#define KV_DTYPE_F32 4   /* norms' weights only */
 
 /* Async error bits, beside KV_ASYNC_BAD_BLOCK of kvx.h. */
 #define KV_ASYNC_BAD_BATCH 2
@@ -60,6 +68,28 @@ typedef struct kv_rows {
     int32_t heads;
     int32_t dtype;        /* KV_DTYPE_BF16 or KV_DTYPE_F16 */
 } kv_rows;
+
+/* The scales of an E4M3 cache's pages: a value is the stored e4m3 times 2^(e - 127), e the byte of its block, K (0) or V
+ * (1), and head, at data + block*block_stride + kv*kv_stride + head; e is 1 to 254.  (Where strides are padded to 16 bytes,
+ * the bytes of a layer are a kv_cache of their own with one token a block, which kv_store and kv_load move by the same
+ * block tables: num_kv_heads 1, head_dim the padded heads, elem_bytes 1, block_size 1, chunk_tokens C / BS.) */
+typedef struct kv_page_scales {
+    uint8_t *data;         /* DEVICE */
+    int64_t block_stride;  /* bytes, >= kv_stride + heads */
+    int64_t kv_stride;     /* bytes, >= heads */
+} kv_page_scales;
+
+/* The pages that each new token chose, for each KV head (heads == 1: the same for all): of row r and head h the first
+ * counts[r] numbers at pages + r*token_stride + h*head_stride, each a place in its sequence's block table.  As kv_keep
+ * leaves them; in any order.  A page that is named twice takes part twice. */
+typedef struct kv_page_list {
+    const int32_t *pages;  /* DEVICE */
+    const int32_t *counts; /* DEVICE int32[num_queries] */
+    int64_t token_stride;  /* elements, >= 0 */
+    int64_t head_stride;
+    int32_t heads;         /* the cache's KV heads, or 1 */
+    int32_t budget;        /* most pages of a row, >= 1 */
+} kv_page_list;
 
 typedef struct kv_batch {
     int32_t num_seqs;            /* sequences; 0 is a no-op */
@@ -107,6 +137,50 @@ KV_API kv_status kv_append(const kv_cache *cache, int32_t layer, const kv_batch 
                            const kv_rows *v, int32_t cache_dtype, float k_scale, float v_scale, void *stream);
 
 /*
+ * kv_append_scaled -- kv_append into an E4M3 cache whose pages have scales.  Of each page that a new token lies in, K and
+ * V, and head, the scale is the smallest power of two with |x| <= 448 * scale for every finite x of the call's new rows
+ * in it, and not smaller than it was where the page holds older tokens (of a page whose slot 0 is a new token's nothing
+ * is older).  Where it grows, the older rows are rounded to it: e4m3(stored * old scale / new scale), which is exact but for
+ * what leaves e4m3's normal numbers.  x is stored as e4m3(clamp(x / scale, -448, 448)), rounded to nearest even; NaN
+ * stays NaN.  Every other byte of the cache and the scales is untouched.  Errors and preconditions as kv_append;
+ * KV_EINVAL also for strides of scales that overlap.
+ */
+KV_API kv_status kv_append_scaled(const kv_cache *cache, int32_t layer, const kv_batch *batch, const kv_rows *k,
+                                  const kv_rows *v, const kv_page_scales *scales, void *stream);
+
+/* Options of kv_rotate.  Zero-initialised fields take the documented defaults. */
+typedef struct kv_rotate_options {
+    int32_t cache_dtype;       /* KV_DTYPE_*: what the cache's elements are (required) */
+    int32_t rotary_dim;        /* columns that are rotated, the first ones of a row: even, 0 to D */
+    int32_t interleaved;       /* pairs of columns i: 0: (i, i + rotary_dim / 2); 1: (2i, 2i + 1) */
+    int32_t weight_dtype;      /* of q_weight and k_weight: KV_DTYPE_F32, or the rows' type */
+    const double *freqs;       /* DEVICE double[rotary_dim / 2]: radians per position of each pair */
+    const int32_t *positions;  /* DEVICE int32[num_queries], or NULL: a token's place in its sequence */
+    const void *q_weight;      /* DEVICE [D], or NULL: queries are not normed */
+    const void *k_weight;      /* DEVICE [D], or NULL: keys are not normed */
+    float eps;                 /* of the norms, >= 0 */
+    float weight_offset;       /* added to the norms' weights */
+    float magnitude;           /* factor of the rotated columns; 0 = 1 */
+    float k_scale, v_scale;    /* 0 = 1; as in kv_append */
+    int32_t reserved;          /* must be 0 */
+    const kv_page_scales *scales;  /* HOST, or NULL; E4M3 caches: as in kv_append_scaled, then k_scale and v_scale are 1 */
+} kv_rotate_options;
+
+/*
+ * kv_rotate -- norm, rotate, and append.  Of each new token's row x of each head of q and k:
+ *   y_d = x_d / sqrt(mean of x^2 + eps) * (weight_offset + weight_d)  (or x_d, without weights), and for each pair (a, b)
+ *   of the first rotary_dim columns, with t = position * freqs[i]: (a cos t - b sin t, b cos t + a sin t) * magnitude.
+ * A row is rounded once, at the end; sums are held in 32 bits, positions times frequencies in 64.  q's rows go to `out`
+ * (same type, heads; may be q itself), k's rotated rows and v's as they are into layer `layer` of the cache, as kv_append (with
+ * scales: kv_append_scaled) puts them there.  Rows of out whose token has no place (before token 0) are rotated by its
+ * place or position all the same; rows of no sequence are left as they were.
+ * Errors as kv_append; KV_EINVAL also for a rotary_dim that is odd or outside [0, D], a NULL freqs with one, and negative or
+ * not finite numbers.
+ */
+KV_API kv_status kv_rotate(const kv_cache *cache, int32_t layer, const kv_batch *batch, const kv_rotate_options *options,
+                           const kv_rows *q, const kv_rows *out, const kv_rows *k, const kv_rows *v, void *stream);
+
+/*
  * kv_attend -- out[row] = v_scale * sum over its tokens of softmax(s) * v, rounded once to q's type, and lse[row] = log
  * of the sum of exp(s), for every new row; query head h reads KV head h / (q->heads / H).  A row that sees no token
  * gets 0 and -infinity.  Sums, largest scores and lse are held in 32 bits.  The weights exp(s) meet V as two numbers of
@@ -132,6 +206,60 @@ KV_API kv_status kv_attend(const kv_cache *cache, int32_t layer, const kv_batch 
  * the kv_status that kv_attend would return. */
 KV_API int64_t kv_attend_workspace(const kv_cache *cache, const kv_batch *batch, const kv_attend_options *options,
                                    const kv_rows *q);
+
+/*
+ * kv_attend_pages -- kv_attend where an E4M3 cache's pages have scales (scales; options' k_scale and v_scale are then 1), or
+ * where each new token attends over the pages that it chose alone (list), or both; one of them must be given.  Token t of a
+ * chosen page takes part where t <= p and, with window > 0, p - t < window, and slopes count in p - t, as in kv_attend; a row that
+ * chose nothing it sees gets 0 and -infinity.  With scales, and with a list in every E4M3 cache, the weights exp(s) times
+ * V's scale meet the stored e4m3 as two numbers of bfloat16, or in sequences of more than 64 rows per KV head without a list, for
+ * bfloat16 rows, and unless full_weights asks for two, as one.  With a list a call reads each row's pages for itself.
+ * weights_in and weights_out must be NULL.  Errors as kv_attend; KV_EINVAL also for a list that contradicts the cache, and
+ * KV_EUNSUPPORTED for weights_out, or more than 2^31 - 1024 tokens in `budget` pages.
+ */
+KV_API kv_status kv_attend_pages(const kv_cache *cache, int32_t layer, const kv_batch *batch,
+                                 const kv_attend_options *options, const kv_page_scales *scales,
+                                 const kv_page_list *list, const kv_rows *q, const kv_rows *out, float *lse,
+                                 void *workspace, int64_t workspace_bytes, void *stream);
+
+/* Bytes of workspace that kv_attend_pages needs, as kv_attend_workspace. */
+KV_API int64_t kv_attend_pages_workspace(const kv_cache *cache, const kv_batch *batch, const kv_attend_options *options,
+                                         const kv_page_scales *scales, const kv_page_list *list, const kv_rows *q);
+
+/*
+ * kv_bounds -- of each page of layer `layer` that a new token lies in, and each KV head, the lowest and the highest stored K
+ * of every column over the page's tokens t < lens[b], new and older ones.  They go where `bounds`, a kv_cache of the same
+ * heads, head_dim, elem_bytes and at least as many blocks with block_size 1, has K and V of the same block's one token,
+ * in the cache's own type (kv_store and kv_load move it as any cache, by the same tables).  Of an E4M3 cache these are
+ * stored values; scales apply to them as to the page.  A NaN does not count; a column without a number gets 0 twice.  Bounds
+ * of other pages are untouched.  For a restored prefix, all its tokens are new ones (lens[b] of them).
+ * Errors as kv_append; KV_EINVAL also for bounds that contradict the cache.
+ */
+KV_API kv_status kv_bounds(const kv_cache *cache, int32_t layer, const kv_batch *batch, int32_t cache_dtype,
+                           const kv_cache *bounds, void *stream);
+
+/* Options of kv_score. */
+typedef struct kv_score_options {
+    int32_t cache_dtype;  /* KV_DTYPE_*: what the bounds' elements are (required) */
+    int32_t block_size;   /* tokens of a page of the cache that the bounds are of */
+    float scale;          /* 0 = 1; e.g. kv_attend's scale times k_scale */
+    int32_t reserved;     /* must be 0 */
+    const kv_page_scales *scales;  /* HOST, or NULL: E4M3 pages' scales, of which K's are read */
+    int64_t token_stride, head_stride;  /* elements between rows of scores */
+} kv_score_options;
+
+/*
+ * kv_score -- for each new row r of token p, KV head h, and page j <= p / block_size of its sequence, scores[r*token_stride +
+ * h*head_stride + j] = scale * max over the query heads of h of sum over d of max(q_d low_d, q_d high_d): no token of the
+ * page has a larger scale * (q . k) with any of these heads.  Sums are held in 32 bits.  A page whose block id is bad gets
+ * -infinity.  counts[r] = p / block_size + 1 (0 for a row before token 0): kv_keep's lens, for num_seqs = num_queries
+ * sequences of pages.  Scores of pages from there on are left as they were.
+ *   bounds: kv_bounds's; batch: the sequences as in kv_attend, max_len in tokens, at most table_len * block_size.
+ *   scores: DEVICE float, rows of (max_len + block_size - 1) / block_size elements; counts: DEVICE int32[num_queries], or NULL.
+ * Errors as kv_attend.
+ */
+KV_API kv_status kv_score(const kv_cache *bounds, int32_t layer, const kv_batch *batch, const kv_score_options *options,
+                          const kv_rows *q, float *scores, int32_t *counts, void *stream);
 
 /*
  * kv_keep -- which tokens of each sequence (and KV head) a cache of `budget` tokens keeps.  A sequence of at most

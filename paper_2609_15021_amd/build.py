@@ -29,7 +29,8 @@ COMMON = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}", "-Wall", "-Wex
 
 KVX_SOURCES = ["kvx_check.cpp", "kvx_engine.cpp", "kvx_gather.hip", "kvx_state.hip", "kvx_index.cpp", "kvx_tier.cpp",
                "kvx_noalloc.hip", "kvx_paged.cpp", "kvx_append.hip", "kvx_attend.hip",
-               "kvx_attend_step.hip", "kvx_attend_tail.hip", "kvx_keep.hip", "kvx_compact.hip"]
+               "kvx_attend_step.hip", "kvx_attend_tail.hip", "kvx_attend_pages.hip", "kvx_attend_tail_scaled.hip",
+               "kvx_scaled.hip", "kvx_rotate.hip", "kvx_choose.hip", "kvx_keep.hip", "kvx_compact.hip"]
 
 
 def _run(cmd, verbose):

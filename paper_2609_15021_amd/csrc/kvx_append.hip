@@ -7,13 +7,11 @@
 #include <algorithm>
 #include <cmath>
 
-#include "kvx_paged.h"
+#include "kvx_rows.h"
 
 namespace kvx {
 
 namespace {
-
-typedef uint32_t vec16 __attribute__((ext_vector_type(4)));
 
 struct AppendArgs {
     Pages pages;
@@ -23,14 +21,6 @@ struct AppendArgs {
     int32_t row_vecs, token_vecs;
     float k_scale, v_scale;
 };
-
-__device__ __forceinline__ float to_float(uint32_t bits, int dtype) {
-    return dtype == KV_DTYPE_BF16 ? __builtin_bit_cast(float, bits << 16)
-                                  : static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(bits)));
-}
-
-// Clamped to e4m3's largest value; NaN stays.
-__device__ __forceinline__ float clamp_e4m3(float x) { return x > 448.f ? 448.f : x < -448.f ? -448.f : x; }
 
 // Eight 2-byte values as e4m3 of x / scale, rounded to nearest even: 8 bytes.  (A division, not a product with the
 // inverse: the quotient is rounded once to 32 bits and once to 8.)
@@ -84,12 +74,10 @@ __global__ __launch_bounds__(kThreads) void append_kernel(const AppendArgs a) {
     }
 }
 
-Rows rows_of(const kv_rows *r) {
-    return Rows{static_cast<uint8_t *>(r->data), r->token_stride * 2, r->head_stride * 2};
-}
+}  // namespace
 
-kv_status append(const kv_cache *cache, int32_t layer, const kv_batch *batch, const kv_rows *k, const kv_rows *v,
-                 int32_t cache_dtype, float k_scale, float v_scale, hipStream_t stream) {
+kv_status check_append(const kv_cache *cache, int32_t layer, const kv_batch *batch, const kv_rows *k, const kv_rows *v,
+                       int32_t cache_dtype) {
     kv_status st = check_layer(cache, layer);
     if (st == KV_OK)
         st = check_dtype(cache, cache_dtype);
@@ -106,15 +94,34 @@ kv_status append(const kv_cache *cache, int32_t layer, const kv_batch *batch, co
         return fail(KV_EINVAL, "rows of %d and %d heads for a cache of %d", k->heads, v->heads, H);
     if (k->dtype != v->dtype)
         return fail(KV_EINVAL, "k and v have different types");
-    const bool quantised = cache_dtype == KV_DTYPE_E4M3;
-    if (!quantised && k->dtype != cache_dtype)
+    if (cache_dtype != KV_DTYPE_E4M3 && k->dtype != cache_dtype)
         return fail(KV_EINVAL, "rows of type %d for a cache of type %d", k->dtype, cache_dtype);
+    return KV_OK;
+}
+
+kv_status check_factors(int32_t cache_dtype, float k_scale, float v_scale) {
     k_scale = k_scale == 0.f ? 1.f : k_scale;
     v_scale = v_scale == 0.f ? 1.f : v_scale;
     if (!(k_scale > 0.f && std::isfinite(k_scale)) || !(v_scale > 0.f && std::isfinite(v_scale)) ||
-        (!quantised && (k_scale != 1.f || v_scale != 1.f)))
+        (cache_dtype != KV_DTYPE_E4M3 && (k_scale != 1.f || v_scale != 1.f)))
         return fail(KV_EINVAL, "scales must be positive and finite, and 1 for a cache of 2-byte elements (got %g and "
                     "%g)", k_scale, v_scale);
+    return KV_OK;
+}
+
+namespace {
+
+kv_status append(const kv_cache *cache, int32_t layer, const kv_batch *batch, const kv_rows *k, const kv_rows *v,
+                 int32_t cache_dtype, float k_scale, float v_scale, hipStream_t stream) {
+    kv_status st = check_append(cache, layer, batch, k, v, cache_dtype);
+    if (st == KV_OK)
+        st = check_factors(cache_dtype, k_scale, v_scale);
+    if (st != KV_OK)
+        return st;
+    const int H = cache->layout.num_kv_heads;
+    const bool quantised = cache_dtype == KV_DTYPE_E4M3;
+    k_scale = k_scale == 0.f ? 1.f : k_scale;
+    v_scale = v_scale == 0.f ? 1.f : v_scale;
     if (batch->num_seqs == 0 || batch->num_queries == 0)
         return KV_OK;
     st = check_on_current_device(cache);

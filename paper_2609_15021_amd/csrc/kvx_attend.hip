@@ -79,6 +79,36 @@ kv_status check_attend(const kv_cache *cache, const kv_batch *batch, const kv_at
     return KV_OK;
 }
 
+// And those of kv_attend_pages.
+kv_status check_pages(const kv_cache *cache, const kv_batch *batch, const kv_attend_options *o,
+                      const kv_page_scales *scales, const kv_page_list *list) {
+    if (!scales && !list)
+        return fail(KV_EINVAL, "scales and list are both NULL");
+    if (o->weights_out)
+        return fail(KV_EUNSUPPORTED, "weights_out with scales of pages or chosen pages");
+    if (scales) {
+        const kv_status st = check_scales(cache, o->cache_dtype, scales);
+        if (st != KV_OK)
+            return st;
+        if ((o->k_scale != 0.f && o->k_scale != 1.f) || (o->v_scale != 0.f && o->v_scale != 1.f))
+            return fail(KV_EINVAL, "k_scale and v_scale (%g and %g) beside scales of pages", o->k_scale, o->v_scale);
+    }
+    if (list) {
+        if (list->heads != 1 && list->heads != cache->layout.num_kv_heads)
+            return fail(KV_EINVAL, "list has %d heads for a cache of %d", list->heads, cache->layout.num_kv_heads);
+        if (list->budget < 1 || list->token_stride < 0 || list->head_stride < 0)
+            return fail(KV_EINVAL, "list: budget must be positive and strides not negative (got %d, %lld, %lld)",
+                        list->budget, static_cast<long long>(list->token_stride),
+                        static_cast<long long>(list->head_stride));
+        if (int64_t{list->budget} * cache->layout.block_size > INT32_MAX - 1023)
+            return fail(KV_EUNSUPPORTED, "%d chosen pages of %d tokens (at most 2^31 - 1024 tokens)", list->budget,
+                        cache->layout.block_size);
+        if (batch->num_seqs > 0 && batch->num_queries > 0 && (!list->pages || !list->counts))
+            return fail(KV_EINVAL, "list: pages and counts must not be NULL");
+    }
+    return KV_OK;
+}
+
 // How a call is cut, and what its workspace holds.  Only the host's numbers count.
 struct Plan {
     int32_t max_queries, max_rows;  // of a sequence; rows per KV head in the step kernel
@@ -183,12 +213,43 @@ Plan plan_of(const kv_cache *cache, const kv_batch *batch, const kv_attend_optio
     return p;
 }
 
+// A call over chosen pages: its rows' lists are cut where rows and heads alone leave workgroups' places free.
+struct PagesPlan {
+    Chosen chosen;
+    int64_t stats, sums, bytes;
+};
+
+PagesPlan plan_of(const kv_cache *cache, const kv_batch *batch, const kv_page_list *list, const kv_rows *q) {
+    const int64_t H = cache->layout.num_kv_heads, D = cache->layout.head_dim, group = q->heads / H;
+    PagesPlan p{};
+    const int64_t rows = batch->num_seqs > 0 ? batch->num_queries : 0, heads = rows * q->heads;
+    const int64_t tile = step_tile_rows(static_cast<int>(std::min<int64_t>(group, INT32_MAX)), static_cast<int>(D));
+    const int64_t groups = std::max<int64_t>(rows * H * ((group + tile - 1) / tile), 1);
+    const int64_t at_once = D <= 64 ? 768 : D > 128 && cache->layout.elem_bytes == 2 ? 256 : 512;
+    const int64_t longest = int64_t{list->budget} * cache->layout.block_size;
+    p.chosen.pages = list->pages;
+    p.chosen.counts = list->counts;
+    p.chosen.token_stride = list->token_stride;
+    p.chosen.head_stride = list->heads == 1 ? 0 : list->head_stride;
+    p.chosen.budget = list->budget;
+    p.chosen.splits = static_cast<int32_t>(
+        std::min({std::max<int64_t>(at_once / groups, 1), (longest + 127) / 128, int64_t{64}}));
+    const int64_t split = p.chosen.splits > 1 ? heads * p.chosen.splits : 0;
+    const int64_t lse = round_up(heads * 4, 16);
+    p.stats = lse;
+    p.sums = p.stats + round_up(split * 8, 16);
+    p.bytes = p.sums + round_up(split * D * 4, 16);
+    return p;
+}
+
 kv_status attend(const kv_cache *cache, int32_t layer, const kv_batch *batch, const kv_attend_options *o,
-                 const kv_rows *q, const kv_rows *out, float *lse, void *workspace, int64_t workspace_bytes,
-                 hipStream_t stream) {
+                 const kv_page_scales *scales, const kv_page_list *list, bool pages, const kv_rows *q,
+                 const kv_rows *out, float *lse, void *workspace, int64_t workspace_bytes, hipStream_t stream) {
     kv_status st = check_layer(cache, layer);
     if (st == KV_OK)
         st = check_attend(cache, batch, o, q);
+    if (st == KV_OK && pages)
+        st = check_pages(cache, batch, o, scales, list);
     if (st == KV_OK)
         st = check_rows(cache, batch, out, "out");
     if (st != KV_OK)
@@ -201,8 +262,11 @@ kv_status attend(const kv_cache *cache, int32_t layer, const kv_batch *batch, co
                                 (batch->num_queries > 0 && out->heads > 1 && out->head_stride < D)))
         return fail(KV_EINVAL, "rows of out (strides %lld and %lld) are shorter than %d elements",
                     static_cast<long long>(out->token_stride), static_cast<long long>(out->head_stride), D);
-    const Plan plan = plan_of(cache, batch, o, q);
-    const int64_t need = plan.bytes;
+    const Plan plan = list ? Plan{} : plan_of(cache, batch, o, q);
+    const PagesPlan listed = list ? plan_of(cache, batch, list, q) : PagesPlan{};
+    const int64_t need = list ? listed.bytes : plan.bytes;
+    if (list && int64_t{batch->num_queries} * listed.chosen.splits > (int64_t{1} << 23))
+        return fail(KV_EUNSUPPORTED, "%d new tokens that chose pages are too many for one call", batch->num_queries);
     if (workspace_bytes < need || (need > 0 && !workspace))
         return fail(KV_EINVAL, "workspace of %lld bytes; %lld are needed", static_cast<long long>(workspace_bytes),
                     static_cast<long long>(need));
@@ -250,14 +314,27 @@ kv_status attend(const kv_cache *cache, int32_t layer, const kv_batch *batch, co
     a.cache_type = o->cache_dtype;
     a.full_weights = o->full_weights;
     a.by_group = divisor(a.group);
+    a.scales = scales_of(scales);
+    if (list) {
+        Chosen chosen = listed.chosen;
+        chosen.stats = at(listed.stats);
+        chosen.sums = at(listed.sums);
+        if (batch->num_queries > 0)
+            KVX_HIP(launch_pages(a, chosen, stream));
+        if (batch->num_queries > 0 && chosen.splits > 1)
+            KVX_HIP(launch_join_pages(a, chosen, std::min(batch->max_queries, batch->num_queries), stream));
+        return KV_OK;
+    }
     if (plan.max_queries > 0) {
         if (plan.listed)
             KVX_HIP(launch_share(a, step, stream));
-        KVX_HIP(launch_step(a, step, plan.max_queries, stream));
+        KVX_HIP(scales ? launch_step_scaled(a, step, plan.max_queries, stream)
+                       : launch_step(a, step, plan.max_queries, stream));
         if (!step.alone)
             KVX_HIP(launch_join_step(a, step, plan.max_queries, stream));
         if (plan.tail) {
-            KVX_HIP(launch_tail(a, tail, plan.max_queries, stream));
+            KVX_HIP(scales ? launch_tail_scaled(a, tail, plan.max_queries, stream)
+                           : launch_tail(a, tail, plan.max_queries, stream));
             if (tail.splits > 1)
                 KVX_HIP(launch_join_tail(a, tail, plan.max_queries, stream));
         }
@@ -289,7 +366,31 @@ kv_status kv_attend(const kv_cache *cache, int32_t layer, const kv_batch *batch,
                     const kv_rows *q, const kv_rows *out, float *lse, void *workspace, int64_t workspace_bytes,
                     void *stream) {
     return kvx::guarded([&]() -> kv_status {
-        return kvx::attend(cache, layer, batch, options, q, out, lse, workspace, workspace_bytes,
+        return kvx::attend(cache, layer, batch, options, nullptr, nullptr, false, q, out, lse, workspace,
+                           workspace_bytes, static_cast<hipStream_t>(stream));
+    });
+}
+
+int64_t kv_attend_pages_workspace(const kv_cache *cache, const kv_batch *batch, const kv_attend_options *options,
+                                  const kv_page_scales *scales, const kv_page_list *list, const kv_rows *q) {
+    int64_t bytes = 0;
+    const kv_status st = kvx::guarded([&]() -> kv_status {
+        kv_status checked = kvx::check_attend(cache, batch, options, q);
+        if (checked == KV_OK)
+            checked = kvx::check_pages(cache, batch, options, scales, list);
+        if (checked == KV_OK)
+            bytes = list ? kvx::plan_of(cache, batch, list, q).bytes : kvx::plan_of(cache, batch, options, q).bytes;
+        return checked;
+    });
+    return st == KV_OK ? bytes : st;
+}
+
+kv_status kv_attend_pages(const kv_cache *cache, int32_t layer, const kv_batch *batch,
+                          const kv_attend_options *options, const kv_page_scales *scales, const kv_page_list *list,
+                          const kv_rows *q, const kv_rows *out, float *lse, void *workspace, int64_t workspace_bytes,
+                          void *stream) {
+    return kvx::guarded([&]() -> kv_status {
+        return kvx::attend(cache, layer, batch, options, scales, list, true, q, out, lse, workspace, workspace_bytes,
                            static_cast<hipStream_t>(stream));
     });
 }

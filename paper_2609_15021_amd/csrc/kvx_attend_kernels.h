@@ -31,6 +31,7 @@ struct AttendArgs {
     float *scores;  // [sequence][KV head][score_cap][score_len] in powers of 2, for weights_out; or NULL
     int64_t score_len;
     int32_t score_cap;
+    Scales scales;  // of pages, where the kernel is for them
 };
 
 // How the tail kernel splits the tokens of a tile of rows over workgroups, and what the parts of a row leave for the
@@ -71,6 +72,15 @@ struct Shares {
     float *sums;                      // [KV head][item][row_cap][D], unscaled
     float *stats;                     // [KV head][item][row_cap][2]: largest score and sum, in powers of 2
     int32_t *items_of;                // NULL, or: length of a part; [sequence]: first item, parts; [item]: sequence, split
+};
+
+// What each new token chose (kv_page_list), and how its pages are cut into parts, each by its own number of them.
+struct Chosen {
+    const int32_t *pages, *counts;
+    int64_t token_stride, head_stride;  // 0 where the heads share a choice
+    int32_t budget, splits;             // most parts of a row
+    float *sums;                        // [row][query head][splits][D], unscaled
+    float *stats;                       // [row][query head][splits][2]: largest score and sum, in powers of 2
 };
 
 // A sequence's part: `split` of `parts`, `len` tokens each; its first part is item `item0`.
@@ -178,6 +188,47 @@ __device__ __forceinline__ bool share_of(const AttendArgs &a, const Shares &shar
     return s.parts > 0;
 }
 
+// Parts of a row that chose `count` pages, and their length; -1 where the number is bad.
+__device__ __forceinline__ int chosen_parts(const AttendArgs &a, const Chosen &chosen, int count, int &len) {
+    if (count < 0 || count > chosen.budget)
+        return -1;
+    const int tokens = count * a.pages.BS;
+    len = max(((tokens + chosen.splits - 1) / chosen.splits + 31) & ~31, 128);
+    return max((tokens + len - 1) / len, 1);
+}
+
+// Workgroup `item` of a launch over chosen pages: its row as a sequence of its own (seq.n tokens, the row's own the last of
+// them), the row's part, and its list for head h; false if there is none.
+__device__ __forceinline__ bool chosen_of(const AttendArgs &a, const Chosen &chosen, int item, int h, Share &s,
+                                          Sequence &seq, int &count, const int32_t *&list) {
+    const int row = item / chosen.splits, lane = threadIdx.x & 63;
+    s.split = item - row * chosen.splits;
+    s.item0 = item;
+    s.b = row;
+    if (a.batch.starts) {
+        // The one sequence whose new tokens the row is among.
+        s.b = -1;
+        for (int b0 = 0; b0 < a.num_seqs && s.b < 0; b0 += 64) {
+            const int b = min(b0 + lane, a.num_seqs - 1);
+            const uint64_t found = __ballot(row >= a.batch.starts[b] && row < a.batch.starts[b + 1]);
+            if (found)
+                s.b = b0 + __builtin_ctzll(found);
+        }
+    }
+    if (s.b < 0 || s.b >= a.num_seqs || !sequence(a.batch, s.b, a.pages.err, seq))
+        return false;
+    const int own = seq.n - seq.nq + (row - seq.q0);
+    count = chosen.counts[row];
+    s.parts = chosen_parts(a, chosen, count, s.len);
+    if (s.parts < 0 && threadIdx.x == 0)
+        report(a.pages.err, KV_ASYNC_BAD_BATCH);
+    if (s.split >= s.parts)
+        return false;
+    seq = Sequence{own + 1, row, 1};
+    list = chosen.pages + row * chosen.token_stride + h * chosen.head_stride;
+    return true;
+}
+
 __device__ __forceinline__ int parts_of(const Span &s, int len) {
     return s.end > s.start ? (s.end - s.start - 1) / len + 1 : 1;
 }
@@ -191,6 +242,11 @@ struct Bf16 {
     static __device__ __forceinline__ uint32_t from_e4m3(uint32_t x, bool high) {
         return high ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.f, true))
                     : __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.f, false));
+    }
+    // Times a power of two.
+    static __device__ __forceinline__ uint32_t from_e4m3(uint32_t x, bool high, float by) {
+        return high ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, by, true))
+                    : __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, by, false));
     }
     static __device__ __forceinline__ uint32_t pack(float a, float b) {
         pair p;
@@ -260,6 +316,11 @@ hipError_t launch_tail(const AttendArgs &a, const Parts &parts, int max_queries,
 // Join what these left of rows in parts.
 hipError_t launch_join_step(const AttendArgs &a, const Shares &shares, int max_queries, hipStream_t stream);
 hipError_t launch_join_tail(const AttendArgs &a, const Parts &parts, int max_queries, hipStream_t stream);
+hipError_t launch_step_scaled(const AttendArgs &a, const Shares &shares, int max_queries, hipStream_t stream);
+hipError_t launch_tail_scaled(const AttendArgs &a, const Parts &parts, int max_queries, hipStream_t stream);
+// Every row over the pages that it chose.
+hipError_t launch_pages(const AttendArgs &a, const Chosen &chosen, hipStream_t stream);
+hipError_t launch_join_pages(const AttendArgs &a, const Chosen &chosen, int max_queries, hipStream_t stream);
 // weights_out, from the scores that the step kernel left, or with the scores taken again.
 hipError_t launch_weigh_step(const AttendArgs &a, hipStream_t stream);
 hipError_t launch_weigh(const AttendArgs &a, hipStream_t stream);

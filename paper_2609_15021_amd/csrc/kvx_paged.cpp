@@ -122,6 +122,19 @@ kv_status check_rows(const kv_cache *cache, const kv_batch *batch, const kv_rows
     return KV_OK;
 }
 
+kv_status check_scales(const kv_cache *cache, int32_t cache_dtype, const kv_page_scales *scales) {
+    if (cache_dtype != KV_DTYPE_E4M3)
+        return fail(KV_EINVAL, "scales of pages for a cache of type %d", cache_dtype);
+    const int64_t H = cache->layout.num_kv_heads;
+    if (!scales->data)
+        return fail(KV_EINVAL, "scales: data must not be NULL");
+    if (scales->kv_stride < H || scales->block_stride < scales->kv_stride ||
+        scales->block_stride - scales->kv_stride < H)
+        return fail(KV_EINVAL, "scales of %lld heads overlap (strides of %lld and %lld bytes)", static_cast<long long>(H),
+                    static_cast<long long>(scales->block_stride), static_cast<long long>(scales->kv_stride));
+    return KV_OK;
+}
+
 kv_status check_on_current_device(const kv_cache *cache) {
     int cur = -1;
     KVX_HIP(hipGetDevice(&cur));
@@ -160,6 +173,14 @@ Batch batch_of(const kv_batch *batch) {
     b.max_queries = batch->max_queries;
     b.max_len = batch->max_len;
     return b;
+}
+
+Scales scales_of(const kv_page_scales *scales) {
+    return scales ? Scales{scales->data, scales->block_stride, scales->kv_stride} : Scales{nullptr, 0, 0};
+}
+
+Rows rows_of(const kv_rows *rows) {
+    return Rows{static_cast<uint8_t *>(rows->data), rows->token_stride * 2, rows->head_stride * 2};
 }
 
 }  // namespace kvx

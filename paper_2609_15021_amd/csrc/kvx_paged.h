@@ -35,6 +35,19 @@ struct Rows {
     int64_t token_stride, head_stride;  // bytes
 };
 
+// kv_page_scales on the device; data NULL: pages have none.
+struct Scales {
+    uint8_t *data;
+    int64_t block_stride, kv_stride;
+};
+
+__device__ __forceinline__ uint8_t *scale_at(const Scales &s, int block, int kv, int h) {
+    return s.data + block * s.block_stride + kv * s.kv_stride + h;
+}
+
+// 2^(e - 127) for e from 1 to 254.
+__device__ __forceinline__ float power_of(int e) { return __builtin_bit_cast(float, e << 23); }
+
 // One sequence of a batch: n tokens, its new ones the rows q0 .. q0 + nq.
 struct Sequence {
     int n, q0, nq;
@@ -88,9 +101,12 @@ kv_status check_layer(const kv_cache *cache, int32_t layer);
 kv_status check_batch(const kv_cache *cache, const kv_batch *batch);
 kv_status check_rows(const kv_cache *cache, const kv_batch *batch, const kv_rows *rows, const char *name);
 kv_status check_dtype(const kv_cache *cache, int32_t cache_dtype);
+kv_status check_scales(const kv_cache *cache, int32_t cache_dtype, const kv_page_scales *scales);
 kv_status check_on_current_device(const kv_cache *cache);
 kv_status error_word(int32_t **out);  // the current device's
 Pages pages_of(const kv_cache *cache, int32_t layer, int32_t *err);
 Batch batch_of(const kv_batch *batch);
+Scales scales_of(const kv_page_scales *scales);  // NULL: none
+Rows rows_of(const kv_rows *rows);
 
 }  // namespace kvx
