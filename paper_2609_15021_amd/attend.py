@@ -15,6 +15,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import struct
 
 import torch
 
@@ -26,6 +27,7 @@ KV_DTYPE_E4M3 = 3
 KV_DTYPE_F32 = 4
 KV_ASYNC_BAD_BATCH = 2
 
+_ROW_TYPES = {torch.bfloat16: KV_DTYPE_BF16, torch.float16: KV_DTYPE_F16}
 _DTYPES = {torch.bfloat16: KV_DTYPE_BF16, torch.float16: KV_DTYPE_F16, torch.float8_e4m3fn: KV_DTYPE_E4M3}
 
 EXPORTS = ("kv_append", "kv_append_scaled", "kv_rotate", "kv_attend", "kv_attend_workspace", "kv_attend_pages",
@@ -76,21 +78,29 @@ class KvScoreOptions(ctypes.Structure):
                 ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
 
 
+# The same structures as bytes, which take a third of the time to make; a call reads them before it returns.
+_pack_rows = struct.Struct("qqqii").pack
+_pack_batch = struct.Struct("iiiiiiqqqq").pack
+_pack_scales = struct.Struct("qqq").pack
+_pack_list = struct.Struct("qqqqii").pack
+_pack_rotate = struct.Struct("iiiiqqqqfffffiP").pack
+_pack_score = struct.Struct("iifiPqq").pack
+
+
 def _declare(lib):
     P, i32, i64, f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
-    cache, batch, rows = ctypes.POINTER(KvCache), ctypes.POINTER(KvBatch), ctypes.POINTER(KvRows)
-    options = ctypes.POINTER(KvAttendOptions)
-    scales, pages = ctypes.POINTER(KvPageScales), ctypes.POINTER(KvPageList)
+    # Structures: a pointer, or bytes.
+    cache, batch, rows, options, scales, pages = ctypes.POINTER(KvCache), P, P, P, P, P
     for name, args, res in (
             ("kv_append", [cache, i32, batch, rows, rows, i32, f32, f32, P], i32),
             ("kv_append_scaled", [cache, i32, batch, rows, rows, scales, P], i32),
-            ("kv_rotate", [cache, i32, batch, ctypes.POINTER(KvRotateOptions), rows, rows, rows, rows, P], i32),
+            ("kv_rotate", [cache, i32, batch, options, rows, rows, rows, rows, P], i32),
             ("kv_attend", [cache, i32, batch, options, rows, rows, P, P, i64, P], i32),
             ("kv_attend_workspace", [cache, batch, options, rows], i64),
             ("kv_attend_pages", [cache, i32, batch, options, scales, pages, rows, rows, P, P, i64, P], i32),
             ("kv_attend_pages_workspace", [cache, batch, options, scales, pages, rows], i64),
             ("kv_bounds", [cache, i32, batch, i32, cache, P], i32),
-            ("kv_score", [cache, i32, batch, ctypes.POINTER(KvScoreOptions), rows, P, P, P], i32),
+            ("kv_score", [cache, i32, batch, options, rows, P, P, P], i32),
             ("kv_keep", [P, i64, i64, P, i32, i32, i32, i32, i32, i32, P, P, P, P, i64, P], i32),
             ("kv_keep_workspace", [i32, i32, i32, i32], i64),
             ("kv_compact", [cache, i32, i32, P, i64, i32, P, i32, i32, P, P, i64, i32, P], i32),
@@ -107,15 +117,23 @@ _declare(_lib)
 
 
 def _ints(t, name: str, dims: int, device: int, rows=None):
-    """A tensor of int32 on the call's device whose last dimension is dense."""
-    if not isinstance(t, torch.Tensor) or t.dtype is not torch.int32 or t.dim() != dims or \
-            (t.stride(-1) != 1 and t.shape[-1] > 1 and t.numel()):
+    """A tensor of int32 on the call's device whose last dimension is dense: its shape and strides."""
+    if not isinstance(t, torch.Tensor) or t.dtype is not torch.int32 or len(shape := t.shape) != dims or \
+            ((strides := t.stride())[-1] != 1 and shape[-1] > 1 and t.numel()):
         raise TypeError(f"{name} must be a {dims}-dimensional int32 device tensor with a dense last dimension")
     if t.get_device() != device:
         _elsewhere(t, name, device)
-    if rows is not None and t.shape[0] != rows:
-        raise ValueError(f"{name} has {t.shape[0]} rows; {rows} are needed")
-    return t
+    if rows is not None and shape[0] != rows:
+        raise ValueError(f"{name} has {shape[0]} rows; {rows} are needed")
+    return shape, strides
+
+
+def _dense_ints(t, name: str, dims: int, device: int, rows: int) -> int:
+    """The address of a contiguous one."""
+    _ints(t, name, dims, device, rows)
+    if not t.is_contiguous():
+        raise TypeError(f"{name} must be contiguous")
+    return t.data_ptr()
 
 
 def _elsewhere(t, name: str, device: int) -> None:
@@ -150,9 +168,9 @@ def _no_gradient(name: str):
                        "torch.no_grad()")
 
 
-def _rows(t, name: str, head_dim: int, device: int) -> KvRows:
-    if not isinstance(t, torch.Tensor) or len(shape := t.shape) != 3 or \
-            (dtype := t.dtype) not in (torch.bfloat16, torch.float16):
+def _rows(t, name: str, head_dim: int, device: int):
+    """(kv_rows, the tensor's shape)."""
+    if not isinstance(t, torch.Tensor) or len(shape := t.shape) != 3 or (dtype := _ROW_TYPES.get(t.dtype)) is None:
         raise TypeError(f"{name} must be a [tokens][heads][D] device tensor of bfloat16 or float16")
     if t.requires_grad and torch.is_grad_enabled():
         _no_gradient(name)
@@ -162,7 +180,7 @@ def _rows(t, name: str, head_dim: int, device: int) -> KvRows:
     token, head, column = t.stride()
     if width != head_dim or (column != 1 and t.numel()):
         raise ValueError(f"{name}: rows of {width} elements {column} apart; dense rows of {head_dim} are needed")
-    return KvRows(t.data_ptr(), token, head, heads, _DTYPES[dtype])
+    return _pack_rows(t.data_ptr(), token, head, heads, dtype), shape
 
 
 def _factor(x, name: str) -> float:
@@ -179,23 +197,24 @@ def _int32(x, name: str) -> int:
     return int(x)
 
 
-def _batch(cache: Cache, tables, lens, starts, tokens: int, max_q, max_len) -> KvBatch:
-    device = cache.struct.device
-    B, pages = _ints(tables, "tables", 2, device).shape
+def _batch(block_size: int, device: int, tables, lens, starts, tokens: int, max_q, max_len):
+    """The numbers of kv_batch, in its order."""
+    (B, pages), (stride, _) = _ints(tables, "tables", 2, device)
     if tokens >= 2**31:
         _int32(tokens, "the number of new tokens")
     _ints(lens, "lens", 1, device, B)
     if starts is None:
         if tokens != B:
             raise ValueError(f"{tokens} new tokens for {B} sequences of one each: starts is needed")
-        max_q, starts_at = 1, None
+        max_q, starts_at = 1, 0
     else:
-        starts_at = _ints(starts, "starts", 1, device, B + 1).data_ptr()
+        _ints(starts, "starts", 1, device, B + 1)
+        starts_at = starts.data_ptr()
         max_q = max(1, tokens if max_q is None else min(tokens, int(max_q)))
-    most = min(pages * cache.layout.block_size, 2**31 - 1024)
+    most = min(pages * block_size, 2**31 - 1024)
     if max_len is not None:
         most = min(most, max(int(max_len), -1))
-    return KvBatch(B, max_q, tokens, most, pages, 0, tables.stride(0), tables.data_ptr(), lens.data_ptr(), starts_at)
+    return B, max_q, tokens, most, pages, 0, stride, tables.data_ptr(), lens.data_ptr(), starts_at
 
 
 def _cache_dtype(cache: Cache, dtype, rows) -> int:
@@ -211,13 +230,22 @@ def _call_stream(stream):
     """(the stream's handle, the context in which the call's own tensors are made): they belong to the call's stream,
     which may be another than the current one."""
     if stream is None:
-        return torch.cuda.current_stream(torch.cuda.current_device()).cuda_stream, _HERE
+        return _current_stream(), _HERE
     if not isinstance(stream, torch.cuda.Stream):
         stream = torch.cuda.ExternalStream(int(stream))
     return stream.cuda_stream, torch.cuda.stream(stream)
 
 
 _HERE = contextlib.nullcontext()
+
+
+def _current_stream() -> int:
+    device = torch.cuda.current_device()
+    return torch.cuda.current_stream(device).cuda_stream if _raw_stream is None else _raw_stream(device)
+
+
+# (Torch's own way to the handle, without a Stream around it, where it has one.)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
 def _used(stream, *tensors) -> None:
@@ -229,19 +257,30 @@ def _used(stream, *tensors) -> None:
                 _in_use_on(t, stream)
 
 
-def _page_scales(t, cache: Cache, device: int) -> KvPageScales:
-    if not isinstance(t, torch.Tensor) or t.dtype not in (torch.uint8, torch.float8_e8m0fnu) or t.dim() != 3:
+def _page_scales(t, cache: Cache, device: int):
+    """kv_page_scales: (address, block stride, K to V)."""
+    if not isinstance(t, torch.Tensor) or (t.dtype is not torch.uint8 and t.dtype is not torch.float8_e8m0fnu) or \
+            len(shape := t.shape) != 3:
         raise TypeError("scales must be a [blocks][2][heads] uint8 or float8_e8m0fnu device tensor")
-    _on(t, "scales", device)
-    blocks, two, heads = t.shape
+    if t.get_device() != device:
+        _elsewhere(t, "scales", device)
+    blocks, two, heads = shape
     if two != 2 or heads != cache.layout.num_kv_heads or blocks < cache.struct.num_blocks:
-        raise ValueError(f"scales of {tuple(t.shape)} for a cache of {cache.struct.num_blocks} blocks of "
+        raise ValueError(f"scales of {tuple(shape)} for a cache of {cache.struct.num_blocks} blocks of "
                          f"{cache.layout.num_kv_heads} heads")
     block, kv, head = t.stride()
     if head != 1 and heads > 1:
         raise TypeError("scales must have a dense last dimension")
-    # (Strides over a single block lead nowhere.)
-    return KvPageScales(t.data_ptr(), block if blocks > 1 else max(block, kv + heads), kv)
+    # (A stride over a single block leads nowhere.)
+    return t.data_ptr(), block if blocks > 1 else max(block, kv + heads), kv
+
+
+def _page_list(pages, counts, tokens: int, device: int):
+    """(kv_page_list, its budget)."""
+    (_, heads, budget), (token, head, _) = _ints(pages, "pages", 3, device, tokens)
+    if counts is None:
+        raise ValueError("pages without counts")
+    return _pack_list(pages.data_ptr(), _dense_ints(counts, "counts", 1, device, tokens), token, head, heads, budget), budget
 
 
 def kv_append(cache: Cache, layer: int, k, v, tables, lens, starts=None, *, max_q=None, max_len=None, dtype=None,
@@ -259,20 +298,22 @@ def kv_append(cache: Cache, layer: int, k, v, tables, lens, starts=None, *, max_
             raise TypeError(f"scales of pages for a cache of {dtype}")
         return kv_append_scaled(cache, layer, k, v, tables, lens, scales, starts, max_q=max_q, max_len=max_len,
                                 stream=stream)
-    D = cache.layout.head_dim
+    layout = cache.layout
+    D = layout.head_dim
     device = cache.struct.device
-    kr, vr = _rows(k, "k", D, device), _rows(v, "v", D, device)
-    if k.shape != v.shape:
-        raise ValueError(f"k and v differ in shape: {tuple(k.shape)} and {tuple(v.shape)}")
-    batch = _batch(cache, tables, lens, starts, k.shape[0], max_q, max_len)
+    (kr, shape), (vr, v_shape) = _rows(k, "k", D, device), _rows(v, "v", D, device)
+    if shape != v_shape:
+        raise ValueError(f"k and v differ in shape: {tuple(shape)} and {tuple(v_shape)}")
+    batch = _pack_batch(*_batch(layout.block_size, device, tables, lens, starts, shape[0], max_q, max_len))
     handle, _ = _call_stream(stream)
     if k_scale != 1.0 or v_scale != 1.0:
         k_scale, v_scale = _factor(k_scale, "k_scale"), _factor(v_scale, "v_scale")
     else:
         k_scale = v_scale = 1.0
-    _raise(_lib.kv_append(ctypes.byref(cache.struct), _int32(layer, "layer"), ctypes.byref(batch), ctypes.byref(kr),
-                          ctypes.byref(vr), _cache_dtype(cache, dtype, k), k_scale, v_scale, handle))
-    _used(stream, k, v, tables, lens, starts)
+    _raise(_lib.kv_append(ctypes.byref(cache.struct), _int32(layer, "layer"), batch, kr, vr, _cache_dtype(cache, dtype, k),
+                          k_scale, v_scale, handle))
+    if stream is not None:
+        _used(stream, k, v, tables, lens, starts)
 
 
 def kv_append_scaled(cache: Cache, layer: int, k, v, tables, lens, scales, starts=None, *, max_q=None, max_len=None,
@@ -280,17 +321,18 @@ def kv_append_scaled(cache: Cache, layer: int, k, v, tables, lens, scales, start
     """kv_append into a float8_e4m3fn cache whose pages have ``scales`` (float8_e8m0fnu, or its bytes as uint8,
     [blocks][2][H]: K's and V's of each head): the new rows' pages take the smallest power of two that brings them, and what a
     page already held, to 448 or less."""
-    D = cache.layout.head_dim
+    layout = cache.layout
+    D = layout.head_dim
     device = cache.struct.device
-    kr, vr = _rows(k, "k", D, device), _rows(v, "v", D, device)
-    if k.shape != v.shape:
-        raise ValueError(f"k and v differ in shape: {tuple(k.shape)} and {tuple(v.shape)}")
-    batch = _batch(cache, tables, lens, starts, k.shape[0], max_q, max_len)
-    by = _page_scales(scales, cache, device)
+    (kr, shape), (vr, v_shape) = _rows(k, "k", D, device), _rows(v, "v", D, device)
+    if shape != v_shape:
+        raise ValueError(f"k and v differ in shape: {tuple(shape)} and {tuple(v_shape)}")
+    batch = _pack_batch(*_batch(layout.block_size, device, tables, lens, starts, shape[0], max_q, max_len))
+    by = _pack_scales(*_page_scales(scales, cache, device))
     handle, _ = _call_stream(stream)
-    _raise(_lib.kv_append_scaled(ctypes.byref(cache.struct), _int32(layer, "layer"), ctypes.byref(batch),
-                                 ctypes.byref(kr), ctypes.byref(vr), ctypes.byref(by), handle))
-    _used(stream, k, v, tables, lens, starts, scales)
+    _raise(_lib.kv_append_scaled(ctypes.byref(cache.struct), _int32(layer, "layer"), batch, kr, vr, by, handle))
+    if stream is not None:
+        _used(stream, k, v, tables, lens, starts, scales)
 
 
 def kv_rotate(cache: Cache, layer: int, q, k, v, tables, lens, starts=None, *, freqs=None, positions=None, q_weight=None,
@@ -306,56 +348,59 @@ def kv_rotate(cache: Cache, layer: int, q, k, v, tables, lens, starts=None, *, f
     [tokens]): by default each token's place in its sequence.  ``dtype``, ``k_scale``, ``v_scale`` and ``scales`` are
     kv_append's.  ``out`` (like ``q``) is made if not given, and may be ``q`` itself; rows of no sequence are left as they
     were."""
-    D = cache.layout.head_dim
+    layout = cache.layout
+    D = layout.head_dim
     device = cache.struct.device
-    qr, kr, vr = _rows(q, "q", D, device), _rows(k, "k", D, device), _rows(v, "v", D, device)
-    if k.shape != v.shape or q.shape[0] != k.shape[0]:
-        raise ValueError(f"q, k and v differ in shape: {tuple(q.shape)}, {tuple(k.shape)} and {tuple(v.shape)}")
-    batch = _batch(cache, tables, lens, starts, q.shape[0], max_q, max_len)
+    (qr, q_shape), (kr, shape), (vr, v_shape) = _rows(q, "q", D, device), _rows(k, "k", D, device), _rows(v, "v", D, device)
+    if shape != v_shape or q_shape[0] != shape[0]:
+        raise ValueError(f"q, k and v differ in shape: {tuple(q_shape)}, {tuple(shape)} and {tuple(v_shape)}")
+    tokens = q_shape[0]
+    batch = _pack_batch(*_batch(layout.block_size, device, tables, lens, starts, tokens, max_q, max_len))
     if k_scale != 1.0 or v_scale != 1.0:
         k_scale, v_scale = _factor(k_scale, "k_scale"), _factor(v_scale, "v_scale")
-    options = KvRotateOptions(_cache_dtype(cache, dtype, k), eps=float(eps), weight_offset=float(weight_offset),
-                              interleaved=1 if interleaved else 0, magnitude=_factor(magnitude, "magnitude"),
-                              k_scale=k_scale, v_scale=v_scale)
+    rotary = freqs_at = 0
     if freqs is not None:
         if not isinstance(freqs, torch.Tensor) or freqs.dtype is not torch.float64 or freqs.dim() != 1 or \
                 not freqs.is_contiguous():
             raise TypeError("freqs must be a contiguous 1-dimensional float64 device tensor")
         if freqs.requires_grad and torch.is_grad_enabled():
             _no_gradient("freqs")
-        _on(freqs, "freqs", device)
-        options.rotary_dim, options.freqs = _int32(2 * freqs.shape[0], "twice the number of freqs"), freqs.data_ptr()
-    if positions is not None:
-        if not _ints(positions, "positions", 1, device, q.shape[0]).is_contiguous():
-            raise TypeError("positions must be contiguous")
-        options.positions = positions.data_ptr()
-    for weight, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
-        if weight is None:
-            continue
-        if not isinstance(weight, torch.Tensor) or weight.shape != (D,) or not weight.is_contiguous() or \
-                weight.dtype not in (torch.float32, q.dtype):
-            raise TypeError(f"{name} must be a contiguous [{D}] device tensor of float32 or {q.dtype}")
-        if weight.requires_grad and torch.is_grad_enabled():
-            _no_gradient(name)
-        _on(weight, name, device)
-        setattr(options, name, weight.data_ptr())
-        options.weight_dtype = KV_DTYPE_F32 if weight.dtype is torch.float32 else _DTYPES[weight.dtype]
-    if q_weight is not None and k_weight is not None and q_weight.dtype != k_weight.dtype:
+        if freqs.get_device() != device:
+            _elsewhere(freqs, "freqs", device)
+        rotary, freqs_at = _int32(2 * freqs.shape[0], "twice the number of freqs"), freqs.data_ptr()
+    positions_at = 0 if positions is None else _dense_ints(positions, "positions", 1, device, tokens)
+    q_weight_at = 0 if q_weight is None else _norm_weight(q_weight, "q_weight", D, q.dtype, device)
+    k_weight_at = 0 if k_weight is None else _norm_weight(k_weight, "k_weight", D, q.dtype, device)
+    weight = q_weight if k_weight is None else k_weight
+    if q_weight is not None and weight.dtype is not q_weight.dtype:
         raise TypeError("q_weight and k_weight have different types")
-    if scales is not None:
-        by = _page_scales(scales, cache, device)
-        options.scales = ctypes.pointer(by)
-    if out is not None and (out.dtype != q.dtype or out.shape != q.shape):
-        raise TypeError("out must have the type and shape of q")
+    weight_dtype = 0 if weight is None else KV_DTYPE_F32 if weight.dtype is torch.float32 else _DTYPES[weight.dtype]
+    by = None if scales is None else KvPageScales(*_page_scales(scales, cache, device))
+    options = _pack_rotate(_cache_dtype(cache, dtype, k), rotary, 1 if interleaved else 0, weight_dtype, freqs_at,
+                           positions_at, q_weight_at, k_weight_at, eps, weight_offset, _factor(magnitude, "magnitude"),
+                           k_scale, v_scale, 0, 0 if by is None else ctypes.addressof(by))
     handle, here = _call_stream(stream)
     if out is None:
         with here:
-            out = q.new_empty(q.shape)
-    outr = _rows(out, "out", D, device)
-    _raise(_lib.kv_rotate(ctypes.byref(cache.struct), _int32(layer, "layer"), ctypes.byref(batch), ctypes.byref(options),
-                          ctypes.byref(qr), ctypes.byref(outr), ctypes.byref(kr), ctypes.byref(vr), handle))
-    _used(stream, q, k, v, tables, lens, starts, freqs, positions, q_weight, k_weight, scales, out)
+            out = q.new_empty(q_shape)
+    elif not isinstance(out, torch.Tensor) or out.dtype != q.dtype or out.shape != q_shape:
+        raise TypeError("out must have the type and shape of q")
+    _raise(_lib.kv_rotate(ctypes.byref(cache.struct), _int32(layer, "layer"), batch, options, qr,
+                          _rows(out, "out", D, device)[0], kr, vr, handle))
+    if stream is not None:
+        _used(stream, q, k, v, tables, lens, starts, freqs, positions, q_weight, k_weight, scales, out)
     return out
+
+
+def _norm_weight(t, name: str, head_dim: int, rows_dtype, device: int) -> int:
+    if not isinstance(t, torch.Tensor) or t.shape != (head_dim,) or not t.is_contiguous() or \
+            (t.dtype is not torch.float32 and t.dtype is not rows_dtype):
+        raise TypeError(f"{name} must be a contiguous [{head_dim}] device tensor of float32 or {rows_dtype}")
+    if t.requires_grad and torch.is_grad_enabled():
+        _no_gradient(name)
+    if t.get_device() != device:
+        _elsewhere(t, name, device)
+    return t.data_ptr()
 
 
 def kv_attend(cache: Cache, layer: int, q, tables, lens, starts=None, *, max_q=None, max_len=None, dtype=None,
@@ -378,56 +423,57 @@ def kv_attend(cache: Cache, layer: int, q, tables, lens, starts=None, *, max_q=N
     goes with ``weights``.
     """
     device = cache.struct.device
-    qr = _rows(q, "q", cache.layout.head_dim, device)
-    batch = _batch(cache, tables, lens, starts, q.shape[0], max_q, max_len)
+    layout = cache.layout
+    qr, q_shape = _rows(q, "q", layout.head_dim, device)
+    tokens, q_heads, _ = q_shape
+    B, max_q, _, most, *table = _batch(layout.block_size, device, tables, lens, starts, tokens, max_q, max_len)
     if k_scale != 1.0 or v_scale != 1.0:
         k_scale, v_scale = _factor(k_scale, "k_scale"), _factor(v_scale, "v_scale")
     else:
         k_scale = v_scale = 1.0
-    options = KvAttendOptions(_cache_dtype(cache, dtype, q), _int32(window, "window") if window else 0,
-                              0.0 if scale is None else _factor(scale, "scale"),
-                              _factor(softcap, "softcap") if softcap else 0.0, k_scale, v_scale)
-    if full_weights:
-        options.full_weights = 1
+    slopes_at = prior_at = weights_at = weights_seq = weights_head = 0
     if slopes is not None:
-        _floats(slopes, "slopes", device, (q.shape[1],))
-        options.slopes = slopes.data_ptr()
+        _floats(slopes, "slopes", device, (q_heads,))
+        slopes_at = slopes.data_ptr()
     if weights is not None:
-        _weights(weights, "weights", device, (tables.shape[0], cache.layout.num_kv_heads))
+        _weights(weights, "weights", device, (B, layout.num_kv_heads))
         if max_len is None:
-            batch.max_len = min(batch.max_len, weights.shape[2])
-        elif weights.shape[2] < batch.max_len:
-            raise ValueError(f"weights of {weights.shape[2]} tokens for sequences of up to {batch.max_len}")
-        options.weights_out = weights.data_ptr()
-        options.weights_seq_stride, options.weights_head_stride = weights.stride(0), weights.stride(1)
+            most = min(most, weights.shape[2])
+        elif weights.shape[2] < most:
+            raise ValueError(f"weights of {weights.shape[2]} tokens for sequences of up to {most}")
+        weights_at, weights_seq, weights_head = weights.data_ptr(), weights.stride(0), weights.stride(1)
         if prior is not None:
             _weights(prior, "prior", device)
             if prior.shape != weights.shape or prior.stride() != weights.stride():
                 raise TypeError("prior must have the shape and strides of weights")
-            options.weights_in = prior.data_ptr()
+            prior_at = prior.data_ptr()
     elif prior is not None:
         raise ValueError("prior without weights")
+    window = _int32(window, "window") if window else 0
+    options = KvAttendOptions(_cache_dtype(cache, dtype, q), window, 0.0 if scale is None else _factor(scale, "scale"),
+                              _factor(softcap, "softcap") if softcap else 0.0, k_scale, v_scale, slopes_at, prior_at,
+                              weights_at, weights_seq, weights_head, 1 if full_weights else 0)
+    batch = KvBatch(B, max_q, tokens, most, *table)
     by = chosen = None
+    budget = -1
     if scales is not None:
-        by = ctypes.byref(_page_scales(scales, cache, device))
+        by = _pack_scales(*_page_scales(scales, cache, device))
     if pages is not None:
-        chosen = ctypes.byref(_page_list(pages, counts, cache, q.shape[0], device))
+        chosen, budget = _page_list(pages, counts, tokens, device)
     elif counts is not None:
         raise ValueError("counts without pages")
-    heads = (q.shape[0], q.shape[1])
-    if out is not None and (out is q or out.dtype != q.dtype or out.shape != q.shape):
+    if out is not None and (out is q or out.dtype != q.dtype or out.shape != q_shape):
         raise TypeError("out must have the type and shape of q, and be another tensor")
+    heads = (tokens, q_heads)
     if lse is not None:
         _floats(lse, "lse", device, heads)
-    layout = cache.layout
-    key = (layout.num_kv_heads, layout.head_dim, layout.elem_bytes, layout.block_size, batch.num_seqs, batch.max_queries,
-           batch.num_queries, batch.max_len, options.window, weights is None, q.shape[1],
-           -1 if pages is None else pages.shape[2])
+    key = (layout.num_kv_heads, layout.head_dim, layout.elem_bytes, layout.block_size, B, max_q, tokens, most, window,
+           weights is None, q_heads, budget)
     need = _attend_bytes.get(key)
+    at, batch, options = ctypes.byref(cache.struct), ctypes.byref(batch), ctypes.byref(options)
     if need is None:
-        args = (ctypes.byref(cache.struct), ctypes.byref(batch), ctypes.byref(options))
-        need = _lib.kv_attend_workspace(*args, ctypes.byref(qr)) if by is None and chosen is None else \
-            _lib.kv_attend_pages_workspace(*args, by, chosen, ctypes.byref(qr))
+        need = _lib.kv_attend_workspace(at, batch, options, qr) if by is None and chosen is None else \
+            _lib.kv_attend_pages_workspace(at, batch, options, by, chosen, qr)
         if need < 0:
             _raise(need)
         if len(_attend_bytes) >= 4096:
@@ -436,19 +482,23 @@ def kv_attend(cache: Cache, layer: int, q, tables, lens, starts=None, *, max_q=N
     handle, here = _call_stream(stream)
     with here:
         if out is None:
-            out = q.new_empty(q.shape)
+            out = q.new_empty(q_shape)
         if lse is None:
-            lse = torch.empty(heads, dtype=torch.float32, device=q.device)
-        workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
-    outr = _rows(out, "out", layout.head_dim, device)
-    args = (ctypes.byref(cache.struct), _int32(layer, "layer"), ctypes.byref(batch), ctypes.byref(options))
-    more = (ctypes.byref(qr), ctypes.byref(outr), lse.data_ptr(), workspace.data_ptr() if need else None, need, handle)
+            lse = q.new_empty(heads, dtype=torch.float32)
+        workspace = q.new_empty(need, dtype=torch.uint8).data_ptr() if need else None
+    outr, _ = _rows(out, "out", layout.head_dim, device)
+    layer = _int32(layer, "layer")
     if by is None and chosen is None:
-        _raise(_lib.kv_attend(*args, *more))
+        _raise(_lib.kv_attend(at, layer, batch, options, qr, outr, lse.data_ptr(), workspace, need, handle))
     else:
-        _raise(_lib.kv_attend_pages(*args, by, chosen, *more))
-    _used(stream, q, tables, lens, starts, slopes, weights, prior, out, lse, scales, pages, counts)
+        _raise(_lib.kv_attend_pages(at, layer, batch, options, by, chosen, qr, outr, lse.data_ptr(), workspace, need,
+                                    handle))
+    if stream is not None:
+        _used(stream, q, tables, lens, starts, slopes, weights, prior, out, lse, scales, pages, counts)
     return out, lse
+
+
+_attend_bytes = {}  # workspaces' bytes by the numbers that they depend on
 
 
 def kv_attend_pages(cache: Cache, layer: int, q, tables, lens, starts=None, *, scales=None, pages=None, counts=None,
@@ -457,19 +507,6 @@ def kv_attend_pages(cache: Cache, layer: int, q, tables, lens, starts=None, *, s
     if scales is None and pages is None:
         raise ValueError("neither scales nor pages")
     return kv_attend(cache, layer, q, tables, lens, starts, scales=scales, pages=pages, counts=counts, **options)
-
-
-def _page_list(pages, counts, cache: Cache, tokens: int, device: int) -> KvPageList:
-    _ints(pages, "pages", 3, device, tokens)
-    if counts is None:
-        raise ValueError("pages without counts")
-    if not _ints(counts, "counts", 1, device, tokens).is_contiguous():
-        raise TypeError("counts must be contiguous")
-    _, heads, budget = pages.shape
-    return KvPageList(pages.data_ptr(), counts.data_ptr(), pages.stride(0), pages.stride(1), heads, budget)
-
-
-_attend_bytes = {}  # kv_attend_workspace by the numbers that it depends on
 
 
 def kv_bounds(cache: Cache, layer: int, bounds: Cache, tables, lens, starts=None, *, max_q=None, max_len=None, dtype=None,
@@ -481,22 +518,23 @@ def kv_bounds(cache: Cache, layer: int, bounds: Cache, tables, lens, starts=None
 
     ``dtype``: the cache's, which 2-byte elements alone do not say."""
     device = cache.struct.device
+    layout = cache.layout
     if starts is None:
-        rows, starts_at = tables.shape[0] if isinstance(tables, torch.Tensor) and tables.dim() else 0, None
+        tokens = tables.shape[0] if isinstance(tables, torch.Tensor) and tables.dim() else 0
     else:
         # (How many rows there are only the device knows: as many as sequences may have tokens.)
-        rows, starts_at = 2**31 - 1, starts
-        if max_q is None:
-            max_q = 2**31 - 1
-    batch = _batch(cache, tables, lens, starts_at, rows, max_q, max_len)
+        tokens = 2**31 - 1
+        max_q = tokens if max_q is None else max_q
+    batch = _pack_batch(*_batch(layout.block_size, device, tables, lens, starts, tokens, max_q, max_len))
     if dtype is None:
-        if cache.layout.elem_bytes != 1:
+        if layout.elem_bytes != 1:
             raise TypeError("dtype is needed: bfloat16 or float16")
         dtype = torch.float8_e4m3fn
     handle, _ = _call_stream(stream)
-    _raise(_lib.kv_bounds(ctypes.byref(cache.struct), _int32(layer, "layer"), ctypes.byref(batch),
-                          _cache_dtype(cache, dtype, None), ctypes.byref(bounds.struct), handle))
-    _used(stream, tables, lens, starts)
+    _raise(_lib.kv_bounds(ctypes.byref(cache.struct), _int32(layer, "layer"), batch, _cache_dtype(cache, dtype, None),
+                          ctypes.byref(bounds.struct), handle))
+    if stream is not None:
+        _used(stream, tables, lens, starts)
 
 
 def kv_score(bounds: Cache, layer: int, q, tables, lens, starts=None, *, block_size: int, max_q=None, max_len=None,
@@ -509,33 +547,31 @@ def kv_score(bounds: Cache, layer: int, q, tables, lens, starts=None, *, block_s
     weights and lens.  ``out`` and ``counts`` are made if not given; scores of pages beyond ``counts``, and rows of no
     sequence, are left as they were (in made ones, scores hold anything and counts 0)."""
     device = bounds.struct.device
-    qr = _rows(q, "q", bounds.layout.head_dim, device)
+    layout = bounds.layout
+    qr, (tokens, _, _) = _rows(q, "q", layout.head_dim, device)
     block_size = _int32(block_size, "block_size")
-    batch = _batch(bounds, tables, lens, starts, q.shape[0], max_q, None)
-    most = min(tables.shape[1] * block_size, 2**31 - 1024)
-    batch.max_len = most if max_len is None else min(most, max(int(max_len), -1))
-    heads = bounds.layout.num_kv_heads
-    pages = -(-max(batch.max_len, 0) // block_size) if block_size > 0 else 0
+    if block_size < 1:
+        raise ValueError(f"block_size must be positive (got {block_size})")
+    batch = _batch(block_size, device, tables, lens, starts, tokens, max_q, max_len)
+    heads = layout.num_kv_heads
+    pages = -(-max(batch[3], 0) // block_size)
     handle, here = _call_stream(stream)
     with here:
         if out is None:
-            out = torch.empty((q.shape[0], heads, pages), dtype=torch.float32, device=q.device)
+            out = q.new_empty((tokens, heads, pages), dtype=torch.float32)
         if counts is None:
-            counts = torch.empty(q.shape[0], dtype=torch.int32, device=q.device) if starts is None else \
-                torch.zeros(q.shape[0], dtype=torch.int32, device=q.device)
-    _weights(out, "out", device, (q.shape[0], heads))
+            counts = (q.new_empty if starts is None else q.new_zeros)(tokens, dtype=torch.int32)
+    _weights(out, "out", device, (tokens, heads))
     if out.shape[2] < pages:
         raise ValueError(f"out of {out.shape[2]} pages for sequences of up to {pages}")
-    if not _ints(counts, "counts", 1, device, q.shape[0]).is_contiguous():
-        raise TypeError("counts must be contiguous")
-    options = KvScoreOptions(_cache_dtype(bounds, dtype, q), block_size, _factor(scale, "scale"))
-    options.token_stride, options.head_stride = out.stride(0), out.stride(1)
-    if scales is not None:
-        by = _page_scales(scales, bounds, device)
-        options.scales = ctypes.pointer(by)
-    _raise(_lib.kv_score(ctypes.byref(bounds.struct), _int32(layer, "layer"), ctypes.byref(batch), ctypes.byref(options),
-                         ctypes.byref(qr), out.data_ptr(), counts.data_ptr(), handle))
-    _used(stream, q, tables, lens, starts, scales, out, counts)
+    token, head, _ = out.stride()
+    by = None if scales is None else KvPageScales(*_page_scales(scales, bounds, device))
+    options = _pack_score(_cache_dtype(bounds, dtype, q), block_size, _factor(scale, "scale"), 0,
+                          0 if by is None else ctypes.addressof(by), token, head)
+    _raise(_lib.kv_score(ctypes.byref(bounds.struct), _int32(layer, "layer"), _pack_batch(*batch), options, qr,
+                         out.data_ptr(), _dense_ints(counts, "counts", 1, device, tokens), handle))
+    if stream is not None:
+        _used(stream, q, tables, lens, starts, scales, out, counts)
     return out, counts
 
 
@@ -574,9 +610,8 @@ def kv_compact(cache: Cache, layer: int, tables, keep, kept_lens, dst_tables, *,
     token j (``keep`` int32 [B][H or 1][budget], contiguous; ``kept_lens`` int32 [B] of them count).  The destination's
     pages are distinct and none of the sources'.  ``window`` and ``slopes`` of later calls count in the new places."""
     device = cache.struct.device
-    B = _ints(tables, "tables", 2, device).shape[0]
-    if not _ints(keep, "keep", 3, device, B).is_contiguous():
-        raise TypeError("keep must be contiguous")
+    B = _ints(tables, "tables", 2, device)[0][0]
+    _dense_ints(keep, "keep", 3, device, B)
     _ints(kept_lens, "kept_lens", 1, device, B)
     _ints(dst_tables, "dst_tables", 2, device, B)
     handle, _ = _call_stream(stream)

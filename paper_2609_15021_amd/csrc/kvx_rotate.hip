@@ -1,11 +1,11 @@
 // kv_rotate: the new tokens' queries and keys normed for each head and rotated by their position, in one pass; keys and
 // values go straight into the cache's pages.
 //
-// Everything is read once and written once.  A workgroup takes a few tokens of a sequence and goes over their rows (query
-// heads, then the heads of K, then of V), 8 columns a lane, so that a row's norm is a few lane shuffles.  The angles are
-// the same for all heads: the workgroup works out its tokens' cosines and sines once, in LDS, while its first rows are on
-// their way, and looks their pages up.  Where a column's partner is half a row away the lane loads the partners too
-// (they come from the cache of the CU).
+// Everything is read once and written once.  A lane has 8 columns of a row, so a row's norm is a few lane shuffles, and so
+// are the partners that lie half a row away.  A group of lanes takes kAtOnce rows (query heads, then heads of K, then of V)
+// of one token, all of them on their way at once; as many groups as a token needs share it, and a workgroup has as many
+// tokens as that leaves room for.  Angles are the same for all heads: the workgroup works out its tokens' cosines and
+// sines once, in LDS, and looks their pages up, while the rows are on their way.
 #include <algorithm>
 #include <cmath>
 
@@ -15,25 +15,29 @@ namespace kvx {
 
 namespace {
 
-constexpr int kTokens = 4;  // most tokens of a workgroup
+constexpr int kAtOnce = 2;
+constexpr int kAngles = 1024;  // of a workgroup
 
 struct RotateArgs {
     Pages pages;
     Batch batch;
     Rows q, out, k, v;
-    Turn turn[2];  // of q, k
+    Turn turn[2];              // of q, k
     int32_t heads, rows_each;  // query heads; rows of a token
-    int32_t tokens, splits;    // tokens of a workgroup, and workgroups that share their rows
-    Divisor by_rows, by_splits, by_half;
+    int32_t each_shift;        // 2^each_shift groups of lanes share a token
+    int32_t tokens;            // of a workgroup
+    int32_t splits;            // workgroups that share their rows
+    Divisor by_splits, by_half;
     float k_scale, v_scale;
 };
 
 // QUANT: the cache holds e4m3.
 template <int DTYPE, int LPR, Pairs PAIRS, bool QUANT>
 __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateArgs a) {
-    constexpr int kSlots = kThreads / LPR;  // rows at once
-    __shared__ float cosines[kTokens][128], sines[kTokens][128];
-    __shared__ int64_t places[kTokens];     // of the tokens' slots in the cache, or -1
+    constexpr int kGroups = kThreads / LPR;         // of lanes: rows at once
+    __shared__ float cosines[kAngles], sines[kAngles];  // [token][pair]
+    __shared__ __align__(16) float weights[2][LPR * 8];  // of q's and K's norms
+    __shared__ int64_t places[kGroups];             // of the tokens' slots in the cache, or -1
     const Pages &p = a.pages;
     const int b = blockIdx.y, tid = threadIdx.x;
     Sequence s;
@@ -43,34 +47,49 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateArgs a) {
     const int i0 = tile * a.tokens, tokens = min(a.tokens, s.nq - i0);
     if (tokens <= 0)
         return;
-    const int rows = tokens * a.rows_each, step = a.splits * kSlots;
     typedef Turner<DTYPE, PAIRS, LPR> Lane;
     const Lane lane(a.turn[0], tid % LPR, p.D);
+    const int each = 1 << a.each_shift, token_step = kGroups >> a.each_shift;
+    const int step = each * a.splits, r0 = split * each + (tid / LPR & (each - 1));
 
-    struct Where {
-        int token, head;  // head: of q, then of K, then of V
-        const uint8_t *from;
+    // What a group has at once: rows r, r + step, ... of a token (of the workgroup's).  A group without any goes along
+    // with the last token's last row: lanes of a wave stay together.
+    struct At {
+        int token, r;
     };
-    const auto where = [&](int r) {
-        Where w;
-        w.token = divide(r, a.by_rows);
-        w.head = r - w.token * a.rows_each;
-        const int of_k = w.head - a.heads, of_v = of_k - p.H;
+    const auto after = [&](At at) {
+        at.r += kAtOnce * step;
+        return at.r < a.rows_each ? at : At{at.token + token_step, r0};
+    };
+    // Row r of the token: of q, of K or of V.
+    const auto from = [&](int row, int r) {
+        const int of_k = r - a.heads, of_v = of_k - p.H;
         const Rows &src = of_k < 0 ? a.q : of_v < 0 ? a.k : a.v;
-        w.from = src.data + int64_t{s.q0 + i0 + w.token} * src.token_stride +
-                 int64_t{of_k < 0 ? w.head : of_v < 0 ? of_k : of_v} * src.head_stride;
-        return w;
+        return src.data + int64_t{row} * src.token_stride + int64_t{of_k < 0 ? r : of_v < 0 ? of_k : of_v} * src.head_stride;
     };
-    // (Rows beyond the last are loaded as the last: all lanes of a row stay together, and a wave's lanes mostly do.)
-    int r = split * kSlots + tid / LPR;
-    Where next = where(min(r, rows - 1));
-    typename Lane::Vec next_vec = lane.load(a.turn[0], next.from);
-    const typename Lane::Weights q_weights = lane.weights(a.turn[0]), k_weights = lane.weights(a.turn[1]);
-    const int first = s.n - s.nq + i0;
-    for (int u = tid; u < tokens * a.turn[0].half; u += kThreads) {
-        const int token = divide(u, a.by_half), i = u - token * a.turn[0].half;
-        const int position = a.turn[0].positions ? a.turn[0].positions[s.q0 + i0 + token] : first + token;
-        turn_by(position, a.turn[0].freqs[i], a.turn[0].magnitude, cosines[token][i], sines[token][i]);
+    struct Vecs {
+        typename Lane::Vec of[kAtOnce];
+    };
+    const auto load = [&](const At &at) {
+        Vecs v;
+        const int row = s.q0 + i0 + min(at.token, tokens - 1);
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k)
+            v.of[k] = lane.load(a.turn[0], from(row, min(at.r + k * step, a.rows_each - 1)));
+        return v;
+    };
+    At at{tid / LPR >> a.each_shift, r0};
+    Vecs next = load(at);
+    for (int u = tid; u < 2 * LPR * 8; u += kThreads) {
+        const Turn &turn = u < LPR * 8 ? a.turn[0] : a.turn[1];
+        const int d = u & (LPR * 8 - 1);
+        weights[u / (LPR * 8)][d] = turn.weight && d < p.D ? norm_weight<DTYPE>(turn, d) : 1.f;
+    }
+    const int first = s.n - s.nq + i0, half = a.turn[0].half;
+    for (int u = tid; u < tokens * half; u += kThreads) {
+        const int t = divide(u, a.by_half), i = u - t * half;
+        const int position = a.turn[0].positions ? a.turn[0].positions[s.q0 + i0 + t] : first + t;
+        turn_by(position, a.turn[0].freqs[i], a.turn[0].magnitude, cosines[u], sines[u]);
     }
     if (tid < tokens && a.rows_each > a.heads) {
         const int t = first + tid, page = divide(max(t, 0), p.by_bs);
@@ -83,56 +102,55 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateArgs a) {
         places[tid] = place;
     }
     __syncthreads();
-    for (; r < rows; r += step) {
-        const Where at = next;
-        const typename Lane::Vec vec = next_vec;
-        if (r + step < rows) {
-            next = where(r + step);
-            next_vec = lane.load(a.turn[0], next.from);
-        }
-        const int of_k = at.head - a.heads, of_v = of_k - p.H;
-        float y[8];
-        if (of_v < 0) {
-            // (q's and K's norms differ by their weights alone, which may be missing for one of them.)
-            const bool is_q = of_k < 0;
-            Turn turn = a.turn[0];
-            turn.weight = is_q ? a.turn[0].weight : a.turn[1].weight;
-            typename Lane::Weights w;
+    while (at.token < tokens) {
+        const Vecs vecs = next;
+        const At now = at;
+        at = after(at);
+        if (at.token < tokens)
+            next = load(at);
+        const int row = s.q0 + i0 + now.token;
+        const typename Lane::Angles angles = lane.angles(a.turn[0], [&](int i, float &c, float &si) {
+            c = cosines[now.token * half + i];
+            si = sines[now.token * half + i];
+        });
+        // (V's rows are worked out with the others, without a use, so that no row's work waits for another's.)
+        float y[kAtOnce][8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                w.own[j] = is_q ? q_weights.own[j] : k_weights.own[j];
-                w.other[j] = is_q ? q_weights.other[j] : k_weights.other[j];
-            }
-            lane.finish(turn, vec, w,
-                        [&](int j, float &c, float &si) {
-                            const int i = lane.pair(turn, j);
-                            c = cosines[at.token][i];
-                            si = sines[at.token][i];
-                        },
-                        y);
-        } else {
-            to_floats<DTYPE>(vec.own, y);
+        for (int k = 0; k < kAtOnce; ++k) {
+            const bool is_q = now.r + k * step < a.heads;
+            const float *of = weights[is_q ? 0 : 1];
+            lane.finish(a.turn[0], vecs.of[k], (is_q ? a.turn[0].weight : a.turn[1].weight) != nullptr,
+                        lane.weights(a.turn[0], [&](int d) { return of[d]; }), angles, y[k]);
         }
         if (!lane.any)
             continue;
-        if (of_k < 0) {
-            uint8_t *to = a.out.data + int64_t{s.q0 + i0 + at.token} * a.out.token_stride + at.head * a.out.head_stride;
-            *reinterpret_cast<vec16 *>(to + 2 * lane.d0) = from_floats<DTYPE>(y);
-            continue;
-        }
-        if (places[at.token] < 0)
-            continue;
-        uint8_t *to = p.base + places[at.token] + (of_v < 0 ? 0u : p.v_bytes) +
-                      static_cast<uint32_t>(of_v < 0 ? of_k : of_v) * p.head_bytes;
-        if constexpr (QUANT) {
-            const float scale = of_v < 0 ? a.k_scale : a.v_scale;
+        const int64_t place = places[now.token];
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                y[j] /= scale;
-            *reinterpret_cast<vec8 *>(to + lane.d0) = to_e4m3(y);
-        } else {
-            // (V's bytes as they are.)
-            *reinterpret_cast<vec16 *>(to + 2 * lane.d0) = of_v < 0 ? from_floats<DTYPE>(y) : vec.own;
+        for (int k = 0; k < kAtOnce; ++k) {
+            const int r = now.r + k * step, of_k = r - a.heads, of_v = of_k - p.H;
+            if (r >= a.rows_each)
+                break;
+            if (of_k < 0) {
+                uint8_t *to = a.out.data + int64_t{row} * a.out.token_stride + r * a.out.head_stride;
+                *reinterpret_cast<vec16 *>(to + 2 * lane.d0) = from_floats<DTYPE>(y[k]);
+                continue;
+            }
+            if (place < 0)
+                continue;
+            uint8_t *to = p.base + place + (of_v < 0 ? 0u : p.v_bytes) +
+                          static_cast<uint32_t>(of_v < 0 ? of_k : of_v) * p.head_bytes;
+            if constexpr (QUANT) {
+                if (of_v >= 0)
+                    to_floats<DTYPE>(vecs.of[k].own, y[k]);
+                const float scale = of_v < 0 ? a.k_scale : a.v_scale;
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    y[k][j] /= scale;
+                *reinterpret_cast<vec8 *>(to + lane.d0) = to_e4m3(y[k]);
+            } else {
+                // (V's bytes as they are.)
+                *reinterpret_cast<vec16 *>(to + 2 * lane.d0) = of_v < 0 ? from_floats<DTYPE>(y[k]) : vecs.of[k].own;
+            }
         }
     }
 }
@@ -234,16 +252,25 @@ kv_status rotate(const kv_cache *cache, int32_t layer, const kv_batch *batch, co
     a.k_scale = o->k_scale == 0.f ? 1.f : o->k_scale;
     a.v_scale = o->v_scale == 0.f ? 1.f : o->v_scale;
     const Pairs pairs = o->interleaved ? kNeighbours : t.half % 8 == 0 ? kHalves : kAnyHalves;
-    // A few tokens share a workgroup; while that leaves CUs idle a token has its own, and while that does, several.
-    const int64_t slots = kThreads / lanes_of(a.pages.D), most = std::min(batch->max_queries, batch->num_queries);
-    const int64_t each = (a.rows_each + slots - 1) / slots;
-    a.tokens = int64_t{batch->num_queries} > 1024 ? kTokens : 1;
-    a.splits = static_cast<int32_t>(int64_t{batch->num_queries} * each > 4096 ? 1 : each);
-    const int64_t groups = (most + a.tokens - 1) / a.tokens * a.splits;
+    // A token has as many groups of lanes as have kAtOnce rows each (or a group for each row, while that leaves CUs idle),
+    // and a workgroup as many tokens as its groups then have at once, or more of them one after the other where all
+    // workgroups would not run at once: what a workgroup does before its first row is then done once for them.
+    const int64_t most = std::min(batch->max_queries, batch->num_queries), groups_each = kThreads / lanes_of(a.pages.D);
+    const int64_t wanted = int64_t{batch->num_queries} * a.rows_each > 16384 ? (a.rows_each + kAtOnce - 1) / kAtOnce
+                                                                             : a.rows_each;
+    while ((int64_t{1} << a.each_shift) < std::min(wanted, groups_each))
+        ++a.each_shift;
+    const int64_t side = groups_each >> a.each_shift;  // tokens side by side
+    a.splits = wanted <= groups_each || int64_t{batch->num_queries} * a.rows_each > 16384
+                   ? 1
+                   : static_cast<int32_t>((wanted + groups_each - 1) / groups_each);
+    const int64_t behind = std::max<int64_t>(batch->num_queries / (side * 1024), 1);
+    const int64_t held = std::min<int64_t>(kAngles / std::max(t.half, 1), groups_each);
+    a.tokens = static_cast<int32_t>(std::max<int64_t>(std::min(side * behind, held), 1));
+    const int64_t groups = ((most - 1) / a.tokens + 1) * a.splits;
     if (groups > INT32_MAX / kThreads)
         return fail(KV_EUNSUPPORTED, "%lld new tokens of a sequence in one call are too many",
                     static_cast<long long>(most));
-    a.by_rows = divisor(a.rows_each);
     a.by_splits = divisor(a.splits);
     a.by_half = divisor(std::max(t.half, 1));
     const dim3 grid(static_cast<uint32_t>(groups), static_cast<uint32_t>(batch->num_seqs));

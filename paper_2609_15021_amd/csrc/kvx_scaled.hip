@@ -58,23 +58,21 @@ __global__ __launch_bounds__(64 * WAVES) void append_scaled_kernel(const ScaledA
     const bool turn = PAIRS != kAsIs && kv == 0;
     typename Turner<DTYPE, PAIRS, LPR>::Weights weights;
     if (turn)
-        weights = turner.weights(a.turn);
+        weights = turner.weights(a.turn, [&](int d) { return a.turn.weight ? norm_weight<DTYPE>(a.turn, d) : 1.f; });
     const int slot = tid / LPR, d0 = turner.d0;
     const Rows &src = a.rows[kv];
     const uint8_t *from = src.data + (int64_t{s.q0} + (t0 - first)) * src.token_stride + h * src.head_stride;
     const auto load = [&](int row) {
         const uint8_t *x = from + row * src.token_stride;
-        return turn ? turner.load(a.turn, x)
-                    : typename Turner<DTYPE, PAIRS, LPR>::Vec{as_is.load(a.turn, x).own, vec16{0, 0, 0, 0}};
+        return turn ? turner.load(a.turn, x) : typename Turner<DTYPE, PAIRS, LPR>::Vec{as_is.load(a.turn, x).own, {}};
     };
     const auto finish = [&](const typename Turner<DTYPE, PAIRS, LPR>::Vec &v, int row, float *y) {
         if (turn) {
             const int position = a.turn.positions ? a.turn.positions[s.q0 + t0 - first + row] : t0 + row;
-            turner.finish(a.turn, v, weights,
-                          [&](int j, float &c, float &si) {
-                              turn_by(position, a.turn.freqs[turner.pair(a.turn, j)], a.turn.magnitude, c, si);
-                          },
-                          y);
+            const auto angles = turner.angles(a.turn, [&](int i, float &c, float &si) {
+                turn_by(position, a.turn.freqs[i], a.turn.magnitude, c, si);
+            });
+            turner.finish(a.turn, v, a.turn.weight != nullptr, weights, angles, y);
         } else {
             to_floats<DTYPE>(v.own, y);
         }

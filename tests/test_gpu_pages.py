@@ -155,6 +155,23 @@ def test_rotate_many(lens, new, fp8):
     run_rotate(c, magnitude=1.25, offset=1.0, weight_dtype=BF16)
 
 
+@pytest.mark.parametrize("rotary", [20, 32])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_rotate_keeps_infinities_in_place(rotary, interleaved):
+    """Without a norm an infinity or NaN reaches its own column and its partner's, and no other."""
+    c = ref.Case(1, 1, 64, 16, [9], [1], seed=1)
+    cache, _, _, _, _, tables, lens, _ = c.device()
+    freqs = torch.full((rotary // 2,), 0.1, dtype=torch.float64, device=DEV)
+    for column in (0, 7, rotary - 1, rotary, rotary + 1, 63):
+        q = torch.ones(1, 1, 64, dtype=BF16, device=DEV)
+        q[0, 0, column] = float("inf") if column % 2 else float("nan")
+        half = rotary // 2
+        partner = column ^ 1 if interleaved else column + half if column < half else column - half
+        hit = {column, partner} if column < rotary else {column}
+        got = attend.kv_rotate(cache, 0, q, q, q, tables, lens, freqs=freqs, interleaved=interleaved)
+        assert set((~torch.isfinite(got[0, 0])).nonzero().view(-1).tolist()) == hit
+
+
 @pytest.mark.parametrize("in_place", [False, True])
 def test_rotate_far_positions(in_place):
     """Positions of their own, up to the largest."""

@@ -230,5 +230,5 @@ def test_binding_refusals():
             attend._page_scales(torch.zeros(shape, dtype=torch.uint8), Fake, -1)
     with pytest.raises(TypeError):
         attend._page_scales(torch.zeros(64, 2, 4, dtype=torch.uint8)[..., ::2], Fake, -1)
-    got = attend._page_scales(torch.zeros(64, 2, 16, dtype=torch.float8_e8m0fnu)[..., :2], Fake, -1)
-    assert (got.block_stride, got.kv_stride) == (32, 16)
+    _, block, kv = attend._page_scales(torch.zeros(64, 2, 16, dtype=torch.float8_e8m0fnu)[..., :2], Fake, -1)
+    assert (block, kv) == (32, 16)
