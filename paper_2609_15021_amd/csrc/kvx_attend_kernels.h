@@ -38,6 +38,7 @@ struct AttendArgs {
 // join.
 struct Parts {
     int32_t len, splits;  // tokens of a part; most parts of a row
+    int32_t ranked;       // 1: tiles in the order of their last tokens over all sequences (at most 64)
     float *sums;          // [row][query head][splits][D], unscaled
     float *stats;         // [row][query head][splits][2]: largest score and sum, in powers of 2
 };
@@ -186,6 +187,53 @@ __device__ __forceinline__ bool share_of(const AttendArgs &a, const Shares &shar
     s.split = by_seq ? 0 : item - s.item0;
     s.len = static_cast<int>(len);
     return s.parts > 0;
+}
+
+// The tail kernel's tile of which `rank` others end behind it (or as far, in an order of their own), whatever sequences they
+// are of: the longest begin first.  False if there are no more.  A lane has a sequence, whose tiles' ends rise; of the ends
+// that may be, 64 are tried at once, a lane each, until one is left.
+__device__ __forceinline__ bool tile_of_rank(const AttendArgs &a, int rank, int &b, int &tile) {
+    const int lane = threadIdx.x & 63;
+    int past = 0, nq = 0, tiles = 0;  // of the lane's sequence; no tiles if the tail kernel has none of it
+    if (lane < a.num_seqs) {
+        const int n = a.batch.lens[lane], q0 = a.batch.starts ? a.batch.starts[lane] : lane;
+        const int q1 = a.batch.starts ? a.batch.starts[lane + 1] : lane + 1;
+        const bool good = n >= 0 && n <= a.batch.max_len && q0 >= 0 && q1 >= q0 && q1 <= a.batch.num_queries &&
+                          q1 - q0 <= a.batch.max_queries;
+        if (!good && blockIdx.x == 0 && threadIdx.x < 64)
+            report(a.pages.err, KV_ASYNC_BAD_BATCH);
+        nq = good ? q1 - q0 : 0;
+        past = n - nq;
+        tiles = nq * a.group > kStepRows ? (nq * a.group + kTailRows - 1) / kTailRows : 0;
+    }
+    // Tiles of a sequence that end at `end` or behind: from the one on that has a row of token end - 1.
+    const auto from = [&](int64_t end, int past, int nq, int tiles) {
+        const int64_t x = end - past;  // that token's place among the new ones, from 1 on
+        return x <= 0 ? tiles : x > nq ? 0 : max(tiles - (static_cast<int>(x) - 1) * a.group / kTailRows, 0);
+    };
+    // More than `rank` tiles end at `end` or behind, and no more than that at end + left or behind.
+    int64_t end = -static_cast<int64_t>(a.batch.max_queries), left = a.batch.max_len - end + 1;
+    while (left > 1) {
+        const int64_t step = (left + 63) / 64, mine = end + (lane + 1) * step;
+        int count = 0;
+        for (int i = 0; i < a.num_seqs; ++i)
+            count += from(mine, __builtin_amdgcn_readlane(past, i), __builtin_amdgcn_readlane(nq, i),
+                          __builtin_amdgcn_readlane(tiles, i));
+        end += __popcll(__ballot(count > rank)) * step;
+        left = step;
+    }
+    // Of the tiles that end right there, by sequence.
+    const int here = from(end, past, nq, tiles), behind = from(end + 1, past, nq, tiles);
+    const int upto = sum_up_to_lane(here), upto_behind = sum_up_to_lane(behind);
+    if (rank >= __builtin_amdgcn_readlane(upto, 63))
+        return false;
+    const int at = rank - __builtin_amdgcn_readlane(upto_behind, 63), first = upto - upto_behind - (here - behind);
+    const uint64_t found = __ballot(at >= first && at < first + here - behind);
+    if (!found)
+        return false;
+    b = __builtin_ctzll(found);
+    tile = __builtin_amdgcn_readlane(tiles - here, b) + at - __builtin_amdgcn_readlane(first, b);
+    return true;
 }
 
 // Parts of a row that chose `count` pages, and their length; -1 where the number is bad.

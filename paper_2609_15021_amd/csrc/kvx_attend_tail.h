@@ -107,9 +107,15 @@ __global__ __launch_bounds__(64 * kRows / RW, 2) void tail_kernel(const AttendAr
     const Pages &pg = a.pages;
     const int tid = threadIdx.x, lane = tid & 63, c = lane & (RW - 1), part = lane / RW;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int groups = a.num_seqs * pg.H, group = blockIdx.x % groups, item = blockIdx.x / groups;
-    const int b = group / pg.H, h = group - b * pg.H;
-    const int split = item % parts.splits, tile = tiles - 1 - item / parts.splits;  // the longest first
+    const int groups = a.num_seqs * pg.H, group = blockIdx.x % groups, h = group % pg.H;
+    int b = group / pg.H, tile = tiles - 1 - blockIdx.x / groups / parts.splits;  // the longest first
+    int split = blockIdx.x / groups % parts.splits;
+    if (parts.ranked) {
+        const int item = blockIdx.x / pg.H;
+        split = item % parts.splits;
+        if (!tile_of_rank(a, item / parts.splits, b, tile))
+            return;
+    }
     Sequence seq;
     if (!sequence(a.batch, b, pg.err, seq))
         return;

@@ -219,10 +219,12 @@ struct ScoreArgs {
     int32_t *counts;
     int64_t token_stride, head_stride;  // elements
     float scale;
-    int32_t group, pad, shift;          // query heads of a KV head, and the power of two 2^shift that they fill, up to 16
+    int32_t BS, group, pad, shift;      // tokens of a page; query heads of a KV head, and the power of two 2^shift that they fill, up to 16
     int32_t page_chunks, tokens;        // of a launch's first dimension; tokens of a workgroup
     Divisor by_bs, by_chunks;
 };
+
+constexpr int kShareTarget = 1536;
 
 typedef short s16x2 __attribute__((ext_vector_type(2)));
 
@@ -234,14 +236,30 @@ __device__ __forceinline__ uint32_t negative(uint32_t x) {
     return __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(s16x2, x), s16x2{0, 0}));
 }
 
-// T: type of q; FP8: bounds are e4m3; DP >= D columns; PG: 16 pages of a wave.
-template <class T, bool FP8, int DP, int PG>
+__device__ __forceinline__ float from_lane(float x, int lane) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_ds_bpermute(lane * 4, __builtin_bit_cast(int, x)));
+}
+
+// A wave's 16-byte loads of 16 rows, a row for every 16th lane, would touch 16 lines of the cache for 64 bytes each, and
+// take 8 times as long as loads of whole rows (36 us instead of 22 for tails of up to 517 tokens over 1,057 pages, 2 heads of 8).  So
+// rows are loaded whole, and turned in LDS: bounds once for each wave, queries by the workgroup for all its waves, twice, so
+// that the next are on their way while one set is used.  Pieces of 16 bytes are permuted there, row by row, so that 16 rows'
+// same piece lies in different banks.
+//
+// T: type of q; FP8: bounds are e4m3; DP >= D columns; PG: 16 pages of a wave; OUT: tokens that a lane has results of
+// (4 heads are a lane's 4 results: 1 where a token's fill them, 2 or 4 of 2 heads or 1).
+template <class T, bool FP8, int DP, int PG, int OUT>
 __global__ __launch_bounds__(kThreads, 2) void score_kernel(const ScoreArgs a) {
-    constexpr int E = FP8 ? 1 : 2;
-    constexpr int KC = DP * E / 64;   // 16-byte pieces of a row in a lane
-    constexpr int KQ = KC * 2 / E;    // the same of a query's
+    constexpr int E = FP8 ? 1 : 2, WAVES = kThreads / 64;
+    constexpr int GB = DP * E / 16, KC = GB / 4;        // pieces of a row of bounds, and of them a lane's
+    constexpr int NB = GB / 4;                          // loads of 16 rows by a wave
+    constexpr int GQ = DP / 8, KQ = GQ / 4;             // the same of a row of queries
+    constexpr int TILES = DP > 128 ? 1 : 2;             // of 16 rows that the workgroup loads at once
+    constexpr int NQ = TILES * GQ * 16 / kThreads > 0 ? TILES * GQ * 16 / kThreads : 1;  // loads of them
+    constexpr int kQueries = TILES * GQ * 16, kBounds = GB * 16;  // pieces
+    __shared__ u32x4 lds[2 * kQueries > WAVES * kBounds ? 2 * kQueries : WAVES * kBounds];
     const Pages &pg = a.bounds;
-    const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4, wave = threadIdx.x >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4, wave = tid >> 6;
     const int h = blockIdx.y, b = blockIdx.z;
     const int share = divide(blockIdx.x, a.by_chunks), chunk = blockIdx.x - share * a.page_chunks;
     Sequence s;
@@ -253,120 +271,182 @@ __global__ __launch_bounds__(kThreads, 2) void score_kernel(const ScoreArgs a) {
     const int i0 = static_cast<int>(i64), i1 = static_cast<int>(min(i64 + a.tokens, int64_t{s.nq}));
     const int past = s.n - s.nq;
     if (a.counts && chunk == 0 && h == 0)
-        for (int i = i0 + static_cast<int>(threadIdx.x); i < i1; i += kThreads)
+        for (int i = i0 + tid; i < i1; i += kThreads)
             a.counts[s.q0 + i] = past + i < 0 ? 0 : divide(past + i, a.by_bs) + 1;
     const int last = past + i1 - 1, pages = last < 0 ? 0 : divide(last, a.by_bs) + 1;
-    const int page0 = (chunk * (kThreads / 64) + wave) * 16 * PG;
-    if (page0 >= pages)
+    if (chunk * WAVES * 16 * PG >= pages)
         return;
+    const int page0 = (chunk * WAVES + wave) * 16 * PG;
+    const bool some = page0 < pages;  // (a wave without pages helps to load the others' queries)
 
-    // This lane's pages, and their bounds.
+    // Rows of queries: row m of a tile is token m / pad (of the tile's) and one of its heads.  A tile beyond the last
+    // repeats it.
+    const int each = 16 >> a.shift;                     // tokens of a tile
+    const int subs = (a.group + 15) / 16;               // tiles of a token, where it has more heads
+    const int tiles = ((i1 - i0 + each - 1) >> (4 - a.shift)) * subs;
+    u32x4 next[NQ];
+    const auto request = [&](int tile0) {
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+            const int u = tid + n * kThreads, row = u / GQ % 16, piece = u % GQ;
+            const int tile = min(tile0 + u / (GQ * 16), tiles - 1), of = subs == 1 ? tile : tile / subs;
+            const int token = min(i0 + of * each + (row >> a.shift), i1 - 1);
+            const int head = h * a.group + min((row & (a.pad - 1)) + (tile - of * subs) * 16, a.group - 1);
+            const uint8_t *x = a.q.data + int64_t{s.q0 + token} * a.q.token_stride + head * a.q.head_stride;
+            next[n] = *reinterpret_cast<const u32x4 *>(x + (piece * 8 < pg.D ? piece * 16 : 0));
+            if (piece * 8 >= pg.D)
+                next[n] = u32x4{0, 0, 0, 0};  // (where bounds repeat their first columns)
+        }
+    };
+    const auto deposit = [&](int buffer) {
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+            const int u = tid + n * kThreads, row = u / GQ, piece = u % GQ;
+            if (kQueries >= kThreads || u < kQueries)
+                lds[buffer * kQueries + row * GQ + (piece ^ (row & (GQ - 1) & 15))] = next[n];
+        }
+    };
+    request(0);
+
+    // This lane's pages, their first tokens, and their bounds.
     u32x4 low[PG][KC], high[PG][KC];
     float factor[PG];
     bool good[PG];
+    int start[PG];
+    if (some) {
+        u32x4 raw[PG][2][NB];
 #pragma unroll
-    for (int j = 0; j < PG; ++j) {
-        const int page = page0 + j * 16 + c;
-        const int block = page < pages ? a.batch.tables[b * a.batch.table_stride + page] : -1;
-        good[j] = page < pages && in_cache(pg, block);
-        const int64_t at = page_offset(pg, good[j] ? block : 0, 0, h);
-        factor[j] = a.scale;
-        if (FP8 && a.scales.data && good[j])
-            factor[j] *= power_of(*scale_at(a.scales, block, 0, h));
+        for (int j = 0; j < PG; ++j) {
+            const int page = page0 + j * 16 + c;
+            start[j] = page < pages ? page * a.BS : INT32_MAX;
+            const int block = page < pages ? a.batch.tables[b * a.batch.table_stride + page] : -1;
+            good[j] = page < pages && in_cache(pg, block);
+            factor[j] = a.scale;
+            if (FP8 && a.scales.data && good[j])
+                factor[j] *= power_of(*scale_at(a.scales, block, 0, h));
 #pragma unroll
-        for (int k = 0; k < KC; ++k) {
-            const int piece = k * 64 + g * 16;
-            const uint8_t *x = pg.base + at + (piece < pg.row_bytes ? piece : 0);
-            low[j][k] = *reinterpret_cast<const u32x4 *>(x);
-            high[j][k] = *reinterpret_cast<const u32x4 *>(x + pg.v_bytes);
+            for (int n = 0; n < NB; ++n) {
+                const int piece = lane % GB, of = __shfl(good[j] ? block : 0, n * (64 / GB) + lane / GB);
+                const uint8_t *x = pg.base + page_offset(pg, of, 0, h) + (piece * 16 < pg.row_bytes ? piece * 16 : 0);
+                raw[j][0][n] = *reinterpret_cast<const u32x4 *>(x);
+                raw[j][1][n] = *reinterpret_cast<const u32x4 *>(x + pg.v_bytes);
+            }
         }
-    }
-
-    // 16 rows of queries: row m is token m / pad (of the tile) and one of its heads.
-    const int each = 16 >> a.shift;                     // tokens of a tile
-    const int subs = (a.group + 15) / 16;               // tiles of a token, where it has more heads
-    const auto load_q = [&](int i, int sub, u32x4 (&q)[KQ]) {
-        const int token = min(i + (c >> a.shift), i1 - 1), head = h * a.group + min((c & (a.pad - 1)) + sub * 16, a.group - 1);
-        const uint8_t *x = a.q.data + int64_t{s.q0 + token} * a.q.token_stride + head * a.q.head_stride;
-#pragma unroll
-        for (int k = 0; k < KQ; ++k) {
-            const int d = FP8 ? (k >> 1) * 64 + g * 16 + (k & 1) * 8 : k * 32 + g * 8;
-            q[k] = d < pg.D ? *reinterpret_cast<const u32x4 *>(x + 2 * d) : u32x4{0, 0, 0, 0};
-        }
-    };
-    u32x4 next[KQ];
-    load_q(i0, 0, next);
-    f32x4 best[PG];
-    for (int i = i0, sub = 0; i < i1;) {
-        u32x4 q[KQ];
-#pragma unroll
-        for (int k = 0; k < KQ; ++k)
-            q[k] = next[k];
-        const bool done = sub + 1 == subs;
-        const int next_i = done ? i + each : i, next_sub = done ? 0 : sub + 1;
-        if (next_i < i1)
-            load_q(next_i, next_sub, next);
-        f32x4 x[PG];
+        u32x4 *mine = lds + wave * kBounds;
 #pragma unroll
         for (int j = 0; j < PG; ++j)
-            x[j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int k = 0; k < KQ; ++k) {
-            u32x4 up, down;
+            for (int kv = 0; kv < 2; ++kv) {
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                up[w] = positive(q[k][w]);
-                down[w] = negative(q[k][w]);
+                for (int n = 0; n < NB; ++n) {
+                    const int row = n * (64 / GB) + lane / GB, piece = lane % GB;
+                    mine[row * GB + (piece ^ (row & (GB - 1) & 15))] = raw[j][kv][n];
+                }
+                __builtin_amdgcn_wave_barrier();  // (LDS serves a wave's accesses in order)
+#pragma unroll
+                for (int k = 0; k < KC; ++k)
+                    (kv ? high : low)[j][k] = mine[c * GB + ((k * 4 + g) ^ (c & (GB - 1) & 15))];
+                __builtin_amdgcn_wave_barrier();
             }
+    }
+    __syncthreads();
+    deposit(0);
+    __syncthreads();
+
+    float *scores = a.scores + h * a.head_stride + page0 + c;
+    f32x4 best[PG];
+    for (int tile0 = 0, buffer = 0; tile0 < tiles; tile0 += TILES, buffer ^= 1) {
+        const bool more = tile0 + TILES < tiles;
+        if (more)
+            request(tile0 + TILES);
 #pragma unroll
-            for (int j = 0; j < PG; ++j) {
-                if constexpr (FP8) {
-                    const int w = (k & 1) * 2;
-                    const uint32_t h0 = high[j][k >> 1][w], h1 = high[j][k >> 1][w + 1];
-                    const uint32_t l0 = low[j][k >> 1][w], l1 = low[j][k >> 1][w + 1];
-                    x[j] = mfma_16x16x32(up, u32x4{T::from_e4m3(h0, false), T::from_e4m3(h0, true),
-                                                   T::from_e4m3(h1, false), T::from_e4m3(h1, true)}, x[j], T{});
-                    x[j] = mfma_16x16x32(down, u32x4{T::from_e4m3(l0, false), T::from_e4m3(l0, true),
-                                                     T::from_e4m3(l1, false), T::from_e4m3(l1, true)}, x[j], T{});
-                } else {
-                    x[j] = mfma_16x16x32(up, high[j][k], x[j], T{});
-                    x[j] = mfma_16x16x32(down, low[j][k], x[j], T{});
+        for (int t = 0; t < TILES; ++t) {
+            const int tile = tile0 + t;
+            if (tile >= tiles || !some)
+                break;
+            f32x4 x[PG];
+#pragma unroll
+            for (int j = 0; j < PG; ++j)
+                x[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < KQ; ++k) {
+                // (Of e4m3 a lane's piece has 16 columns, and the two products' queries lie side by side.)
+                const int piece = FP8 ? (k >> 1) * 8 + g * 2 + (k & 1) : k * 4 + g;
+                const u32x4 q = lds[buffer * kQueries + (t * 16 + c) * GQ + (piece ^ (c & (GQ - 1) & 15))];
+                u32x4 up, down;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    up[w] = positive(q[w]);
+                    down[w] = negative(q[w]);
+                }
+#pragma unroll
+                for (int j = 0; j < PG; ++j) {
+                    if constexpr (FP8) {
+                        const int w = (k & 1) * 2;
+                        const uint32_t h0 = high[j][k >> 1][w], h1 = high[j][k >> 1][w + 1];
+                        x[j] = mfma_16x16x32(up, u32x4{T::from_e4m3(h0, false), T::from_e4m3(h0, true),
+                                                       T::from_e4m3(h1, false), T::from_e4m3(h1, true)}, x[j], T{});
+                    } else {
+                        x[j] = mfma_16x16x32(up, high[j][k], x[j], T{});
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < PG; ++j) {
+                    if constexpr (FP8) {
+                        const int w = (k & 1) * 2;
+                        const uint32_t l0 = low[j][k >> 1][w], l1 = low[j][k >> 1][w + 1];
+                        x[j] = mfma_16x16x32(down, u32x4{T::from_e4m3(l0, false), T::from_e4m3(l0, true),
+                                                         T::from_e4m3(l1, false), T::from_e4m3(l1, true)}, x[j], T{});
+                    } else {
+                        x[j] = mfma_16x16x32(down, low[j][k], x[j], T{});
+                    }
                 }
             }
-        }
+            const int of = subs == 1 ? tile : tile / subs, sub = tile - of * subs;
 #pragma unroll
-        for (int j = 0; j < PG; ++j)
+            for (int j = 0; j < PG; ++j)
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-                best[j][r] = sub == 0 ? x[j][r] : fmaxf(best[j][r], x[j][r]);
-        if (done) {
+                for (int r = 0; r < 4; ++r)
+                    best[j][r] = subs == 1 || sub == 0 ? x[j][r] : fmaxf(best[j][r], x[j][r]);
+            if (sub + 1 < subs)
+                continue;
 #pragma unroll
             for (int j = 0; j < PG; ++j) {
                 f32x4 y = best[j];
-                if (a.pad >= 2) {
+                if constexpr (OUT <= 2) {
                     y[0] = fmaxf(y[0], y[1]);
-                    y[2] = fmaxf(y[2], y[3]);
+                    y[1] = fmaxf(y[2], y[3]);
                 }
-                if (a.pad >= 4)
-                    y[0] = fmaxf(y[0], y[2]);
-                if (a.pad >= 8)
-                    y[0] = fmaxf(y[0], __shfl_xor(y[0], 16));
-                if (a.pad == 16)
-                    y[0] = fmaxf(y[0], __shfl_xor(y[0], 32));
-                const int page = page0 + j * 16 + c;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int m = g * 4 + r, token = i + (m >> a.shift);
-                    if ((m & (a.pad - 1)) != 0 || token >= i1 || past + token < 0 || page > divide(past + token, a.by_bs))
+                if constexpr (OUT == 1) {
+                    y[0] = fmaxf(y[0], y[1]);
+                    if (a.shift >= 3)
+                        y[0] = fmaxf(y[0], from_lane(y[0], lane ^ 16));
+                    if (a.shift == 4)
+                        y[0] = fmaxf(y[0], from_lane(y[0], lane ^ 32));
+                    if (g & ((a.pad >> 2) - 1))
                         continue;
-                    a.scores[int64_t{s.q0 + token} * a.token_stride + h * a.head_stride + page] =
-                        good[j] ? y[r] * factor[j] : -INFINITY;
+                }
+#pragma unroll
+                for (int r = 0; r < OUT; ++r) {
+                    const int token = i0 + of * each + (OUT == 1 ? g * 4 >> a.shift : g * OUT + r);
+                    if (token < i1 && start[j] <= past + token)
+                        scores[int64_t{s.q0 + token} * a.token_stride + j * 16] = good[j] ? y[r] * factor[j] : -INFINITY;
                 }
             }
         }
-        i = next_i;
-        sub = next_sub;
+        if (more) {
+            deposit(buffer ^ 1);
+            __syncthreads();
+        }
     }
+}
+
+template <class T, bool FP8, int DP, int PG>
+hipError_t launch_score_to(const ScoreArgs &a, const dim3 &grid, hipStream_t stream) {
+    const auto kernel = a.shift == 0   ? score_kernel<T, FP8, DP, PG, 4>
+                        : a.shift == 1 ? score_kernel<T, FP8, DP, PG, 2>
+                                       : score_kernel<T, FP8, DP, PG, 1>;
+    return launch_kernel(kernel, grid, kThreads, stream, a);
 }
 
 template <class T, bool FP8, int DP, int PG>
@@ -374,16 +454,16 @@ hipError_t launch_score(ScoreArgs a, int num_seqs, int most, int64_t pages, hipS
     const int64_t chunks = (pages + 16 * PG * (kThreads / 64) - 1) / (16 * PG * (kThreads / 64));
     // Rows are shared out where the pages alone leave CUs idle.
     const int each = 16 / a.pad;
-    const int64_t tiles = (int64_t{most} + each - 1) / each, groups = chunks * a.bounds.H * num_seqs;
-    const int64_t shares = std::min(tiles, std::max<int64_t>((2048 + groups - 1) / groups, 1));
-    a.tokens = static_cast<int32_t>((tiles + shares - 1) / shares * each);
+    const int64_t tiles = (int64_t{most} + each - 1) / each, groups = chunks * a.bounds.H;
+    // (Of all sequences there are about as many tiles as of their tokens in one.)
+    const int64_t all = std::min(tiles * num_seqs, (int64_t{a.batch.num_queries} + each - 1) / each + num_seqs);
+    const int64_t share = std::max<int64_t>(all * groups / kShareTarget, 1);
+    a.tokens = static_cast<int32_t>(std::min((share + 1) / 2 * 2, tiles) * each);
     a.page_chunks = static_cast<int32_t>(chunks);
     a.by_chunks = divisor(chunks);
     const int64_t grid = chunks * ((int64_t{most} + a.tokens - 1) / a.tokens);
-    return launch_kernel(score_kernel<T, FP8, DP, PG>,
-                         dim3(static_cast<uint32_t>(grid), static_cast<uint32_t>(a.bounds.H),
-                              static_cast<uint32_t>(num_seqs)),
-                         kThreads, stream, a);
+    return launch_score_to<T, FP8, DP, PG>(a, dim3(static_cast<uint32_t>(grid), static_cast<uint32_t>(a.bounds.H),
+                                                   static_cast<uint32_t>(num_seqs)), stream);
 }
 
 template <class T, bool FP8>
@@ -461,6 +541,7 @@ kv_status score(const kv_cache *bounds, int32_t layer, const kv_batch *batch, co
     a.head_stride = o->head_stride;
     a.scale = o->scale == 0.f ? 1.f : o->scale;
     a.by_bs = divisor(o->block_size);
+    a.BS = o->block_size;
     a.group = q->heads / H;
     while ((1 << a.shift) < a.group && a.shift < 4)
         ++a.shift;
