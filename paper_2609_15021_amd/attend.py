@@ -21,6 +21,11 @@ import torch
 
 from .kvx import Cache, KvCache, _in_use_on, _lib, _raise
 
+try:
+    from . import _tensors
+except ImportError as e:
+    raise ImportError("the binding's module _tensors is not built: python -c 'import __graft_entry__ as g; g.build()'") from e
+
 KV_DTYPE_BF16 = 1
 KV_DTYPE_F16 = 2
 KV_DTYPE_E4M3 = 3
@@ -112,8 +117,9 @@ def _declare(lib):
 _declare(_lib)
 
 
-# A decoding step makes a call per layer, and short calls are bound by this module: checks read each property once, and
-# what only the numbers decide is remembered by them.
+# A decoding step makes a call per layer, and short calls are bound by this module: a tensor that is as it should be is
+# looked at by _tensors, in one call; where that answers None, the checks here say what is wrong.  What only the numbers
+# decide is remembered by them.
 
 
 def _ints(t, name: str, dims: int, device: int, rows=None):
@@ -130,6 +136,9 @@ def _ints(t, name: str, dims: int, device: int, rows=None):
 
 def _dense_ints(t, name: str, dims: int, device: int, rows: int) -> int:
     """The address of a contiguous one."""
+    at = _tensors.ints(t, dims, device, rows)
+    if at is not None:
+        return at
     _ints(t, name, dims, device, rows)
     if not t.is_contiguous():
         raise TypeError(f"{name} must be contiguous")
@@ -170,6 +179,9 @@ def _no_gradient(name: str):
 
 def _rows(t, name: str, head_dim: int, device: int):
     """(kv_rows, the tensor's shape)."""
+    found = _tensors.rows(t, head_dim, device)
+    if found is not None:
+        return found
     if not isinstance(t, torch.Tensor) or len(shape := t.shape) != 3 or (dtype := _ROW_TYPES.get(t.dtype)) is None:
         raise TypeError(f"{name} must be a [tokens][heads][D] device tensor of bfloat16 or float16")
     if t.requires_grad and torch.is_grad_enabled():
@@ -198,7 +210,10 @@ def _int32(x, name: str) -> int:
 
 
 def _batch(block_size: int, device: int, tables, lens, starts, tokens: int, max_q, max_len):
-    """The numbers of kv_batch, in its order."""
+    """(kv_batch, its num_seqs, max_queries and max_len)."""
+    found = _tensors.batch(block_size, device, tables, lens, starts, tokens, max_q, max_len)
+    if found is not None:
+        return found
     (B, pages), (stride, _) = _ints(tables, "tables", 2, device)
     if tokens >= 2**31:
         _int32(tokens, "the number of new tokens")
@@ -214,7 +229,8 @@ def _batch(block_size: int, device: int, tables, lens, starts, tokens: int, max_
     most = min(pages * block_size, 2**31 - 1024)
     if max_len is not None:
         most = min(most, max(int(max_len), -1))
-    return B, max_q, tokens, most, pages, 0, stride, tables.data_ptr(), lens.data_ptr(), starts_at
+    batch = _pack_batch(B, max_q, tokens, most, pages, 0, stride, tables.data_ptr(), lens.data_ptr(), starts_at)
+    return batch, B, max_q, most
 
 
 def _cache_dtype(cache: Cache, dtype, rows) -> int:
@@ -259,6 +275,9 @@ def _used(stream, *tensors) -> None:
 
 def _page_scales(t, cache: Cache, device: int):
     """kv_page_scales: (address, block stride, K to V)."""
+    found = _tensors.scales(t, cache.layout.num_kv_heads, cache.struct.num_blocks, device)
+    if found is not None:
+        return found
     if not isinstance(t, torch.Tensor) or (t.dtype is not torch.uint8 and t.dtype is not torch.float8_e8m0fnu) or \
             len(shape := t.shape) != 3:
         raise TypeError("scales must be a [blocks][2][heads] uint8 or float8_e8m0fnu device tensor")
@@ -304,7 +323,7 @@ def kv_append(cache: Cache, layer: int, k, v, tables, lens, starts=None, *, max_
     (kr, shape), (vr, v_shape) = _rows(k, "k", D, device), _rows(v, "v", D, device)
     if shape != v_shape:
         raise ValueError(f"k and v differ in shape: {tuple(shape)} and {tuple(v_shape)}")
-    batch = _pack_batch(*_batch(layout.block_size, device, tables, lens, starts, shape[0], max_q, max_len))
+    batch = _batch(layout.block_size, device, tables, lens, starts, shape[0], max_q, max_len)[0]
     handle, _ = _call_stream(stream)
     if k_scale != 1.0 or v_scale != 1.0:
         k_scale, v_scale = _factor(k_scale, "k_scale"), _factor(v_scale, "v_scale")
@@ -327,7 +346,7 @@ def kv_append_scaled(cache: Cache, layer: int, k, v, tables, lens, scales, start
     (kr, shape), (vr, v_shape) = _rows(k, "k", D, device), _rows(v, "v", D, device)
     if shape != v_shape:
         raise ValueError(f"k and v differ in shape: {tuple(shape)} and {tuple(v_shape)}")
-    batch = _pack_batch(*_batch(layout.block_size, device, tables, lens, starts, shape[0], max_q, max_len))
+    batch = _batch(layout.block_size, device, tables, lens, starts, shape[0], max_q, max_len)[0]
     by = _pack_scales(*_page_scales(scales, cache, device))
     handle, _ = _call_stream(stream)
     _raise(_lib.kv_append_scaled(ctypes.byref(cache.struct), _int32(layer, "layer"), batch, kr, vr, by, handle))
@@ -355,26 +374,24 @@ def kv_rotate(cache: Cache, layer: int, q, k, v, tables, lens, starts=None, *, f
     if shape != v_shape or q_shape[0] != shape[0]:
         raise ValueError(f"q, k and v differ in shape: {tuple(q_shape)}, {tuple(shape)} and {tuple(v_shape)}")
     tokens = q_shape[0]
-    batch = _pack_batch(*_batch(layout.block_size, device, tables, lens, starts, tokens, max_q, max_len))
+    batch = _batch(layout.block_size, device, tables, lens, starts, tokens, max_q, max_len)[0]
     if k_scale != 1.0 or v_scale != 1.0:
         k_scale, v_scale = _factor(k_scale, "k_scale"), _factor(v_scale, "v_scale")
     rotary = freqs_at = 0
     if freqs is not None:
-        if not isinstance(freqs, torch.Tensor) or freqs.dtype is not torch.float64 or freqs.dim() != 1 or \
-                not freqs.is_contiguous():
-            raise TypeError("freqs must be a contiguous 1-dimensional float64 device tensor")
-        if freqs.requires_grad and torch.is_grad_enabled():
-            _no_gradient("freqs")
-        if freqs.get_device() != device:
-            _elsewhere(freqs, "freqs", device)
-        rotary, freqs_at = _int32(2 * freqs.shape[0], "twice the number of freqs"), freqs.data_ptr()
+        freqs_at = _tensors.vector(freqs, -1, 64, device)
+        if freqs_at is None:
+            freqs_at = _freqs(freqs, device)
+        rotary = _int32(2 * freqs.shape[0], "twice the number of freqs")
     positions_at = 0 if positions is None else _dense_ints(positions, "positions", 1, device, tokens)
-    q_weight_at = 0 if q_weight is None else _norm_weight(q_weight, "q_weight", D, q.dtype, device)
-    k_weight_at = 0 if k_weight is None else _norm_weight(k_weight, "k_weight", D, q.dtype, device)
-    weight = q_weight if k_weight is None else k_weight
-    if q_weight is not None and weight.dtype is not q_weight.dtype:
-        raise TypeError("q_weight and k_weight have different types")
-    weight_dtype = 0 if weight is None else KV_DTYPE_F32 if weight.dtype is torch.float32 else _DTYPES[weight.dtype]
+    q_weight_at = k_weight_at = weight_dtype = 0
+    if q_weight is not None:
+        q_weight_at, weight_dtype = _norm_weight(q_weight, "q_weight", D, q.dtype, device)
+    if k_weight is not None:
+        k_weight_at, k_dtype = _norm_weight(k_weight, "k_weight", D, q.dtype, device)
+        if weight_dtype and weight_dtype != k_dtype:
+            raise TypeError("q_weight and k_weight have different types")
+        weight_dtype = k_dtype
     by = None if scales is None else KvPageScales(*_page_scales(scales, cache, device))
     options = _pack_rotate(_cache_dtype(cache, dtype, k), rotary, 1 if interleaved else 0, weight_dtype, freqs_at,
                            positions_at, q_weight_at, k_weight_at, eps, weight_offset, _factor(magnitude, "magnitude"),
@@ -382,25 +399,45 @@ def kv_rotate(cache: Cache, layer: int, q, k, v, tables, lens, starts=None, *, f
     handle, here = _call_stream(stream)
     if out is None:
         with here:
-            out = q.new_empty(q_shape)
+            out, outr = _new_rows(q, q_shape)
     elif not isinstance(out, torch.Tensor) or out.dtype != q.dtype or out.shape != q_shape:
         raise TypeError("out must have the type and shape of q")
-    _raise(_lib.kv_rotate(ctypes.byref(cache.struct), _int32(layer, "layer"), batch, options, qr,
-                          _rows(out, "out", D, device)[0], kr, vr, handle))
+    else:
+        outr, _ = _rows(out, "out", D, device)
+    _raise(_lib.kv_rotate(ctypes.byref(cache.struct), _int32(layer, "layer"), batch, options, qr, outr, kr, vr, handle))
     if stream is not None:
         _used(stream, q, k, v, tables, lens, starts, freqs, positions, q_weight, k_weight, scales, out)
     return out
 
 
-def _norm_weight(t, name: str, head_dim: int, rows_dtype, device: int) -> int:
+def _freqs(t, device: int) -> int:
+    if not isinstance(t, torch.Tensor) or t.dtype is not torch.float64 or t.dim() != 1 or not t.is_contiguous():
+        raise TypeError("freqs must be a contiguous 1-dimensional float64 device tensor")
+    if t.requires_grad and torch.is_grad_enabled():
+        _no_gradient("freqs")
+    _on(t, "freqs", device)
+    return t.data_ptr()
+
+
+def _norm_weight(t, name: str, head_dim: int, rows_dtype, device: int):
+    """(address, KV_DTYPE)"""
+    at = _tensors.vector(t, head_dim, KV_DTYPE_F32, device)
+    if at is not None:
+        return at, KV_DTYPE_F32
     if not isinstance(t, torch.Tensor) or t.shape != (head_dim,) or not t.is_contiguous() or \
             (t.dtype is not torch.float32 and t.dtype is not rows_dtype):
         raise TypeError(f"{name} must be a contiguous [{head_dim}] device tensor of float32 or {rows_dtype}")
     if t.requires_grad and torch.is_grad_enabled():
         _no_gradient(name)
-    if t.get_device() != device:
-        _elsewhere(t, name, device)
-    return t.data_ptr()
+    _on(t, name, device)
+    return t.data_ptr(), KV_DTYPE_F32 if t.dtype is torch.float32 else _DTYPES[t.dtype]
+
+
+def _new_rows(like, shape):
+    """(a contiguous tensor like the rows `like`, its kv_rows)."""
+    tokens, heads, width = shape
+    t, at = _tensors.empty(like, 0, tokens, heads, width)
+    return t, _pack_rows(at, heads * width, width, heads, _ROW_TYPES[like.dtype])
 
 
 def kv_attend(cache: Cache, layer: int, q, tables, lens, starts=None, *, max_q=None, max_len=None, dtype=None,
@@ -426,7 +463,9 @@ def kv_attend(cache: Cache, layer: int, q, tables, lens, starts=None, *, max_q=N
     layout = cache.layout
     qr, q_shape = _rows(q, "q", layout.head_dim, device)
     tokens, q_heads, _ = q_shape
-    B, max_q, _, most, *table = _batch(layout.block_size, device, tables, lens, starts, tokens, max_q, max_len)
+    if weights is not None and max_len is None and isinstance(weights, torch.Tensor) and weights.dim() == 3:
+        max_len = weights.shape[2]
+    batch, B, max_q, most = _batch(layout.block_size, device, tables, lens, starts, tokens, max_q, max_len)
     if k_scale != 1.0 or v_scale != 1.0:
         k_scale, v_scale = _factor(k_scale, "k_scale"), _factor(v_scale, "v_scale")
     else:
@@ -437,9 +476,7 @@ def kv_attend(cache: Cache, layer: int, q, tables, lens, starts=None, *, max_q=N
         slopes_at = slopes.data_ptr()
     if weights is not None:
         _weights(weights, "weights", device, (B, layout.num_kv_heads))
-        if max_len is None:
-            most = min(most, weights.shape[2])
-        elif weights.shape[2] < most:
+        if weights.shape[2] < most:
             raise ValueError(f"weights of {weights.shape[2]} tokens for sequences of up to {most}")
         weights_at, weights_seq, weights_head = weights.data_ptr(), weights.stride(0), weights.stride(1)
         if prior is not None:
@@ -453,7 +490,6 @@ def kv_attend(cache: Cache, layer: int, q, tables, lens, starts=None, *, max_q=N
     options = KvAttendOptions(_cache_dtype(cache, dtype, q), window, 0.0 if scale is None else _factor(scale, "scale"),
                               _factor(softcap, "softcap") if softcap else 0.0, k_scale, v_scale, slopes_at, prior_at,
                               weights_at, weights_seq, weights_head, 1 if full_weights else 0)
-    batch = KvBatch(B, max_q, tokens, most, *table)
     by = chosen = None
     budget = -1
     if scales is not None:
@@ -470,7 +506,8 @@ def kv_attend(cache: Cache, layer: int, q, tables, lens, starts=None, *, max_q=N
     key = (layout.num_kv_heads, layout.head_dim, layout.elem_bytes, layout.block_size, B, max_q, tokens, most, window,
            weights is None, q_heads, budget)
     need = _attend_bytes.get(key)
-    at, batch, options = ctypes.byref(cache.struct), ctypes.byref(batch), ctypes.byref(options)
+    at, batch = ctypes.byref(cache.struct), ctypes.byref(KvBatch.from_buffer_copy(batch))
+    options = ctypes.byref(options)
     if need is None:
         need = _lib.kv_attend_workspace(at, batch, options, qr) if by is None and chosen is None else \
             _lib.kv_attend_pages_workspace(at, batch, options, by, chosen, qr)
@@ -480,19 +517,23 @@ def kv_attend(cache: Cache, layer: int, q, tables, lens, starts=None, *, max_q=N
             _attend_bytes.clear()
         _attend_bytes[key] = need
     handle, here = _call_stream(stream)
+    workspace = None
     with here:
         if out is None:
-            out = q.new_empty(q_shape)
+            out, outr = _new_rows(q, q_shape)
+        else:
+            outr, _ = _rows(out, "out", layout.head_dim, device)
         if lse is None:
-            lse = q.new_empty(heads, dtype=torch.float32)
-        workspace = q.new_empty(need, dtype=torch.uint8).data_ptr() if need else None
-    outr, _ = _rows(out, "out", layout.head_dim, device)
+            lse, lse_at = _tensors.empty(q, 1, tokens, q_heads)
+        else:
+            lse_at = lse.data_ptr()
+        if need:
+            space, workspace = _tensors.empty(q, 3, need)
     layer = _int32(layer, "layer")
     if by is None and chosen is None:
-        _raise(_lib.kv_attend(at, layer, batch, options, qr, outr, lse.data_ptr(), workspace, need, handle))
+        _raise(_lib.kv_attend(at, layer, batch, options, qr, outr, lse_at, workspace, need, handle))
     else:
-        _raise(_lib.kv_attend_pages(at, layer, batch, options, by, chosen, qr, outr, lse.data_ptr(), workspace, need,
-                                    handle))
+        _raise(_lib.kv_attend_pages(at, layer, batch, options, by, chosen, qr, outr, lse_at, workspace, need, handle))
     if stream is not None:
         _used(stream, q, tables, lens, starts, slopes, weights, prior, out, lse, scales, pages, counts)
     return out, lse
@@ -525,7 +566,7 @@ def kv_bounds(cache: Cache, layer: int, bounds: Cache, tables, lens, starts=None
         # (How many rows there are only the device knows: as many as sequences may have tokens.)
         tokens = 2**31 - 1
         max_q = tokens if max_q is None else max_q
-    batch = _pack_batch(*_batch(layout.block_size, device, tables, lens, starts, tokens, max_q, max_len))
+    batch = _batch(layout.block_size, device, tables, lens, starts, tokens, max_q, max_len)[0]
     if dtype is None:
         if layout.elem_bytes != 1:
             raise TypeError("dtype is needed: bfloat16 or float16")
@@ -552,15 +593,15 @@ def kv_score(bounds: Cache, layer: int, q, tables, lens, starts=None, *, block_s
     block_size = _int32(block_size, "block_size")
     if block_size < 1:
         raise ValueError(f"block_size must be positive (got {block_size})")
-    batch = _batch(block_size, device, tables, lens, starts, tokens, max_q, max_len)
+    batch, _, _, most = _batch(block_size, device, tables, lens, starts, tokens, max_q, max_len)
     heads = layout.num_kv_heads
-    pages = -(-max(batch[3], 0) // block_size)
+    pages = -(-max(most, 0) // block_size)
     handle, here = _call_stream(stream)
     with here:
         if out is None:
-            out = q.new_empty((tokens, heads, pages), dtype=torch.float32)
+            out, _ = _tensors.empty(q, 1, tokens, heads, pages)
         if counts is None:
-            counts = (q.new_empty if starts is None else q.new_zeros)(tokens, dtype=torch.int32)
+            counts = _tensors.empty(q, 2, tokens)[0] if starts is None else q.new_zeros(tokens, dtype=torch.int32)
     _weights(out, "out", device, (tokens, heads))
     if out.shape[2] < pages:
         raise ValueError(f"out of {out.shape[2]} pages for sequences of up to {pages}")
@@ -568,7 +609,7 @@ def kv_score(bounds: Cache, layer: int, q, tables, lens, starts=None, *, block_s
     by = None if scales is None else KvPageScales(*_page_scales(scales, bounds, device))
     options = _pack_score(_cache_dtype(bounds, dtype, q), block_size, _factor(scale, "scale"), 0,
                           0 if by is None else ctypes.addressof(by), token, head)
-    _raise(_lib.kv_score(ctypes.byref(bounds.struct), _int32(layer, "layer"), _pack_batch(*batch), options, qr,
+    _raise(_lib.kv_score(ctypes.byref(bounds.struct), _int32(layer, "layer"), batch, options, qr,
                          out.data_ptr(), _dense_ints(counts, "counts", 1, device, tokens), handle))
     if stream is not None:
         _used(stream, q, tables, lens, starts, scales, out, counts)

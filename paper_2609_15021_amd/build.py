@@ -113,8 +113,28 @@ def build_tierd(verbose: bool = False) -> str:
     return TIERD_BIN
 
 
+TENSORS_SRC = os.path.join(CSRC, "kvx_tensors.cpp")
+TENSORS_LIB = os.path.join(PKG, "_tensors.so")
+
+
+def build_tensors(verbose: bool = False) -> str:
+    """The binding's questions to torch tensors, as a Python module over torch's own headers."""
+    import sysconfig
+
+    import torch
+    home = os.path.dirname(torch.__file__)
+    tmp = TENSORS_LIB + ".tmp"
+    _run(["g++", "-std=c++17", "-O2", "-Wall", "-Wextra", "-fPIC", "-shared", "-fvisibility=hidden",
+          f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", INCLUDE,
+          "-isystem", os.path.join(home, "include"), "-isystem", sysconfig.get_paths()["include"], TENSORS_SRC, "-o", tmp,
+          "-L", os.path.join(home, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"], verbose)
+    os.replace(tmp, TENSORS_LIB)
+    return TENSORS_LIB
+
+
 def build_all(verbose: bool = False):
-    return build_kvx(verbose), build_harness(verbose), build_native_caller(verbose), build_tierd(verbose)
+    return (build_kvx(verbose), build_harness(verbose), build_native_caller(verbose), build_tierd(verbose),
+            build_tensors(verbose))
 
 
 if __name__ == "__main__":
