@@ -79,7 +79,7 @@ typedef struct kv_page_scales {
     int64_t kv_stride;     /* bytes, >= heads */
 } kv_page_scales;
 
-/* The pages that each new token chose, for each KV head (heads == 1: the same for all): of row r and head h the first
+/* The pages that each new token chose, for each KV head (heads == 1: the same for all): of row r and head h, with room for budget, the first
  * counts[r] numbers at pages + r*token_stride + h*head_stride, each a place in its sequence's block table.  As kv_keep
  * leaves them; in any order.  A page that is named twice takes part twice. */
 typedef struct kv_page_list {

@@ -237,8 +237,10 @@ PagesPlan plan_of(const kv_cache *cache, const kv_batch *batch, const kv_page_li
     p.chosen.token_stride = list->token_stride;
     p.chosen.head_stride = list->heads == 1 ? 0 : list->head_stride;
     p.chosen.budget = list->budget;
-    p.chosen.splits = static_cast<int32_t>(
-        std::min({std::max<int64_t>(at_once / groups, 1), (longest + 127) / 128, int64_t{64}}));
+    // Parts of whole rounds of the workgroup's waves (32 tokens each), as many as run at once.
+    const int64_t splits = std::min({std::max<int64_t>(at_once / groups, 1), (longest + 127) / 128, int64_t{64}});
+    p.chosen.len = static_cast<int32_t>(std::min<int64_t>(round_up((longest + splits - 1) / splits, 128), INT32_MAX - 1023));
+    p.chosen.splits = static_cast<int32_t>((longest + p.chosen.len - 1) / p.chosen.len);
     const int64_t split = p.chosen.splits > 1 ? heads * p.chosen.splits : 0;
     const int64_t lse = round_up(heads * 4, 16);
     p.stats = lse;

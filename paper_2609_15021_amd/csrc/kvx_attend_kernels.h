@@ -75,11 +75,11 @@ struct Shares {
     int32_t *items_of;                // NULL, or: length of a part; [sequence]: first item, parts; [item]: sequence, split
 };
 
-// What each new token chose (kv_page_list), and how its pages are cut into parts, each by its own number of them.
+// What each new token chose (kv_page_list), and how its pages are cut into parts.
 struct Chosen {
     const int32_t *pages, *counts;
     int64_t token_stride, head_stride;  // 0 where the heads share a choice
-    int32_t budget, splits;             // most parts of a row
+    int32_t budget, splits, len;        // pages and parts of a row at most, tokens of a part
     float *sums;                        // [row][query head][splits][D], unscaled
     float *stats;                       // [row][query head][splits][2]: largest score and sum, in powers of 2
 };
@@ -236,22 +236,20 @@ __device__ __forceinline__ bool tile_of_rank(const AttendArgs &a, int rank, int 
     return true;
 }
 
-// Parts of a row that chose `count` pages, and their length; -1 where the number is bad.
-__device__ __forceinline__ int chosen_parts(const AttendArgs &a, const Chosen &chosen, int count, int &len) {
+// Parts of a row that chose `count` pages; -1 where the number is bad.
+__device__ __forceinline__ int chosen_parts(const AttendArgs &a, const Chosen &chosen, int count) {
     if (count < 0 || count > chosen.budget)
         return -1;
-    const int tokens = count * a.pages.BS;
-    len = max(((tokens + chosen.splits - 1) / chosen.splits + 31) & ~31, 128);
-    return max((tokens + len - 1) / len, 1);
+    return max((count * a.pages.BS - 1) / chosen.len + 1, 1);
 }
 
-// Workgroup `item` of a launch over chosen pages: its row as a sequence of its own (seq.n tokens, the row's own the last of
-// them), the row's part, and its list for head h; false if there is none.
-__device__ __forceinline__ bool chosen_of(const AttendArgs &a, const Chosen &chosen, int item, int h, Share &s,
-                                          Sequence &seq, int &count, const int32_t *&list) {
-    const int row = item / chosen.splits, lane = threadIdx.x & 63;
-    s.split = item - row * chosen.splits;
-    s.item0 = item;
+// Row `row` of a launch over chosen pages as a sequence of its own (seq.n tokens, the row's own the last of them), in the
+// sequence s.b, and its parts; false if it has no part s.split.
+__device__ __forceinline__ bool chosen_of(const AttendArgs &a, const Chosen &chosen, int row, Share &s, Sequence &seq,
+                                          int &count) {
+    const int lane = threadIdx.x & 63;
+    count = chosen.counts[row];
+    s.len = chosen.len;
     s.b = row;
     if (a.batch.starts) {
         // The one sequence whose new tokens the row is among.
@@ -266,14 +264,12 @@ __device__ __forceinline__ bool chosen_of(const AttendArgs &a, const Chosen &cho
     if (s.b < 0 || s.b >= a.num_seqs || !sequence(a.batch, s.b, a.pages.err, seq))
         return false;
     const int own = seq.n - seq.nq + (row - seq.q0);
-    count = chosen.counts[row];
-    s.parts = chosen_parts(a, chosen, count, s.len);
+    s.parts = chosen_parts(a, chosen, count);
     if (s.parts < 0 && threadIdx.x == 0)
         report(a.pages.err, KV_ASYNC_BAD_BATCH);
     if (s.split >= s.parts)
         return false;
     seq = Sequence{own + 1, row, 1};
-    list = chosen.pages + row * chosen.token_stride + h * chosen.head_stride;
     return true;
 }
 

@@ -74,8 +74,15 @@ __global__ __launch_bounds__(64 * kWaves, !FP8 && DP > 128 ? 1 : 2) void step_ke
     Sequence seq;
     [[maybe_unused]] int count = 0;                          // LISTED: pages of the list
     [[maybe_unused]] const int32_t *list = nullptr;
+    [[maybe_unused]] int first_entry = 0;
     if constexpr (LISTED) {
-        if (!chosen_of(a, shares, blockIdx.x, h, share, seq, count, list))
+        const int row = blockIdx.x / shares.splits;
+        share.split = blockIdx.x - row * shares.splits;
+        list = shares.pages + row * shares.token_stride + h * shares.head_stride;
+        // (The list's first entry for the wave's tokens is on its way while the row is looked up.)
+        const int64_t first = static_cast<int64_t>(share.split) * shares.len + wave * 32 + (lane & 31);
+        first_entry = list[min(divide(static_cast<int>(min(first, int64_t{INT32_MAX})), pg.by_bs), shares.budget - 1)];
+        if (!chosen_of(a, shares, row, share, seq, count))
             return;
     } else {
         if (!share_of(a, shares, blockIdx.x, false, share) || !sequence(a.batch, share.b, pg.err, seq))
@@ -220,7 +227,7 @@ __global__ __launch_bounds__(64 * kWaves, !FP8 && DP > 128 ? 1 : 2) void step_ke
         int page, next_page = 0, next_block = 0, next_entry = 0;
         [[maybe_unused]] int k_exponent = 0, v_exponent = 0;
         bool shown, next_shown = false;
-        int block = page_at(base, entry_at(base), page, shown);
+        int block = page_at(base, first_entry, page, shown);
         int64_t off = offset_at(base, page, shown, block);
         if (stop - base > kStride) {
             next_block = page_at(base + kStride, entry_at(base + kStride), next_page, next_shown);

@@ -98,9 +98,8 @@ __device__ __forceinline__ Row parts_at(const AttendArgs &a, const Parts &from, 
 
 __device__ __forceinline__ Row parts_at(const AttendArgs &a, const Chosen &from, int, int h, int r, const Sequence &seq) {
     const int i = divide(r, a.by_group), head = h * a.group + r - i * a.group;
-    int len;
     return Row{(static_cast<int64_t>(seq.q0 + i) * a.heads + head) * from.splits, 1,
-               max(chosen_parts(a, from, from.counts[seq.q0 + i], len), 0)};
+               max(chosen_parts(a, from, from.counts[seq.q0 + i]), 0)};
 }
 
 // The parts of a row joined: sum_s 2^(m_s - m) x_s / sum_s 2^(m_s - m) l_s.  4 columns per lane; a workgroup takes one
