@@ -48,11 +48,6 @@ __global__ __launch_bounds__(64 * WAVES) void append_scaled_kernel(const ScaledA
     const int t0 = max(begin, start), old = t0 - start;
     const int rows = static_cast<int>(min(int64_t{s.n}, int64_t{start} + p.BS)) - t0;
     const int block = a.batch.tables[b * a.batch.table_stride + page];
-    if (!in_cache(p, block))
-        return;
-    uint8_t *exponent = scale_at(a.scales, block, kv, h);
-    const int before = old > 0 ? *exponent : 0;
-
     const Turner<DTYPE, PAIRS, LPR> turner(a.turn, tid % LPR, p.D);
     const Turner<DTYPE, kAsIs, LPR> as_is(a.turn, tid % LPR, p.D);
     const bool turn = PAIRS != kAsIs && kv == 0;
@@ -77,6 +72,16 @@ __global__ __launch_bounds__(64 * WAVES) void append_scaled_kernel(const ScaledA
             to_floats<DTYPE>(v.own, y);
         }
     };
+    // (All lanes of a row take part in its norm; rows beyond the last repeat it.  They are on their way while the page is
+    // looked up.)
+    typename Turner<DTYPE, PAIRS, LPR>::Vec v[kHeld];
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k)
+        v[k] = load(min(slot + k * kSlots, rows - 1));
+    if (!in_cache(p, block))
+        return;
+    uint8_t *exponent = scale_at(a.scales, block, kv, h);
+    const int before = old > 0 ? *exponent : 0;
     uint32_t most = 0;  // bits of the largest finite |x|
     const auto count = [&](const float *y) {
 #pragma unroll
@@ -86,18 +91,11 @@ __global__ __launch_bounds__(64 * WAVES) void append_scaled_kernel(const ScaledA
         }
     };
 
-    // (All lanes of a row take part in its norm; rows beyond the last repeat it.)
     float held[kHeld][8];
-    {
-        typename Turner<DTYPE, PAIRS, LPR>::Vec v[kHeld];
 #pragma unroll
-        for (int k = 0; k < kHeld; ++k)
-            v[k] = load(min(slot + k * kSlots, rows - 1));
-#pragma unroll
-        for (int k = 0; k < kHeld; ++k) {
-            finish(v[k], min(slot + k * kSlots, rows - 1), held[k]);
-            count(held[k]);
-        }
+    for (int k = 0; k < kHeld; ++k) {
+        finish(v[k], min(slot + k * kSlots, rows - 1), held[k]);
+        count(held[k]);
     }
     for (int row = slot + kHeld * kSlots; row < rows; row += kSlots) {
         float y[8];
