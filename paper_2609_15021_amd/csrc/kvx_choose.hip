@@ -224,7 +224,7 @@ struct ScoreArgs {
     float scale;
     int32_t BS, group, pad, shift;      // tokens of a page; query heads of a KV head, and the power of two 2^shift that they fill, up to 16
     int32_t page_chunks, tokens;        // of a launch's first dimension; tokens of a workgroup
-    Divisor by_bs, by_chunks;
+    Divisor by_bs, by_chunks, by_subs;
 };
 
 constexpr int kShareTarget = 1536;
@@ -298,7 +298,7 @@ __global__ __launch_bounds__(kThreads, 2) void score_kernel(const ScoreArgs a) {
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {
             const int u = tid + n * kThreads, row = u / GQ % 16, piece = u % GQ;
-            const int tile = min(tile0 + u / (GQ * 16), tiles - 1), of = subs == 1 ? tile : tile / subs;
+            const int tile = min(tile0 + u / (GQ * 16), tiles - 1), of = divide(tile, a.by_subs);
             const int token = min(i0 + of * each + (row >> a.shift), i1 - 1);
             const int head = h * a.group + min((row & (a.pad - 1)) + (tile - of * subs) * 16, a.group - 1);
             const uint8_t *x = a.q.data + int64_t{s.q0 + token} * a.q.token_stride + head * a.q.head_stride;
@@ -411,17 +411,20 @@ __global__ __launch_bounds__(kThreads, 2) void score_kernel(const ScoreArgs a) {
                     }
                 }
             }
-            const int of = subs == 1 ? tile : tile / subs, sub = tile - of * subs;
+            const int of = divide(tile, a.by_subs);
+            if (subs > 1) {  // the largest over a token's tiles
+                const int sub = tile - of * subs;
 #pragma unroll
-            for (int j = 0; j < PG; ++j)
+                for (int j = 0; j < PG; ++j)
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    best[j][r] = subs == 1 || sub == 0 ? x[j][r] : fmaxf(best[j][r], x[j][r]);
-            if (sub + 1 < subs)
-                continue;
+                    for (int r = 0; r < 4; ++r)
+                        x[j][r] = best[j][r] = sub == 0 ? x[j][r] : fmaxf(best[j][r], x[j][r]);
+                if (sub + 1 < subs)
+                    continue;
+            }
 #pragma unroll
             for (int j = 0; j < PG; ++j) {
-                f32x4 y = best[j];
+                f32x4 y = x[j];
                 if constexpr (OUT <= 2) {
                     y[0] = fmaxf(y[0], y[1]);
                     y[1] = fmaxf(y[2], y[3]);
@@ -555,6 +558,7 @@ kv_status score(const kv_cache *bounds, int32_t layer, const kv_batch *batch, co
     while ((1 << a.shift) < a.group && a.shift < 4)
         ++a.shift;
     a.pad = 1 << a.shift;
+    a.by_subs = divisor((a.group + 15) / 16);
     const bool fp8 = o->cache_dtype == KV_DTYPE_E4M3;
     const int64_t some = std::max<int64_t>(most_pages, 1);  // (counts are written where no sequence has a token)
     if (q->dtype == KV_DTYPE_BF16)
