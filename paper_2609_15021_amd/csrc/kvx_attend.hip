@@ -237,9 +237,12 @@ PagesPlan plan_of(const kv_cache *cache, const kv_batch *batch, const kv_page_li
     p.chosen.token_stride = list->token_stride;
     p.chosen.head_stride = list->heads == 1 ? 0 : list->head_stride;
     p.chosen.budget = list->budget;
-    // Parts of whole rounds of the workgroup's waves (32 tokens each), as many as run at once.
-    const int64_t splits = std::min({std::max<int64_t>(at_once / groups, 1), (longest + 127) / 128, int64_t{64}});
-    p.chosen.len = static_cast<int32_t>(std::min<int64_t>(round_up((longest + splits - 1) / splits, 128), INT32_MAX - 1023));
+    // Parts of whole rounds of the workgroup's waves (32 tokens each), as many as run at once.  A row hardly has more tokens
+    // than its sequence may; where it does, which names pages twice, there are up to 4 times the parts, or longer ones.
+    const int64_t likely = std::min(longest, round_up(std::max(batch->max_len, 1), cache->layout.block_size));
+    const int64_t splits = std::min({std::max<int64_t>(at_once / groups, 1), (likely + 127) / 128, int64_t{64}});
+    const int64_t len = splits == 1 ? longest : std::max((likely + splits - 1) / splits, (longest + 4 * splits - 1) / (4 * splits));
+    p.chosen.len = static_cast<int32_t>(std::min<int64_t>(round_up(len, 128), INT32_MAX - 1023));
     p.chosen.splits = static_cast<int32_t>((longest + p.chosen.len - 1) / p.chosen.len);
     const int64_t split = p.chosen.splits > 1 ? heads * p.chosen.splits : 0;
     const int64_t lse = round_up(heads * 4, 16);

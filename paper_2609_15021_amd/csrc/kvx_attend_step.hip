@@ -97,6 +97,8 @@ __device__ __forceinline__ Row parts_at(const AttendArgs &a, const Parts &from, 
 }
 
 __device__ __forceinline__ Row parts_at(const AttendArgs &a, const Chosen &from, int, int h, int r, const Sequence &seq) {
+    if (seq.nq == 0)
+        return Row{0, 0, 0};
     const int i = divide(r, a.by_group), head = h * a.group + r - i * a.group;
     return Row{(static_cast<int64_t>(seq.q0 + i) * a.heads + head) * from.splits, 1,
                max(chosen_parts(a, from, from.counts[seq.q0 + i]), 0)};

@@ -184,6 +184,8 @@ kv_status check_rotate(const kv_cache *cache, int32_t layer, const kv_batch *bat
         st = check_factors(o->cache_dtype, o->k_scale, o->v_scale);
     if (st == KV_OK && o->scales)
         st = check_scales(cache, o->cache_dtype, o->scales);
+    if (st == KV_OK && o->scales)
+        st = check_append_scaled(cache, batch);
     if (st != KV_OK)
         return st;
     if (o->scales && ((o->k_scale != 0.f && o->k_scale != 1.f) || (o->v_scale != 0.f && o->v_scale != 1.f)))
@@ -261,9 +263,8 @@ kv_status rotate(const kv_cache *cache, int32_t layer, const kv_batch *batch, co
     while ((int64_t{1} << a.each_shift) < std::min(wanted, groups_each))
         ++a.each_shift;
     const int64_t side = groups_each >> a.each_shift;  // tokens side by side
-    a.splits = wanted <= groups_each || int64_t{batch->num_queries} * a.rows_each > 16384
-                   ? 1
-                   : static_cast<int32_t>((wanted + groups_each - 1) / groups_each);
+    a.splits = static_cast<int32_t>(std::max<int64_t>(
+        std::min((wanted + groups_each - 1) / groups_each, 1024 / std::max<int64_t>(batch->num_queries, 1)), 1));
     const int64_t behind = std::max<int64_t>(batch->num_queries / (side * 1024), 1);
     const int64_t held = std::min<int64_t>(kAngles / std::max(t.half, 1), groups_each);
     a.tokens = static_cast<int32_t>(std::max<int64_t>(std::min(side * behind, held), 1));
@@ -283,8 +284,9 @@ kv_status rotate(const kv_cache *cache, int32_t layer, const kv_batch *batch, co
                            : launch<KV_DTYPE_F16, false>(a, grid, pairs, stream)));
     if (!o->scales)
         return KV_OK;
-    return launch_append_scaled(a.pages, a.batch, batch->num_seqs, a.k, a.v, k->dtype, scales_of(o->scales), a.turn[1],
-                                pairs, stream);
+    KVX_HIP(launch_append_scaled(a.pages, a.batch, batch->num_seqs, a.k, a.v, k->dtype, scales_of(o->scales), a.turn[1],
+                                 pairs, stream));
+    return KV_OK;
 }
 
 }  // namespace

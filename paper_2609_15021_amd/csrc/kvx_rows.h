@@ -253,9 +253,11 @@ struct Turner {
 // Lanes of a row of D columns, as a power of two.
 inline int lanes_of(int D) { return D > 128 ? 32 : D > 64 ? 16 : 8; }
 
+// What it takes of a batch: refused before anything is enqueued.
+kv_status check_append_scaled(const kv_cache *cache, const kv_batch *batch);
 // kv_append_scaled's kernel, with K normed and rotated where `turn` is given (and pairs are not kAsIs).
-kv_status launch_append_scaled(const Pages &pages, const Batch &batch, int32_t num_seqs, const Rows &k, const Rows &v,
-                               int32_t dtype, const Scales &scales, const Turn &turn, Pairs pairs, hipStream_t stream);
+hipError_t launch_append_scaled(const Pages &pages, const Batch &batch, int32_t num_seqs, const Rows &k, const Rows &v,
+                                int32_t dtype, const Scales &scales, const Turn &turn, Pairs pairs, hipStream_t stream);
 // Checks that kv_append and kv_append_scaled share: the sizes and types of k and v.
 kv_status check_append(const kv_cache *cache, int32_t layer, const kv_batch *batch, const kv_rows *k, const kv_rows *v,
                        int32_t cache_dtype);

@@ -191,6 +191,8 @@ kv_status append_scaled(const kv_cache *cache, int32_t layer, const kv_batch *ba
     if (!scales)
         return fail(KV_EINVAL, "scales must not be NULL");
     st = check_scales(cache, KV_DTYPE_E4M3, scales);
+    if (st == KV_OK)
+        st = check_append_scaled(cache, batch);
     if (st != KV_OK || batch->num_seqs == 0 || batch->num_queries == 0)
         return st;
     st = check_on_current_device(cache);
@@ -199,16 +201,28 @@ kv_status append_scaled(const kv_cache *cache, int32_t layer, const kv_batch *ba
         st = error_word(&err);
     if (st != KV_OK)
         return st;
-    return launch_append_scaled(pages_of(cache, layer, err), batch_of(batch), batch->num_seqs, rows_of(k), rows_of(v),
-                                k->dtype, scales_of(scales), Turn{}, kAsIs, stream);
+    KVX_HIP(launch_append_scaled(pages_of(cache, layer, err), batch_of(batch), batch->num_seqs, rows_of(k), rows_of(v),
+                                 k->dtype, scales_of(scales), Turn{}, kAsIs, stream));
+    return KV_OK;
 }
+
+// Tokens of a sequence that are new at most, and pages that they may lie in.
+int most_new(int max_queries, int num_queries, int max_len) { return std::min({max_queries, num_queries, max_len}); }
+int64_t most_touched(int most, int BS) { return (int64_t{most} + BS - 2) / BS + 1; }
 
 }  // namespace
 
-kv_status launch_append_scaled(const Pages &pages, const Batch &batch, int32_t num_seqs, const Rows &k, const Rows &v,
-                               int32_t dtype, const Scales &scales, const Turn &turn, Pairs pairs, hipStream_t stream) {
-    if (pages.H > 32767)
-        return fail(KV_EUNSUPPORTED, "%d KV heads (at most 32,767)", pages.H);
+kv_status check_append_scaled(const kv_cache *cache, const kv_batch *batch) {
+    if (cache->layout.num_kv_heads > 32767)
+        return fail(KV_EUNSUPPORTED, "%d KV heads (at most 32,767)", cache->layout.num_kv_heads);
+    const int most = most_new(batch->max_queries, batch->num_queries, batch->max_len);
+    if (most_touched(most, cache->layout.block_size) > int64_t{1} << 23)
+        return fail(KV_EUNSUPPORTED, "%d new tokens of a sequence in one call are too many", most);
+    return KV_OK;
+}
+
+hipError_t launch_append_scaled(const Pages &pages, const Batch &batch, int32_t num_seqs, const Rows &k, const Rows &v,
+                                int32_t dtype, const Scales &scales, const Turn &turn, Pairs pairs, hipStream_t stream) {
     ScaledArgs a{};
     a.pages = pages;
     a.batch = batch;
@@ -216,18 +230,14 @@ kv_status launch_append_scaled(const Pages &pages, const Batch &batch, int32_t n
     a.rows[1] = v;
     a.scales = scales;
     a.turn = turn;
-    const int most = std::min({batch.max_queries, batch.num_queries, batch.max_len});
+    const int most = most_new(batch.max_queries, batch.num_queries, batch.max_len);
     if (most == 0)
-        return KV_OK;
-    // Pages that `most` tokens may lie in.
-    const int64_t touched = (int64_t{most} + pages.BS - 2) / pages.BS + 1;
-    if (touched > int64_t{1} << 23)
-        return fail(KV_EUNSUPPORTED, "%d new tokens of a sequence in one call are too many", most);
-    const dim3 grid(static_cast<uint32_t>(touched), static_cast<uint32_t>(num_seqs), static_cast<uint32_t>(2 * pages.H));
+        return hipSuccess;
+    const dim3 grid(static_cast<uint32_t>(most_touched(most, pages.BS)), static_cast<uint32_t>(num_seqs),
+                    static_cast<uint32_t>(2 * pages.H));
     const int rows = std::min(most, pages.BS);
-    KVX_HIP(dtype == KV_DTYPE_BF16 ? launch<KV_DTYPE_BF16>(a, grid, rows, pairs, stream)
-                                   : launch<KV_DTYPE_F16>(a, grid, rows, pairs, stream));
-    return KV_OK;
+    return dtype == KV_DTYPE_BF16 ? launch<KV_DTYPE_BF16>(a, grid, rows, pairs, stream)
+                                  : launch<KV_DTYPE_F16>(a, grid, rows, pairs, stream);
 }
 
 }  // namespace kvx

@@ -470,6 +470,29 @@ def test_attend_chosen_long():
     run_chosen(ref.Case(2, 5, 64, 16, [1500] * 9, [1] * 9, seed=14), 80, 2)
 
 
+def test_attend_chosen_behind_the_last_row():
+    """Sequences without new tokens, the last ones among them, where lists are joined: there is no row to look up."""
+    c = ref.Case(2, 2, 64, 16, [900, 40, 700, 30, 20], [1, 0, 2, 0, 0], seed=18)
+    run_chosen(c, 30, 2)
+    run_chosen(c, 57, 1)
+
+
+def test_attend_chosen_more_than_there_is():
+    """Lists with far more room than a sequence has pages, and lists that name its few pages many times over."""
+    for n in (60, 700):
+        c = ref.Case(1, 2, 64, 16, [n, n - 9], [1, 1], seed=n)
+        run_chosen(c, 400, 1)
+        pages = torch.arange(400, dtype=torch.int32).remainder(3).view(1, 1, 400).expand(2, 1, 400).contiguous()
+        counts = torch.tensor([400, 399], dtype=torch.int32)
+        cache, _, q, _, _, tables, lens, _ = c.device()
+        want = pref.attend_chosen(c, pages, counts)
+        for max_len in (None, n):
+            out, lse = attend.kv_attend(cache, 0, q, tables, lens, pages=pages.to(DEV), counts=counts.to(DEV),
+                                        max_len=max_len)
+            ref.check(lse, want[1], want[3], "lse")
+            ref.check(out, want[0], want[2], "out")
+
+
 def test_attend_all_pages_chosen():
     """All pages, in order, are attention over everything."""
     c = ref.Case(2, 4, 128, 16, [333, 50], [1, 1], seed=15)

@@ -82,6 +82,11 @@ def test_rotate_refusals():
     assert call(fp8, 0, batch, k_scale=0.5, scales=_scales(attend, 2)) == kvx.KV_EINVAL
     for changes in BAD_SCALES:
         assert call(fp8, 0, batch, scales=_scales(attend, 2, **changes)) == kvx.KV_EINVAL, changes
+    # Too many tokens for a launch: refused as a whole, rotated queries too.
+    tiny = _cache(kvx, kvx.make_layout(1, 2, 64, 1, 1, 1))
+    many = _batch(attend, num_queries=1 << 24, max_queries=1 << 24, max_len=1 << 24, table_len=1 << 24,
+                  table_stride=1 << 24, starts=SOME)
+    assert call(tiny, 0, many, scales=_scales(attend, 2)) == kvx.KV_EUNSUPPORTED
     for name in ("q", "out", "k", "v"):
         heads = 8 if name in ("q", "out") else 2
         for changes, status in ((dict(data=None), -1), (dict(data=SOME + 8), -4), (dict(heads=heads + 1), -1),
