@@ -5,6 +5,7 @@
 """
 from __future__ import annotations
 
+import concurrent.futures
 import os
 import subprocess
 import sys
@@ -49,11 +50,12 @@ def _run(cmd, verbose):
 
 def _compile_objs(sources, src_dir, tag, extra, verbose):
     os.makedirs(BUILD_DIR, exist_ok=True)
-    objs = []
-    for src in sources:
-        obj = os.path.join(BUILD_DIR, f"{tag}_{os.path.splitext(src)[0]}.o")
-        _run([HIPCC, *COMMON, *extra, "-x", "hip", "-c", os.path.join(src_dir, src), "-o", obj], verbose)
-        objs.append(obj)
+    objs = [os.path.join(BUILD_DIR, f"{tag}_{os.path.splitext(src)[0]}.o") for src in sources]
+    # A few at a time: each takes up to 1 GB.
+    with concurrent.futures.ThreadPoolExecutor(min(6, os.cpu_count() or 1)) as pool:
+        for done in [pool.submit(_run, [HIPCC, *COMMON, *extra, "-x", "hip", "-c", os.path.join(src_dir, src), "-o", obj],
+                                 verbose) for src, obj in zip(sources, objs)]:
+            done.result()
     return objs
 
 

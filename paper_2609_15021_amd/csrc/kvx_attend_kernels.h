@@ -84,6 +84,9 @@ struct Chosen {
     float *stats;                       // [row][query head][splits][2]: largest score and sum, in powers of 2
 };
 
+// The same, of which every row is one part, and a wave's own.
+struct Alone : Chosen {};
+
 // A sequence's part: `split` of `parts`, `len` tokens each; its first part is item `item0`.
 struct Share {
     int b, split, parts, len, item0;
@@ -261,11 +264,16 @@ __device__ __forceinline__ bool chosen_of(const AttendArgs &a, const Chosen &cho
                 s.b = b0 + __builtin_ctzll(found);
         }
     }
-    if (s.b < 0 || s.b >= a.num_seqs || !sequence(a.batch, s.b, a.pages.err, seq))
+    if (s.b < 0 || s.b >= a.num_seqs)
         return false;
+    if (!sequence(a.batch, s.b, a.pages.err, seq)) {
+        if (lane == 0)
+            report(a.pages.err, KV_ASYNC_BAD_BATCH);
+        return false;
+    }
     const int own = seq.n - seq.nq + (row - seq.q0);
     s.parts = chosen_parts(a, chosen, count);
-    if (s.parts < 0 && threadIdx.x == 0)
+    if (s.parts < 0 && lane == 0)
         report(a.pages.err, KV_ASYNC_BAD_BATCH);
     if (s.split >= s.parts)
         return false;
@@ -364,6 +372,7 @@ hipError_t launch_step_scaled(const AttendArgs &a, const Shares &shares, int max
 hipError_t launch_tail_scaled(const AttendArgs &a, const Parts &parts, int max_queries, hipStream_t stream);
 // Every row over the pages that it chose.
 hipError_t launch_pages(const AttendArgs &a, const Chosen &chosen, hipStream_t stream);
+hipError_t launch_pages(const AttendArgs &a, const Alone &chosen, hipStream_t stream);
 hipError_t launch_join_pages(const AttendArgs &a, const Chosen &chosen, int max_queries, hipStream_t stream);
 // weights_out, from the scores that the step kernel left, or with the scores taken again.
 hipError_t launch_weigh_step(const AttendArgs &a, hipStream_t stream);

@@ -13,13 +13,26 @@ hipError_t launch_step_scaled(const AttendArgs &a, const Shares &shares, int max
                                      : launch_rows<F16, true, true>(a, shares, shares.items, max_rows, stream);
 }
 
-hipError_t launch_pages(const AttendArgs &a, const Chosen &chosen, hipStream_t stream) {
+namespace {
+
+template <class From>
+hipError_t launch_chosen(const AttendArgs &a, const From &chosen, hipStream_t stream) {
     const int items = a.batch.num_queries * chosen.splits;
     if (a.cache_type == KV_DTYPE_E4M3)
         return a.q_type == KV_DTYPE_BF16 ? launch_rows<Bf16, true, true>(a, chosen, items, a.group, stream)
                                          : launch_rows<F16, true, true>(a, chosen, items, a.group, stream);
     return a.q_type == KV_DTYPE_BF16 ? launch_rows<Bf16, false, false>(a, chosen, items, a.group, stream)
                                      : launch_rows<F16, false, false>(a, chosen, items, a.group, stream);
+}
+
+}  // namespace
+
+hipError_t launch_pages(const AttendArgs &a, const Chosen &chosen, hipStream_t stream) {
+    return launch_chosen(a, chosen, stream);
+}
+
+hipError_t launch_pages(const AttendArgs &a, const Alone &chosen, hipStream_t stream) {
+    return launch_chosen(a, chosen, stream);
 }
 
 }  // namespace kvx

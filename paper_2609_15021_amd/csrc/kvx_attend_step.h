@@ -55,11 +55,14 @@ __device__ __forceinline__ int64_t slot_in(const Chosen &chosen, int, int, int64
 // then meet V in bfloat16: float16's range would not hold the products.  They are loaded with K, a lane a token.
 //
 // From: Shares, or Chosen: each new token is a sequence of its own, of the pages that it chose, one after the other.  A
-// page's place in the list says where its tokens are, and which: the list is read a round before the table.
+// page's place in the list says where its tokens are, and which: the list is read a round before the table.  Or Alone:
+// the same where there are rows enough for every wave to have one for itself, and nothing to join: 111 new tokens of each of
+// 17 sequences over one page of 32 (3 heads of 12 rows, D 256) take 30 us instead of 103.
 template <class T, bool FP8, int DP, int NT, bool SCALED, class From>
 __global__ __launch_bounds__(64 * kWaves, !FP8 && DP > 128 ? 1 : 2) void step_kernel(const AttendArgs a,
                                                                                      const From shares) {
-    constexpr bool LISTED = std::is_same_v<From, Chosen>;
+    constexpr bool LISTED = std::is_base_of_v<Chosen, From>, ALONE = std::is_same_v<From, Alone>;
+    constexpr int TEAM = ALONE ? 1 : kWaves;             // waves of a row
     typedef std::conditional_t<SCALED, Bf16, T> W;       // type of the weights
     constexpr int E = FP8 ? 1 : 2;                       // bytes of a cached element
     constexpr int KC = DP * E / 64;                      // 16-byte pieces of a token's K in a lane
@@ -76,11 +79,13 @@ __global__ __launch_bounds__(64 * kWaves, !FP8 && DP > 128 ? 1 : 2) void step_ke
     [[maybe_unused]] const int32_t *list = nullptr;
     [[maybe_unused]] int first_entry = 0;
     if constexpr (LISTED) {
-        const int row = blockIdx.x / shares.splits;
-        share.split = blockIdx.x - row * shares.splits;
+        const int item = ALONE ? blockIdx.x * kWaves + wave : blockIdx.x, row = ALONE ? item : item / shares.splits;
+        if (ALONE && row >= a.batch.num_queries)
+            return;
+        share.split = ALONE ? 0 : item - row * shares.splits;
         list = shares.pages + row * shares.token_stride + h * shares.head_stride;
         // (The list's first entry for the wave's tokens is on its way while the row is looked up.)
-        const int64_t first = static_cast<int64_t>(share.split) * shares.len + wave * 32 + (lane & 31);
+        const int64_t first = static_cast<int64_t>(share.split) * shares.len + (ALONE ? 0 : wave * 32) + (lane & 31);
         first_entry = list[min(divide(static_cast<int>(min(first, int64_t{INT32_MAX})), pg.by_bs), shares.budget - 1)];
         if (!chosen_of(a, shares, row, share, seq, count))
             return;
@@ -221,8 +226,8 @@ __global__ __launch_bounds__(64 * kWaves, !FP8 && DP > 128 ? 1 : 2) void step_ke
             acc[nt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
-    constexpr int kStride = 32 * kWaves;
-    int base = begin + wave * 32;
+    constexpr int kStride = 32 * TEAM;
+    int base = begin + (ALONE ? 0 : wave * 32);
     if (base < stop) {
         int page, next_page = 0, next_block = 0, next_entry = 0;
         [[maybe_unused]] int k_exponent = 0, v_exponent = 0;
@@ -426,82 +431,115 @@ __global__ __launch_bounds__(64 * kWaves, !FP8 && DP > 128 ? 1 : 2) void step_ke
         }
     }
 
-    // Join the waves: every wave's largest score and sum, then wave w collects component w of every tile, which are VE
-    // consecutive columns per lane.
-    __shared__ float stats[kWaves][NT * 16][2];
-    __shared__ float parts[kWaves][kWaves - 1][NT * TILES][64];
+    if constexpr (ALONE) {
+        // (A row's columns are in the lanes of its column, 4 times VE of each 64 in each.)
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-        l[nt] += __shfl_xor(l[nt], 16);
-        l[nt] += __shfl_xor(l[nt], 32);
-        if (g == 0) {
-            stats[wave][nt * 16 + c][0] = m[nt];
-            stats[wave][nt * 16 + c][1] = l[nt];
-        }
-    }
-    __syncthreads();
-    float most[NT], total[NT];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-        const int col = nt * 16 + c;
-        most[nt] = fmaxf(fmaxf(stats[0][col][0], stats[1][col][0]), fmaxf(stats[2][col][0], stats[3][col][0]));
-        total[nt] = 0.f;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w)
-            total[nt] += stats[w][col][1] * __builtin_amdgcn_exp2f(stats[w][col][0] - most[nt]);
-        const float f = __builtin_amdgcn_exp2f(m[nt] - most[nt]);
-#pragma unroll
-        for (int t = 0; t < TILES; ++t) {
-            acc[nt][t] *= f;
-#pragma unroll
-            for (int r = 0; r < kWaves; ++r)
-                if (r != wave)
-                    parts[r][wave - (wave > r)][nt * TILES + t][lane] = acc[nt][t][r];
-        }
-    }
-    __syncthreads();
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-        const int r = row0 + nt * 16 + c;
-        if (r >= rows)
-            continue;
-        const int i = divide(r, a.by_group), head = h * a.group + r - i * a.group, row = seq.q0 + i;
-        const int64_t slot = slot_in(shares, h, r, static_cast<int64_t>(row) * a.heads + head, share.split);
-        const float inv = total[nt] == 0.f ? 0.f : a.v_scale / total[nt];
-#pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            const int d = v * 16 * VE + (g * 4 + wave) * VE;
-            float x[VE];
-#pragma unroll
-            for (int j = 0; j < VE; ++j) {
-                const f32x4 &own = acc[nt][v * VE + j];
-                x[j] = wave == 0 ? own[0] : wave == 1 ? own[1] : wave == 2 ? own[2] : own[3];
-#pragma unroll
-                for (int k = 0; k < kWaves - 1; ++k)
-                    x[j] += parts[wave][k][nt * TILES + v * VE + j][lane];
-            }
-            if (d >= pg.D)
+        for (int nt = 0; nt < NT; ++nt) {
+            l[nt] += __shfl_xor(l[nt], 16);
+            l[nt] += __shfl_xor(l[nt], 32);
+            const int r = row0 + nt * 16 + c;
+            if (r >= rows)
                 continue;
-            if (whole) {
-                uint8_t *to = a.out.data + row * a.out.token_stride + head * a.out.head_stride + 2 * d;
+            const int head = h * a.group + r, row = seq.q0;
+            const float inv = l[nt] == 0.f ? 0.f : a.v_scale / l[nt];
 #pragma unroll
-                for (int j = 0; j < VE; j += 4)
-                    *reinterpret_cast<u32x2 *>(to + 2 * j) = u32x2{T::pack(x[j] * inv, x[j + 1] * inv),
-                                                                    T::pack(x[j + 2] * inv, x[j + 3] * inv)};
-            } else {
-                float *to = shares.sums + slot * pg.D + d;
+            for (int v = 0; v < NV; ++v)
 #pragma unroll
-                for (int j = 0; j < VE; j += 4)
-                    *reinterpret_cast<f32x4 *>(to + j) = f32x4{x[j], x[j + 1], x[j + 2], x[j + 3]};
+                for (int k = 0; k < 4; ++k) {
+                    const int d = v * 16 * VE + (g * 4 + k) * VE;
+                    if (d >= pg.D)
+                        continue;
+                    uint8_t *to = a.out.data + row * a.out.token_stride + head * a.out.head_stride + 2 * d;
+#pragma unroll
+                    for (int j = 0; j < VE; j += 4) {
+                        const f32x4 *x = acc[nt] + v * VE + j;
+                        *reinterpret_cast<u32x2 *>(to + 2 * j) =
+                            u32x2{T::pack(x[0][k] * inv, x[1][k] * inv), T::pack(x[2][k] * inv, x[3][k] * inv)};
+                    }
+                }
+            if (g == 0)
+                a.lse[static_cast<int64_t>(row) * a.heads + head] =
+                    l[nt] == 0.f ? -INFINITY : (m[nt] - W::kShift + __builtin_amdgcn_logf(l[nt])) * kLn2;
+        }
+        return;
+    } else {
+        // Join the waves: every wave's largest score and sum, then wave w collects component w of every tile, which are VE
+        // consecutive columns per lane.
+        __shared__ float stats[kWaves][NT * 16][2];
+        __shared__ float parts[kWaves][kWaves - 1][NT * TILES][64];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            l[nt] += __shfl_xor(l[nt], 16);
+            l[nt] += __shfl_xor(l[nt], 32);
+            if (g == 0) {
+                stats[wave][nt * 16 + c][0] = m[nt];
+                stats[wave][nt * 16 + c][1] = l[nt];
             }
         }
-        if (wave == 0 && g == 0) {
-            if (whole) {
-                a.lse[static_cast<int64_t>(row) * a.heads + head] =
-                    total[nt] == 0.f ? -INFINITY : (most[nt] - W::kShift + __builtin_amdgcn_logf(total[nt])) * kLn2;
-            } else {
-                shares.stats[slot * 2] = most[nt] - W::kShift;
-                shares.stats[slot * 2 + 1] = total[nt];
+        __syncthreads();
+        float most[NT], total[NT];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const int col = nt * 16 + c;
+            most[nt] = fmaxf(fmaxf(stats[0][col][0], stats[1][col][0]), fmaxf(stats[2][col][0], stats[3][col][0]));
+            total[nt] = 0.f;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w)
+                total[nt] += stats[w][col][1] * __builtin_amdgcn_exp2f(stats[w][col][0] - most[nt]);
+            const float f = __builtin_amdgcn_exp2f(m[nt] - most[nt]);
+#pragma unroll
+            for (int t = 0; t < TILES; ++t) {
+                acc[nt][t] *= f;
+#pragma unroll
+                for (int r = 0; r < kWaves; ++r)
+                    if (r != wave)
+                        parts[r][wave - (wave > r)][nt * TILES + t][lane] = acc[nt][t][r];
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const int r = row0 + nt * 16 + c;
+            if (r >= rows)
+                continue;
+            const int i = divide(r, a.by_group), head = h * a.group + r - i * a.group, row = seq.q0 + i;
+            const int64_t slot = slot_in(shares, h, r, static_cast<int64_t>(row) * a.heads + head, share.split);
+            const float inv = total[nt] == 0.f ? 0.f : a.v_scale / total[nt];
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                const int d = v * 16 * VE + (g * 4 + wave) * VE;
+                float x[VE];
+#pragma unroll
+                for (int j = 0; j < VE; ++j) {
+                    const f32x4 &own = acc[nt][v * VE + j];
+                    x[j] = wave == 0 ? own[0] : wave == 1 ? own[1] : wave == 2 ? own[2] : own[3];
+#pragma unroll
+                    for (int k = 0; k < kWaves - 1; ++k)
+                        x[j] += parts[wave][k][nt * TILES + v * VE + j][lane];
+                }
+                if (d >= pg.D)
+                    continue;
+                if (whole) {
+                    uint8_t *to = a.out.data + row * a.out.token_stride + head * a.out.head_stride + 2 * d;
+#pragma unroll
+                    for (int j = 0; j < VE; j += 4)
+                        *reinterpret_cast<u32x2 *>(to + 2 * j) = u32x2{T::pack(x[j] * inv, x[j + 1] * inv),
+                                                                        T::pack(x[j + 2] * inv, x[j + 3] * inv)};
+                } else {
+                    float *to = shares.sums + slot * pg.D + d;
+#pragma unroll
+                    for (int j = 0; j < VE; j += 4)
+                        *reinterpret_cast<f32x4 *>(to + j) = f32x4{x[j], x[j + 1], x[j + 2], x[j + 3]};
+                }
+            }
+            if (wave == 0 && g == 0) {
+                if (whole) {
+                    a.lse[static_cast<int64_t>(row) * a.heads + head] =
+                        total[nt] == 0.f ? -INFINITY : (most[nt] - W::kShift + __builtin_amdgcn_logf(total[nt])) * kLn2;
+                } else {
+                    shares.stats[slot * 2] = most[nt] - W::kShift;
+                    shares.stats[slot * 2 + 1] = total[nt];
+                }
             }
         }
     }
@@ -510,11 +548,12 @@ __global__ __launch_bounds__(64 * kWaves, !FP8 && DP > 128 ? 1 : 2) void step_ke
 template <class T, bool FP8, int DP, int NT, bool SCALED, class From>
 hipError_t launch_tiles(const AttendArgs &a, const From &from, int items, int max_rows, hipStream_t stream) {
     const int tiles = (max_rows + 16 * NT - 1) / (16 * NT);
-    return launch_kernel(step_kernel<T, FP8, DP, NT, SCALED, From>, dim3(items, tiles * a.pages.H), 64 * kWaves, stream, a,
+    const int groups = std::is_same_v<From, Alone> ? (items + kWaves - 1) / kWaves : items;
+    return launch_kernel(step_kernel<T, FP8, DP, NT, SCALED, From>, dim3(groups, tiles * a.pages.H), 64 * kWaves, stream, a,
                          from);
 }
 
-// `items` workgroups for each KV head and tile of up to max_rows rows.
+// `items` workgroups (Alone: waves) for each KV head and tile of up to max_rows rows.
 template <class T, bool FP8, bool SCALED, class From>
 hipError_t launch_rows(const AttendArgs &a, const From &from, int items, int max_rows, hipStream_t stream) {
     const bool two = step_tile_rows(max_rows, a.pages.D) == 32;

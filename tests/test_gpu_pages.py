@@ -470,6 +470,35 @@ def test_attend_chosen_long():
     run_chosen(ref.Case(2, 5, 64, 16, [1500] * 9, [1] * 9, seed=14), 80, 2)
 
 
+@pytest.mark.parametrize("H,G,D,BS,fp8,scaled,dtype", [(2, 3, 128, 16, False, False, BF16), (3, 1, 64, 8, False, False, F16),
+                                                       (1, 2, 256, 16, False, False, BF16), (2, 2, 256, 32, True, True, F16),
+                                                       (2, 17, 80, 7, False, False, BF16), (3, 2, 16, 16, True, False, BF16)])
+def test_attend_chosen_by_many(H, G, D, BS, fp8, scaled, dtype):
+    """So many rows that every wave has one for itself; rows before the first sequence's and behind the last's, bad ones."""
+    if scaled:
+        c = pref.ScaledCase(H, G, D, BS, [600, 0, 511, 3], [520, 0, 511, 1], dtype=dtype, seed=D)
+    else:
+        c = ref.Case(H, G, D, BS, [600, 0, 511, 3], [520, 0, 511, 1], fp8=fp8, dtype=dtype, seed=D)
+    run_chosen(c, 3, H, scaled=scaled)
+    run_chosen(c, 9, 1, dict(window=50, softcap=3.0, slopes=[2.0**-(1 + i % 7) for i in range(H * G)]), scaled=scaled)
+    pages, counts = pref.choose(c, 2, 1, 0)
+    counts[700], counts[701] = 3, -1
+    want = pref.attend_chosen(c, pages, counts.clamp(0, 2))
+    cache, _, q, _, _, tables, lens, starts = c.device()
+    out, lse = torch.full((c.T + 2, H * G, D), 9.0, dtype=dtype, device=DEV), torch.full((c.T + 2, H * G), 9.0, device=DEV)
+    wide = lambda x: torch.cat([x[:1], x, x[:1]])  # noqa: E731
+    scales = dict(scales=c.scales.to(DEV)) if scaled else dict(k_scale=c.k_scale, v_scale=c.v_scale)
+    with fault(attend.KV_ASYNC_BAD_BATCH):
+        attend.kv_attend(cache, 0, wide(q), tables, lens, starts + 1, pages=wide(pages).to(DEV), counts=wide(counts).to(DEV),
+                         out=out, lse=lse, **scales)
+    for row in (0, 701, 702, c.T + 1):
+        assert bool((out[row] == 9).all()) and bool((lse[row] == 9).all())
+    keep = torch.ones(c.T, dtype=torch.bool)
+    keep[700:702] = False
+    ref.check(out[1:-1][keep.to(DEV)], want[0][keep], want[2][keep], "out")
+    ref.check(lse[1:-1][keep.to(DEV)], want[1][keep], want[3][keep], "lse")
+
+
 def test_attend_chosen_behind_the_last_row():
     """Sequences without new tokens, the last ones among them, where lists are joined: there is no row to look up."""
     c = ref.Case(2, 2, 64, 16, [900, 40, 700, 30, 20], [1, 0, 2, 0, 0], seed=18)
