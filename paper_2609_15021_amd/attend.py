@@ -86,6 +86,7 @@ class KvScoreOptions(ctypes.Structure):
 # The same structures as bytes, which take a third of the time to make; a call reads them before it returns.
 _pack_rows = struct.Struct("qqqii").pack
 _pack_batch = struct.Struct("iiiiiiqqqq").pack
+_pack_attend = struct.Struct("iiffffqqqqqii").pack
 _pack_scales = struct.Struct("qqq").pack
 _pack_list = struct.Struct("qqqqii").pack
 _pack_rotate = struct.Struct("iiiiqqqqfffffiP").pack
@@ -296,6 +297,9 @@ def _page_scales(t, cache: Cache, device: int):
 
 def _page_list(pages, counts, tokens: int, device: int):
     """(kv_page_list, its budget)."""
+    found = _tensors.lists(pages, counts, tokens, device)
+    if found is not None:
+        return found
     (_, heads, budget), (token, head, _) = _ints(pages, "pages", 3, device, tokens)
     if counts is None:
         raise ValueError("pages without counts")
@@ -377,25 +381,11 @@ def kv_rotate(cache: Cache, layer: int, q, k, v, tables, lens, starts=None, *, f
     batch = _batch(layout.block_size, device, tables, lens, starts, tokens, max_q, max_len)[0]
     if k_scale != 1.0 or v_scale != 1.0:
         k_scale, v_scale = _factor(k_scale, "k_scale"), _factor(v_scale, "v_scale")
-    rotary = freqs_at = 0
-    if freqs is not None:
-        freqs_at = _tensors.vector(freqs, -1, 64, device)
-        if freqs_at is None:
-            freqs_at = _freqs(freqs, device)
-        rotary = _int32(2 * freqs.shape[0], "twice the number of freqs")
-    positions_at = 0 if positions is None else _dense_ints(positions, "positions", 1, device, tokens)
-    q_weight_at = k_weight_at = weight_dtype = 0
-    if q_weight is not None:
-        q_weight_at, weight_dtype = _norm_weight(q_weight, "q_weight", D, q.dtype, device)
-    if k_weight is not None:
-        k_weight_at, k_dtype = _norm_weight(k_weight, "k_weight", D, q.dtype, device)
-        if weight_dtype and weight_dtype != k_dtype:
-            raise TypeError("q_weight and k_weight have different types")
-        weight_dtype = k_dtype
+    rotary, weight_dtype, *at = _rotate_arguments(q.dtype, D, tokens, device, freqs, positions, q_weight, k_weight)
     by = None if scales is None else KvPageScales(*_page_scales(scales, cache, device))
-    options = _pack_rotate(_cache_dtype(cache, dtype, k), rotary, 1 if interleaved else 0, weight_dtype, freqs_at,
-                           positions_at, q_weight_at, k_weight_at, eps, weight_offset, _factor(magnitude, "magnitude"),
-                           k_scale, v_scale, 0, 0 if by is None else ctypes.addressof(by))
+    options = _pack_rotate(_cache_dtype(cache, dtype, k), rotary, 1 if interleaved else 0, weight_dtype, *at, eps,
+                           weight_offset, _factor(magnitude, "magnitude"), k_scale, v_scale, 0,
+                           0 if by is None else ctypes.addressof(by))
     handle, here = _call_stream(stream)
     if out is None:
         with here:
@@ -410,27 +400,38 @@ def kv_rotate(cache: Cache, layer: int, q, k, v, tables, lens, starts=None, *, f
     return out
 
 
-def _freqs(t, device: int) -> int:
-    if not isinstance(t, torch.Tensor) or t.dtype is not torch.float64 or t.dim() != 1 or not t.is_contiguous():
-        raise TypeError("freqs must be a contiguous 1-dimensional float64 device tensor")
-    if t.requires_grad and torch.is_grad_enabled():
-        _no_gradient("freqs")
-    _on(t, "freqs", device)
-    return t.data_ptr()
-
-
-def _norm_weight(t, name: str, head_dim: int, rows_dtype, device: int):
-    """(address, KV_DTYPE)"""
-    at = _tensors.vector(t, head_dim, KV_DTYPE_F32, device)
-    if at is not None:
-        return at, KV_DTYPE_F32
-    if not isinstance(t, torch.Tensor) or t.shape != (head_dim,) or not t.is_contiguous() or \
-            (t.dtype is not torch.float32 and t.dtype is not rows_dtype):
-        raise TypeError(f"{name} must be a contiguous [{head_dim}] device tensor of float32 or {rows_dtype}")
-    if t.requires_grad and torch.is_grad_enabled():
-        _no_gradient(name)
-    _on(t, name, device)
-    return t.data_ptr(), KV_DTYPE_F32 if t.dtype is torch.float32 else _DTYPES[t.dtype]
+def _rotate_arguments(rows_dtype, head_dim: int, tokens: int, device: int, freqs, positions, q_weight, k_weight):
+    """(rotary_dim, weight_dtype, freqs, positions, q_weight, k_weight) of kv_rotate_options."""
+    found = _tensors.rotation(_ROW_TYPES[rows_dtype], head_dim, tokens, device, freqs, positions, q_weight, k_weight)
+    if found is not None:
+        return found
+    rotary = freqs_at = weight_dtype = 0
+    if freqs is not None:
+        if not isinstance(freqs, torch.Tensor) or freqs.dtype is not torch.float64 or freqs.dim() != 1 or \
+                not freqs.is_contiguous():
+            raise TypeError("freqs must be a contiguous 1-dimensional float64 device tensor")
+        if freqs.requires_grad and torch.is_grad_enabled():
+            _no_gradient("freqs")
+        _on(freqs, "freqs", device)
+        rotary, freqs_at = _int32(2 * freqs.shape[0], "twice the number of freqs"), freqs.data_ptr()
+    positions_at = 0 if positions is None else _dense_ints(positions, "positions", 1, device, tokens)
+    at = []
+    for weight, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+        if weight is None:
+            at.append(0)
+            continue
+        if not isinstance(weight, torch.Tensor) or weight.shape != (head_dim,) or not weight.is_contiguous() or \
+                (weight.dtype is not torch.float32 and weight.dtype is not rows_dtype):
+            raise TypeError(f"{name} must be a contiguous [{head_dim}] device tensor of float32 or {rows_dtype}")
+        if weight.requires_grad and torch.is_grad_enabled():
+            _no_gradient(name)
+        _on(weight, name, device)
+        of = KV_DTYPE_F32 if weight.dtype is torch.float32 else _DTYPES[weight.dtype]
+        if weight_dtype not in (0, of):
+            raise TypeError("q_weight and k_weight have different types")
+        weight_dtype = of
+        at.append(weight.data_ptr())
+    return rotary, weight_dtype, freqs_at, positions_at, *at
 
 
 def _new_rows(like, shape):
@@ -487,9 +488,9 @@ def kv_attend(cache: Cache, layer: int, q, tables, lens, starts=None, *, max_q=N
     elif prior is not None:
         raise ValueError("prior without weights")
     window = _int32(window, "window") if window else 0
-    options = KvAttendOptions(_cache_dtype(cache, dtype, q), window, 0.0 if scale is None else _factor(scale, "scale"),
-                              _factor(softcap, "softcap") if softcap else 0.0, k_scale, v_scale, slopes_at, prior_at,
-                              weights_at, weights_seq, weights_head, 1 if full_weights else 0)
+    options = (_cache_dtype(cache, dtype, q), window, 0.0 if scale is None else _factor(scale, "scale"),
+               _factor(softcap, "softcap") if softcap else 0.0, k_scale, v_scale, slopes_at, prior_at, weights_at,
+               weights_seq, weights_head, 1 if full_weights else 0, 0)
     by = chosen = None
     budget = -1
     if scales is not None:
@@ -506,10 +507,13 @@ def kv_attend(cache: Cache, layer: int, q, tables, lens, starts=None, *, max_q=N
     key = (layout.num_kv_heads, layout.head_dim, layout.elem_bytes, layout.block_size, B, max_q, tokens, most, window,
            weights is None, q_heads, budget)
     need = _attend_bytes.get(key)
-    at, batch = ctypes.byref(cache.struct), ctypes.byref(KvBatch.from_buffer_copy(batch))
-    options = ctypes.byref(options)
+    at, plain = ctypes.byref(cache.struct), by is None and chosen is None
+    if plain:
+        batch, options = ctypes.byref(KvBatch.from_buffer_copy(batch)), ctypes.byref(KvAttendOptions(*options))
+    else:
+        options = _pack_attend(*options)
     if need is None:
-        need = _lib.kv_attend_workspace(at, batch, options, qr) if by is None and chosen is None else \
+        need = _lib.kv_attend_workspace(at, batch, options, qr) if plain else \
             _lib.kv_attend_pages_workspace(at, batch, options, by, chosen, qr)
         if need < 0:
             _raise(need)
@@ -530,7 +534,7 @@ def kv_attend(cache: Cache, layer: int, q, tables, lens, starts=None, *, max_q=N
         if need:
             space, workspace = _tensors.empty(q, 3, need)
     layer = _int32(layer, "layer")
-    if by is None and chosen is None:
+    if plain:
         _raise(_lib.kv_attend(at, layer, batch, options, qr, outr, lse_at, workspace, need, handle))
     else:
         _raise(_lib.kv_attend_pages(at, layer, batch, options, by, chosen, qr, outr, lse_at, workspace, need, handle))

@@ -147,24 +147,72 @@ PyObject *scales(PyObject *, PyObject *const *args, Py_ssize_t count) {
                          static_cast<long long>(t->stride(0)), static_cast<long long>(t->stride(1)));
 }
 
-// vector(tensor, elements (-1: any), type, device): the address of a contiguous one of one dimension; type: KV_DTYPE_*, or
-// 64 for float64
-PyObject *vector(PyObject *, PyObject *const *args, Py_ssize_t count) {
+// lists(pages, counts, tokens, device): (kv_page_list, budget)
+PyObject *lists(PyObject *, PyObject *const *args, Py_ssize_t count) {
     if (count != 4)
         Py_RETURN_NONE;
-    const int64_t elements = PyLong_AsLongLong(args[1]);
-    const long type = PyLong_AsLong(args[2]);
-    const at::Tensor *t = tensor_of(args[0], static_cast<int>(PyLong_AsLong(args[3])));
+    const int64_t tokens = PyLong_AsLongLong(args[2]);
+    const int device = static_cast<int>(PyLong_AsLong(args[3]));
     if (PyErr_Occurred())
         return nullptr;
-    const at::ScalarType is = type == 64                ? at::kDouble
-                              : type == KV_DTYPE_F32    ? at::kFloat
-                              : type == KV_DTYPE_BF16   ? at::kBFloat16
-                                                        : at::kHalf;
-    if (!t || t->scalar_type() != is || t->dim() != 1 || (elements >= 0 && t->size(0) != elements) ||
-        !t->is_contiguous())
+    const at::Tensor *pages = ints_of(args[0], 3, device, tokens), *counts = ints_of(args[1], 1, device, tokens);
+    if (!pages || !counts || !counts->is_contiguous() || pages->size(1) > INT32_MAX || pages->size(2) > INT32_MAX)
         Py_RETURN_NONE;
-    return PyLong_FromUnsignedLongLong(reinterpret_cast<uintptr_t>(t->data_ptr()));
+    kv_page_list x{};
+    x.pages = static_cast<const int32_t *>(pages->data_ptr());
+    x.counts = static_cast<const int32_t *>(counts->data_ptr());
+    x.token_stride = pages->stride(0);
+    x.head_stride = pages->stride(1);
+    x.heads = static_cast<int32_t>(pages->size(1));
+    x.budget = static_cast<int32_t>(pages->size(2));
+    return Py_BuildValue("(NL)", bytes_of(&x, sizeof(x)), static_cast<long long>(pages->size(2)));
+}
+
+// A contiguous tensor of one dimension and so many elements (any, if negative), or NULL.
+const at::Tensor *vector_of(PyObject *x, int64_t elements, int device) {
+    const at::Tensor *t = tensor_of(x, device);
+    return t && t->dim() == 1 && (elements < 0 || t->size(0) == elements) && t->is_contiguous() ? t : nullptr;
+}
+
+// rotation(row type, head_dim, tokens, device, freqs, positions, q_weight, k_weight): (rotary_dim, weights' type, freqs,
+// positions, q_weight, k_weight), as kv_rotate_options has them; None for those that are not given
+PyObject *rotation(PyObject *, PyObject *const *args, Py_ssize_t count) {
+    if (count != 8)
+        Py_RETURN_NONE;
+    const long type = PyLong_AsLong(args[0]);
+    const int64_t head_dim = PyLong_AsLongLong(args[1]), tokens = PyLong_AsLongLong(args[2]);
+    const int device = static_cast<int>(PyLong_AsLong(args[3]));
+    if (PyErr_Occurred())
+        return nullptr;
+    int64_t rotary = 0;
+    int of_weights = 0;
+    const void *at[4] = {};
+    if (args[4] != Py_None) {
+        const at::Tensor *freqs = vector_of(args[4], -1, device);
+        if (!freqs || freqs->scalar_type() != at::kDouble || freqs->size(0) > head_dim)
+            Py_RETURN_NONE;
+        rotary = 2 * freqs->size(0);
+        at[0] = freqs->data_ptr();
+    }
+    if (args[5] != Py_None) {
+        const at::Tensor *positions = vector_of(args[5], tokens, device);
+        if (!positions || positions->scalar_type() != at::kInt)
+            Py_RETURN_NONE;
+        at[1] = positions->data_ptr();
+    }
+    for (int i = 0; i < 2; ++i) {
+        if (args[6 + i] == Py_None)
+            continue;
+        const at::Tensor *weight = vector_of(args[6 + i], head_dim, device);
+        const int is = !weight ? 0 : weight->scalar_type() == at::kFloat ? KV_DTYPE_F32 : row_type(*weight);
+        if (!is || (is != KV_DTYPE_F32 && is != type) || (of_weights && of_weights != is))
+            Py_RETURN_NONE;
+        of_weights = is;
+        at[2 + i] = weight->data_ptr();
+    }
+    const auto address = [&](int i) { return static_cast<unsigned long long>(reinterpret_cast<uintptr_t>(at[i])); };
+    return Py_BuildValue("(LiKKKK)", static_cast<long long>(rotary), of_weights, address(0), address(1), address(2),
+                         address(3));
 }
 
 PyObject *failed(const std::exception &e) {
@@ -215,7 +263,8 @@ PyMethodDef methods[] = {
     {"ints", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(guarded<ints>)), METH_FASTCALL, nullptr},
     {"batch", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(guarded<batch>)), METH_FASTCALL, nullptr},
     {"scales", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(guarded<scales>)), METH_FASTCALL, nullptr},
-    {"vector", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(guarded<vector>)), METH_FASTCALL, nullptr},
+    {"lists", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(guarded<lists>)), METH_FASTCALL, nullptr},
+    {"rotation", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(guarded<rotation>)), METH_FASTCALL, nullptr},
     {"empty", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(empty)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 

@@ -192,6 +192,54 @@ def test_bounds_and_score_refusals():
     assert score(low_high, 0, _batch(attend, **EMPTY)) == kvx.KV_OK
 
 
+@pytest.mark.parametrize("name,pack", [("KvRows", "rows"), ("KvBatch", "batch"), ("KvAttendOptions", "attend"),
+                                       ("KvPageScales", "scales"), ("KvPageList", "list"), ("KvRotateOptions", "rotate"),
+                                       ("KvScoreOptions", "score")])
+def test_structures_as_bytes(name, pack):
+    """What the binding packs is the structure, field by field."""
+    from paper_2609_15021_amd import attend
+    kind = getattr(attend, name)
+    numbers = [i + 1 for i in range(len(kind._fields_))]
+    data = getattr(attend, f"_pack_{pack}")(*numbers)
+    assert len(data) == ctypes.sizeof(kind)
+    x = kind.from_buffer_copy(data)
+    for number, (field, kind_of) in zip(numbers, kind._fields_):
+        got = getattr(x, field)
+        assert (ctypes.cast(got, ctypes.c_void_p).value if isinstance(got, ctypes._Pointer) else got) == number, field
+
+
+def test_tensors_answer_as_the_binding_does(monkeypatch):
+    """The compiled module and the checks in Python give the same structures, for tensors of every kind of stride."""
+    from paper_2609_15021_amd import _tensors, attend, kvx
+    lay = kvx.make_layout(1, 2, 64, 1, 16, 16)
+
+    class Fake:
+        layout, struct = lay, _cache(kvx, lay)
+
+    wide = torch.zeros(3, 8, 64, dtype=torch.bfloat16)
+    meta = torch.zeros(4, 9, dtype=torch.int32)
+    scales, counts = torch.zeros(70, 2, 16, dtype=torch.uint8)[..., :2], torch.zeros(3, dtype=torch.int32)
+    freqs, weight = torch.ones(32, dtype=torch.float64), torch.ones(64)
+    calls = [lambda: attend._rows(wide, "x", 64, -1), lambda: attend._rows(wide[:, 2:5], "x", 64, -1),
+             lambda: attend._rows(wide[:1].half(), "x", 64, -1), lambda: attend._rows(wide.transpose(0, 1), "x", 64, -1),
+             lambda: attend._batch(16, -1, meta[:3], counts, None, 3, None, None),
+             lambda: attend._batch(16, -1, meta[:3, :5], counts, meta[0, :4], 7, 5, 33),
+             lambda: attend._batch(16, -1, meta[:3], counts, meta[0, :4], 7, 2**70, -2**70),
+             lambda: attend._batch(2**20, -1, torch.zeros(3, 4000, dtype=torch.int32), counts, None, 3, 9, 2**40),
+             lambda: attend._page_scales(scales, Fake, -1),
+             lambda: attend._page_scales(scales.view(torch.float8_e8m0fnu), Fake, -1),
+             lambda: attend._page_list(meta[:3].view(3, 3, 3), counts, 3, -1),
+             lambda: attend._dense_ints(counts, "x", 1, -1, 3),
+             lambda: attend._rotate_arguments(torch.bfloat16, 64, 3, -1, freqs, counts, weight, weight),
+             lambda: attend._rotate_arguments(torch.bfloat16, 64, 3, -1, None, None, weight.bfloat16(), None)]
+    fast = [call() for call in calls]
+    for name in ("rows", "batch", "scales", "lists", "ints", "rotation"):
+        monkeypatch.setattr(_tensors, name, lambda *args: None)
+    for a, call in zip(fast, calls):
+        b = call()
+        assert (tuple(a) if isinstance(a, (tuple, list)) else a) == (tuple(b) if isinstance(b, (tuple, list)) else b)
+
+
 def test_exponents():
     """The smallest power of two that brings a page to 448: on both sides of every border."""
     for e in (1, 2, 90, 127, 200):
