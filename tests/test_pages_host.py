@@ -220,18 +220,20 @@ def test_tensors_answer_as_the_binding_does(monkeypatch):
     meta = torch.zeros(4, 9, dtype=torch.int32)
     scales, counts = torch.zeros(70, 2, 16, dtype=torch.uint8)[..., :2], torch.zeros(3, dtype=torch.int32)
     freqs, weight = torch.ones(32, dtype=torch.float64), torch.ones(64)
+    half, short = wide[:1].half(), weight.bfloat16()
+    pages = torch.zeros(3, 4000, dtype=torch.int32)
     calls = [lambda: attend._rows(wide, "x", 64, -1), lambda: attend._rows(wide[:, 2:5], "x", 64, -1),
-             lambda: attend._rows(wide[:1].half(), "x", 64, -1), lambda: attend._rows(wide.transpose(0, 1), "x", 64, -1),
+             lambda: attend._rows(half, "x", 64, -1), lambda: attend._rows(wide.transpose(0, 1), "x", 64, -1),
              lambda: attend._batch(16, -1, meta[:3], counts, None, 3, None, None),
              lambda: attend._batch(16, -1, meta[:3, :5], counts, meta[0, :4], 7, 5, 33),
              lambda: attend._batch(16, -1, meta[:3], counts, meta[0, :4], 7, 2**70, -2**70),
-             lambda: attend._batch(2**20, -1, torch.zeros(3, 4000, dtype=torch.int32), counts, None, 3, 9, 2**40),
+             lambda: attend._batch(2**20, -1, pages, counts, None, 3, 9, 2**40),
              lambda: attend._page_scales(scales, Fake, -1),
              lambda: attend._page_scales(scales.view(torch.float8_e8m0fnu), Fake, -1),
              lambda: attend._page_list(meta[:3].view(3, 3, 3), counts, 3, -1),
              lambda: attend._dense_ints(counts, "x", 1, -1, 3),
              lambda: attend._rotate_arguments(torch.bfloat16, 64, 3, -1, freqs, counts, weight, weight),
-             lambda: attend._rotate_arguments(torch.bfloat16, 64, 3, -1, None, None, weight.bfloat16(), None)]
+             lambda: attend._rotate_arguments(torch.bfloat16, 64, 3, -1, None, None, short, None)]
     fast = [call() for call in calls]
     for name in ("rows", "batch", "scales", "lists", "ints", "rotation"):
         monkeypatch.setattr(_tensors, name, lambda *args: None)
