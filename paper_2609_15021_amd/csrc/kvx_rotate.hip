@@ -132,7 +132,7 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateArgs a) {
                 break;
             if (of_k < 0) {
                 uint8_t *to = a.out.data + int64_t{row} * a.out.token_stride + r * a.out.head_stride;
-                *reinterpret_cast<vec16 *>(to + 2 * lane.d0) = from_floats<DTYPE>(y[k]);
+                __builtin_nontemporal_store(from_floats<DTYPE>(y[k]), reinterpret_cast<vec16 *>(to + 2 * lane.d0));
                 continue;
             }
             if (place < 0)
@@ -149,7 +149,8 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateArgs a) {
                 *reinterpret_cast<vec8 *>(to + lane.d0) = to_e4m3(y[k]);
             } else {
                 // (V's bytes as they are.)
-                *reinterpret_cast<vec16 *>(to + 2 * lane.d0) = of_v < 0 ? from_floats<DTYPE>(y[k]) : vecs.of[k].own;
+                __builtin_nontemporal_store(of_v < 0 ? from_floats<DTYPE>(y[k]) : vecs.of[k].own,
+                                            reinterpret_cast<vec16 *>(to + 2 * lane.d0));
             }
         }
     }
