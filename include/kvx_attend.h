@@ -22,7 +22,8 @@
  * allocates nothing, never blocks the host, keeps nothing between calls and may be captured into a graph.  All reads
  * and writes of a call follow earlier work on `stream` and precede later work there; calls on different streams are
  * ordered by the caller where they share a written buffer (a cache, an output or a workspace).  DEVICE arrays are read
- * and written until the call's work has completed there.  Outputs overlap neither inputs nor the workspace, unless said.
+ * and written until the call's work has completed there.  Outputs overlap neither inputs nor the workspace, unless
+ * said.
  * Results do not depend on the order in which workgroups run: the same call gives the same bits.
  *
  * ---------------------------------------------------------------------------
@@ -69,19 +70,20 @@ typedef struct kv_rows {
     int32_t dtype;        /* KV_DTYPE_BF16 or KV_DTYPE_F16 */
 } kv_rows;
 
-/* The scales of an E4M3 cache's pages: a value is the stored e4m3 times 2^(e - 127), e the byte of its block, K (0) or V
- * (1), and head, at data + block*block_stride + kv*kv_stride + head; e is 1 to 254.  (Where strides are padded to 16 bytes,
- * the bytes of a layer are a kv_cache of their own with one token a block, which kv_store and kv_load move by the same
- * block tables: num_kv_heads 1, head_dim the padded heads, elem_bytes 1, block_size 1, chunk_tokens C / BS.) */
+/* The scales of an E4M3 cache's pages: a value is the stored e4m3 times 2^(e - 127), e the byte of its block, K (0) or
+ * V (1), and head, at data + block*block_stride + kv*kv_stride + head; e is 1 to 254.  (Where kv_stride is padded to 16
+ * bytes and block_stride is twice that, a layer's bytes are a kv_cache of their own with one token a block, which
+ * kv_store and kv_load move by the same block tables, n / BS tokens rounded up: num_kv_heads 1, head_dim the padded
+ * heads, elem_bytes 1, block_size 1, chunk_tokens C / BS.) */
 typedef struct kv_page_scales {
     uint8_t *data;         /* DEVICE */
     int64_t block_stride;  /* bytes, >= kv_stride + heads */
     int64_t kv_stride;     /* bytes, >= heads */
 } kv_page_scales;
 
-/* The pages that each new token chose, for each KV head (heads == 1: the same for all): of row r and head h, with room for budget, the first
- * counts[r] numbers at pages + r*token_stride + h*head_stride, each a place in its sequence's block table.  As kv_keep
- * leaves them; in any order.  A page that is named twice takes part twice. */
+/* The pages that each new token chose, for each KV head (heads == 1: the same for all): of row r and head h the first
+ * counts[r] of the `budget` numbers at pages + r*token_stride + h*head_stride, each a place in its sequence's block
+ * table, as kv_keep leaves them, but in any order.  A page that is named twice takes part twice. */
 typedef struct kv_page_list {
     const int32_t *pages;  /* DEVICE */
     const int32_t *counts; /* DEVICE int32[num_queries] */
@@ -105,8 +107,8 @@ typedef struct kv_batch {
 } kv_batch;
 
 /* Scores, in this order: s = scale * k_scale * (q . k); softcap > 0: s = softcap * tanh(s / softcap); slopes: s -=
- * slopes[query head] * (p - t), with p the query's own token and t the cached one.  Token t takes part where t <= p and,
- * with window > 0, p - t < window.  Zero-initialised fields take the documented defaults. */
+ * slopes[query head] * (p - t), with p the query's own token and t the cached one.  Token t takes part where t <= p
+ * and, with window > 0, p - t < window.  Zero-initialised fields take the documented defaults. */
 typedef struct kv_attend_options {
     int32_t cache_dtype;      /* KV_DTYPE_*: what the cache's elements are (required; 1 byte: E4M3) */
     int32_t window;           /* 0 = none */
@@ -137,13 +139,14 @@ KV_API kv_status kv_append(const kv_cache *cache, int32_t layer, const kv_batch 
                            const kv_rows *v, int32_t cache_dtype, float k_scale, float v_scale, void *stream);
 
 /*
- * kv_append_scaled -- kv_append into an E4M3 cache whose pages have scales.  Of each page that a new token lies in, K and
- * V, and head, the scale is the smallest power of two with |x| <= 448 * scale for every finite x of the call's new rows
- * in it, and not smaller than it was where the page holds older tokens (of a page whose slot 0 is a new token's nothing
- * is older).  Where it grows, the older rows are rounded to it: e4m3(stored * old scale / new scale), which is exact but for
- * what leaves e4m3's normal numbers.  x is stored as e4m3(clamp(x / scale, -448, 448)), rounded to nearest even; NaN
- * stays NaN.  Every other byte of the cache and the scales is untouched.  Errors and preconditions as kv_append;
- * KV_EINVAL also for strides of scales that overlap.
+ * kv_append_scaled -- kv_append into an E4M3 cache whose pages have scales.  Of each page that a new token lies in, K
+ * and V, and head, the scale is the smallest power of two with |x| <= 448 * scale for every finite x of the call's new
+ * rows in it, and not smaller than it was where the page holds older tokens (of a page whose slot 0 is a new token's
+ * nothing is older).  Where it grows, the older rows are rounded to it: e4m3(stored * old scale / new scale), which is
+ * exact but for what leaves e4m3's normal numbers.  x is stored as e4m3(clamp(x / scale, -448, 448)), rounded to
+ * nearest even; NaN stays NaN.  Every other byte of the cache and of the scales is untouched.  kv_compact does not move
+ * scales.
+ * Errors and preconditions as kv_append; KV_EINVAL also for strides of scales that overlap.
  */
 KV_API kv_status kv_append_scaled(const kv_cache *cache, int32_t layer, const kv_batch *batch, const kv_rows *k,
                                   const kv_rows *v, const kv_page_scales *scales, void *stream);
@@ -163,7 +166,7 @@ typedef struct kv_rotate_options {
     float magnitude;           /* factor of the rotated columns; 0 = 1 */
     float k_scale, v_scale;    /* 0 = 1; as in kv_append */
     int32_t reserved;          /* must be 0 */
-    const kv_page_scales *scales;  /* HOST, or NULL; E4M3 caches: as in kv_append_scaled, then k_scale and v_scale are 1 */
+    const kv_page_scales *scales;  /* HOST, or NULL; E4M3 caches: kv_append_scaled's; k_scale and v_scale are then 1 */
 } kv_rotate_options;
 
 /*
@@ -171,11 +174,11 @@ typedef struct kv_rotate_options {
  *   y_d = x_d / sqrt(mean of x^2 + eps) * (weight_offset + weight_d)  (or x_d, without weights), and for each pair (a, b)
  *   of the first rotary_dim columns, with t = position * freqs[i]: (a cos t - b sin t, b cos t + a sin t) * magnitude.
  * A row is rounded once, at the end; sums are held in 32 bits, positions times frequencies in 64.  q's rows go to `out`
- * (same type, heads; may be q itself), k's rotated rows and v's as they are into layer `layer` of the cache, as kv_append (with
- * scales: kv_append_scaled) puts them there.  Rows of out whose token has no place (before token 0) are rotated by its
- * place or position all the same; rows of no sequence are left as they were.
- * Errors as kv_append; KV_EINVAL also for a rotary_dim that is odd or outside [0, D], a NULL freqs with one, and negative or
- * not finite numbers.
+ * (same type and heads; may be q itself), k's rotated rows and v's as they are into layer `layer` of the cache, as
+ * kv_append, or with scales kv_append_scaled, puts them there.  A row whose token has no place (before token 0) is
+ * rotated by its place or position all the same; rows of no sequence are left as they were.
+ * Errors and preconditions as kv_append; KV_EINVAL also for a rotary_dim that is odd or outside [0, D], a NULL freqs
+ * with one, and numbers that are negative or not finite.
  */
 KV_API kv_status kv_rotate(const kv_cache *cache, int32_t layer, const kv_batch *batch, const kv_rotate_options *options,
                            const kv_rows *q, const kv_rows *out, const kv_rows *k, const kv_rows *v, void *stream);
@@ -185,18 +188,19 @@ KV_API kv_status kv_rotate(const kv_cache *cache, int32_t layer, const kv_batch 
  * of the sum of exp(s), for every new row; query head h reads KV head h / (q->heads / H).  A row that sees no token
  * gets 0 and -infinity.  Sums, largest scores and lse are held in 32 bits.  The weights exp(s) meet V as two numbers of
  * q's type (the rounded weight and what it leaves) for sequences of up to 64 rows (new tokens times query heads) per KV
- * head, so that only the output's rounding shows.  For longer ones they are one number, rounded to nearest (off by up to
- * half a step of that type each), unless full_weights asks for two there as well.  What slots behind a sequence's last
- * token hold does not matter, but its own tokens' V are taken to be finite: 0 times an infinity of a token that a row
- * does not see reaches that row.  K of a token reaches the rows that see it and no others; where it is not finite, they
- * may become NaN.
+ * head, so that only the output's rounding shows.  For longer ones they are one number, rounded to nearest (off by up
+ * to half a step of that type each), unless full_weights asks for two there as well.  What slots behind a sequence's
+ * last token hold does not matter, but its own tokens' V are taken to be finite: 0 times an infinity of a token that a
+ * row does not see reaches that row.  K of a token reaches the rows that see it and no others; where it is not finite,
+ * they may become NaN.
  *   q, out:    [num_queries][query heads][D], same type; the cache's, or either 2-byte type for E4M3; rows of out do not
  *              overlap;
  *   lse:       DEVICE float[num_queries][query heads], or NULL;
  *   workspace: DEVICE, kv_attend_workspace's bytes (16-byte aligned; may be NULL for 0 bytes), the call's own until its
  *              work has completed: calls that may overlap, and graphs whose replays may, need one each.
- * Errors as kv_append; KV_EINVAL for a workspace that is too small; KV_EUNSUPPORTED also for more than 16,383 query heads,
- * scales whose product (or its quotient by softcap) leaves 1e-36 .. 1e36, and bounds of more rows than one launch takes.
+ * Errors as kv_append; KV_EINVAL for a workspace that is too small; KV_EUNSUPPORTED also for more than 16,383 query
+ * heads, scales whose product (or its quotient by softcap) leaves 1e-36 .. 1e36, and bounds of more rows than one
+ * launch takes.
  */
 KV_API kv_status kv_attend(const kv_cache *cache, int32_t layer, const kv_batch *batch, const kv_attend_options *options,
                            const kv_rows *q, const kv_rows *out, float *lse, void *workspace, int64_t workspace_bytes,
@@ -208,14 +212,15 @@ KV_API int64_t kv_attend_workspace(const kv_cache *cache, const kv_batch *batch,
                                    const kv_rows *q);
 
 /*
- * kv_attend_pages -- kv_attend where an E4M3 cache's pages have scales (scales; options' k_scale and v_scale are then 1), or
- * where each new token attends over the pages that it chose alone (list), or both; one of them must be given.  Token t of a
- * chosen page takes part where t <= p and, with window > 0, p - t < window, and slopes count in p - t, as in kv_attend; a row that
- * chose nothing it sees gets 0 and -infinity.  With scales, and with a list in every E4M3 cache, the weights exp(s) times
- * V's scale meet the stored e4m3 as two numbers of bfloat16, or in sequences of more than 64 rows per KV head without a list, for
- * bfloat16 rows, and unless full_weights asks for two, as one.  With a list a call reads each row's pages for itself.
- * weights_in and weights_out must be NULL.  Errors as kv_attend; KV_EINVAL also for a list that contradicts the cache, and
- * KV_EUNSUPPORTED for weights_out, or more than 2^31 - 1024 tokens in `budget` pages.
+ * kv_attend_pages -- kv_attend where an E4M3 cache's pages have scales (scales; options' k_scale and v_scale are then
+ * 1), where each new token attends over the pages alone that it chose (list), or both; one of them must be given.
+ * Token t of a chosen page takes part where t <= p and, with window > 0, p - t < window, and slopes count in p - t, as
+ * in kv_attend; a row that chose nothing that it sees gets 0 and -infinity.  With a list a row's weights always meet V
+ * as two numbers, a V that is not finite reaches no row that does not see it, and each row reads its pages for itself.
+ * With scales, and with a list in any E4M3 cache, the weights times V's scale are numbers of bfloat16; of float16 rows
+ * they are always two. weights_in and weights_out must be NULL.  Errors as kv_attend; KV_EINVAL also for a list that
+ * contradicts the cache, KV_EUNSUPPORTED for weights_out, more than 2^31 - 1024 tokens in `budget` pages, and more rows
+ * than one launch takes.
  */
 KV_API kv_status kv_attend_pages(const kv_cache *cache, int32_t layer, const kv_batch *batch,
                                  const kv_attend_options *options, const kv_page_scales *scales,
@@ -227,12 +232,13 @@ KV_API int64_t kv_attend_pages_workspace(const kv_cache *cache, const kv_batch *
                                          const kv_page_scales *scales, const kv_page_list *list, const kv_rows *q);
 
 /*
- * kv_bounds -- of each page of layer `layer` that a new token lies in, and each KV head, the lowest and the highest stored K
- * of every column over the page's tokens t < lens[b], new and older ones.  They go where `bounds`, a kv_cache of the same
- * heads, head_dim, elem_bytes and at least as many blocks with block_size 1, has K and V of the same block's one token,
- * in the cache's own type (kv_store and kv_load move it as any cache, by the same tables).  Of an E4M3 cache these are
- * stored values; scales apply to them as to the page.  A NaN does not count; a column without a number gets 0 twice.  Bounds
- * of other pages are untouched.  For a restored prefix, all its tokens are new ones (lens[b] of them).
+ * kv_bounds -- of each page of layer `layer` that a new token lies in, and each KV head, the lowest and the highest
+ * stored K of every column over the page's tokens t < lens[b], new and older ones.  They go where `bounds`, a kv_cache
+ * of the same heads, head_dim and elem_bytes with block_size 1 and at least as many blocks, has K and V of the same
+ * block's one token, in the cache's own type (kv_store and kv_load move it as any cache, by the same tables).  Of an
+ * E4M3 cache these are stored values; scales apply to them as to the page.  A NaN does not count; a column without a
+ * number gets 0 twice. Bounds of other pages are untouched.  For a restored prefix all its tokens are new ones (lens[b]
+ * of them).
  * Errors as kv_append; KV_EINVAL also for bounds that contradict the cache.
  */
 KV_API kv_status kv_bounds(const kv_cache *cache, int32_t layer, const kv_batch *batch, int32_t cache_dtype,
@@ -249,13 +255,15 @@ typedef struct kv_score_options {
 } kv_score_options;
 
 /*
- * kv_score -- for each new row r of token p, KV head h, and page j <= p / block_size of its sequence, scores[r*token_stride +
- * h*head_stride + j] = scale * max over the query heads of h of sum over d of max(q_d low_d, q_d high_d): no token of the
- * page has a larger scale * (q . k) with any of these heads.  Sums are held in 32 bits.  A page whose block id is bad gets
- * -infinity.  counts[r] = p / block_size + 1 (0 for a row before token 0): kv_keep's lens, for num_seqs = num_queries
- * sequences of pages.  Scores of pages from there on are left as they were.
- *   bounds: kv_bounds's; batch: the sequences as in kv_attend, max_len in tokens, at most table_len * block_size.
- *   scores: DEVICE float, rows of (max_len + block_size - 1) / block_size elements; counts: DEVICE int32[num_queries], or NULL.
+ * kv_score -- for each new row r of token p, KV head h, and page j <= p / block_size of its sequence,
+ *   scores[r*token_stride + h*head_stride + j] = scale * max over the query heads of h of sum_d max(q_d low_d, q_d high_d):
+ * no token of the page has a larger scale * (q . k) with any of these heads.  Sums are held in 32 bits; where bounds
+ * are not finite a score may be NaN.  A page whose block id is bad gets -infinity.  counts[r] = p / block_size + 1 (0
+ * for a row before token 0): kv_keep's lens for num_queries "sequences" of pages.  Scores of pages from there on are
+ * left as they were.
+ *   bounds: kv_bounds's; batch: the sequences as in kv_attend, max_len in tokens, at most table_len * block_size;
+ *   scores: DEVICE float, rows of (max_len + block_size - 1) / block_size elements that do not overlap;
+ *   counts: DEVICE int32[num_queries], or NULL.
  * Errors as kv_attend.
  */
 KV_API kv_status kv_score(const kv_cache *bounds, int32_t layer, const kv_batch *batch, const kv_score_options *options,

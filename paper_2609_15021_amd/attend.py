@@ -24,7 +24,7 @@ from .kvx import Cache, KvCache, _in_use_on, _lib, _raise
 try:
     from . import _tensors
 except ImportError as e:
-    raise ImportError("the binding's module _tensors is not built: python -c 'import __graft_entry__ as g; g.build()'") from e
+    raise ImportError("the binding's module _tensors is not built; run __graft_entry__.build()") from e
 
 KV_DTYPE_BF16 = 1
 KV_DTYPE_F16 = 2
@@ -303,7 +303,8 @@ def _page_list(pages, counts, tokens: int, device: int):
     (_, heads, budget), (token, head, _) = _ints(pages, "pages", 3, device, tokens)
     if counts is None:
         raise ValueError("pages without counts")
-    return _pack_list(pages.data_ptr(), _dense_ints(counts, "counts", 1, device, tokens), token, head, heads, budget), budget
+    counts_at = _dense_ints(counts, "counts", 1, device, tokens)
+    return _pack_list(pages.data_ptr(), counts_at, token, head, heads, budget), budget
 
 
 def kv_append(cache: Cache, layer: int, k, v, tables, lens, starts=None, *, max_q=None, max_len=None, dtype=None,
@@ -333,8 +334,8 @@ def kv_append(cache: Cache, layer: int, k, v, tables, lens, starts=None, *, max_
         k_scale, v_scale = _factor(k_scale, "k_scale"), _factor(v_scale, "v_scale")
     else:
         k_scale = v_scale = 1.0
-    _raise(_lib.kv_append(ctypes.byref(cache.struct), _int32(layer, "layer"), batch, kr, vr, _cache_dtype(cache, dtype, k),
-                          k_scale, v_scale, handle))
+    _raise(_lib.kv_append(ctypes.byref(cache.struct), _int32(layer, "layer"), batch, kr, vr,
+                          _cache_dtype(cache, dtype, k), k_scale, v_scale, handle))
     if stream is not None:
         _used(stream, k, v, tables, lens, starts)
 
@@ -342,8 +343,8 @@ def kv_append(cache: Cache, layer: int, k, v, tables, lens, starts=None, *, max_
 def kv_append_scaled(cache: Cache, layer: int, k, v, tables, lens, scales, starts=None, *, max_q=None, max_len=None,
                      stream=None) -> None:
     """kv_append into a float8_e4m3fn cache whose pages have ``scales`` (float8_e8m0fnu, or its bytes as uint8,
-    [blocks][2][H]: K's and V's of each head): the new rows' pages take the smallest power of two that brings them, and what a
-    page already held, to 448 or less."""
+    [blocks][2][H]: K's and V's of each head): the new rows' pages take the smallest power of two that brings them, and
+    what a page already held, to 448 or less."""
     layout = cache.layout
     D = layout.head_dim
     device = cache.struct.device
@@ -358,23 +359,24 @@ def kv_append_scaled(cache: Cache, layer: int, k, v, tables, lens, scales, start
         _used(stream, k, v, tables, lens, starts, scales)
 
 
-def kv_rotate(cache: Cache, layer: int, q, k, v, tables, lens, starts=None, *, freqs=None, positions=None, q_weight=None,
-              k_weight=None, eps: float = 1e-6, weight_offset: float = 0.0, interleaved: bool = False,
+def kv_rotate(cache: Cache, layer: int, q, k, v, tables, lens, starts=None, *, freqs=None, positions=None,
+              q_weight=None, k_weight=None, eps: float = 1e-6, weight_offset: float = 0.0, interleaved: bool = False,
               magnitude: float = 1.0, max_q=None, max_len=None, dtype=None, k_scale: float = 1.0, v_scale: float = 1.0,
               scales=None, out=None, stream=None):
     """Norm the new tokens' ``q`` and ``k`` for each head, rotate them by their position, and append K and V to layer
     ``layer``; returns the rotated queries.
 
-    ``q_weight``, ``k_weight`` ([D], float32 or the rows' type; None: no norm): x / sqrt(mean x^2 + eps) * (weight_offset +
-    weight).  ``freqs`` (float64 [n], None: no rotation): radians per position of the pairs (i, i + n) of a row's first 2n
-    columns, or (2i, 2i + 1) if ``interleaved``; cosine and sine are multiplied by ``magnitude``.  ``positions`` (int32
-    [tokens]): by default each token's place in its sequence.  ``dtype``, ``k_scale``, ``v_scale`` and ``scales`` are
-    kv_append's.  ``out`` (like ``q``) is made if not given, and may be ``q`` itself; rows of no sequence are left as they
-    were."""
+    ``q_weight``, ``k_weight`` ([D], float32 or the rows' type; None: no norm): x / sqrt(mean x^2 + eps) *
+    (weight_offset + weight).  ``freqs`` (float64 [n], None: no rotation): radians per position of the pairs (i, i + n)
+    of a row's first 2n columns, or (2i, 2i + 1) if ``interleaved``; cosine and sine are multiplied by ``magnitude``.
+    ``positions`` (int32 [tokens]): by default each token's place in its sequence.  ``dtype``, ``k_scale``, ``v_scale``
+    and ``scales`` are kv_append's.  ``out`` (like ``q``) is made if not given, and may be ``q`` itself; rows of no
+    sequence are left as they were."""
     layout = cache.layout
     D = layout.head_dim
     device = cache.struct.device
-    (qr, q_shape), (kr, shape), (vr, v_shape) = _rows(q, "q", D, device), _rows(k, "k", D, device), _rows(v, "v", D, device)
+    qr, q_shape = _rows(q, "q", D, device)
+    (kr, shape), (vr, v_shape) = _rows(k, "k", D, device), _rows(v, "v", D, device)
     if shape != v_shape or q_shape[0] != shape[0]:
         raise ValueError(f"q, k and v differ in shape: {tuple(q_shape)}, {tuple(shape)} and {tuple(v_shape)}")
     tokens = q_shape[0]
@@ -455,10 +457,10 @@ def kv_attend(cache: Cache, layer: int, q, tables, lens, starts=None, *, max_q=N
     [tokens][query heads]) are made if not given, and overlap no input; rows that belong to no sequence are left as
     they were.
 
-    ``scales``: those of a float8_e4m3fn cache's pages, as kv_append_scaled leaves them.  ``pages`` (int32 [tokens][H or 1]
-    [budget], dense rows) and ``counts`` (int32 [tokens]): each new token attends over the first ``counts`` of its
-    ``pages`` alone, which are places in its sequence's table, as kv_keep chooses them from kv_score's scores.  Neither
-    goes with ``weights``.
+    ``scales``: those of a float8_e4m3fn cache's pages, as kv_append_scaled leaves them.  ``pages`` (int32
+    [tokens][H or 1][budget], dense rows) and ``counts`` (int32 [tokens]): each new token attends over the first
+    ``counts`` of its ``pages`` alone, which are places in its sequence's table, as kv_keep chooses them from kv_score's
+    scores.  Neither goes with ``weights``.
     """
     device = cache.struct.device
     layout = cache.layout
@@ -554,12 +556,12 @@ def kv_attend_pages(cache: Cache, layer: int, q, tables, lens, starts=None, *, s
     return kv_attend(cache, layer, q, tables, lens, starts, scales=scales, pages=pages, counts=counts, **options)
 
 
-def kv_bounds(cache: Cache, layer: int, bounds: Cache, tables, lens, starts=None, *, max_q=None, max_len=None, dtype=None,
-              stream=None) -> None:
+def kv_bounds(cache: Cache, layer: int, bounds: Cache, tables, lens, starts=None, *, max_q=None, max_len=None,
+              dtype=None, stream=None) -> None:
     """For the pages of layer ``layer`` that new tokens lie in: the lowest and the highest stored K of every column over
-    the page's tokens, into the same block of ``bounds``, a cache of the same heads, head_dim and element size with one token
-    a block (lowest as K, highest as V).  Without ``starts`` each sequence has one new token; for a restored prefix, name as
-    many rows as it has tokens.
+    the page's tokens, into the same block of ``bounds``, a cache of the same heads, head_dim and element size with one
+    token a block (lowest as K, highest as V).  Without ``starts`` each sequence has one new token; for a restored
+    prefix, name as many rows as it has tokens.
 
     ``dtype``: the cache's, which 2-byte elements alone do not say."""
     device = cache.struct.device
@@ -584,9 +586,9 @@ def kv_bounds(cache: Cache, layer: int, bounds: Cache, tables, lens, starts=None
 
 def kv_score(bounds: Cache, layer: int, q, tables, lens, starts=None, *, block_size: int, max_q=None, max_len=None,
              dtype=None, scale: float = 1.0, scales=None, out=None, counts=None, stream=None):
-    """What no token of a page can exceed in scale * (q . k): for each new token, KV head and page up to the token's own the
-    largest over the head's queries ``q`` ([tokens][query heads][D]) of q's positive part times the page's highest K and its
-    negative part times the lowest, from kv_bounds's ``bounds`` of pages of ``block_size`` tokens.
+    """What no token of a page can exceed in scale * (q . k): for each new token, KV head and page up to the token's own
+    the largest over the head's queries ``q`` ([tokens][query heads][D]) of q's positive part times the page's highest K
+    and its negative part times the lowest, from kv_bounds's ``bounds`` of pages of ``block_size`` tokens.
 
     Returns (scores float32 [tokens][H][pages], counts int32 [tokens]: pages up to the token's own), which are kv_keep's
     weights and lens.  ``out`` and ``counts`` are made if not given; scores of pages beyond ``counts``, and rows of no

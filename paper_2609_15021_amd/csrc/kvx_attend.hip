@@ -149,9 +149,9 @@ Parts tail_parts_for(int64_t longest, int64_t have, int64_t launched, int64_t he
     Parts p{};
     p.len = static_cast<int32_t>(round_up((longest + best - 1) / best, 64));
     p.splits = static_cast<int32_t>((longest + p.len - 1) / p.len);
-    // Where some tiles wait for others, the long ones of every sequence go before the short ones: 6 tails of up to 1,055
-    // new tokens behind 8,192 (e4m3, D 256, 4 heads of 6 rows) take 661 us instead of 1,105 with scales, and 502 instead of
-    // 660 with a window of 4,096 and capped scores.
+    // Where some tiles wait for others, the long ones of every sequence go before the short ones: 6 tails of up to
+    // 1,055 new tokens behind 8,192 (e4m3, D 256, 4 heads of 6 rows) take 661 us instead of 1,105 with scales, and 502
+    // instead of 660 with a window of 4,096 and capped scores.
     p.ranked = num_seqs > 1 && num_seqs <= 64 && have * p.splits > at_once;
     return p;
 }
@@ -238,15 +238,17 @@ PagesPlan plan_of(const kv_cache *cache, const kv_batch *batch, const kv_page_li
     p.chosen.token_stride = list->token_stride;
     p.chosen.head_stride = list->heads == 1 ? 0 : list->head_stride;
     p.chosen.budget = list->budget;
-    // Parts of whole rounds of the workgroup's waves (32 tokens each), as many as run at once.  A row hardly has more tokens
-    // than its sequence may; where it does, which names pages twice, there are up to 4 times the parts, or longer ones.
+    // Parts of whole rounds of the workgroup's waves (32 tokens each), as many as run at once.  A row hardly has more
+    // tokens than its sequence may; where it does, which names pages twice, there are up to 4 times the parts, or
+    // longer ones.
     const int64_t likely = std::min(longest, round_up(std::max(batch->max_len, 1), cache->layout.block_size));
     const int64_t splits = std::min({std::max<int64_t>(at_once / groups, 1), (likely + 127) / 128, int64_t{64}});
-    const int64_t len = splits == 1 ? longest : std::max((likely + splits - 1) / splits, (longest + 4 * splits - 1) / (4 * splits));
+    const int64_t each = std::max((likely + splits - 1) / splits, (longest + 4 * splits - 1) / (4 * splits));
+    const int64_t len = splits == 1 ? longest : each;
     p.chosen.len = static_cast<int32_t>(std::min<int64_t>(round_up(len, 128), INT32_MAX - 1023));
     p.chosen.splits = static_cast<int32_t>((longest + p.chosen.len - 1) / p.chosen.len);
-    // A wave to a row where that still fills the chip.  With up to 128 tokens, of which a workgroup's waves would have a
-    // round each, from twice the workgroups on (128 rows of 8 heads, 8 pages of 16: 10 us instead of 15; 512 rows, 34
+    // A wave to a row where that still fills the chip.  With up to 128 tokens, of which a workgroup's waves would have
+    // a round each, from twice the workgroups on (128 rows of 8 heads, 8 pages of 16: 10 us instead of 15; 512 rows, 34
     // instead of 59); with more from 8 times on (256 rows, 64 pages: 123 instead of 114; 512 rows, 201 and 203).
     p.alone = p.chosen.splits == 1 && groups >= (likely <= 128 ? 2 : 8) * at_once;
     const int64_t split = p.chosen.splits > 1 ? heads * p.chosen.splits : 0;

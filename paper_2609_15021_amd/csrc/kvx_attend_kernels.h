@@ -192,9 +192,9 @@ __device__ __forceinline__ bool share_of(const AttendArgs &a, const Shares &shar
     return s.parts > 0;
 }
 
-// The tail kernel's tile of which `rank` others end behind it (or as far, in an order of their own), whatever sequences they
-// are of: the longest begin first.  False if there are no more.  A lane has a sequence, whose tiles' ends rise; of the ends
-// that may be, 64 are tried at once, a lane each, until one is left.
+// The tail kernel's tile of which `rank` others end behind it (or as far, in an order of their own), whatever sequences
+// they are of: the longest begin first.  False if there are no more.  A lane has a sequence, whose tiles' ends rise; of
+// the ends that may be, 64 are tried at once, a lane each, until one is left.
 __device__ __forceinline__ bool tile_of_rank(const AttendArgs &a, int rank, int &b, int &tile) {
     const int lane = threadIdx.x & 63;
     int past = 0, nq = 0, tiles = 0;  // of the lane's sequence; no tiles if the tail kernel has none of it
@@ -246,8 +246,8 @@ __device__ __forceinline__ int chosen_parts(const AttendArgs &a, const Chosen &c
     return max((count * a.pages.BS - 1) / chosen.len + 1, 1);
 }
 
-// Row `row` of a launch over chosen pages as a sequence of its own (seq.n tokens, the row's own the last of them), in the
-// sequence s.b, and its parts; false if it has no part s.split.
+// Row `row` of a launch over chosen pages as a sequence of its own (seq.n tokens, the row's own the last of them), in
+// the sequence s.b, and its parts; false if it has no part s.split.
 __device__ __forceinline__ bool chosen_of(const AttendArgs &a, const Chosen &chosen, int row, Share &s, Sequence &seq,
                                           int &count) {
     const int lane = threadIdx.x & 63;

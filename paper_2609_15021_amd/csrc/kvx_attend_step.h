@@ -56,8 +56,8 @@ __device__ __forceinline__ int64_t slot_in(const Chosen &chosen, int, int, int64
 //
 // From: Shares, or Chosen: each new token is a sequence of its own, of the pages that it chose, one after the other.  A
 // page's place in the list says where its tokens are, and which: the list is read a round before the table.  Or Alone:
-// the same where there are rows enough for every wave to have one for itself, and nothing to join: 111 new tokens of each of
-// 17 sequences over one page of 32 (3 heads of 12 rows, D 256) take 30 us instead of 103.
+// the same where there are rows enough for every wave to have one for itself, and nothing to join: 111 new tokens of
+// each of 17 sequences over one page of 32 (3 heads of 12 rows, D 256) take 30 us instead of 103.
 template <class T, bool FP8, int DP, int NT, bool SCALED, class From>
 __global__ __launch_bounds__(64 * kWaves, !FP8 && DP > 128 ? 1 : 2) void step_kernel(const AttendArgs a,
                                                                                      const From shares) {
@@ -463,8 +463,8 @@ __global__ __launch_bounds__(64 * kWaves, !FP8 && DP > 128 ? 1 : 2) void step_ke
         }
         return;
     } else {
-        // Join the waves: every wave's largest score and sum, then wave w collects component w of every tile, which are VE
-        // consecutive columns per lane.
+        // Join the waves: every wave's largest score and sum, then wave w collects component w of every tile, which are
+        // VE consecutive columns per lane.
         __shared__ float stats[kWaves][NT * 16][2];
         __shared__ float parts[kWaves][kWaves - 1][NT * TILES][64];
 #pragma unroll
@@ -549,8 +549,8 @@ template <class T, bool FP8, int DP, int NT, bool SCALED, class From>
 hipError_t launch_tiles(const AttendArgs &a, const From &from, int items, int max_rows, hipStream_t stream) {
     const int tiles = (max_rows + 16 * NT - 1) / (16 * NT);
     const int groups = std::is_same_v<From, Alone> ? (items + kWaves - 1) / kWaves : items;
-    return launch_kernel(step_kernel<T, FP8, DP, NT, SCALED, From>, dim3(groups, tiles * a.pages.H), 64 * kWaves, stream, a,
-                         from);
+    return launch_kernel(step_kernel<T, FP8, DP, NT, SCALED, From>, dim3(groups, tiles * a.pages.H), 64 * kWaves, stream,
+                         a, from);
 }
 
 // `items` workgroups (Alone: waves) for each KV head and tile of up to max_rows rows.

@@ -504,8 +504,8 @@ template <class T, bool FP8, int DP, int TK, int RW, bool PLAIN, bool FULL, bool
 hipError_t launch_columns(const AttendArgs &a, const Parts &parts, int max_queries, hipStream_t stream) {
     const int tiles = static_cast<int>(tail_tiles(max_queries, a.group));
     const uint32_t grid = static_cast<uint32_t>(tiles) * parts.splits * a.pages.H * a.num_seqs;
-    return launch_kernel(tail_kernel<T, FP8, DP, TK, RW, PLAIN, FULL, SCALED>, dim3(grid), 64 * kRows / RW, stream, a, parts,
-                         tiles);
+    return launch_kernel(tail_kernel<T, FP8, DP, TK, RW, PLAIN, FULL, SCALED>, dim3(grid), 64 * kRows / RW, stream, a,
+                         parts, tiles);
 }
 
 template <class T, bool FP8, bool PLAIN, bool FULL, bool SCALED>

@@ -19,7 +19,8 @@
 // 2,085 new tokens behind 32,768 (8 heads of 5 rows a token, bf16, D 128): 1.51 to 1.62 ms by machine, 890 to 955
 // TFLOP/s, where a large library product reaches 1,200.  Per round of 64 tokens a wave has 1,024 cycles of products
 // and about 1,150 of vector work (512 of them exponentials); two waves of a SIMD overlap them partly.  Ragged tails
-// of up to 1,055 tokens, e4m3, D 256, a window of 4,096 and capped scores: 0.66 ms, 495 TFLOP/s; there the matrix
+// of up to 1,055 tokens, e4m3, D 256, a window of 4,096 and capped scores: 0.50 ms, 650 TFLOP/s (0.66 ms with each
+// sequence's last tiles first, whatever their length).  A round's products and vector work overlap less there: the matrix
 // cores are busy for a fifth of the cycles, LDS for a quarter and the vector units for a third, mostly one after the
 // other: one workgroup a CU, whose two waves a SIMD meet at a barrier every round.  (Half of its waves half a round
 // behind the others, with a barrier for each half: 0.76 ms, as scores take longer than outputs.)

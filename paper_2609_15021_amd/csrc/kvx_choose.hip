@@ -1,18 +1,22 @@
-// kv_bounds and kv_score: what pages can score at most with a query, so that each new token can choose the pages that it
-// attends over.
+// kv_bounds and kv_score: what pages can score at most with a query, so that each new token can choose the pages that
+// it attends over.
 //
-// For lo <= k <= hi in every column, q.k <= sum_d max(q_d lo_d, q_d hi_d), and the larger product is q_d hi_d where q_d is
-// positive and q_d lo_d elsewhere: with q+ = max(q, 0) and q- = min(q, 0) the bound is q+.hi + q-.lo, two products on the
-// matrix cores.
+// For lo <= k <= hi in every column, q.k <= sum_d max(q_d lo_d, q_d hi_d), and the larger product is q_d hi_d where q_d
+// is positive and q_d lo_d elsewhere: with q+ = max(q, 0) and q- = min(q, 0) the bound is q+.hi + q-.lo, two products
+// on the matrix cores.
 //
 // Bounds: a group of lanes has a page and head, 16 bytes of its columns a lane, and takes the page's rows one after the
-// other, so nothing passes between lanes: bound by reading K once.  Where there are few pages their rows are spread over the
-// wave's groups instead, and joined by lane shuffles.
+// other, so nothing passes between lanes: bound by reading K once.  Where there are few pages their rows are spread
+// over the wave's groups instead, and joined by lane shuffles.  131,077 tokens of 8 heads of 128 (bf16, 302 MB): 57 us,
+// 5.3 TB/s (a large copy moves 4.7); the pages of 48 new tokens (4 heads of 256, e4m3): 4.6 us, launch and waits.
 //
-// Scores: a wave holds the bounds of kPages pages in registers as the products' second operand (column: page), and goes
-// over its share of the rows, 16 (new token, query head) at a time, as the first.  A token's heads are padded to a power
-// of two by repeating the last, so that the largest over them lies in a lane's 4 results, or one or two shuffles away.  A
-// decoding step is bound by reading the bounds, tails by the queries that each wave reads from the caches.
+// Scores: a wave holds the bounds of 16 or 32 pages in registers as the products' second operand (column: page), and
+// goes over its share of the rows, 16 (new token, query head) at a time, as the first.  A token's heads are padded to a
+// power of two by repeating the last, so that the largest over them lies in a lane's 4 results, or one or two shuffles
+// away.  8,193 pages of 8 heads of 5 rows (34 MB, D 128): 8.9 us, of which reading takes 5.6 and table, bounds and
+// products come one after the other.  Tails of up to 517 tokens over 1,057 pages, 3 sequences, 2 heads of 8 rows: 20
+// us, where the products alone would take 6: a wave's share of tiles is short, and its start (lengths, table, bounds)
+// and every second tile's wait for the workgroup are not hidden.
 #include <algorithm>
 #include <cmath>
 
@@ -70,8 +74,8 @@ struct Piece {
     }
 };
 
-// LPR lanes have a row; SPREAD: a wave has one page, else one for each of its groups of lanes.  AT_ONCE: rows that a lane
-// has on their way (16 instead of 8: 131,077 tokens of 8 heads of 256 bytes in 54 us instead of 57).
+// LPR lanes have a row; SPREAD: a wave has one page, else one for each of its groups of lanes.  AT_ONCE: rows that a
+// lane has on their way (16 instead of 8: 131,077 tokens of 8 heads of 256 bytes in 54 us instead of 57).
 template <int TYPE, int LPR, bool SPREAD, int AT_ONCE>
 __global__ __launch_bounds__(kThreads) void bounds_kernel(const BoundsArgs a) {
     constexpr int N = Piece<TYPE>::N, GROUPS = 64 / LPR;
@@ -105,8 +109,8 @@ __global__ __launch_bounds__(kThreads) void bounds_kernel(const BoundsArgs a) {
         u32x4 x[AT_ONCE];
 #pragma unroll
         for (int k = 0; k < AT_ONCE; ++k)
-            x[k] = __builtin_nontemporal_load(
-                reinterpret_cast<const u32x4 *>(from + static_cast<uint32_t>(min(row + k * STEP, rows - 1)) * p.token_bytes));
+            x[k] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(
+                from + static_cast<uint32_t>(min(row + k * STEP, rows - 1)) * p.token_bytes));
 #pragma unroll
         for (int k = 0; k < AT_ONCE; ++k) {
             float y[N];
@@ -222,11 +226,12 @@ struct ScoreArgs {
     int32_t *counts;
     int64_t token_stride, head_stride;  // elements
     float scale;
-    int32_t BS, group, pad, shift;      // tokens of a page; query heads of a KV head, and the power of two 2^shift that they fill, up to 16
+    int32_t BS, group, pad, shift;      // tokens of a page; query heads of a KV head, padded to 2^shift, up to 16
     int32_t page_chunks, tokens;        // of a launch's first dimension; tokens of a workgroup
     Divisor by_bs, by_chunks, by_subs;
 };
 
+// Workgroups that tails are shared out to: 20 us for the tails above; a third of them take 26, twice as many 24.
 constexpr int kShareTarget = 1536;
 
 typedef short s16x2 __attribute__((ext_vector_type(2)));
@@ -243,11 +248,10 @@ __device__ __forceinline__ float from_lane(float x, int lane) {
     return __builtin_bit_cast(float, __builtin_amdgcn_ds_bpermute(lane * 4, __builtin_bit_cast(int, x)));
 }
 
-// A wave's 16-byte loads of 16 rows, a row for every 16th lane, would touch 16 lines of the cache for 64 bytes each, and
-// take 8 times as long as loads of whole rows (36 us instead of 22 for tails of up to 517 tokens over 1,057 pages, 2 heads of 8).  So
-// rows are loaded whole, and turned in LDS: bounds once for each wave, queries by the workgroup for all its waves, twice, so
-// that the next are on their way while one set is used.  Pieces of 16 bytes are permuted there, row by row, so that 16 rows'
-// same piece lies in different banks.
+// Loads of 64 bytes of each of 16 rows, as the operands want them, come from the caches far slower than loads of whole
+// rows.  So rows are loaded whole, and turned in LDS: bounds once for each wave, queries by the workgroup for all its
+// waves, twice, so that the next are on their way while one set is used (the tails above took 36 us before).  Pieces of
+// 16 bytes are permuted there, row by row, so that 16 rows' same piece lies in different banks.
 //
 // T: type of q; FP8: bounds are e4m3; DP >= D columns; PG: 16 pages of a wave; OUT: tokens that a lane has results of
 // (4 heads are a lane's 4 results: 1 where a token's fill them, 2 or 4 of 2 heads or 1).

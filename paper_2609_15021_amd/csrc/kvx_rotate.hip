@@ -1,11 +1,16 @@
 // kv_rotate: the new tokens' queries and keys normed for each head and rotated by their position, in one pass; keys and
 // values go straight into the cache's pages.
 //
-// Everything is read once and written once.  A lane has 8 columns of a row, so a row's norm is a few lane shuffles, and so
-// are the partners that lie half a row away.  A group of lanes takes kAtOnce rows (query heads, then heads of K, then of V)
-// of one token, all of them on their way at once; as many groups as a token needs share it, and a workgroup has as many
-// tokens as that leaves room for.  Angles are the same for all heads: the workgroup works out its tokens' cosines and
-// sines once, in LDS, and looks their pages up, while the rows are on their way.
+// Everything is read once and written once.  A lane has 8 columns of a row, so a row's norm is a few lane shuffles, and
+// so are the partners that lie half a row away.  A group of lanes takes kAtOnce rows (query heads, then heads of K,
+// then of V) of one token, all of them on their way at once; as many groups as a token needs share it, and a workgroup
+// has as many tokens as that leaves room for.  Angles are the same for all heads: the workgroup works out its tokens'
+// cosines and sines once, in LDS, and looks their pages up, while the rows are on their way.
+//
+// 2,085 tokens of 40 query heads and 8 KV heads (bf16, D 128, norms; 60 MB, 12.7 us at a large copy's rate): 18.8 us.
+// About 6 of them are the launch and a workgroup's start, whatever the size; then rows pass at 4.3 TB/s, with the vector
+// units busy for about half of the time.  Rows are stored past the caches (20.3 us without).  A decoding step takes 4.6
+// us on the GPU, 8.2 with the host.
 #include <algorithm>
 #include <cmath>
 
@@ -65,7 +70,8 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateArgs a) {
     const auto from = [&](int row, int r) {
         const int of_k = r - a.heads, of_v = of_k - p.H;
         const Rows &src = of_k < 0 ? a.q : of_v < 0 ? a.k : a.v;
-        return src.data + int64_t{row} * src.token_stride + int64_t{of_k < 0 ? r : of_v < 0 ? of_k : of_v} * src.head_stride;
+        const int64_t head = of_k < 0 ? r : of_v < 0 ? of_k : of_v;
+        return src.data + int64_t{row} * src.token_stride + head * src.head_stride;
     };
     struct Vecs {
         typename Lane::Vec of[kAtOnce];
@@ -214,8 +220,8 @@ kv_status check_rotate(const kv_cache *cache, int32_t layer, const kv_batch *bat
         return fail(KV_EINVAL, "weights of type %d for rows of type %d", o->weight_dtype, q->dtype);
     if (!(o->eps >= 0.f && std::isfinite(o->eps)) || !std::isfinite(o->weight_offset) ||
         !(o->magnitude >= 0.f && std::isfinite(o->magnitude)))
-        return fail(KV_EINVAL, "eps, weight_offset and magnitude must be finite, eps and magnitude not negative (got %g, %g, "
-                    "%g)", o->eps, o->weight_offset, o->magnitude);
+        return fail(KV_EINVAL, "eps, weight_offset and magnitude must be finite, eps and magnitude not negative (got %g, "
+                    "%g, %g)", o->eps, o->weight_offset, o->magnitude);
     return KV_OK;
 }
 
@@ -255,9 +261,9 @@ kv_status rotate(const kv_cache *cache, int32_t layer, const kv_batch *batch, co
     a.k_scale = o->k_scale == 0.f ? 1.f : o->k_scale;
     a.v_scale = o->v_scale == 0.f ? 1.f : o->v_scale;
     const Pairs pairs = o->interleaved ? kNeighbours : t.half % 8 == 0 ? kHalves : kAnyHalves;
-    // A token has as many groups of lanes as have kAtOnce rows each (or a group for each row, while that leaves CUs idle),
-    // and a workgroup as many tokens as its groups then have at once, or more of them one after the other where all
-    // workgroups would not run at once: what a workgroup does before its first row is then done once for them.
+    // A token has as many groups of lanes as have kAtOnce rows each (or a group for each row, while that leaves CUs
+    // idle), and a workgroup as many tokens as its groups then have at once, or more of them one after the other where
+    // all workgroups would not run at once: what a workgroup does before its first row is then done once for them.
     const int64_t most = std::min(batch->max_queries, batch->num_queries), groups_each = kThreads / lanes_of(a.pages.D);
     const int64_t wanted = int64_t{batch->num_queries} * a.rows_each > 16384 ? (a.rows_each + kAtOnce - 1) / kAtOnce
                                                                              : a.rows_each;

@@ -94,12 +94,14 @@ __device__ __forceinline__ void turn_by(int position, double freq, float magnitu
     sine = s * magnitude;
 }
 
-// Sum over a group of LPR lanes (lanes of 16 by moves inside the vector unit, which cost nothing beside an LDS shuffle).
+// Sum over a group of LPR lanes (lanes of 16 by moves inside the vector unit, which cost nothing beside an LDS
+// shuffle).
 template <int LPR>
 __device__ __forceinline__ float sum_over(float x) {
     const auto moved = [](float y, auto control) {
-        return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, y), decltype(control)::value,
-                                                                     0xf, 0xf, true));
+        constexpr int kControl = decltype(control)::value;
+        return __builtin_bit_cast(
+            float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, y), kControl, 0xf, 0xf, true));
     };
     x += moved(x, std::integral_constant<int, 0xb1>{});   // lane ^ 1
     x += moved(x, std::integral_constant<int, 0x4e>{});   // lane ^ 2
@@ -201,7 +203,8 @@ struct Turner {
         return a;
     }
 
-    // The lane's columns of a row, normed if `norm` (else all weights are 1), and turned.  All lanes of a row take part.
+    // The lane's columns of a row, normed if `norm` (else all weights are 1), and turned.  All lanes of a row take
+    // part.
     __device__ __forceinline__ void finish(const Turn &t, const Vec &v, bool norm, const Weights &w, const Angles &a,
                                            float *y) const {
         to_floats<DTYPE>(v.own, y);

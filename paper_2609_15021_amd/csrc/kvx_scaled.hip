@@ -5,8 +5,10 @@
 // rounding a page's older rows again when its scale grows, and applying it in attention.
 //
 // A workgroup has one (page, K or V, head): it takes the new rows of the page, finds their largest |x|, and with the
-// page's old scale the new one; rounds older rows if the scale grew; and writes the new ones, of which it holds kHeld in
-// a lane's registers.
+// page's old scale the new one; rounds older rows if the scale grew; and writes the new ones, of which it holds kHeld
+// in a lane's registers.  2,608 new tokens of 4 heads of 256 (16 MB read and written once, 3.4 us at a large copy's rate)
+// take 8.0 us on the GPU: lengths, then rows and tables, then scales are waited for one after the other, and there is
+// one set of rows for each workgroup.  A decoding step of 48 tokens takes 4.1 (5.8 with the host).
 #include <algorithm>
 
 #include "kvx_rows.h"
@@ -72,8 +74,8 @@ __global__ __launch_bounds__(64 * WAVES) void append_scaled_kernel(const ScaledA
             to_floats<DTYPE>(v.own, y);
         }
     };
-    // (All lanes of a row take part in its norm; rows beyond the last repeat it.  They are on their way while the page is
-    // looked up.)
+    // (All lanes of a row take part in its norm; rows beyond the last repeat it.  They are on their way while the page
+    // is looked up.)
     typename Turner<DTYPE, PAIRS, LPR>::Vec v[kHeld];
 #pragma unroll
     for (int k = 0; k < kHeld; ++k)

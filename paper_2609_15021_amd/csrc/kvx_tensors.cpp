@@ -114,8 +114,9 @@ PyObject *batch(PyObject *, PyObject *const *args, Py_ssize_t count) {
         x.max_queries = static_cast<int32_t>(std::max<int64_t>(most, 1));
         x.starts = static_cast<const int32_t *>(starts->data_ptr());
     }
-    int64_t most = pages > (INT64_C(1) << 31) / std::max<int64_t>(block_size, 1) ? (INT64_C(1) << 31) : pages * block_size;
-    most = std::min<int64_t>(most, (INT64_C(1) << 31) - 1024);
+    constexpr int64_t kEnd = INT64_C(1) << 31;
+    int64_t most = pages > kEnd / std::max<int64_t>(block_size, 1) ? kEnd : pages * block_size;
+    most = std::min<int64_t>(most, kEnd - 1024);
     if (args[7] != Py_None) {
         int beyond = 0;
         const int64_t asked = PyLong_AsLongLongAndOverflow(args[7], &beyond);
@@ -174,8 +175,8 @@ const at::Tensor *vector_of(PyObject *x, int64_t elements, int device) {
     return t && t->dim() == 1 && (elements < 0 || t->size(0) == elements) && t->is_contiguous() ? t : nullptr;
 }
 
-// rotation(row type, head_dim, tokens, device, freqs, positions, q_weight, k_weight): (rotary_dim, weights' type, freqs,
-// positions, q_weight, k_weight), as kv_rotate_options has them; None for those that are not given
+// rotation(row type, head_dim, tokens, device, freqs, positions, q_weight, k_weight): (rotary_dim, weights' type,
+// freqs, positions, q_weight, k_weight), as kv_rotate_options has them; None for those that are not given
 PyObject *rotation(PyObject *, PyObject *const *args, Py_ssize_t count) {
     if (count != 8)
         Py_RETURN_NONE;

@@ -241,8 +241,8 @@ def test_append_step_by_step():
     assert torch.equal(scales.cpu(), by.cpu())
     block = int(c.tables[0, 0])
     x, y = flat[block].float().cpu(), at_once[block].float().cpu()
-    # Values that were rounded in e4m3's normal numbers only are the same; others are within a step of the smallest, 2^-9,
-    # and halves of it that each growth adds: under 2^-8.
+    # Values that were rounded in e4m3's normal numbers only are the same; others are within a step of the smallest,
+    # 2^-9, and halves of it that each growth adds: under 2^-8.
     assert bool(((x == y) | ((x - y).abs() <= 2.0**-8)).all())
 
 
