@@ -173,10 +173,10 @@ typedef struct kv_rotate_options {
  * kv_rotate -- norm, rotate, and append.  Of each new token's row x of each head of q and k:
  *   y_d = x_d / sqrt(mean of x^2 + eps) * (weight_offset + weight_d)  (or x_d, without weights), and for each pair (a, b)
  *   of the first rotary_dim columns, with t = position * freqs[i]: (a cos t - b sin t, b cos t + a sin t) * magnitude.
- * A row is rounded once, at the end; sums are held in 32 bits, positions times frequencies in 64.  q's rows go to `out`
- * (same type and heads; may be q itself), k's rotated rows and v's as they are into layer `layer` of the cache, as
- * kv_append, or with scales kv_append_scaled, puts them there.  A row whose token has no place (before token 0) is
- * rotated by its place or position all the same; rows of no sequence are left as they were.
+ * A row is rounded once, at the end; sums are held in 32 bits (so a normed row's |x| stay under 1e18), positions times
+ * frequencies in 64.  q's rows go to `out` (same type and heads; may be q itself), k's rotated rows and v's as they are
+ * into layer `layer` of the cache, as kv_append, or with scales kv_append_scaled, puts them there.  A row whose token has
+ * no place (before token 0) is rotated by its place or position all the same; rows of no sequence are left as they were.
  * Errors and preconditions as kv_append; KV_EINVAL also for a rotary_dim that is odd or outside [0, D], a NULL freqs
  * with one, and numbers that are negative or not finite.
  */
@@ -215,12 +215,12 @@ KV_API int64_t kv_attend_workspace(const kv_cache *cache, const kv_batch *batch,
  * kv_attend_pages -- kv_attend where an E4M3 cache's pages have scales (scales; options' k_scale and v_scale are then
  * 1), where each new token attends over the pages alone that it chose (list), or both; one of them must be given.
  * Token t of a chosen page takes part where t <= p and, with window > 0, p - t < window, and slopes count in p - t, as
- * in kv_attend; a row that chose nothing that it sees gets 0 and -infinity.  With a list a row's weights always meet V
- * as two numbers, a V that is not finite reaches no row that does not see it, and each row reads its pages for itself.
- * With scales, and with a list in any E4M3 cache, the weights times V's scale are numbers of bfloat16; of float16 rows
- * they are always two. weights_in and weights_out must be NULL.  Errors as kv_attend; KV_EINVAL also for a list that
- * contradicts the cache, KV_EUNSUPPORTED for weights_out, more than 2^31 - 1024 tokens in `budget` pages, and more rows
- * than one launch takes.
+ * in kv_attend; a row that chose nothing that it sees gets 0 and -infinity, and pages that a row sees no token of are
+ * not looked up in its table.  With a list a row's weights always meet V as two numbers, a V that is not finite reaches
+ * no row that does not see it, and each row reads its pages for itself.  With scales, and with a list in any E4M3 cache,
+ * the weights times V's scale are numbers of bfloat16; of float16 rows they are always two.  weights_in and weights_out
+ * must be NULL.  Errors as kv_attend; KV_EINVAL also for a list that contradicts the cache, KV_EUNSUPPORTED for
+ * weights_out, more than 2^31 - 1024 tokens in `budget` pages, and more rows than one launch takes.
  */
 KV_API kv_status kv_attend_pages(const kv_cache *cache, int32_t layer, const kv_batch *batch,
                                  const kv_attend_options *options, const kv_page_scales *scales,

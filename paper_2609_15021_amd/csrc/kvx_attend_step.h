@@ -157,7 +157,9 @@ __global__ __launch_bounds__(64 * kWaves, !FP8 && DP > 128 ? 1 : 2) void step_ke
             shown = t < stop && entry >= 0 && entry < a.batch.table_len;
             if (t < stop && !shown)
                 report(pg.err, KV_ASYNC_BAD_BATCH);
-            shown = shown && static_cast<int64_t>(entry) * pg.BS <= p_first;
+            // (A page that lies before the window may have no block, or one without a scale.)
+            const int64_t start = static_cast<int64_t>(entry) * pg.BS;
+            shown = shown && start <= p_first && (a.window == 0 || p_first - (start + pg.BS - 1) < a.window);
         } else {
             page = divide(t, pg.by_bs);
             shown = t < stop && (page + 1) * static_cast<int64_t>(pg.BS) > span.first;

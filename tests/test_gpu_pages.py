@@ -556,6 +556,32 @@ def test_attend_chosen_lists_as_they_come():
     assert bool(torch.isfinite(lse[0]).all())
 
 
+def test_attend_chosen_before_the_window():
+    """A page that lies before the window may be given away: its block and its scales are not looked at."""
+    c = pref.ScaledCase(2, 3, 64, 16, [100, 90], [1, 2], seed=19)
+    pages = torch.tensor([0, 5, 6, 1, 4], dtype=torch.int32).expand(3, 1, 5).contiguous()
+    counts = torch.tensor([5, 5, 4], dtype=torch.int32)
+    cache, _, q, _, _, tables, lens, starts = c.device()
+    by = c.scales.to(DEV)
+    want = pref.attend_chosen(c, pages, counts, window=20)
+    gone = tables.clone()
+    gone[0, :4], gone[1, :4] = -1, 1 << 30
+    other = by.clone()
+    other.view(torch.uint8)[tables[0, :4].long()] = 255
+    for table, scales in ((tables, by), (gone, by), (tables, other)):
+        out, lse = attend.kv_attend(cache, 0, q, table, lens, starts, pages=pages.to(DEV), counts=counts.to(DEV),
+                                    window=20, scales=scales)
+        ref.check(lse, want[1], want[3], "lse")
+        ref.check(out, want[0], want[2], "out")
+
+
+def test_rotate_many_in_place():
+    """Queries that are overwritten, while a workgroup has the next ones on their way."""
+    c = ref.Case(2, 5, 64, 16, [700, 90], [650, 33], seed=21)
+    run_rotate(c, rotary=20, in_place=True)
+    run_rotate(c, in_place=True)
+
+
 # ---- Bad numbers on the device, streams, graphs -------------------------------------------
 
 
