@@ -109,52 +109,55 @@ __device__ __forceinline__ int share_tokens(const AttendArgs &a, int b, bool tel
     return max(span.end - span.start, 0);
 }
 
-__device__ __forceinline__ int64_t sum_of_wave(int64_t x) {
-#pragma unroll
-    for (int o = 32; o; o >>= 1)
-        x += __shfl_xor(x, o);
-    return x;
-}
-
+// Sums over the lanes up to this one, by moves inside the vector unit: shuffles through LDS take 10 times as long, and
+// every wave begins with some.  All lanes take part.
 __device__ __forceinline__ int sum_up_to_lane(int x) {
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const int y = __shfl_up(x, o);
-        x += lane >= o ? y : 0;
-    }
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);   // lane - 1, of 16
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);   // lane - 2
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);   // lane - 4
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);   // lane - 8
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // lane 15 to the second 16, lane 47 to the last
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // lane 31 to the upper half
     return x;
 }
 
-// Parts of sequence b at a length.
-__device__ __forceinline__ int share_parts(const AttendArgs &a, int b, int64_t len) {
-    bool rows;
-    const int tokens = share_tokens(a, b, false, rows);
-    return rows ? static_cast<int>(max((tokens + len - 1) / len, int64_t{1})) : 0;
+// Of x from 0 to 2^49.
+__device__ __forceinline__ int64_t sum_of_wave(int64_t x) {
+    const int low = sum_up_to_lane(static_cast<int>(x & 0xffffff)), high = sum_up_to_lane(static_cast<int>(x >> 24));
+    return (static_cast<int64_t>(__builtin_amdgcn_readlane(high, 63)) << 24) + __builtin_amdgcn_readlane(low, 63);
 }
 
-// The shortest length of a part, up to a few percent, that makes no more parts than wanted.  `first` and `step`: this
-// lane's sequences; sum(x): x over all lanes.
-template <class Sum>
-__device__ __forceinline__ int64_t share_len(const AttendArgs &a, const Shares &shares, int first, int step, bool tell,
-                                             Sum &&sum) {
-    const auto round_len = [&](int64_t len) { return max((len + 31) / 32 * 32, int64_t{shares.shortest}); };
+// Parts of so many tokens at a length.
+__device__ __forceinline__ int share_parts(int tokens, bool rows, int len) {
+    return rows ? max((static_cast<uint32_t>(tokens) + len - 1) / static_cast<uint32_t>(len), 1u) : 0;
+}
+
+// x / y for 0 <= x < 2^53, in a fraction of the instructions of a division of 64 bits: every wave begins with some.
+__device__ __forceinline__ int64_t quotient(int64_t x, int y) {
+    const int64_t q = static_cast<int64_t>(static_cast<double>(x) / static_cast<double>(y)), rest = x - q * y;
+    return rest < 0 ? q - 1 : rest >= y ? q + 1 : q;
+}
+
+// The shortest length of a part, up to a few percent, that makes no more parts than wanted.  each(f): f(tokens, rows)
+// of every sequence of this lane's; sum(x): x over all lanes.
+template <class Each, class Sum>
+__device__ __forceinline__ int share_len(const Shares &shares, Each &&each, Sum &&sum) {
+    const auto round_len = [&](int64_t len) {
+        return static_cast<int>(min(max((len + 31) & ~int64_t{31}, int64_t{shares.shortest}), int64_t{INT32_MAX}));
+    };
     int64_t total = 0;
-    for (int b = first; b < shares.num_seqs; b += step) {
-        bool rows;
-        total += share_tokens(a, b, tell, rows);
-    }
-    int64_t len = round_len((sum(total) + shares.target - 1) / shares.target);
+    each([&](int tokens, bool) { total += tokens; });
+    int len = round_len(quotient(sum(total) + shares.target - 1, shares.target));
     for (int tries = 0; tries < 4 && shares.num_seqs > 1; ++tries) {
         int64_t parts = 0;
-        for (int b = first; b < shares.num_seqs; b += step)
-            parts += share_parts(a, b, len);
+        each([&](int tokens, bool rows) { parts += share_parts(tokens, rows, len); });
         parts = sum(parts);
         if (parts <= max(int64_t{shares.target}, 2 * int64_t{shares.num_seqs}))
             break;
-        len = round_len(len * parts / shares.target);
+        // (Parts times their length are hardly more than all tokens and a part for each sequence: under 2^49.)
+        len = round_len(quotient(len * parts, shares.target));
     }
-    return min(len, int64_t{INT32_MAX});
+    return len;
 }
 
 // The part that is item `item`, or (by_seq) sequence `item`'s parts; false if there is none.  Every wave for itself.
@@ -178,8 +181,10 @@ __device__ __forceinline__ bool share_of(const AttendArgs &a, const Shares &shar
     }
     const int lane = threadIdx.x & 63;
     const bool tell = !by_seq && item == 0 && blockIdx.y == 0 && threadIdx.x < 64;
-    const int64_t len = share_len(a, shares, lane, 64, tell, sum_of_wave);
-    const int mine = lane < shares.num_seqs ? share_parts(a, lane, len) : 0;
+    bool rows = false;
+    const int tokens = lane < shares.num_seqs ? share_tokens(a, lane, tell, rows) : 0;
+    const int len = share_len(shares, [&](auto &&f) { f(tokens, rows); }, sum_of_wave);
+    const int mine = share_parts(tokens, rows, len);
     const int from = sum_up_to_lane(mine) - mine;
     const uint64_t found = __ballot(by_seq ? lane == item : item >= from && item < from + mine);
     if (!found)
@@ -188,7 +193,7 @@ __device__ __forceinline__ bool share_of(const AttendArgs &a, const Shares &shar
     s.parts = __builtin_amdgcn_readlane(mine, s.b);
     s.item0 = __builtin_amdgcn_readlane(from, s.b);
     s.split = by_seq ? 0 : item - s.item0;
-    s.len = static_cast<int>(len);
+    s.len = len;
     return s.parts > 0;
 }
 
@@ -328,6 +333,7 @@ struct F16 {
     static __device__ __forceinline__ float high(uint32_t x) { return static_cast<float>(__builtin_bit_cast(pair, x)[1]); }
 };
 
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));

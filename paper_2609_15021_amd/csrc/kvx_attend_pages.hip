@@ -7,8 +7,8 @@
 // One token over 256 of 8,193 pages of 16 (8 heads of 5 rows, bf16, D 128; 17 MB): 9.2 us, launch and four dependent
 // reads, and 3.9 to join 32 parts.  48 tokens over 128 pages each (2 heads of 8 rows, 96 MB, 15 us at 6.3 TB/s): 22 us
 // and 4 to join.  2,048 new tokens of 8 heads over 64 pages each take 615 us, 14 TB/s, mostly from the caches.
-// Scales cost decoding nothing: 16 sequences of up to 32,768 tokens (e4m3, 4 heads of 6 rows, D 256) take 116 us and 7
-// to join, 4.8 TB/s.
+// Scales cost decoding nothing: 16 sequences of up to 32,768 tokens (e4m3, 4 heads of 6 rows, D 256) take 114 us and 6
+// to join, 4.9 TB/s.
 #include "kvx_attend_step.h"
 
 namespace kvx {

@@ -17,10 +17,10 @@
 // 32 tokens is requested as soon as the scores have used the last, V as soon as the second product has: a wave has 16
 // KiB in flight (bf16, D 128) without a second set of registers, and 2 waves of a SIMD 128 KiB a CU.
 //
-// One sequence behind 131,077 tokens (8 heads of 5 rows, bf16, D 128): 95 us and 7 to join, 5.2 TB/s with both (a
+// One sequence behind 131,077 tokens (8 heads of 5 rows, bf16, D 128): 95 us and 6 to join, 5.3 TB/s with both (a
 // large reduction reads 6.1, a large copy moves 4.8).  16 sequences of up to 32,768 tokens in e4m3 (4 heads of 6
-// rows, D 256): 117 us and 8 to join, 4.8 TB/s.  48 of up to 8,192 with weights (2 heads of 8 rows): 53 us (209 MB of
-// K and V read, 13 MB of scores written), 8 to join, 7 for what each token received.
+// rows, D 256): 114 us and 6 to join, 4.9 TB/s.  48 of up to 8,192 with weights (2 heads of 8 rows): 52 us (209 MB of
+// K and V read, 13 MB of scores written), 6 to join, 7 for what each token received.
 #include <algorithm>
 
 #include "kvx_attend_step.h"
@@ -44,11 +44,23 @@ __global__ __launch_bounds__(1024) void share_kernel(const AttendArgs a, const S
             x += wave_sums[i];
         return x;
     };
-    const int64_t len = share_len(a, shares, tid, 1024, true, sum);
+    bool told = false;
+    const auto each = [&](auto &&f) {
+        for (int b = tid; b < shares.num_seqs; b += 1024) {
+            bool rows;
+            const int tokens = share_tokens(a, b, !told, rows);
+            f(tokens, rows);
+        }
+        told = true;
+    };
+    const int len = share_len(shares, each, sum);
     int32_t *seqs = shares.items_of + 2, *items = seqs + 2 * static_cast<int64_t>(shares.num_seqs);
     int base = 0;
     for (int b0 = 0; b0 < shares.num_seqs; b0 += 1024) {
-        const int b = b0 + tid, mine = b < shares.num_seqs ? share_parts(a, b, len) : 0, upto = sum_up_to_lane(mine);
+        const int b = b0 + tid;
+        bool rows = false;
+        const int tokens = b < shares.num_seqs ? share_tokens(a, b, false, rows) : 0;
+        const int mine = share_parts(tokens, rows, len), upto = sum_up_to_lane(mine);
         __syncthreads();
         if (lane == 63)
             wave_sums[wave] = upto;
@@ -70,7 +82,7 @@ __global__ __launch_bounds__(1024) void share_kernel(const AttendArgs a, const S
     for (int i = base + tid; i < shares.items; i += 1024)
         items[2 * i] = -1;
     if (tid == 0)
-        shares.items_of[0] = static_cast<int>(len);
+        shares.items_of[0] = len;
 }
 
 // Where the parts of a row lie.
@@ -124,43 +136,60 @@ __global__ __launch_bounds__(256) void join_kernel(const AttendArgs a, const Fro
     const float *stats = from.stats + row_at.slot * 2;
     const int64_t step = row_at.stride;
     float most = kLowest, total = 0.f;
-    // (The first parts' sums are on their way while the row's largest score is looked for.)
+    // (A lane's first parts are on their way together, their sums while the row's largest score is looked for.)
     constexpr int EARLY = SPREAD ? 8 : 4;
     const int s0 = SPREAD ? mine : 0, ds = SPREAD ? groups : 1;
-    f32x4 early[EARLY];
-    float early_most[EARLY];
+    struct Sums {
+        f32x4 x[EARLY];
+        float most[EARLY];
+    };
+    const auto load = [&](int first) {
+        Sums sums_of;
 #pragma unroll
-    for (int k = 0; k < EARLY; ++k) {
-        const int s = s0 + k * ds;
-        const bool is = row && s < parts;
-        early[k] = is ? *reinterpret_cast<const f32x4 *>(from.sums + (row_at.slot + s * step) * D + d)
-                      : f32x4{0.f, 0.f, 0.f, 0.f};
-        early_most[k] = is ? stats[2 * s * step] : kLowest;
+        for (int k = 0; k < EARLY; ++k) {
+            const int s = first + k * ds;
+            const bool is = row && s < parts;
+            sums_of.x[k] = is ? *reinterpret_cast<const f32x4 *>(from.sums + (row_at.slot + s * step) * D + d)
+                              : f32x4{0.f, 0.f, 0.f, 0.f};
+            sums_of.most[k] = is ? stats[2 * s * step] : kLowest;
+        }
+        return sums_of;
+    };
+    constexpr int HELD = 4;  // statistics that a lane keeps
+    const int t0 = SPREAD ? tid & 63 : 0, dt = SPREAD ? 64 : 1;
+    f32x2 held[HELD];
+#pragma unroll
+    for (int k = 0; k < HELD; ++k) {
+        const int s = t0 + k * dt;
+        held[k] = s < parts ? *reinterpret_cast<const f32x2 *>(stats + 2 * s * step) : f32x2{kLowest, 0.f};
     }
-    if constexpr (SPREAD) {  // every wave for itself
-        const int lane = tid & 63;
-        for (int s = lane; s < parts; s += 64)
-            most = fmaxf(most, stats[2 * s * step]);
+    const Sums early = load(s0);
+#pragma unroll
+    for (int k = 0; k < HELD; ++k)
+        most = fmaxf(most, held[k][0]);
+    for (int s = t0 + HELD * dt; s < parts; s += dt)
+        most = fmaxf(most, stats[2 * s * step]);
+    if constexpr (SPREAD)  // every wave for itself
         for (int o = 32; o; o >>= 1)
             most = fmaxf(most, __shfl_xor(most, o));
-        for (int s = lane; s < parts; s += 64)
-            total += stats[2 * s * step + 1] * __builtin_amdgcn_exp2f(stats[2 * s * step] - most);
+#pragma unroll
+    for (int k = 0; k < HELD; ++k)
+        total += held[k][1] * __builtin_amdgcn_exp2f(held[k][0] - most);
+    for (int s = t0 + HELD * dt; s < parts; s += dt)
+        total += stats[2 * s * step + 1] * __builtin_amdgcn_exp2f(stats[2 * s * step] - most);
+    if constexpr (SPREAD)
         for (int o = 32; o; o >>= 1)
             total += __shfl_xor(total, o);
-    } else {
-        for (int s = 0; s < parts; ++s)
-            most = fmaxf(most, stats[2 * s * step]);
-        for (int s = 0; s < parts; ++s)
-            total += stats[2 * s * step + 1] * __builtin_amdgcn_exp2f(stats[2 * s * step] - most);
-    }
     f32x4 x{0.f, 0.f, 0.f, 0.f};
+    const auto add = [&](const Sums &sums_of) {
 #pragma unroll
-    for (int k = 0; k < EARLY; ++k)
-        x += early[k] * __builtin_amdgcn_exp2f(early_most[k] - most);
+        for (int k = 0; k < EARLY; ++k)
+            x += sums_of.x[k] * __builtin_amdgcn_exp2f(sums_of.most[k] - most);
+    };
+    add(early);
     if (row)
-        for (int s = s0 + EARLY * ds; s < parts; s += ds)
-            x += *reinterpret_cast<const f32x4 *>(from.sums + (row_at.slot + s * step) * D + d) *
-                 __builtin_amdgcn_exp2f(stats[2 * s * step] - most);
+        for (int s = s0 + EARLY * ds; s < parts; s += EARLY * ds)
+            add(load(s));
     if constexpr (SPREAD) {
         sums[tid] = x;
         __syncthreads();
