@@ -203,6 +203,15 @@ struct Turner {
         return a;
     }
 
+    // kHalves: of cosines and sines of the lane's pairs, whatever they are where it is not turned, its columns'.
+    __device__ __forceinline__ void settle(const Turn &t, Angles &a) const {
+#pragma unroll
+        for (int j = 0; j < kAngles; ++j) {
+            a.cosine[j] = turned ? a.cosine[j] : 1.f;
+            a.sine[j] = !turned ? 0.f : d0 < t.half ? -a.sine[j] : a.sine[j];
+        }
+    }
+
     // The lane's columns of a row, normed if `norm` (else all weights are 1), and turned.  All lanes of a row take
     // part.
     __device__ __forceinline__ void finish(const Turn &t, const Vec &v, bool norm, const Weights &w, const Angles &a,

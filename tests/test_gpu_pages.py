@@ -575,6 +575,22 @@ def test_attend_chosen_before_the_window():
         ref.check(out, want[0], want[2], "out")
 
 
+@pytest.mark.parametrize("k_scale,v_scale", [(1.0, 0.37), (3.3, 2.0**-70), (1e-30, 3e30), (2.0**-10, 7e-4)])
+def test_rotate_stores_what_append_does(k_scale, v_scale):
+    """Without norms and a rotation an e4m3 cache holds the same bytes after either, whatever the scales."""
+    c = ref.Case(2, 2, 64, 16, [300, 17], [290, 3], fp8=True, seed=22)
+    _, flat, q, k, v, tables, lens, starts = c.device()
+    k, v = ((x.double() * s).clamp(-3e38, 3e38).to(BF16) for x, s in ((k, k_scale), (v, v_scale)))
+    k[0, 0, :4] = torch.tensor([float("inf"), -float("inf"), 0.0, -0.0], dtype=BF16)
+    caches = []
+    for f in (attend.kv_append, lambda cache, layer, *x, **kw: attend.kv_rotate(cache, layer, q, *x, **kw)):
+        cache, flat, *_ = c.device()
+        f(cache, 0, k, v, tables, lens, starts, k_scale=k_scale, v_scale=v_scale)
+        torch.cuda.synchronize()
+        caches.append(flat.cpu())
+    same_bytes(caches[0], caches[1], "cache")
+
+
 def test_rotate_many_in_place():
     """Queries that are overwritten, while a workgroup has the next ones on their way."""
     c = ref.Case(2, 5, 64, 16, [700, 90], [650, 33], seed=21)
