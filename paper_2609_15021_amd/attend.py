@@ -507,7 +507,7 @@ def kv_attend(cache: Cache, layer: int, q, tables, lens, starts=None, *, max_q=N
     if lse is not None:
         _floats(lse, "lse", device, heads)
     key = (layout.num_kv_heads, layout.head_dim, layout.elem_bytes, layout.block_size, B, max_q, tokens, most, window,
-           weights is None, q_heads, budget)
+           weights is None, q_heads, budget, by is None)
     need = _attend_bytes.get(key)
     at, plain = ctypes.byref(cache.struct), by is None and chosen is None
     if plain:

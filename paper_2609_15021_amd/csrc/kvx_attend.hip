@@ -112,7 +112,8 @@ kv_status check_pages(const kv_cache *cache, const kv_batch *batch, const kv_att
 // How a call is cut, and what its workspace holds.  Only the host's numbers count.
 struct Plan {
     int32_t max_queries, max_rows;  // of a sequence; rows per KV head in the step kernel
-    bool tail;                      // some sequence may have more than kStepRows rows
+    int32_t step_rows;              // the most that the step kernel takes
+    bool tail;                      // some sequence may have more than that
     bool scores;                    // weights_out from the step kernel's scores
     bool listed;                    // the step kernel's parts are listed by a kernel
     int64_t score_len, lists, step_stats, step_sums, tail_stats, tail_sums, scores_at, bytes;
@@ -156,7 +157,14 @@ Parts tail_parts_for(int64_t longest, int64_t have, int64_t launched, int64_t he
     return p;
 }
 
-Plan plan_of(const kv_cache *cache, const kv_batch *batch, const kv_attend_options *o, const kv_rows *q) {
+// Rounds of 128 tokens of a tile that the step kernel takes of sequences with many rows over scaled pages, where the tail
+// kernel would leave most CUs idle: 56 new tokens of each of 2 sequences of 129 (3 heads of 5 rows, D 80) take 14 us
+// instead of 19, 18 of each of 7 sequences of 430 (420 rounds; 3 heads of 8 rows, D 128) 20.5 instead of 24, 24 of each
+// of 4 of 512 (576; 4 heads of 6 rows, D 256) 24 instead of 31; but 32 of each of 4 of 512 (1,024; 8 heads of 8 rows)
+// 37 instead of 25.
+constexpr int64_t kStepRounds = 640;
+
+Plan plan_of(const kv_cache *cache, const kv_batch *batch, const kv_attend_options *o, const kv_rows *q, bool scaled) {
     const int64_t H = cache->layout.num_kv_heads, D = cache->layout.head_dim, group = q->heads / H;
     const int64_t heads = batch->num_seqs * H;
     Plan p{};
@@ -164,8 +172,16 @@ Plan plan_of(const kv_cache *cache, const kv_batch *batch, const kv_attend_optio
     if (heads == 0 || p.max_queries == 0)
         return p;
     const int64_t all_rows = p.max_queries * group;
-    p.max_rows = static_cast<int32_t>(std::min<int64_t>(all_rows, kStepRows));
-    p.tail = all_rows > kStepRows;
+    p.step_rows = kStepRows;
+    if (scaled && all_rows > kStepRows) {
+        const int64_t tile = step_tile_rows(kStepRows, static_cast<int>(D));
+        const int64_t seen = o->window > 0 ? o->window + int64_t{p.max_queries} + 31 : batch->max_len;
+        const int64_t rounds = (std::min<int64_t>(seen, batch->max_len) + 127) / 128;
+        if ((all_rows + tile - 1) / tile * heads * rounds <= kStepRounds)
+            p.step_rows = static_cast<int32_t>(all_rows);
+    }
+    p.max_rows = static_cast<int32_t>(std::min<int64_t>(all_rows, p.step_rows));
+    p.tail = all_rows > p.step_rows;
     // With more rows than a tile has the scores would outgrow K itself: they are taken again instead.  So they are
     // where the host's bounds, which may be far above what the sequences hold, would ask for more than 1 GiB of them.
     p.score_len = round_up(batch->max_len, 32);
@@ -174,13 +190,14 @@ Plan plan_of(const kv_cache *cache, const kv_batch *batch, const kv_attend_optio
     // 2-byte rows), or one for each sequence where that is more.
     const int64_t tile = step_tile_rows(p.max_rows, static_cast<int>(D)), tiles = (p.max_rows + tile - 1) / tile;
     const int64_t at_once = D <= 64 ? 768 : D > 128 && cache->layout.elem_bytes == 2 ? 256 : 512;
-    const int64_t window = o->window > 0 ? o->window + int64_t{kStepRows} + 31 : batch->max_len;
+    const int64_t window = o->window > 0 ? o->window + int64_t{p.max_rows} + 31 : batch->max_len;
     const int64_t longest = std::max<int64_t>(std::min<int64_t>(window, batch->max_len), 1);
     // A part has 32 tokens a wave at least; where the sequences alone fill the chip, enough that splitting and joining
     // take less than the wait for a long one does (2,000 sequences of up to 300 tokens: 82 us whole, 129 in parts).
     Shares &s = p.shares;
     s.shortest = heads * tiles >= at_once ? 512 : 128;
     const int64_t most = (longest + s.shortest - 1) / s.shortest * batch->num_seqs;  // parts that can be
+    s.most = static_cast<int32_t>((longest + s.shortest - 1) / s.shortest);
     s.num_seqs = batch->num_seqs;
     // (Many sequences are cut for three rounds of workgroups, of which the last may be nearly empty: 64 of up to 4,096
     // tokens on 8 heads take 143 us in one to one and a half rounds, 136 in three.)
@@ -279,7 +296,7 @@ kv_status attend(const kv_cache *cache, int32_t layer, const kv_batch *batch, co
                                 (batch->num_queries > 0 && out->heads > 1 && out->head_stride < D)))
         return fail(KV_EINVAL, "rows of out (strides %lld and %lld) are shorter than %d elements",
                     static_cast<long long>(out->token_stride), static_cast<long long>(out->head_stride), D);
-    const Plan plan = list ? Plan{} : plan_of(cache, batch, o, q);
+    const Plan plan = list ? Plan{} : plan_of(cache, batch, o, q, scales != nullptr);
     const PagesPlan listed = list ? plan_of(cache, batch, list, q) : PagesPlan{};
     const int64_t need = list ? listed.bytes : plan.bytes;
     if (list && int64_t{batch->num_queries} * listed.chosen.splits > (int64_t{1} << 23))
@@ -330,6 +347,7 @@ kv_status attend(const kv_cache *cache, int32_t layer, const kv_batch *batch, co
     a.q_type = q->dtype;
     a.cache_type = o->cache_dtype;
     a.full_weights = o->full_weights;
+    a.step_rows = plan.step_rows;
     a.by_group = divisor(a.group);
     a.scales = scales_of(scales);
     if (list) {
@@ -373,7 +391,7 @@ int64_t kv_attend_workspace(const kv_cache *cache, const kv_batch *batch, const 
     const kv_status st = kvx::guarded([&]() -> kv_status {
         const kv_status checked = kvx::check_attend(cache, batch, options, q);
         if (checked == KV_OK)
-            bytes = kvx::plan_of(cache, batch, options, q).bytes;
+            bytes = kvx::plan_of(cache, batch, options, q, false).bytes;
         return checked;
     });
     return st == KV_OK ? bytes : st;
@@ -396,7 +414,8 @@ int64_t kv_attend_pages_workspace(const kv_cache *cache, const kv_batch *batch, 
         if (checked == KV_OK)
             checked = kvx::check_pages(cache, batch, options, scales, list);
         if (checked == KV_OK)
-            bytes = list ? kvx::plan_of(cache, batch, list, q).bytes : kvx::plan_of(cache, batch, options, q).bytes;
+            bytes = list ? kvx::plan_of(cache, batch, list, q).bytes
+                         : kvx::plan_of(cache, batch, options, q, true).bytes;
         return checked;
     });
     return st == KV_OK ? bytes : st;

@@ -28,6 +28,7 @@ struct AttendArgs {
     Divisor by_group;
     int32_t q_type, cache_type;
     int32_t full_weights;
+    int32_t step_rows;  // rows per KV head that the step kernel takes of a sequence at most
     float *scores;  // [sequence][KV head][score_cap][score_len] in powers of 2, for weights_out; or NULL
     int64_t score_len;
     int32_t score_cap;
@@ -69,6 +70,7 @@ struct Shares {
     int32_t target, items, num_seqs;  // items >= the parts of any batch
     int32_t shortest;                 // tokens of a part at least
     int32_t alone;                    // every sequence is one part
+    int32_t most;                     // parts of a sequence at most
     int32_t row_cap;                  // most rows per KV head of a sequence
     float *sums;                      // [KV head][item][row_cap][D], unscaled
     float *stats;                     // [KV head][item][row_cap][2]: largest score and sum, in powers of 2
@@ -102,7 +104,7 @@ __device__ __forceinline__ int share_tokens(const AttendArgs &a, int b, bool tel
                       nq <= a.batch.max_queries;
     if (!good && tell)
         report(a.pages.err, KV_ASYNC_BAD_BATCH);
-    rows = good && nq > 0 && nq <= kStepRows && nq * a.group <= kStepRows;
+    rows = good && nq > 0 && nq <= a.step_rows && nq * a.group <= a.step_rows;
     if (!rows)
         return 0;
     const Span span = span_of(n, nq, 0, nq, a.window);

@@ -14,7 +14,7 @@
 namespace kvx {
 
 hipError_t launch_step_scaled(const AttendArgs &a, const Shares &shares, int max_queries, hipStream_t stream) {
-    const int max_rows = static_cast<int>(std::min<int64_t>(kStepRows, static_cast<int64_t>(max_queries) * a.group));
+    const int max_rows = static_cast<int>(std::min<int64_t>(a.step_rows, static_cast<int64_t>(max_queries) * a.group));
     return a.q_type == KV_DTYPE_BF16 ? launch_rows<Bf16, true, true>(a, shares, shares.items, max_rows, stream)
                                      : launch_rows<F16, true, true>(a, shares, shares.items, max_rows, stream);
 }

@@ -270,7 +270,7 @@ hipError_t launch_share(const AttendArgs &a, const Shares &shares, hipStream_t s
 }
 
 hipError_t launch_step(const AttendArgs &a, const Shares &shares, int max_queries, hipStream_t stream) {
-    const int max_rows = static_cast<int>(std::min<int64_t>(kStepRows, static_cast<int64_t>(max_queries) * a.group));
+    const int max_rows = static_cast<int>(std::min<int64_t>(a.step_rows, static_cast<int64_t>(max_queries) * a.group));
     const bool fp8 = a.cache_type == KV_DTYPE_E4M3;
     if (a.q_type == KV_DTYPE_BF16)
         return fp8 ? launch_rows<Bf16, true, false>(a, shares, shares.items, max_rows, stream)
@@ -280,7 +280,10 @@ hipError_t launch_step(const AttendArgs &a, const Shares &shares, int max_querie
 }
 
 hipError_t launch_join_step(const AttendArgs &a, const Shares &shares, int max_queries, hipStream_t stream) {
-    return launch_join<true>(a, shares, std::min(max_queries, std::max(kStepRows / a.group, 1)), stream);
+    const int most = std::min(max_queries, std::max(a.step_rows / a.group, 1));
+    const int64_t rows = int64_t{most} * a.heads * a.num_seqs;
+    return a.scales.data && shares.most <= 8 && rows >= 1024 ? launch_join<false>(a, shares, most, stream)
+                                            : launch_join<true>(a, shares, most, stream);
 }
 
 hipError_t launch_join_tail(const AttendArgs &a, const Parts &parts, int max_queries, hipStream_t stream) {

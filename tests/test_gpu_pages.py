@@ -274,6 +274,21 @@ def test_attend_scaled(H, G, D, BS, nhd, dtype, lens, new):
     run_scaled(pref.ScaledCase(H, G, D, BS, lens, new, nhd=nhd, dtype=dtype, seed=7 * D + G))
 
 
+@pytest.mark.parametrize("lens,new", [([40, 300, 70], [2, 67, 70]), ([70, 129], [70, 129]), ([513, 0], [256, 0]),
+                                      ([260, 255, 800], [130, 129, 5])])
+@pytest.mark.parametrize("H,G,D,BS,nhd,dtype", [(2, 1, 64, 16, False, BF16), (1, 5, 128, 16, False, F16),
+                                                (1, 6, 256, 32, True, BF16), (1, 3, 80, 24, True, F16),
+                                                (2, 2, 192, 7, False, BF16), (1, 20, 16, 1, False, F16),
+                                                (1, 4, 256, 12, False, F16)])
+def test_attend_scaled_within_wide_bounds(H, G, D, BS, nhd, dtype, lens, new):
+    """The host's bounds leave room for far longer sequences, which would need many tiles."""
+    c = pref.ScaledCase(H, G, D, BS, lens, new, nhd=nhd, dtype=dtype, seed=7 * D + G)
+    wide = torch.full((len(lens), 100000 // BS), -1, dtype=torch.int32)
+    wide[:, :c.tables.shape[1]] = c.tables
+    c.tables = wide
+    run_scaled(c)
+
+
 OPTIONS = [dict(softcap=5.0), dict(softcap=100.0), dict(window=1), dict(window=37), dict(slopes=True),
            dict(softcap=2.0, window=50, slopes=True, scale=0.3)]
 
@@ -286,6 +301,17 @@ def test_attend_scaled_options(new, dtype, options):
     if options.get("slopes"):
         options["slopes"] = [2.0**-(1 + i % 7) for i in range(8)]
     c = pref.ScaledCase(2, 4, 128, 16, [300, 200, 129, 64], new, dtype=dtype, seed=11)
+    run_scaled(c, options)
+    run_scaled(c, options, full_weights=True)
+
+
+@pytest.mark.parametrize("options", OPTIONS)
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_attend_scaled_options_of_many_rows(dtype, options):
+    options = dict(options)
+    if options.get("slopes"):
+        options["slopes"] = [2.0**-(1 + i % 7) for i in range(16)]
+    c = pref.ScaledCase(4, 4, 128, 16, [300, 200, 129, 64], [1, 200, 17, 64], dtype=dtype, seed=23)
     run_scaled(c, options)
     run_scaled(c, options, full_weights=True)
 
