@@ -605,18 +605,22 @@ def kv_score(bounds: Cache, layer: int, q, tables, lens, starts=None, *, block_s
     handle, here = _call_stream(stream)
     with here:
         if out is None:
-            out, _ = _tensors.empty(q, 1, tokens, heads, pages)
+            out, out_at = _tensors.empty(q, 1, tokens, heads, pages)
+            token, head = heads * pages, pages
+        else:
+            _weights(out, "out", device, (tokens, heads))
+            if out.shape[2] < pages:
+                raise ValueError(f"out of {out.shape[2]} pages for sequences of up to {pages}")
+            out_at, (token, head, _) = out.data_ptr(), out.stride()
         if counts is None:
-            counts = _tensors.empty(q, 2, tokens)[0] if starts is None else q.new_zeros(tokens, dtype=torch.int32)
-    _weights(out, "out", device, (tokens, heads))
-    if out.shape[2] < pages:
-        raise ValueError(f"out of {out.shape[2]} pages for sequences of up to {pages}")
-    token, head, _ = out.stride()
+            counts, counts_at = (_tensors.empty if starts is None else _tensors.zeros)(q, 2, tokens)
+        else:
+            counts_at = _dense_ints(counts, "counts", 1, device, tokens)
     by = None if scales is None else KvPageScales(*_page_scales(scales, bounds, device))
     options = _pack_score(_cache_dtype(bounds, dtype, q), block_size, _factor(scale, "scale"), 0,
                           0 if by is None else ctypes.addressof(by), token, head)
-    _raise(_lib.kv_score(ctypes.byref(bounds.struct), _int32(layer, "layer"), batch, options, qr,
-                         out.data_ptr(), _dense_ints(counts, "counts", 1, device, tokens), handle))
+    _raise(_lib.kv_score(ctypes.byref(bounds.struct), _int32(layer, "layer"), batch, options, qr, out_at, counts_at,
+                         handle))
     if stream is not None:
         _used(stream, q, tables, lens, starts, scales, out, counts)
     return out, counts

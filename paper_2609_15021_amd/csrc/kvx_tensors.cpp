@@ -221,11 +221,12 @@ PyObject *failed(const std::exception &e) {
     return nullptr;
 }
 
-// empty(like, type, sizes...): (a contiguous tensor on like's device, its address); type: 0 like's, 1 float32, 2 int32,
-// 3 bytes
-PyObject *empty(PyObject *, PyObject *const *args, Py_ssize_t count) {
+// empty(like, type, sizes...), zeros(...): (a contiguous tensor on like's device, its address); type: 0 like's, 1
+// float32, 2 int32, 3 bytes
+template <bool ZEROS>
+PyObject *make(PyObject *, PyObject *const *args, Py_ssize_t count) {
     if (count < 3 || count > 5 || !THPVariable_Check(args[0])) {
-        PyErr_SetString(PyExc_TypeError, "empty(tensor, type, sizes...)");
+        PyErr_SetString(PyExc_TypeError, "a tensor, a type, and up to 3 sizes are needed");
         return nullptr;
     }
     const at::Tensor &like = THPVariable_Unpack(args[0]);
@@ -240,7 +241,10 @@ PyObject *empty(PyObject *, PyObject *const *args, Py_ssize_t count) {
                               : type == 2 ? at::kInt
                                           : at::kByte;
     try {
-        at::Tensor t = at::empty(at::IntArrayRef(sizes, static_cast<size_t>(count - 2)), like.options().dtype(of));
+        const at::IntArrayRef shape(sizes, static_cast<size_t>(count - 2));
+        at::Tensor t = at::empty(shape, like.options().dtype(of));
+        if (ZEROS)
+            t.zero_();
         const auto address = static_cast<unsigned long long>(reinterpret_cast<uintptr_t>(t.data_ptr()));
         PyObject *wrapped = THPVariable_Wrap(std::move(t));
         return wrapped ? Py_BuildValue("(NK)", wrapped, address) : nullptr;
@@ -266,7 +270,8 @@ PyMethodDef methods[] = {
     {"scales", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(guarded<scales>)), METH_FASTCALL, nullptr},
     {"lists", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(guarded<lists>)), METH_FASTCALL, nullptr},
     {"rotation", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(guarded<rotation>)), METH_FASTCALL, nullptr},
-    {"empty", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(empty)), METH_FASTCALL, nullptr},
+    {"empty", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(make<false>)), METH_FASTCALL, nullptr},
+    {"zeros", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(make<true>)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tensors", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
