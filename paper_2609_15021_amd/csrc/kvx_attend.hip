@@ -114,6 +114,7 @@ struct Plan {
     int32_t max_queries, max_rows;  // of a sequence; rows per KV head in the step kernel
     int32_t step_rows;              // the most that the step kernel takes
     bool tail;                      // some sequence may have more than that
+    bool step;                      // the tail kernel does not take the others too
     bool scores;                    // weights_out from the step kernel's scores
     bool listed;                    // the step kernel's parts are listed by a kernel
     int64_t score_len, lists, step_stats, step_sums, tail_stats, tail_sums, scores_at, bytes;
@@ -163,6 +164,12 @@ Parts tail_parts_for(int64_t longest, int64_t have, int64_t launched, int64_t he
 // of 4 of 512 (576; 4 heads of 6 rows, D 256) 24 instead of 31; but 32 of each of 4 of 512 (1,024; 8 heads of 8 rows)
 // 37 instead of 25.
 constexpr int64_t kStepRounds = 640;
+// Tokens that rows over scaled pages see, up to which the tail kernel takes all sequences, with full_weights, where
+// bounds ask for it at all: the step kernel and its join would be two launches more.  32 sequences of up to 48 new
+// tokens of up to 512 (8 heads of 5 rows, D 128) take 33 us instead of 46, 24 of up to 43 (3 heads of 8 rows) 11
+// instead of 20, 8 prompts of up to 512 (4 heads of 6 rows, D 256) 41 instead of 45; but 8 prompts of up to 1,024 (8 heads
+// of 5 rows, D 128) 79 instead of 75.
+constexpr int64_t kTailAlone = 512;
 
 Plan plan_of(const kv_cache *cache, const kv_batch *batch, const kv_attend_options *o, const kv_rows *q, bool scaled) {
     const int64_t H = cache->layout.num_kv_heads, D = cache->layout.head_dim, group = q->heads / H;
@@ -173,12 +180,15 @@ Plan plan_of(const kv_cache *cache, const kv_batch *batch, const kv_attend_optio
         return p;
     const int64_t all_rows = p.max_queries * group;
     p.step_rows = kStepRows;
+    p.step = true;
     if (scaled && all_rows > kStepRows) {
         const int64_t tile = step_tile_rows(kStepRows, static_cast<int>(D));
-        const int64_t seen = o->window > 0 ? o->window + int64_t{p.max_queries} + 31 : batch->max_len;
-        const int64_t rounds = (std::min<int64_t>(seen, batch->max_len) + 127) / 128;
-        if ((all_rows + tile - 1) / tile * heads * rounds <= kStepRounds)
+        const int64_t window = o->window > 0 ? o->window + int64_t{p.max_queries} + 31 : batch->max_len;
+        const int64_t seen = std::min<int64_t>(window, batch->max_len);
+        if ((all_rows + tile - 1) / tile * heads * ((seen + 127) / 128) <= kStepRounds)
             p.step_rows = static_cast<int32_t>(all_rows);
+        else
+            p.step = seen > kTailAlone;
     }
     p.max_rows = static_cast<int32_t>(std::min<int64_t>(all_rows, p.step_rows));
     p.tail = all_rows > p.step_rows;
@@ -221,8 +231,8 @@ Plan plan_of(const kv_cache *cache, const kv_batch *batch, const kv_attend_optio
         at += round_up(bytes, 16);
         return here;
     };
-    const int64_t shared = s.alone ? 0 : H * s.items * s.row_cap;
-    p.listed = !s.alone && s.num_seqs > kShareSeqs;
+    const int64_t shared = s.alone || !p.step ? 0 : H * s.items * s.row_cap;
+    p.listed = p.step && !s.alone && s.num_seqs > kShareSeqs;
     p.lists = take(p.listed ? (2 + 2 * (int64_t{s.num_seqs} + s.items)) * 4 : 0);
     p.step_stats = take(shared * 8);
     p.step_sums = take(shared * D * 4);
@@ -346,8 +356,9 @@ kv_status attend(const kv_cache *cache, int32_t layer, const kv_batch *batch, co
     a.num_seqs = batch->num_seqs;
     a.q_type = q->dtype;
     a.cache_type = o->cache_dtype;
-    a.full_weights = o->full_weights;
+    a.full_weights = o->full_weights || !plan.step;
     a.step_rows = plan.step_rows;
+    a.tail_above = plan.step ? kStepRows : 0;
     a.by_group = divisor(a.group);
     a.scales = scales_of(scales);
     if (list) {
@@ -361,12 +372,14 @@ kv_status attend(const kv_cache *cache, int32_t layer, const kv_batch *batch, co
         return KV_OK;
     }
     if (plan.max_queries > 0) {
-        if (plan.listed)
-            KVX_HIP(launch_share(a, step, stream));
-        KVX_HIP(scales ? launch_step_scaled(a, step, plan.max_queries, stream)
-                       : launch_step(a, step, plan.max_queries, stream));
-        if (!step.alone)
-            KVX_HIP(launch_join_step(a, step, plan.max_queries, stream));
+        if (plan.step) {
+            if (plan.listed)
+                KVX_HIP(launch_share(a, step, stream));
+            KVX_HIP(scales ? launch_step_scaled(a, step, plan.max_queries, stream)
+                           : launch_step(a, step, plan.max_queries, stream));
+            if (!step.alone)
+                KVX_HIP(launch_join_step(a, step, plan.max_queries, stream));
+        }
         if (plan.tail) {
             KVX_HIP(scales ? launch_tail_scaled(a, tail, plan.max_queries, stream)
                            : launch_tail(a, tail, plan.max_queries, stream));

@@ -29,6 +29,7 @@ struct AttendArgs {
     int32_t q_type, cache_type;
     int32_t full_weights;
     int32_t step_rows;  // rows per KV head that the step kernel takes of a sequence at most
+    int32_t tail_above; // the tail kernel takes sequences of more rows than these
     float *scores;  // [sequence][KV head][score_cap][score_len] in powers of 2, for weights_out; or NULL
     int64_t score_len;
     int32_t score_cap;
@@ -214,7 +215,7 @@ __device__ __forceinline__ bool tile_of_rank(const AttendArgs &a, int rank, int 
             report(a.pages.err, KV_ASYNC_BAD_BATCH);
         nq = good ? q1 - q0 : 0;
         past = n - nq;
-        tiles = nq * a.group > kStepRows ? (nq * a.group + kTailRows - 1) / kTailRows : 0;
+        tiles = nq * a.group > a.tail_above ? (nq * a.group + kTailRows - 1) / kTailRows : 0;
     }
     // Tiles of a sequence that end at `end` or behind: from the one on that has a row of token end - 1.
     const auto from = [&](int64_t end, int past, int nq, int tiles) {

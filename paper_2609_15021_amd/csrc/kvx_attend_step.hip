@@ -100,7 +100,7 @@ __device__ __forceinline__ Row parts_at(const AttendArgs &a, const Shares &from,
 }
 __device__ __forceinline__ Row parts_at(const AttendArgs &a, const Parts &from, int, int h, int r, const Sequence &seq) {
     const int rows = seq.nq * a.group, row0 = r - r % kTailRows;
-    if (rows <= kStepRows)
+    if (rows <= a.tail_above)
         return Row{0, 0, 0};
     const Span span = span_of(seq.n, seq.nq, divide(row0, a.by_group),
                               divide(min(row0 + kTailRows, rows) - 1, a.by_group) + 1, a.window);

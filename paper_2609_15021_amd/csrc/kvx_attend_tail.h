@@ -120,7 +120,7 @@ __global__ __launch_bounds__(64 * kRows / RW, 2) void tail_kernel(const AttendAr
     if (!sequence(a.batch, b, pg.err, seq))
         return;
     const int rows = seq.nq * a.group, row0 = tile * kRows;
-    if (row0 >= rows || rows <= kStepRows)
+    if (row0 >= rows || rows <= a.tail_above)
         return;
     const int i0 = divide(row0, a.by_group), i1 = divide(min(row0 + kRows, rows) - 1, a.by_group) + 1;
     const Span span = span_of(seq.n, seq.nq, i0, i1, a.window);

@@ -289,6 +289,13 @@ def test_attend_scaled_within_wide_bounds(H, G, D, BS, nhd, dtype, lens, new):
     run_scaled(c)
 
 
+@pytest.mark.parametrize("H,G,D,BS,dtype", [(8, 5, 64, 16, BF16), (6, 8, 128, 7, F16), (4, 6, 256, 32, BF16)])
+def test_attend_scaled_short_prompts(H, G, D, BS, dtype):
+    """Whole prompts beside single tokens, rows before token 0, and sequences without rows, of few tokens each."""
+    lens = [130, 1, 64, 200, 3, 0, 90, 250]
+    run_scaled(pref.ScaledCase(H, G, D, BS, lens, [130, 1, 2, 67, 5, 0, 0, 250], dtype=dtype, seed=H))
+
+
 OPTIONS = [dict(softcap=5.0), dict(softcap=100.0), dict(window=1), dict(window=37), dict(slopes=True),
            dict(softcap=2.0, window=50, slopes=True, scale=0.3)]
 
@@ -303,6 +310,16 @@ def test_attend_scaled_options(new, dtype, options):
     c = pref.ScaledCase(2, 4, 128, 16, [300, 200, 129, 64], new, dtype=dtype, seed=11)
     run_scaled(c, options)
     run_scaled(c, options, full_weights=True)
+
+
+@pytest.mark.parametrize("options", [dict(softcap=5.0), dict(window=600), dict(window=570, slopes=True, softcap=20.0)])
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_attend_scaled_options_of_longer_tails(dtype, options):
+    options = dict(options)
+    if options.get("slopes"):
+        options["slopes"] = [2.0**-(1 + i % 7) for i in range(16)]
+    c = pref.ScaledCase(4, 4, 64, 16, [900, 700, 64], [1, 200, 17], dtype=dtype, seed=24)
+    run_scaled(c, options)
 
 
 @pytest.mark.parametrize("options", OPTIONS)
