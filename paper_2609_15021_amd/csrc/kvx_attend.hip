@@ -276,8 +276,9 @@ PagesPlan plan_of(const kv_cache *cache, const kv_batch *batch, const kv_page_li
     p.chosen.splits = static_cast<int32_t>((longest + p.chosen.len - 1) / p.chosen.len);
     // A wave to a row where that still fills the chip.  With up to 128 tokens, of which a workgroup's waves would have
     // a round each, from twice the workgroups on (128 rows of 8 heads, 8 pages of 16: 10 us instead of 15; 512 rows, 34
-    // instead of 59); with more from 8 times on (256 rows, 64 pages: 123 instead of 114; 512 rows, 201 and 203).
-    p.alone = p.chosen.splits == 1 && groups >= (likely <= 128 ? 2 : 8) * at_once;
+    // instead of 59); with more from 4 times on (256 rows, 64 pages: 84 us instead of 104, in e4m3 with D 256 95 instead
+    // of 122; 128 rows, 60 instead of 54).
+    p.alone = p.chosen.splits == 1 && groups >= (likely <= 128 ? 2 : 4) * at_once;
     const int64_t split = p.chosen.splits > 1 ? heads * p.chosen.splits : 0;
     const int64_t lse = round_up(heads * 4, 16);
     p.stats = lse;
@@ -309,7 +310,7 @@ kv_status attend(const kv_cache *cache, int32_t layer, const kv_batch *batch, co
     const Plan plan = list ? Plan{} : plan_of(cache, batch, o, q, scales != nullptr);
     const PagesPlan listed = list ? plan_of(cache, batch, list, q) : PagesPlan{};
     const int64_t need = list ? listed.bytes : plan.bytes;
-    if (list && int64_t{batch->num_queries} * listed.chosen.splits > (int64_t{1} << 23))
+    if (list && int64_t{batch->num_queries} * listed.chosen.splits * cache->layout.num_kv_heads > (int64_t{1} << 23))
         return fail(KV_EUNSUPPORTED, "%d new tokens that chose pages are too many for one call", batch->num_queries);
     if (workspace_bytes < need || (need > 0 && !workspace))
         return fail(KV_EINVAL, "workspace of %lld bytes; %lld are needed", static_cast<long long>(workspace_bytes),

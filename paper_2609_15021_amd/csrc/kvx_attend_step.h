@@ -57,7 +57,9 @@ __device__ __forceinline__ int64_t slot_in(const Chosen &chosen, int, int, int64
 // From: Shares, or Chosen: each new token is a sequence of its own, of the pages that it chose, one after the other.  A
 // page's place in the list says where its tokens are, and which: the list is read a round before the table.  Or Alone:
 // the same where there are rows enough for every wave to have one for itself, and nothing to join: 111 new tokens of
-// each of 17 sequences over one page of 32 (3 heads of 12 rows, D 256) take 30 us instead of 103.
+// each of 17 sequences over one page of 32 (3 heads of 12 rows, D 256) take 30 us instead of 103.  Heads run fastest in
+// their grid, so that a head's workgroups come 8 apart where there are 8 heads, and so on one XCD, whose L2 then has
+// that head's pages alone: 512 new tokens over 64 of 2,048 pages each take 160 us instead of 204.
 template <class T, bool FP8, int DP, int NT, bool SCALED, class From>
 __global__ __launch_bounds__(64 * kWaves, !FP8 && DP > 128 ? 1 : 2) void step_kernel(const AttendArgs a,
                                                                                      const From shares) {
@@ -72,14 +74,15 @@ __global__ __launch_bounds__(64 * kWaves, !FP8 && DP > 128 ? 1 : 2) void step_ke
     const Pages &pg = a.pages;
     const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int tile = blockIdx.y / pg.H, h = blockIdx.y - tile * pg.H;
+    const int across = LISTED ? blockIdx.x : blockIdx.y, place = across / pg.H, h = across - place * pg.H;
+    const int tile = LISTED ? blockIdx.y : place;
     Share share;
     Sequence seq;
     [[maybe_unused]] int count = 0;                          // LISTED: pages of the list
     [[maybe_unused]] const int32_t *list = nullptr;
     [[maybe_unused]] int first_entry = 0;
     if constexpr (LISTED) {
-        const int item = ALONE ? blockIdx.x * kWaves + wave : blockIdx.x, row = ALONE ? item : item / shares.splits;
+        const int item = ALONE ? place * kWaves + wave : place, row = ALONE ? item : item / shares.splits;
         if (ALONE && row >= a.batch.num_queries)
             return;
         share.split = ALONE ? 0 : item - row * shares.splits;
@@ -551,8 +554,8 @@ template <class T, bool FP8, int DP, int NT, bool SCALED, class From>
 hipError_t launch_tiles(const AttendArgs &a, const From &from, int items, int max_rows, hipStream_t stream) {
     const int tiles = (max_rows + 16 * NT - 1) / (16 * NT);
     const int groups = std::is_same_v<From, Alone> ? (items + kWaves - 1) / kWaves : items;
-    return launch_kernel(step_kernel<T, FP8, DP, NT, SCALED, From>, dim3(groups, tiles * a.pages.H), 64 * kWaves, stream,
-                         a, from);
+    const dim3 grid = std::is_base_of_v<Chosen, From> ? dim3(groups * a.pages.H, tiles) : dim3(groups, tiles * a.pages.H);
+    return launch_kernel(step_kernel<T, FP8, DP, NT, SCALED, From>, grid, 64 * kWaves, stream, a, from);
 }
 
 // `items` workgroups (Alone: waves) for each KV head and tile of up to max_rows rows.
