@@ -13,7 +13,7 @@
 // Scores: a wave holds the bounds of 16 or 32 pages in registers as the products' second operand (column: page), and
 // goes over its share of the rows, 16 (new token, query head) at a time, as the first.  A token's heads are padded to a
 // power of two by repeating the last, so that the largest over them lies in a lane's 4 results, or one or two shuffles
-// away.  8,193 pages of 8 heads of 5 rows (34 MB, D 128): 8.9 us, of which reading takes 5.6 and table, bounds and
+// away.  8,193 pages of 8 heads of 5 rows (34 MB, D 128): 8.7 us, of which reading takes 5.6 and table, bounds and
 // products come one after the other.  Tails of up to 517 tokens over 1,057 pages, 3 sequences, 2 heads of 8 rows: 20
 // us, where the products alone would take 6: a wave's share of tiles is short, and its start (lengths, table, bounds)
 // and every second tile's wait for the workgroup are not hidden.
@@ -227,8 +227,8 @@ struct ScoreArgs {
     int64_t token_stride, head_stride;  // elements
     float scale;
     int32_t BS, group, pad, shift;      // tokens of a page; query heads of a KV head, padded to 2^shift, up to 16
-    int32_t page_chunks, tokens;        // of a launch's first dimension; tokens of a workgroup
-    Divisor by_bs, by_chunks, by_subs;
+    int32_t shares, tokens;             // workgroups that share a sequence's tokens; tokens of each
+    Divisor by_bs, by_shares, by_subs;
 };
 
 // Workgroups that tails are shared out to: 20 us for the tails above; a third of them take 26, twice as many 24.
@@ -267,8 +267,10 @@ __global__ __launch_bounds__(kThreads, 2) void score_kernel(const ScoreArgs a) {
     __shared__ u32x4 lds[2 * kQueries > WAVES * kBounds ? 2 * kQueries : WAVES * kBounds];
     const Pages &pg = a.bounds;
     const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4, wave = tid >> 6;
-    const int h = blockIdx.y, b = blockIdx.z;
-    const int share = divide(blockIdx.x, a.by_chunks), chunk = blockIdx.x - share * a.page_chunks;
+    // (Heads run fastest, so that a head's workgroups come 8 apart where there are 8 heads, and so on one XCD, and then
+    // the shares that read the same bounds: 512 new tokens over 2,048 pages, 8 heads of 5 rows, 55 us instead of 59.)
+    const int b = blockIdx.y, place = blockIdx.x / pg.H, h = blockIdx.x - place * pg.H;
+    const int chunk = divide(place, a.by_shares), share = place - chunk * a.shares;
     const int page0 = (chunk * WAVES + wave) * 16 * PG;
     // (The table is read, within what may be, while the sequence is looked up.)
     int blocks[PG];
@@ -475,11 +477,10 @@ hipError_t launch_score(ScoreArgs a, int num_seqs, int most, int64_t pages, hipS
     const int64_t all = std::min(tiles * num_seqs, (int64_t{a.batch.num_queries} + each - 1) / each + num_seqs);
     const int64_t share = std::max<int64_t>(all * groups / kShareTarget, 1);
     a.tokens = static_cast<int32_t>(std::min((share + 1) / 2 * 2, tiles) * each);
-    a.page_chunks = static_cast<int32_t>(chunks);
-    a.by_chunks = divisor(chunks);
-    const int64_t grid = chunks * ((int64_t{most} + a.tokens - 1) / a.tokens);
-    return launch_score_to<T, FP8, DP, PG>(a, dim3(static_cast<uint32_t>(grid), static_cast<uint32_t>(a.bounds.H),
-                                                   static_cast<uint32_t>(num_seqs)), stream);
+    a.shares = static_cast<int32_t>((int64_t{most} + a.tokens - 1) / a.tokens);
+    a.by_shares = divisor(a.shares);
+    const int64_t grid = chunks * ((int64_t{most} + a.tokens - 1) / a.tokens) * a.bounds.H;
+    return launch_score_to<T, FP8, DP, PG>(a, dim3(static_cast<uint32_t>(grid), static_cast<uint32_t>(num_seqs)), stream);
 }
 
 template <class T, bool FP8>
@@ -537,9 +538,10 @@ kv_status score(const kv_cache *bounds, int32_t layer, const kv_batch *batch, co
                     static_cast<long long>(most_pages));
     if (!scores && most_pages > 0)
         return fail(KV_EINVAL, "scores must not be NULL");
-    if (most_pages > int64_t{1} << 29)
-        return fail(KV_EUNSUPPORTED, "%lld pages of a sequence in one call are too many",
-                    static_cast<long long>(most_pages));
+    // (Shares add at most kShareTarget workgroups and as many again.)
+    if ((most_pages + 63) / 64 * H > int64_t{1} << 21)
+        return fail(KV_EUNSUPPORTED, "%lld pages of %d heads of a sequence in one call are too many",
+                    static_cast<long long>(most_pages), H);
     st = check_on_current_device(bounds);
     int32_t *err = nullptr;
     if (st == KV_OK)
