@@ -14,7 +14,7 @@
 // goes over its share of the rows, 16 (new token, query head) at a time, as the first.  A token's heads are padded to a
 // power of two by repeating the last, so that the largest over them lies in a lane's 4 results, or one or two shuffles
 // away.  8,193 pages of 8 heads of 5 rows (34 MB, D 128): 8.7 us, of which reading takes 5.6 and table, bounds and
-// products come one after the other.  Tails of up to 517 tokens over 1,057 pages, 3 sequences, 2 heads of 8 rows: 20
+// products come one after the other.  Tails of up to 517 tokens over 1,057 pages, 3 sequences, 2 heads of 8 rows: 19
 // us, where the products alone would take 6: a wave's share of tiles is short, and its start (lengths, table, bounds)
 // and every second tile's wait for the workgroup are not hidden.
 #include <algorithm>
