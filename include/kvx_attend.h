@@ -216,9 +216,9 @@ KV_API int64_t kv_attend_workspace(const kv_cache *cache, const kv_batch *batch,
  * 1), where each new token attends over the pages alone that it chose (list), or both; one of them must be given.
  * Token t of a chosen page takes part where t <= p and, with window > 0, p - t < window, and slopes count in p - t, as
  * in kv_attend; a row that chose nothing that it sees gets 0 and -infinity, and pages that a row sees no token of are
- * not looked up in its table.  With a list a row's weights always meet V as two numbers, a V that is not finite reaches
- * no row that does not see it, and each row reads its pages for itself.  With scales, and with a list in any E4M3 cache,
- * the weights times V's scale are numbers of bfloat16; of float16 rows they are always two.  weights_in and weights_out
+ * not looked up in its table.  Weights always meet V as two numbers, whatever the rows and full_weights, so that only
+ * the output's rounding shows (with scales, and with a list in any E4M3 cache, in bfloat16).  With a list a V that is
+ * not finite reaches no row that does not see it, and each row reads its pages for itself.  weights_in and weights_out
  * must be NULL.  Errors as kv_attend; KV_EINVAL also for a list that contradicts the cache, KV_EUNSUPPORTED for
  * weights_out, more than 2^31 - 1024 tokens in `budget` pages, and more rows than one launch takes.
  */

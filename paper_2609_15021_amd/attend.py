@@ -460,7 +460,7 @@ def kv_attend(cache: Cache, layer: int, q, tables, lens, starts=None, *, max_q=N
     ``scales``: those of a float8_e4m3fn cache's pages, as kv_append_scaled leaves them.  ``pages`` (int32
     [tokens][H or 1][budget], dense rows) and ``counts`` (int32 [tokens]): each new token attends over the first
     ``counts`` of its ``pages`` alone, which are places in its sequence's table, as kv_keep chooses them from kv_score's
-    scores.  Neither goes with ``weights``.
+    scores.  Neither goes with ``weights``, and with either all rows are as with ``full_weights``.
     """
     device = cache.struct.device
     layout = cache.layout

@@ -164,8 +164,7 @@ Parts tail_parts_for(int64_t longest, int64_t have, int64_t launched, int64_t he
 // of 4 of 512 (576; 4 heads of 6 rows, D 256) 24 instead of 31; but 32 of each of 4 of 512 (1,024; 8 heads of 8 rows)
 // 37 instead of 25.
 constexpr int64_t kStepRounds = 640;
-// Tokens that rows over scaled pages see, up to which the tail kernel takes all sequences, with full_weights, where
-// bounds ask for it at all: the step kernel and its join would be two launches more.  32 sequences of up to 48 new
+// Tokens that rows over scaled pages see, up to which the tail kernel takes all sequences where bounds ask for it at all: the step kernel and its join would be two launches more.  32 sequences of up to 48 new
 // tokens of up to 512 (8 heads of 5 rows, D 128) take 33 us instead of 46, 24 of up to 43 (3 heads of 8 rows) 11
 // instead of 20, 8 prompts of up to 512 (4 heads of 6 rows, D 256) 41 instead of 45; but 8 prompts of up to 1,024 (8 heads
 // of 5 rows, D 128) 79 instead of 75.
@@ -357,7 +356,7 @@ kv_status attend(const kv_cache *cache, int32_t layer, const kv_batch *batch, co
     a.num_seqs = batch->num_seqs;
     a.q_type = q->dtype;
     a.cache_type = o->cache_dtype;
-    a.full_weights = o->full_weights || !plan.step;
+    a.full_weights = o->full_weights;
     a.step_rows = plan.step_rows;
     a.tail_above = plan.step ? kStepRows : 0;
     a.by_group = divisor(a.group);

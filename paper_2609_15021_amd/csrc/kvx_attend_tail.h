@@ -72,7 +72,7 @@ __device__ __forceinline__ void interleave() {
 // meet V as two numbers of T, the second being what the first leaves, so that the output's rounding alone shows: off
 // by 0.00166 of its norm (bf16).  Else one, rounded, since a second product and its operands cost 1.28 times the time
 // for the turn above (2.00 ms instead of 1.57) and 1.18 for the ragged tails (0.78 instead of 0.66): 0.00225 and
-// 0.00233.
+// 0.00233.  SCALED is always FULL.
 //
 // SCALED (e4m3): pages have scales.  V is widened to bfloat16 with its scale, which costs nothing, and the weights are
 // bfloat16 too; so is K where q is.  float16 does not hold K times its scale: there K's scales wait in LDS and multiply

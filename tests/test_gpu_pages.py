@@ -354,6 +354,23 @@ def test_attend_scaled_sizes(dtype, exponents):
         ref.check(np.where(ok, out.double().cpu().numpy(), 0), np.where(ok, want[0], 0), off, "out")
 
 
+@pytest.mark.parametrize("H,G,D,BS,dtype", [(2, 4, 64, 16, BF16), (4, 3, 128, 32, BF16), (2, 3, 256, 7, BF16),
+                                            (2, 4, 64, 16, F16)])
+@pytest.mark.parametrize("options", [dict(), dict(softcap=5.0, window=700)])
+def test_attend_scaled_tails_round_their_output_alone(H, G, D, BS, dtype, options):
+    """Longer tails' weights meet V as two numbers too, whatever the host's bounds: the bounds here are attend_chosen's,
+    which leave no room for a weight rounded to the rows' type."""
+    c = pref.ScaledCase(H, G, D, BS, [1100, 90], [330, 2], dtype=dtype, seed=D + G)
+    every = torch.arange(-(-1100 // BS), dtype=torch.int32).expand(c.T, 1, -1)
+    want = pref.attend_chosen(c, every, torch.full((c.T,), every.shape[2]), **options)
+    cache, _, q, _, _, tables, lens, starts = c.device()
+    for bounds in (dict(max_len=1100, max_q=330), dict()):
+        out, lse = attend.kv_attend(cache, 0, q, tables, lens, starts, scales=c.scales.to(DEV), **options, **bounds)
+        torch.cuda.synchronize()
+        ref.check(lse, want[1], want[3], "lse")
+        ref.check(out, want[0], want[2], "out")
+
+
 def test_attend_scaled_long():
     """Few rows over many tokens, split and joined, and many sequences."""
     run_scaled(pref.ScaledCase(1, 3, 128, 16, [5000, 3000], [1, 70], seed=13))
