@@ -64,18 +64,24 @@ kv_status check_attend(const kv_cache *cache, const kv_batch *batch, const kv_at
                     o->reserved);
     if (o->weights_in && !o->weights_out)
         return fail(KV_EINVAL, "weights_in without weights_out");
-    // Rows are counted in 32 bits, and the tail kernel's workgroups by what one launch takes.
-    const int64_t queries = std::min(batch->max_queries, batch->num_queries), group = q->heads / H;
-    if (queries * group > INT32_MAX / 2 || (queries * group > kStepRows &&
-                                            tail_tiles(queries, group) * H * batch->num_seqs > kMaxWorkgroups))
-        return fail(KV_EUNSUPPORTED, "up to %lld new tokens in each of %d sequences of %d query heads are too many for "
-                    "one call", static_cast<long long>(queries), batch->num_seqs, q->heads);
     if (o->weights_out && (o->weights_seq_stride < 0 || o->weights_head_stride < 0 ||
                            (batch->num_seqs > 0 && H > 1 && o->weights_head_stride < batch->max_len) ||
                            (batch->num_seqs > 1 && o->weights_seq_stride < batch->max_len)))
         return fail(KV_EINVAL, "rows of weights (strides %lld and %lld) are shorter than max_len %d",
                     static_cast<long long>(o->weights_seq_stride), static_cast<long long>(o->weights_head_stride),
                     batch->max_len);
+    return KV_OK;
+}
+
+// Where sequences' rows come in tiles: rows are counted in 32 bits, and the tail kernel's workgroups by what one launch
+// takes.
+kv_status check_tiles(const kv_cache *cache, const kv_batch *batch, const kv_rows *q) {
+    const int64_t H = cache->layout.num_kv_heads, group = q->heads / H;
+    const int64_t queries = std::min(batch->max_queries, batch->num_queries);
+    if (queries * group > INT32_MAX / 2 || (queries * group > kStepRows &&
+                                            tail_tiles(queries, group) * H * batch->num_seqs > kMaxWorkgroups))
+        return fail(KV_EUNSUPPORTED, "up to %lld new tokens in each of %d sequences of %d query heads are too many for "
+                    "one call", static_cast<long long>(queries), batch->num_seqs, q->heads);
     return KV_OK;
 }
 
@@ -286,6 +292,14 @@ PagesPlan plan_of(const kv_cache *cache, const kv_batch *batch, const kv_page_li
     return p;
 }
 
+// Over chosen pages rows come one by one, whatever their sequences: a launch takes so many of their parts.
+kv_status check_parts(const kv_cache *cache, const kv_batch *batch, const PagesPlan &plan) {
+    if (batch->num_seqs > 0 &&
+        int64_t{batch->num_queries} * plan.chosen.splits * cache->layout.num_kv_heads > (int64_t{1} << 23))
+        return fail(KV_EUNSUPPORTED, "%d new tokens that chose pages are too many for one call", batch->num_queries);
+    return KV_OK;
+}
+
 kv_status attend(const kv_cache *cache, int32_t layer, const kv_batch *batch, const kv_attend_options *o,
                  const kv_page_scales *scales, const kv_page_list *list, bool pages, const kv_rows *q,
                  const kv_rows *out, float *lse, void *workspace, int64_t workspace_bytes, hipStream_t stream) {
@@ -294,6 +308,8 @@ kv_status attend(const kv_cache *cache, int32_t layer, const kv_batch *batch, co
         st = check_attend(cache, batch, o, q);
     if (st == KV_OK && pages)
         st = check_pages(cache, batch, o, scales, list);
+    if (st == KV_OK && !list)
+        st = check_tiles(cache, batch, q);
     if (st == KV_OK)
         st = check_rows(cache, batch, out, "out");
     if (st != KV_OK)
@@ -309,8 +325,10 @@ kv_status attend(const kv_cache *cache, int32_t layer, const kv_batch *batch, co
     const Plan plan = list ? Plan{} : plan_of(cache, batch, o, q, scales != nullptr);
     const PagesPlan listed = list ? plan_of(cache, batch, list, q) : PagesPlan{};
     const int64_t need = list ? listed.bytes : plan.bytes;
-    if (list && int64_t{batch->num_queries} * listed.chosen.splits * cache->layout.num_kv_heads > (int64_t{1} << 23))
-        return fail(KV_EUNSUPPORTED, "%d new tokens that chose pages are too many for one call", batch->num_queries);
+    if (list)
+        st = check_parts(cache, batch, listed);
+    if (st != KV_OK)
+        return st;
     if (workspace_bytes < need || (need > 0 && !workspace))
         return fail(KV_EINVAL, "workspace of %lld bytes; %lld are needed", static_cast<long long>(workspace_bytes),
                     static_cast<long long>(need));
@@ -402,7 +420,9 @@ int64_t kv_attend_workspace(const kv_cache *cache, const kv_batch *batch, const 
                             const kv_rows *q) {
     int64_t bytes = 0;
     const kv_status st = kvx::guarded([&]() -> kv_status {
-        const kv_status checked = kvx::check_attend(cache, batch, options, q);
+        kv_status checked = kvx::check_attend(cache, batch, options, q);
+        if (checked == KV_OK)
+            checked = kvx::check_tiles(cache, batch, q);
         if (checked == KV_OK)
             bytes = kvx::plan_of(cache, batch, options, q, false).bytes;
         return checked;
@@ -426,9 +446,14 @@ int64_t kv_attend_pages_workspace(const kv_cache *cache, const kv_batch *batch, 
         kv_status checked = kvx::check_attend(cache, batch, options, q);
         if (checked == KV_OK)
             checked = kvx::check_pages(cache, batch, options, scales, list);
-        if (checked == KV_OK)
-            bytes = list ? kvx::plan_of(cache, batch, list, q).bytes
-                         : kvx::plan_of(cache, batch, options, q, true).bytes;
+        if (checked == KV_OK && list) {
+            const kvx::PagesPlan plan = kvx::plan_of(cache, batch, list, q);
+            checked = kvx::check_parts(cache, batch, plan);
+            bytes = plan.bytes;
+        } else if (checked == KV_OK) {
+            checked = kvx::check_tiles(cache, batch, q);
+            bytes = checked == KV_OK ? kvx::plan_of(cache, batch, options, q, true).bytes : 0;
+        }
         return checked;
     });
     return st == KV_OK ? bytes : st;

@@ -566,6 +566,30 @@ def test_attend_chosen_behind_the_last_row():
     run_chosen(c, 57, 1)
 
 
+def test_attend_chosen_by_many_sequences():
+    """More sequences than a wave looks at at once, without new tokens where it looks again, in a call whose bound of new
+    tokens is the binding's default, all of them.  All pages, in order, are attention over everything."""
+    gen = np.random.default_rng(5)
+    new = [int(x) for x in gen.choice([0, 1, 1, 3], 2000)]
+    for at in (0, 63, 64, 127, 128, 129, 1999):
+        new[at] = 0
+    new[65], new[1998] = 2, 1
+    lens = [int(x) + n for x, n in zip(gen.integers(1, 30, 2000), new)]
+    c = ref.Case(8, 16, 16, 16, lens, new, seed=33)
+    assert -(-c.T * 16 // 128) * 8 * 2000 > 1 << 22  # (as tiles, too many for a launch)
+    cache, _, q, _, _, tables, lens_d, starts = c.device()
+    want, want_lse = attend.kv_attend(cache, 0, q, tables, lens_d, starts, max_q=3)
+    seq = np.repeat(np.arange(2000), new)
+    pages = torch.arange(3, dtype=torch.int32, device=DEV).expand(c.T, 1, 3)
+    counts = torch.tensor([-(-lens[b] // 16) for b in seq], dtype=torch.int32, device=DEV)
+    tight = attend.kv_attend(cache, 0, q, tables, lens_d, starts, pages=pages, counts=counts, max_q=3)
+    out, lse = attend.kv_attend(cache, 0, q, tables, lens_d, starts, pages=pages, counts=counts)
+    assert torch.equal(out, tight[0]) and torch.equal(lse, tight[1])
+    # Both outputs are within half a step of the same numbers, and what is beside their last rounding.
+    assert (lse - want_lse).abs().max() < 2.0**-17
+    assert ((out.float() - want.float()).abs() <= want.float().abs() * 2.0**-7 * 1.01 + 2.0**-13).all()
+
+
 def test_attend_chosen_more_than_there_is():
     """Lists with far more room than a sequence has pages, and lists that name its few pages many times over."""
     for n in (60, 700):

@@ -145,6 +145,37 @@ def test_attend_pages_refusals():
     assert call(good, 0, _batch(attend, **EMPTY), pages=_list(pages=None, counts=None)) == kvx.KV_OK
 
 
+@pytest.mark.parametrize("fp8", [False, True])
+def test_chosen_pages_of_many_sequences(fp8):
+    """Lists know no sequence's bounds: max_queries may be all of a large batch's new tokens, as the binding has it by
+    default, and only rows, parts and heads are limited, for the workspace as for the call."""
+    from paper_2609_15021_amd import attend, kvx
+    cache = _cache(kvx, kvx.make_layout(1, 8, 64, 1 if fp8 else 2, 16, 16))
+    q = _rows(attend, 40, token_stride=2560)
+    o = attend.KvAttendOptions(cache_dtype=attend.KV_DTYPE_E4M3 if fp8 else attend.KV_DTYPE_BF16)
+    by = _scales(attend, 8) if fp8 else None
+
+    def call(tokens, max_queries, q=q, cache=cache, seqs=2048):
+        batch = _batch(attend, num_seqs=seqs, num_queries=tokens, max_queries=max_queries, starts=SOME)
+        pages = attend.KvPageList(pages=SOME, counts=SOME, token_stride=32, head_stride=4, heads=cache.layout.num_kv_heads,
+                                  budget=4)
+        args = (ctypes.byref(o), ctypes.byref(by) if by else None, ctypes.byref(pages), ctypes.byref(q))
+        need = kvx._lib.kv_attend_pages_workspace(ctypes.byref(cache), ctypes.byref(batch), *args)
+        # (A workspace that is too small: what is not refused before comes to that.)
+        got = kvx._lib.kv_attend_pages(ctypes.byref(cache), 0, ctypes.byref(batch), *args, ctypes.byref(q), SOME, SOME, 0,
+                                       None)
+        assert got == (kvx.KV_EINVAL if need > 0 else need)
+        return need
+
+    assert call(8192, 8192) == call(8192, 4) > 0
+    assert call(1 << 20, 1 << 20) == call(1 << 20, 512) > 0
+    assert call((1 << 20) + 1, 4) == kvx.KV_EUNSUPPORTED
+    # Rows beyond 32 bits in a sequence, which only tiles of a sequence's rows would have to count.
+    one, wide = _cache(kvx, kvx.make_layout(1, 1, 64, 1 if fp8 else 2, 16, 16)), _rows(attend, 16383, token_stride=1 << 20)
+    by = _scales(attend, 1) if fp8 else None
+    assert call(1 << 18, 1 << 18, wide, one, 1) > 0
+
+
 def test_bounds_and_score_refusals():
     from paper_2609_15021_amd import attend, kvx
     ones = lambda *dims, **kw: _cache(kvx, kvx.make_layout(*dims, 1, 1), **kw)  # noqa: E731
