@@ -282,6 +282,8 @@ def _page_scales(t, cache: Cache, device: int):
     if not isinstance(t, torch.Tensor) or (t.dtype is not torch.uint8 and t.dtype is not torch.float8_e8m0fnu) or \
             len(shape := t.shape) != 3:
         raise TypeError("scales must be a [blocks][2][heads] uint8 or float8_e8m0fnu device tensor")
+    if t.requires_grad and torch.is_grad_enabled():
+        _no_gradient("scales")
     if t.get_device() != device:
         _elsewhere(t, "scales", device)
     blocks, two, heads = shape

@@ -188,6 +188,25 @@ def test_binding_refuses_what_requires_a_gradient(host_cache):
     attend.kv_attend(cache, 0, leaf_q.detach(), tables, lens, slopes=leaf_s.detach())
 
 
+def test_binding_refuses_scales_that_require_a_gradient(host_cache):
+    """Scales may be of a floating-point type, float8_e8m0fnu, and then leaves as well."""
+    from paper_2609_15021_amd import attend
+    cache, _ = host_cache
+    q, kv = torch.zeros(2, 4, 64, dtype=torch.bfloat16), torch.zeros(2, 2, 64, dtype=torch.bfloat16)
+    tables, lens = torch.zeros(2, 4, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+    scales = torch.zeros(64, 2, 2, dtype=torch.float8_e8m0fnu)
+    calls = [lambda s: attend.kv_append(cache, 0, kv, kv, tables, lens, scales=s),
+             lambda s: attend.kv_rotate(cache, 0, q, kv, kv, tables, lens, scales=s),
+             lambda s: attend.kv_attend(cache, 0, q, tables, lens, scales=s),
+             lambda s: attend.kv_score(cache, 0, q, tables, lens, block_size=16, scales=s)]
+    for call in calls:
+        with pytest.raises(RuntimeError, match="gradient"):
+            call(scales.clone().requires_grad_())
+        with torch.no_grad():
+            call(scales.clone().requires_grad_())
+        call(scales)
+
+
 def test_full_weights_is_a_choice_of_two(host_cache):
     from paper_2609_15021_amd import attend, kvx
     cache, batch, rows = _cache(kvx, kvx.make_layout(1, 2, 64, 2, 16, 16)), _batch(attend), _rows(attend, 4)
