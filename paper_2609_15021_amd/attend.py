@@ -9,7 +9,8 @@ three are device tensors; ``max_q`` and ``max_len`` are the host's bounds of new
 default (and at most) what the shapes allow.  Tight bounds size the launches better; numbers beyond them are refused on
 the device (``kv_attend_async_error``), and such a sequence's rows of the outputs hold what they held before.
 
-There is no backward pass: tensors that require a gradient are refused while torch records one.
+There is no backward pass: tensors that require a gradient are refused while torch records one, and those that carry a
+forward-mode tangent always.
 """
 from __future__ import annotations
 
@@ -18,6 +19,7 @@ import ctypes
 import struct
 
 import torch
+from torch.autograd import forward_ad
 
 from .kvx import Cache, KvCache, _in_use_on, _lib, _raise
 
@@ -158,8 +160,7 @@ def _on(t, name: str, device: int) -> None:
 def _floats(t, name: str, device: int, shape) -> None:
     if not isinstance(t, torch.Tensor) or t.dtype is not torch.float32 or t.shape != shape or not t.is_contiguous():
         raise TypeError(f"{name} must be a contiguous float32 device tensor of {tuple(shape)}")
-    if t.requires_grad and torch.is_grad_enabled():
-        _no_gradient(name)
+    _plain(t, name)
     _on(t, name, device)
 
 
@@ -168,14 +169,18 @@ def _weights(t, name: str, device: int, rows=None) -> None:
             (t.stride(2) != 1 and t.shape[2] > 1 and t.numel()) or (rows is not None and t.shape[:2] != rows):
         raise TypeError(f"{name} must be a [sequences][heads][tokens] float32 device tensor with dense rows"
                         f"{'' if rows is None else f' ({rows} of them)'}")
-    if t.requires_grad and torch.is_grad_enabled():
-        _no_gradient(name)
+    _plain(t, name)
     _on(t, name, device)
 
 
-def _no_gradient(name: str):
-    raise RuntimeError(f"{name} requires a gradient, and these operators have none: detach it, or call under "
-                       "torch.no_grad()")
+def _plain(t, name: str) -> None:
+    """These operators have no derivatives: what asks for one is refused."""
+    if t.requires_grad and torch.is_grad_enabled():
+        raise RuntimeError(f"{name} requires a gradient, and these operators have none: detach it, or call under "
+                           "torch.no_grad()")
+    if forward_ad.unpack_dual(t).tangent is not None:
+        raise RuntimeError(f"{name} carries a tangent, and these operators have no forward-mode derivative: pass its "
+                           "primal")
 
 
 def _rows(t, name: str, head_dim: int, device: int):
@@ -185,8 +190,7 @@ def _rows(t, name: str, head_dim: int, device: int):
         return found
     if not isinstance(t, torch.Tensor) or len(shape := t.shape) != 3 or (dtype := _ROW_TYPES.get(t.dtype)) is None:
         raise TypeError(f"{name} must be a [tokens][heads][D] device tensor of bfloat16 or float16")
-    if t.requires_grad and torch.is_grad_enabled():
-        _no_gradient(name)
+    _plain(t, name)
     if t.get_device() != device:
         _elsewhere(t, name, device)
     _, heads, width = shape
@@ -282,8 +286,7 @@ def _page_scales(t, cache: Cache, device: int):
     if not isinstance(t, torch.Tensor) or (t.dtype is not torch.uint8 and t.dtype is not torch.float8_e8m0fnu) or \
             len(shape := t.shape) != 3:
         raise TypeError("scales must be a [blocks][2][heads] uint8 or float8_e8m0fnu device tensor")
-    if t.requires_grad and torch.is_grad_enabled():
-        _no_gradient("scales")
+    _plain(t, "scales")
     if t.get_device() != device:
         _elsewhere(t, "scales", device)
     blocks, two, heads = shape
@@ -414,8 +417,7 @@ def _rotate_arguments(rows_dtype, head_dim: int, tokens: int, device: int, freqs
         if not isinstance(freqs, torch.Tensor) or freqs.dtype is not torch.float64 or freqs.dim() != 1 or \
                 not freqs.is_contiguous():
             raise TypeError("freqs must be a contiguous 1-dimensional float64 device tensor")
-        if freqs.requires_grad and torch.is_grad_enabled():
-            _no_gradient("freqs")
+        _plain(freqs, "freqs")
         _on(freqs, "freqs", device)
         rotary, freqs_at = _int32(2 * freqs.shape[0], "twice the number of freqs"), freqs.data_ptr()
     positions_at = 0 if positions is None else _dense_ints(positions, "positions", 1, device, tokens)
@@ -427,8 +429,7 @@ def _rotate_arguments(rows_dtype, head_dim: int, tokens: int, device: int, freqs
         if not isinstance(weight, torch.Tensor) or weight.shape != (head_dim,) or not weight.is_contiguous() or \
                 (weight.dtype is not torch.float32 and weight.dtype is not rows_dtype):
             raise TypeError(f"{name} must be a contiguous [{head_dim}] device tensor of float32 or {rows_dtype}")
-        if weight.requires_grad and torch.is_grad_enabled():
-            _no_gradient(name)
+        _plain(weight, name)
         _on(weight, name, device)
         of = KV_DTYPE_F32 if weight.dtype is torch.float32 else _DTYPES[weight.dtype]
         if weight_dtype not in (0, of):

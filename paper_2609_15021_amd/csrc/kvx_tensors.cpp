@@ -16,12 +16,13 @@
 
 namespace {
 
-// The tensor behind an argument on `device`, without a gradient to record, or NULL.
+// The tensor behind an argument on `device`, without a gradient to record or a forward-mode tangent (there is one level
+// of them), or NULL.
 const at::Tensor *tensor_of(PyObject *x, int device) {
     if (!THPVariable_Check(x))
         return nullptr;
     const at::Tensor &t = THPVariable_Unpack(x);
-    if (!t.defined() || t.layout() != at::kStrided || t.requires_grad() ||
+    if (!t.defined() || t.layout() != at::kStrided || t.requires_grad() || t._fw_grad(0).defined() ||
         (t.is_cpu() ? -1 : static_cast<int>(t.get_device())) != device)
         return nullptr;
     return &t;

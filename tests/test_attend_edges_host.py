@@ -207,6 +207,43 @@ def test_binding_refuses_scales_that_require_a_gradient(host_cache):
         call(scales)
 
 
+def test_binding_refuses_what_carries_a_tangent(host_cache):
+    """Nor is there a forward-mode derivative: an output without a tangent must not stand for one, with or without
+    gradients being recorded."""
+    from torch.autograd import forward_ad
+
+    from paper_2609_15021_amd import attend
+    cache, _ = host_cache
+    q, kv = torch.zeros(2, 4, 64, dtype=torch.bfloat16), torch.zeros(2, 2, 64, dtype=torch.bfloat16)
+    tables, lens = torch.zeros(2, 4, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+    weights, slopes, norm = torch.zeros(2, 2, 64), torch.zeros(4), torch.ones(64)
+    freqs = torch.ones(32, dtype=torch.float64)
+    scales = torch.zeros(64, 2, 2, dtype=torch.uint8)
+    rotate = lambda *x, **kw: attend.kv_rotate(cache, 0, *x, tables, lens, **kw)  # noqa: E731
+    calls = [(kv, lambda x: attend.kv_append(cache, 0, x, kv, tables, lens)),
+             (kv, lambda x: attend.kv_append(cache, 0, kv, x * 2, tables, lens)),
+             (kv, lambda x: attend.kv_append_scaled(cache, 0, x, kv, tables, lens, scales)),
+             (q, lambda x: attend.kv_attend(cache, 0, x, tables, lens)),
+             (q, lambda x: attend.kv_attend(cache, 0, q, tables, lens, out=x)),
+             (slopes, lambda x: attend.kv_attend(cache, 0, q, tables, lens, slopes=x)),
+             (weights, lambda x: attend.kv_attend(cache, 0, q, tables, lens, weights=weights, prior=x)),
+             (weights, lambda x: attend.kv_keep(x, lens, 4)),
+             (q, lambda x: rotate(x, kv, kv)), (kv, lambda x: rotate(q, kv, x)),
+             (freqs, lambda x: rotate(q, kv, kv, freqs=x)), (norm, lambda x: rotate(q, kv, kv, q_weight=x)),
+             (norm, lambda x: rotate(q, kv, kv, k_weight=x)),
+             (q, lambda x: attend.kv_score(cache, 0, x, tables, lens, block_size=16))]
+    for tensor, call in calls:
+        with forward_ad.dual_level():
+            dual = forward_ad.make_dual(tensor.clone(), torch.ones_like(tensor))
+            with pytest.raises(RuntimeError, match="tangent"):
+                call(dual)
+            with torch.no_grad(), pytest.raises(RuntimeError, match="tangent"):
+                call(dual)
+            call(tensor.clone())
+            call(forward_ad.unpack_dual(dual).primal)
+        call(dual)  # (its level is left, and its tangent with it)
+
+
 def test_full_weights_is_a_choice_of_two(host_cache):
     from paper_2609_15021_amd import attend, kvx
     cache, batch, rows = _cache(kvx, kvx.make_layout(1, 2, 64, 2, 16, 16)), _batch(attend), _rows(attend, 4)
