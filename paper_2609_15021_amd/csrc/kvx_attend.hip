@@ -165,16 +165,17 @@ Parts tail_parts_for(int64_t longest, int64_t have, int64_t launched, int64_t he
 }
 
 // Rounds of 128 tokens of a tile that the step kernel takes of sequences with many rows over scaled pages, where the tail
-// kernel would leave most CUs idle: 56 new tokens of each of 2 sequences of 129 (3 heads of 5 rows, D 80) take 14 us
-// instead of 19, 18 of each of 7 sequences of 430 (420 rounds; 3 heads of 8 rows, D 128) 20.5 instead of 24, 24 of each
-// of 4 of 512 (576; 4 heads of 6 rows, D 256) 24 instead of 31; but 32 of each of 4 of 512 (1,024; 8 heads of 8 rows)
-// 37 instead of 25.
+// kernel would leave most CUs idle: 18 of each of 7 sequences of 430 (420 rounds; 3 heads of 8 rows, D 128) take 19 us
+// instead of 22, 24 of each of 4 of 512 (576; 4 heads of 6 rows, D 256) 23 instead of 25; but 32 of each of 4 of 512
+// (1,024; 8 heads of 8 rows) 36 instead of 25.
 constexpr int64_t kStepRounds = 640;
-// Tokens that rows over scaled pages see, up to which the tail kernel takes all sequences where bounds ask for it at all: the step kernel and its join would be two launches more.  32 sequences of up to 48 new
-// tokens of up to 512 (8 heads of 5 rows, D 128) take 33 us instead of 46, 24 of up to 43 (3 heads of 8 rows) 11
-// instead of 20, 8 prompts of up to 512 (4 heads of 6 rows, D 256) 41 instead of 45; but 8 prompts of up to 1,024 (8 heads
-// of 5 rows, D 128) 79 instead of 75.
-constexpr int64_t kTailAlone = 512;
+// Tokens that rows over scaled pages see, up to which the tail kernel takes all sequences where bounds ask for it at all:
+// the step kernel and its join would be two launches more.  100 new tokens of a sequence of 2,048 beside single ones of 47
+// of up to that (8 heads of 5 rows, D 128) take 95 us instead of 144, 32 sequences of up to 48 of up to 512 32 instead of
+// 45, 8 prompts of up to 512 (4 heads of 6 rows, D 256) 43 instead of 49, of up to 1,024 (8 of 5, D 128) 84 instead of 90.
+// Beyond, single tokens of wide rows read faster in the step kernel: 100 of 4,096 beside 47 (4 heads of 6 rows, D 256) 237
+// instead of 246, of 8,192 321 instead of 376.
+constexpr int64_t kTailAlone = 2048;
 
 Plan plan_of(const kv_cache *cache, const kv_batch *batch, const kv_attend_options *o, const kv_rows *q, bool scaled) {
     const int64_t H = cache->layout.num_kv_heads, D = cache->layout.head_dim, group = q->heads / H;

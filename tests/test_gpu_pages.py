@@ -371,6 +371,14 @@ def test_attend_scaled_tails_round_their_output_alone(H, G, D, BS, dtype, option
         ref.check(out, want[0], want[2], "out")
 
 
+@pytest.mark.parametrize("H,G,D,BS,dtype", [(4, 3, 128, 16, BF16), (2, 6, 256, 32, F16), (3, 4, 64, 7, BF16)])
+def test_attend_scaled_single_tokens_beside_tails(H, G, D, BS, dtype):
+    """Few rows over many tokens, in parts, where the batch has tails."""
+    c = pref.ScaledCase(H, G, D, BS, [2000, 64, 1999, 5, 40, 700], [1, 30, 100, 1, 0, 2], dtype=dtype, seed=H)
+    run_scaled(c)
+    run_scaled(c, dict(window=300, softcap=20.0))
+
+
 def test_attend_scaled_long():
     """Few rows over many tokens, split and joined, and many sequences."""
     run_scaled(pref.ScaledCase(1, 3, 128, 16, [5000, 3000], [1, 70], seed=13))
