@@ -15,8 +15,8 @@
 // power of two by repeating the last, so that the largest over them lies in a lane's 4 results, or one or two shuffles
 // away.  8,193 pages of 8 heads of 5 rows (34 MB, D 128): 8.7 us, of which reading takes 5.6 and table, bounds and
 // products come one after the other.  Tails of up to 517 tokens over 1,057 pages, 3 sequences, 2 heads of 8 rows: 19
-// us, where the products alone would take 6: a wave's share of tiles is short, and its start (lengths, table, bounds)
-// and every second tile's wait for the workgroup are not hidden.
+// us, the matrix cores busy for 11% of it: a wave's share of tiles is short, and its start (lengths, table, bounds) and
+// every second tile's wait for the workgroup are not hidden.
 #include <algorithm>
 #include <cmath>
 
@@ -75,7 +75,8 @@ struct Piece {
 };
 
 // LPR lanes have a row; SPREAD: a wave has one page, else one for each of its groups of lanes.  AT_ONCE: rows that a
-// lane has on their way (16 instead of 8: 131,077 tokens of 8 heads of 256 bytes in 54 us instead of 57).
+// lane has on their way.  131,077 tokens of 8 heads of 128 in pages of 16 take 57 us with 16 of them and 60 with 8 in
+// bfloat16, but 71 and 60 in float16, where the compiler does not keep 16 apart, and 30 with either in e4m3.
 template <int TYPE, int LPR, bool SPREAD, int AT_ONCE>
 __global__ __launch_bounds__(kThreads) void bounds_kernel(const BoundsArgs a) {
     constexpr int N = Piece<TYPE>::N, GROUPS = 64 / LPR;
@@ -149,9 +150,10 @@ hipError_t launch_bounds(const BoundsArgs &a, int num_seqs, hipStream_t stream) 
     const bool spread = items * num_seqs <= 8192;
     const int64_t each = waves * (spread ? 1 : 64 / LPR);
     const dim3 grid(static_cast<uint32_t>((items + each - 1) / each), static_cast<uint32_t>(num_seqs));
+    constexpr int MOST = TYPE == KV_DTYPE_BF16 ? 16 : 8;
     const auto kernel = spread            ? bounds_kernel<TYPE, LPR, true, 4>
                         : a.pages.BS <= 8 ? bounds_kernel<TYPE, LPR, false, 8>
-                                          : bounds_kernel<TYPE, LPR, false, 16>;
+                                          : bounds_kernel<TYPE, LPR, false, MOST>;
     return launch_kernel(kernel, grid, kThreads, stream, a);
 }
 
@@ -231,7 +233,9 @@ struct ScoreArgs {
     Divisor by_bs, by_shares, by_subs;
 };
 
-// Workgroups that tails are shared out to: 20 us for the tails above; a third of them take 26, twice as many 24.
+// Workgroups that tails are shared out to: 20 us for the tails above (2-byte bounds, D 128, of which 1,024 workgroups run
+// at once; half of the launched ones may have no tokens); a third of them take 26, twice as many 24.  Other variants, of
+// which 512 (wide e4m3) to 1,280 (up to 64 columns) run at once, have not been tried with other numbers.
 constexpr int kShareTarget = 1536;
 
 typedef short s16x2 __attribute__((ext_vector_type(2)));

@@ -480,6 +480,23 @@ def test_scores_are_bounds():
                     assert np.allclose(pages[:, j], best, atol=1e-4)
 
 
+@pytest.mark.parametrize("D,fp8,dtype", [(64, False, BF16), (64, False, F16), (80, True, BF16), (144, False, F16)])
+def test_bounds_of_many_long_pages(D, fp8, dtype):
+    """The same of pages of more rows than a lane has on their way, in every type, with numbers that are not finite."""
+    c = ref.Case(8, 1, D, 20, [16500, 4507], [16500, 4507], fp8=fp8, dtype=dtype, seed=34)
+    some = c.flat[int(c.tables[0, 1]), :2 * 20 * 8 * D].view(c.shape)
+    some[0, 1, 3:19, 5] = float("nan")
+    some[0, 2, :, 6] = float("nan")
+    if not fp8:
+        some[0, 0, 17, 1], some[0, 0, 9, 2] = float("inf"), -float("inf")
+    cache, _, _, _, _, tables, lens, starts = c.device()
+    low_high, t = bounds_cache(c, 0.0)
+    attend.kv_bounds(cache, 0, low_high, tables, lens, starts, dtype=c.cache_dtype)
+    want = pref.bounds(c, c.flat)
+    got = t[:, :, :, 0].double().cpu().numpy()
+    assert np.array_equal(got, np.where(np.isnan(want), 0.0, want))
+
+
 # ---- Attention over chosen pages ----------------------------------------------------------
 
 
