@@ -595,7 +595,7 @@ def kv_score(bounds: Cache, layer: int, q, tables, lens, starts=None, *, block_s
 
     Returns (scores float32 [tokens][H][pages], counts int32 [tokens]: pages up to the token's own), which are kv_keep's
     weights and lens.  ``out`` and ``counts`` are made if not given; scores of pages beyond ``counts``, and rows of no
-    sequence, are left as they were (in made ones, scores hold anything and counts 0)."""
+    sequence, are left as they were (in made ones, scores hold anything, and counts 0 with ``starts``)."""
     device = bounds.struct.device
     layout = bounds.layout
     qr, (tokens, _, _) = _rows(q, "q", layout.head_dim, device)
