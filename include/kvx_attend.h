@@ -173,11 +173,11 @@ typedef struct kv_rotate_options {
  * kv_rotate -- norm, rotate, and append.  Of each new token's row x of each head of q and k:
  *   y_d = x_d / sqrt(mean of x^2 + eps) * (weight_offset + weight_d)  (or x_d, without weights), and for each pair (a, b)
  *   of the first rotary_dim columns, with t = position * freqs[i]: (a cos t - b sin t, b cos t + a sin t) * magnitude.
- * A row is rounded once, at the end; sums are held in 32 bits (so a normed row's |x| stay under 1e18, and where eps is 0
- * the largest over 1e-18), positions times frequencies in 64.  q's rows go to `out` (same type and heads; may be q
+ * A row is rounded once, at the end; sums are held in 32 bits (so a normed row's |x| stay under 1e18, and where eps is
+ * 0 the largest over 1e-18), positions times frequencies in 64.  q's rows go to `out` (same type and heads; may be q
  * itself), k's rotated rows and v's as they are into layer `layer` of the cache, as kv_append, or with scales
- * kv_append_scaled, puts them there.  A row whose token has no place (before token 0) is rotated by its place or position
- * all the same; rows of no sequence are left as they were.
+ * kv_append_scaled, puts them there.  A row whose token has no place (before token 0) is rotated by its place or
+ * position all the same; rows of no sequence are left as they were.
  * Errors and preconditions as kv_append; KV_EINVAL also for a rotary_dim that is odd or outside [0, D], a NULL freqs
  * with one, and numbers that are negative or not finite.
  */

@@ -169,12 +169,12 @@ Parts tail_parts_for(int64_t longest, int64_t have, int64_t launched, int64_t he
 // instead of 22, 24 of each of 4 of 512 (576; 4 heads of 6 rows, D 256) 23 instead of 25; but 32 of each of 4 of 512
 // (1,024; 8 heads of 8 rows) 36 instead of 25.
 constexpr int64_t kStepRounds = 640;
-// Tokens that rows over scaled pages see, up to which the tail kernel takes all sequences where bounds ask for it at all:
-// the step kernel and its join would be two launches more.  100 new tokens of a sequence of 2,048 beside single ones of 47
-// of up to that (8 heads of 5 rows, D 128) take 95 us instead of 144, 32 sequences of up to 48 of up to 512 32 instead of
-// 45, 8 prompts of up to 512 (4 heads of 6 rows, D 256) 43 instead of 49, of up to 1,024 (8 of 5, D 128) 84 instead of 90.
-// Beyond, single tokens of wide rows read faster in the step kernel: 100 of 4,096 beside 47 (4 heads of 6 rows, D 256) 237
-// instead of 246, of 8,192 321 instead of 376.
+// Tokens that rows over scaled pages see, up to which the tail kernel takes all sequences where bounds ask for it at
+// all: the step kernel and its join would be two launches more.  100 new tokens of a sequence of 2,048 beside single
+// ones of 47 of up to that (8 heads of 5 rows, D 128) take 95 us instead of 144, 32 sequences of up to 48 of up to 512
+// 32 instead of 45, 8 prompts of up to 512 (4 heads of 6 rows, D 256) 43 instead of 49, of up to 1,024 (8 of 5, D 128)
+// 84 instead of 90.  Beyond, single tokens of wide rows read faster in the step kernel: 100 of 4,096 beside 47 (4 heads
+// of 6 rows, D 256) 237 instead of 246, of 8,192 321 instead of 376.
 constexpr int64_t kTailAlone = 2048;
 
 Plan plan_of(const kv_cache *cache, const kv_batch *batch, const kv_attend_options *o, const kv_rows *q, bool scaled) {

@@ -49,8 +49,8 @@ __device__ __forceinline__ int64_t slot_in(const Chosen &chosen, int, int, int64
 }
 
 // T: type of q, of the weights and of out; FP8: the cache holds e4m3; DP >= D columns; NT: tiles of 16 rows.
-// (2 waves a SIMD, for which wide 2-byte rows would have to spill most of their registers, and one wave runs them.  Two
-// tiles of 128 columns spill 3 to 18 all the same, as do scaled or chosen e4m3 rows of 256 columns over chosen pages, 5.)
+// (2 waves a SIMD; wide 2-byte rows would need to spill for that, and one wave runs them.  Two tiles of up to 128
+// columns spill 3 to 18 registers in some variants, chosen pages of e4m3 with up to 256 columns 5.)
 //
 // SCALED: pages have scales (or where a.scales has none, scales of 1): K's multiply the scores, V's the weights, which
 // then meet V in bfloat16: float16's range would not hold the products.  They are loaded with K, a lane a token.

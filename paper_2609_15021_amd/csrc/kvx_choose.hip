@@ -233,9 +233,9 @@ struct ScoreArgs {
     Divisor by_bs, by_shares, by_subs;
 };
 
-// Workgroups that tails are shared out to: 20 us for the tails above (2-byte bounds, D 128, of which 1,024 workgroups run
-// at once; half of the launched ones may have no tokens); a third of them take 26, twice as many 24.  Other variants, of
-// which 512 (wide e4m3) to 1,280 (up to 64 columns) run at once, have not been tried with other numbers.
+// Workgroups that tails are shared out to: 20 us for the tails above (2-byte bounds, D 128, of which 1,024 workgroups
+// run at once; half of the launched ones may have no tokens); a third of them take 26, twice as many 24.  Other
+// variants, of which 512 (wide e4m3) to 1,280 (up to 64 columns) run at once, have not been tried with other numbers.
 constexpr int kShareTarget = 1536;
 
 typedef short s16x2 __attribute__((ext_vector_type(2)));

@@ -6,14 +6,15 @@
 //
 // A workgroup has one (page, K or V, head): it takes the new rows of the page, finds their largest |x|, and with the
 // page's old scale the new one; rounds older rows if the scale grew; and writes the new ones, of which it holds kHeld
-// in a lane's registers.  2,608 new tokens of 4 heads of 256 (16 MB read and written once, 3.4 us at a large copy's rate)
-// take 8.0 us on the GPU: beside the launch, lengths, then rows and tables are waited for one after the other (a scale
-// only where a page has older rows), and there is one set of rows for each workgroup.  A decoding step of 48 tokens takes
-// 4.1 (5.8 with the host).
+// in a lane's registers.  2,608 new tokens of 4 heads of 256 (16 MB read and written once, 3.4 us at a large copy's
+// rate) take 8.0 us on the GPU: beside the launch, lengths, then rows and tables are waited for one after the other (a
+// scale only where a page has older rows), and there is one set of rows for each workgroup.  A decoding step of 48
+// tokens takes 4.1 (5.8 with the host).
 //
-// For kv_rotate K is normed and rotated here, with angles worked out in every lane, for every row and head: that is most
-// of kv_rotate's time with scales.  2,085 tokens of 40 query heads and 8 KV heads (D 128) take 39 us in both launches (17
-// with one factor for the cache, 12 at a large copy's rate; 23 without norms and angles), 3 tokens 14 (4.5).
+// For kv_rotate K is normed and rotated here, with angles worked out in every lane, for every row and head: that is
+// most of kv_rotate's time with scales.  2,085 tokens of 40 query heads and 8 KV heads (D 128) take 39 us in both
+// launches (17 with one factor for the cache, 12 at a large copy's rate; 23 without norms and angles), 3 tokens 14
+// (4.5).
 #include <algorithm>
 
 #include "kvx_rows.h"

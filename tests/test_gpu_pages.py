@@ -592,8 +592,8 @@ def test_attend_chosen_behind_the_last_row():
 
 
 def test_attend_chosen_by_many_sequences():
-    """More sequences than a wave looks at at once, without new tokens where it looks again, in a call whose bound of new
-    tokens is the binding's default, all of them.  All pages, in order, are attention over everything."""
+    """More sequences than a wave looks at at once, without new tokens where it looks again, in a call whose bound of
+    new tokens is the binding's default, all of them.  All pages, in order, are attention over everything."""
     gen = np.random.default_rng(5)
     new = [int(x) for x in gen.choice([0, 1, 1, 3], 2000)]
     for at in (0, 63, 64, 127, 128, 129, 1999):

@@ -157,13 +157,13 @@ def test_chosen_pages_of_many_sequences(fp8):
 
     def call(tokens, max_queries, q=q, cache=cache, seqs=2048):
         batch = _batch(attend, num_seqs=seqs, num_queries=tokens, max_queries=max_queries, starts=SOME)
-        pages = attend.KvPageList(pages=SOME, counts=SOME, token_stride=32, head_stride=4, heads=cache.layout.num_kv_heads,
-                                  budget=4)
+        pages = attend.KvPageList(pages=SOME, counts=SOME, token_stride=32, head_stride=4, budget=4,
+                                  heads=cache.layout.num_kv_heads)
         args = (ctypes.byref(o), ctypes.byref(by) if by else None, ctypes.byref(pages), ctypes.byref(q))
         need = kvx._lib.kv_attend_pages_workspace(ctypes.byref(cache), ctypes.byref(batch), *args)
         # (A workspace that is too small: what is not refused before comes to that.)
-        got = kvx._lib.kv_attend_pages(ctypes.byref(cache), 0, ctypes.byref(batch), *args, ctypes.byref(q), SOME, SOME, 0,
-                                       None)
+        got = kvx._lib.kv_attend_pages(ctypes.byref(cache), 0, ctypes.byref(batch), *args, ctypes.byref(q), SOME, SOME,
+                                       0, None)
         assert got == (kvx.KV_EINVAL if need > 0 else need)
         return need
 
@@ -171,7 +171,8 @@ def test_chosen_pages_of_many_sequences(fp8):
     assert call(1 << 20, 1 << 20) == call(1 << 20, 512) > 0
     assert call((1 << 20) + 1, 4) == kvx.KV_EUNSUPPORTED
     # Rows beyond 32 bits in a sequence, which only tiles of a sequence's rows would have to count.
-    one, wide = _cache(kvx, kvx.make_layout(1, 1, 64, 1 if fp8 else 2, 16, 16)), _rows(attend, 16383, token_stride=1 << 20)
+    one = _cache(kvx, kvx.make_layout(1, 1, 64, 1 if fp8 else 2, 16, 16))
+    wide = _rows(attend, 16383, token_stride=1 << 20)
     by = _scales(attend, 1) if fp8 else None
     assert call(1 << 18, 1 << 18, wide, one, 1) > 0
 
